@@ -19,6 +19,7 @@
 #ifndef PXR_H
 #define PXR_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -277,6 +278,106 @@ int pxr_pipeline_step(pxr_pipeline* p, const float* d_poses, const float* d_shap
 int pxr_pipeline_set_overlap_from(pxr_pipeline* p, uint64_t bytes);
 /* Into how many chunks a step of B environments is cut (host only; no passage of the paper).  Errors: INVALID_ARG. */
 int pxr_pipeline_info(const pxr_pipeline* p, uint32_t B, uint32_t* chunks);
+
+/* ---- a policy's memory: layer norm and linear attention ----
+ * The paper's loop (section 2) ends with the first layer of a policy.  What stands behind that layer in a policy that
+ * remembers: a normalisation, and a state per environment that each step reads and adds to.  Element types are fp32 and
+ * bfloat16; statistics, sums and states are fp32.  All calls only enqueue: no allocation, no synchronisation. */
+enum { PXR_F32 = 0, PXR_BF16 = 1 };
+
+/* Layer norm over rows of `width` values:
+ *   mean = sum x / width,  rstd = 1 / sqrt(sum (x - mean)^2 / width + eps),  y = (x - mean) * rstd * weight + bias
+ * Strides are in elements between the starts of rows; values inside a row are adjacent.  weight and bias are of param_dtype,
+ * which is PXR_F32 or dtype. */
+typedef struct {
+    uint32_t dtype, param_dtype;
+    uint64_t n_rows;
+    uint32_t width;
+    float eps;
+    int64_t x_stride; /* rows of x */
+    int64_t y_stride; /* rows of y (forward) or of dy (backward) */
+    int64_t dx_stride; /* rows of dx (backward) */
+} pxr_layer_norm_desc;
+
+/* d_weight, d_bias [width] or NULL (1 and 0); d_mean, d_rstd [n_rows] fp32, written, or NULL where no backward pass
+ * follows.  y may be x itself with the same stride.  n_rows == 0 is a call that does nothing.  Values are not validated: a
+ * row with a NaN or an infinity comes out as NaN, the other rows are not touched by it.
+ * Errors: INVALID_ARG (null, width == 0 or above 2^30, a type that is none, eps negative or not finite, a row stride
+ * smaller than the width, a buffer that is not aligned to its elements, n_rows above 2^31-1); DEVICE. */
+int pxr_layer_norm_forward(const pxr_layer_norm_desc* d, const void* d_x, const void* d_weight, const void* d_bias,
+                           void* d_y, float* d_mean, float* d_rstd, void* hip_stream);
+
+/* Bytes of workspace that pxr_layer_norm_backward needs for this description (host only; may be 0).  Errors: as above. */
+int pxr_layer_norm_workspace(const pxr_layer_norm_desc* d, size_t* bytes);
+
+/* Gradients, with g = weight * dy and xh = (x - mean) * rstd from the forward pass' mean and rstd:
+ *   dx = rstd * (g - sum g / width - xh * sum(g * xh) / width),  dweight = sum over rows dy * xh,  dbias = sum over rows dy
+ * d_dweight, d_dbias [width] of param_dtype, written (not added to), each NULL if not wanted; zeros for n_rows == 0.  dx may
+ * be dy or x itself with the same stride.  The sums over rows are taken in an order that depends on the sizes alone: equal
+ * inputs give equal bits.  d_workspace: 16-byte aligned, of at least the bytes that pxr_layer_norm_workspace names, used until
+ * the call's kernels end.  Errors: as above, and INVALID_ARG (workspace missing, too small or misaligned). */
+int pxr_layer_norm_backward(const pxr_layer_norm_desc* d, const void* d_dy, const void* d_x, const float* d_mean,
+                            const float* d_rstd, const void* d_weight, void* d_dx, void* d_dweight, void* d_dbias,
+                            void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Linear attention with a decay for each head.  Every environment e and head h has a state S [d_key,d_value]:
+ *   S_t = (resets[e,t] ? 0 : exp(log_decay[h]) * S_{t-1}) + k_t v_t^T        o_t = scale * S_t^T q_t
+ * resets[e,t] != 0 says that step t begins an episode: nothing from before it reaches it, whatever the state held.  The
+ * decays are constants of the layer, copied at creation; no gradient is formed for them. */
+typedef struct pxr_linear_attention pxr_linear_attention; /* opaque, owned by the library */
+typedef struct {
+    uint32_t n_heads, d_key, d_value;
+    float scale;
+    const float* log_decay; /* host [n_heads], natural logarithm of the decay per step: finite, <= 0 */
+} pxr_linear_attention_desc;
+
+/* Host only; one small allocation and upload.  Errors: INVALID_ARG (null, n_heads == 0 or above 65535, a size that is 0, a
+ * scale that is not finite, a log_decay that is positive or not finite); UNSUPPORTED (d_key or d_value above 256); OOM; DEVICE. */
+int pxr_linear_attention_create(const pxr_linear_attention_desc* desc, pxr_linear_attention** out);
+/* Free a layer; NULL accepted; synchronise streams still using it first. */
+int pxr_linear_attention_destroy(pxr_linear_attention* a);
+
+/* A view [environments, steps, heads, d] of a device buffer: strides in elements, the d values of a head adjacent.  Inputs
+ * may have any strides (0 where heads or environments share); views that are written must not overlap themselves. */
+typedef struct {
+    void* data;
+    int64_t env, step, head;
+} pxr_tokens;
+
+/* What the layer reads.  d_state [n_envs,n_heads,d_key,d_value] fp32 before the first step, or NULL = zeros. */
+typedef struct {
+    uint32_t dtype;            /* of q, k, v and of everything that is [.., d]: PXR_F32 or PXR_BF16 */
+    uint32_t n_envs, n_steps;
+    pxr_tokens q, k, v;
+    const uint8_t* d_resets;   /* [n_envs,n_steps] bytes, or NULL = none */
+    int64_t resets_env, resets_step; /* its strides */
+    const float* d_state;
+} pxr_rollout;
+
+/* Bytes of workspace that the forward (backward == 0) or backward pass needs (host only; may be 0).
+ * Errors: INVALID_ARG (null, n_envs == 0). */
+int pxr_linear_attention_workspace(const pxr_linear_attention* a, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, uint32_t backward,
+                                   size_t* bytes);
+
+/* All steps of a rollout at once: out [n_envs,n_steps,n_heads,d_value] of the rollout's type, and the state after the last step
+ * in d_state_out [n_envs,n_heads,d_key,d_value] (NULL if not wanted; not the buffer of d_state).  n_steps == 0 passes the
+ * state on.  An infinity or NaN in a step's k or v reaches that step and the later ones of the same episode and no others.
+ * Errors: INVALID_ARG (null, n_envs == 0, n_envs * n_heads above 2^31-1, a type that is none, a buffer not aligned to its elements, states that
+ * overlap, workspace missing, too small or not 16-byte aligned); DEVICE. */
+int pxr_linear_attention_forward(pxr_linear_attention* a, const pxr_rollout* r, const pxr_tokens* out, float* d_state_out,
+                                 void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradients for the outputs' gradients dout (strides as given) and d_dstate_out (of the state after the last step; NULL = zeros):
+ * dq, dk [n_envs,n_steps,n_heads,d_key], dv [.., d_value] of the rollout's type and, unless NULL, d_dstate
+ * [n_envs,n_heads,d_key,d_value] fp32, of the state before the first step.  Probabilities and states are computed again, nothing
+ * is kept from the forward pass.  Equal inputs give equal bits.  Errors: as for the forward pass. */
+int pxr_linear_attention_backward(pxr_linear_attention* a, const pxr_rollout* r, const pxr_tokens* dout,
+                                  const float* d_dstate_out, const pxr_tokens* dq, const pxr_tokens* dk, const pxr_tokens* dv,
+                                  float* d_dstate, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One step of every environment: r->n_steps must be 1 (the step strides do not matter), d_state [n_envs,n_heads,d_key,d_value]
+ * is updated in place (r->d_state is not read; 4-byte aligned).  One kernel.  Errors: as for the forward pass. */
+int pxr_linear_attention_step(pxr_linear_attention* a, const pxr_rollout* r, float* d_state, const pxr_tokens* out, void* hip_stream);
 
 /* Scene facts for callers and tests (sizes of what pxr_create_scene built; no passage of the paper): total
  * template vertices and triangles, dynamic LDS bytes per frame workgroup, threads per workgroup.  Any out

@@ -220,6 +220,37 @@ int prepare_fk_kernel(std::string& err);
 int launch_fk(const SkeletonConsts& sk, const float* d_free_poses, const float* d_angles, uint32_t n_frames,
               float* d_poses, void* stream, std::string& err);
 
+// layer_norm.hip (arguments as checked by memory_api.cpp)
+size_t layer_norm_workspace(const pxr_layer_norm_desc& d);
+int launch_layer_norm_forward(const pxr_layer_norm_desc& d, const void* x, const void* w, const void* b, void* y, float* mean, float* rstd,
+                              void* stream, std::string& err);
+int launch_layer_norm_backward(const pxr_layer_norm_desc& d, const void* dy, const void* x, const float* mean, const float* rstd,
+                               const void* w, void* dx, void* dw, void* db, void* ws, void* stream, std::string& err);
+
+// A head's decay g = exp(log_decay).  A state decays once for every step that passes, and a rounding of g that is always the
+// same would add up over a long look-back (4096 steps: 2^-12 of a state), so g is held as a sum of two floats.
+struct LinearAttentionHead {
+    double log_decay;
+    float decay, decay_rest;
+};
+void fill_head(LinearAttentionHead& h, float log_decay);
+
+struct LinearAttentionConsts {
+    uint32_t n_heads, dk, dv, n_cus;
+    float scale;
+    const LinearAttentionHead* heads;  // [n_heads] on the device
+};
+
+// linear_attention.hip (arguments as checked by memory_api.cpp)
+size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, bool backward);
+int launch_linear_attention_forward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& out, float* state_out, void* ws,
+                                    void* stream, std::string& err);
+int launch_linear_attention_backward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& dout, const float* dstate_out,
+                                     const pxr_tokens& dq, const pxr_tokens& dk, const pxr_tokens& dv, float* dstate, void* ws,
+                                     void* stream, std::string& err);
+int launch_linear_attention_step(const LinearAttentionConsts& c, const pxr_rollout& r, float* state, const pxr_tokens& out, void* stream,
+                                 std::string& err);
+
 // pipeline.cpp works through these (api.cpp / conv_api.cpp own the handles' layouts).
 constexpr uint32_t kMaxPipelineChunks = 16;
 void scene_shape(const pxr_scene* s, uint32_t* K, uint32_t* H, uint32_t* W);

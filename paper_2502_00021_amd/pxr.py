@@ -2,7 +2,8 @@
 
 Mirrors include/pxr.h one to one: create_scene / destroy_scene /
 apply_distractor / render_batch, set_skeleton / pose_batch /
-render_batch_kinematic (+ scene_info, set_block_threads, host_tables).  PyTorch is used only to hold device memory and name the stream.
+render_batch_kinematic (+ scene_info, set_block_threads, host_tables), the policy's first layer (Conv) and its memory
+(layer_norm, layer_norm_backward, LinearAttention).  PyTorch is used only to hold device memory and name the stream.
 There is no fallback: a missing library or a failing call raises.
 """
 import ctypes as C
@@ -63,6 +64,26 @@ class ConvDesc(C.Structure):
                 ("weights", C.c_void_p), ("bias", C.c_void_p), ("relu", C.c_uint32)]
 
 
+class LayerNormDesc(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("param_dtype", C.c_uint32), ("n_rows", C.c_uint64), ("width", C.c_uint32),
+                ("eps", C.c_float), ("x_stride", C.c_int64), ("y_stride", C.c_int64), ("dx_stride", C.c_int64)]
+
+
+class LinearAttentionDesc(C.Structure):
+    _fields_ = [("n_heads", C.c_uint32), ("d_key", C.c_uint32), ("d_value", C.c_uint32), ("scale", C.c_float),
+                ("log_decay", C.c_void_p)]
+
+
+class Tokens(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("env", C.c_int64), ("step", C.c_int64), ("head", C.c_int64)]
+
+
+class Rollout(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("n_envs", C.c_uint32), ("n_steps", C.c_uint32),
+                ("q", Tokens), ("k", Tokens), ("v", Tokens),
+                ("d_resets", C.c_void_p), ("resets_env", C.c_int64), ("resets_step", C.c_int64), ("d_state", C.c_void_p)]
+
+
 _lib = None
 _lib_path = LIB_PATH
 
@@ -119,6 +140,21 @@ def lib():
         for name in ("pxr_pipeline_create", "pxr_pipeline_destroy", "pxr_pipeline_step", "pxr_pipeline_set_overlap_from",
                      "pxr_pipeline_info"):
             getattr(L, name).restype = C.c_int
+        size = C.POINTER(C.c_size_t)
+        tokens, rollout, norm = C.POINTER(Tokens), C.POINTER(Rollout), C.POINTER(LayerNormDesc)
+        L.pxr_layer_norm_forward.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp]
+        L.pxr_layer_norm_workspace.argtypes = [norm, size]
+        L.pxr_layer_norm_backward.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.pxr_linear_attention_create.argtypes = [C.POINTER(LinearAttentionDesc), C.POINTER(vp)]
+        L.pxr_linear_attention_destroy.argtypes = [vp]
+        L.pxr_linear_attention_workspace.argtypes = [vp, u32, u32, u32, u32, size]
+        L.pxr_linear_attention_forward.argtypes = [vp, rollout, tokens, vp, vp, C.c_size_t, vp]
+        L.pxr_linear_attention_backward.argtypes = [vp, rollout, tokens, vp, tokens, tokens, tokens, vp, vp, C.c_size_t, vp]
+        L.pxr_linear_attention_step.argtypes = [vp, rollout, vp, tokens, vp]
+        for name in ("layer_norm_forward", "layer_norm_workspace", "layer_norm_backward", "linear_attention_create",
+                     "linear_attention_destroy", "linear_attention_workspace", "linear_attention_forward",
+                     "linear_attention_backward", "linear_attention_step"):
+            getattr(L, "pxr_" + name).restype = C.c_int
         L.pxr_selftest_arithmetic.argtypes = [vp]
         L.pxr_selftest_arithmetic.restype = C.c_int
         L.pxr_measure_peaks.argtypes = [vp, vp, vp, vp, vp]
@@ -507,6 +543,186 @@ class Pipeline:
         _check(_lib.pxr_pipeline_step(self._h, poses.data_ptr(), None if shapes is None else shapes.data_ptr(), B,
                                       int(step0), int(env0), frames.data_ptr(), features.data_ptr(), stream))
         return frames, features
+
+
+def _dtype_code(torch, dtype):
+    if dtype == torch.float32:
+        return 0
+    assert dtype == torch.bfloat16, f"float32 or bfloat16, not {dtype}"
+    return 1
+
+
+def _empty(torch, like, stream, shape, dtype):
+    """Device memory for a call's outputs and workspace.  On a stream of the caller's it comes from that stream's pool: the
+    allocator may hand it out again as soon as it is let go, which is in order on that stream and on no other."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=like.device)):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _rows(x):
+    """[..., D] as [N, D] without a copy, and the stride between rows (raises if there is no single one)."""
+    assert x.is_cuda and x.dim() >= 1 and x.shape[-1] > 0, "a CUDA tensor [..., width]"
+    r = x if x.dim() == 2 else x.view(-1, x.shape[-1])
+    n, width = r.shape
+    assert width == 1 or r.stride(1) == 1 or n == 0, "the values of a row must be adjacent"
+    return r, n, width, (r.stride(0) if n > 1 else width)
+
+
+def _params(torch, x, width, *params):
+    """dtype code of the weight and bias (those that there are), checked."""
+    dtype = None
+    for p in params:
+        if p is not None:
+            assert p.is_cuda and p.is_contiguous() and p.shape == (width,), tuple(p.shape)
+            assert p.dtype in (torch.float32, x.dtype) and dtype in (None, p.dtype), "weight and bias: both float32 or both of x's type"
+            dtype = p.dtype
+    return torch.float32 if dtype is None else dtype
+
+
+def _ptr(x):
+    return None if x is None else x.data_ptr()
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
+    """x: CUDA float32 or bfloat16 [..., D] (rows a constant stride apart, their values adjacent); weight, bias: [D], float32
+    or of x's type, or None.  Returns (y like x, mean, rstd: float32, x's leading shape), the latter two for
+    layer_norm_backward; enqueue only."""
+    torch = _torch or _torch_module()
+    r, n, width, x_stride = _rows(x)
+    params = _params(torch, x, width, weight, bias)
+    y = _empty(torch, x, stream, x.shape, x.dtype) if out is None else out
+    assert y.is_cuda and y.dtype == x.dtype and y.shape == x.shape
+    y_stride = _rows(y)[3]
+    stats = _empty(torch, x, stream, (2,) + tuple(x.shape[:-1]), torch.float32)
+    mean, rstd = stats[0], stats[1]
+    d = LayerNormDesc(_dtype_code(torch, x.dtype), _dtype_code(torch, params), n, width, eps, x_stride, y_stride, width)
+    _check((_lib or lib()).pxr_layer_norm_forward(C.byref(d), r.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean.data_ptr(),
+                                                  rstd.data_ptr(), _stream_handle(stream, x)))
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, params_dtype=None, stream=None):
+    """Gradients of layer_norm for dy (x's shape and type), with the mean and rstd that it returned.  Returns (dx, dweight,
+    dbias), the latter two [D] of the weight's type (without a weight: params_dtype, float32 unless given); enqueue only."""
+    torch = _torch or _torch_module()
+    r, n, width, x_stride = _rows(x)
+    assert dy.dtype == x.dtype and dy.shape == x.shape
+    g, _, _, dy_stride = _rows(dy)
+    for s in (mean, rstd):
+        assert s.is_cuda and s.dtype == torch.float32 and s.is_contiguous() and s.numel() == n, "mean and rstd: one float32 for each row"
+    params = _params(torch, x, width, weight) if weight is not None else params_dtype or torch.float32
+    assert params in (torch.float32, x.dtype)
+    dx = _empty(torch, x, stream, x.shape, x.dtype) if dx is None else dx
+    assert dx.is_cuda and dx.dtype == x.dtype and dx.shape == x.shape
+    dparams = _empty(torch, x, stream, (2, width), params)
+    d = LayerNormDesc(_dtype_code(torch, x.dtype), _dtype_code(torch, params), n, width, 0.0, x_stride, dy_stride, _rows(dx)[3])
+    L = _lib or lib()
+    need = C.c_size_t()
+    _check(L.pxr_layer_norm_workspace(C.byref(d), C.byref(need)))
+    ws = _empty(torch, x, stream, (need.value,), torch.uint8) if need.value else None
+    _check(L.pxr_layer_norm_backward(C.byref(d), g.data_ptr(), r.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dx.data_ptr(),
+                                     dparams[0].data_ptr(), dparams[1].data_ptr(), _ptr(ws), need.value, _stream_handle(stream, x)))
+    return dx, dparams[0], dparams[1]
+
+
+class LinearAttention:
+    """Owns one pxr_linear_attention handle: a state [d_key, d_value] per environment and head that decays by
+    exp(log_decay[h]) with every step, takes in k v^T and answers scale S^T q; cut where an episode begins."""
+
+    def __init__(self, n_heads, d_key, d_value, log_decay, scale=None):
+        """log_decay: n_heads natural logarithms, <= 0 (constants: no gradient); scale: d_key ** -0.5 unless given."""
+        ld = np.ascontiguousarray(log_decay, dtype=np.float32)
+        assert ld.shape == (n_heads,), ld.shape
+        d = LinearAttentionDesc(int(n_heads), int(d_key), int(d_value), float(d_key ** -0.5 if scale is None else scale), ld.ctypes.data)
+        h = C.c_void_p()
+        _check(lib().pxr_linear_attention_create(C.byref(d), C.byref(h)))
+        self._h = h
+        self.H, self.dk, self.dv, self.scale = int(n_heads), int(d_key), int(d_value), d.scale
+
+    def close(self):
+        if getattr(self, "_h", None):
+            _check(lib().pxr_linear_attention_destroy(self._h))
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _view(self, x, lead, d, like):
+        """A [B, T, H, d] or (acting) [B, H, d] tensor as pxr_tokens."""
+        assert x.is_cuda and x.dtype == like.dtype and x.shape == (*lead, self.H, d), (tuple(x.shape), (*lead, self.H, d))
+        s = x.stride()
+        assert d == 1 or s[-1] == 1 or x.numel() == 0, "a head's values must be adjacent"
+        return Tokens(x.data_ptr(), s[0], s[1] if len(s) == 4 else 0, s[-2])
+
+    def _state(self, torch, state, B):
+        assert state.is_cuda and state.dtype == torch.float32 and state.is_contiguous()
+        assert state.shape == (B, self.H, self.dk, self.dv), tuple(state.shape)
+        return state.data_ptr()
+
+    def _rollout(self, torch, q, k, v, resets, state):
+        lead = tuple(q.shape[:-2])
+        assert q.is_cuda and len(lead) in (1, 2), "queries [B, T, H, d_key], of one step [B, H, d_key]"
+        r = Rollout()
+        r.dtype, r.n_envs, r.n_steps = _dtype_code(torch, q.dtype), lead[0], lead[1] if len(lead) == 2 else 1
+        r.q, r.k, r.v = self._view(q, lead, self.dk, q), self._view(k, lead, self.dk, q), self._view(v, lead, self.dv, q)
+        if resets is not None:
+            assert resets.is_cuda and resets.dtype in (torch.bool, torch.uint8) and resets.shape == lead, tuple(resets.shape)
+            r.d_resets, r.resets_env, r.resets_step = resets.data_ptr(), resets.stride(0), resets.stride(1) if len(lead) == 2 else 0
+        if state is not None:
+            r.d_state = self._state(torch, state, lead[0])
+        return r, lead
+
+    def _workspace(self, torch, r, backward, like, stream):
+        need = C.c_size_t()
+        _check(_lib.pxr_linear_attention_workspace(self._h, r.dtype, r.n_envs, r.n_steps, backward, C.byref(need)))
+        return _empty(torch, like, stream, (need.value,), torch.uint8) if need.value else None, need.value
+
+    def forward(self, q, k, v, resets=None, state=None, out=None, state_out=None, stream=None):
+        """q, k: CUDA float32 or bfloat16 [B,T,H,d_key], v: [B,T,H,d_value] (any strides, a head's values adjacent); resets:
+        bool or uint8 [B,T], true where a step begins an episode, or None; state: float32 [B,H,d_key,d_value] before the
+        first step, or None = zeros.  Returns (out [B,T,H,d_value], the state after the last step); enqueue only."""
+        torch = _torch or _torch_module()
+        assert q.dim() == 4
+        r, lead = self._rollout(torch, q, k, v, resets, state)
+        out = _empty(torch, q, stream, (*lead, self.H, self.dv), q.dtype) if out is None else out
+        state_out = _empty(torch, q, stream, (lead[0], self.H, self.dk, self.dv), torch.float32) if state_out is None else state_out
+        ws, need = self._workspace(torch, r, 0, q, stream)
+        _check(_lib.pxr_linear_attention_forward(self._h, C.byref(r), C.byref(self._view(out, lead, self.dv, q)),
+                                                 self._state(torch, state_out, lead[0]), _ptr(ws), need, _stream_handle(stream, q)))
+        return out, state_out
+
+    def backward(self, dout, q, k, v, resets=None, state=None, dstate=None, stream=None):
+        """Gradients for dout [B,T,H,d_value] and dstate [B,H,d_key,d_value] (of the state after the last step, or None = zeros)
+        of a forward call with these inputs.  Returns (dq, dk, dv, the gradient of the state before the first step or, where
+        there was none, None); enqueue only."""
+        torch = _torch or _torch_module()
+        assert q.dim() == 4
+        r, lead = self._rollout(torch, q, k, v, resets, state)
+        dq, dk = (_empty(torch, q, stream, (*lead, self.H, self.dk), q.dtype) for _ in range(2))
+        dv = _empty(torch, q, stream, (*lead, self.H, self.dv), q.dtype)
+        dfirst = None if state is None else _empty(torch, q, stream, state.shape, torch.float32)
+        ws, need = self._workspace(torch, r, 1, q, stream)
+        _check(_lib.pxr_linear_attention_backward(
+            self._h, C.byref(r), C.byref(self._view(dout, lead, self.dv, q)), None if dstate is None else self._state(torch, dstate, lead[0]),
+            C.byref(self._view(dq, lead, self.dk, q)), C.byref(self._view(dk, lead, self.dk, q)), C.byref(self._view(dv, lead, self.dv, q)),
+            _ptr(dfirst), _ptr(ws), need, _stream_handle(stream, q)))
+        return dq, dk, dv, dfirst
+
+    def step(self, q, k, v, state, resets=None, out=None, stream=None):
+        """One step of every environment: q, k [B,H,d_key], v [B,H,d_value], resets [B] or None; state float32
+        [B,H,d_key,d_value] is updated in place.  Returns out [B,H,d_value]; enqueue only."""
+        torch = _torch or _torch_module()
+        assert q.dim() == 3
+        r, lead = self._rollout(torch, q, k, v, resets, None)
+        out = _empty(torch, q, stream, (*lead, self.H, self.dv), q.dtype) if out is None else out
+        _check(_lib.pxr_linear_attention_step(self._h, C.byref(r), self._state(torch, state, lead[0]),
+                                              C.byref(self._view(out, lead, self.dv, q)), _stream_handle(stream, q)))
+        return out
 
 
 def make_skeleton_desc(skel, n_free, n_angles):
