@@ -3,7 +3,19 @@
 //   mean = sum x / D,  rstd = 1 / sqrt(sum (x - mean)^2 / D + eps),  y = (x - mean) rstd w + b
 //   dx = rstd (g - sum g / D - xh sum(g xh) / D),  g = w dy,  xh = (x - mean) rstd;  dw = sum_rows dy xh,  db = sum_rows dy
 //
-// All sums are fp32; the deviations are squared after the mean is taken off, so a row far from zero keeps its variance.
+// Both directions are bound by HBM: a few operations for every byte.  So a row is read once and stays in registers, as it came,
+// until it leaves: the deviations are squared after the mean is taken off (a row far from zero keeps its variance), from the
+// registers.  All sums are fp32.
+//
+// A lane holds VPL vectors of 16 bytes of a row, lanes of a row next to each other.  Who takes a row goes by the number of its
+// vectors:
+//   up to 64      a part of a wavefront, 1 to 64 lanes: eight rows of 64 bfloat16 values in a wavefront
+//   up to 256     a wavefront, two or four vectors a lane
+//   up to 8192    a workgroup of 512 or 1024 threads
+//   more          a workgroup that reads the row again for each sum (from the caches, mostly)
+// Workgroups are persistent and walk the rows, so that weights and biases are read once by a wavefront, or once for four rows by a workgroup:
+// in 32 bits they are twice the bytes of a bfloat16 row, each.  The sums over rows of the backward pass stay in registers as well, and
+// leave once for each workgroup; a second kernel adds the workgroups' sums in their order, so that equal inputs give equal bits.
 
 #include <hip/hip_runtime.h>
 
@@ -12,103 +24,621 @@
 namespace pxr {
 namespace {
 
-constexpr uint32_t kThreads = 256;
-
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __bf16* p) { return (float)*p; }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__bf16* p, float v) { *p = (__bf16)v; }  // round to nearest even
 
-// Sum over the workgroup, the same bits in every lane.
-__device__ __forceinline__ float group_sum(float v, float* lds) {
-    for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m);
-    __syncthreads();
-    if ((threadIdx.x & 63u) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+// 16 bytes of a row: 4 or 8 values, as they came.  Rows may begin at any element: the memory takes 16-byte requests at any address.
+template <class T>
+struct Vec {
+    static constexpr int N = 16 / sizeof(T);
+    uint32_t w[4];
+
+    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(w, p, 16); }
+    // The first `count` of them alone (rows narrower than a vector).
+    __device__ __forceinline__ void load_some(const T* p, int count) {
+        T v[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = e < count ? p[e] : (T)0.0f;
+        __builtin_memcpy(w, v, 16);
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+    }
+    // Zero in place of the values that are not in [from, to).
+    __device__ __forceinline__ void keep(int from, int to) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < from || e >= to) {
+                if constexpr (sizeof(T) == 4)
+                    w[e] = 0u;
+                else
+                    w[e >> 1] &= (e & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+            }
+    }
+    // What follows takes the values from these registers again instead of keeping them all as floats in others.
+    __device__ __forceinline__ void as_they_came() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));
+    }
+    static __device__ __forceinline__ void store(T* p, const float (&f)[N], int from, int to) {
+        T v[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (T)f[e];  // round to nearest even
+        if (from == 0 && to >= N) {
+            __builtin_memcpy(p, v, 16);
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e >= from && e < to) p[e] = v[e];
+    }
+};
+
+// Where a lane's vector lies in the row and which of its values [from, to) are the lane's own.  A row that ends inside a vector has its last
+// vector moved back to its end, so that it is one request like the others (the values it shares with the vector before it
+// are that one's); lanes past the end have the last vector as well, and none of it is theirs.  kTiny: rows narrower than a vector.
+template <int N, bool kTiny>
+struct Place {
+    uint32_t at;
+    int from, to;
+    __device__ __forceinline__ Place(uint32_t vector, uint32_t D) {
+        const uint32_t want = vector * N;
+        if (kTiny) {
+            at = 0;
+            from = 0;
+            to = vector == 0 ? (int)D : 0;
+        } else {
+            at = min(want, D - N);
+            from = (int)min(want - at, (uint32_t)N);
+            to = N;
+        }
+    }
+    __device__ __forceinline__ bool whole() const { return kTiny ? to == N : from == 0; }
+    __device__ __forceinline__ bool any() const { return from < to; }
+    __device__ __forceinline__ bool own(int e) const { return kTiny ? e < to : e >= from; }
+};
+
+// The parameters of a vector, `def` where there is no array.
+template <class P, int N, bool kTiny>
+__device__ __forceinline__ void load_params(const P* p, float def, const Place<N, kTiny>& at, float (&f)[N]) {
+    if (!p) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = def;
+    } else if (kTiny) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = at.own(e) ? load1(p + e) : def;
+    } else {
+        P v[N];
+        __builtin_memcpy(v, p + at.at, sizeof(v));
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = (float)v[e];
+    }
 }
 
+// Sums of U values over a row's lanes, the same bits in each of them.  NT == 0: `lanes` (a power of two) next to each other in a
+// wavefront; otherwise the NT threads of the workgroup, through `lds` [U][NT / 64], with one barrier (the caller does not write these words
+// again before another barrier).
+template <int NT, int U>
+__device__ __forceinline__ void row_sums(float (&v)[U], uint32_t lanes, float* lds) {
+    if constexpr (NT == 0) {
+        for (uint32_t m = lanes >> 1; m >= 1; m >>= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] += __shfl_xor(v[u], m);
+    } else {
+        constexpr uint32_t W = NT / 64;
+#pragma unroll
+        for (uint32_t m = 32; m >= 1; m >>= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] += __shfl_xor(v[u], m);
+        if ((threadIdx.x & 63u) == 0)
+#pragma unroll
+            for (int u = 0; u < U; ++u) lds[u * W + (threadIdx.x >> 6)] = v[u];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = lds[u * W + (threadIdx.x & (W - 1u))];
+#pragma unroll
+        for (uint32_t m = W >> 1; m >= 1; m >>= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] += __shfl_xor(v[u], m);
+    }
+}
+
+constexpr uint32_t kSubThreads = 512;  // of a workgroup whose rows take a wavefront or less each
+constexpr uint32_t kThreadsOf(int nt) { return nt ? (uint32_t)nt : kSubThreads; }
+
+struct NormForward {
+    const void *x, *weight, *bias;
+    void* y;
+    float *mean, *rstd;
+    int64_t x_stride, y_stride;
+    uint32_t n, D, lanes;
+    float eps;
+};
+
+// U rows at a time: their requests are in flight together, and they share one read of weight and bias.
+template <class T, class P, int NT, int VPL, int U, bool kTiny = false>
+__global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const NormForward a) {
+    constexpr int N = Vec<T>::N;
+    constexpr bool kKeep = NT == 0;  // parameters stay in registers
+    typedef Place<N, kTiny> At;
+    __shared__ float lds[2 * U * 16];
+    const uint32_t lanes = NT ? NT : a.lanes, l = threadIdx.x & (lanes - 1u), group = threadIdx.x / lanes, groups = kThreadsOf(NT) / lanes;
+    const P *weight = static_cast<const P*>(a.weight), *bias = static_cast<const P*>(a.bias);
+    float w[kKeep ? VPL : 1][N], b[kKeep ? VPL : 1][N];
+    if (kKeep)
+#pragma unroll
+        for (int p = 0; p < VPL; ++p) {
+            load_params(weight, 1.0f, At(l + p * lanes, a.D), w[kKeep ? p : 0]);
+            load_params(bias, 0.0f, At(l + p * lanes, a.D), b[kKeep ? p : 0]);
+        }
+    const float width = (float)a.D;  // (divided by: a product with 1 / D would move the mean of equal values)
+    for (uint64_t row0 = ((uint64_t)blockIdx.x * groups + group) * U; row0 < a.n; row0 += (uint64_t)gridDim.x * groups * U) {
+        Vec<T> x[U][VPL];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const T* xr = static_cast<const T*>(a.x) + (int64_t)min(row0 + u, (uint64_t)a.n - 1u) * a.x_stride;
+#pragma unroll
+            for (int p = 0; p < VPL; ++p) {
+                const At at(l + p * lanes, a.D);
+                if (kTiny)
+                    x[u][p].load_some(xr, at.to);
+                else
+                    x[u][p].load(xr + at.at);
+            }
+        }
+        float mean[U], rstd[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            mean[u] = 0.0f;
+#pragma unroll
+            for (int p = 0; p < VPL; ++p) {
+                const At at(l + p * lanes, a.D);
+                float s = 0.0f;
+#pragma unroll
+                for (int e = 0; e < N; ++e) s += x[u][p].get(e);
+                if (!at.whole()) {
+                    s = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) s += at.own(e) ? x[u][p].get(e) : 0.0f;
+                }
+                mean[u] += s;
+                x[u][p].as_they_came();
+            }
+        }
+        row_sums<NT, U>(mean, lanes, lds);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            mean[u] /= width;
+            rstd[u] = 0.0f;
+#pragma unroll
+            for (int p = 0; p < VPL; ++p) {
+                const At at(l + p * lanes, a.D);
+                float s = 0.0f;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float c = x[u][p].get(e) - mean[u];
+                    s = __builtin_fmaf(c, c, s);
+                }
+                if (!at.whole()) {
+                    s = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float c = at.own(e) ? x[u][p].get(e) - mean[u] : 0.0f;
+                        s = __builtin_fmaf(c, c, s);
+                    }
+                }
+                rstd[u] += s;
+                x[u][p].as_they_came();
+            }
+        }
+        row_sums<NT, U>(rstd, lanes, lds + U * 16);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            rstd[u] = 1.0f / sqrtf(rstd[u] / width + a.eps);
+            if (l == 0 && row0 + u < a.n) {
+                if (a.mean) a.mean[row0 + u] = mean[u];
+                if (a.rstd) a.rstd[row0 + u] = rstd[u];
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < VPL; ++p) {
+            const At at(l + p * lanes, a.D);
+            if (!kKeep) {
+                load_params(weight, 1.0f, at, w[0]);
+                load_params(bias, 0.0f, at, b[0]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (row0 + u >= a.n || !at.any()) continue;
+                float y[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) y[e] = __builtin_fmaf((x[u][p].get(e) - mean[u]) * rstd[u], w[kKeep ? p : 0][e], b[kKeep ? p : 0][e]);
+                Vec<T>::store(static_cast<T*>(a.y) + ((int64_t)(row0 + u) * a.y_stride + at.at), y, at.from, at.to);
+            }
+        }
+    }
+}
+
+// Rows of any width, read again for each sum.
 template <class T, class P>
-__global__ __launch_bounds__(kThreads) void norm_forward_kernel(const T* x, const P* weight, const P* bias, T* y, float* mean_out,
-                                                                float* rstd_out, uint32_t D, int64_t x_stride, int64_t y_stride, float eps) {
-    __shared__ float lds[4];
-    const T* xr = x + (int64_t)blockIdx.x * x_stride;
-    T* yr = y + (int64_t)blockIdx.x * y_stride;
-    float s = 0.0f;
-    for (uint32_t i = threadIdx.x; i < D; i += kThreads) s += load1(xr + i);
-    const float mean = group_sum(s, lds) / (float)D;
-    s = 0.0f;
-    for (uint32_t i = threadIdx.x; i < D; i += kThreads) {
-        const float c = load1(xr + i) - mean;
-        s = __builtin_fmaf(c, c, s);
+__global__ __launch_bounds__(1024) void norm_forward_wide_kernel(const NormForward a) {
+    __shared__ float lds[32];
+    const T* xr = static_cast<const T*>(a.x) + (int64_t)blockIdx.x * a.x_stride;
+    T* yr = static_cast<T*>(a.y) + (int64_t)blockIdx.x * a.y_stride;
+    const P *weight = static_cast<const P*>(a.weight), *bias = static_cast<const P*>(a.bias);
+    const float width = (float)a.D;
+    float mean[1] = {0.0f}, rstd[1] = {0.0f};
+    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u) mean[0] += load1(xr + i);
+    row_sums<1024, 1>(mean, 0, lds);
+    mean[0] /= width;
+    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u) {
+        const float c = load1(xr + i) - mean[0];
+        rstd[0] = __builtin_fmaf(c, c, rstd[0]);
     }
-    const float rstd = 1.0f / sqrtf(group_sum(s, lds) / (float)D + eps);
-    for (uint32_t i = threadIdx.x; i < D; i += kThreads) {
-        const float h = (load1(xr + i) - mean) * rstd;
-        store1(yr + i, __builtin_fmaf(h, weight ? load1(weight + i) : 1.0f, bias ? load1(bias + i) : 0.0f));
-    }
+    row_sums<1024, 1>(rstd, 0, lds + 16);
+    rstd[0] = 1.0f / sqrtf(rstd[0] / width + a.eps);
+    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u)
+        store1(yr + i, __builtin_fmaf((load1(xr + i) - mean[0]) * rstd[0], weight ? load1(weight + i) : 1.0f, bias ? load1(bias + i) : 0.0f));
     if (threadIdx.x == 0) {
-        if (mean_out) mean_out[blockIdx.x] = mean;
-        if (rstd_out) rstd_out[blockIdx.x] = rstd;
+        if (a.mean) a.mean[blockIdx.x] = mean[0];
+        if (a.rstd) a.rstd[blockIdx.x] = rstd[0];
     }
 }
 
+struct NormBackward {
+    const void *dy, *x;
+    const float *mean, *rstd;
+    const void* weight;
+    void* dx;
+    float* sums;  // [workgroups][2][D]: dw, db of a workgroup's rows; null = not wanted
+    int64_t dy_stride, x_stride, dx_stride;
+    uint32_t n, D, lanes;
+};
+
+// kSums: the sums over rows are formed here as well.
+template <class T, class P, int NT, int VPL, int U, bool kSums, bool kTiny = false>
+__global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const NormBackward a) {
+    constexpr int N = Vec<T>::N;
+    constexpr bool kKeep = NT == 0 && VPL <= 2;
+    typedef Place<N, kTiny> At;
+    extern __shared__ __align__(16) float lds[];  // 2 x 2 U x 16 floats, or (NT == 0) the sums of a wavefront's lanes
+    const uint32_t lanes = NT ? NT : a.lanes, l = threadIdx.x & (lanes - 1u), group = threadIdx.x / lanes, groups = kThreadsOf(NT) / lanes;
+    const P* weight = static_cast<const P*>(a.weight);
+    float w[kKeep ? VPL : 1][N];
+    if (kKeep)
+#pragma unroll
+        for (int p = 0; p < VPL; ++p) load_params(weight, 1.0f, At(l + p * lanes, a.D), w[kKeep ? p : 0]);
+    float dw[kSums ? VPL : 1][N] = {}, db[kSums ? VPL : 1][N] = {};
+    const float per = 1.0f / (float)a.D;
+    uint32_t turn = 0;
+    for (uint64_t row0 = ((uint64_t)blockIdx.x * groups + group) * U; row0 < a.n; row0 += (uint64_t)gridDim.x * groups * U) {
+        Vec<T> g[U][VPL], x[U][VPL];
+        float mean[U], rstd[U], s[2 * U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint64_t row = min(row0 + u, (uint64_t)a.n - 1u);
+            const T *gr = static_cast<const T*>(a.dy) + (int64_t)row * a.dy_stride, *xr = static_cast<const T*>(a.x) + (int64_t)row * a.x_stride;
+#pragma unroll
+            for (int p = 0; p < VPL; ++p) {
+                const At at(l + p * lanes, a.D);
+                if (kTiny) {
+                    g[u][p].load_some(gr, at.to);
+                    x[u][p].load_some(xr, at.to);
+                } else {
+                    g[u][p].load(gr + at.at);
+                    x[u][p].load(xr + at.at);
+                }
+            }
+            mean[u] = a.mean[row];
+            rstd[u] = a.rstd[row];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) s[2 * u] = s[2 * u + 1] = 0.0f;
+#pragma unroll
+        for (int p = 0; p < VPL; ++p) {
+            const At at(l + p * lanes, a.D);
+            // (one vector's weights and floats after the other: all of them at once do not fit the registers of 1024 threads)
+            if (NT == 1024) __builtin_amdgcn_sched_barrier(0);
+            if (!kKeep) load_params(weight, 1.0f, at, w[0]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                // What is not the lane's own is nothing: its gradient is zero here, and so is what it adds to a sum.  (x beside it is of the same
+                // row: where it is no number, the row's gradient is none either.  A row past the last must not reach the sums over rows.)
+                if (!at.whole()) g[u][p].keep(at.from, at.to);
+                if (row0 + u >= a.n) {
+                    g[u][p].keep(0, 0);
+                    x[u][p].keep(0, 0);
+                    mean[u] = rstd[u] = 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float d = g[u][p].get(e), xh = (x[u][p].get(e) - mean[u]) * rstd[u];
+                    const float wd = d * w[kKeep ? p : 0][e];
+                    s[2 * u] += wd;
+                    s[2 * u + 1] = __builtin_fmaf(wd, xh, s[2 * u + 1]);
+                    if (kSums) {
+                        dw[kSums ? p : 0][e] = __builtin_fmaf(d, xh, dw[kSums ? p : 0][e]);
+                        db[kSums ? p : 0][e] += d;
+                    }
+                }
+                g[u][p].as_they_came();
+                x[u][p].as_they_came();
+            }
+        }
+        row_sums<NT, 2 * U>(s, lanes, lds + (turn & 1u) * (2 * U * 16));
+        ++turn;
+#pragma unroll
+        for (int p = 0; p < VPL; ++p) {
+            const At at(l + p * lanes, a.D);
+            // (one vector's weights and floats after the other: all of them at once do not fit the registers of 1024 threads)
+            if (NT == 1024) __builtin_amdgcn_sched_barrier(0);
+            if (!kKeep) load_params(weight, 1.0f, at, w[0]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (row0 + u >= a.n || !at.any()) continue;
+                float dx[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float xh = (x[u][p].get(e) - mean[u]) * rstd[u];
+                    dx[e] = rstd[u] * __builtin_fmaf(-xh, s[2 * u + 1] * per, __builtin_fmaf(g[u][p].get(e), w[kKeep ? p : 0][e], -s[2 * u] * per));
+                }
+                Vec<T>::store(static_cast<T*>(a.dx) + ((int64_t)(row0 + u) * a.dx_stride + at.at), dx, at.from, at.to);
+            }
+        }
+    }
+    if (!kSums || !a.sums) return;
+    float* out = a.sums + (size_t)blockIdx.x * 2u * a.D;
+    if constexpr (NT == 0) {
+        // the rows' groups of a wavefront, then the wavefronts one after the other
+        for (uint32_t m = lanes; m < 64u; m <<= 1)
+#pragma unroll
+            for (int p = 0; p < VPL; ++p)
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    dw[kSums ? p : 0][e] += __shfl_xor(dw[kSums ? p : 0][e], m);
+                    db[kSums ? p : 0][e] += __shfl_xor(db[kSums ? p : 0][e], m);
+                }
+        const uint32_t span = lanes * VPL * N;
+        for (uint32_t wave = 0; wave < kSubThreads / 64u; ++wave) {
+            __syncthreads();
+            if (threadIdx.x >> 6 == wave && (threadIdx.x & 63u) < lanes)
+#pragma unroll
+                for (int p = 0; p < VPL; ++p)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        float* q = lds + (p * N + e) * lanes + l;
+                        q[0] = (wave ? q[0] : 0.0f) + dw[kSums ? p : 0][e];
+                        q[span] = (wave ? q[span] : 0.0f) + db[kSums ? p : 0][e];
+                    }
+        }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < a.D; i += kSubThreads) {
+            const uint32_t v = i / N, e = i - At(v, a.D).at, at = (v / lanes * N + e) * lanes + (v & (lanes - 1u));
+            out[i] = lds[at];
+            out[a.D + i] = lds[span + at];
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < VPL; ++p) {
+            const At at(l + p * lanes, a.D);
+            if (!at.any()) continue;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (at.own(e)) {
+                    out[at.at + e] = dw[kSums ? p : 0][e];
+                    out[a.D + at.at + e] = db[kSums ? p : 0][e];
+                }
+        }
+    }
+}
+
+// dx alone, rows of any width.
 template <class T, class P>
-__global__ __launch_bounds__(kThreads) void norm_dx_kernel(const T* dy, const T* x, const float* mean, const float* rstd, const P* weight,
-                                                           T* dx, uint32_t D, int64_t dy_stride, int64_t x_stride, int64_t dx_stride) {
-    __shared__ float lds[4];
-    const T* dyr = dy + (int64_t)blockIdx.x * dy_stride;
-    const T* xr = x + (int64_t)blockIdx.x * x_stride;
-    T* dxr = dx + (int64_t)blockIdx.x * dx_stride;
-    const float m = mean[blockIdx.x], r = rstd[blockIdx.x];
-    float sg = 0.0f, sgx = 0.0f;
-    for (uint32_t i = threadIdx.x; i < D; i += kThreads) {
+__global__ __launch_bounds__(1024) void norm_dx_wide_kernel(const NormBackward a) {
+    __shared__ float lds[32];
+    const T* dyr = static_cast<const T*>(a.dy) + (int64_t)blockIdx.x * a.dy_stride;
+    const T* xr = static_cast<const T*>(a.x) + (int64_t)blockIdx.x * a.x_stride;
+    T* dxr = static_cast<T*>(a.dx) + (int64_t)blockIdx.x * a.dx_stride;
+    const P* weight = static_cast<const P*>(a.weight);
+    const float m = a.mean[blockIdx.x], r = a.rstd[blockIdx.x];
+    float s[2] = {0.0f, 0.0f};
+    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u) {
         const float g = load1(dyr + i) * (weight ? load1(weight + i) : 1.0f);
-        sg += g;
-        sgx = __builtin_fmaf(g, (load1(xr + i) - m) * r, sgx);
+        s[0] += g;
+        s[1] = __builtin_fmaf(g, (load1(xr + i) - m) * r, s[1]);
     }
-    sg = group_sum(sg, lds) / (float)D;
-    sgx = group_sum(sgx, lds) / (float)D;
-    for (uint32_t i = threadIdx.x; i < D; i += kThreads) {
+    row_sums<1024, 2>(s, 0, lds);
+    const float per = 1.0f / (float)a.D;
+    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u) {
         const float g = load1(dyr + i) * (weight ? load1(weight + i) : 1.0f);
-        const float h = (load1(xr + i) - m) * r;
-        store1(dxr + i, r * __builtin_fmaf(-h, sgx, g - sg));
+        store1(dxr + i, r * __builtin_fmaf(-(load1(xr + i) - m) * r, s[1] * per, __builtin_fmaf(-s[0], per, g)));
     }
 }
 
-template <class T, class P>
-__global__ __launch_bounds__(kThreads) void norm_dw_kernel(const T* dy, const T* x, const float* mean, const float* rstd, P* dweight,
-                                                           P* dbias, uint32_t n, uint32_t D, int64_t dy_stride, int64_t x_stride) {
-    const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-    if (i >= D) return;
-    float w = 0.0f, b = 0.0f;
-    for (uint32_t k = 0; k < n; ++k) {
-        const float g = load1(dy + k * dy_stride + i);
-        w = __builtin_fmaf(g, (load1(x + k * x_stride + i) - mean[k]) * rstd[k], w);
-        b += g;
+// The sums over rows alone, for rows whose sums a workgroup cannot hold: a wavefront takes 64 vectors of columns and every fourth row of its
+// workgroup's.
+template <class T>
+__global__ __launch_bounds__(256) void norm_sums_kernel(const NormBackward a, uint32_t rows) {
+    constexpr int N = Vec<T>::N;
+    __shared__ float lds[2 * N * 64];
+    const uint32_t l = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const Place<N, false> at(blockIdx.x * 64u + l, a.D);
+    const size_t col = at.at;
+    float dw[N] = {}, db[N] = {};
+    const uint64_t first = (uint64_t)blockIdx.y * rows, last = min(first + rows, (uint64_t)a.n);
+    if (at.any())
+#pragma unroll 2
+        for (uint64_t row = first + wave; row < last; row += 4) {
+            Vec<T> g, x;
+            g.load(static_cast<const T*>(a.dy) + (int64_t)row * a.dy_stride + col);
+            x.load(static_cast<const T*>(a.x) + (int64_t)row * a.x_stride + col);
+            const float m = a.mean[row], r = a.rstd[row];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                dw[e] = __builtin_fmaf(g.get(e), (x.get(e) - m) * r, dw[e]);
+                db[e] += g.get(e);
+            }
+        }
+    for (uint32_t k = 0; k < 4; ++k) {
+        if (wave == k)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                dw[e] += k ? lds[e * 64 + l] : 0.0f;
+                db[e] += k ? lds[(N + e) * 64 + l] : 0.0f;
+                lds[e * 64 + l] = dw[e];
+                lds[(N + e) * 64 + l] = db[e];
+            }
+        __syncthreads();
     }
-    if (dweight) store1(dweight + i, w);
-    if (dbias) store1(dbias + i, b);
+    float* out = a.sums + (size_t)blockIdx.y * 2u * a.D;
+    if (wave == 3)
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (at.own(e)) {
+                out[col + e] = dw[e];
+                out[a.D + col + e] = db[e];
+            }
+}
+
+// The workgroups' sums in their order: 64 columns a workgroup, their sums dealt to 16 wavefronts.
+template <class P>
+__global__ __launch_bounds__(1024) void norm_finish_kernel(const float* sums, uint32_t parts, uint32_t D, P* dw, P* db) {
+    __shared__ float lds[16][64];
+    const uint32_t l = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const size_t i = (size_t)blockIdx.x * 64u + l;
+    float s = 0.0f;
+    if (i < 2u * (size_t)D)
+#pragma unroll 8
+        for (uint32_t k = wave; k < parts; k += 16u) s += sums[(size_t)k * 2u * D + i];
+    lds[wave][l] = s;
+    __syncthreads();
+    if (wave) return;
+    for (uint32_t k = 1; k < 16u; ++k) s += lds[k][l];
+    if (i < D) {
+        if (dw) store1(dw + i, s);
+    } else if (i < 2u * (size_t)D) {
+        if (db) store1(db + (i - D), s);
+    }
+}
+
+// How a description is laid out on the device.
+struct Plan {
+    uint32_t vectors, lanes, groups;  // of a row; lanes of a row (0 = a workgroup); rows that a workgroup takes in one go
+    bool sums_inside;                 // the backward kernel forms the sums over rows
+    uint32_t parts, rows;             // workgroups' sums, and rows for each where a kernel of their own forms them
+};
+
+constexpr uint32_t kCus = 256;  // compute units of the device this library is for
+
+Plan plan_of(const pxr_layer_norm_desc& d) {
+    const uint32_t N = d.dtype == PXR_F32 ? 4u : 8u;
+    Plan p{};
+    p.vectors = (d.width + N - 1u) / N;
+    p.lanes = 0;
+    p.groups = 1;
+    if (p.vectors <= 256u) {
+        p.lanes = 64;
+        while (p.lanes > 1u && p.lanes / 2u >= p.vectors) p.lanes /= 2u;
+        p.groups = kSubThreads / p.lanes;
+    }
+    // (a lane's sums: 2 N floats for each vector, 64 of them at most beside the row itself)
+    p.sums_inside = p.vectors <= 4096u;
+    if (p.sums_inside) {
+        // two workgroups of 512 threads, or one of 1024, for each compute unit
+        const uint64_t need = (d.n_rows + p.groups - 1u) / p.groups;
+        p.parts = (uint32_t)(need < (p.vectors <= 1024u ? 2u * kCus : kCus) ? need : (p.vectors <= 1024u ? 2u * kCus : kCus));
+    } else {
+        const uint32_t across = (p.vectors + 63u) / 64u;
+        uint64_t parts = (4u * kCus + across - 1u) / across;
+        if (parts > (d.n_rows + 15u) / 16u) parts = (d.n_rows + 15u) / 16u;
+        if (parts == 0) parts = 1;
+        p.rows = (uint32_t)((d.n_rows + parts - 1u) / parts);
+        p.parts = p.rows ? (uint32_t)((d.n_rows + p.rows - 1u) / p.rows) : 0u;
+    }
+    return p;
 }
 
 template <class T, class P>
-void forward_as(const pxr_layer_norm_desc& d, const void* x, const void* w, const void* b, void* y, float* mean, float* rstd, hipStream_t st) {
-    hipLaunchKernelGGL((norm_forward_kernel<T, P>), dim3((uint32_t)d.n_rows), dim3(kThreads), 0, st, static_cast<const T*>(x),
-                       static_cast<const P*>(w), static_cast<const P*>(b), static_cast<T*>(y), mean, rstd, d.width, d.x_stride, d.y_stride, d.eps);
+void forward_as(const pxr_layer_norm_desc& d, NormForward a, hipStream_t st) {
+    const Plan p = plan_of(d);
+    const auto grid = [&](uint32_t rows_each, uint32_t most) {
+        const uint64_t need = (d.n_rows + rows_each - 1u) / rows_each;
+        return dim3((uint32_t)(need < most ? need : most));
+    };
+    a.lanes = p.lanes;
+#define PXR_NORM(NT, VPL, U, GROUPS, MOST) \
+    hipLaunchKernelGGL((norm_forward_kernel<T, P, NT, VPL, U>), grid(GROUPS * U, MOST), dim3(kThreadsOf(NT)), 0, st, a)
+    // Rows that do not fill the device go one by one; many go four at a time.
+    const bool many = d.n_rows >= 4u * kCus;
+    if (d.width < (uint32_t)Vec<T>::N)
+        hipLaunchKernelGGL((norm_forward_kernel<T, P, 0, 1, 4, true>), grid(4u * p.groups, 4u * kCus), dim3(kSubThreads), 0, st, a);
+    else if (p.vectors <= 64u)
+        PXR_NORM(0, 1, 4, p.groups, 4u * kCus);
+    else if (p.vectors <= 128u)
+        PXR_NORM(0, 2, 2, p.groups, 4u * kCus);
+    else if (p.vectors <= 256u)
+        PXR_NORM(0, 4, 1, p.groups, 4u * kCus);
+    else if (p.vectors <= 1024u) {
+        if (many)
+            PXR_NORM(512, 2, 4, 1u, 4u * kCus);
+        else
+            PXR_NORM(512, 2, 1, 1u, 4u * kCus);
+    } else if (p.vectors <= 4096u) {
+        if (many)
+            PXR_NORM(1024, 4, 4, 1u, 2u * kCus);
+        else
+            PXR_NORM(1024, 4, 1, 1u, 2u * kCus);
+    } else if (p.vectors <= 8192u)
+        PXR_NORM(1024, 8, 1, 1u, 2u * kCus);
+    else
+        hipLaunchKernelGGL((norm_forward_wide_kernel<T, P>), dim3((uint32_t)d.n_rows), dim3(1024), 0, st, a);
+#undef PXR_NORM
 }
 
 template <class T, class P>
-void backward_as(const pxr_layer_norm_desc& d, const void* dy, const void* x, const float* mean, const float* rstd, const void* w,
-                 void* dx, void* dw, void* db, void*, hipStream_t st) {
-    // (the sums over rows first: dx may be dy or x itself)
+void backward_as(const pxr_layer_norm_desc& d, NormBackward a, void* dw, void* db, hipStream_t st) {
+    constexpr uint32_t N = Vec<T>::N;
+    const Plan p = plan_of(d);
+    a.lanes = p.lanes;
+    const auto lds_of = [&](uint32_t vpl, uint32_t u) {
+        const uint32_t sums = p.lanes * vpl * N * 2u * 4u, turns = 2u * 2u * u * 16u * 4u;
+        return p.lanes ? sums : turns;
+    };
+#define PXR_NORM(NT, VPL, U, SUMS, GRID) \
+    hipLaunchKernelGGL((norm_backward_kernel<T, P, NT, VPL, U, SUMS>), dim3(GRID), dim3(kThreadsOf(NT)), lds_of(VPL, U), st, a)
+    if (p.sums_inside) {
+        if (d.n_rows) {
+            if (d.width < N)
+                hipLaunchKernelGGL((norm_backward_kernel<T, P, 0, 1, 2, true, true>), dim3(p.parts), dim3(kSubThreads), lds_of(1, 2), st, a);
+            else if (p.vectors <= 64u)
+                PXR_NORM(0, 1, 2, true, p.parts);
+            else if (p.vectors <= 128u)
+                PXR_NORM(0, 2, 1, true, p.parts);
+            else if (p.vectors <= 256u)
+                PXR_NORM(0, 4, 1, true, p.parts);
+            else if (p.vectors <= 1024u)
+                PXR_NORM(512, 2, 1, true, p.parts);
+            else
+                PXR_NORM(1024, 4, 1, true, p.parts);
+        }
+    } else {
+        // (the sums first: dx may be dy or x itself)
+        if (a.sums && d.n_rows)
+            hipLaunchKernelGGL((norm_sums_kernel<T>), dim3((p.vectors + 63u) / 64u, p.parts), dim3(256), 0, st, a, p.rows);
+        if (d.n_rows) {
+            if (p.vectors <= 8192u)
+                PXR_NORM(1024, 8, 1, false, (uint32_t)(d.n_rows < 2u * kCus ? d.n_rows : 2u * kCus));
+            else
+                hipLaunchKernelGGL((norm_dx_wide_kernel<T, P>), dim3((uint32_t)d.n_rows), dim3(1024), 0, st, a);
+        }
+    }
+#undef PXR_NORM
     if (dw || db)
-        hipLaunchKernelGGL((norm_dw_kernel<T, P>), dim3((d.width + kThreads - 1) / kThreads), dim3(kThreads), 0, st,
-                           static_cast<const T*>(dy), static_cast<const T*>(x), mean, rstd, static_cast<P*>(dw), static_cast<P*>(db),
-                           (uint32_t)d.n_rows, d.width, d.y_stride, d.x_stride);
-    if (d.n_rows)
-        hipLaunchKernelGGL((norm_dx_kernel<T, P>), dim3((uint32_t)d.n_rows), dim3(kThreads), 0, st, static_cast<const T*>(dy),
-                           static_cast<const T*>(x), mean, rstd, static_cast<const P*>(w), static_cast<T*>(dx), d.width, d.y_stride,
-                           d.x_stride, d.dx_stride);
+        hipLaunchKernelGGL((norm_finish_kernel<P>), dim3((uint32_t)((2ull * d.width + 63u) / 64u)), dim3(1024), 0, st, a.sums, p.parts, d.width,
+                           static_cast<P*>(dw), static_cast<P*>(db));
 }
 
 int launched(std::string& err) {
@@ -120,30 +650,33 @@ int launched(std::string& err) {
 
 }  // namespace
 
-size_t layer_norm_workspace(const pxr_layer_norm_desc&) { return 0; }
+size_t layer_norm_workspace(const pxr_layer_norm_desc& d) { return (size_t)plan_of(d).parts * 2u * d.width * sizeof(float); }
 
 int launch_layer_norm_forward(const pxr_layer_norm_desc& d, const void* x, const void* w, const void* b, void* y, float* mean, float* rstd,
                               void* stream, std::string& err) {
     if (d.n_rows == 0) return PXR_OK;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    const NormForward a{x, w, b, y, mean, rstd, d.x_stride, d.y_stride, (uint32_t)d.n_rows, d.width, 0u, d.eps};
     if (d.dtype == PXR_F32)
-        forward_as<float, float>(d, x, w, b, y, mean, rstd, st);
+        forward_as<float, float>(d, a, st);
     else if (d.param_dtype == PXR_F32)
-        forward_as<__bf16, float>(d, x, w, b, y, mean, rstd, st);
+        forward_as<__bf16, float>(d, a, st);
     else
-        forward_as<__bf16, __bf16>(d, x, w, b, y, mean, rstd, st);
+        forward_as<__bf16, __bf16>(d, a, st);
     return launched(err);
 }
 
 int launch_layer_norm_backward(const pxr_layer_norm_desc& d, const void* dy, const void* x, const float* mean, const float* rstd,
                                const void* w, void* dx, void* dw, void* db, void* ws, void* stream, std::string& err) {
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    const NormBackward a{dy, x, mean, rstd, w, dx, dw || db ? static_cast<float*>(ws) : nullptr, d.y_stride, d.x_stride, d.dx_stride,
+                         (uint32_t)d.n_rows, d.width, 0u};
     if (d.dtype == PXR_F32)
-        backward_as<float, float>(d, dy, x, mean, rstd, w, dx, dw, db, ws, st);
+        backward_as<float, float>(d, a, dw, db, st);
     else if (d.param_dtype == PXR_F32)
-        backward_as<__bf16, float>(d, dy, x, mean, rstd, w, dx, dw, db, ws, st);
+        backward_as<__bf16, float>(d, a, dw, db, st);
     else
-        backward_as<__bf16, __bf16>(d, dy, x, mean, rstd, w, dx, dw, db, ws, st);
+        backward_as<__bf16, __bf16>(d, a, dw, db, st);
     return launched(err);
 }
 
