@@ -101,6 +101,17 @@ struct Place {
     __device__ __forceinline__ bool own(int e) const { return kTiny ? e < to : e >= from; }
 };
 
+// A lane's number where 1024 threads hold a row: the places of its vectors are worked out again where they are used, since the
+// registers are full without them.
+template <int NT>
+__device__ __forceinline__ uint32_t again(uint32_t l) {
+    if (NT == 1024) asm volatile("" : "+v"(l));
+    return l;
+}
+
+// A sum is formed up to here: the compiler would otherwise put off what it is made of, and keep all of it, until the sum is read.
+__device__ __forceinline__ void formed(float& v) { asm volatile("" : "+v"(v)); }
+
 // The parameters of a vector, `def` where there is no array.
 template <class P, int N, bool kTiny>
 __device__ __forceinline__ void load_params(const P* p, float def, const Place<N, kTiny>& at, float (&f)[N]) {
@@ -165,7 +176,8 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
     constexpr bool kKeep = NT == 0;  // parameters stay in registers
     typedef Place<N, kTiny> At;
     __shared__ float lds[2 * U * 16];
-    const uint32_t lanes = NT ? NT : a.lanes, l = threadIdx.x & (lanes - 1u), group = threadIdx.x / lanes, groups = kThreadsOf(NT) / lanes;
+    const uint32_t lanes = NT ? NT : a.lanes, l = NT ? threadIdx.x : threadIdx.x & (lanes - 1u);
+    const uint32_t group = NT ? 0u : threadIdx.x / lanes, groups = NT ? 1u : kThreadsOf(NT) / lanes;
     const P *weight = static_cast<const P*>(a.weight), *bias = static_cast<const P*>(a.bias);
     float w[kKeep ? VPL : 1][N], b[kKeep ? VPL : 1][N];
     if (kKeep)
@@ -182,7 +194,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
             const T* xr = static_cast<const T*>(a.x) + (int64_t)min(row0 + u, (uint64_t)a.n - 1u) * a.x_stride;
 #pragma unroll
             for (int p = 0; p < VPL; ++p) {
-                const At at(l + p * lanes, a.D);
+                const At at(again<NT>(l) + p * lanes, a.D);
                 if (kTiny)
                     x[u][p].load_some(xr, at.to);
                 else
@@ -195,7 +207,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
             mean[u] = 0.0f;
 #pragma unroll
             for (int p = 0; p < VPL; ++p) {
-                const At at(l + p * lanes, a.D);
+                const At at(again<NT>(l) + p * lanes, a.D);
                 float s = 0.0f;
 #pragma unroll
                 for (int e = 0; e < N; ++e) s += x[u][p].get(e);
@@ -205,6 +217,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
                     for (int e = 0; e < N; ++e) s += at.own(e) ? x[u][p].get(e) : 0.0f;
                 }
                 mean[u] += s;
+                formed(mean[u]);
                 x[u][p].as_they_came();
             }
         }
@@ -215,7 +228,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
             rstd[u] = 0.0f;
 #pragma unroll
             for (int p = 0; p < VPL; ++p) {
-                const At at(l + p * lanes, a.D);
+                const At at(again<NT>(l) + p * lanes, a.D);
                 float s = 0.0f;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
@@ -231,6 +244,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
                     }
                 }
                 rstd[u] += s;
+                formed(rstd[u]);
                 x[u][p].as_they_came();
             }
         }
@@ -245,7 +259,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
         }
 #pragma unroll
         for (int p = 0; p < VPL; ++p) {
-            const At at(l + p * lanes, a.D);
+            const At at(again<NT>(l) + p * lanes, a.D);
             if (!kKeep) {
                 load_params(weight, 1.0f, at, w[0]);
                 load_params(bias, 0.0f, at, b[0]);
@@ -298,48 +312,71 @@ struct NormBackward {
     uint32_t n, D, lanes;
 };
 
-// kSums: the sums over rows are formed here as well.
+// kSums: the sums over rows are formed here as well.  Workgroups of 1024 threads hold those of db in LDS, each lane its own words: beside dw and a
+// row they do not fit the registers.  Where the weights stay in registers a workgroup asks for its next rows before it works on the present ones
+// (a request for weights behind them would have to wait for them: the memory answers in order).
 template <class T, class P, int NT, int VPL, int U, bool kSums, bool kTiny = false>
 __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const NormBackward a) {
     constexpr int N = Vec<T>::N;
-    constexpr bool kKeep = NT == 0 && VPL <= 2;
+    constexpr bool kKeep = VPL * N <= 16, kAhead = NT != 0 && VPL <= 2, kLds = kSums && NT == 1024;
+    static_assert(kKeep || !kAhead);
     typedef Place<N, kTiny> At;
-    extern __shared__ __align__(16) float lds[];  // 2 x 2 U x 16 floats, or (NT == 0) the sums of a wavefront's lanes
-    const uint32_t lanes = NT ? NT : a.lanes, l = threadIdx.x & (lanes - 1u), group = threadIdx.x / lanes, groups = kThreadsOf(NT) / lanes;
+    extern __shared__ __align__(16) float lds[];  // 2 x 2 U x 16 floats and db, or (NT == 0) the sums of a wavefront's lanes
+    float* const db_lds = lds + 2 * (2 * U * 16);  // [VPL N][1024]
+    const uint32_t lanes = NT ? NT : a.lanes, l = NT ? threadIdx.x : threadIdx.x & (lanes - 1u);
+    const uint32_t group = NT ? 0u : threadIdx.x / lanes, groups = NT ? 1u : kThreadsOf(NT) / lanes;
     const P* weight = static_cast<const P*>(a.weight);
     float w[kKeep ? VPL : 1][N];
     if (kKeep)
 #pragma unroll
         for (int p = 0; p < VPL; ++p) load_params(weight, 1.0f, At(l + p * lanes, a.D), w[kKeep ? p : 0]);
-    float dw[kSums ? VPL : 1][N] = {}, db[kSums ? VPL : 1][N] = {};
+    float dw[kSums ? VPL : 1][N] = {}, db[kSums && !kLds ? VPL : 1][N] = {};
+    if (kLds)
+#pragma unroll
+        for (int i = 0; i < VPL * N; ++i) db_lds[i * 1024 + l] = 0.0f;
     const float per = 1.0f / (float)a.D;
-    uint32_t turn = 0;
-    for (uint64_t row0 = ((uint64_t)blockIdx.x * groups + group) * U; row0 < a.n; row0 += (uint64_t)gridDim.x * groups * U) {
+    struct Rows {
         Vec<T> g[U][VPL], x[U][VPL];
-        float mean[U], rstd[U], s[2 * U];
+        float mean[U], rstd[U];
+    };
+    const auto ask = [&](Rows& r, uint64_t row0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint64_t row = min(row0 + u, (uint64_t)a.n - 1u);
             const T *gr = static_cast<const T*>(a.dy) + (int64_t)row * a.dy_stride, *xr = static_cast<const T*>(a.x) + (int64_t)row * a.x_stride;
 #pragma unroll
             for (int p = 0; p < VPL; ++p) {
-                const At at(l + p * lanes, a.D);
+                const At at(again<NT>(l) + p * lanes, a.D);
                 if (kTiny) {
-                    g[u][p].load_some(gr, at.to);
-                    x[u][p].load_some(xr, at.to);
+                    r.g[u][p].load_some(gr, at.to);
+                    r.x[u][p].load_some(xr, at.to);
                 } else {
-                    g[u][p].load(gr + at.at);
-                    x[u][p].load(xr + at.at);
+                    r.g[u][p].load(gr + at.at);
+                    r.x[u][p].load(xr + at.at);
                 }
             }
-            mean[u] = a.mean[row];
-            rstd[u] = a.rstd[row];
+            r.mean[u] = a.mean[row];
+            r.rstd[u] = a.rstd[row];
         }
+    };
+    uint32_t turn = 0;
+    uint64_t row0 = ((uint64_t)blockIdx.x * groups + group) * U;
+    const uint64_t stride = (uint64_t)gridDim.x * groups * U;
+    Rows r, ahead;
+    if (kAhead && row0 < a.n) ask(ahead, row0);
+    for (; row0 < a.n; row0 += stride) {
+        if (kAhead) {
+            r = ahead;
+            if (row0 + stride < a.n) ask(ahead, row0 + stride);
+        } else {
+            ask(r, row0);
+        }
+        float s[2 * U];
 #pragma unroll
         for (int u = 0; u < U; ++u) s[2 * u] = s[2 * u + 1] = 0.0f;
 #pragma unroll
         for (int p = 0; p < VPL; ++p) {
-            const At at(l + p * lanes, a.D);
+            const At at(again<NT>(l) + p * lanes, a.D);
             // (one vector's weights and floats after the other: all of them at once do not fit the registers of 1024 threads)
             if (NT == 1024) __builtin_amdgcn_sched_barrier(0);
             if (!kKeep) load_params(weight, 1.0f, at, w[0]);
@@ -347,33 +384,36 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
             for (int u = 0; u < U; ++u) {
                 // What is not the lane's own is nothing: its gradient is zero here, and so is what it adds to a sum.  (x beside it is of the same
                 // row: where it is no number, the row's gradient is none either.  A row past the last must not reach the sums over rows.)
-                if (!at.whole()) g[u][p].keep(at.from, at.to);
+                if (!at.whole()) r.g[u][p].keep(at.from, at.to);
                 if (row0 + u >= a.n) {
-                    g[u][p].keep(0, 0);
-                    x[u][p].keep(0, 0);
-                    mean[u] = rstd[u] = 0.0f;
+                    r.g[u][p].keep(0, 0);
+                    r.x[u][p].keep(0, 0);
+                    r.mean[u] = r.rstd[u] = 0.0f;
                 }
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const float d = g[u][p].get(e), xh = (x[u][p].get(e) - mean[u]) * rstd[u];
+                    const float d = r.g[u][p].get(e), xh = (r.x[u][p].get(e) - r.mean[u]) * r.rstd[u];
                     const float wd = d * w[kKeep ? p : 0][e];
                     s[2 * u] += wd;
                     s[2 * u + 1] = __builtin_fmaf(wd, xh, s[2 * u + 1]);
-                    if (kSums) {
-                        dw[kSums ? p : 0][e] = __builtin_fmaf(d, xh, dw[kSums ? p : 0][e]);
-                        db[kSums ? p : 0][e] += d;
-                    }
+                    if (kSums) dw[kSums ? p : 0][e] = __builtin_fmaf(d, xh, dw[kSums ? p : 0][e]);
+                    if (kLds) formed(dw[kSums ? p : 0][e]);
+                    if (kLds)
+                        db_lds[(p * N + e) * 1024 + again<NT>(l)] += d;
+                    else if (kSums)
+                        db[kSums && !kLds ? p : 0][e] += d;
                 }
-                g[u][p].as_they_came();
-                x[u][p].as_they_came();
+                formed(s[2 * u]);
+                formed(s[2 * u + 1]);
+                r.g[u][p].as_they_came();
+                r.x[u][p].as_they_came();
             }
         }
         row_sums<NT, 2 * U>(s, lanes, lds + (turn & 1u) * (2 * U * 16));
         ++turn;
 #pragma unroll
         for (int p = 0; p < VPL; ++p) {
-            const At at(l + p * lanes, a.D);
-            // (one vector's weights and floats after the other: all of them at once do not fit the registers of 1024 threads)
+            const At at(again<NT>(l) + p * lanes, a.D);
             if (NT == 1024) __builtin_amdgcn_sched_barrier(0);
             if (!kKeep) load_params(weight, 1.0f, at, w[0]);
 #pragma unroll
@@ -382,8 +422,8 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
                 float dx[N];
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const float xh = (x[u][p].get(e) - mean[u]) * rstd[u];
-                    dx[e] = rstd[u] * __builtin_fmaf(-xh, s[2 * u + 1] * per, __builtin_fmaf(g[u][p].get(e), w[kKeep ? p : 0][e], -s[2 * u] * per));
+                    const float xh = (r.x[u][p].get(e) - r.mean[u]) * r.rstd[u];
+                    dx[e] = r.rstd[u] * __builtin_fmaf(-xh, s[2 * u + 1] * per, __builtin_fmaf(r.g[u][p].get(e), w[kKeep ? p : 0][e], -s[2 * u] * per));
                 }
                 Vec<T>::store(static_cast<T*>(a.dx) + ((int64_t)(row0 + u) * a.dx_stride + at.at), dx, at.from, at.to);
             }
@@ -399,7 +439,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     dw[kSums ? p : 0][e] += __shfl_xor(dw[kSums ? p : 0][e], m);
-                    db[kSums ? p : 0][e] += __shfl_xor(db[kSums ? p : 0][e], m);
+                    db[kSums && !kLds ? p : 0][e] += __shfl_xor(db[kSums && !kLds ? p : 0][e], m);
                 }
         const uint32_t span = lanes * VPL * N;
         for (uint32_t wave = 0; wave < kSubThreads / 64u; ++wave) {
@@ -411,7 +451,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
                     for (int e = 0; e < N; ++e) {
                         float* q = lds + (p * N + e) * lanes + l;
                         q[0] = (wave ? q[0] : 0.0f) + dw[kSums ? p : 0][e];
-                        q[span] = (wave ? q[span] : 0.0f) + db[kSums ? p : 0][e];
+                        q[span] = (wave ? q[span] : 0.0f) + db[kSums && !kLds ? p : 0][e];
                     }
         }
         __syncthreads();
@@ -423,13 +463,13 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
     } else {
 #pragma unroll
         for (int p = 0; p < VPL; ++p) {
-            const At at(l + p * lanes, a.D);
+            const At at(again<NT>(l) + p * lanes, a.D);
             if (!at.any()) continue;
 #pragma unroll
             for (int e = 0; e < N; ++e)
                 if (at.own(e)) {
                     out[at.at + e] = dw[kSums ? p : 0][e];
-                    out[a.D + at.at + e] = db[kSums ? p : 0][e];
+                    out[a.D + at.at + e] = kLds ? db_lds[(p * N + e) * 1024 + l] : db[kSums && !kLds ? p : 0][e];
                 }
         }
     }
@@ -533,23 +573,22 @@ struct Plan {
 
 constexpr uint32_t kCus = 256;  // compute units of the device this library is for
 
-Plan plan_of(const pxr_layer_norm_desc& d) {
+Plan plan_of(const pxr_layer_norm_desc& d, uint32_t widest) {
     const uint32_t N = d.dtype == PXR_F32 ? 4u : 8u;
     Plan p{};
     p.vectors = (d.width + N - 1u) / N;
     p.lanes = 0;
     p.groups = 1;
-    if (p.vectors <= 256u) {
+    if (p.vectors <= widest) {  // (the widest row that a wavefront takes)
         p.lanes = 64;
         while (p.lanes > 1u && p.lanes / 2u >= p.vectors) p.lanes /= 2u;
         p.groups = kSubThreads / p.lanes;
     }
-    // (a lane's sums: 2 N floats for each vector, 64 of them at most beside the row itself)
-    p.sums_inside = p.vectors <= 4096u;
+    p.sums_inside = p.vectors * N <= 32768u;  // 32 values a lane of 1024: what its registers hold of dw and LDS of db
     if (p.sums_inside) {
-        // two workgroups of 512 threads, or one of 1024, for each compute unit
-        const uint64_t need = (d.n_rows + p.groups - 1u) / p.groups;
-        p.parts = (uint32_t)(need < (p.vectors <= 1024u ? 2u * kCus : kCus) ? need : (p.vectors <= 1024u ? 2u * kCus : kCus));
+        // two workgroups of up to 512 threads, or one of 1024, for each compute unit
+        const uint64_t need = (d.n_rows + p.groups - 1u) / p.groups, most = p.vectors <= 1024u ? 2u * kCus : kCus;
+        p.parts = (uint32_t)(need < most ? need : most);
     } else {
         const uint32_t across = (p.vectors + 63u) / 64u;
         uint64_t parts = (4u * kCus + across - 1u) / across;
@@ -560,10 +599,11 @@ Plan plan_of(const pxr_layer_norm_desc& d) {
     }
     return p;
 }
+constexpr uint32_t kWidestForward = 256u, kWidestBackward = 128u;
 
 template <class T, class P>
 void forward_as(const pxr_layer_norm_desc& d, NormForward a, hipStream_t st) {
-    const Plan p = plan_of(d);
+    const Plan p = plan_of(d, kWidestForward);
     const auto grid = [&](uint32_t rows_each, uint32_t most) {
         const uint64_t need = (d.n_rows + rows_each - 1u) / rows_each;
         return dim3((uint32_t)(need < most ? need : most));
@@ -601,38 +641,48 @@ void forward_as(const pxr_layer_norm_desc& d, NormForward a, hipStream_t st) {
 template <class T, class P>
 void backward_as(const pxr_layer_norm_desc& d, NormBackward a, void* dw, void* db, hipStream_t st) {
     constexpr uint32_t N = Vec<T>::N;
-    const Plan p = plan_of(d);
+    const Plan p = plan_of(d, kWidestBackward);
     a.lanes = p.lanes;
-    const auto lds_of = [&](uint32_t vpl, uint32_t u) {
+    const auto lds_of = [&](uint32_t vpl, uint32_t u, bool in_lds) {
         const uint32_t sums = p.lanes * vpl * N * 2u * 4u, turns = 2u * 2u * u * 16u * 4u;
-        return p.lanes ? sums : turns;
+        return p.lanes ? sums : turns + (in_lds ? vpl * N * 1024u * 4u : 0u);
     };
-#define PXR_NORM(NT, VPL, U, SUMS, GRID) \
-    hipLaunchKernelGGL((norm_backward_kernel<T, P, NT, VPL, U, SUMS>), dim3(GRID), dim3(kThreadsOf(NT)), lds_of(VPL, U), st, a)
+    const dim3 parts(p.parts);
+#define PXR_NORM(NT, VPL, U, SUMS, GRID)                                                                                                  \
+    hipLaunchKernelGGL((norm_backward_kernel<T, P, NT, VPL, U, SUMS>), GRID, dim3(kThreadsOf(NT)), lds_of(VPL, U, SUMS && NT == 1024), st, a)
     if (p.sums_inside) {
         if (d.n_rows) {
             if (d.width < N)
-                hipLaunchKernelGGL((norm_backward_kernel<T, P, 0, 1, 2, true, true>), dim3(p.parts), dim3(kSubThreads), lds_of(1, 2), st, a);
+                hipLaunchKernelGGL((norm_backward_kernel<T, P, 0, 1, 2, true, true>), parts, dim3(kSubThreads), lds_of(1, 2, false), st, a);
             else if (p.vectors <= 64u)
-                PXR_NORM(0, 1, 2, true, p.parts);
+                PXR_NORM(0, 1, 2, true, parts);
             else if (p.vectors <= 128u)
-                PXR_NORM(0, 2, 1, true, p.parts);
+                PXR_NORM(0, 2, 1, true, parts);
             else if (p.vectors <= 256u)
-                PXR_NORM(0, 4, 1, true, p.parts);
+                PXR_NORM(256, 1, 2, true, parts);
+            else if (p.vectors <= 512u)
+                PXR_NORM(512, 1, 2, true, parts);
             else if (p.vectors <= 1024u)
-                PXR_NORM(512, 2, 1, true, p.parts);
-            else
-                PXR_NORM(1024, 4, 1, true, p.parts);
+                PXR_NORM(512, 2, 1, true, parts);
+            else if (p.vectors <= 2048u)
+                PXR_NORM(1024, 2, 1, true, parts);
+            else if (N == 8u || p.vectors <= 4096u)
+                PXR_NORM(1024, 4, 1, true, parts);
+            else if constexpr (N == 4u)
+                PXR_NORM(1024, 8, 1, true, parts);
         }
     } else {
         // (the sums first: dx may be dy or x itself)
         if (a.sums && d.n_rows)
             hipLaunchKernelGGL((norm_sums_kernel<T>), dim3((p.vectors + 63u) / 64u, p.parts), dim3(256), 0, st, a, p.rows);
         if (d.n_rows) {
-            if (p.vectors <= 8192u)
-                PXR_NORM(1024, 8, 1, false, (uint32_t)(d.n_rows < 2u * kCus ? d.n_rows : 2u * kCus));
-            else
-                hipLaunchKernelGGL((norm_dx_wide_kernel<T, P>), dim3((uint32_t)d.n_rows), dim3(1024), 0, st, a);
+            bool done = false;
+            if constexpr (N == 8u)
+                if (p.vectors <= 8192u) {
+                    PXR_NORM(1024, 8, 1, false, dim3((uint32_t)(d.n_rows < 2u * kCus ? d.n_rows : 2u * kCus)));
+                    done = true;
+                }
+            if (!done) hipLaunchKernelGGL((norm_dx_wide_kernel<T, P>), dim3((uint32_t)d.n_rows), dim3(1024), 0, st, a);
         }
     }
 #undef PXR_NORM
@@ -650,7 +700,7 @@ int launched(std::string& err) {
 
 }  // namespace
 
-size_t layer_norm_workspace(const pxr_layer_norm_desc& d) { return (size_t)plan_of(d).parts * 2u * d.width * sizeof(float); }
+size_t layer_norm_workspace(const pxr_layer_norm_desc& d) { return (size_t)plan_of(d, kWidestBackward).parts * 2u * d.width * sizeof(float); }
 
 int launch_layer_norm_forward(const pxr_layer_norm_desc& d, const void* x, const void* w, const void* b, void* y, float* mean, float* rstd,
                               void* stream, std::string& err) {

@@ -556,7 +556,7 @@ def _empty(torch, like, stream, shape, dtype):
     """Device memory for a call's outputs and workspace.  On a stream of the caller's it comes from that stream's pool: the
     allocator may hand it out again as soon as it is let go, which is in order on that stream and on no other."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=like.device)):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
@@ -592,11 +592,12 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     torch = _torch or _torch_module()
     r, n, width, x_stride = _rows(x)
     params = _params(torch, x, width, weight, bias)
-    y = _empty(torch, x, stream, x.shape, x.dtype) if out is None else out
-    assert y.is_cuda and y.dtype == x.dtype and y.shape == x.shape
-    y_stride = _rows(y)[3]
-    stats = _empty(torch, x, stream, (2,) + tuple(x.shape[:-1]), torch.float32)
-    mean, rstd = stats[0], stats[1]
+    if out is None:
+        y, y_stride = _empty(torch, x, stream, x.shape, x.dtype), width
+    else:
+        assert out.is_cuda and out.dtype == x.dtype and out.shape == x.shape
+        y, y_stride = out, _rows(out)[3]
+    mean, rstd = (_empty(torch, x, stream, x.shape[:-1], torch.float32) for _ in range(2))
     d = LayerNormDesc(_dtype_code(torch, x.dtype), _dtype_code(torch, params), n, width, eps, x_stride, y_stride, width)
     _check((_lib or lib()).pxr_layer_norm_forward(C.byref(d), r.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean.data_ptr(),
                                                   rstd.data_ptr(), _stream_handle(stream, x)))
@@ -614,17 +615,20 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, params_dtype=No
         assert s.is_cuda and s.dtype == torch.float32 and s.is_contiguous() and s.numel() == n, "mean and rstd: one float32 for each row"
     params = _params(torch, x, width, weight) if weight is not None else params_dtype or torch.float32
     assert params in (torch.float32, x.dtype)
-    dx = _empty(torch, x, stream, x.shape, x.dtype) if dx is None else dx
-    assert dx.is_cuda and dx.dtype == x.dtype and dx.shape == x.shape
-    dparams = _empty(torch, x, stream, (2, width), params)
-    d = LayerNormDesc(_dtype_code(torch, x.dtype), _dtype_code(torch, params), n, width, 0.0, x_stride, dy_stride, _rows(dx)[3])
+    if dx is None:
+        dx, dx_stride = _empty(torch, x, stream, x.shape, x.dtype), width
+    else:
+        assert dx.is_cuda and dx.dtype == x.dtype and dx.shape == x.shape
+        dx_stride = _rows(dx)[3]
+    dweight, dbias = (_empty(torch, x, stream, (width,), params) for _ in range(2))
+    d = LayerNormDesc(_dtype_code(torch, x.dtype), _dtype_code(torch, params), n, width, 0.0, x_stride, dy_stride, dx_stride)
     L = _lib or lib()
     need = C.c_size_t()
     _check(L.pxr_layer_norm_workspace(C.byref(d), C.byref(need)))
     ws = _empty(torch, x, stream, (need.value,), torch.uint8) if need.value else None
     _check(L.pxr_layer_norm_backward(C.byref(d), g.data_ptr(), r.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dx.data_ptr(),
-                                     dparams[0].data_ptr(), dparams[1].data_ptr(), _ptr(ws), need.value, _stream_handle(stream, x)))
-    return dx, dparams[0], dparams[1]
+                                     dweight.data_ptr(), dbias.data_ptr(), _ptr(ws), need.value, _stream_handle(stream, x)))
+    return dx, dweight, dbias
 
 
 class LinearAttention:
