@@ -355,14 +355,14 @@ typedef struct {
 } pxr_rollout;
 
 /* Bytes of workspace that the forward (backward == 0) or backward pass needs (host only; may be 0).
- * Errors: INVALID_ARG (null, n_envs == 0). */
+ * Errors: INVALID_ARG (null, sizes or a type that the calls refuse). */
 int pxr_linear_attention_workspace(const pxr_linear_attention* a, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, uint32_t backward,
                                    size_t* bytes);
 
 /* All steps of a rollout at once: out [n_envs,n_steps,n_heads,d_value] of the rollout's type, and the state after the last step
  * in d_state_out [n_envs,n_heads,d_key,d_value] (NULL if not wanted; not the buffer of d_state).  n_steps == 0 passes the
  * state on.  An infinity or NaN in a step's k or v reaches that step and the later ones of the same episode and no others.
- * Errors: INVALID_ARG (null, n_envs == 0, n_envs * n_heads above 2^31-1, a type that is none, a buffer not aligned to its elements, states that
+ * Errors: INVALID_ARG (null, n_envs == 0, n_envs * n_heads above 2^21, n_steps above 2^31-1, a type that is none, a buffer not aligned to its elements, states that
  * overlap, workspace missing, too small or not 16-byte aligned); DEVICE. */
 int pxr_linear_attention_forward(pxr_linear_attention* a, const pxr_rollout* r, const pxr_tokens* out, float* d_state_out,
                                  void* d_workspace, size_t workspace_bytes, void* hip_stream);

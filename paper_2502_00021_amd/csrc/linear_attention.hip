@@ -7,6 +7,25 @@
 //   dq is the scan of (do, v, k): dq_t = scale S_t do_t, and the states are the forward pass' transposed;
 //   dk and dv are scans from the last step to the first, of (v, do, q) and of (k, q, do): their state
 //     R_t = scale q_t do_t^T + (t + 1 begins an episode ? 0 : g R_{t+1}) gives dk_t = R_t v_t, dv_t = R_t^T k_t.
+//
+// A scan takes C steps at a time.  With positions i, j in such a chunk, S the state before it and n of its steps there:
+//   P_ij = g^(i-j) key_scale (x_i . y_j) where j <= i and no episode begins in (j, i], else 0
+//   out_i = out_scale (sum_j P_ij z_j + [no episode begins up to i] g^(i+1) S^T x_i)
+//   S <- [no episode begins] g^n S + sum_j [no episode begins after j] g^(n-1-j) key_scale y_j z_j^T
+// and mirrored from the end for the reverse scans, whose state decays on its way out of a step instead of on its way in.
+//
+// All four products run on the matrix cores, 32 x 32 tiles, sums in fp32.  A wavefront has 32 columns of z and of the state; its state stays in
+// its accumulators [a][32] for the whole scan.  What makes that cheap is that a product's result lies in a lane as the next product wants
+// its operand: a lane has one column and, of every 16 rows, the eight 4h .. 4h+3, 8+4h .. 8+4h+3 (h = lane / 32), and an operand's lane has one row and
+// eight values of the axis that is summed over, whose order is free as long as both operands agree on it.  So P^T = y x^T (a column is a
+// step i) is the right operand of out^T = z^T P^T, and S the left one of S^T x^T, without a move between lanes.  z and y are also
+// wanted with steps along the summed axis: bfloat16 by the transposing LDS read, fp32 by four-byte reads.
+//
+// bfloat16 rounds what is multiplied again: P, S and the weighted z are fp32 and go in as sums of two bfloat16 (P, S: relative error 2^-17 instead of
+// 2^-9, so that an output has its own rounding and no other) or three (z: 2^-25, the state is an fp32 result).  The matrix cores have the time: the scan is
+// bound by memory.
+//
+// Steps that hold an infinity or NaN in y or z are taken one by one: 0 times such a value would reach steps that it must not.
 
 #include <hip/hip_runtime.h>
 
@@ -14,6 +33,12 @@
 
 namespace pxr {
 namespace {
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __bf16* p) { return (float)*p; }
@@ -27,8 +52,22 @@ struct Scan {
     const float* state_in;  // null = zeros
     float* state_out;       // null = not wanted
     uint32_t state_row, state_col;
+    const float* before;  // [segments - 1][environments * heads][a * b], strides as above: the states before the segments but the first
     float out_scale, key_scale;
     uint32_t reverse;
+};
+
+struct Scans {
+    Scan s[3];
+};
+
+// How the steps are cut: a workgroup takes one segment of one (environment, head) and 32 columns a wavefront.
+struct Cut {
+    uint32_t n_heads, rows, n_steps;  // rows = environments * heads
+    uint32_t segments, seg_steps, tiles, waves;
+    const LinearAttentionHead* heads;
+    const uint8_t* resets;
+    int64_t resets_env, resets_step;
 };
 
 template <class T>
@@ -36,38 +75,363 @@ __device__ __forceinline__ T* head_of(const pxr_tokens& t, uint32_t e, uint32_t 
     return static_cast<T*>(t.data) + ((int64_t)e * t.env + (int64_t)h * t.head);
 }
 
-// One lane per column of the state, which lies in LDS; one step after the other.
+// ---- operands: eight values of the summed axis, positions 4h + {0..3, 8..11} of a run of 16
+
 template <class T>
-__global__ __launch_bounds__(64) void scan_kernel(const Scan s, const LinearAttentionHead* heads, uint32_t n_heads, uint32_t n_steps,
-                                                  const uint8_t* resets, int64_t resets_env, int64_t resets_step) {
-    extern __shared__ float state[];  // [a][64]
-    const uint32_t e = blockIdx.x / n_heads, h = blockIdx.x - e * n_heads, lane = threadIdx.x, col = blockIdx.y * 64u + lane;
-    const bool on = col < s.b;
-    const float decay = heads[h].decay, decay_rest = heads[h].decay_rest;
-    const size_t base = (size_t)blockIdx.x * s.a * s.b;
-    for (uint32_t d = 0; d < s.a; ++d)
-        state[d * 64u + lane] = on && s.state_in ? s.state_in[base + (size_t)d * s.state_row + (size_t)col * s.state_col] : 0.0f;
-    const T *x = head_of<const T>(s.x, e, h), *y = head_of<const T>(s.y, e, h), *z = head_of<const T>(s.z, e, h);
-    T* out = head_of<T>(s.out, e, h);
-    for (uint32_t k = 0; k < n_steps; ++k) {
-        const int64_t t = s.reverse ? n_steps - 1u - k : k;
-        // forward: the state decays before a step is added, and not at all into a step that begins an episode; in reverse it
-        // decays after, on its way to the step before
-        const bool cut = resets && resets[e * resets_env + t * resets_step];
-        const float zc = on ? load1(z + t * s.z.step + col) * s.key_scale : 0.0f;
-        float sum = 0.0f;
-        for (uint32_t d = 0; d < s.a; ++d) {
-            float v = state[d * 64u + lane];
-            if (!s.reverse) v = cut ? 0.0f : __builtin_fmaf(v, decay, v * decay_rest);
-            v = __builtin_fmaf(load1(y + t * s.y.step + d), zc, v);
-            sum = __builtin_fmaf(load1(x + t * s.x.step + d), v, sum);
-            if (s.reverse) v = cut ? 0.0f : __builtin_fmaf(v, decay, v * decay_rest);
-            state[d * 64u + lane] = v;
+struct Frag;
+template <>
+struct Frag<__bf16> {
+    bf16x8 v;
+};
+template <>
+struct Frag<float> {
+    float v[8];
+};
+
+__device__ __forceinline__ f32x16 mma(const Frag<__bf16>& a, const Frag<__bf16>& b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(const Frag<float>& a, const Frag<float>& b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+    return c;
+}
+
+// From a row that lies along the summed axis: p = the row's run of 16 in LDS.
+__device__ __forceinline__ Frag<__bf16> along(const __bf16* p, uint32_t h) {
+    const bf16x4 lo = *reinterpret_cast<const bf16x4*>(p + 4 * h), hi = *reinterpret_cast<const bf16x4*>(p + 8 + 4 * h);
+    return {__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)};
+}
+__device__ __forceinline__ Frag<float> along(const float* p, uint32_t h) {
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(p + 4 * h), hi = *reinterpret_cast<const f32x4*>(p + 8 + 4 * h);
+    return {{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
+}
+
+// From 16 rows that lie across it: p = the first row's 32 columns in LDS, `stride` values from row to row; the lane's column is lane % 32.
+__device__ __forceinline__ Frag<__bf16> across(const __bf16* p, uint32_t stride, uint32_t lane) {
+    // The transposing read: lane i of 16 gives the address of four columns of row i / 4 and gets four rows of column i.
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const uint32_t h = lane >> 5, i = lane & 15u;
+    const __bf16* q = p + (4 * h + (i >> 2)) * stride + (lane & 16u) + 4 * (i & 3u);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + 8 * stride));
+    return {__builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7))};
+}
+__device__ __forceinline__ Frag<float> across(const float* p, uint32_t stride, uint32_t lane) {
+    const float* q = p + (4 * (lane >> 5)) * stride + (lane & 31u);
+    Frag<float> f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e] = q[(e & 3) * stride + (e >> 2) * 8 * stride];
+    return f;
+}
+
+__device__ __forceinline__ float value(const Frag<__bf16>& f, int e) { return (float)f.v[e]; }
+__device__ __forceinline__ float value(const Frag<float>& f, int e) { return f.v[e]; }
+
+// fp32 values as an operand: `kParts` bfloat16 operands whose sum they are, up to the rounding of the last, or as they are.
+template <class T, int kParts>
+struct Parts;
+template <int kParts>
+struct Parts<__bf16, kParts> {
+    Frag<__bf16> part[kParts];
+    __device__ __forceinline__ explicit Parts(const float (&f)[8]) {
+        float rest[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rest[e] = f[e];
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part[k].v[e] = (__bf16)rest[e];
+            if (k + 1 < kParts)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) rest[e] -= (float)part[k].v[e];
         }
-        if (on) store1(out + t * s.out.step + col, sum * s.out_scale);
     }
-    if (on && s.state_out)
-        for (uint32_t d = 0; d < s.a; ++d) s.state_out[base + (size_t)d * s.state_row + (size_t)col * s.state_col] = state[d * 64u + lane];
+    __device__ __forceinline__ f32x16 on_the_left(const Frag<__bf16>& b, f32x16 c) const {
+#pragma unroll
+        for (int k = kParts - 1; k >= 0; --k) c = mma(part[k], b, c);
+        return c;
+    }
+    __device__ __forceinline__ f32x16 on_the_right(const Frag<__bf16>& a, f32x16 c) const {
+#pragma unroll
+        for (int k = kParts - 1; k >= 0; --k) c = mma(a, part[k], c);
+        return c;
+    }
+};
+template <int kParts>
+struct Parts<float, kParts> {
+    Frag<float> all;
+    __device__ __forceinline__ explicit Parts(const float (&f)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) all.v[e] = f[e];
+    }
+    __device__ __forceinline__ f32x16 on_the_left(const Frag<float>& b, f32x16 c) const { return mma(all, b, c); }
+    __device__ __forceinline__ f32x16 on_the_right(const Frag<float>& a, f32x16 c) const { return mma(a, all, c); }
+};
+
+// ---- tiles of steps in LDS: rows of `width` values (a multiple of 32), 16 bytes apart from each other so that 16 rows' words at one column lie in
+// different banks
+
+template <class T>
+constexpr uint32_t kPad = 16 / sizeof(T);
+
+// The largest bit pattern of the values, without their signs: at or above infinity's where one is not finite.
+template <class T>
+__device__ __forceinline__ uint32_t magnitude(uint32_t most, uint32_t word) {
+    if constexpr (sizeof(T) == 4) return max(most, word & 0x7FFFFFFFu);
+    return max(most, max((word & 0x7FFFu) << 16, word & 0x7FFF0000u));
+}
+
+// `count` steps of `d` values from t (`step` apart in memory) to `rows` x `width`, zeros where there is nothing.
+template <class T, bool kCheck>
+__device__ __forceinline__ void stage(const T* from, int64_t step, uint32_t count, uint32_t d, T* tile, uint32_t rows, uint32_t width, uint32_t& most) {
+    constexpr uint32_t N = 16 / sizeof(T);
+    const uint32_t across = width / N;  // a power of two, or three of them
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < rows * across; i += blockDim.x) {
+        const uint32_t row = i / across, col = (i - row * across) * N;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (row < count) {
+            const T* p = from + (int64_t)row * step + col;
+            if (col + N <= d)
+                __builtin_memcpy(w, p, 16);
+            else if (col < d) {
+                T v[N];
+#pragma unroll
+                for (uint32_t e = 0; e < N; ++e) v[e] = col + e < d ? p[e] : (T)0.0f;
+                __builtin_memcpy(w, v, 16);
+            }
+        }
+        if (kCheck)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) most = magnitude<T>(most, w[k]);
+        *reinterpret_cast<uint4*>(tile + row * (width + kPad<T>) + col) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// Positions of a chunk up to and including i, as bits.
+__device__ __forceinline__ uint64_t up_to(uint32_t i) { return (2ull << i) - 1ull; }
+
+// A (a padded to 32, 64, 128 or 256), C steps of a chunk (32 or 64); kOut: outputs (else the state after a segment alone, from zeros).
+template <class T, int A, int C, bool kOut>
+__global__ __launch_bounds__(256) void scan_kernel(const Scans scans, const Cut cut, uint32_t roles, float* local0, float* local1,
+                                                   uint32_t* whole0, uint32_t* whole1) {
+    constexpr uint32_t kStrideA = A + kPad<T>;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h32 = lane >> 5, col32 = lane & 31u;
+    // Workgroups go to the eight dies in turn: those that read the same steps are eight apart, on one die and behind one L2.
+    const uint32_t per_die = cut.tiles * roles, group = blockIdx.x / (8u * per_die), in_group = blockIdx.x - group * 8u * per_die;
+    const uint32_t item = group * 8u + (in_group & 7u), part = in_group >> 3, tile = part / roles, role = part - tile * roles;
+    if (item >= cut.rows * (kOut ? cut.segments : cut.segments - 1u)) return;
+    const uint32_t seg = item / cut.rows, row = item - seg * cut.rows, env = row / cut.n_heads, head = row - env * cut.n_heads;
+    const Scan& s = scans.s[role];
+    if (tile * cut.waves * 32u >= s.b) return;  // (roles whose z is narrower)
+    const LinearAttentionHead& hd = cut.heads[head];
+    const uint32_t widthZ = cut.waves * 32u, strideZ = widthZ + kPad<T>, n0 = tile * widthZ, col = n0 + wave * 32u + col32;
+    T* ys = reinterpret_cast<T*>(lds);
+    T* zs = ys + C * kStrideA;
+    T* xs = zs + C * strideZ;
+    float* pw = reinterpret_cast<float*>(xs + (kOut ? C * kStrideA : 0));  // g^0 .. g^C
+    float* weight = pw + 80 + wave * 64u;                                 // a wavefront's g^(n-1-j)
+    uint32_t* flag = reinterpret_cast<uint32_t*>(pw + 80 + cut.waves * 64u);  // [2]
+    for (uint32_t i = threadIdx.x; i <= (uint32_t)C; i += blockDim.x) pw[i] = hd.power[i];
+    if (threadIdx.x < 2) flag[threadIdx.x] = 0;
+    __syncthreads();
+
+    // the factors of P in a tile on the diagonal and in the one beside it: position i of a lane's column, j of its rows
+    float near[kOut ? 16 : 1], far[kOut && C == 64 ? 16 : 1];
+    if (kOut)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const uint32_t j = (r & 3) + 8 * (r >> 2) + 4 * h32, i = col32;
+            near[r] = s.key_scale * (s.reverse ? (j >= i ? pw[j - i] : 0.0f) : (i >= j ? pw[i - j] : 0.0f));
+            if (C == 64) far[C == 64 ? r : 0] = s.key_scale * (s.reverse ? pw[32 + j - i] : pw[32 + i - j]);
+        }
+
+    f32x16 state[A / 32];
+    const size_t cells = (size_t)s.a * s.b;
+    const float* from = kOut ? (seg ? s.before + ((size_t)(seg - 1u) * cut.rows + row) * cells : s.state_in ? s.state_in + row * cells : nullptr) : nullptr;
+#pragma unroll
+    for (int db = 0; db < A / 32; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
+            state[db][r] = from && d < s.a && col < s.b ? from[d * s.state_row + col * s.state_col] : 0.0f;
+        }
+
+    const T *xh = head_of<const T>(s.x, env, head), *yh = head_of<const T>(s.y, env, head), *zh = head_of<const T>(s.z, env, head) + n0;
+    T* oh = head_of<T>(s.out, env, head);
+    const uint8_t* resets = cut.resets ? cut.resets + (int64_t)env * cut.resets_env : nullptr;
+    const uint32_t widthB = min(s.b - n0, widthZ);
+    // the segment's steps in the order in which they are taken; in reverse, position p of the scan is step n_steps - 1 - p
+    const uint32_t begin = seg * cut.seg_steps, end = min(begin + cut.seg_steps, cut.n_steps);
+    uint32_t singles = 0, turn = 0;  // steps still to be taken one by one
+    bool uncut = true;
+    for (uint32_t at = begin; at < end;) {
+        const uint32_t n = singles ? 1u : min((uint32_t)C, end - at);
+        const int64_t t = s.reverse ? (int64_t)(cut.n_steps - at - n) : (int64_t)at;  // the chunk's first step in memory
+        uint32_t most = 0, unused = 0;
+        const bool begins = resets && lane < n && resets[(t + lane) * cut.resets_step] != 0;
+        stage<T, true>(yh + t * s.y.step, s.y.step, n, s.a, ys, C, A, most);
+        stage<T, true>(zh + t * s.z.step, s.z.step, n, widthB, zs, C, widthZ, most);
+        if (kOut) stage<T, false>(xh + t * s.x.step, s.x.step, n, s.a, xs, C, A, unused);
+        if (most >= 0x7F800000u) flag[turn & 1u] = 1;
+        const uint64_t m = __ballot(begins);
+        __syncthreads();
+        const bool broken = flag[turn & 1u] != 0;
+        if (threadIdx.x == 0) flag[(turn + 1u) & 1u] = 0;
+        ++turn;
+        if (broken && n > 1) {
+            singles = n;
+            __syncthreads();
+            continue;
+        }
+        // the first episode boundary after, and the last one up to, each position of the chunk
+        const uint64_t later = m & ~up_to(lane), earlier = m & up_to(lane);
+        const bool out_of = s.reverse ? earlier == 0 : later == 0;  // what position `lane` adds to the state stays in it
+        weight[lane] = lane < n && out_of ? s.key_scale * pw[s.reverse ? lane + 1u : n - 1u - lane] : 0.0f;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+
+        if constexpr (kOut) {
+            f32x16 acc[C / 32];
+#pragma unroll
+            for (int ib = 0; ib < C / 32; ++ib)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[ib][r] = 0.0f;
+            // out^T = S^T x^T, columns = steps
+#pragma unroll
+            for (int db = 0; db < A / 32; ++db)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float f[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] = state[db][8 * k + e];
+                    const Parts<T, 2> sp(f);
+#pragma unroll
+                    for (int ib = 0; ib < C / 32; ++ib) acc[ib] = sp.on_the_left(along(xs + (ib * 32 + col32) * kStrideA + db * 32 + k * 16, h32), acc[ib]);
+                }
+#pragma unroll
+            for (int ib = 0; ib < C / 32; ++ib) {
+                const uint32_t i = ib * 32 + col32;
+                const bool into = s.reverse ? (m & ~up_to(i)) == 0 : (m & up_to(i)) == 0;
+                const float f = pw[s.reverse ? (i < n ? n - 1u - i : 0u) : i + 1u];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[ib][r] = into ? acc[ib][r] * f : 0.0f;
+            }
+            // out^T += z^T P^T, tile by tile of P
+            const auto tile_of_p = [&](uint32_t ib, uint32_t jb, const float(&factor)[16], f32x16 c) {
+                f32x16 p;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < A / 16; ++k) p = mma(along(ys + (jb * 32 + col32) * kStrideA + k * 16, h32), along(xs + (ib * 32 + col32) * kStrideA + k * 16, h32), p);
+                // the positions that reach i: [first, first + many)
+                const uint32_t i = ib * 32 + col32;
+                const uint64_t upto = m & up_to(i), after = m & ~up_to(i);
+                const uint32_t first = s.reverse ? i : upto ? 63u - (uint32_t)__builtin_clzll(upto) : 0u;
+                const uint32_t past = s.reverse ? (after ? (uint32_t)__builtin_ctzll(after) : 64u) : i + 1u;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float f[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int r = 8 * k + e;
+                        const uint32_t j = jb * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
+                        f[e] = j - first < past - first ? p[r] * factor[r] : 0.0f;
+                    }
+                    c = Parts<T, 2>(f).on_the_right(across(zs + (jb * 32 + k * 16) * strideZ + wave * 32u, strideZ, lane), c);
+                }
+                return c;
+            };
+#pragma unroll
+            for (int ib = 0; ib < C / 32; ++ib) acc[ib] = tile_of_p(ib, ib, near, acc[ib]);
+            if constexpr (C == 64) {
+                f32x16 beside;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) beside[r] = 0.0f;
+                beside = tile_of_p(s.reverse ? 0u : 1u, s.reverse ? 1u : 0u, far, beside);
+                if (s.reverse)
+                    acc[0] += beside;
+                else
+                    acc[1] += beside;
+            }
+#pragma unroll
+            for (int ib = 0; ib < C / 32; ++ib) {
+                const uint32_t i = ib * 32 + col32;
+                if (i < n) {
+                    T* o = oh + (t + i) * s.out.step;
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4) {
+                        const uint32_t c = n0 + wave * 32u + 2 * r + 4 * h32;
+                        T v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = (T)(acc[ib][r + e] * s.out_scale);
+                        if (c + 4 <= s.b)
+                            __builtin_memcpy(o + c, v, sizeof(v));
+                        else
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (c + e < s.b) o[c + e] = v[e];
+                    }
+                }
+            }
+        }
+
+        // S <- g^n S + y^T (weights z)
+        uncut = uncut && m == 0;
+        const float keep = n == (uint32_t)C ? hd.decay_chunk[C / 32 - 1] : n == 1u ? hd.decay : pw[n];
+        const float keep_rest = n == (uint32_t)C ? hd.decay_chunk_rest[C / 32 - 1] : n == 1u ? hd.decay_rest : 0.0f;
+#pragma unroll
+        for (int db = 0; db < A / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) state[db][r] = m == 0 ? __builtin_fmaf(state[db][r], keep, state[db][r] * keep_rest) : 0.0f;
+#pragma unroll
+        for (int k = 0; k < C / 16; ++k) {
+            const Frag<T> z = across(zs + k * 16 * strideZ + wave * 32u, strideZ, lane);
+            const f32x4 w0 = *reinterpret_cast<const f32x4*>(weight + k * 16 + 4 * h32), w1 = *reinterpret_cast<const f32x4*>(weight + k * 16 + 8 + 4 * h32);
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = value(z, e) * (e < 4 ? w0[e & 3] : w1[e & 3]);
+            const Parts<T, 3> zp(f);
+#pragma unroll
+            for (int db = 0; db < A / 32; ++db) state[db] = zp.on_the_right(across(ys + k * 16 * kStrideA + db * 32, kStrideA, lane), state[db]);
+        }
+        __syncthreads();
+        at += n;
+        if (singles) --singles;
+    }
+
+    float* to = kOut ? (seg + 1u == cut.segments && s.state_out ? s.state_out + row * cells : nullptr)
+                     : (role ? local1 : local0) + ((size_t)seg * cut.rows + row) * cells;
+    if (to)
+#pragma unroll
+        for (int db = 0; db < A / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
+                if (d < s.a && col < s.b) to[d * s.state_row + col * s.state_col] = state[db][r];
+            }
+    if (!kOut && tile == 0 && threadIdx.x == 0) (role ? whole1 : whole0)[seg * cut.rows + row] = uncut ? 1u : 0u;
+}
+
+// The segments' own states, one after the other, to the states before the segments that follow: one lane per cell of a state.
+__global__ __launch_bounds__(256) void join_kernel(const Cut cut, uint32_t cells, const float* in0, const float* in1, float* local0, float* local1,
+                                                   const uint32_t* whole0, const uint32_t* whole1) {
+    const uint32_t i = blockIdx.x * 256u + threadIdx.x, row = blockIdx.y;
+    if (i >= cells) return;
+    const float* in = blockIdx.z ? in1 : in0;
+    float* local = blockIdx.z ? local1 : local0;
+    const uint32_t* whole = blockIdx.z ? whole1 : whole0;
+    const double g = exp(cut.heads[row % cut.n_heads].log_decay * (double)cut.seg_steps);
+    const float keep = (float)g, rest = (float)(g - (double)keep);
+    float v = in ? in[(size_t)row * cells + i] : 0.0f;
+    for (uint32_t k = 0; k + 1u < cut.segments; ++k) {
+        float* p = local + ((size_t)k * cut.rows + row) * cells + i;
+        v = *p + (whole[(size_t)k * cut.rows + row] ? __builtin_fmaf(v, keep, v * rest) : 0.0f);
+        *p = v;
+    }
 }
 
 // One step of every environment: four wavefronts per (environment, head) and 64 columns, rows dealt to the wavefronts.
@@ -105,32 +469,147 @@ int launched(std::string& err) {
     return PXR_ERR_DEVICE;
 }
 
-void enqueue(const LinearAttentionConsts& c, const pxr_rollout& r, const Scan& s, hipStream_t st) {
-    const dim3 grid(r.n_envs * c.n_heads, (s.b + 63u) / 64u);
-    const size_t lds = (size_t)s.a * 64u * 4u;
-    if (r.dtype == PXR_F32)
-        hipLaunchKernelGGL((scan_kernel<float>), grid, dim3(64), lds, st, s, c.heads, c.n_heads, r.n_steps, r.d_resets, r.resets_env, r.resets_step);
+// Chunks: 64 steps in bfloat16 (32 where the rollout has no more), 32 in fp32, whose products cost 16 times as much and of which a shorter
+// chunk has fewer.
+uint32_t chunk_of(uint32_t dtype, uint32_t n_steps) { return dtype == PXR_BF16 && n_steps > 32u ? 64u : 32u; }
+
+uint32_t waves_of(uint32_t b) { return b <= 32u ? 1u : b <= 64u ? 2u : 4u; }
+
+// Segments of a rollout's steps: as many as it takes to give each compute unit two workgroups, of four chunks at least.
+uint32_t segments_of(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, uint32_t roles, uint32_t* seg_steps) {
+    const uint32_t C = chunk_of(dtype, n_steps);
+    const uint64_t chunks = ((uint64_t)n_steps + C - 1u) / C, rows = (uint64_t)n_envs * c.n_heads * roles;
+    uint64_t want = 2ull * c.n_cus / rows;
+    if (want > chunks / 4u) want = chunks / 4u;
+    if (want < 2u) {
+        *seg_steps = n_steps;
+        return 1u;
+    }
+    const uint64_t each = (chunks + want - 1u) / want;
+    *seg_steps = (uint32_t)(each * C);
+    return (uint32_t)((chunks + each - 1u) / each);
+}
+
+// Chunks of 256 values take more than the 64 KB of LDS that a launch has by default.
+template <class T, int C>
+hipError_t allow_lds() {
+    const void* fns[2] = {reinterpret_cast<const void*>(&scan_kernel<T, 256, C, true>), reinterpret_cast<const void*>(&scan_kernel<T, 256, C, false>)};
+    for (const void* f : fns)
+        if (const hipError_t rc = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); rc != hipSuccess) return rc;
+    return hipSuccess;
+}
+
+template <class T, int C, bool kOut>
+void enqueue_as(const Scan* s, uint32_t roles, const Cut& cut, float* const* local, uint32_t* const* whole, hipStream_t st) {
+    uint32_t a = 0;
+    for (uint32_t i = 0; i < roles; ++i) a = s[i].a > a ? s[i].a : a;
+    const uint32_t A = a <= 32u ? 32u : a <= 64u ? 64u : a <= 128u ? 128u : 256u;
+    const uint32_t items = cut.rows * (kOut ? cut.segments : cut.segments - 1u);
+    const dim3 grid((items + 7u) / 8u * 8u * cut.tiles * roles), block(cut.waves * 64u);
+    const size_t lds = (size_t)C * ((kOut ? 2u : 1u) * (A + kPad<T>) + cut.waves * 32u + kPad<T>) * sizeof(T) + (80u + cut.waves * 64u + 2u) * 4u;
+    const Scans scans{{s[0], s[roles > 1 ? 1 : 0], s[roles > 2 ? 2 : 0]}};
+#define PXR_SCAN(AA) \
+    hipLaunchKernelGGL((scan_kernel<T, AA, C, kOut>), grid, block, lds, st, scans, cut, roles, local[0], local[1], whole[0], whole[1])
+    if (A == 32u)
+        PXR_SCAN(32);
+    else if (A == 64u)
+        PXR_SCAN(64);
+    else if (A == 128u)
+        PXR_SCAN(128);
     else
-        hipLaunchKernelGGL((scan_kernel<__bf16>), grid, dim3(64), lds, st, s, c.heads, c.n_heads, r.n_steps, r.d_resets, r.resets_env, r.resets_step);
+        PXR_SCAN(256);
+#undef PXR_SCAN
+}
+
+template <bool kOut>
+void enqueue(uint32_t dtype, const Scan* s, uint32_t roles, const Cut& cut, float* const* local, uint32_t* const* whole, hipStream_t st) {
+    if (dtype == PXR_F32)
+        enqueue_as<float, 32, kOut>(s, roles, cut, local, whole, st);
+    else if (chunk_of(dtype, cut.n_steps) == 32u)
+        enqueue_as<__bf16, 32, kOut>(s, roles, cut, local, whole, st);
+    else
+        enqueue_as<__bf16, 64, kOut>(s, roles, cut, local, whole, st);
+}
+
+Cut cut_of(const LinearAttentionConsts& c, const pxr_rollout& r, uint32_t roles, uint32_t b) {
+    Cut cut{};
+    cut.n_heads = c.n_heads;
+    cut.rows = r.n_envs * c.n_heads;
+    cut.n_steps = r.n_steps;
+    cut.segments = segments_of(c, r.dtype, r.n_envs, r.n_steps, roles, &cut.seg_steps);
+    cut.waves = waves_of(b);
+    cut.tiles = (b + cut.waves * 32u - 1u) / (cut.waves * 32u);
+    cut.heads = c.heads;
+    cut.resets = r.d_resets;
+    cut.resets_env = r.resets_env;
+    cut.resets_step = r.resets_step;
+    return cut;
+}
+
+// Bytes of one set of segments' states, and of the words beside them.
+size_t state_bytes(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t segments) {
+    return (size_t)(segments - 1u) * n_envs * c.n_heads * c.dk * c.dv * 4u;
+}
+size_t whole_bytes(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t segments) {
+    return ((size_t)(segments - 1u) * n_envs * c.n_heads * 4u + 15u) & ~(size_t)15u;
 }
 
 }  // namespace
 
-size_t linear_attention_workspace(const LinearAttentionConsts&, uint32_t, uint32_t, uint32_t, bool) { return 0; }
+int prepare_linear_attention_kernels(std::string& err) {
+    hipError_t rc = allow_lds<float, 32>();
+    if (rc == hipSuccess) rc = allow_lds<__bf16, 32>();
+    if (rc == hipSuccess) rc = allow_lds<__bf16, 64>();
+    if (rc == hipSuccess) return PXR_OK;
+    err = std::string("hipFuncSetAttribute(MaxDynamicSharedMemorySize) failed: ") + hipGetErrorString(rc);
+    return PXR_ERR_DEVICE;
+}
 
-int launch_linear_attention_forward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& out, float* state_out, void*,
+size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, bool backward) {
+    uint32_t steps;
+    const uint32_t segments = segments_of(c, dtype, n_envs, n_steps, backward ? 3u : 1u, &steps);
+    const size_t one = ((state_bytes(c, n_envs, segments) + 15u) & ~(size_t)15u) + whole_bytes(c, n_envs, segments);
+    return backward ? 2u * one : one;
+}
+
+int launch_linear_attention_forward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& out, float* state_out, void* ws,
                                     void* stream, std::string& err) {
-    enqueue(c, r, Scan{r.q, r.k, r.v, out, c.dk, c.dv, r.d_state, state_out, c.dv, 1u, c.scale, 1.0f, 0u}, reinterpret_cast<hipStream_t>(stream));
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    const Cut cut = cut_of(c, r, 1u, c.dv);
+    Scan s{r.q, r.k, r.v, out, c.dk, c.dv, r.d_state, state_out, c.dv, 1u, nullptr, c.scale, 1.0f, 0u};
+    float* local[2] = {static_cast<float*>(ws), nullptr};
+    uint32_t* whole[2] = {reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + ((state_bytes(c, r.n_envs, cut.segments) + 15u) & ~(size_t)15u)), nullptr};
+    if (cut.segments > 1u) {
+        enqueue<false>(r.dtype, &s, 1u, cut, local, whole, st);
+        hipLaunchKernelGGL(join_kernel, dim3((c.dk * c.dv + 255u) / 256u, cut.rows, 1), dim3(256), 0, st, cut, c.dk * c.dv, r.d_state, nullptr, local[0], nullptr,
+                           whole[0], nullptr);
+        s.before = local[0];
+    }
+    enqueue<true>(r.dtype, &s, 1u, cut, local, whole, st);
     return launched(err);
 }
 
 int launch_linear_attention_backward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& dout, const float* dstate_out,
-                                     const pxr_tokens& dq, const pxr_tokens& dk, const pxr_tokens& dv, float* dstate, void*,
+                                     const pxr_tokens& dq, const pxr_tokens& dk, const pxr_tokens& dv, float* dstate, void* ws,
                                      void* stream, std::string& err) {
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    enqueue(c, r, Scan{dout, r.v, r.k, dq, c.dv, c.dk, r.d_state, nullptr, 1u, c.dv, c.scale, 1.0f, 0u}, st);
-    enqueue(c, r, Scan{r.v, dout, r.q, dk, c.dv, c.dk, dstate_out, nullptr, 1u, c.dv, 1.0f, c.scale, 1u}, st);
-    enqueue(c, r, Scan{r.k, r.q, dout, dv, c.dk, c.dv, dstate_out, dstate, c.dv, 1u, 1.0f, c.scale, 1u}, st);
+    const Cut cut = cut_of(c, r, 3u, c.dk > c.dv ? c.dk : c.dv);
+    const size_t states = (state_bytes(c, r.n_envs, cut.segments) + 15u) & ~(size_t)15u, words = whole_bytes(c, r.n_envs, cut.segments);
+    char* w = static_cast<char*>(ws);
+    float* local[2] = {reinterpret_cast<float*>(w), reinterpret_cast<float*>(w + states + words)};
+    uint32_t* whole[2] = {reinterpret_cast<uint32_t*>(w + states), reinterpret_cast<uint32_t*>(w + 2u * states + words)};
+    if (cut.segments > 1u) {
+        // the states [dk][dv] of the forward scan and of the reverse one, which dk and dv share
+        const Scan both[2] = {Scan{r.q, r.k, r.v, dout, c.dk, c.dv, nullptr, nullptr, c.dv, 1u, nullptr, 1.0f, 1.0f, 0u},
+                              Scan{r.k, r.q, dout, dout, c.dk, c.dv, nullptr, nullptr, c.dv, 1u, nullptr, 1.0f, c.scale, 1u}};
+        enqueue<false>(r.dtype, both, 2u, cut_of(c, r, 3u, c.dv), local, whole, st);
+        hipLaunchKernelGGL(join_kernel, dim3((c.dk * c.dv + 255u) / 256u, cut.rows, 2), dim3(256), 0, st, cut, c.dk * c.dv, r.d_state, dstate_out, local[0],
+                           local[1], whole[0], whole[1]);
+    }
+    const Scan three[3] = {Scan{dout, r.v, r.k, dq, c.dv, c.dk, r.d_state, nullptr, 1u, c.dv, local[0], c.scale, 1.0f, 0u},
+                           Scan{r.v, dout, r.q, dk, c.dv, c.dk, dstate_out, nullptr, 1u, c.dv, local[1], 1.0f, c.scale, 1u},
+                           Scan{r.k, r.q, dout, dv, c.dk, c.dv, dstate_out, dstate, c.dv, 1u, local[1], 1.0f, c.scale, 1u}};
+    enqueue<true>(r.dtype, three, 3u, cut, local, whole, st);
     return launched(err);
 }
 

@@ -28,11 +28,12 @@ const char* wrong_norm(const pxr_layer_norm_desc* d, bool backward) {
     return nullptr;
 }
 
-// A rollout's own arguments; `inputs`: the views that are read.
+// A rollout's own arguments.
 const char* wrong_rollout(const pxr_linear_attention* a, const pxr_rollout* r, bool step) {
     if (!a || !r) return "null argument";
     if (r->dtype > PXR_BF16) return "dtype must be fp32 or bfloat16";
-    if (r->n_envs == 0 || (uint64_t)r->n_envs * a->c.n_heads > 0x7FFFFFFFull) return "n_envs must be positive and n_envs * n_heads below 2^31";
+    // (a launch counts its threads in 32 bits: 2^21 rows are 3 gradients x 2 tiles x 256 threads of them)
+    if (r->n_envs == 0 || (uint64_t)r->n_envs * a->c.n_heads > (1u << 21)) return "n_envs must be positive and n_envs * n_heads at most 2^21";
     if (r->n_steps > 0x7FFFFFFFu) return "n_steps must be below 2^31";
     if (step && r->n_steps != 1) return "n_steps must be 1";
     if (!aligned(r->d_state, 4)) return "the state must be 4-byte aligned";
@@ -119,10 +120,11 @@ int pxr_linear_attention_create(const pxr_linear_attention_desc* d, pxr_linear_a
     if (rc == hipSuccess) rc = hipGetDevice(&dev);
     if (rc == hipSuccess) rc = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
     delete[] heads;
-    if (rc != hipSuccess) {
+    std::string err;
+    if (rc != hipSuccess || pxr::prepare_linear_attention_kernels(err) != PXR_OK) {
         (void)hipFree(table);
         delete a;
-        return set_error(oom ? PXR_ERR_OOM : PXR_ERR_DEVICE, std::string(call) + ": " + hipGetErrorString(rc));
+        return set_error(oom ? PXR_ERR_OOM : PXR_ERR_DEVICE, std::string(call) + ": " + (rc != hipSuccess ? hipGetErrorString(rc) : err.c_str()));
     }
     a->c.heads = static_cast<const pxr::LinearAttentionHead*>(table);
     a->c.n_cus = (uint32_t)cus;
@@ -140,7 +142,8 @@ int pxr_linear_attention_destroy(pxr_linear_attention* a) {
 
 int pxr_linear_attention_workspace(const pxr_linear_attention* a, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, uint32_t backward,
                                    size_t* bytes) {
-    if (!a || !bytes || n_envs == 0 || dtype > PXR_BF16) return refuse("pxr_linear_attention_workspace", "null argument, no environments or a dtype that is none");
+    if (!a || !bytes || n_envs == 0 || (uint64_t)n_envs * a->c.n_heads > (1u << 21) || n_steps > 0x7FFFFFFFu || dtype > PXR_BF16)
+        return refuse("pxr_linear_attention_workspace", "null argument, no or too many environments or steps, or a dtype that is none");
     *bytes = pxr::linear_attention_workspace(a->c, dtype, n_envs, n_steps, backward != 0);
     return PXR_OK;
 }
@@ -190,8 +193,12 @@ int pxr_linear_attention_step(pxr_linear_attention* a, const pxr_rollout* r, flo
 }  // extern "C"
 
 void pxr::fill_head(LinearAttentionHead& h, float log_decay) {
+    const auto split = [](double g, float& head, float& rest) {
+        head = (float)g;
+        rest = (float)(g - (double)head);
+    };
     h.log_decay = (double)log_decay;
-    const double g = std::exp((double)log_decay);
-    h.decay = (float)g;
-    h.decay_rest = (float)(g - (double)h.decay);
+    split(std::exp((double)log_decay), h.decay, h.decay_rest);
+    for (int k = 0; k < 2; ++k) split(std::exp((double)log_decay * (32.0 * (k + 1))), h.decay_chunk[k], h.decay_chunk_rest[k]);
+    for (int n = 0; n <= 64; ++n) h.power[n] = (float)std::exp((double)log_decay * n);
 }
