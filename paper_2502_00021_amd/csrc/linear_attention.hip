@@ -8,7 +8,7 @@
 //   dk and dv are scans from the last step to the first, of (v, do, q) and of (k, q, do): their state
 //     R_t = scale q_t do_t^T + (t + 1 begins an episode ? 0 : g R_{t+1}) gives dk_t = R_t v_t, dv_t = R_t^T k_t.
 //
-// A scan takes C steps at a time.  With positions i, j in such a chunk, S the state before it and n of its steps there:
+// A scan takes C = 32 steps at a time.  With positions i, j in such a chunk, S the state before it and n of its steps there:
 //   P_ij = g^(i-j) key_scale (x_i . y_j) where j <= i and no episode begins in (j, i], else 0
 //   out_i = out_scale (sum_j P_ij z_j + [no episode begins up to i] g^(i+1) S^T x_i)
 //   S <- [no episode begins] g^n S + sum_j [no episode begins after j] g^(n-1-j) key_scale y_j z_j^T
@@ -34,10 +34,15 @@
 namespace pxr {
 namespace {
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ float load1(const float* p) { return *p; }
@@ -61,10 +66,12 @@ struct Scans {
     Scan s[3];
 };
 
+constexpr int C = 32;  // steps of a chunk
+
 // How the steps are cut: a workgroup takes one segment of one (environment, head) and 32 columns a wavefront.
 struct Cut {
     uint32_t n_heads, rows, n_steps;  // rows = environments * heads
-    uint32_t segments, seg_steps, tiles, waves;
+    uint32_t segments, seg_steps, tiles, waves, width;  // width: a's, padded
     const LinearAttentionHead* heads;
     const uint8_t* resets;
     int64_t resets_env, resets_step;
@@ -85,7 +92,7 @@ struct Frag<__bf16> {
 };
 template <>
 struct Frag<float> {
-    float v[8];
+    f32x8 v;
 };
 
 __device__ __forceinline__ f32x16 mma(const Frag<__bf16>& a, const Frag<__bf16>& b, f32x16 c) {
@@ -104,7 +111,7 @@ __device__ __forceinline__ Frag<__bf16> along(const __bf16* p, uint32_t h) {
 }
 __device__ __forceinline__ Frag<float> along(const float* p, uint32_t h) {
     const f32x4 lo = *reinterpret_cast<const f32x4*>(p + 4 * h), hi = *reinterpret_cast<const f32x4*>(p + 8 + 4 * h);
-    return {{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
+    return {__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)};
 }
 
 // From 16 rows that lie across it: p = the first row's 32 columns in LDS, `stride` values from row to row; the lane's column is lane % 32.
@@ -125,8 +132,24 @@ __device__ __forceinline__ Frag<float> across(const float* p, uint32_t stride, u
     return f;
 }
 
-__device__ __forceinline__ float value(const Frag<__bf16>& f, int e) { return (float)f.v[e]; }
-__device__ __forceinline__ float value(const Frag<float>& f, int e) { return f.v[e]; }
+__device__ __forceinline__ f32x8 values(const Frag<__bf16>& f) {
+    const u32x4 w = __builtin_bit_cast(u32x4, f.v);
+    f32x8 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+    return v;
+}
+__device__ __forceinline__ f32x8 values(const Frag<float>& f) { return f.v; }
+// Half of a product's result in a lane, which is a run of 16 of its rows.
+__device__ __forceinline__ f32x8 half(const f32x16& c, int k) {
+    return k ? __builtin_shufflevector(c, c, 8, 9, 10, 11, 12, 13, 14, 15) : __builtin_shufflevector(c, c, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ f32x8 eight(const float* lo, const float* hi) {
+    return __builtin_shufflevector(*reinterpret_cast<const f32x4*>(lo), *reinterpret_cast<const f32x4*>(hi), 0, 1, 2, 3, 4, 5, 6, 7);
+}
 
 // fp32 values as an operand: `kParts` bfloat16 operands whose sum they are, up to the rounding of the last, or as they are.
 template <class T, int kParts>
@@ -134,17 +157,19 @@ struct Parts;
 template <int kParts>
 struct Parts<__bf16, kParts> {
     Frag<__bf16> part[kParts];
-    __device__ __forceinline__ explicit Parts(const float (&f)[8]) {
-        float rest[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) rest[e] = f[e];
+    __device__ __forceinline__ explicit Parts(f32x8 rest) {
 #pragma unroll
         for (int k = 0; k < kParts; ++k) {
+            u32x4 w;  // (two values an instruction: conversions of eight at once come out one by one)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) part[k].v[e] = (__bf16)rest[e];
-            if (k + 1 < kParts)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) rest[e] -= (float)part[k].v[e];
+            for (int i = 0; i < 4; ++i) {
+                w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{rest[2 * i], rest[2 * i + 1]}, bf16x2));  // round to nearest even
+                if (k + 1 < kParts) {
+                    rest[2 * i] -= __uint_as_float(w[i] << 16);
+                    rest[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+                }
+            }
+            part[k].v = __builtin_bit_cast(bf16x8, w);
         }
     }
     __device__ __forceinline__ f32x16 on_the_left(const Frag<__bf16>& b, f32x16 c) const {
@@ -161,10 +186,7 @@ struct Parts<__bf16, kParts> {
 template <int kParts>
 struct Parts<float, kParts> {
     Frag<float> all;
-    __device__ __forceinline__ explicit Parts(const float (&f)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) all.v[e] = f[e];
-    }
+    __device__ __forceinline__ explicit Parts(f32x8 f) : all{f} {}
     __device__ __forceinline__ f32x16 on_the_left(const Frag<float>& b, f32x16 c) const { return mma(all, b, c); }
     __device__ __forceinline__ f32x16 on_the_right(const Frag<float>& a, f32x16 c) const { return mma(a, all, c); }
 };
@@ -175,48 +197,98 @@ struct Parts<float, kParts> {
 template <class T>
 constexpr uint32_t kPad = 16 / sizeof(T);
 
-// The largest bit pattern of the values, without their signs: at or above infinity's where one is not finite.
+// The largest bit patterns of the values, without their signs.
 template <class T>
-__device__ __forceinline__ uint32_t magnitude(uint32_t most, uint32_t word) {
-    if constexpr (sizeof(T) == 4) return max(most, word & 0x7FFFFFFFu);
-    return max(most, max((word & 0x7FFFu) << 16, word & 0x7FFF0000u));
-}
+struct Most;
+template <>
+struct Most<float> {
+    uint32_t m = 0;
+    __device__ __forceinline__ void with(uint32_t w) { m = max(m, w & 0x7FFFFFFFu); }
+    __device__ __forceinline__ bool infinite() const { return m >= 0x7F800000u; }
+};
+template <>
+struct Most<__bf16> {
+    u16x2 m = {0, 0};
+    __device__ __forceinline__ void with(uint32_t w) { m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)); }
+    __device__ __forceinline__ bool infinite() const { return max(m[0], m[1]) >= 0x7F80u; }
+};
 
-// `count` steps of `d` values from t (`step` apart in memory) to `rows` x `width`, zeros where there is nothing.
-template <class T, bool kCheck>
-__device__ __forceinline__ void stage(const T* from, int64_t step, uint32_t count, uint32_t d, T* tile, uint32_t rows, uint32_t width, uint32_t& most) {
-    constexpr uint32_t N = 16 / sizeof(T);
-    const uint32_t across = width / N;  // a power of two, or three of them
-#pragma unroll 4
-    for (uint32_t i = threadIdx.x; i < rows * across; i += blockDim.x) {
-        const uint32_t row = i / across, col = (i - row * across) * N;
-        uint32_t w[4] = {0, 0, 0, 0};
-        if (row < count) {
-            const T* p = from + (int64_t)row * step + col;
-            if (col + N <= d)
-                __builtin_memcpy(w, p, 16);
-            else if (col < d) {
-                T v[N];
+// A chunk's steps on their way to a tile: C rows of `kWidth` values, dealt to kThreads lanes in vectors of 16 bytes.  The requests of a chunk go out
+// together, a chunk ahead.  Rows may begin at any element (the memory takes 16-byte requests at any address).  A row of d values that ends inside a
+// vector has its last vector moved back to its end; rows past the last and vectors past a row's end read what is there instead and are not written,
+// or written as zeros.  The columns past d are zero from the start and nothing writes them.  Rows shorter than a vector are read value by value,
+// when they are written.
+template <class T, int kWidth, int kThreads>
+struct Steps {
+    static constexpr uint32_t N = 16 / sizeof(T), kPerRow = kWidth / N, kCount = (C * kPerRow + kThreads - 1) / kThreads, kStride = kWidth + kPad<T>;
+    static constexpr uint32_t kRowsEach = kThreads / kPerRow;  // rows that the lanes take together
+    static_assert(kThreads % kPerRow == 0);
+    uint32_t row, col, d;
+    int64_t step, offset;  // values from row to row; the lane's first vector from the chunk's first value
+    uint4 v[kCount];
+
+    __device__ __forceinline__ Steps(int64_t step, uint32_t d) : row(threadIdx.x / kPerRow), col(threadIdx.x % kPerRow * N), d(d), step(step) {
+        offset = (int64_t)row * step + (d < N ? 0u : min(col, d - N));
+    }
+    // n >= 1 rows
+    __device__ __forceinline__ void ask(const T* from, uint32_t n) {
+        if (d < N) return;
 #pragma unroll
-                for (uint32_t e = 0; e < N; ++e) v[e] = col + e < d ? p[e] : (T)0.0f;
-                __builtin_memcpy(w, v, 16);
+        for (uint32_t i = 0; i < kCount; ++i) {
+            const T* p = from + (int64_t)(i * kRowsEach) * step + offset;
+            if (n < (uint32_t)C && row + i * kRowsEach >= n) p = from + min(col, d - N);
+            __builtin_memcpy(&v[i], p, 16);
+        }
+    }
+    // The tile's rows past n are zeros.  kCheck: collects bit patterns.
+    template <bool kCheck>
+    __device__ __forceinline__ void put(const T* from, T* tile, uint32_t n, Most<T>& most) {
+        if (d < N) {
+            for (uint32_t i = threadIdx.x; i < C * d; i += kThreads) {
+                const uint32_t r = i / d, c = i - r * d;
+                const T e = r < n ? from[(int64_t)r * step + c] : (T)0.0f;
+                if (kCheck) most.with(sizeof(T) == 4 ? __builtin_bit_cast(uint32_t, (float)e) : __builtin_bit_cast(uint32_t, (float)e) >> 16);
+                tile[r * kStride + c] = e;
+            }
+            return;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kCount; ++i) {
+            const uint32_t r = row + i * kRowsEach;
+            if (C * kPerRow % kThreads && r >= (uint32_t)C) continue;
+            uint4 w = v[i];
+            if (n < (uint32_t)C && r >= n) w = make_uint4(0, 0, 0, 0);
+            if (kCheck) {
+                most.with(w.x);
+                most.with(w.y);
+                most.with(w.z);
+                most.with(w.w);
+            }
+            if (col + N <= d) {
+                *reinterpret_cast<uint4*>(tile + r * kStride + col) = w;
+            } else if (col < d) {
+                T e[N];
+                __builtin_memcpy(e, &w, 16);
+#pragma unroll
+                for (uint32_t k = 0; k < N; ++k) tile[r * kStride + d - N + k] = e[k];
             }
         }
-        if (kCheck)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) most = magnitude<T>(most, w[k]);
-        *reinterpret_cast<uint4*>(tile + row * (width + kPad<T>) + col) = make_uint4(w[0], w[1], w[2], w[3]);
     }
-}
+};
+
+// Nothing moves across: the compiler would otherwise begin the LDS reads of all products at once, and hold what they bring.
+__device__ __forceinline__ void part_of_chunk() { __builtin_amdgcn_sched_barrier(0); }
 
 // Positions of a chunk up to and including i, as bits.
 __device__ __forceinline__ uint64_t up_to(uint32_t i) { return (2ull << i) - 1ull; }
 
-// A (a padded to 32, 64, 128 or 256), C steps of a chunk (32 or 64); kOut: outputs (else the state after a segment alone, from zeros).
-template <class T, int A, int C, bool kOut>
-__global__ __launch_bounds__(256) void scan_kernel(const Scans scans, const Cut cut, uint32_t roles, float* local0, float* local1,
-                                                   uint32_t* whole0, uint32_t* whole1) {
-    constexpr uint32_t kStrideA = A + kPad<T>;
+// A (a padded to 32, 64, 128 or 256), kWaves wavefronts; kOut: outputs (else the state after a segment alone, from zeros).
+template <class T, int A, int kWaves, bool kOut>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <= 128 ? 2 : 1))) void scan_kernel(
+    const Scans scans, const Cut cut, uint32_t roles, float* local0, float* local1, uint32_t* whole0, uint32_t* whole1) {
+    // (requests a chunk ahead take registers; where they do not fit, a chunk's requests go out together when it begins)
+    constexpr bool kAhead = sizeof(T) == 2 && A <= 64;
+    constexpr uint32_t kThreads = kWaves * 64, kWidthZ = kWaves * 32, kStrideA = A + kPad<T>, kStrideZ = kWidthZ + kPad<T>;
     extern __shared__ __align__(16) unsigned char lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h32 = lane >> 5, col32 = lane & 31u;
     // Workgroups go to the eight dies in turn: those that read the same steps are eight apart, on one die and behind one L2.
@@ -225,182 +297,186 @@ __global__ __launch_bounds__(256) void scan_kernel(const Scans scans, const Cut 
     if (item >= cut.rows * (kOut ? cut.segments : cut.segments - 1u)) return;
     const uint32_t seg = item / cut.rows, row = item - seg * cut.rows, env = row / cut.n_heads, head = row - env * cut.n_heads;
     const Scan& s = scans.s[role];
-    if (tile * cut.waves * 32u >= s.b) return;  // (roles whose z is narrower)
+    if (tile * kWidthZ >= s.b) return;  // (roles whose z is narrower)
     const LinearAttentionHead& hd = cut.heads[head];
-    const uint32_t widthZ = cut.waves * 32u, strideZ = widthZ + kPad<T>, n0 = tile * widthZ, col = n0 + wave * 32u + col32;
+    const uint32_t n0 = tile * kWidthZ, col = n0 + wave * 32u + col32;
     T* ys = reinterpret_cast<T*>(lds);
     T* zs = ys + C * kStrideA;
-    T* xs = zs + C * strideZ;
+    T* xs = zs + C * kStrideZ;
     float* pw = reinterpret_cast<float*>(xs + (kOut ? C * kStrideA : 0));  // g^0 .. g^C
-    float* weight = pw + 80 + wave * 64u;                                 // a wavefront's g^(n-1-j)
-    uint32_t* flag = reinterpret_cast<uint32_t*>(pw + 80 + cut.waves * 64u);  // [2]
-    for (uint32_t i = threadIdx.x; i <= (uint32_t)C; i += blockDim.x) pw[i] = hd.power[i];
-    if (threadIdx.x < 2) flag[threadIdx.x] = 0;
-    __syncthreads();
+    float* weight = pw + 36 + wave * 64u;                                  // a wavefront's g^(n-1-j)
+    uint32_t* flag = reinterpret_cast<uint32_t*>(pw + 36 + kWaves * 64);   // [2]
+    for (uint32_t i = threadIdx.x; i <= (uint32_t)C; i += kThreads) pw[i] = hd.power[i];
+    if (threadIdx.x < 2u) flag[threadIdx.x] = 0;
+    const uint32_t widthB = min(s.b - n0, kWidthZ);
+    if (s.a < (uint32_t)A || widthB < kWidthZ)
+        for (uint32_t i = threadIdx.x; i < C * (kStrideA * (kOut ? 2 : 1) + kStrideZ) * sizeof(T) / 16u; i += kThreads) reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
 
-    // the factors of P in a tile on the diagonal and in the one beside it: position i of a lane's column, j of its rows
-    float near[kOut ? 16 : 1], far[kOut && C == 64 ? 16 : 1];
-    if (kOut)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const uint32_t j = (r & 3) + 8 * (r >> 2) + 4 * h32, i = col32;
-            near[r] = s.key_scale * (s.reverse ? (j >= i ? pw[j - i] : 0.0f) : (i >= j ? pw[i - j] : 0.0f));
-            if (C == 64) far[C == 64 ? r : 0] = s.key_scale * (s.reverse ? pw[32 + j - i] : pw[32 + i - j]);
-        }
+    const T *xh = head_of<const T>(s.x, env, head), *yh = head_of<const T>(s.y, env, head), *zh = head_of<const T>(s.z, env, head) + n0;
+    T* oh = head_of<T>(s.out, env, head);
+    const uint8_t* resets = cut.resets ? cut.resets + (int64_t)env * cut.resets_env : nullptr;
+    // the segment's steps in the order in which they are taken; in reverse, position p of the scan is step n_steps - 1 - p
+    const uint32_t begin = seg * cut.seg_steps, end = min(begin + cut.seg_steps, cut.n_steps);
+    Steps<T, A, kThreads> y_steps(s.y.step, s.a), x_steps(s.x.step, s.a);
+    Steps<T, kWidthZ, kThreads> z_steps(s.z.step, widthB);
+    uint32_t reset = 0;
+    const auto step_of = [&](uint32_t at, uint32_t n) { return s.reverse ? (int64_t)(cut.n_steps - at - n) : (int64_t)at; };  // a chunk's first step in memory
+    const auto ask = [&](uint32_t at, uint32_t n) {
+        const int64_t t = step_of(at, n);
+        reset = resets && lane < n ? resets[(t + lane) * cut.resets_step] : 0u;
+        y_steps.ask(yh + t * s.y.step, n);
+        z_steps.ask(zh + t * s.z.step, n);
+        if (kOut) x_steps.ask(xh + t * s.x.step, n);
+    };
+    if (kAhead && begin < end) ask(begin, min((uint32_t)C, end - begin));
 
+    // the state: a lane's column, rows (r & 3) + 8 (r >> 2) + 4 h32 of every 32
     f32x16 state[A / 32];
     const size_t cells = (size_t)s.a * s.b;
     const float* from = kOut ? (seg ? s.before + ((size_t)(seg - 1u) * cut.rows + row) * cells : s.state_in ? s.state_in + row * cells : nullptr) : nullptr;
+    const bool whole_state = s.a == (uint32_t)A && n0 + kWidthZ <= s.b;
 #pragma unroll
     for (int db = 0; db < A / 32; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
-            state[db][r] = from && d < s.a && col < s.b ? from[d * s.state_row + col * s.state_col] : 0.0f;
+            state[db][r] = 0.0f;
+            if (from) {
+                state[db][r] = from[min(d, s.a - 1u) * s.state_row + min(col, s.b - 1u) * s.state_col];
+                if (!whole_state && (d >= s.a || col >= s.b)) state[db][r] = 0.0f;
+            }
+        }
+    __syncthreads();
+
+    // the factors of P: position i is a lane's column, j its rows
+    float near[kOut ? 16 : 1];
+    if (kOut)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int j = (r & 3) + 8 * (r >> 2) + 4 * (int)h32, gap = s.reverse ? j - (int)col32 : (int)col32 - j;
+            near[r] = gap >= 0 ? s.out_scale * s.key_scale * pw[gap] : 0.0f;
         }
 
-    const T *xh = head_of<const T>(s.x, env, head), *yh = head_of<const T>(s.y, env, head), *zh = head_of<const T>(s.z, env, head) + n0;
-    T* oh = head_of<T>(s.out, env, head);
-    const uint8_t* resets = cut.resets ? cut.resets + (int64_t)env * cut.resets_env : nullptr;
-    const uint32_t widthB = min(s.b - n0, widthZ);
-    // the segment's steps in the order in which they are taken; in reverse, position p of the scan is step n_steps - 1 - p
-    const uint32_t begin = seg * cut.seg_steps, end = min(begin + cut.seg_steps, cut.n_steps);
     uint32_t singles = 0, turn = 0;  // steps still to be taken one by one
-    bool uncut = true;
+    bool uncut = true, weights_plain = false;
     for (uint32_t at = begin; at < end;) {
         const uint32_t n = singles ? 1u : min((uint32_t)C, end - at);
-        const int64_t t = s.reverse ? (int64_t)(cut.n_steps - at - n) : (int64_t)at;  // the chunk's first step in memory
-        uint32_t most = 0, unused = 0;
-        const bool begins = resets && lane < n && resets[(t + lane) * cut.resets_step] != 0;
-        stage<T, true>(yh + t * s.y.step, s.y.step, n, s.a, ys, C, A, most);
-        stage<T, true>(zh + t * s.z.step, s.z.step, n, widthB, zs, C, widthZ, most);
-        if (kOut) stage<T, false>(xh + t * s.x.step, s.x.step, n, s.a, xs, C, A, unused);
-        if (most >= 0x7F800000u) flag[turn & 1u] = 1;
-        const uint64_t m = __ballot(begins);
+        const int64_t t = step_of(at, n);
+        if (!kAhead) ask(at, n);
+        Most<T> most, unused;
+        y_steps.template put<true>(yh + t * s.y.step, ys, n, most);
+        z_steps.template put<true>(zh + t * s.z.step, zs, n, most);
+        if (kOut) x_steps.template put<false>(xh + t * s.x.step, xs, n, unused);
+        if (most.infinite()) flag[turn & 1u] = 1;
+        const uint64_t m = __ballot(reset != 0u);
         __syncthreads();
         const bool broken = flag[turn & 1u] != 0;
         if (threadIdx.x == 0) flag[(turn + 1u) & 1u] = 0;
         ++turn;
         if (broken && n > 1) {
             singles = n;
+            if (kAhead) ask(at, 1u);
             __syncthreads();
             continue;
         }
-        // the first episode boundary after, and the last one up to, each position of the chunk
-        const uint64_t later = m & ~up_to(lane), earlier = m & up_to(lane);
-        const bool out_of = s.reverse ? earlier == 0 : later == 0;  // what position `lane` adds to the state stays in it
-        weight[lane] = lane < n && out_of ? s.key_scale * pw[s.reverse ? lane + 1u : n - 1u - lane] : 0.0f;
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const uint32_t after = at + n;
+        if (singles) --singles;
+        if (kAhead && after < end) ask(after, singles ? 1u : min((uint32_t)C, end - after));
+        // what position `lane` adds to the state; the same for every whole chunk in which no episode begins
+        const bool plain = n == (uint32_t)C && m == 0;
+        if (!plain || !weights_plain) {
+            const bool stays = s.reverse ? (m & up_to(lane)) == 0 : (m & ~up_to(lane)) == 0;
+            weight[lane] = lane < n && stays ? s.key_scale * pw[s.reverse ? lane + 1u : n - 1u - lane] : 0.0f;
+            weights_plain = plain;
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
 
+        part_of_chunk();
         if constexpr (kOut) {
-            f32x16 acc[C / 32];
-#pragma unroll
-            for (int ib = 0; ib < C / 32; ++ib)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[ib][r] = 0.0f;
+            f32x16 acc = (f32x16)0.0f;
             // out^T = S^T x^T, columns = steps
 #pragma unroll
             for (int db = 0; db < A / 32; ++db)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    float f[8];
+                for (int k = 0; k < 2; ++k)
+                    acc = Parts<T, 2>(half(state[db], k)).on_the_left(along(xs + col32 * kStrideA + db * 32 + k * 16, h32), acc);
+            acc *= s.out_scale * pw[s.reverse ? (col32 < n ? n - 1u - col32 : 0u) : col32 + 1u];
+            if (m) {
+                const bool into = s.reverse ? (m & ~up_to(col32)) == 0 : (m & up_to(col32)) == 0;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] = state[db][8 * k + e];
-                    const Parts<T, 2> sp(f);
-#pragma unroll
-                    for (int ib = 0; ib < C / 32; ++ib) acc[ib] = sp.on_the_left(along(xs + (ib * 32 + col32) * kStrideA + db * 32 + k * 16, h32), acc[ib]);
-                }
-#pragma unroll
-            for (int ib = 0; ib < C / 32; ++ib) {
-                const uint32_t i = ib * 32 + col32;
-                const bool into = s.reverse ? (m & ~up_to(i)) == 0 : (m & up_to(i)) == 0;
-                const float f = pw[s.reverse ? (i < n ? n - 1u - i : 0u) : i + 1u];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[ib][r] = into ? acc[ib][r] * f : 0.0f;
+                for (int r = 0; r < 16; ++r) acc[r] = into ? acc[r] : 0.0f;
             }
-            // out^T += z^T P^T, tile by tile of P
-            const auto tile_of_p = [&](uint32_t ib, uint32_t jb, const float(&factor)[16], f32x16 c) {
-                f32x16 p;
+            part_of_chunk();
+            // P^T, then out^T += z^T P^T
+            f32x16 p = (f32x16)0.0f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] = 0.0f;
+            for (int k = 0; k < A / 16; ++k) p = mma(along(ys + col32 * kStrideA + k * 16, h32), along(xs + col32 * kStrideA + k * 16, h32), p);
+            // (a choice and no product with 0: an overflow in a pair that does not count stays out)
 #pragma unroll
-                for (int k = 0; k < A / 16; ++k) p = mma(along(ys + (jb * 32 + col32) * kStrideA + k * 16, h32), along(xs + (ib * 32 + col32) * kStrideA + k * 16, h32), p);
-                // the positions that reach i: [first, first + many)
-                const uint32_t i = ib * 32 + col32;
-                const uint64_t upto = m & up_to(i), after = m & ~up_to(i);
-                const uint32_t first = s.reverse ? i : upto ? 63u - (uint32_t)__builtin_clzll(upto) : 0u;
-                const uint32_t past = s.reverse ? (after ? (uint32_t)__builtin_ctzll(after) : 64u) : i + 1u;
+            for (int r = 0; r < 16; ++r) p[r] = near[r] != 0.0f ? p[r] * near[r] : 0.0f;
+            if (m) {
+                // no episode begins in (j, i]
+                const uint64_t upto = m & up_to(col32), later = m & ~up_to(col32);
+                const uint32_t first = s.reverse || !upto ? 0u : 63u - (uint32_t)__builtin_clzll(upto), past = s.reverse && later ? (uint32_t)__builtin_ctzll(later) : 64u;
+                uint32_t lowest = 4u * h32 - first;
+                asm volatile("" : "+v"(lowest));  // (or 16 sums with h32 are kept from chunk to chunk)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    float f[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int r = 8 * k + e;
-                        const uint32_t j = jb * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
-                        f[e] = j - first < past - first ? p[r] * factor[r] : 0.0f;
-                    }
-                    c = Parts<T, 2>(f).on_the_right(across(zs + (jb * 32 + k * 16) * strideZ + wave * 32u, strideZ, lane), c);
-                }
-                return c;
-            };
-#pragma unroll
-            for (int ib = 0; ib < C / 32; ++ib) acc[ib] = tile_of_p(ib, ib, near, acc[ib]);
-            if constexpr (C == 64) {
-                f32x16 beside;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) beside[r] = 0.0f;
-                beside = tile_of_p(s.reverse ? 0u : 1u, s.reverse ? 1u : 0u, far, beside);
-                if (s.reverse)
-                    acc[0] += beside;
-                else
-                    acc[1] += beside;
+                for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] : 0.0f;
             }
+            part_of_chunk();
 #pragma unroll
-            for (int ib = 0; ib < C / 32; ++ib) {
-                const uint32_t i = ib * 32 + col32;
-                if (i < n) {
-                    T* o = oh + (t + i) * s.out.step;
+            for (int k = 0; k < 2; ++k) acc = Parts<T, 2>(half(p, k)).on_the_right(across(zs + k * 16 * kStrideZ + wave * 32u, kStrideZ, lane), acc);
+            part_of_chunk();
+            if (col32 < n) {
+                T* o = oh + (t + col32) * s.out.step + (n0 + wave * 32u);
 #pragma unroll
-                    for (int r = 0; r < 16; r += 4) {
-                        const uint32_t c = n0 + wave * 32u + 2 * r + 4 * h32;
-                        T v[4];
+                for (int r = 0; r < 16; r += 4) {
+                    const uint32_t c = 2 * r + 4 * h32;
+                    T v[4];
+                    if constexpr (sizeof(T) == 2) {
+                        const uint32_t w[2] = {__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r], acc[r + 1]}, bf16x2)),
+                                               __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r + 2], acc[r + 3]}, bf16x2))};
+                        __builtin_memcpy(v, w, 8);
+                    } else {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = (T)(acc[ib][r + e] * s.out_scale);
-                        if (c + 4 <= s.b)
-                            __builtin_memcpy(o + c, v, sizeof(v));
-                        else
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (c + e < s.b) o[c + e] = v[e];
+                        for (int e = 0; e < 4; ++e) v[e] = acc[r + e];
                     }
+                    if (n0 + kWidthZ <= s.b || n0 + wave * 32u + c + 4 <= s.b)
+                        __builtin_memcpy(o + c, v, sizeof(v));
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (n0 + wave * 32u + c + e < s.b) o[c + e] = v[e];
                 }
             }
         }
 
+        part_of_chunk();
         // S <- g^n S + y^T (weights z)
-        uncut = uncut && m == 0;
-        const float keep = n == (uint32_t)C ? hd.decay_chunk[C / 32 - 1] : n == 1u ? hd.decay : pw[n];
-        const float keep_rest = n == (uint32_t)C ? hd.decay_chunk_rest[C / 32 - 1] : n == 1u ? hd.decay_rest : 0.0f;
+        if (m == 0) {
+            const float keep = n == (uint32_t)C ? hd.decay_chunk : n == 1u ? hd.decay : pw[n];
+            const float keep_rest = n == (uint32_t)C ? hd.decay_chunk_rest : n == 1u ? hd.decay_rest : 0.0f;
 #pragma unroll
-        for (int db = 0; db < A / 32; ++db)
+            for (int db = 0; db < A / 32; ++db)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) state[db][r] = m == 0 ? __builtin_fmaf(state[db][r], keep, state[db][r] * keep_rest) : 0.0f;
+                for (int r = 0; r < 16; ++r) state[db][r] = __builtin_fmaf(state[db][r], keep, state[db][r] * keep_rest);
+        } else {
+            uncut = false;
+#pragma unroll
+            for (int db = 0; db < A / 32; ++db) state[db] = (f32x16)0.0f;
+        }
 #pragma unroll
         for (int k = 0; k < C / 16; ++k) {
-            const Frag<T> z = across(zs + k * 16 * strideZ + wave * 32u, strideZ, lane);
-            const f32x4 w0 = *reinterpret_cast<const f32x4*>(weight + k * 16 + 4 * h32), w1 = *reinterpret_cast<const f32x4*>(weight + k * 16 + 8 + 4 * h32);
-            float f[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = value(z, e) * (e < 4 ? w0[e & 3] : w1[e & 3]);
-            const Parts<T, 3> zp(f);
+            part_of_chunk();
+            const Frag<T> z = across(zs + k * 16 * kStrideZ + wave * 32u, kStrideZ, lane);
+            const Parts<T, 3> zp(values(z) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
 #pragma unroll
             for (int db = 0; db < A / 32; ++db) state[db] = zp.on_the_right(across(ys + k * 16 * kStrideA + db * 32, kStrideA, lane), state[db]);
         }
         __syncthreads();
-        at += n;
-        if (singles) --singles;
+        at = after;
     }
 
     float* to = kOut ? (seg + 1u == cut.segments && s.state_out ? s.state_out + row * cells : nullptr)
@@ -411,7 +487,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const Scans scans, const Cut 
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
-                if (d < s.a && col < s.b) to[d * s.state_row + col * s.state_col] = state[db][r];
+                if (whole_state || (d < s.a && col < s.b)) to[d * s.state_row + col * s.state_col] = state[db][r];
             }
     if (!kOut && tile == 0 && threadIdx.x == 0) (role ? whole1 : whole0)[seg * cut.rows + row] = uncut ? 1u : 0u;
 }
@@ -469,15 +545,11 @@ int launched(std::string& err) {
     return PXR_ERR_DEVICE;
 }
 
-// Chunks: 64 steps in bfloat16 (32 where the rollout has no more), 32 in fp32, whose products cost 16 times as much and of which a shorter
-// chunk has fewer.
-uint32_t chunk_of(uint32_t dtype, uint32_t n_steps) { return dtype == PXR_BF16 && n_steps > 32u ? 64u : 32u; }
-
-uint32_t waves_of(uint32_t b) { return b <= 32u ? 1u : b <= 64u ? 2u : 4u; }
+// Wavefronts of a workgroup: enough for z, four at most, and no fewer than it takes to bring the steps of long heads.
+uint32_t waves_of(uint32_t a, uint32_t b) { return a > 128u ? 4u : b <= 32u && a <= 64u ? 1u : b <= 64u ? 2u : 4u; }
 
 // Segments of a rollout's steps: as many as it takes to give each compute unit two workgroups, of four chunks at least.
-uint32_t segments_of(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, uint32_t roles, uint32_t* seg_steps) {
-    const uint32_t C = chunk_of(dtype, n_steps);
+uint32_t segments_of(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, uint32_t roles, uint32_t* seg_steps) {
     const uint64_t chunks = ((uint64_t)n_steps + C - 1u) / C, rows = (uint64_t)n_envs * c.n_heads * roles;
     uint64_t want = 2ull * c.n_cus / rows;
     if (want > chunks / 4u) want = chunks / 4u;
@@ -490,54 +562,61 @@ uint32_t segments_of(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_
     return (uint32_t)((chunks + each - 1u) / each);
 }
 
+template <class T, int A, int kWaves, bool kOut>
+constexpr size_t scan_lds() {
+    return (size_t)C * ((kOut ? 2 : 1) * (A + kPad<T>) + kWaves * 32 + kPad<T>) * sizeof(T) + (36 + kWaves * 64 + 2) * 4;
+}
+
 // Chunks of 256 values take more than the 64 KB of LDS that a launch has by default.
-template <class T, int C>
+template <class T>
 hipError_t allow_lds() {
-    const void* fns[2] = {reinterpret_cast<const void*>(&scan_kernel<T, 256, C, true>), reinterpret_cast<const void*>(&scan_kernel<T, 256, C, false>)};
+    const void* fns[2] = {reinterpret_cast<const void*>(&scan_kernel<T, 256, 4, true>), reinterpret_cast<const void*>(&scan_kernel<T, 256, 4, false>)};
+    static_assert(scan_lds<T, 128, 4, true>() <= 64 * 1024 && scan_lds<T, 256, 4, true>() <= 160 * 1024);
     for (const void* f : fns)
         if (const hipError_t rc = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); rc != hipSuccess) return rc;
     return hipSuccess;
 }
 
-template <class T, int C, bool kOut>
+template <class T, bool kOut>
 void enqueue_as(const Scan* s, uint32_t roles, const Cut& cut, float* const* local, uint32_t* const* whole, hipStream_t st) {
-    uint32_t a = 0;
-    for (uint32_t i = 0; i < roles; ++i) a = s[i].a > a ? s[i].a : a;
-    const uint32_t A = a <= 32u ? 32u : a <= 64u ? 64u : a <= 128u ? 128u : 256u;
     const uint32_t items = cut.rows * (kOut ? cut.segments : cut.segments - 1u);
-    const dim3 grid((items + 7u) / 8u * 8u * cut.tiles * roles), block(cut.waves * 64u);
-    const size_t lds = (size_t)C * ((kOut ? 2u : 1u) * (A + kPad<T>) + cut.waves * 32u + kPad<T>) * sizeof(T) + (80u + cut.waves * 64u + 2u) * 4u;
+    const dim3 grid((items + 7u) / 8u * 8u * cut.tiles * roles);
     const Scans scans{{s[0], s[roles > 1 ? 1 : 0], s[roles > 2 ? 2 : 0]}};
-#define PXR_SCAN(AA) \
-    hipLaunchKernelGGL((scan_kernel<T, AA, C, kOut>), grid, block, lds, st, scans, cut, roles, local[0], local[1], whole[0], whole[1])
-    if (A == 32u)
-        PXR_SCAN(32);
-    else if (A == 64u)
-        PXR_SCAN(64);
-    else if (A == 128u)
-        PXR_SCAN(128);
-    else
-        PXR_SCAN(256);
+#define PXR_SCAN(A, W)                                                                                                                            \
+    case A + W:                                                                                                                                   \
+        hipLaunchKernelGGL((scan_kernel<T, A, W, kOut>), grid, dim3(W * 64), (scan_lds<T, A, W, kOut>()), st, scans, cut, roles, local[0], local[1], \
+                           whole[0], whole[1]);                                                                                                   \
+        break
+    switch (cut.width + cut.waves) {
+        PXR_SCAN(32, 1);
+        PXR_SCAN(32, 2);
+        PXR_SCAN(32, 4);
+        PXR_SCAN(64, 1);
+        PXR_SCAN(64, 2);
+        PXR_SCAN(64, 4);
+        PXR_SCAN(128, 2);
+        PXR_SCAN(128, 4);
+        PXR_SCAN(256, 4);
+    }
 #undef PXR_SCAN
 }
 
 template <bool kOut>
 void enqueue(uint32_t dtype, const Scan* s, uint32_t roles, const Cut& cut, float* const* local, uint32_t* const* whole, hipStream_t st) {
     if (dtype == PXR_F32)
-        enqueue_as<float, 32, kOut>(s, roles, cut, local, whole, st);
-    else if (chunk_of(dtype, cut.n_steps) == 32u)
-        enqueue_as<__bf16, 32, kOut>(s, roles, cut, local, whole, st);
+        enqueue_as<float, kOut>(s, roles, cut, local, whole, st);
     else
-        enqueue_as<__bf16, 64, kOut>(s, roles, cut, local, whole, st);
+        enqueue_as<__bf16, kOut>(s, roles, cut, local, whole, st);
 }
 
-Cut cut_of(const LinearAttentionConsts& c, const pxr_rollout& r, uint32_t roles, uint32_t b) {
+Cut cut_of(const LinearAttentionConsts& c, const pxr_rollout& r, uint32_t roles, uint32_t a, uint32_t b) {
     Cut cut{};
     cut.n_heads = c.n_heads;
     cut.rows = r.n_envs * c.n_heads;
     cut.n_steps = r.n_steps;
-    cut.segments = segments_of(c, r.dtype, r.n_envs, r.n_steps, roles, &cut.seg_steps);
-    cut.waves = waves_of(b);
+    cut.segments = segments_of(c, r.n_envs, r.n_steps, roles, &cut.seg_steps);
+    cut.width = a <= 32u ? 32u : a <= 64u ? 64u : a <= 128u ? 128u : 256u;
+    cut.waves = waves_of(a, b);
     cut.tiles = (b + cut.waves * 32u - 1u) / (cut.waves * 32u);
     cut.heads = c.heads;
     cut.resets = r.d_resets;
@@ -557,17 +636,16 @@ size_t whole_bytes(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t seg
 }  // namespace
 
 int prepare_linear_attention_kernels(std::string& err) {
-    hipError_t rc = allow_lds<float, 32>();
-    if (rc == hipSuccess) rc = allow_lds<__bf16, 32>();
-    if (rc == hipSuccess) rc = allow_lds<__bf16, 64>();
+    hipError_t rc = allow_lds<float>();
+    if (rc == hipSuccess) rc = allow_lds<__bf16>();
     if (rc == hipSuccess) return PXR_OK;
     err = std::string("hipFuncSetAttribute(MaxDynamicSharedMemorySize) failed: ") + hipGetErrorString(rc);
     return PXR_ERR_DEVICE;
 }
 
-size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, bool backward) {
+size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, bool backward) {
     uint32_t steps;
-    const uint32_t segments = segments_of(c, dtype, n_envs, n_steps, backward ? 3u : 1u, &steps);
+    const uint32_t segments = segments_of(c, n_envs, n_steps, backward ? 3u : 1u, &steps);
     const size_t one = ((state_bytes(c, n_envs, segments) + 15u) & ~(size_t)15u) + whole_bytes(c, n_envs, segments);
     return backward ? 2u * one : one;
 }
@@ -575,7 +653,7 @@ size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t dtype
 int launch_linear_attention_forward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& out, float* state_out, void* ws,
                                     void* stream, std::string& err) {
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const Cut cut = cut_of(c, r, 1u, c.dv);
+    const Cut cut = cut_of(c, r, 1u, c.dk, c.dv);
     Scan s{r.q, r.k, r.v, out, c.dk, c.dv, r.d_state, state_out, c.dv, 1u, nullptr, c.scale, 1.0f, 0u};
     float* local[2] = {static_cast<float*>(ws), nullptr};
     uint32_t* whole[2] = {reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + ((state_bytes(c, r.n_envs, cut.segments) + 15u) & ~(size_t)15u)), nullptr};
@@ -593,7 +671,8 @@ int launch_linear_attention_backward(const LinearAttentionConsts& c, const pxr_r
                                      const pxr_tokens& dq, const pxr_tokens& dk, const pxr_tokens& dv, float* dstate, void* ws,
                                      void* stream, std::string& err) {
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const Cut cut = cut_of(c, r, 3u, c.dk > c.dv ? c.dk : c.dv);
+    const uint32_t most = c.dk > c.dv ? c.dk : c.dv;
+    const Cut cut = cut_of(c, r, 3u, most, most);
     const size_t states = (state_bytes(c, r.n_envs, cut.segments) + 15u) & ~(size_t)15u, words = whole_bytes(c, r.n_envs, cut.segments);
     char* w = static_cast<char*>(ws);
     float* local[2] = {reinterpret_cast<float*>(w), reinterpret_cast<float*>(w + states + words)};
@@ -602,7 +681,7 @@ int launch_linear_attention_backward(const LinearAttentionConsts& c, const pxr_r
         // the states [dk][dv] of the forward scan and of the reverse one, which dk and dv share
         const Scan both[2] = {Scan{r.q, r.k, r.v, dout, c.dk, c.dv, nullptr, nullptr, c.dv, 1u, nullptr, 1.0f, 1.0f, 0u},
                               Scan{r.k, r.q, dout, dout, c.dk, c.dv, nullptr, nullptr, c.dv, 1u, nullptr, 1.0f, c.scale, 1u}};
-        enqueue<false>(r.dtype, both, 2u, cut_of(c, r, 3u, c.dv), local, whole, st);
+        enqueue<false>(r.dtype, both, 2u, cut_of(c, r, 3u, c.dk, c.dv), local, whole, st);
         hipLaunchKernelGGL(join_kernel, dim3((c.dk * c.dv + 255u) / 256u, cut.rows, 2), dim3(256), 0, st, cut, c.dk * c.dv, r.d_state, dstate_out, local[0],
                            local[1], whole[0], whole[1]);
     }

@@ -231,9 +231,9 @@ int launch_layer_norm_backward(const pxr_layer_norm_desc& d, const void* dy, con
 // same would add up over a long look-back (4096 steps: 2^-12 of a state), so g is held as a sum of two floats.
 struct LinearAttentionHead {
     double log_decay;
-    float decay, decay_rest;                          // g
-    float decay_chunk[2], decay_chunk_rest[2];        // g^32, g^64
-    float power[65];                                  // g^0 .. g^64, each rounded by itself
+    float decay, decay_rest;              // g
+    float decay_chunk, decay_chunk_rest;  // g^32
+    float power[33];                      // g^0 .. g^32, each rounded by itself
 };
 void fill_head(LinearAttentionHead& h, float log_decay);
 
@@ -245,7 +245,7 @@ struct LinearAttentionConsts {
 
 // linear_attention.hip (arguments as checked by memory_api.cpp)
 int prepare_linear_attention_kernels(std::string& err);
-size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, bool backward);
+size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, bool backward);
 int launch_linear_attention_forward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& out, float* state_out, void* ws,
                                     void* stream, std::string& err);
 int launch_linear_attention_backward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& dout, const float* dstate_out,
