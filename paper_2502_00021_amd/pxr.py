@@ -9,6 +9,7 @@ There is no fallback: a missing library or a failing call raises.
 import ctypes as C
 import math
 import os
+import struct
 
 import numpy as np
 
@@ -84,6 +85,12 @@ class Rollout(C.Structure):
                 ("d_resets", C.c_void_p), ("resets_env", C.c_int64), ("resets_step", C.c_int64), ("d_state", C.c_void_p)]
 
 
+# The same three as bytes: a call packs its arguments in a fraction of the time that it takes to fill the structures.
+_pack_norm = struct.Struct("@IIQIfqqq").pack
+_pack_tokens = struct.Struct("@Pqqq").pack
+_pack_rollout = struct.Struct("@III4xPqqqPqqqPqqqPqqP").pack
+
+
 _lib = None
 _lib_path = LIB_PATH
 
@@ -141,7 +148,7 @@ def lib():
                      "pxr_pipeline_info"):
             getattr(L, name).restype = C.c_int
         size = C.POINTER(C.c_size_t)
-        tokens, rollout, norm = C.POINTER(Tokens), C.POINTER(Rollout), C.POINTER(LayerNormDesc)
+        tokens = rollout = norm = vp  # (structures, or their packed bytes)
         L.pxr_layer_norm_forward.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp]
         L.pxr_layer_norm_workspace.argtypes = [norm, size]
         L.pxr_layer_norm_backward.argtypes = [norm, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
@@ -545,11 +552,15 @@ class Pipeline:
         return frames, features
 
 
+_dtype_codes = {}
+
+
 def _dtype_code(torch, dtype):
-    if dtype == torch.float32:
-        return 0
-    assert dtype == torch.bfloat16, f"float32 or bfloat16, not {dtype}"
-    return 1
+    if not _dtype_codes:
+        _dtype_codes.update({torch.float32: 0, torch.bfloat16: 1})
+    code = _dtype_codes.get(dtype)
+    assert code is not None, f"float32 or bfloat16, not {dtype}"
+    return code
 
 
 def _empty(torch, like, stream, shape, dtype):
@@ -562,20 +573,21 @@ def _empty(torch, like, stream, shape, dtype):
 
 
 def _rows(x):
-    """[..., D] as [N, D] without a copy, and the stride between rows (raises if there is no single one)."""
+    """Rows, width and the values from row to row of [..., D] (raises if there is no single such number)."""
     assert x.is_cuda and x.dim() >= 1 and x.shape[-1] > 0, "a CUDA tensor [..., width]"
     r = x if x.dim() == 2 else x.view(-1, x.shape[-1])
     n, width = r.shape
-    assert width == 1 or r.stride(1) == 1 or n == 0, "the values of a row must be adjacent"
-    return r, n, width, (r.stride(0) if n > 1 else width)
+    step, inner = r.stride()
+    assert inner == 1 or width == 1 or n == 0, "the values of a row must be adjacent"
+    return n, width, step if n > 1 else width
 
 
 def _params(torch, x, width, *params):
-    """dtype code of the weight and bias (those that there are), checked."""
+    """dtype of the weight and bias (those that there are), checked."""
     dtype = None
     for p in params:
         if p is not None:
-            assert p.is_cuda and p.is_contiguous() and p.shape == (width,), tuple(p.shape)
+            assert p.is_cuda and p.is_contiguous() and p.dim() == 1 and p.shape[0] == width, tuple(p.shape)
             assert p.dtype in (torch.float32, x.dtype) and dtype in (None, p.dtype), "weight and bias: both float32 or both of x's type"
             dtype = p.dtype
     return torch.float32 if dtype is None else dtype
@@ -590,44 +602,48 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     or of x's type, or None.  Returns (y like x, mean, rstd: float32, x's leading shape), the latter two for
     layer_norm_backward; enqueue only."""
     torch = _torch or _torch_module()
-    r, n, width, x_stride = _rows(x)
+    n, width, x_stride = _rows(x)
+    dtype = x.dtype
     params = _params(torch, x, width, weight, bias)
     if out is None:
-        y, y_stride = _empty(torch, x, stream, x.shape, x.dtype), width
+        out, y_stride = _empty(torch, x, stream, x.shape, dtype), width
     else:
-        assert out.is_cuda and out.dtype == x.dtype and out.shape == x.shape
-        y, y_stride = out, _rows(out)[3]
-    mean, rstd = (_empty(torch, x, stream, x.shape[:-1], torch.float32) for _ in range(2))
-    d = LayerNormDesc(_dtype_code(torch, x.dtype), _dtype_code(torch, params), n, width, eps, x_stride, y_stride, width)
-    _check((_lib or lib()).pxr_layer_norm_forward(C.byref(d), r.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mean.data_ptr(),
+        assert out.is_cuda and out.dtype == dtype and out.shape == x.shape
+        y_stride = _rows(out)[2]
+    lead = x.shape[:-1]
+    mean, rstd = _empty(torch, x, stream, lead, torch.float32), _empty(torch, x, stream, lead, torch.float32)
+    d = _pack_norm(_dtype_code(torch, dtype), _dtype_code(torch, params), n, width, eps, x_stride, y_stride, width)
+    _check((_lib or lib()).pxr_layer_norm_forward(d, x.data_ptr(), _ptr(weight), _ptr(bias), out.data_ptr(), mean.data_ptr(),
                                                   rstd.data_ptr(), _stream_handle(stream, x)))
-    return y, mean, rstd
+    return out, mean, rstd
 
 
 def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, params_dtype=None, stream=None):
     """Gradients of layer_norm for dy (x's shape and type), with the mean and rstd that it returned.  Returns (dx, dweight,
     dbias), the latter two [D] of the weight's type (without a weight: params_dtype, float32 unless given); enqueue only."""
     torch = _torch or _torch_module()
-    r, n, width, x_stride = _rows(x)
-    assert dy.dtype == x.dtype and dy.shape == x.shape
-    g, _, _, dy_stride = _rows(dy)
+    n, width, x_stride = _rows(x)
+    dtype = x.dtype
+    assert dy.dtype == dtype and dy.shape == x.shape
+    dy_stride = _rows(dy)[2]
     for s in (mean, rstd):
         assert s.is_cuda and s.dtype == torch.float32 and s.is_contiguous() and s.numel() == n, "mean and rstd: one float32 for each row"
     params = _params(torch, x, width, weight) if weight is not None else params_dtype or torch.float32
-    assert params in (torch.float32, x.dtype)
+    assert params in (torch.float32, dtype)
     if dx is None:
-        dx, dx_stride = _empty(torch, x, stream, x.shape, x.dtype), width
+        dx, dx_stride = _empty(torch, x, stream, x.shape, dtype), width
     else:
-        assert dx.is_cuda and dx.dtype == x.dtype and dx.shape == x.shape
-        dx_stride = _rows(dx)[3]
-    dweight, dbias = (_empty(torch, x, stream, (width,), params) for _ in range(2))
-    d = LayerNormDesc(_dtype_code(torch, x.dtype), _dtype_code(torch, params), n, width, 0.0, x_stride, dy_stride, dx_stride)
+        assert dx.is_cuda and dx.dtype == dtype and dx.shape == x.shape
+        dx_stride = _rows(dx)[2]
+    dweight, dbias = _empty(torch, x, stream, (width,), params), _empty(torch, x, stream, (width,), params)
+    d = _pack_norm(_dtype_code(torch, dtype), _dtype_code(torch, params), n, width, 0.0, x_stride, dy_stride, dx_stride)
     L = _lib or lib()
     need = C.c_size_t()
-    _check(L.pxr_layer_norm_workspace(C.byref(d), C.byref(need)))
-    ws = _empty(torch, x, stream, (need.value,), torch.uint8) if need.value else None
-    _check(L.pxr_layer_norm_backward(C.byref(d), g.data_ptr(), r.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dx.data_ptr(),
-                                     dweight.data_ptr(), dbias.data_ptr(), _ptr(ws), need.value, _stream_handle(stream, x)))
+    _check(L.pxr_layer_norm_workspace(d, need))
+    need = need.value
+    ws = _empty(torch, x, stream, (need,), torch.uint8) if need else None
+    _check(L.pxr_layer_norm_backward(d, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dx.data_ptr(),
+                                     dweight.data_ptr(), dbias.data_ptr(), _ptr(ws), need, _stream_handle(stream, x)))
     return dx, dweight, dbias
 
 
@@ -656,12 +672,12 @@ class LinearAttention:
         except Exception:
             pass
 
-    def _view(self, x, lead, d, like):
-        """A [B, T, H, d] or (acting) [B, H, d] tensor as pxr_tokens."""
-        assert x.is_cuda and x.dtype == like.dtype and x.shape == (*lead, self.H, d), (tuple(x.shape), (*lead, self.H, d))
+    def _view(self, x, shape, dtype):
+        """The fields of pxr_tokens for a [B, T, H, d] or (one step) [B, H, d] tensor of this shape and type."""
+        assert x.is_cuda and x.dtype == dtype and x.shape == shape, (tuple(x.shape), shape, x.dtype)
         s = x.stride()
-        assert d == 1 or s[-1] == 1 or x.numel() == 0, "a head's values must be adjacent"
-        return Tokens(x.data_ptr(), s[0], s[1] if len(s) == 4 else 0, s[-2])
+        assert s[-1] == 1 or shape[-1] == 1 or x.numel() == 0, "a head's values must be adjacent"
+        return (x.data_ptr(), s[0], s[1], s[2]) if len(s) == 4 else (x.data_ptr(), s[0], 0, s[1])
 
     def _state(self, torch, state, B):
         assert state.is_cuda and state.dtype == torch.float32 and state.is_contiguous()
@@ -669,22 +685,26 @@ class LinearAttention:
         return state.data_ptr()
 
     def _rollout(self, torch, q, k, v, resets, state):
-        lead = tuple(q.shape[:-2])
-        assert q.is_cuda and len(lead) in (1, 2), "queries [B, T, H, d_key], of one step [B, H, d_key]"
-        r = Rollout()
-        r.dtype, r.n_envs, r.n_steps = _dtype_code(torch, q.dtype), lead[0], lead[1] if len(lead) == 2 else 1
-        r.q, r.k, r.v = self._view(q, lead, self.dk, q), self._view(k, lead, self.dk, q), self._view(v, lead, self.dv, q)
+        """The bytes of pxr_rollout; the shapes of keys and of values; environments and steps."""
+        keys, dtype = q.shape, q.dtype
+        lead = keys[:-2]
+        values = (*lead, self.H, self.dv)
+        B, T = lead if len(lead) == 2 else (lead[0], 1)
+        assert keys[-2] == self.H and keys[-1] == self.dk, (tuple(keys), self.H, self.dk)
+        marks = (0, 0, 0)
         if resets is not None:
             assert resets.is_cuda and resets.dtype in (torch.bool, torch.uint8) and resets.shape == lead, tuple(resets.shape)
-            r.d_resets, r.resets_env, r.resets_step = resets.data_ptr(), resets.stride(0), resets.stride(1) if len(lead) == 2 else 0
-        if state is not None:
-            r.d_state = self._state(torch, state, lead[0])
-        return r, lead
+            s = resets.stride()
+            marks = (resets.data_ptr(), s[0], s[1] if len(s) == 2 else 0)
+        packed = _pack_rollout(_dtype_code(torch, dtype), B, T, *self._view(q, keys, dtype), *self._view(k, keys, dtype),
+                               *self._view(v, values, dtype), *marks, 0 if state is None else self._state(torch, state, B))
+        return packed, keys, values, B, T
 
-    def _workspace(self, torch, r, backward, like, stream):
+    def _workspace(self, torch, like, B, T, backward, stream):
         need = C.c_size_t()
-        _check(_lib.pxr_linear_attention_workspace(self._h, r.dtype, r.n_envs, r.n_steps, backward, C.byref(need)))
-        return _empty(torch, like, stream, (need.value,), torch.uint8) if need.value else None, need.value
+        _check(_lib.pxr_linear_attention_workspace(self._h, _dtype_code(torch, like.dtype), B, T, backward, need))
+        need = need.value
+        return _empty(torch, like, stream, (need,), torch.uint8) if need else None, need
 
     def forward(self, q, k, v, resets=None, state=None, out=None, state_out=None, stream=None):
         """q, k: CUDA float32 or bfloat16 [B,T,H,d_key], v: [B,T,H,d_value] (any strides, a head's values adjacent); resets:
@@ -692,12 +712,12 @@ class LinearAttention:
         first step, or None = zeros.  Returns (out [B,T,H,d_value], the state after the last step); enqueue only."""
         torch = _torch or _torch_module()
         assert q.dim() == 4
-        r, lead = self._rollout(torch, q, k, v, resets, state)
-        out = _empty(torch, q, stream, (*lead, self.H, self.dv), q.dtype) if out is None else out
-        state_out = _empty(torch, q, stream, (lead[0], self.H, self.dk, self.dv), torch.float32) if state_out is None else state_out
-        ws, need = self._workspace(torch, r, 0, q, stream)
-        _check(_lib.pxr_linear_attention_forward(self._h, C.byref(r), C.byref(self._view(out, lead, self.dv, q)),
-                                                 self._state(torch, state_out, lead[0]), _ptr(ws), need, _stream_handle(stream, q)))
+        r, keys, values, B, T = self._rollout(torch, q, k, v, resets, state)
+        out = _empty(torch, q, stream, values, q.dtype) if out is None else out
+        state_out = _empty(torch, q, stream, (B, self.H, self.dk, self.dv), torch.float32) if state_out is None else state_out
+        ws, need = self._workspace(torch, q, B, T, 0, stream)
+        _check(_lib.pxr_linear_attention_forward(self._h, r, _pack_tokens(*self._view(out, values, q.dtype)), self._state(torch, state_out, B),
+                                                 _ptr(ws), need, _stream_handle(stream, q)))
         return out, state_out
 
     def backward(self, dout, q, k, v, resets=None, state=None, dstate=None, stream=None):
@@ -706,14 +726,14 @@ class LinearAttention:
         there was none, None); enqueue only."""
         torch = _torch or _torch_module()
         assert q.dim() == 4
-        r, lead = self._rollout(torch, q, k, v, resets, state)
-        dq, dk = (_empty(torch, q, stream, (*lead, self.H, self.dk), q.dtype) for _ in range(2))
-        dv = _empty(torch, q, stream, (*lead, self.H, self.dv), q.dtype)
+        r, keys, values, B, T = self._rollout(torch, q, k, v, resets, state)
+        dtype = q.dtype
+        dq, dk, dv = (_empty(torch, q, stream, shape, dtype) for shape in (keys, keys, values))
         dfirst = None if state is None else _empty(torch, q, stream, state.shape, torch.float32)
-        ws, need = self._workspace(torch, r, 1, q, stream)
+        ws, need = self._workspace(torch, q, B, T, 1, stream)
         _check(_lib.pxr_linear_attention_backward(
-            self._h, C.byref(r), C.byref(self._view(dout, lead, self.dv, q)), None if dstate is None else self._state(torch, dstate, lead[0]),
-            C.byref(self._view(dq, lead, self.dk, q)), C.byref(self._view(dk, lead, self.dk, q)), C.byref(self._view(dv, lead, self.dv, q)),
+            self._h, r, _pack_tokens(*self._view(dout, values, dtype)), None if dstate is None else self._state(torch, dstate, B),
+            _pack_tokens(*self._view(dq, keys, dtype)), _pack_tokens(*self._view(dk, keys, dtype)), _pack_tokens(*self._view(dv, values, dtype)),
             _ptr(dfirst), _ptr(ws), need, _stream_handle(stream, q)))
         return dq, dk, dv, dfirst
 
@@ -722,10 +742,10 @@ class LinearAttention:
         [B,H,d_key,d_value] is updated in place.  Returns out [B,H,d_value]; enqueue only."""
         torch = _torch or _torch_module()
         assert q.dim() == 3
-        r, lead = self._rollout(torch, q, k, v, resets, None)
-        out = _empty(torch, q, stream, (*lead, self.H, self.dv), q.dtype) if out is None else out
-        _check(_lib.pxr_linear_attention_step(self._h, C.byref(r), self._state(torch, state, lead[0]),
-                                              C.byref(self._view(out, lead, self.dv, q)), _stream_handle(stream, q)))
+        r, _, values, B, _ = self._rollout(torch, q, k, v, resets, None)
+        out = _empty(torch, q, stream, values, q.dtype) if out is None else out
+        _check(_lib.pxr_linear_attention_step(self._h, r, self._state(torch, state, B), _pack_tokens(*self._view(out, values, q.dtype)),
+                                              _stream_handle(stream, q)))
         return out
 
 

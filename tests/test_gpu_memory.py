@@ -556,9 +556,12 @@ def test_attention_refusals(torch, pxr):
     # the C calls themselves
     import ctypes as C
     L = pxr.lib()
-    roll, lead = layer._rollout(torch, q, k, v, r, s)
+    packed = layer._rollout(torch, q, k, v, r, s)[0]
+    assert len(packed) == C.sizeof(pxr.Rollout)
+    roll = pxr.Rollout.from_buffer_copy(packed)
+    assert (roll.n_envs, roll.n_steps, roll.q.data, roll.v.head, roll.resets_step, roll.d_state) == (2, 600, q.data_ptr(), 24, 1, s.data_ptr())
     out = torch.empty_like(v)
-    view = layer._view(out, lead, 24, q)
+    view = pxr.Tokens(out.data_ptr(), *out.stride()[:3])
     need = C.c_size_t()
     assert L.pxr_linear_attention_workspace(layer._h, 0, 2, 600, 1, C.byref(need)) == 0
     ws = torch.empty(need.value + 16, dtype=torch.uint8, device="cuda")
