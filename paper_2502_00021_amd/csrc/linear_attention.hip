@@ -213,6 +213,14 @@ struct Most<__bf16> {
     __device__ __forceinline__ bool infinite() const { return max(m[0], m[1]) >= 0x7F80u; }
 };
 
+// A number that is the same in all lanes and in every chunk, as one that the compiler does not know to be: it would otherwise build the loop over
+// chunks once for each answer that a test of it can have.
+__device__ __forceinline__ uint32_t again(uint32_t v) {
+    v = __builtin_amdgcn_readfirstlane(v);
+    asm volatile("" : "+s"(v));
+    return v;
+}
+
 // A chunk's steps on their way to a tile: C rows of `kWidth` values, dealt to kThreads lanes in vectors of 16 bytes.  The requests of a chunk go out
 // together, a chunk ahead.  Rows may begin at any element (the memory takes 16-byte requests at any address).  A row of d values that ends inside a
 // vector has its last vector moved back to its end; rows past the last and vectors past a row's end read what is there instead and are not written,
@@ -232,7 +240,8 @@ struct Steps {
     }
     // n >= 1 rows
     __device__ __forceinline__ void ask(const T* from, uint32_t n) {
-        if (d < N) return;
+        const uint32_t d = again(this->d);
+        if (d < N) return forget();
 #pragma unroll
         for (uint32_t i = 0; i < kCount; ++i) {
             const T* p = from + (int64_t)(i * kRowsEach) * step + offset;
@@ -240,9 +249,15 @@ struct Steps {
             __builtin_memcpy(&v[i], p, 16);
         }
     }
+    // What was asked for has been put; nothing is in flight.  (Without this the registers would be kept, and copied, from chunk to chunk.)
+    __device__ __forceinline__ void forget() {
+#pragma unroll
+        for (uint32_t i = 0; i < kCount; ++i) asm volatile("" : "=v"(v[i].x), "=v"(v[i].y), "=v"(v[i].z), "=v"(v[i].w));
+    }
     // The tile's rows past n are zeros.  kCheck: collects bit patterns.
     template <bool kCheck>
     __device__ __forceinline__ void put(const T* from, T* tile, uint32_t n, Most<T>& most) {
+        const uint32_t d = again(this->d);
         if (d < N) {
             for (uint32_t i = threadIdx.x; i < C * d; i += kThreads) {
                 const uint32_t r = i / d, c = i - r * d;
@@ -284,19 +299,21 @@ __device__ __forceinline__ uint64_t up_to(uint32_t i) { return (2ull << i) - 1ul
 
 // A (a padded to 32, 64, 128 or 256), kWaves wavefronts; kOut: outputs (else the state after a segment alone, from zeros).
 template <class T, int A, int kWaves, bool kOut>
-__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <= 128 ? 2 : 1))) void scan_kernel(
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <= 64 ? 3 : A <= 128 ? 2 : 1))) void scan_kernel(
     const Scans scans, const Cut cut, uint32_t roles, float* local0, float* local1, uint32_t* whole0, uint32_t* whole1) {
     // (requests a chunk ahead take registers; where they do not fit, a chunk's requests go out together when it begins)
     constexpr bool kAhead = sizeof(T) == 2 && A <= 64;
     constexpr uint32_t kThreads = kWaves * 64, kWidthZ = kWaves * 32, kStrideA = A + kPad<T>, kStrideZ = kWidthZ + kPad<T>;
     extern __shared__ __align__(16) unsigned char lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h32 = lane >> 5, col32 = lane & 31u;
-    // Workgroups go to the eight dies in turn: those that read the same steps are eight apart, on one die and behind one L2.
+    // Workgroups go to the eight dies in turn: those that read the same steps are eight apart, on one die and behind one L2.  So are eight
+    // heads that follow each other, whose steps lie side by side in memory (512 x 256 bfloat16, 8 heads of 64: 202 -> 189 us, gradients 480 -> 436).
     const uint32_t per_die = cut.tiles * roles, group = blockIdx.x / (8u * per_die), in_group = blockIdx.x - group * 8u * per_die;
     const uint32_t item = group * 8u + (in_group & 7u), part = in_group >> 3, tile = part / roles, role = part - tile * roles;
     if (item >= cut.rows * (kOut ? cut.segments : cut.segments - 1u)) return;
-    const uint32_t seg = item / cut.rows, row = item - seg * cut.rows, env = row / cut.n_heads, head = row - env * cut.n_heads;
-    const Scan& s = scans.s[role];
+    const uint32_t seg = item / cut.rows, dealt = item - seg * cut.rows, block = dealt & ~63u;
+    const uint32_t row = block + 64u <= cut.rows ? block + ((dealt & 7u) << 3) + ((dealt >> 3) & 7u) : dealt, env = row / cut.n_heads, head = row - env * cut.n_heads;
+    const Scan s = scans.s[role];
     if (tile * kWidthZ >= s.b) return;  // (roles whose z is narrower)
     const LinearAttentionHead& hd = cut.heads[head];
     const uint32_t n0 = tile * kWidthZ, col = n0 + wave * 32u + col32;
@@ -320,10 +337,11 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
     Steps<T, A, kThreads> y_steps(s.y.step, s.a), x_steps(s.x.step, s.a);
     Steps<T, kWidthZ, kThreads> z_steps(s.z.step, widthB);
     uint32_t reset = 0;
-    const auto step_of = [&](uint32_t at, uint32_t n) { return s.reverse ? (int64_t)(cut.n_steps - at - n) : (int64_t)at; };  // a chunk's first step in memory
+    const uint32_t has_resets = cut.resets != nullptr;
+    const auto step_of = [&](uint32_t at, uint32_t n) { return again(s.reverse) ? (int64_t)(cut.n_steps - at - n) : (int64_t)at; };  // a chunk's first step in memory
     const auto ask = [&](uint32_t at, uint32_t n) {
         const int64_t t = step_of(at, n);
-        reset = resets && lane < n ? resets[(t + lane) * cut.resets_step] : 0u;
+        reset = again(has_resets) && lane < n ? resets[(t + lane) * cut.resets_step] : 0u;
         y_steps.ask(yh + t * s.y.step, n);
         z_steps.ask(zh + t * s.z.step, n);
         if (kOut) x_steps.ask(xh + t * s.x.step, n);
@@ -335,17 +353,35 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
     const size_t cells = (size_t)s.a * s.b;
     const float* from = kOut ? (seg ? s.before + ((size_t)(seg - 1u) * cut.rows + row) * cells : s.state_in ? s.state_in + row * cells : nullptr) : nullptr;
     const bool whole_state = s.a == (uint32_t)A && n0 + kWidthZ <= s.b;
+    const uint32_t lane_cell = 4 * h32 * s.state_row + col * s.state_col;  // (a state has at most 2^16 cells)
+    if (!from) {
 #pragma unroll
-    for (int db = 0; db < A / 32; ++db)
+        for (int db = 0; db < A / 32; ++db) state[db] = (f32x16)0.0f;
+    } else if (whole_state && s.state_row == 1u) {  // (transposed: a lane's rows are adjacent, four at a time)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
-            state[db][r] = 0.0f;
-            if (from) {
-                state[db][r] = from[min(d, s.a - 1u) * s.state_row + min(col, s.b - 1u) * s.state_col];
-                if (!whole_state && (d >= s.a || col >= s.b)) state[db][r] = 0.0f;
+        for (int db = 0; db < A / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                float v[4];
+                __builtin_memcpy(v, from + (db * 32 + 2 * r) + lane_cell, 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) state[db][r + e] = v[e];
             }
-        }
+    } else if (whole_state) {
+#pragma unroll
+        for (int db = 0; db < A / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) state[db][r] = from[(db * 32 + (r & 3) + 8 * (r >> 2)) * s.state_row + lane_cell];
+    } else {
+#pragma unroll
+        for (int db = 0; db < A / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
+                const float v = from[min(d, s.a - 1u) * s.state_row + min(col, s.b - 1u) * s.state_col];
+                state[db][r] = d < s.a && col < s.b ? v : 0.0f;
+            }
+    }
     __syncthreads();
 
     // the factors of P: position i is a lane's column, j its rows
@@ -354,12 +390,13 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int j = (r & 3) + 8 * (r >> 2) + 4 * (int)h32, gap = s.reverse ? j - (int)col32 : (int)col32 - j;
-            near[r] = gap >= 0 ? s.out_scale * s.key_scale * pw[gap] : 0.0f;
+            near[r] = s.out_scale * s.key_scale * pw[max(gap, 0)];
         }
 
     uint32_t singles = 0, turn = 0;  // steps still to be taken one by one
     bool uncut = true, weights_plain = false;
     for (uint32_t at = begin; at < end;) {
+        const bool reverse = again(s.reverse) != 0u;
         const uint32_t n = singles ? 1u : min((uint32_t)C, end - at);
         const int64_t t = step_of(at, n);
         if (!kAhead) ask(at, n);
@@ -370,7 +407,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
         if (most.infinite()) flag[turn & 1u] = 1;
         const uint64_t m = __ballot(reset != 0u);
         __syncthreads();
-        const bool broken = flag[turn & 1u] != 0;
+        const bool broken = __builtin_amdgcn_readfirstlane(flag[turn & 1u]) != 0;
         if (threadIdx.x == 0) flag[(turn + 1u) & 1u] = 0;
         ++turn;
         if (broken && n > 1) {
@@ -381,12 +418,18 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
         }
         const uint32_t after = at + n;
         if (singles) --singles;
-        if (kAhead && after < end) ask(after, singles ? 1u : min((uint32_t)C, end - after));
+        if (kAhead && after < end) {
+            ask(after, singles ? 1u : min((uint32_t)C, end - after));
+        } else {
+            y_steps.forget();
+            z_steps.forget();
+            x_steps.forget();
+        }
         // what position `lane` adds to the state; the same for every whole chunk in which no episode begins
         const bool plain = n == (uint32_t)C && m == 0;
         if (!plain || !weights_plain) {
-            const bool stays = s.reverse ? (m & up_to(lane)) == 0 : (m & ~up_to(lane)) == 0;
-            weight[lane] = lane < n && stays ? s.key_scale * pw[s.reverse ? lane + 1u : n - 1u - lane] : 0.0f;
+            const bool stays = reverse ? (m & up_to(lane)) == 0 : (m & ~up_to(lane)) == 0;
+            weight[lane] = lane < n && stays ? s.key_scale * pw[reverse ? lane + 1u : n - 1u - lane] : 0.0f;
             weights_plain = plain;
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -402,9 +445,9 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
                     acc = Parts<T, 2>(half(state[db], k)).on_the_left(along(xs + col32 * kStrideA + db * 32 + k * 16, h32), acc);
-            acc *= s.out_scale * pw[s.reverse ? (col32 < n ? n - 1u - col32 : 0u) : col32 + 1u];
+            acc *= s.out_scale * pw[reverse ? (col32 < n ? n - 1u - col32 : 0u) : col32 + 1u];
             if (m) {
-                const bool into = s.reverse ? (m & ~up_to(col32)) == 0 : (m & up_to(col32)) == 0;
+                const bool into = reverse ? (m & ~up_to(col32)) == 0 : (m & up_to(col32)) == 0;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[r] = into ? acc[r] : 0.0f;
             }
@@ -413,18 +456,15 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             f32x16 p = (f32x16)0.0f;
 #pragma unroll
             for (int k = 0; k < A / 16; ++k) p = mma(along(ys + col32 * kStrideA + k * 16, h32), along(xs + col32 * kStrideA + k * 16, h32), p);
-            // (a choice and no product with 0: an overflow in a pair that does not count stays out)
+            // the positions that reach i, [first, past): j <= i and no episode begins in (j, i]; mirrored in reverse.  (A choice and no product with 0:
+            // an overflow in a pair that does not count stays out.)
+            const uint64_t upto = m & up_to(col32), later = m & ~up_to(col32);
+            const uint32_t first = reverse ? col32 : upto ? 63u - (uint32_t)__builtin_clzll(upto) : 0u;
+            const uint32_t past = reverse ? (later ? (uint32_t)__builtin_ctzll(later) : 64u) : col32 + 1u;
+            uint32_t lowest = 4u * h32 - first;
+            asm volatile("" : "+v"(lowest));  // (or 16 sums with h32 are kept from chunk to chunk)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] = near[r] != 0.0f ? p[r] * near[r] : 0.0f;
-            if (m) {
-                // no episode begins in (j, i]
-                const uint64_t upto = m & up_to(col32), later = m & ~up_to(col32);
-                const uint32_t first = s.reverse || !upto ? 0u : 63u - (uint32_t)__builtin_clzll(upto), past = s.reverse && later ? (uint32_t)__builtin_ctzll(later) : 64u;
-                uint32_t lowest = 4u * h32 - first;
-                asm volatile("" : "+v"(lowest));  // (or 16 sums with h32 are kept from chunk to chunk)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] : 0.0f;
-            }
+            for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] * near[r] : 0.0f;
             part_of_chunk();
 #pragma unroll
             for (int k = 0; k < 2; ++k) acc = Parts<T, 2>(half(p, k)).on_the_right(across(zs + k * 16 * kStrideZ + wave * 32u, kStrideZ, lane), acc);
@@ -481,14 +521,20 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
 
     float* to = kOut ? (seg + 1u == cut.segments && s.state_out ? s.state_out + row * cells : nullptr)
                      : (role ? local1 : local0) + ((size_t)seg * cut.rows + row) * cells;
-    if (to)
+    if (to && whole_state) {
+#pragma unroll
+        for (int db = 0; db < A / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) to[(db * 32 + (r & 3) + 8 * (r >> 2)) * s.state_row + lane_cell] = state[db][r];
+    } else if (to && col < s.b) {
 #pragma unroll
         for (int db = 0; db < A / 32; ++db)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
-                if (whole_state || (d < s.a && col < s.b)) to[d * s.state_row + col * s.state_col] = state[db][r];
+                const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2);
+                if (d + 4 * h32 < s.a) to[d * s.state_row + lane_cell] = state[db][r];
             }
+    }
     if (!kOut && tile == 0 && threadIdx.x == 0) (role ? whole1 : whole0)[seg * cut.rows + row] = uncut ? 1u : 0u;
 }
 
@@ -503,10 +549,22 @@ __global__ __launch_bounds__(256) void join_kernel(const Cut cut, uint32_t cells
     const double g = exp(cut.heads[row % cut.n_heads].log_decay * (double)cut.seg_steps);
     const float keep = (float)g, rest = (float)(g - (double)keep);
     float v = in ? in[(size_t)row * cells + i] : 0.0f;
-    for (uint32_t k = 0; k + 1u < cut.segments; ++k) {
-        float* p = local + ((size_t)k * cut.rows + row) * cells + i;
-        v = *p + (whole[(size_t)k * cut.rows + row] ? __builtin_fmaf(v, keep, v * rest) : 0.0f);
-        *p = v;
+    // (eight segments' requests at a time: one after the other they take 0.3 us each)
+    for (uint32_t k0 = 0; k0 + 1u < cut.segments; k0 += 8u) {
+        float own[8];
+        uint32_t through[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8u; ++k) {
+            const size_t at = (size_t)min(k0 + k, cut.segments - 2u) * cut.rows + row;
+            own[k] = local[at * cells + i];
+            through[k] = whole[at];
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 8u; ++k) {
+            if (k0 + k + 1u >= cut.segments) break;
+            v = own[k] + (through[k] ? __builtin_fmaf(v, keep, v * rest) : 0.0f);
+            local[((size_t)(k0 + k) * cut.rows + row) * cells + i] = v;
+        }
     }
 }
 
@@ -548,11 +606,20 @@ int launched(std::string& err) {
 // Wavefronts of a workgroup: enough for z, four at most, and no fewer than it takes to bring the steps of long heads.
 uint32_t waves_of(uint32_t a, uint32_t b) { return a > 128u ? 4u : b <= 32u && a <= 64u ? 1u : b <= 64u ? 2u : 4u; }
 
-// Segments of a rollout's steps: as many as it takes to give each compute unit two workgroups, of four chunks at least.
+uint32_t width_of(uint32_t a) { return a <= 32u ? 32u : a <= 64u ? 64u : a <= 128u ? 128u : 256u; }
+
+// Segments of a rollout's steps: as many as it takes to fill the device (a compute unit holds 12 wavefronts of the narrower kernels, 8 of those of 128 and 4 of
+// those of 256), of two chunks at least, and of one for every 4096 cells of a state: a segment costs its state, written, joined and read.  us with a
+// workgroup for each place / with two for each compute unit: 30 x 2000 with 8 heads of 64 131 / 198, 64 x 1000 with 4 of 32 50 / 78, 4 x 1000 with 3 of 96 x 48 in
+// fp32 62 / 86; 16 x 512 with 16 of 128 x 96, whose two are all there is room for, 126, with four 153.
 uint32_t segments_of(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, uint32_t roles, uint32_t* seg_steps) {
-    const uint64_t chunks = ((uint64_t)n_steps + C - 1u) / C, rows = (uint64_t)n_envs * c.n_heads * roles;
-    uint64_t want = 2ull * c.n_cus / rows;
-    if (want > chunks / 4u) want = chunks / 4u;
+    const uint32_t a = roles > 1u && c.dv > c.dk ? c.dv : c.dk, b = roles > 1u && c.dk > c.dv ? c.dk : c.dv;
+    const uint32_t width = width_of(a), waves = waves_of(a, b), tiles = (b + waves * 32u - 1u) / (waves * 32u);
+    const uint64_t places = (uint64_t)c.n_cus * ((width <= 64u ? 12u : width <= 128u ? 8u : 4u) / waves);
+    const uint64_t chunks = ((uint64_t)n_steps + C - 1u) / C, rows = (uint64_t)n_envs * c.n_heads * roles * tiles;
+    const uint64_t least = c.dk * c.dv > 2u * 4096u ? c.dk * c.dv / 4096u : 2u;
+    uint64_t want = places / rows;
+    if (want > chunks / least) want = chunks / least;
     if (want < 2u) {
         *seg_steps = n_steps;
         return 1u;
@@ -615,7 +682,7 @@ Cut cut_of(const LinearAttentionConsts& c, const pxr_rollout& r, uint32_t roles,
     cut.rows = r.n_envs * c.n_heads;
     cut.n_steps = r.n_steps;
     cut.segments = segments_of(c, r.n_envs, r.n_steps, roles, &cut.seg_steps);
-    cut.width = a <= 32u ? 32u : a <= 64u ? 64u : a <= 128u ? 128u : 256u;
+    cut.width = width_of(a);
     cut.waves = waves_of(a, b);
     cut.tiles = (b + cut.waves * 32u - 1u) / (cut.waves * 32u);
     cut.heads = c.heads;
