@@ -233,7 +233,7 @@ struct Steps {
     static_assert(kThreads % kPerRow == 0);
     uint32_t row, col, d;
     int64_t step, offset;  // values from row to row; the lane's first vector from the chunk's first value
-    uint4 v[kCount];
+    u32x4 v[kCount];
 
     __device__ __forceinline__ Steps(int64_t step, uint32_t d) : row(threadIdx.x / kPerRow), col(threadIdx.x % kPerRow * N), d(d), step(step) {
         offset = (int64_t)row * step + (d < N ? 0u : min(col, d - N));
@@ -252,7 +252,7 @@ struct Steps {
     // What was asked for has been put; nothing is in flight.  (Without this the registers would be kept, and copied, from chunk to chunk.)
     __device__ __forceinline__ void forget() {
 #pragma unroll
-        for (uint32_t i = 0; i < kCount; ++i) asm volatile("" : "=v"(v[i].x), "=v"(v[i].y), "=v"(v[i].z), "=v"(v[i].w));
+        for (uint32_t i = 0; i < kCount; ++i) asm volatile("" : "=v"(v[i]));
     }
     // The tile's rows past n are zeros.  kCheck: collects bit patterns.
     template <bool kCheck>
@@ -271,16 +271,13 @@ struct Steps {
         for (uint32_t i = 0; i < kCount; ++i) {
             const uint32_t r = row + i * kRowsEach;
             if (C * kPerRow % kThreads && r >= (uint32_t)C) continue;
-            uint4 w = v[i];
-            if (n < (uint32_t)C && r >= n) w = make_uint4(0, 0, 0, 0);
-            if (kCheck) {
-                most.with(w.x);
-                most.with(w.y);
-                most.with(w.z);
-                most.with(w.w);
-            }
+            u32x4 w = v[i];
+            if (n < (uint32_t)C && r >= n) w = u32x4{0, 0, 0, 0};
+            if (kCheck)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) most.with(w[k]);
             if (col + N <= d) {
-                *reinterpret_cast<uint4*>(tile + r * kStride + col) = w;
+                *reinterpret_cast<u32x4*>(tile + r * kStride + col) = w;
             } else if (col < d) {
                 T e[N];
                 __builtin_memcpy(e, &w, 16);
@@ -290,9 +287,6 @@ struct Steps {
         }
     }
 };
-
-// Nothing moves across: the compiler would otherwise begin the LDS reads of all products at once, and hold what they bring.
-__device__ __forceinline__ void part_of_chunk() { __builtin_amdgcn_sched_barrier(0); }
 
 // Positions of a chunk up to and including i, as bits.
 __device__ __forceinline__ uint64_t up_to(uint32_t i) { return (2ull << i) - 1ull; }
@@ -393,6 +387,9 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             near[r] = s.out_scale * s.key_scale * pw[max(gap, 0)];
         }
 
+    // (read, and there, before the loop: a wait for them inside it would be one for the steps asked for ahead as well)
+    const auto there = [](float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); };
+    const float decay = there(hd.decay), decay_rest = there(hd.decay_rest), decay_chunk = there(hd.decay_chunk), decay_chunk_rest = there(hd.decay_chunk_rest);
     uint32_t singles = 0, turn = 0;  // steps still to be taken one by one
     bool uncut = true, weights_plain = false;
     for (uint32_t at = begin; at < end;) {
@@ -436,7 +433,6 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
 
-        part_of_chunk();
         if constexpr (kOut) {
             f32x16 acc = (f32x16)0.0f;
             // out^T = S^T x^T, columns = steps
@@ -451,7 +447,6 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[r] = into ? acc[r] : 0.0f;
             }
-            part_of_chunk();
             // P^T, then out^T += z^T P^T
             f32x16 p = (f32x16)0.0f;
 #pragma unroll
@@ -465,10 +460,8 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             asm volatile("" : "+v"(lowest));  // (or 16 sums with h32 are kept from chunk to chunk)
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] * near[r] : 0.0f;
-            part_of_chunk();
 #pragma unroll
             for (int k = 0; k < 2; ++k) acc = Parts<T, 2>(half(p, k)).on_the_right(across(zs + k * 16 * kStrideZ + wave * 32u, kStrideZ, lane), acc);
-            part_of_chunk();
             if (col32 < n) {
                 T* o = oh + (t + col32) * s.out.step + (n0 + wave * 32u);
 #pragma unroll
@@ -493,11 +486,10 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             }
         }
 
-        part_of_chunk();
         // S <- g^n S + y^T (weights z)
         if (m == 0) {
-            const float keep = n == (uint32_t)C ? hd.decay_chunk : n == 1u ? hd.decay : pw[n];
-            const float keep_rest = n == (uint32_t)C ? hd.decay_chunk_rest : n == 1u ? hd.decay_rest : 0.0f;
+            const float keep = n == (uint32_t)C ? decay_chunk : n == 1u ? decay : pw[n];
+            const float keep_rest = n == (uint32_t)C ? decay_chunk_rest : n == 1u ? decay_rest : 0.0f;
 #pragma unroll
             for (int db = 0; db < A / 32; ++db)
 #pragma unroll
@@ -509,7 +501,6 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
         }
 #pragma unroll
         for (int k = 0; k < C / 16; ++k) {
-            part_of_chunk();
             const Frag<T> z = across(zs + k * 16 * kStrideZ + wave * 32u, kStrideZ, lane);
             const Parts<T, 3> zp(values(z) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
 #pragma unroll
