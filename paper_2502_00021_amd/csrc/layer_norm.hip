@@ -13,6 +13,9 @@
 //   up to 256     a wavefront, two or four vectors a lane
 //   up to 8192    a workgroup of 512 or 1024 threads
 //   more          a workgroup that reads the row again for each sum (from the caches, mostly)
+// What leaves is not read again by the kernel and goes past the caches that it would push x out of (524288 x 64 bfloat16 31 -> 24 us, 4096 x 30752 146 -> 110;
+// requests that go past them as well are slower where x lies in them).
+//
 // Workgroups are persistent and walk the rows, so that weights and biases are read once by a wavefront, or once for four rows by a workgroup:
 // in 32 bits they are twice the bytes of a bfloat16 row, each.  The sums over rows of the backward pass stay in registers as well, and
 // leave once for each workgroup; a second kernel adds the workgroups' sums in their order, so that equal inputs give equal bits.
@@ -28,6 +31,8 @@ __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __bf16* p) { return (float)*p; }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__bf16* p, float v) { *p = (__bf16)v; }  // round to nearest even
+
+typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));  // at the address of any value
 
 // 16 bytes of a row: 4 or 8 values, as they came.  Rows may begin at any element: the memory takes 16-byte requests at any address.
 template <class T>
@@ -68,7 +73,9 @@ struct Vec {
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = (T)f[e];  // round to nearest even
         if (from == 0 && to >= N) {
-            __builtin_memcpy(p, v, 16);
+            any_u32x4 w;
+            __builtin_memcpy(&w, v, 16);
+            __builtin_nontemporal_store(w, reinterpret_cast<any_u32x4*>(p));
             return;
         }
 #pragma unroll

@@ -288,6 +288,8 @@ struct Steps {
     }
 };
 
+typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));  // at the address of any value
+
 // Positions of a chunk up to and including i, as bits.
 __device__ __forceinline__ uint64_t up_to(uint32_t i) { return (2ull << i) - 1ull; }
 
@@ -433,6 +435,9 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
 
+        const auto z_of = [&](int k) { return across(zs + k * 16 * kStrideZ + wave * 32u, kStrideZ, lane); };
+        Frag<T> z[2];
+        if (sizeof(T) == 2) z[0] = z_of(0), z[1] = z_of(1);
         if constexpr (kOut) {
             f32x16 acc = (f32x16)0.0f;
             // out^T = S^T x^T, columns = steps
@@ -461,23 +466,45 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] * near[r] : 0.0f;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) acc = Parts<T, 2>(half(p, k)).on_the_right(across(zs + k * 16 * kStrideZ + wave * 32u, kStrideZ, lane), acc);
-            if (col32 < n) {
+            for (int k = 0; k < 2; ++k) acc = Parts<T, 2>(half(p, k)).on_the_right(sizeof(T) == 2 ? z[k] : z_of(k), acc);
+            if constexpr (sizeof(T) == 2) {
+                // The outputs take the place of the wavefront's own columns of z in LDS (z itself is in registers), so that they leave as 16 bytes a lane,
+                // rows of 64 bytes, past the caches: they are not read again (512 x 256 186 -> 171 us; parts of rows past the caches 345).
+                __bf16* own = zs + wave * 32u;
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    uint32_t* w = reinterpret_cast<uint32_t*>(own + col32 * kStrideZ + 2 * r + 4 * h32);
+                    w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r], acc[r + 1]}, bf16x2));
+                    w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r + 2], acc[r + 3]}, bf16x2));
+                }
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                const uint32_t c = lane % 4u * 8u, have = min(s.b - min(s.b, n0 + wave * 32u), 32u);
+#pragma unroll
+                for (uint32_t i = 0; i < 2; ++i) {
+                    const uint32_t r = i * 16u + lane / 4u;
+                    const any_u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kStrideZ + c);
+                    if (r >= n || c >= have) continue;
+                    T* o = oh + (t + r) * s.out.step + (n0 + wave * 32u + c);
+                    if (c + 8 <= have) {
+                        __builtin_nontemporal_store(v, reinterpret_cast<any_u32x4*>(o));
+                    } else {
+                        T e[8];
+                        __builtin_memcpy(e, &v, 16);
+#pragma unroll
+                        for (uint32_t k = 0; k < 8; ++k)
+                            if (c + k < have) o[k] = e[k];
+                    }
+                }
+            } else if (col32 < n) {
                 T* o = oh + (t + col32) * s.out.step + (n0 + wave * 32u);
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const uint32_t c = 2 * r + 4 * h32;
-                    T v[4];
-                    if constexpr (sizeof(T) == 2) {
-                        const uint32_t w[2] = {__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r], acc[r + 1]}, bf16x2)),
-                                               __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r + 2], acc[r + 3]}, bf16x2))};
-                        __builtin_memcpy(v, w, 8);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = acc[r + e];
-                    }
+                    const f32x4 v = {acc[r], acc[r + 1], acc[r + 2], acc[r + 3]};
                     if (n0 + kWidthZ <= s.b || n0 + wave * 32u + c + 4 <= s.b)
-                        __builtin_memcpy(o + c, v, sizeof(v));
+                        __builtin_memcpy(o + c, &v, sizeof(v));
                     else
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -501,8 +528,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
         }
 #pragma unroll
         for (int k = 0; k < C / 16; ++k) {
-            const Frag<T> z = across(zs + k * 16 * kStrideZ + wave * 32u, kStrideZ, lane);
-            const Parts<T, 3> zp(values(z) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
+            const Parts<T, 3> zp(values(sizeof(T) == 2 ? z[k] : z_of(k)) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
 #pragma unroll
             for (int db = 0; db < A / 32; ++db) state[db] = zp.on_the_right(across(ys + k * 16 * kStrideA + db * 32, kStrideA, lane), state[db]);
         }
