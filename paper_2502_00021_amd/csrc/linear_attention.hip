@@ -317,9 +317,14 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
     T* zs = ys + C * kStrideA;
     T* xs = zs + C * kStrideZ;
     float* pw = reinterpret_cast<float*>(xs + (kOut ? C * kStrideA : 0));  // g^0 .. g^C
-    float* weight = pw + 36 + wave * 64u;                                  // a wavefront's g^(n-1-j)
-    uint32_t* flag = reinterpret_cast<uint32_t*>(pw + 36 + kWaves * 64);   // [2]
+    float* factor = pw + 36;                                               // of P by j - i + 31
+    float* weight = factor + 64 + wave * (uint32_t)C;                      // a wavefront's g^(n-1-j)
+    uint32_t* flag = reinterpret_cast<uint32_t*>(factor + 64 + kWaves * C);   // [2]
     for (uint32_t i = threadIdx.x; i <= (uint32_t)C; i += kThreads) pw[i] = hd.power[i];
+    if (kOut && threadIdx.x < 63u) {
+        const int gap = s.reverse ? (int)threadIdx.x - 31 : 31 - (int)threadIdx.x;
+        factor[threadIdx.x] = gap >= 0 ? s.out_scale * s.key_scale * hd.power[max(gap, 0)] : 0.0f;
+    }
     if (threadIdx.x < 2u) flag[threadIdx.x] = 0;
     const uint32_t widthB = min(s.b - n0, kWidthZ);
     if (s.a < (uint32_t)A || widthB < kWidthZ)
@@ -380,15 +385,14 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
     }
     __syncthreads();
 
-    // the factors of P: position i is a lane's column, j its rows
-    float near[kOut ? 16 : 1];
-    if (kOut)
+    // the factors of P: position i is a lane's column, j its rows.  The narrower kernels, three wavefronts of which share a SIMD's registers, read them
+    // for every chunk (512 x 256 bfloat16 179 -> 169 us; those of 128, two to a SIMD, would lose as much).
+    constexpr bool kFactors = kOut && A > 64;
+    const uint32_t f0 = 31u + 4u * h32 - col32;
+    float factors[kFactors ? 16 : 1];
+    if (kFactors)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int j = (r & 3) + 8 * (r >> 2) + 4 * (int)h32, gap = s.reverse ? j - (int)col32 : (int)col32 - j;
-            near[r] = s.out_scale * s.key_scale * pw[max(gap, 0)];
-        }
-
+        for (int r = 0; r < 16; ++r) factors[kFactors ? r : 0] = factor[f0 + ((r & 3) + 8 * (r >> 2))];
     // (read, and there, before the loop: a wait for them inside it would be one for the steps asked for ahead as well)
     const auto there = [](float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); };
     const float decay = there(hd.decay), decay_rest = there(hd.decay_rest), decay_chunk = there(hd.decay_chunk), decay_chunk_rest = there(hd.decay_chunk_rest);
@@ -428,7 +432,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
         const bool plain = n == (uint32_t)C && m == 0;
         if (!plain || !weights_plain) {
             const bool stays = reverse ? (m & up_to(lane)) == 0 : (m & ~up_to(lane)) == 0;
-            weight[lane] = lane < n && stays ? s.key_scale * pw[reverse ? lane + 1u : n - 1u - lane] : 0.0f;
+            if (lane < (uint32_t)C) weight[lane] = lane < n && stays ? s.key_scale * pw[reverse ? lane + 1u : n - 1u - lane] : 0.0f;
             weights_plain = plain;
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -461,10 +465,10 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             const uint64_t upto = m & up_to(col32), later = m & ~up_to(col32);
             const uint32_t first = reverse ? col32 : upto ? 63u - (uint32_t)__builtin_clzll(upto) : 0u;
             const uint32_t past = reverse ? (later ? (uint32_t)__builtin_ctzll(later) : 64u) : col32 + 1u;
-            uint32_t lowest = 4u * h32 - first;
-            asm volatile("" : "+v"(lowest));  // (or 16 sums with h32 are kept from chunk to chunk)
+            uint32_t lowest = 4u * h32 - first, f = f0;
+            asm volatile("" : "+v"(f), "+v"(lowest));  // (or what they give with 16 numbers is kept from chunk to chunk)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] * near[r] : 0.0f;
+            for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] * (kFactors ? factors[kFactors ? r : 0] : factor[f + ((r & 3) + 8 * (r >> 2))]) : 0.0f;
 #pragma unroll
             for (int k = 0; k < 2; ++k) acc = Parts<T, 2>(half(p, k)).on_the_right(sizeof(T) == 2 ? z[k] : z_of(k), acc);
             if constexpr (sizeof(T) == 2) {
@@ -715,7 +719,7 @@ uint32_t segments_of(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n
 
 template <class T, int A, int kWaves, bool kOut>
 constexpr size_t scan_lds() {
-    return (size_t)C * ((kOut ? 2 : 1) * (A + kPad<T>) + kWaves * 32 + kPad<T>) * sizeof(T) + (36 + kWaves * 64 + 2) * 4;
+    return (size_t)C * ((kOut ? 2 : 1) * (A + kPad<T>) + kWaves * 32 + kPad<T>) * sizeof(T) + (36 + 64 + kWaves * C + 2) * 4;
 }
 
 // Chunks of 256 values take more than the 64 KB of LDS that a launch has by default.
