@@ -29,6 +29,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "pxr_internal.h"
 
 namespace pxr {
@@ -310,7 +312,6 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
     const uint32_t seg = item / cut.rows, dealt = item - seg * cut.rows, block = dealt & ~63u;
     const uint32_t row = block + 64u <= cut.rows ? block + ((dealt & 7u) << 3) + ((dealt >> 3) & 7u) : dealt, env = row / cut.n_heads, head = row - env * cut.n_heads;
     const Scan s = scans.s[role];
-    if (tile * kWidthZ >= s.b) return;  // (roles whose z is narrower)
     const LinearAttentionHead& hd = cut.heads[head];
     const uint32_t n0 = tile * kWidthZ, col = n0 + wave * 32u + col32;
     T* ys = reinterpret_cast<T*>(lds);
@@ -559,30 +560,44 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
     if (!kOut && tile == 0 && threadIdx.x == 0) (role ? whole1 : whole0)[seg * cut.rows + row] = uncut ? 1u : 0u;
 }
 
-// The segments' own states, one after the other, to the states before the segments that follow: one lane per cell of a state.
+// The segments' own states, one after the other, to the states before the segments that follow: one lane per cell of a state.  kBatch segments' requests
+// are on their way while the kBatch before them are added up, as many as there are, 16 at most (89 segments of 8 heads of 64 x 128: 16 at a time 13 us,
+// 8 with none on their way 22; 2 segments of 256 states of 128 x 96, whole pass: 2 or 4 at a time 112 us, 8 120).
+template <uint32_t kBatch>
 __global__ __launch_bounds__(256) void join_kernel(const Cut cut, uint32_t cells, const float* in0, const float* in1, float* local0, float* local1,
-                                                   const uint32_t* whole0, const uint32_t* whole1) {
+                                                   const uint32_t* __restrict__ whole0, const uint32_t* __restrict__ whole1) {
     const uint32_t i = blockIdx.x * 256u + threadIdx.x, row = blockIdx.y;
     if (i >= cells) return;
     const float* in = blockIdx.z ? in1 : in0;
     float* local = blockIdx.z ? local1 : local0;
     const uint32_t* whole = blockIdx.z ? whole1 : whole0;
+    const uint32_t last = cut.segments - 2u;
+    float next[kBatch];
+    uint32_t through_next[kBatch];
+    const auto ask = [&](uint32_t k0) {
+#pragma unroll
+        for (uint32_t k = 0; k < kBatch; ++k) {
+            const size_t at = (size_t)min(k0 + k, last) * cut.rows + row;
+            next[k] = local[at * cells + i];
+            through_next[k] = whole[at];
+        }
+    };
+    ask(0);
+    float v = in ? in[(size_t)row * cells + i] : 0.0f;
     const double g = exp(cut.heads[row % cut.n_heads].log_decay * (double)cut.seg_steps);
     const float keep = (float)g, rest = (float)(g - (double)keep);
-    float v = in ? in[(size_t)row * cells + i] : 0.0f;
-    // (eight segments' requests at a time: one after the other they take 0.3 us each)
-    for (uint32_t k0 = 0; k0 + 1u < cut.segments; k0 += 8u) {
-        float own[8];
-        uint32_t through[8];
+    for (uint32_t k0 = 0; k0 <= last; k0 += kBatch) {
+        float own[kBatch];
+        uint32_t through[kBatch];
 #pragma unroll
-        for (uint32_t k = 0; k < 8u; ++k) {
-            const size_t at = (size_t)min(k0 + k, cut.segments - 2u) * cut.rows + row;
-            own[k] = local[at * cells + i];
-            through[k] = whole[at];
+        for (uint32_t k = 0; k < kBatch; ++k) {
+            own[k] = next[k];
+            through[k] = through_next[k];
         }
+        if (k0 + kBatch <= last) ask(k0 + kBatch);
 #pragma unroll
-        for (uint32_t k = 0; k < 8u; ++k) {
-            if (k0 + k + 1u >= cut.segments) break;
+        for (uint32_t k = 0; k < kBatch; ++k) {
+            if (k0 + k > last) break;
             v = own[k] + (through[k] ? __builtin_fmaf(v, keep, v * rest) : 0.0f);
             local[((size_t)(k0 + k) * cut.rows + row) * cells + i] = v;
         }
@@ -696,17 +711,25 @@ uint32_t waves_of(uint32_t a, uint32_t b) { return a > 128u ? 4u : b <= 32u && a
 
 uint32_t width_of(uint32_t a) { return a <= 32u ? 32u : a <= 64u ? 64u : a <= 128u ? 128u : 256u; }
 
+// Whether one launch takes the three scans of the backward pass: the steps that they share are then read once.  Keys and values of different widths would all
+// take the kernel for the larger of both (256 x 128 with 8 heads of 64 x 128 407 us together, 196 apart; 20000 steps of them 257 / 187; 4 x 1000 with 3
+// heads of 96 x 48 in fp32, which do not fill the device, 83 / 92).
+bool together(const LinearAttentionConsts& c) { return width_of(c.dk) == width_of(c.dv) && waves_of(c.dk, c.dv) == waves_of(c.dv, c.dk); }
+
 // Segments of a rollout's steps: as many as it takes to fill the device (a compute unit holds 12 wavefronts of the narrower kernels, 8 of those of 128 and 4 of
 // those of 256), of two chunks at least, and of one for every 4096 cells of a state: a segment costs its state, written, joined and read.  us with a
 // workgroup for each place / with two for each compute unit: 30 x 2000 with 8 heads of 64 131 / 198, 64 x 1000 with 4 of 32 50 / 78, 4 x 1000 with 3 of 96 x 48 in
 // fp32 62 / 86; 16 x 512 with 16 of 128 x 96, whose two are all there is room for, 126, with four 153.
-uint32_t segments_of(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, uint32_t roles, uint32_t* seg_steps) {
-    const uint32_t a = roles > 1u && c.dv > c.dk ? c.dv : c.dk, b = roles > 1u && c.dk > c.dv ? c.dk : c.dv;
-    const uint32_t width = width_of(a), waves = waves_of(a, b), tiles = (b + waves * 32u - 1u) / (waves * 32u);
-    const uint64_t places = (uint64_t)c.n_cus * ((width <= 64u ? 12u : width <= 128u ? 8u : 4u) / waves);
-    const uint64_t chunks = ((uint64_t)n_steps + C - 1u) / C, rows = (uint64_t)n_envs * c.n_heads * roles * tiles;
+uint32_t segments_of(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, bool backward, uint32_t* seg_steps) {
+    const auto fit = [&](uint32_t a, uint32_t b, uint64_t roles) {
+        const uint32_t width = width_of(a), waves = waves_of(a, b), tiles = (b + waves * 32u - 1u) / (waves * 32u);
+        const uint64_t places = (uint64_t)c.n_cus * ((width <= 64u ? 12u : width <= 128u ? 8u : 4u) / waves);
+        return places / ((uint64_t)n_envs * c.n_heads * roles * tiles);
+    };
+    uint64_t want = fit(c.dk, c.dv, !backward ? 1u : together(c) ? 3u : 1u);
+    if (backward && !together(c)) want = std::min(want, fit(c.dv, c.dk, 2u));
+    const uint64_t chunks = ((uint64_t)n_steps + C - 1u) / C;
     const uint64_t least = c.dk * c.dv > 2u * 4096u ? c.dk * c.dv / 4096u : 2u;
-    uint64_t want = places / rows;
     if (want > chunks / least) want = chunks / least;
     if (want < 2u) {
         *seg_steps = n_steps;
@@ -764,12 +787,19 @@ void enqueue(uint32_t dtype, const Scan* s, uint32_t roles, const Cut& cut, floa
         enqueue_as<__bf16, kOut>(s, roles, cut, local, whole, st);
 }
 
-Cut cut_of(const LinearAttentionConsts& c, const pxr_rollout& r, uint32_t roles, uint32_t a, uint32_t b) {
+void join(const Cut& cut, uint32_t cells, uint32_t sets, const float* in0, const float* in1, float* const* local, uint32_t* const* whole, hipStream_t st) {
+    const dim3 grid((cells + 255u) / 256u, cut.rows, sets);
+    const uint32_t states = cut.segments - 1u;
+    const auto kernel = states > 8u ? join_kernel<16> : states > 4u ? join_kernel<8> : states > 2u ? join_kernel<4> : join_kernel<2>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, cut, cells, in0, in1, local[0], local[1], whole[0], whole[1]);
+}
+
+Cut cut_of(const LinearAttentionConsts& c, const pxr_rollout& r, bool backward, uint32_t a, uint32_t b) {
     Cut cut{};
     cut.n_heads = c.n_heads;
     cut.rows = r.n_envs * c.n_heads;
     cut.n_steps = r.n_steps;
-    cut.segments = segments_of(c, r.n_envs, r.n_steps, roles, &cut.seg_steps);
+    cut.segments = segments_of(c, r.n_envs, r.n_steps, backward, &cut.seg_steps);
     cut.width = width_of(a);
     cut.waves = waves_of(a, b);
     cut.tiles = (b + cut.waves * 32u - 1u) / (cut.waves * 32u);
@@ -800,7 +830,7 @@ int prepare_linear_attention_kernels(std::string& err) {
 
 size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, bool backward) {
     uint32_t steps;
-    const uint32_t segments = segments_of(c, n_envs, n_steps, backward ? 3u : 1u, &steps);
+    const uint32_t segments = segments_of(c, n_envs, n_steps, backward, &steps);
     const size_t one = ((state_bytes(c, n_envs, segments) + 15u) & ~(size_t)15u) + whole_bytes(c, n_envs, segments);
     return backward ? 2u * one : one;
 }
@@ -808,14 +838,13 @@ size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t n_env
 int launch_linear_attention_forward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& out, float* state_out, void* ws,
                                     void* stream, std::string& err) {
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const Cut cut = cut_of(c, r, 1u, c.dk, c.dv);
+    const Cut cut = cut_of(c, r, false, c.dk, c.dv);
     Scan s{r.q, r.k, r.v, out, c.dk, c.dv, r.d_state, state_out, c.dv, 1u, nullptr, c.scale, 1.0f, 0u};
     float* local[2] = {static_cast<float*>(ws), nullptr};
     uint32_t* whole[2] = {reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + ((state_bytes(c, r.n_envs, cut.segments) + 15u) & ~(size_t)15u)), nullptr};
     if (cut.segments > 1u) {
         enqueue<false>(r.dtype, &s, 1u, cut, local, whole, st);
-        hipLaunchKernelGGL(join_kernel, dim3((c.dk * c.dv + 255u) / 256u, cut.rows, 1), dim3(256), 0, st, cut, c.dk * c.dv, r.d_state, nullptr, local[0], nullptr,
-                           whole[0], nullptr);
+        join(cut, c.dk * c.dv, 1u, r.d_state, nullptr, local, whole, st);
         s.before = local[0];
     }
     enqueue<true>(r.dtype, &s, 1u, cut, local, whole, st);
@@ -826,24 +855,27 @@ int launch_linear_attention_backward(const LinearAttentionConsts& c, const pxr_r
                                      const pxr_tokens& dq, const pxr_tokens& dk, const pxr_tokens& dv, float* dstate, void* ws,
                                      void* stream, std::string& err) {
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const uint32_t most = c.dk > c.dv ? c.dk : c.dv;
-    const Cut cut = cut_of(c, r, 3u, most, most);
-    const size_t states = (state_bytes(c, r.n_envs, cut.segments) + 15u) & ~(size_t)15u, words = whole_bytes(c, r.n_envs, cut.segments);
+    const Cut cut_v = cut_of(c, r, true, c.dk, c.dv), cut_k = cut_of(c, r, true, c.dv, c.dk);
+    const size_t states = (state_bytes(c, r.n_envs, cut_v.segments) + 15u) & ~(size_t)15u, words = whole_bytes(c, r.n_envs, cut_v.segments);
     char* w = static_cast<char*>(ws);
     float* local[2] = {reinterpret_cast<float*>(w), reinterpret_cast<float*>(w + states + words)};
     uint32_t* whole[2] = {reinterpret_cast<uint32_t*>(w + states), reinterpret_cast<uint32_t*>(w + 2u * states + words)};
-    if (cut.segments > 1u) {
+    if (cut_v.segments > 1u) {
         // the states [dk][dv] of the forward scan and of the reverse one, which dk and dv share
         const Scan both[2] = {Scan{r.q, r.k, r.v, dout, c.dk, c.dv, nullptr, nullptr, c.dv, 1u, nullptr, 1.0f, 1.0f, 0u},
                               Scan{r.k, r.q, dout, dout, c.dk, c.dv, nullptr, nullptr, c.dv, 1u, nullptr, 1.0f, c.scale, 1u}};
-        enqueue<false>(r.dtype, both, 2u, cut_of(c, r, 3u, c.dk, c.dv), local, whole, st);
-        hipLaunchKernelGGL(join_kernel, dim3((c.dk * c.dv + 255u) / 256u, cut.rows, 2), dim3(256), 0, st, cut, c.dk * c.dv, r.d_state, dstate_out, local[0],
-                           local[1], whole[0], whole[1]);
+        enqueue<false>(r.dtype, both, 2u, cut_v, local, whole, st);
+        join(cut_v, c.dk * c.dv, 2u, r.d_state, dstate_out, local, whole, st);
     }
     const Scan three[3] = {Scan{dout, r.v, r.k, dq, c.dv, c.dk, r.d_state, nullptr, 1u, c.dv, local[0], c.scale, 1.0f, 0u},
                            Scan{r.v, dout, r.q, dk, c.dv, c.dk, dstate_out, nullptr, 1u, c.dv, local[1], 1.0f, c.scale, 1u},
                            Scan{r.k, r.q, dout, dv, c.dk, c.dv, dstate_out, dstate, c.dv, 1u, local[1], 1.0f, c.scale, 1u}};
-    enqueue<true>(r.dtype, three, 3u, cut, local, whole, st);
+    if (together(c)) {
+        enqueue<true>(r.dtype, three, 3u, cut_k, local, whole, st);
+    } else {
+        enqueue<true>(r.dtype, three, 2u, cut_k, local, whole, st);
+        enqueue<true>(r.dtype, three + 2, 1u, cut_v, local, whole, st);
+    }
     return launched(err);
 }
 
