@@ -30,6 +30,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pxr_internal.h"
 
@@ -42,6 +43,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
@@ -86,56 +88,82 @@ __device__ __forceinline__ T* head_of(const pxr_tokens& t, uint32_t e, uint32_t 
 
 // ---- operands: eight values of the summed axis, positions 4h + {0..3, 8..11} of a run of 16
 
-template <class T>
-struct Frag;
-template <>
-struct Frag<__bf16> {
-    bf16x8 v;
-};
-template <>
-struct Frag<float> {
-    f32x8 v;
+// Eight values as the sum of n bfloat16 operands, the largest first.
+template <int n>
+struct Parts {
+    bf16x8 part[n];
 };
 
-__device__ __forceinline__ f32x16 mma(const Frag<__bf16>& a, const Frag<__bf16>& b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x16 mma(const Frag<float>& a, const Frag<float>& b, f32x16 c) {
+// fp32 values to n parts: their sum, up to the rounding of the last.
+template <int n>
+__device__ __forceinline__ Parts<n> split(f32x8 rest) {
+    Parts<n> f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+    for (int k = 0; k < n; ++k) {
+        u32x4 w;  // (two values an instruction: conversions of eight at once come out one by one)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{rest[2 * i], rest[2 * i + 1]}, bf16x2));  // round to nearest even
+            if (k + 1 < n) {
+                rest[2 * i] -= __uint_as_float(w[i] << 16);
+                rest[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        }
+        f.part[k] = __builtin_bit_cast(bf16x8, w);
+    }
+    return f;
+}
+
+// Products of parts whose share of the result is above the last part's rounding, the smallest first.
+template <int n, int m>
+__device__ __forceinline__ f32x16 mma(const Parts<n>& a, const Parts<m>& b, f32x16 c) {
+#pragma unroll
+    for (int order = (n > m ? n : m) - 1; order >= 0; --order)
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+            if (order - i >= 0 && order - i < m) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.part[i], b.part[order - i], c, 0, 0, 0);
     return c;
 }
 
-// From a row that lies along the summed axis: p = the row's run of 16 in LDS.
-__device__ __forceinline__ Frag<__bf16> along(const __bf16* p, uint32_t h) {
-    const bf16x4 lo = *reinterpret_cast<const bf16x4*>(p + 4 * h), hi = *reinterpret_cast<const bf16x4*>(p + 8 + 4 * h);
-    return {__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)};
-}
-__device__ __forceinline__ Frag<float> along(const float* p, uint32_t h) {
-    const f32x4 lo = *reinterpret_cast<const f32x4*>(p + 4 * h), hi = *reinterpret_cast<const f32x4*>(p + 8 + 4 * h);
-    return {__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)};
+// From rows that lie along the summed axis: p = the row's run of 16 in LDS, `plane` values from part to part.
+template <int n>
+__device__ __forceinline__ Parts<n> along(const __bf16* p, uint32_t plane, uint32_t h) {
+    Parts<n> f;
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+        const bf16x4 lo = *reinterpret_cast<const bf16x4*>(p + k * plane + 4 * h), hi = *reinterpret_cast<const bf16x4*>(p + k * plane + 8 + 4 * h);
+        f.part[k] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    return f;
 }
 
 // From 16 rows that lie across it: p = the first row's 32 columns in LDS, `stride` values from row to row; the lane's column is lane % 32.
-__device__ __forceinline__ Frag<__bf16> across(const __bf16* p, uint32_t stride, uint32_t lane) {
+__device__ __forceinline__ bf16x8 across(const __bf16* p, uint32_t stride, uint32_t lane) {
     // The transposing read: lane i of 16 gives the address of four columns of row i / 4 and gets four rows of column i.
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const uint32_t h = lane >> 5, i = lane & 15u;
     const __bf16* q = p + (4 * h + (i >> 2)) * stride + (lane & 16u) + 4 * (i & 3u);
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + 8 * stride));
-    return {__builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7))};
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
-__device__ __forceinline__ Frag<float> across(const float* p, uint32_t stride, uint32_t lane) {
+__device__ __forceinline__ f32x8 across(const float* p, uint32_t stride, uint32_t lane) {
     const float* q = p + (4 * (lane >> 5)) * stride + (lane & 31u);
-    Frag<float> f;
+    f32x8 f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.v[e] = q[(e & 3) * stride + (e >> 2) * 8 * stride];
+    for (int e = 0; e < 8; ++e) f[e] = q[(e & 3) * stride + (e >> 2) * 8 * stride];
+    return f;
+}
+template <int n>
+__device__ __forceinline__ Parts<n> across(const __bf16* p, uint32_t plane, uint32_t stride, uint32_t lane) {
+    Parts<n> f;
+#pragma unroll
+    for (int k = 0; k < n; ++k) f.part[k] = across(p + k * plane, stride, lane);
     return f;
 }
 
-__device__ __forceinline__ f32x8 values(const Frag<__bf16>& f) {
-    const u32x4 w = __builtin_bit_cast(u32x4, f.v);
+__device__ __forceinline__ f32x8 values(const bf16x8& f) {
+    const u32x4 w = __builtin_bit_cast(u32x4, f);
     f32x8 v;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -144,7 +172,9 @@ __device__ __forceinline__ f32x8 values(const Frag<__bf16>& f) {
     }
     return v;
 }
-__device__ __forceinline__ f32x8 values(const Frag<float>& f) { return f.v; }
+__device__ __forceinline__ f32x8 values(const f32x8& f) { return f; }
+__device__ __forceinline__ Parts<1> parts_of(const bf16x8& f) { return {{f}}; }
+__device__ __forceinline__ Parts<3> parts_of(const f32x8& f) { return split<3>(f); }
 // Half of a product's result in a lane, which is a run of 16 of its rows.
 __device__ __forceinline__ f32x8 half(const f32x16& c, int k) {
     return k ? __builtin_shufflevector(c, c, 8, 9, 10, 11, 12, 13, 14, 15) : __builtin_shufflevector(c, c, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -153,51 +183,16 @@ __device__ __forceinline__ f32x8 eight(const float* lo, const float* hi) {
     return __builtin_shufflevector(*reinterpret_cast<const f32x4*>(lo), *reinterpret_cast<const f32x4*>(hi), 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// fp32 values as an operand: `kParts` bfloat16 operands whose sum they are, up to the rounding of the last, or as they are.
-template <class T, int kParts>
-struct Parts;
-template <int kParts>
-struct Parts<__bf16, kParts> {
-    Frag<__bf16> part[kParts];
-    __device__ __forceinline__ explicit Parts(f32x8 rest) {
-#pragma unroll
-        for (int k = 0; k < kParts; ++k) {
-            u32x4 w;  // (two values an instruction: conversions of eight at once come out one by one)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{rest[2 * i], rest[2 * i + 1]}, bf16x2));  // round to nearest even
-                if (k + 1 < kParts) {
-                    rest[2 * i] -= __uint_as_float(w[i] << 16);
-                    rest[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
-                }
-            }
-            part[k].v = __builtin_bit_cast(bf16x8, w);
-        }
-    }
-    __device__ __forceinline__ f32x16 on_the_left(const Frag<__bf16>& b, f32x16 c) const {
-#pragma unroll
-        for (int k = kParts - 1; k >= 0; --k) c = mma(part[k], b, c);
-        return c;
-    }
-    __device__ __forceinline__ f32x16 on_the_right(const Frag<__bf16>& a, f32x16 c) const {
-#pragma unroll
-        for (int k = kParts - 1; k >= 0; --k) c = mma(a, part[k], c);
-        return c;
-    }
-};
-template <int kParts>
-struct Parts<float, kParts> {
-    Frag<float> all;
-    __device__ __forceinline__ explicit Parts(f32x8 f) : all{f} {}
-    __device__ __forceinline__ f32x16 on_the_left(const Frag<float>& b, f32x16 c) const { return mma(all, b, c); }
-    __device__ __forceinline__ f32x16 on_the_right(const Frag<float>& a, f32x16 c) const { return mma(a, all, c); }
-};
-
 // ---- tiles of steps in LDS: rows of `width` values (a multiple of 32), 16 bytes apart from each other so that 16 rows' words at one column lie in
 // different banks
 
 template <class T>
 constexpr uint32_t kPad = 16 / sizeof(T);
+// Parts of a value of x or y in LDS, and of the fp32 values that are multiplied again.
+template <class T>
+constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
+template <class T>
+constexpr int kAgain = sizeof(T) == 2 ? 2 : 3;
 
 // The largest bit patterns of the values, without their signs.
 template <class T>
@@ -206,7 +201,7 @@ template <>
 struct Most<float> {
     uint32_t m = 0;
     __device__ __forceinline__ void with(uint32_t w) { m = max(m, w & 0x7FFFFFFFu); }
-    __device__ __forceinline__ bool infinite() const { return m >= 0x7F800000u; }
+    __device__ __forceinline__ bool infinite() const { return m >= 0x7F7F8000u; }  // (what rounds to an infinity of bfloat16 among them)
 };
 template <>
 struct Most<__bf16> {
@@ -228,9 +223,11 @@ __device__ __forceinline__ uint32_t again(uint32_t v) {
 // vector has its last vector moved back to its end; rows past the last and vectors past a row's end read what is there instead and are not written,
 // or written as zeros.  The columns past d are zero from the start and nothing writes them.  Rows shorter than a vector are read value by value,
 // when they are written.
-template <class T, int kWidth, int kThreads>
+// kSplit: fp32 values go to LDS as three planes of bfloat16 parts.
+template <class T, int kWidth, int kThreads, bool kSplit>
 struct Steps {
-    static constexpr uint32_t N = 16 / sizeof(T), kPerRow = kWidth / N, kCount = (C * kPerRow + kThreads - 1) / kThreads, kStride = kWidth + kPad<T>;
+    typedef std::conditional_t<kSplit, __bf16, T> E;  // of the tile
+    static constexpr uint32_t N = 16 / sizeof(T), kPerRow = kWidth / N, kCount = (C * kPerRow + kThreads - 1) / kThreads, kStride = kWidth + kPad<E>, kPlane = C * kStride;
     static constexpr uint32_t kRowsEach = kThreads / kPerRow;  // rows that the lanes take together
     static_assert(kThreads % kPerRow == 0);
     uint32_t row, col, d;
@@ -256,16 +253,28 @@ struct Steps {
 #pragma unroll
         for (uint32_t i = 0; i < kCount; ++i) asm volatile("" : "=v"(v[i]));
     }
+    static __device__ __forceinline__ void put_one(E* at, T e) {
+        if constexpr (kSplit) {
+            float rest = e;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                at[k * kPlane] = (__bf16)rest;  // round to nearest even
+                rest -= (float)at[k * kPlane];
+            }
+        } else {
+            *at = e;
+        }
+    }
     // The tile's rows past n are zeros.  kCheck: collects bit patterns.
     template <bool kCheck>
-    __device__ __forceinline__ void put(const T* from, T* tile, uint32_t n, Most<T>& most) {
+    __device__ __forceinline__ void put(const T* from, E* tile, uint32_t n, Most<T>& most) {
         const uint32_t d = again(this->d);
         if (d < N) {
             for (uint32_t i = threadIdx.x; i < C * d; i += kThreads) {
                 const uint32_t r = i / d, c = i - r * d;
                 const T e = r < n ? from[(int64_t)r * step + c] : (T)0.0f;
                 if (kCheck) most.with(sizeof(T) == 4 ? __builtin_bit_cast(uint32_t, (float)e) : __builtin_bit_cast(uint32_t, (float)e) >> 16);
-                tile[r * kStride + c] = e;
+                put_one(tile + r * kStride + c, e);
             }
             return;
         }
@@ -279,12 +288,27 @@ struct Steps {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) most.with(w[k]);
             if (col + N <= d) {
-                *reinterpret_cast<u32x4*>(tile + r * kStride + col) = w;
+                if constexpr (kSplit) {
+                    f32x4 rest = __builtin_bit_cast(f32x4, w);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        u32x2 p;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            p[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{rest[2 * i], rest[2 * i + 1]}, bf16x2));
+                            rest[2 * i] -= __uint_as_float(p[i] << 16);
+                            rest[2 * i + 1] -= __uint_as_float(p[i] & 0xFFFF0000u);
+                        }
+                        *reinterpret_cast<u32x2*>(tile + k * kPlane + r * kStride + col) = p;
+                    }
+                } else {
+                    *reinterpret_cast<u32x4*>(tile + r * kStride + col) = w;
+                }
             } else if (col < d) {
                 T e[N];
                 __builtin_memcpy(e, &w, 16);
 #pragma unroll
-                for (uint32_t k = 0; k < N; ++k) tile[r * kStride + d - N + k] = e[k];
+                for (uint32_t k = 0; k < N; ++k) put_one(tile + r * kStride + d - N + k, e[k]);
             }
         }
     }
@@ -295,13 +319,24 @@ typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));  // 
 // Positions of a chunk up to and including i, as bits.
 __device__ __forceinline__ uint64_t up_to(uint32_t i) { return (2ull << i) - 1ull; }
 
+constexpr uint32_t kLds = 160 * 1024;  // of a compute unit
+
+// LDS of a workgroup.
+constexpr uint32_t scan_lds(uint32_t element, uint32_t width, uint32_t waves, bool out) {
+    return C * ((out ? 2 : 1) * (width + 8) * 2 * (element == 2 ? 1 : 3) + waves * 32 * element + 16) + (36 + 64 + waves * C + 2) * 4;
+}
+
+// Wavefronts that share a SIMD's registers.
+constexpr uint32_t waves_per_simd(uint32_t width, uint32_t element) { return width <= 64u && element == 2u ? 3u : width <= 128u ? 2u : 1u; }
+
 // A (a padded to 32, 64, 128 or 256), kWaves wavefronts; kOut: outputs (else the state after a segment alone, from zeros).
 template <class T, int A, int kWaves, bool kOut>
-__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <= 64 ? 3 : A <= 128 ? 2 : 1))) void scan_kernel(
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(waves_per_simd(A, sizeof(T))))) void scan_kernel(
     const Scans scans, const Cut cut, uint32_t roles, float* local0, float* local1, uint32_t* whole0, uint32_t* whole1) {
     // (requests a chunk ahead take registers; where they do not fit, a chunk's requests go out together when it begins)
-    constexpr bool kAhead = sizeof(T) == 2 && A <= 64;
-    constexpr uint32_t kThreads = kWaves * 64, kWidthZ = kWaves * 32, kStrideA = A + kPad<T>, kStrideZ = kWidthZ + kPad<T>;
+    constexpr bool kAhead = A <= 64;
+    constexpr uint32_t kThreads = kWaves * 64, kWidthZ = kWaves * 32, kStrideA = A + kPad<__bf16>, kStrideZ = kWidthZ + kPad<T>;
+    constexpr uint32_t kPlane = C * kStrideA, kTile = kPlane * kParts<T>;  // of x and y
     extern __shared__ __align__(16) unsigned char lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h32 = lane >> 5, col32 = lane & 31u;
     // Workgroups go to the eight dies in turn: those that read the same steps are eight apart, on one die and behind one L2.  So are eight
@@ -314,10 +349,10 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
     const Scan s = scans.s[role];
     const LinearAttentionHead& hd = cut.heads[head];
     const uint32_t n0 = tile * kWidthZ, col = n0 + wave * 32u + col32;
-    T* ys = reinterpret_cast<T*>(lds);
-    T* zs = ys + C * kStrideA;
-    T* xs = zs + C * kStrideZ;
-    float* pw = reinterpret_cast<float*>(xs + (kOut ? C * kStrideA : 0));  // g^0 .. g^C
+    __bf16* ys = reinterpret_cast<__bf16*>(lds);
+    T* zs = reinterpret_cast<T*>(ys + kTile);
+    __bf16* xs = reinterpret_cast<__bf16*>(zs + C * kStrideZ);
+    float* pw = reinterpret_cast<float*>(xs + (kOut ? kTile : 0));  // g^0 .. g^C
     float* factor = pw + 36;                                               // of P by j - i + 31
     float* weight = factor + 64 + wave * (uint32_t)C;                      // a wavefront's g^(n-1-j)
     uint32_t* flag = reinterpret_cast<uint32_t*>(factor + 64 + kWaves * C);   // [2]
@@ -329,15 +364,15 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
     if (threadIdx.x < 2u) flag[threadIdx.x] = 0;
     const uint32_t widthB = min(s.b - n0, kWidthZ);
     if (s.a < (uint32_t)A || widthB < kWidthZ)
-        for (uint32_t i = threadIdx.x; i < C * (kStrideA * (kOut ? 2 : 1) + kStrideZ) * sizeof(T) / 16u; i += kThreads) reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
+        for (uint32_t i = threadIdx.x; i < (kTile * (kOut ? 2 : 1) * 2 + C * kStrideZ * sizeof(T)) / 16u; i += kThreads) reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
 
     const T *xh = head_of<const T>(s.x, env, head), *yh = head_of<const T>(s.y, env, head), *zh = head_of<const T>(s.z, env, head) + n0;
     T* oh = head_of<T>(s.out, env, head);
     const uint8_t* resets = cut.resets ? cut.resets + (int64_t)env * cut.resets_env : nullptr;
     // the segment's steps in the order in which they are taken; in reverse, position p of the scan is step n_steps - 1 - p
     const uint32_t begin = seg * cut.seg_steps, end = min(begin + cut.seg_steps, cut.n_steps);
-    Steps<T, A, kThreads> y_steps(s.y.step, s.a), x_steps(s.x.step, s.a);
-    Steps<T, kWidthZ, kThreads> z_steps(s.z.step, widthB);
+    Steps<T, A, kThreads, sizeof(T) == 4> y_steps(s.y.step, s.a), x_steps(s.x.step, s.a);
+    Steps<T, kWidthZ, kThreads, false> z_steps(s.z.step, widthB);
     uint32_t reset = 0;
     const uint32_t has_resets = cut.resets != nullptr;
     const auto step_of = [&](uint32_t at, uint32_t n) { return again(s.reverse) ? (int64_t)(cut.n_steps - at - n) : (int64_t)at; };  // a chunk's first step in memory
@@ -388,7 +423,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
 
     // the factors of P: position i is a lane's column, j its rows.  The narrower kernels, three wavefronts of which share a SIMD's registers, read them
     // for every chunk (512 x 256 bfloat16 179 -> 169 us; those of 128, two to a SIMD, would lose as much).
-    constexpr bool kFactors = kOut && A > 64;
+    constexpr bool kFactors = kOut && A > 64 && sizeof(T) == 2;
     const uint32_t f0 = 31u + 4u * h32 - col32;
     float factors[kFactors ? 16 : 1];
     if (kFactors)
@@ -440,9 +475,8 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
 
-        const auto z_of = [&](int k) { return across(zs + k * 16 * kStrideZ + wave * 32u, kStrideZ, lane); };
-        Frag<T> z[2];
-        if (sizeof(T) == 2) z[0] = z_of(0), z[1] = z_of(1);
+        // z is in registers before the outputs take its place in LDS
+        const auto z0 = across(zs + wave * 32u, kStrideZ, lane), z1 = across(zs + 16 * kStrideZ + wave * 32u, kStrideZ, lane);
         if constexpr (kOut) {
             f32x16 acc = (f32x16)0.0f;
             // out^T = S^T x^T, columns = steps
@@ -450,7 +484,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             for (int db = 0; db < A / 32; ++db)
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
-                    acc = Parts<T, 2>(half(state[db], k)).on_the_left(along(xs + col32 * kStrideA + db * 32 + k * 16, h32), acc);
+                    acc = mma(split<kAgain<T>>(half(state[db], k)), along<kParts<T>>(xs + col32 * kStrideA + db * 32 + k * 16, kPlane, h32), acc);
             acc *= s.out_scale * pw[reverse ? (col32 < n ? n - 1u - col32 : 0u) : col32 + 1u];
             if (m) {
                 const bool into = reverse ? (m & ~up_to(col32)) == 0 : (m & up_to(col32)) == 0;
@@ -460,7 +494,8 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             // P^T, then out^T += z^T P^T
             f32x16 p = (f32x16)0.0f;
 #pragma unroll
-            for (int k = 0; k < A / 16; ++k) p = mma(along(ys + col32 * kStrideA + k * 16, h32), along(xs + col32 * kStrideA + k * 16, h32), p);
+            for (int k = 0; k < A / 16; ++k) 
+                p = mma(along<kParts<T>>(ys + col32 * kStrideA + k * 16, kPlane, h32), along<kParts<T>>(xs + col32 * kStrideA + k * 16, kPlane, h32), p);
             // the positions that reach i, [first, past): j <= i and no episode begins in (j, i]; mirrored in reverse.  (A choice and no product with 0:
             // an overflow in a pair that does not count stays out.)
             const uint64_t upto = m & up_to(col32), later = m & ~up_to(col32);
@@ -470,50 +505,41 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
             asm volatile("" : "+v"(f), "+v"(lowest));  // (or what they give with 16 numbers is kept from chunk to chunk)
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] * (kFactors ? factors[kFactors ? r : 0] : factor[f + ((r & 3) + 8 * (r >> 2))]) : 0.0f;
+            acc = mma(parts_of(z0), split<kAgain<T>>(half(p, 0)), acc);
+            acc = mma(parts_of(z1), split<kAgain<T>>(half(p, 1)), acc);
+            // The outputs take the place of the wavefront's own columns of z in LDS, so that they leave as 16 bytes a lane, rows of 64 or 128
+            // bytes, past the caches: they are not read again (512 x 256 bfloat16 186 -> 171 us; parts of rows past the caches 345).
+            T* own = zs + wave * 32u;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) acc = Parts<T, 2>(half(p, k)).on_the_right(sizeof(T) == 2 ? z[k] : z_of(k), acc);
-            if constexpr (sizeof(T) == 2) {
-                // The outputs take the place of the wavefront's own columns of z in LDS (z itself is in registers), so that they leave as 16 bytes a lane,
-                // rows of 64 bytes, past the caches: they are not read again (512 x 256 186 -> 171 us; parts of rows past the caches 345).
-                __bf16* own = zs + wave * 32u;
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    uint32_t* w = reinterpret_cast<uint32_t*>(own + col32 * kStrideZ + 2 * r + 4 * h32);
-                    w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r], acc[r + 1]}, bf16x2));
-                    w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r + 2], acc[r + 3]}, bf16x2));
+            for (int r = 0; r < 16; r += 4) {
+                T* w = own + col32 * kStrideZ + 2 * r + 4 * h32;
+                if constexpr (sizeof(T) == 2) {
+                    const u32x2 v = {__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r], acc[r + 1]}, bf16x2)),
+                                     __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[r + 2], acc[r + 3]}, bf16x2))};
+                    *reinterpret_cast<u32x2*>(w) = v;
+                } else {
+                    *reinterpret_cast<f32x4*>(w) = f32x4{acc[r], acc[r + 1], acc[r + 2], acc[r + 3]};
                 }
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                const uint32_t c = lane % 4u * 8u, have = min(s.b - min(s.b, n0 + wave * 32u), 32u);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            constexpr uint32_t N = 16 / sizeof(T), kLanes = 32 / N;  // values of a vector, lanes of a row
+            const uint32_t c = lane % kLanes * N, have = min(s.b - min(s.b, n0 + wave * 32u), 32u);
 #pragma unroll
-                for (uint32_t i = 0; i < 2; ++i) {
-                    const uint32_t r = i * 16u + lane / 4u;
-                    const any_u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kStrideZ + c);
-                    if (r >= n || c >= have) continue;
-                    T* o = oh + (t + r) * s.out.step + (n0 + wave * 32u + c);
-                    if (c + 8 <= have) {
-                        __builtin_nontemporal_store(v, reinterpret_cast<any_u32x4*>(o));
-                    } else {
-                        T e[8];
-                        __builtin_memcpy(e, &v, 16);
+            for (uint32_t i = 0; i < kLanes / 2; ++i) {
+                const uint32_t r = i * (64u / kLanes) + lane / kLanes;
+                const any_u32x4 v = *reinterpret_cast<const u32x4*>(own + r * kStrideZ + c);
+                if (r >= n || c >= have) continue;
+                T* o = oh + (t + r) * s.out.step + (n0 + wave * 32u + c);
+                if (c + N <= have) {
+                    __builtin_nontemporal_store(v, reinterpret_cast<any_u32x4*>(o));
+                } else {
+                    T e[N];
+                    __builtin_memcpy(e, &v, 16);
 #pragma unroll
-                        for (uint32_t k = 0; k < 8; ++k)
-                            if (c + k < have) o[k] = e[k];
-                    }
-                }
-            } else if (col32 < n) {
-                T* o = oh + (t + col32) * s.out.step + (n0 + wave * 32u);
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const uint32_t c = 2 * r + 4 * h32;
-                    const f32x4 v = {acc[r], acc[r + 1], acc[r + 2], acc[r + 3]};
-                    if (n0 + kWidthZ <= s.b || n0 + wave * 32u + c + 4 <= s.b)
-                        __builtin_memcpy(o + c, &v, sizeof(v));
-                    else
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (n0 + wave * 32u + c + e < s.b) o[c + e] = v[e];
+                    for (uint32_t k = 0; k < N; ++k)
+                        if (c + k < have) o[k] = e[k];
                 }
             }
         }
@@ -533,9 +559,9 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(A <
         }
 #pragma unroll
         for (int k = 0; k < C / 16; ++k) {
-            const Parts<T, 3> zp(values(sizeof(T) == 2 ? z[k] : z_of(k)) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
+            const Parts<3> zp = split<3>(values(k ? z1 : z0) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
 #pragma unroll
-            for (int db = 0; db < A / 32; ++db) state[db] = zp.on_the_right(across(ys + k * 16 * kStrideA + db * 32, kStrideA, lane), state[db]);
+            for (int db = 0; db < A / 32; ++db) state[db] = mma(across<kParts<T>>(ys + k * 16 * kStrideA + db * 32, kPlane, kStrideA, lane), zp, state[db]);
         }
         __syncthreads();
         at = after;
@@ -720,10 +746,11 @@ bool together(const LinearAttentionConsts& c) { return width_of(c.dk) == width_o
 // those of 256), of two chunks at least, and of one for every 4096 cells of a state: a segment costs its state, written, joined and read.  us with a
 // workgroup for each place / with two for each compute unit: 30 x 2000 with 8 heads of 64 131 / 198, 64 x 1000 with 4 of 32 50 / 78, 4 x 1000 with 3 of 96 x 48 in
 // fp32 62 / 86; 16 x 512 with 16 of 128 x 96, whose two are all there is room for, 126, with four 153.
-uint32_t segments_of(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, bool backward, uint32_t* seg_steps) {
+uint32_t segments_of(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, bool backward, uint32_t* seg_steps) {
     const auto fit = [&](uint32_t a, uint32_t b, uint64_t roles) {
         const uint32_t width = width_of(a), waves = waves_of(a, b), tiles = (b + waves * 32u - 1u) / (waves * 32u);
-        const uint64_t places = (uint64_t)c.n_cus * ((width <= 64u ? 12u : width <= 128u ? 8u : 4u) / waves);
+        const uint32_t element = dtype == PXR_F32 ? 4u : 2u;
+        const uint64_t places = (uint64_t)c.n_cus * std::min(4u * waves_per_simd(width, element) / waves, kLds / scan_lds(element, width, waves, true));
         return places / ((uint64_t)n_envs * c.n_heads * roles * tiles);
     };
     uint64_t want = fit(c.dk, c.dv, !backward ? 1u : together(c) ? 3u : 1u);
@@ -740,18 +767,14 @@ uint32_t segments_of(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n
     return (uint32_t)((chunks + each - 1u) / each);
 }
 
-template <class T, int A, int kWaves, bool kOut>
-constexpr size_t scan_lds() {
-    return (size_t)C * ((kOut ? 2 : 1) * (A + kPad<T>) + kWaves * 32 + kPad<T>) * sizeof(T) + (36 + 64 + kWaves * C + 2) * 4;
-}
-
-// Chunks of 256 values take more than the 64 KB of LDS that a launch has by default.
+// Chunks of long heads take more than the 64 KB of LDS that a launch has by default.
 template <class T>
 hipError_t allow_lds() {
-    const void* fns[2] = {reinterpret_cast<const void*>(&scan_kernel<T, 256, 4, true>), reinterpret_cast<const void*>(&scan_kernel<T, 256, 4, false>)};
-    static_assert(scan_lds<T, 128, 4, true>() <= 64 * 1024 && scan_lds<T, 256, 4, true>() <= 160 * 1024);
+    const void* fns[] = {reinterpret_cast<const void*>(&scan_kernel<T, 128, 2, true>),  reinterpret_cast<const void*>(&scan_kernel<T, 128, 4, true>),
+                         reinterpret_cast<const void*>(&scan_kernel<T, 256, 4, true>),  reinterpret_cast<const void*>(&scan_kernel<T, 256, 4, false>)};
+    static_assert(scan_lds(sizeof(T), 64, 4, true) <= 64 * 1024 && scan_lds(sizeof(T), 128, 4, false) <= 64 * 1024 && scan_lds(sizeof(T), 256, 4, true) <= kLds);
     for (const void* f : fns)
-        if (const hipError_t rc = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); rc != hipSuccess) return rc;
+        if (const hipError_t rc = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds); rc != hipSuccess) return rc;
     return hipSuccess;
 }
 
@@ -762,7 +785,7 @@ void enqueue_as(const Scan* s, uint32_t roles, const Cut& cut, float* const* loc
     const Scans scans{{s[0], s[roles > 1 ? 1 : 0], s[roles > 2 ? 2 : 0]}};
 #define PXR_SCAN(A, W)                                                                                                                            \
     case A + W:                                                                                                                                   \
-        hipLaunchKernelGGL((scan_kernel<T, A, W, kOut>), grid, dim3(W * 64), (scan_lds<T, A, W, kOut>()), st, scans, cut, roles, local[0], local[1], \
+        hipLaunchKernelGGL((scan_kernel<T, A, W, kOut>), grid, dim3(W * 64), scan_lds(sizeof(T), A, W, kOut), st, scans, cut, roles, local[0], local[1], \
                            whole[0], whole[1]);                                                                                                   \
         break
     switch (cut.width + cut.waves) {
@@ -799,7 +822,7 @@ Cut cut_of(const LinearAttentionConsts& c, const pxr_rollout& r, bool backward, 
     cut.n_heads = c.n_heads;
     cut.rows = r.n_envs * c.n_heads;
     cut.n_steps = r.n_steps;
-    cut.segments = segments_of(c, r.n_envs, r.n_steps, backward, &cut.seg_steps);
+    cut.segments = segments_of(c, r.dtype, r.n_envs, r.n_steps, backward, &cut.seg_steps);
     cut.width = width_of(a);
     cut.waves = waves_of(a, b);
     cut.tiles = (b + cut.waves * 32u - 1u) / (cut.waves * 32u);
@@ -828,9 +851,9 @@ int prepare_linear_attention_kernels(std::string& err) {
     return PXR_ERR_DEVICE;
 }
 
-size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, bool backward) {
+size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, bool backward) {
     uint32_t steps;
-    const uint32_t segments = segments_of(c, n_envs, n_steps, backward, &steps);
+    const uint32_t segments = segments_of(c, dtype, n_envs, n_steps, backward, &steps);
     const size_t one = ((state_bytes(c, n_envs, segments) + 15u) & ~(size_t)15u) + whole_bytes(c, n_envs, segments);
     return backward ? 2u * one : one;
 }

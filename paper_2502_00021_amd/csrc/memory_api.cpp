@@ -144,7 +144,7 @@ int pxr_linear_attention_workspace(const pxr_linear_attention* a, uint32_t dtype
                                    size_t* bytes) {
     if (!a || !bytes || n_envs == 0 || (uint64_t)n_envs * a->c.n_heads > (1u << 21) || n_steps > 0x7FFFFFFFu || dtype > PXR_BF16)
         return refuse("pxr_linear_attention_workspace", "null argument, no or too many environments or steps, or a dtype that is none");
-    *bytes = pxr::linear_attention_workspace(a->c, n_envs, n_steps, backward != 0);
+    *bytes = pxr::linear_attention_workspace(a->c, dtype, n_envs, n_steps, backward != 0);
     return PXR_OK;
 }
 
@@ -156,7 +156,7 @@ int pxr_linear_attention_forward(pxr_linear_attention* a, const pxr_rollout* r, 
         wrong_view(out, r->dtype, r->n_steps) || !aligned(d_state_out, 4))
         return refuse(call, "a buffer is null or not aligned to its elements");
     if (overlap(r->d_state, d_state_out, (size_t)r->n_envs * a->c.n_heads * a->c.dk * a->c.dv)) return refuse(call, "the states overlap");
-    const size_t need = pxr::linear_attention_workspace(a->c, r->n_envs, r->n_steps, false);
+    const size_t need = pxr::linear_attention_workspace(a->c, r->dtype, r->n_envs, r->n_steps, false);
     if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
         return refuse(call, "the workspace is missing, too small or not 16-byte aligned");
     std::string err;
@@ -173,7 +173,7 @@ int pxr_linear_attention_backward(pxr_linear_attention* a, const pxr_rollout* r,
     if (!aligned(d_dstate_out, 4) || !aligned(d_dstate, 4)) return refuse(call, "a buffer is null or not aligned to its elements");
     const size_t n = (size_t)r->n_envs * a->c.n_heads * a->c.dk * a->c.dv;
     if (overlap(r->d_state, d_dstate, n) || overlap(d_dstate_out, d_dstate, n)) return refuse(call, "the states overlap");
-    const size_t need = pxr::linear_attention_workspace(a->c, r->n_envs, r->n_steps, true);
+    const size_t need = pxr::linear_attention_workspace(a->c, r->dtype, r->n_envs, r->n_steps, true);
     if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
         return refuse(call, "the workspace is missing, too small or not 16-byte aligned");
     std::string err;

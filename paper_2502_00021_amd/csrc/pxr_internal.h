@@ -245,7 +245,7 @@ struct LinearAttentionConsts {
 
 // linear_attention.hip (arguments as checked by memory_api.cpp)
 int prepare_linear_attention_kernels(std::string& err);
-size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t n_envs, uint32_t n_steps, bool backward);
+size_t linear_attention_workspace(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, bool backward);
 int launch_linear_attention_forward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& out, float* state_out, void* ws,
                                     void* stream, std::string& err);
 int launch_linear_attention_backward(const LinearAttentionConsts& c, const pxr_rollout& r, const pxr_tokens& dout, const float* dstate_out,
