@@ -125,29 +125,33 @@ __device__ __forceinline__ f32x16 mma(const Parts<n>& a, const Parts<m>& b, f32x
     return c;
 }
 
+// Tiles of x and y have every run of 16 columns in the order 0-3, 8-11, 4-7, 12-15, so that a lane's eight values are 16 bytes that lie together.  With four a column
+// apart a row, 16 rows of them at one column lie in different banks.
+__device__ __forceinline__ constexpr uint32_t place(uint32_t c) { return (c & ~12u) | ((c & 4u) << 1) | ((c & 8u) >> 1); }
+
 // From rows that lie along the summed axis: p = the row's run of 16 in LDS, `plane` values from part to part.
 template <int n>
 __device__ __forceinline__ Parts<n> along(const __bf16* p, uint32_t plane, uint32_t h) {
     Parts<n> f;
 #pragma unroll
-    for (int k = 0; k < n; ++k) {
-        const bf16x4 lo = *reinterpret_cast<const bf16x4*>(p + k * plane + 4 * h), hi = *reinterpret_cast<const bf16x4*>(p + k * plane + 8 + 4 * h);
-        f.part[k] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
+    for (int k = 0; k < n; ++k) f.part[k] = *reinterpret_cast<const bf16x8*>(p + k * plane + 8 * h);
     return f;
 }
 
 // From 16 rows that lie across it: p = the first row's 32 columns in LDS, `stride` values from row to row; the lane's column is lane % 32.
+template <bool kPlaced>
 __device__ __forceinline__ bf16x8 across(const __bf16* p, uint32_t stride, uint32_t lane) {
     // The transposing read: lane i of 16 gives the address of four columns of row i / 4 and gets four rows of column i.
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const uint32_t h = lane >> 5, i = lane & 15u;
-    const __bf16* q = p + (4 * h + (i >> 2)) * stride + (lane & 16u) + 4 * (i & 3u);
+    const __bf16* q = p + (4 * h + (i >> 2)) * stride + (lane & 16u) + (kPlaced ? place(4 * (i & 3u)) : 4 * (i & 3u));
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + 8 * stride));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
+template <bool kPlaced>
 __device__ __forceinline__ f32x8 across(const float* p, uint32_t stride, uint32_t lane) {
+    static_assert(!kPlaced);
     const float* q = p + (4 * (lane >> 5)) * stride + (lane & 31u);
     f32x8 f;
 #pragma unroll
@@ -155,10 +159,10 @@ __device__ __forceinline__ f32x8 across(const float* p, uint32_t stride, uint32_
     return f;
 }
 template <int n>
-__device__ __forceinline__ Parts<n> across(const __bf16* p, uint32_t plane, uint32_t stride, uint32_t lane) {
+__device__ __forceinline__ Parts<n> across_placed(const __bf16* p, uint32_t plane, uint32_t stride, uint32_t lane) {
     Parts<n> f;
 #pragma unroll
-    for (int k = 0; k < n; ++k) f.part[k] = across(p + k * plane, stride, lane);
+    for (int k = 0; k < n; ++k) f.part[k] = across<true>(p + k * plane, stride, lane);
     return f;
 }
 
@@ -223,9 +227,10 @@ __device__ __forceinline__ uint32_t again(uint32_t v) {
 // vector has its last vector moved back to its end; rows past the last and vectors past a row's end read what is there instead and are not written,
 // or written as zeros.  The columns past d are zero from the start and nothing writes them.  Rows shorter than a vector are read value by value,
 // when they are written.
-// kSplit: fp32 values go to LDS as three planes of bfloat16 parts.
-template <class T, int kWidth, int kThreads, bool kSplit>
+// kOperand: a tile of x or y, its columns placed and fp32 values as three planes of bfloat16 parts.
+template <class T, int kWidth, int kThreads, bool kOperand>
 struct Steps {
+    static constexpr bool kSplit = kOperand && sizeof(T) == 4;
     typedef std::conditional_t<kSplit, __bf16, T> E;  // of the tile
     static constexpr uint32_t N = 16 / sizeof(T), kPerRow = kWidth / N, kCount = (C * kPerRow + kThreads - 1) / kThreads, kStride = kWidth + kPad<E>, kPlane = C * kStride;
     static constexpr uint32_t kRowsEach = kThreads / kPerRow;  // rows that the lanes take together
@@ -253,7 +258,8 @@ struct Steps {
 #pragma unroll
         for (uint32_t i = 0; i < kCount; ++i) asm volatile("" : "=v"(v[i]));
     }
-    static __device__ __forceinline__ void put_one(E* at, T e) {
+    static __device__ __forceinline__ void put_one(E* row, uint32_t c, T e) {
+        E* at = row + (kOperand ? place(c) : c);
         if constexpr (kSplit) {
             float rest = e;
 #pragma unroll
@@ -274,7 +280,7 @@ struct Steps {
                 const uint32_t r = i / d, c = i - r * d;
                 const T e = r < n ? from[(int64_t)r * step + c] : (T)0.0f;
                 if (kCheck) most.with(sizeof(T) == 4 ? __builtin_bit_cast(uint32_t, (float)e) : __builtin_bit_cast(uint32_t, (float)e) >> 16);
-                put_one(tile + r * kStride + c, e);
+                put_one(tile + r * kStride, c, e);
             }
             return;
         }
@@ -299,8 +305,11 @@ struct Steps {
                             rest[2 * i] -= __uint_as_float(p[i] << 16);
                             rest[2 * i + 1] -= __uint_as_float(p[i] & 0xFFFF0000u);
                         }
-                        *reinterpret_cast<u32x2*>(tile + k * kPlane + r * kStride + col) = p;
+                        *reinterpret_cast<u32x2*>(tile + k * kPlane + r * kStride + place(col)) = p;
                     }
+                } else if constexpr (kOperand) {
+                    *reinterpret_cast<u32x2*>(tile + r * kStride + place(col)) = u32x2{w[0], w[1]};
+                    *reinterpret_cast<u32x2*>(tile + r * kStride + place(col + 4)) = u32x2{w[2], w[3]};
                 } else {
                     *reinterpret_cast<u32x4*>(tile + r * kStride + col) = w;
                 }
@@ -308,7 +317,7 @@ struct Steps {
                 T e[N];
                 __builtin_memcpy(e, &w, 16);
 #pragma unroll
-                for (uint32_t k = 0; k < N; ++k) put_one(tile + r * kStride + d - N + k, e[k]);
+                for (uint32_t k = 0; k < N; ++k) put_one(tile + r * kStride, d - N + k, e[k]);
             }
         }
     }
@@ -371,7 +380,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
     const uint8_t* resets = cut.resets ? cut.resets + (int64_t)env * cut.resets_env : nullptr;
     // the segment's steps in the order in which they are taken; in reverse, position p of the scan is step n_steps - 1 - p
     const uint32_t begin = seg * cut.seg_steps, end = min(begin + cut.seg_steps, cut.n_steps);
-    Steps<T, A, kThreads, sizeof(T) == 4> y_steps(s.y.step, s.a), x_steps(s.x.step, s.a);
+    Steps<T, A, kThreads, true> y_steps(s.y.step, s.a), x_steps(s.x.step, s.a);
     Steps<T, kWidthZ, kThreads, false> z_steps(s.z.step, widthB);
     uint32_t reset = 0;
     const uint32_t has_resets = cut.resets != nullptr;
@@ -476,26 +485,22 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
         }
 
         // z is in registers before the outputs take its place in LDS
-        const auto z0 = across(zs + wave * 32u, kStrideZ, lane), z1 = across(zs + 16 * kStrideZ + wave * 32u, kStrideZ, lane);
+        const auto z0 = across<false>(zs + wave * 32u, kStrideZ, lane), z1 = across<false>(zs + 16 * kStrideZ + wave * 32u, kStrideZ, lane);
         if constexpr (kOut) {
-            f32x16 acc = (f32x16)0.0f;
-            // out^T = S^T x^T, columns = steps
+            // out^T = S^T x^T and P^T = y x^T, columns = steps
+            f32x16 acc = (f32x16)0.0f, p = (f32x16)0.0f;
 #pragma unroll
-            for (int db = 0; db < A / 32; ++db)
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    acc = mma(split<kAgain<T>>(half(state[db], k)), along<kParts<T>>(xs + col32 * kStrideA + db * 32 + k * 16, kPlane, h32), acc);
+            for (int k = 0; k < A / 16; ++k) {
+                const Parts<kParts<T>> x = along<kParts<T>>(xs + col32 * kStrideA + k * 16, kPlane, h32);
+                acc = mma(split<kAgain<T>>(half(state[k / 2], k % 2)), x, acc);
+                p = mma(along<kParts<T>>(ys + col32 * kStrideA + k * 16, kPlane, h32), x, p);
+            }
             acc *= s.out_scale * pw[reverse ? (col32 < n ? n - 1u - col32 : 0u) : col32 + 1u];
             if (m) {
                 const bool into = reverse ? (m & ~up_to(col32)) == 0 : (m & up_to(col32)) == 0;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[r] = into ? acc[r] : 0.0f;
             }
-            // P^T, then out^T += z^T P^T
-            f32x16 p = (f32x16)0.0f;
-#pragma unroll
-            for (int k = 0; k < A / 16; ++k) 
-                p = mma(along<kParts<T>>(ys + col32 * kStrideA + k * 16, kPlane, h32), along<kParts<T>>(xs + col32 * kStrideA + k * 16, kPlane, h32), p);
             // the positions that reach i, [first, past): j <= i and no episode begins in (j, i]; mirrored in reverse.  (A choice and no product with 0:
             // an overflow in a pair that does not count stays out.)
             const uint64_t upto = m & up_to(col32), later = m & ~up_to(col32);
@@ -505,6 +510,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
             asm volatile("" : "+v"(f), "+v"(lowest));  // (or what they give with 16 numbers is kept from chunk to chunk)
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] * (kFactors ? factors[kFactors ? r : 0] : factor[f + ((r & 3) + 8 * (r >> 2))]) : 0.0f;
+            // out^T += z^T P^T
             acc = mma(parts_of(z0), split<kAgain<T>>(half(p, 0)), acc);
             acc = mma(parts_of(z1), split<kAgain<T>>(half(p, 1)), acc);
             // The outputs take the place of the wavefront's own columns of z in LDS, so that they leave as 16 bytes a lane, rows of 64 or 128
@@ -561,7 +567,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
         for (int k = 0; k < C / 16; ++k) {
             const Parts<3> zp = split<3>(values(k ? z1 : z0) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
 #pragma unroll
-            for (int db = 0; db < A / 32; ++db) state[db] = mma(across<kParts<T>>(ys + k * 16 * kStrideA + db * 32, kPlane, kStrideA, lane), zp, state[db]);
+            for (int db = 0; db < A / 32; ++db) state[db] = mma(across_placed<kParts<T>>(ys + k * 16 * kStrideA + db * 32, kPlane, kStrideA, lane), zp, state[db]);
         }
         __syncthreads();
         at = after;
