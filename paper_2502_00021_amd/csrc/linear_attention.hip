@@ -398,35 +398,35 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
     f32x16 state[A / 32];
     const size_t cells = (size_t)s.a * s.b;
     const float* from = kOut ? (seg ? s.before + ((size_t)(seg - 1u) * cut.rows + row) * cells : s.state_in ? s.state_in + row * cells : nullptr) : nullptr;
-    const bool whole_state = s.a == (uint32_t)A && n0 + kWidthZ <= s.b;
-    const uint32_t lane_cell = 4 * h32 * s.state_row + col * s.state_col;  // (a state has at most 2^16 cells)
-    if (!from) {
+    const uint32_t lane_cell = 4 * h32 * s.state_row + min(col, s.b - 1u) * s.state_col;  // (a state has at most 2^16 cells)
 #pragma unroll
-        for (int db = 0; db < A / 32; ++db) state[db] = (f32x16)0.0f;
-    } else if (whole_state && s.state_row == 1u) {  // (transposed: a lane's rows are adjacent, four at a time)
-#pragma unroll
-        for (int db = 0; db < A / 32; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                float v[4];
-                __builtin_memcpy(v, from + (db * 32 + 2 * r) + lane_cell, 16);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) state[db][r + e] = v[e];
-            }
-    } else if (whole_state) {
-#pragma unroll
-        for (int db = 0; db < A / 32; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) state[db][r] = from[(db * 32 + (r & 3) + 8 * (r >> 2)) * s.state_row + lane_cell];
-    } else {
-#pragma unroll
-        for (int db = 0; db < A / 32; ++db)
+    for (int db = 0; db < A / 32; ++db) {
+        const float* block = from + (size_t)db * 32 * s.state_row;
+        if (!from || db * 32u >= s.a) {
+            state[db] = (f32x16)0.0f;
+            continue;
+        } else if (db * 32u + 32u > s.a) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32;
                 const float v = from[min(d, s.a - 1u) * s.state_row + min(col, s.b - 1u) * s.state_col];
-                state[db][r] = d < s.a && col < s.b ? v : 0.0f;
+                state[db][r] = d < s.a ? v : 0.0f;
             }
+        } else if (s.state_row == 1u) {  // (transposed: a lane's rows are adjacent, four at a time)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                float v[4];
+                __builtin_memcpy(v, block + 2 * r + lane_cell, 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) state[db][r + e] = v[e];
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) state[db][r] = block[((r & 3) + 8 * (r >> 2)) * s.state_row + lane_cell];
+        }
+        if (n0 + kWidthZ > s.b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) state[db][r] = col < s.b ? state[db][r] : 0.0f;
     }
     __syncthreads();
 
@@ -575,19 +575,20 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
 
     float* to = kOut ? (seg + 1u == cut.segments && s.state_out ? s.state_out + row * cells : nullptr)
                      : (role ? local1 : local0) + ((size_t)seg * cut.rows + row) * cells;
-    if (to && whole_state) {
+    if (to && col < s.b) {
 #pragma unroll
-        for (int db = 0; db < A / 32; ++db)
+        for (int db = 0; db < A / 32; ++db) {
+            if (db * 32u >= s.a) break;
+            float* block = to + (size_t)db * 32 * s.state_row;
+            if (db * 32u + 32u <= s.a) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) to[(db * 32 + (r & 3) + 8 * (r >> 2)) * s.state_row + lane_cell] = state[db][r];
-    } else if (to && col < s.b) {
+                for (int r = 0; r < 16; ++r) block[((r & 3) + 8 * (r >> 2)) * s.state_row + lane_cell] = state[db][r];
+            } else {
 #pragma unroll
-        for (int db = 0; db < A / 32; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t d = db * 32 + (r & 3) + 8 * (r >> 2);
-                if (d + 4 * h32 < s.a) to[d * s.state_row + lane_cell] = state[db][r];
+                for (int r = 0; r < 16; ++r)
+                    if (db * 32 + (r & 3) + 8 * (r >> 2) + 4 * h32 < s.a) block[((r & 3) + 8 * (r >> 2)) * s.state_row + lane_cell] = state[db][r];
             }
+        }
     }
     if (!kOut && tile == 0 && threadIdx.x == 0) (role ? whole1 : whole0)[seg * cut.rows + row] = uncut ? 1u : 0u;
 }
