@@ -10,10 +10,12 @@
 // A lane holds VPL vectors of 16 bytes of a row, lanes of a row next to each other.  Who takes a row goes by the number of its
 // vectors:
 //   up to 64      a part of a wavefront, 1 to 64 lanes: eight rows of 64 bfloat16 values in a wavefront
-//   up to 256     a wavefront, two or four vectors a lane
-//   up to 8192    a workgroup of 512 or 1024 threads
-//   more          a workgroup that reads the row again for each sum (from the caches, mostly)
-// What leaves is not read again by the kernel and goes past the caches that it would push x out of (524288 x 64 bfloat16 31 -> 24 us, 4096 x 30752 146 -> 110;
+//   up to 256     a wavefront, two or four vectors a lane (backward: 128)
+//   up to 16384   a workgroup of 256 to 1024 threads, two to sixteen vectors a lane: what a lane has in flight counts for more than lanes do
+//                 (forward, 30000 x 7000 bfloat16: 256 threads 175 us, 512 of them 188; 9000 x 5000 fp32: 512 threads 59, 1024 of them 80; 4096 x 30752 bfloat16:
+//                 two rows at a time 85, four 98)
+//   more          a workgroup that reads the row again for each sum (from the caches, mostly): 800 x 50000 fp32 124 us, 70 from registers
+// What leaves is not read again by the kernel and goes past the caches that it would push x out of (524288 x 64 bfloat16 31 -> 25 us, 4096 x 30752 146 -> 110;
 // requests that go past them as well are slower where x lies in them).
 //
 // Workgroups are persistent and walk the rows, so that weights and biases are read once by a wavefront, or once for four rows by a workgroup:
@@ -176,7 +178,9 @@ struct NormForward {
     float eps;
 };
 
-// U rows at a time: their requests are in flight together, and they share one read of weight and bias.
+// U rows at a time: their requests are in flight together, and they share one read of weight and bias.  Where rows are shorter than a line of
+// memory, a wavefront's groups of lanes have rows next to each other, so that a request is of whole lines (2 000 000 x 8 in fp32 54 -> 24 us); longer
+// ones lie together for each group (524288 x 64 bfloat16 24.8 us, otherwise 26.6).
 template <class T, class P, int NT, int VPL, int U, bool kTiny = false>
 __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const NormForward a) {
     constexpr int N = Vec<T>::N;
@@ -185,6 +189,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
     __shared__ float lds[2 * U * 16];
     const uint32_t lanes = NT ? NT : a.lanes, l = NT ? threadIdx.x : threadIdx.x & (lanes - 1u);
     const uint32_t group = NT ? 0u : threadIdx.x / lanes, groups = NT ? 1u : kThreadsOf(NT) / lanes;
+    const uint32_t apart = NT || lanes >= 8u ? 1u : 64u / lanes, in_wave = group & (apart - 1u);  // rows from one of the U to the next
     const P *weight = static_cast<const P*>(a.weight), *bias = static_cast<const P*>(a.bias);
     float w[kKeep ? VPL : 1][N], b[kKeep ? VPL : 1][N];
     if (kKeep)
@@ -194,11 +199,13 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
             load_params(bias, 0.0f, At(l + p * lanes, a.D), b[kKeep ? p : 0]);
         }
     const float width = (float)a.D;  // (divided by: a product with 1 / D would move the mean of equal values)
-    for (uint64_t row0 = ((uint64_t)blockIdx.x * groups + group) * U; row0 < a.n; row0 += (uint64_t)gridDim.x * groups * U) {
+    for (uint64_t row0 = ((uint64_t)blockIdx.x * groups + (group - in_wave)) * U + in_wave; row0 < a.n; row0 += (uint64_t)gridDim.x * groups * U) {
         Vec<T> x[U][VPL];
+        const T* first = static_cast<const T*>(a.x) + (int64_t)row0 * a.x_stride;
+        T* to = static_cast<T*>(a.y) + (int64_t)row0 * a.y_stride;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const T* xr = static_cast<const T*>(a.x) + (int64_t)min(row0 + u, (uint64_t)a.n - 1u) * a.x_stride;
+            const T* xr = first + (row0 + u * apart < a.n ? (int64_t)(u * apart) * a.x_stride : 0);
 #pragma unroll
             for (int p = 0; p < VPL; ++p) {
                 const At at(again<NT>(l) + p * lanes, a.D);
@@ -259,9 +266,9 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             rstd[u] = 1.0f / sqrtf(rstd[u] / width + a.eps);
-            if (l == 0 && row0 + u < a.n) {
-                if (a.mean) a.mean[row0 + u] = mean[u];
-                if (a.rstd) a.rstd[row0 + u] = rstd[u];
+            if (l == 0 && row0 + u * apart < a.n) {
+                if (a.mean) a.mean[row0 + u * apart] = mean[u];
+                if (a.rstd) a.rstd[row0 + u * apart] = rstd[u];
             }
         }
 #pragma unroll
@@ -273,11 +280,11 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (row0 + u >= a.n || !at.any()) continue;
+                if (row0 + u * apart >= a.n || !at.any()) continue;
                 float y[N];
 #pragma unroll
                 for (int e = 0; e < N; ++e) y[e] = __builtin_fmaf((x[u][p].get(e) - mean[u]) * rstd[u], w[kKeep ? p : 0][e], b[kKeep ? p : 0][e]);
-                Vec<T>::store(static_cast<T*>(a.y) + ((int64_t)(row0 + u) * a.y_stride + at.at), y, at.from, at.to);
+                Vec<T>::store(to + ((int64_t)(u * apart) * a.y_stride + at.at), y, at.from, at.to);
             }
         }
     }
@@ -286,23 +293,46 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_forward_kernel(const Norm
 // Rows of any width, read again for each sum.
 template <class T, class P>
 __global__ __launch_bounds__(1024) void norm_forward_wide_kernel(const NormForward a) {
+    constexpr int N = Vec<T>::N;
+    typedef Place<N, false> At;
     __shared__ float lds[32];
     const T* xr = static_cast<const T*>(a.x) + (int64_t)blockIdx.x * a.x_stride;
     T* yr = static_cast<T*>(a.y) + (int64_t)blockIdx.x * a.y_stride;
-    const P *weight = static_cast<const P*>(a.weight), *bias = static_cast<const P*>(a.bias);
+    const uint32_t vectors = (a.D + N - 1u) / N;
     const float width = (float)a.D;
     float mean[1] = {0.0f}, rstd[1] = {0.0f};
-    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u) mean[0] += load1(xr + i);
+    for (uint32_t i = threadIdx.x; i < vectors; i += 1024u) {
+        const At at(i, a.D);
+        Vec<T> x;
+        x.load(xr + at.at);
+#pragma unroll
+        for (int e = 0; e < N; ++e) mean[0] += at.own(e) ? x.get(e) : 0.0f;
+    }
     row_sums<1024, 1>(mean, 0, lds);
     mean[0] /= width;
-    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u) {
-        const float c = load1(xr + i) - mean[0];
-        rstd[0] = __builtin_fmaf(c, c, rstd[0]);
+    for (uint32_t i = threadIdx.x; i < vectors; i += 1024u) {
+        const At at(i, a.D);
+        Vec<T> x;
+        x.load(xr + at.at);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float c = at.own(e) ? x.get(e) - mean[0] : 0.0f;
+            rstd[0] = __builtin_fmaf(c, c, rstd[0]);
+        }
     }
     row_sums<1024, 1>(rstd, 0, lds + 16);
     rstd[0] = 1.0f / sqrtf(rstd[0] / width + a.eps);
-    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u)
-        store1(yr + i, __builtin_fmaf((load1(xr + i) - mean[0]) * rstd[0], weight ? load1(weight + i) : 1.0f, bias ? load1(bias + i) : 0.0f));
+    for (uint32_t i = threadIdx.x; i < vectors; i += 1024u) {
+        const At at(i, a.D);
+        Vec<T> x;
+        x.load(xr + at.at);
+        float w[N], b[N], y[N];
+        load_params(static_cast<const P*>(a.weight), 1.0f, at, w);
+        load_params(static_cast<const P*>(a.bias), 0.0f, at, b);
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = __builtin_fmaf((x.get(e) - mean[0]) * rstd[0], w[e], b[e]);
+        Vec<T>::store(yr + at.at, y, at.from, at.to);
+    }
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[blockIdx.x] = mean[0];
         if (a.rstd) a.rstd[blockIdx.x] = rstd[0];
@@ -332,6 +362,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
     float* const db_lds = lds + 2 * (2 * U * 16);  // [VPL N][1024]
     const uint32_t lanes = NT ? NT : a.lanes, l = NT ? threadIdx.x : threadIdx.x & (lanes - 1u);
     const uint32_t group = NT ? 0u : threadIdx.x / lanes, groups = NT ? 1u : kThreadsOf(NT) / lanes;
+    const uint32_t apart = NT || lanes >= 8u ? 1u : 64u / lanes, in_wave = group & (apart - 1u);  // rows from one of the U to the next
     const P* weight = static_cast<const P*>(a.weight);
     float w[kKeep ? VPL : 1][N];
     if (kKeep)
@@ -349,7 +380,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
     const auto ask = [&](Rows& r, uint64_t row0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint64_t row = min(row0 + u, (uint64_t)a.n - 1u);
+            const uint64_t row = min(row0 + u * apart, (uint64_t)a.n - 1u);
             const T *gr = static_cast<const T*>(a.dy) + (int64_t)row * a.dy_stride, *xr = static_cast<const T*>(a.x) + (int64_t)row * a.x_stride;
 #pragma unroll
             for (int p = 0; p < VPL; ++p) {
@@ -367,7 +398,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
         }
     };
     uint32_t turn = 0;
-    uint64_t row0 = ((uint64_t)blockIdx.x * groups + group) * U;
+    uint64_t row0 = ((uint64_t)blockIdx.x * groups + (group - in_wave)) * U + in_wave;
     const uint64_t stride = (uint64_t)gridDim.x * groups * U;
     Rows r, ahead;
     if (kAhead && row0 < a.n) ask(ahead, row0);
@@ -392,7 +423,7 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
                 // What is not the lane's own is nothing: its gradient is zero here, and so is what it adds to a sum.  (x beside it is of the same
                 // row: where it is no number, the row's gradient is none either.  A row past the last must not reach the sums over rows.)
                 if (!at.whole()) r.g[u][p].keep(at.from, at.to);
-                if (row0 + u >= a.n) {
+                if (row0 + u * apart >= a.n) {
                     r.g[u][p].keep(0, 0);
                     r.x[u][p].keep(0, 0);
                     r.mean[u] = r.rstd[u] = 0.0f;
@@ -425,14 +456,14 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
             if (!kKeep) load_params(weight, 1.0f, at, w[0]);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (row0 + u >= a.n || !at.any()) continue;
+                if (row0 + u * apart >= a.n || !at.any()) continue;
                 float dx[N];
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float xh = (r.x[u][p].get(e) - r.mean[u]) * r.rstd[u];
                     dx[e] = r.rstd[u] * __builtin_fmaf(-xh, s[2 * u + 1] * per, __builtin_fmaf(r.g[u][p].get(e), w[kKeep ? p : 0][e], -s[2 * u] * per));
                 }
-                Vec<T>::store(static_cast<T*>(a.dx) + ((int64_t)(row0 + u) * a.dx_stride + at.at), dx, at.from, at.to);
+                Vec<T>::store(static_cast<T*>(a.dx) + ((int64_t)(row0 + u * apart) * a.dx_stride + at.at), dx, at.from, at.to);
             }
         }
     }
@@ -485,23 +516,43 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
 // dx alone, rows of any width.
 template <class T, class P>
 __global__ __launch_bounds__(1024) void norm_dx_wide_kernel(const NormBackward a) {
+    constexpr int N = Vec<T>::N;
+    typedef Place<N, false> At;
     __shared__ float lds[32];
     const T* dyr = static_cast<const T*>(a.dy) + (int64_t)blockIdx.x * a.dy_stride;
     const T* xr = static_cast<const T*>(a.x) + (int64_t)blockIdx.x * a.x_stride;
     T* dxr = static_cast<T*>(a.dx) + (int64_t)blockIdx.x * a.dx_stride;
     const P* weight = static_cast<const P*>(a.weight);
+    const uint32_t vectors = (a.D + N - 1u) / N;
     const float m = a.mean[blockIdx.x], r = a.rstd[blockIdx.x];
     float s[2] = {0.0f, 0.0f};
-    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u) {
-        const float g = load1(dyr + i) * (weight ? load1(weight + i) : 1.0f);
-        s[0] += g;
-        s[1] = __builtin_fmaf(g, (load1(xr + i) - m) * r, s[1]);
+    for (uint32_t i = threadIdx.x; i < vectors; i += 1024u) {
+        const At at(i, a.D);
+        Vec<T> dy, x;
+        dy.load(dyr + at.at);
+        x.load(xr + at.at);
+        float w[N];
+        load_params(weight, 1.0f, at, w);
+        if (!at.whole()) dy.keep(at.from, at.to);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float g = dy.get(e) * w[e];
+            s[0] += g;
+            s[1] = __builtin_fmaf(g, (x.get(e) - m) * r, s[1]);
+        }
     }
     row_sums<1024, 2>(s, 0, lds);
     const float per = 1.0f / (float)a.D;
-    for (uint32_t i = threadIdx.x; i < a.D; i += 1024u) {
-        const float g = load1(dyr + i) * (weight ? load1(weight + i) : 1.0f);
-        store1(dxr + i, r * __builtin_fmaf(-(load1(xr + i) - m) * r, s[1] * per, __builtin_fmaf(-s[0], per, g)));
+    for (uint32_t i = threadIdx.x; i < vectors; i += 1024u) {
+        const At at(i, a.D);
+        Vec<T> dy, x;
+        dy.load(dyr + at.at);
+        x.load(xr + at.at);
+        float w[N], dx[N];
+        load_params(weight, 1.0f, at, w);
+#pragma unroll
+        for (int e = 0; e < N; ++e) dx[e] = r * __builtin_fmaf(-(x.get(e) - m) * r, s[1] * per, __builtin_fmaf(dy.get(e), w[e], -s[0] * per));
+        Vec<T>::store(dxr + at.at, dx, at.from, at.to);
     }
 }
 
@@ -618,7 +669,7 @@ void forward_as(const pxr_layer_norm_desc& d, NormForward a, hipStream_t st) {
     a.lanes = p.lanes;
 #define PXR_NORM(NT, VPL, U, GROUPS, MOST) \
     hipLaunchKernelGGL((norm_forward_kernel<T, P, NT, VPL, U>), grid(GROUPS * U, MOST), dim3(kThreadsOf(NT)), 0, st, a)
-    // Rows that do not fill the device go one by one; many go four at a time.
+    // Rows that do not fill the device go one by one; many go two or four at a time.
     const bool many = d.n_rows >= 4u * kCus;
     if (d.width < (uint32_t)Vec<T>::N)
         hipLaunchKernelGGL((norm_forward_kernel<T, P, 0, 1, 4, true>), grid(4u * p.groups, 4u * kCus), dim3(kSubThreads), 0, st, a);
@@ -628,18 +679,30 @@ void forward_as(const pxr_layer_norm_desc& d, NormForward a, hipStream_t st) {
         PXR_NORM(0, 2, 2, p.groups, 4u * kCus);
     else if (p.vectors <= 256u)
         PXR_NORM(0, 4, 1, p.groups, 4u * kCus);
-    else if (p.vectors <= 1024u) {
+    else if (p.vectors <= 512u) {
         if (many)
-            PXR_NORM(512, 2, 4, 1u, 4u * kCus);
+            PXR_NORM(256, 2, 4, 1u, 4u * kCus);
         else
-            PXR_NORM(512, 2, 1, 1u, 4u * kCus);
+            PXR_NORM(256, 2, 1, 1u, 4u * kCus);
+    } else if (p.vectors <= 1024u) {
+        if (many)
+            PXR_NORM(256, 4, 2, 1u, 4u * kCus);
+        else
+            PXR_NORM(256, 4, 1, 1u, 4u * kCus);
+    } else if (p.vectors <= 2048u) {
+        if (many)
+            PXR_NORM(512, 4, 2, 1u, 2u * kCus);
+        else
+            PXR_NORM(512, 4, 1, 1u, 4u * kCus);
     } else if (p.vectors <= 4096u) {
         if (many)
-            PXR_NORM(1024, 4, 4, 1u, 2u * kCus);
+            PXR_NORM(1024, 4, 2, 1u, 2u * kCus);
         else
             PXR_NORM(1024, 4, 1, 1u, 2u * kCus);
     } else if (p.vectors <= 8192u)
         PXR_NORM(1024, 8, 1, 1u, 2u * kCus);
+    else if (p.vectors <= 16384u)
+        PXR_NORM(1024, 16, 1, 1u, kCus);
     else
         hipLaunchKernelGGL((norm_forward_wide_kernel<T, P>), dim3((uint32_t)d.n_rows), dim3(1024), 0, st, a);
 #undef PXR_NORM

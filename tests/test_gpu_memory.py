@@ -103,6 +103,29 @@ def test_layer_norm_of_many_rows(torch, pxr, N, D, dtype):
                gpu(torch, rng.standard_normal((N, D)), dtype))
 
 
+@pytest.mark.parametrize("N,D,dtype", [(1500, 1299, "f32"), (1031, 2601, "bf16"), (1025, 4095, "f32"), (1024, 8000, "bf16"), (1030, 7777, "f32"),
+                                       (1027, 12345, "bf16"), (1100, 9000, "f32"), (1033, 20002, "bf16"), (3, 160001, "f32"), (2, 300007, "bf16")])
+def test_layer_norm_of_many_long_rows(torch, pxr, N, D, dtype):
+    """Rows of a workgroup's, several at a time, and rows that no workgroup holds."""
+    rng = np.random.default_rng(N + D)
+    check_norm(torch, pxr, gpu(torch, rng.standard_normal((N, D), dtype=np.float32), dtype), gpu(torch, 1 + 0.2 * rng.standard_normal(D)),
+               gpu(torch, rng.standard_normal(D)), gpu(torch, rng.standard_normal((N, D), dtype=np.float32), dtype))
+
+
+@pytest.mark.parametrize("D,dtype", [(34001, "f32"), (70003, "f32"), (140003, "bf16")])
+def test_layer_norm_of_the_longest_rows_in_place(torch, pxr, D, dtype):
+    rng = np.random.default_rng(D)
+    x, dy, w = gpu(torch, rng.standard_normal((7, D)), dtype), gpu(torch, rng.standard_normal((7, D)), dtype), gpu(torch, rng.standard_normal(D))
+    y, mean, rstd = pxr.layer_norm(x, w)
+    z = x.clone()
+    pxr.layer_norm(z, w, out=z)
+    assert torch.equal(z, y)
+    got = pxr.layer_norm_backward(dy, x, mean, rstd, w)
+    for alias in (0, 1):
+        t = [dy.clone(), x.clone()]
+        assert all(torch.equal(a, b) for a, b in zip(got, pxr.layer_norm_backward(t[0], t[1], mean, rstd, w, dx=t[alias])))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_layer_norm_without_parameters_and_of_any_leading_shape(torch, pxr, dtype):
     rng = np.random.default_rng(3)
