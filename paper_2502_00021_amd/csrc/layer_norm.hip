@@ -344,7 +344,8 @@ struct NormBackward {
     const float *mean, *rstd;
     const void* weight;
     void* dx;
-    float* sums;  // [workgroups][2][D]: dw, db of a workgroup's rows; null = not wanted
+    float* sums;    // [workgroups][2][D]: dw, db of a workgroup's rows; null = not wanted
+    void *dw, *db;  // where one workgroup has all rows: the results themselves; null = not wanted
     int64_t dy_stride, x_stride, dx_stride;
     uint32_t n, D, lanes;
 };
@@ -467,8 +468,17 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
             }
         }
     }
-    if (!kSums || !a.sums) return;
-    float* out = a.sums + (size_t)blockIdx.x * 2u * a.D;
+    if (!kSums || !(a.sums || a.dw || a.db)) return;
+    const auto put = [&](uint32_t i, float w_sum, float b_sum) {
+        if (a.sums) {
+            float* out = a.sums + (size_t)blockIdx.x * 2u * a.D;
+            out[i] = w_sum;
+            out[a.D + i] = b_sum;
+        } else {
+            if (a.dw) store1(static_cast<P*>(a.dw) + i, w_sum);
+            if (a.db) store1(static_cast<P*>(a.db) + i, b_sum);
+        }
+    };
     if constexpr (NT == 0) {
         // the rows' groups of a wavefront, then the wavefronts one after the other
         for (uint32_t m = lanes; m < 64u; m <<= 1)
@@ -495,20 +505,36 @@ __global__ __launch_bounds__(kThreadsOf(NT)) void norm_backward_kernel(const Nor
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < a.D; i += kSubThreads) {
             const uint32_t v = i / N, e = i - At(v, a.D).at, at = (v / lanes * N + e) * lanes + (v & (lanes - 1u));
-            out[i] = lds[at];
-            out[a.D + i] = lds[span + at];
+            put(i, lds[at], lds[span + at]);
         }
     } else {
 #pragma unroll
         for (int p = 0; p < VPL; ++p) {
             const At at(again<NT>(l) + p * lanes, a.D);
             if (!at.any()) continue;
+            float b[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) b[e] = kLds ? db_lds[(p * N + e) * 1024 + l] : db[kSums && !kLds ? p : 0][e];
+            if (at.whole()) {  // (whole vectors: value by value 4096 x 30752 bfloat16 took 229 us, 204 so)
+                if (a.sums) {
+                    float* out = a.sums + (size_t)blockIdx.x * 2u * a.D + at.at;
+                    __builtin_memcpy(out, dw[kSums ? p : 0], sizeof(b));
+                    __builtin_memcpy(out + a.D, b, sizeof(b));
+                } else {
+                    P wp[N], bp[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        store1(wp + e, dw[kSums ? p : 0][e]);
+                        store1(bp + e, b[e]);
+                    }
+                    if (a.dw) __builtin_memcpy(static_cast<P*>(a.dw) + at.at, wp, sizeof(wp));
+                    if (a.db) __builtin_memcpy(static_cast<P*>(a.db) + at.at, bp, sizeof(bp));
+                }
+                continue;
+            }
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (at.own(e)) {
-                    out[at.at + e] = dw[kSums ? p : 0][e];
-                    out[a.D + at.at + e] = kLds ? db_lds[(p * N + e) * 1024 + l] : db[kSums && !kLds ? p : 0][e];
-                }
+                if (at.own(e)) put(at.at + e, dw[kSums ? p : 0][e], b[e]);
         }
     }
 }
@@ -592,13 +618,18 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const NormBackward a, ui
         __syncthreads();
     }
     float* out = a.sums + (size_t)blockIdx.y * 2u * a.D;
-    if (wave == 3)
+    if (wave != 3) return;
+    if (at.whole()) {
+        __builtin_memcpy(out + col, dw, sizeof(dw));
+        __builtin_memcpy(out + a.D + col, db, sizeof(db));
+        return;
+    }
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (at.own(e)) {
-                out[col + e] = dw[e];
-                out[a.D + col + e] = db[e];
-            }
+    for (int e = 0; e < N; ++e)
+        if (at.own(e)) {
+            out[col + e] = dw[e];
+            out[a.D + col + e] = db[e];
+        }
 }
 
 // The workgroups' sums in their order: 64 columns a workgroup, their sums dealt to 16 wavefronts.
@@ -646,7 +677,10 @@ Plan plan_of(const pxr_layer_norm_desc& d, uint32_t widest) {
     if (p.sums_inside) {
         // two workgroups of up to 512 threads, or one of 1024, for each compute unit
         const uint64_t need = (d.n_rows + p.groups - 1u) / p.groups, most = p.vectors <= 1024u ? 2u * kCus : kCus;
-        p.parts = (uint32_t)(need < most ? need : most);
+        // Few rows are one workgroup's, whose sums are the results: no second kernel and no workspace (a call from Python, fp32: 16 x 256 12.2 us, otherwise 16.5;
+        // 2 x 5000 12.7 / 17.0; but 4 x 30000 43 / 26).
+        const bool few = need == 1u || (need <= 4u && need * p.vectors <= 4096u);
+        p.parts = few && need ? 1u : (uint32_t)(need < most ? need : most);
     } else {
         const uint32_t across = (p.vectors + 63u) / 64u;
         uint64_t parts = (4u * kCus + across - 1u) / across;
@@ -709,10 +743,15 @@ void forward_as(const pxr_layer_norm_desc& d, NormForward a, hipStream_t st) {
 }
 
 template <class T, class P>
-void backward_as(const pxr_layer_norm_desc& d, NormBackward a, void* dw, void* db, hipStream_t st) {
+void backward_as(const pxr_layer_norm_desc& d, NormBackward a, float* sums, void* dw, void* db, hipStream_t st) {
     constexpr uint32_t N = Vec<T>::N;
     const Plan p = plan_of(d, kWidestBackward);
     a.lanes = p.lanes;
+    const bool alone = p.sums_inside && p.parts == 1u;
+    if (alone)
+        a.dw = dw, a.db = db;
+    else if (dw || db)
+        a.sums = sums;
     const auto lds_of = [&](uint32_t vpl, uint32_t u, bool in_lds) {
         const uint32_t sums = p.lanes * vpl * N * 2u * 4u, turns = 2u * 2u * u * 16u * 4u;
         return p.lanes ? sums : turns + (in_lds ? vpl * N * 1024u * 4u : 0u);
@@ -756,7 +795,7 @@ void backward_as(const pxr_layer_norm_desc& d, NormBackward a, void* dw, void* d
         }
     }
 #undef PXR_NORM
-    if (dw || db)
+    if ((dw || db) && !alone)
         hipLaunchKernelGGL((norm_finish_kernel<P>), dim3((uint32_t)((2ull * d.width + 63u) / 64u)), dim3(1024), 0, st, a.sums, p.parts, d.width,
                            static_cast<P*>(dw), static_cast<P*>(db));
 }
@@ -770,7 +809,10 @@ int launched(std::string& err) {
 
 }  // namespace
 
-size_t layer_norm_workspace(const pxr_layer_norm_desc& d) { return (size_t)plan_of(d, kWidestBackward).parts * 2u * d.width * sizeof(float); }
+size_t layer_norm_workspace(const pxr_layer_norm_desc& d) {
+    const Plan p = plan_of(d, kWidestBackward);
+    return p.sums_inside && p.parts == 1u ? 0 : (size_t)p.parts * 2u * d.width * sizeof(float);
+}
 
 int launch_layer_norm_forward(const pxr_layer_norm_desc& d, const void* x, const void* w, const void* b, void* y, float* mean, float* rstd,
                               void* stream, std::string& err) {
@@ -789,14 +831,14 @@ int launch_layer_norm_forward(const pxr_layer_norm_desc& d, const void* x, const
 int launch_layer_norm_backward(const pxr_layer_norm_desc& d, const void* dy, const void* x, const float* mean, const float* rstd,
                                const void* w, void* dx, void* dw, void* db, void* ws, void* stream, std::string& err) {
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const NormBackward a{dy, x, mean, rstd, w, dx, dw || db ? static_cast<float*>(ws) : nullptr, d.y_stride, d.x_stride, d.dx_stride,
-                         (uint32_t)d.n_rows, d.width, 0u};
+    const NormBackward a{dy, x, mean, rstd, w, dx, nullptr, nullptr, nullptr, d.y_stride, d.x_stride, d.dx_stride, (uint32_t)d.n_rows, d.width, 0u};
+    float* sums = static_cast<float*>(ws);
     if (d.dtype == PXR_F32)
-        backward_as<float, float>(d, a, dw, db, st);
+        backward_as<float, float>(d, a, sums, dw, db, st);
     else if (d.param_dtype == PXR_F32)
-        backward_as<__bf16, float>(d, a, dw, db, st);
+        backward_as<__bf16, float>(d, a, sums, dw, db, st);
     else
-        backward_as<__bf16, __bf16>(d, a, dw, db, st);
+        backward_as<__bf16, __bf16>(d, a, sums, dw, db, st);
     return launched(err);
 }
 

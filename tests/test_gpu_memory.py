@@ -232,6 +232,33 @@ def test_layer_norm_gradient_by_differences(torch, pxr):
         assert abs((f(*move(h * d)) - f(*move(-h * d))) / (2 * h) - want) < 3 * h * h * size + 8 * U * np.sqrt(8000.0) / h
 
 
+@pytest.mark.parametrize("N,D", [(1, 100), (16, 256), (60, 64), (3, 1300), (2, 8000), (1, 30000), (500, 64), (40, 5000), (5, 40000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layer_norm_sums_of_one_kind(torch, pxr, N, D, dtype):
+    """dweight without dbias, dbias without dweight, neither: the same as of both, and what is not asked for is not written."""
+    import ctypes as C
+    rng = np.random.default_rng(N + D)
+    x, dy = gpu(torch, rng.standard_normal((N, D)), dtype), gpu(torch, rng.standard_normal((N, D)), dtype)
+    w = gpu(torch, rng.standard_normal(D))
+    _, mean, rstd = pxr.layer_norm(x, w)
+    both = pxr.layer_norm_backward(dy, x, mean, rstd, w)
+    code = 1 if dtype == "bf16" else 0
+    d = pxr.LayerNormDesc(code, 0, N, D, 0.0, D, D, D)
+    need = C.c_size_t()
+    assert pxr.lib().pxr_layer_norm_workspace(C.byref(d), C.byref(need)) == pxr.OK
+    ws = torch.empty(max(16, need.value), dtype=torch.uint8, device="cuda")
+    for want in ((1, 0), (0, 1), (0, 0)):
+        dx = torch.empty_like(x)
+        sums = [torch.full((D + 2,), 7.0, device="cuda") for _ in want]
+        at = [s[1:].data_ptr() if k else None for s, k in zip(sums, want)]
+        assert pxr.lib().pxr_layer_norm_backward(C.byref(d), dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), w.data_ptr(), dx.data_ptr(),
+                                                 *at, ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == pxr.OK
+        assert torch.equal(dx, both[0])
+        for s, k, ref in zip(sums, want, both[1:]):
+            assert s[0] == 7 and s[-1] == 7
+            assert torch.equal(s[1:-1], ref) if k else bool((s == 7).all())
+
+
 def test_layer_norm_sums_have_one_order(torch, pxr):
     rng = np.random.default_rng(8)
     for N, D in ((5000, 64), (300, 30752), (70000, 33)):
