@@ -361,22 +361,26 @@ int pxr_linear_attention_workspace(const pxr_linear_attention* a, uint32_t dtype
 
 /* All steps of a rollout at once: out [n_envs,n_steps,n_heads,d_value] of the rollout's type, and the state after the last step
  * in d_state_out [n_envs,n_heads,d_key,d_value] (NULL if not wanted; not the buffer of d_state).  n_steps == 0 passes the
- * state on.  An infinity or NaN in a step's k or v reaches that step and the later ones of the same episode and no others.
- * Errors: INVALID_ARG (null, n_envs == 0, n_envs * n_heads above 2^21, n_steps above 2^31-1, a type that is none, a buffer not aligned to its elements, states that
- * overlap, workspace missing, too small or not 16-byte aligned); DEVICE. */
+ * state on.  An infinity or NaN in a step's k or v reaches that step and the later ones of the same episode and no others (an
+ * infinity may come out as NaN; fp32 values above bfloat16's largest, 3.389e38, count as one, and those below 1e-33 keep fewer
+ * digits).  out must not overlap what is read.
+ * Errors: INVALID_ARG (null, n_envs == 0, n_envs * n_heads above 2^21, n_steps above 2^31-1, a type that is none, a buffer
+ * not aligned to its elements, states that overlap, workspace missing, too small or not 16-byte aligned); DEVICE. */
 int pxr_linear_attention_forward(pxr_linear_attention* a, const pxr_rollout* r, const pxr_tokens* out, float* d_state_out,
                                  void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Gradients for the outputs' gradients dout (strides as given) and d_dstate_out (of the state after the last step; NULL = zeros):
  * dq, dk [n_envs,n_steps,n_heads,d_key], dv [.., d_value] of the rollout's type and, unless NULL, d_dstate
  * [n_envs,n_heads,d_key,d_value] fp32, of the state before the first step.  Probabilities and states are computed again, nothing
- * is kept from the forward pass.  Equal inputs give equal bits.  Errors: as for the forward pass. */
+ * is kept from the forward pass.  What is written must not overlap what is read.  Equal inputs give equal bits.
+ * Errors: as for the forward pass. */
 int pxr_linear_attention_backward(pxr_linear_attention* a, const pxr_rollout* r, const pxr_tokens* dout,
                                   const float* d_dstate_out, const pxr_tokens* dq, const pxr_tokens* dk, const pxr_tokens* dv,
                                   float* d_dstate, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 /* One step of every environment: r->n_steps must be 1 (the step strides do not matter), d_state [n_envs,n_heads,d_key,d_value]
- * is updated in place (r->d_state is not read; 4-byte aligned).  One kernel.  Errors: as for the forward pass. */
+ * is updated in place (r->d_state is not read; 4-byte aligned); out must not overlap what is read.  One kernel.
+ * Errors: as for the forward pass. */
 int pxr_linear_attention_step(pxr_linear_attention* a, const pxr_rollout* r, float* d_state, const pxr_tokens* out, void* hip_stream);
 
 /* Scene facts for callers and tests (sizes of what pxr_create_scene built; no passage of the paper): total

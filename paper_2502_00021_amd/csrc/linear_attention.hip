@@ -14,18 +14,24 @@
 //   S <- [no episode begins] g^n S + sum_j [no episode begins after j] g^(n-1-j) key_scale y_j z_j^T
 // and mirrored from the end for the reverse scans, whose state decays on its way out of a step instead of on its way in.
 //
-// All four products run on the matrix cores, 32 x 32 tiles, sums in fp32.  A wavefront has 32 columns of z and of the state; its state stays in
-// its accumulators [a][32] for the whole scan.  What makes that cheap is that a product's result lies in a lane as the next product wants
-// its operand: a lane has one column and, of every 16 rows, the eight 4h .. 4h+3, 8+4h .. 8+4h+3 (h = lane / 32), and an operand's lane has one row and
-// eight values of the axis that is summed over, whose order is free as long as both operands agree on it.  So P^T = y x^T (a column is a
-// step i) is the right operand of out^T = z^T P^T, and S the left one of S^T x^T, without a move between lanes.  z and y are also
-// wanted with steps along the summed axis: bfloat16 by the transposing LDS read, fp32 by four-byte reads.
+// All four products run on the matrix cores, 32 x 32 tiles of 16 summed values, bfloat16 operands, sums in fp32.  A wavefront has 32 columns of z and of the
+// state; its state stays in its accumulators [a][32] for the whole scan.  What makes that cheap is that a product's result lies in a lane as the next product
+// wants its operand: a lane has one column and, of every 16 rows, the eight 4h .. 4h+3, 8+4h .. 8+4h+3 (h = lane / 32), and an operand's lane has one row and
+// eight values of the axis that is summed over, whose order is free as long as both operands agree on it.  So P^T = y x^T (a column is a step i) is the right
+// operand of out^T = z^T P^T, and S the left one of S^T x^T, without a move between lanes.  z and y are also wanted with steps along the summed axis: by the
+// transposing LDS read.
 //
-// bfloat16 rounds what is multiplied again: P, S and the weighted z are fp32 and go in as sums of two bfloat16 (P, S: relative error 2^-17 instead of
-// 2^-9, so that an output has its own rounding and no other) or three (z: 2^-25, the state is an fp32 result).  The matrix cores have the time: the scan is
-// bound by memory.
+// Roundings.  What is fp32 goes in as a sum of bfloat16 parts.  Of bfloat16 tensors: P and S as two (relative error 2^-17, an output has its own rounding of 2^-9
+// and no other), the weighted z as three (2^-25, the state is an fp32 result).  Of fp32 tensors: everything as three, six products of the nine, the rest is below
+// 2^-25; six instructions of 32 clocks instead of eight of 64 (128 x 256 with 8 heads of 128: 295 us with fp32 operands, 243 so; gradients 760, 593).  The
+// last parts of values under 2^-110 are below the smallest normal number and go: such values keep fewer digits.
 //
-// Steps that hold an infinity or NaN in y or z are taken one by one: 0 times such a value would reach steps that it must not.
+// Bound by memory where heads and environments fill the device: 512 x 256 with 8 heads of 64 in bfloat16 169 us (4.0 TB/s), its gradients 400 (2.9; each step's
+// rows are read by up to three scans, from one die's L2), 4000 single steps of 8 heads 201 (5.3).  Few long rollouts are cut into segments, whose own states are
+// found first and joined: 20000 steps of 8 heads of 64 x 128 81 us, twice the reading.  A chunk alone on a compute unit takes 3 us, 5 in fp32: instructions, one after the other.
+//
+// Steps that hold an infinity or NaN (or what rounds to an infinity of bfloat16) in y or z are taken one by one: 0 times such a value would reach steps that it
+// must not.  Where it does reach, parts of an infinity are no numbers, so that a NaN may come out in its place.
 
 #include <hip/hip_runtime.h>
 
@@ -749,8 +755,7 @@ uint32_t width_of(uint32_t a) { return a <= 32u ? 32u : a <= 64u ? 64u : a <= 12
 // heads of 96 x 48 in fp32, which do not fill the device, 83 / 92).
 bool together(const LinearAttentionConsts& c) { return width_of(c.dk) == width_of(c.dv) && waves_of(c.dk, c.dv) == waves_of(c.dv, c.dk); }
 
-// Segments of a rollout's steps: as many as it takes to fill the device (a compute unit holds 12 wavefronts of the narrower kernels, 8 of those of 128 and 4 of
-// those of 256), of two chunks at least, and of one for every 4096 cells of a state: a segment costs its state, written, joined and read.  us with a
+// Segments of a rollout's steps: as many as it takes to fill the device (the places that registers and LDS leave on each compute unit), of two chunks at least, and of one for every 4096 cells of a state: a segment costs its state, written, joined and read.  us with a
 // workgroup for each place / with two for each compute unit: 30 x 2000 with 8 heads of 64 131 / 198, 64 x 1000 with 4 of 32 50 / 78, 4 x 1000 with 3 of 96 x 48 in
 // fp32 62 / 86; 16 x 512 with 16 of 128 x 96, whose two are all there is room for, 126, with four 153.
 uint32_t segments_of(const LinearAttentionConsts& c, uint32_t dtype, uint32_t n_envs, uint32_t n_steps, bool backward, uint32_t* seg_steps) {
