@@ -572,6 +572,13 @@ def _empty(torch, like, stream, shape, dtype):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
+def _empty_like(torch, like, stream):
+    """Device memory of a tensor's shape and type, contiguous (for one that is contiguous itself, at less cost)."""
+    if stream is None and like.is_contiguous():
+        return torch.empty_like(like)
+    return _empty(torch, like, stream, like.shape, like.dtype)
+
+
 def _rows(x):
     """Rows, width and the values from row to row of [..., D] (raises if there is no single such number)."""
     assert x.is_cuda and x.dim() >= 1 and x.shape[-1] > 0, "a CUDA tensor [..., width]"
@@ -606,12 +613,12 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     dtype = x.dtype
     params = _params(torch, x, width, weight, bias)
     if out is None:
-        out, y_stride = _empty(torch, x, stream, x.shape, dtype), width
+        out, y_stride = _empty_like(torch, x, stream), width
     else:
         assert out.is_cuda and out.dtype == dtype and out.shape == x.shape
         y_stride = _rows(out)[2]
-    lead = x.shape[:-1]
-    mean, rstd = _empty(torch, x, stream, lead, torch.float32), _empty(torch, x, stream, lead, torch.float32)
+    mean = _empty(torch, x, stream, x.shape[:-1], torch.float32)
+    rstd = _empty_like(torch, mean, stream)
     d = _pack_norm(_dtype_code(torch, dtype), _dtype_code(torch, params), n, width, eps, x_stride, y_stride, width)
     _check((_lib or lib()).pxr_layer_norm_forward(d, x.data_ptr(), _ptr(weight), _ptr(bias), out.data_ptr(), mean.data_ptr(),
                                                   rstd.data_ptr(), _stream_handle(stream, x)))
@@ -631,11 +638,12 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, params_dtype=No
     params = _params(torch, x, width, weight) if weight is not None else params_dtype or torch.float32
     assert params in (torch.float32, dtype)
     if dx is None:
-        dx, dx_stride = _empty(torch, x, stream, x.shape, dtype), width
+        dx, dx_stride = _empty_like(torch, x, stream), width
     else:
         assert dx.is_cuda and dx.dtype == dtype and dx.shape == x.shape
         dx_stride = _rows(dx)[2]
-    dweight, dbias = _empty(torch, x, stream, (width,), params), _empty(torch, x, stream, (width,), params)
+    dweight = _empty(torch, x, stream, (width,), params)
+    dbias = _empty_like(torch, dweight, stream)
     d = _pack_norm(_dtype_code(torch, dtype), _dtype_code(torch, params), n, width, 0.0, x_stride, dy_stride, dx_stride)
     L = _lib or lib()
     need = C.c_size_t()
@@ -659,6 +667,7 @@ class LinearAttention:
         h = C.c_void_p()
         _check(lib().pxr_linear_attention_create(C.byref(d), C.byref(h)))
         self._h = h
+        self._asked = (None, 0)
         self.H, self.dk, self.dv, self.scale = int(n_heads), int(d_key), int(d_value), d.scale
 
     def close(self):
@@ -701,9 +710,13 @@ class LinearAttention:
         return packed, keys, values, B, T
 
     def _workspace(self, torch, like, B, T, backward, stream):
-        need = C.c_size_t()
-        _check(_lib.pxr_linear_attention_workspace(self._h, _dtype_code(torch, like.dtype), B, T, backward, need))
-        need = need.value
+        sizes = (like.dtype, B, T, backward)
+        asked, need = self._asked  # (the bytes for the sizes that were asked for last are known)
+        if asked != sizes:
+            n = C.c_size_t()
+            _check(_lib.pxr_linear_attention_workspace(self._h, _dtype_code(torch, like.dtype), B, T, backward, n))
+            need = n.value
+            self._asked = (sizes, need)
         return _empty(torch, like, stream, (need,), torch.uint8) if need else None, need
 
     def forward(self, q, k, v, resets=None, state=None, out=None, state_out=None, stream=None):
@@ -713,8 +726,10 @@ class LinearAttention:
         torch = _torch or _torch_module()
         assert q.dim() == 4
         r, keys, values, B, T = self._rollout(torch, q, k, v, resets, state)
-        out = _empty(torch, q, stream, values, q.dtype) if out is None else out
-        state_out = _empty(torch, q, stream, (B, self.H, self.dk, self.dv), torch.float32) if state_out is None else state_out
+        out = _empty_like(torch, v, stream) if out is None else out
+        if state_out is None:
+            state_out = (_empty(torch, q, stream, (B, self.H, self.dk, self.dv), torch.float32) if state is None else
+                         _empty_like(torch, state, stream))
         ws, need = self._workspace(torch, q, B, T, 0, stream)
         _check(_lib.pxr_linear_attention_forward(self._h, r, _pack_tokens(*self._view(out, values, q.dtype)), self._state(torch, state_out, B),
                                                  _ptr(ws), need, _stream_handle(stream, q)))
@@ -728,8 +743,9 @@ class LinearAttention:
         assert q.dim() == 4
         r, keys, values, B, T = self._rollout(torch, q, k, v, resets, state)
         dtype = q.dtype
-        dq, dk, dv = (_empty(torch, q, stream, shape, dtype) for shape in (keys, keys, values))
-        dfirst = None if state is None else _empty(torch, q, stream, state.shape, torch.float32)
+        dq = _empty_like(torch, q, stream)
+        dk, dv = _empty_like(torch, dq, stream), _empty_like(torch, v, stream)
+        dfirst = None if state is None else _empty_like(torch, state, stream)
         ws, need = self._workspace(torch, q, B, T, 1, stream)
         _check(_lib.pxr_linear_attention_backward(
             self._h, r, _pack_tokens(*self._view(dout, values, dtype)), None if dstate is None else self._state(torch, dstate, B),
@@ -743,7 +759,7 @@ class LinearAttention:
         torch = _torch or _torch_module()
         assert q.dim() == 3
         r, _, values, B, _ = self._rollout(torch, q, k, v, resets, None)
-        out = _empty(torch, q, stream, values, q.dtype) if out is None else out
+        out = _empty_like(torch, v, stream) if out is None else out
         _check(_lib.pxr_linear_attention_step(self._h, r, self._state(torch, state, B), _pack_tokens(*self._view(out, values, q.dtype)),
                                               _stream_handle(stream, q)))
         return out
