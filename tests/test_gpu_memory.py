@@ -330,6 +330,23 @@ def check_attention(torch, pxr, q, k, v, r, s, ld, dout, ds, scale=None, backwar
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [128, 200, 330, 500, 580, 1100, 2300])
+def test_attention_of_few_long_rollouts(torch, pxr, T, dtype):
+    """Cut into 2 to 35 segments, whose states are joined a few at a time."""
+    rng = np.random.default_rng(T)
+    check_attention(torch, pxr, *inputs(torch, rng, 1, T, 1, 24, 16, dtype, resets=0.003))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,H,dk,dv", [(1, 700, 1, 64, 128), (2, 40, 3, 128, 64), (1, 900, 2, 16, 100), (3, 70, 2, 100, 33), (1, 600, 1, 200, 40), (2, 65, 1, 40, 250),
+                                         (2, 33, 2, 32, 64), (1, 300, 2, 60, 30)])
+def test_attention_of_keys_and_values_of_different_widths(torch, pxr, B, T, H, dk, dv, dtype):
+    """Their gradients take kernels of their own; states whose last block of 32 rows is not whole, columns too."""
+    rng = np.random.default_rng(T + dk)
+    check_attention(torch, pxr, *inputs(torch, rng, B, T, H, dk, dv, dtype, resets=0.01))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [1, 2, 15, 16, 31, 32, 33, 63, 64, 65, 96, 127, 129, 200, 333])
 def test_attention_lengths(torch, pxr, T, dtype):
     rng = np.random.default_rng(T)
