@@ -625,9 +625,13 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     return out, mean, rstd
 
 
+_norm_asked = (None, 0)
+
+
 def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, params_dtype=None, stream=None):
     """Gradients of layer_norm for dy (x's shape and type), with the mean and rstd that it returned.  Returns (dx, dweight,
     dbias), the latter two [D] of the weight's type (without a weight: params_dtype, float32 unless given); enqueue only."""
+    global _norm_asked
     torch = _torch or _torch_module()
     n, width, x_stride = _rows(x)
     dtype = x.dtype
@@ -646,9 +650,12 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, params_dtype=No
     dbias = _empty_like(torch, dweight, stream)
     d = _pack_norm(_dtype_code(torch, dtype), _dtype_code(torch, params), n, width, 0.0, x_stride, dy_stride, dx_stride)
     L = _lib or lib()
-    need = C.c_size_t()
-    _check(L.pxr_layer_norm_workspace(d, need))
-    need = need.value
+    asked, need = _norm_asked  # (the bytes for the description that was asked for last are known)
+    if asked != d:
+        size = C.c_size_t()
+        _check(L.pxr_layer_norm_workspace(d, size))
+        need = size.value
+        _norm_asked = (d, need)
     ws = _empty(torch, x, stream, (need,), torch.uint8) if need else None
     _check(L.pxr_layer_norm_backward(d, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dx.data_ptr(),
                                      dweight.data_ptr(), dbias.data_ptr(), _ptr(ws), need, _stream_handle(stream, x)))
