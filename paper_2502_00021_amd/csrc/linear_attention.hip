@@ -348,7 +348,8 @@ constexpr uint32_t waves_per_simd(uint32_t width, uint32_t element) { return wid
 template <class T, int A, int kWaves, bool kOut>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(waves_per_simd(A, sizeof(T))))) void scan_kernel(
     const Scans scans, const Cut cut, uint32_t roles, float* local0, float* local1, uint32_t* whole0, uint32_t* whole1) {
-    // (requests a chunk ahead take registers; where they do not fit, a chunk's requests go out together when it begins)
+    // (requests a chunk ahead take registers; where they do not fit, a chunk's requests go out together when it begins: 256 x 128 with 8 heads of 64 50 us
+    // ahead, 53 not; with 4 of 128 x 64 37 not, 40 ahead)
     constexpr bool kAhead = A <= 64;
     constexpr uint32_t kThreads = kWaves * 64, kWidthZ = kWaves * 32, kStrideA = A + kPad<__bf16>, kStrideZ = kWidthZ + kPad<T>;
     constexpr uint32_t kPlane = C * kStrideA, kTile = kPlane * kParts<T>;  // of x and y
@@ -760,7 +761,8 @@ int launched(std::string& err) {
     return PXR_ERR_DEVICE;
 }
 
-// Wavefronts of a workgroup: enough for z, four at most, and no fewer than it takes to bring the steps of long heads.
+// Wavefronts of a workgroup: enough for z, four at most, and no fewer than it takes to bring the steps of long heads (256 x 128 with 8 heads in bfloat16:
+// 64 x 64 two 50 us, four 73; 64 x 128 four 72, two 79; 32 x 32 one 21.9, two 22.6).
 uint32_t waves_of(uint32_t a, uint32_t b) { return a > 128u ? 4u : b <= 32u && a <= 64u ? 1u : b <= 64u ? 2u : 4u; }
 
 uint32_t width_of(uint32_t a) { return a <= 32u ? 32u : a <= 64u ? 64u : a <= 128u ? 128u : 256u; }
@@ -935,8 +937,9 @@ int launch_linear_attention_step(const LinearAttentionConsts& c, const pxr_rollo
     Step a{r.q, r.k, r.v, out, c.dk, c.dv, c.n_heads, r.n_envs * c.n_heads, 1u, c.scale, c.heads, r.d_resets, r.resets_env, state};
     const uint32_t vec = c.dv < 4u ? 1u : 4u;
     while (a.lanes * vec < c.dv) a.lanes *= 2u;
-    // a wavefront for a state of up to 16 KB; four for longer ones, and where there are so few that the device has wavefronts to spare
-    const bool four = c.dk * c.dv > 4096u || a.rows < 4u * c.n_cus;
+    // A wavefront for a state of up to 16 KB; four for longer ones (8000 of 128 x 128 203 us, with one 217; 32000 of 32 x 32 42, with four 114), and where there are
+    // so few that the device has wavefronts to spare (400 of 64 x 64 5.0, with one 5.9; 800 7.7, with one 6.7).
+    const bool four = c.dk * c.dv > 4096u || a.rows < 2u * c.n_cus;
     const dim3 grid(four ? a.rows : (a.rows + 3u) / 4u);
 #define PXR_STEP(T, V, W) hipLaunchKernelGGL((step_kernel<T, V, W>), grid, dim3(256), 0, st, a)
 #define PXR_STEP_AS(T)          \
