@@ -39,6 +39,7 @@
 #include <type_traits>
 
 #include "pxr_internal.h"
+#include "steps.h"
 
 namespace pxr {
 namespace {
@@ -75,8 +76,6 @@ struct Scan {
 struct Scans {
     Scan s[3];
 };
-
-constexpr int C = 32;  // steps of a chunk
 
 // How the steps are cut: a workgroup takes one segment of one (environment, head) and 32 columns a wavefront.
 struct Cut {
@@ -229,35 +228,27 @@ __device__ __forceinline__ uint32_t again(uint32_t v) {
 }
 
 // A chunk's steps on their way to a tile: C rows of `kWidth` values, dealt to kThreads lanes in vectors of 16 bytes.  The requests of a chunk go out
-// together, a chunk ahead.  Rows may begin at any element (the memory takes 16-byte requests at any address).  A row of d values that ends inside a
-// vector has its last vector moved back to its end; rows past the last and vectors past a row's end read what is there instead and are not written,
-// or written as zeros.  The columns past d are zero from the start and nothing writes them.  Rows shorter than a vector are read value by value,
-// when they are written.
+// together, a chunk ahead.  Rows may begin at any element (the memory takes 16-byte requests at any address).  What a lane asks for is in steps.h: what it
+// asks for in place of rows past the last and vectors past a row's end is not written, or written as zeros.  The columns past d are zero from the start and
+// nothing writes them.  Rows shorter than a vector are read value by value, when they are written.
 // kOperand: a tile of x or y, its columns placed and fp32 values as three planes of bfloat16 parts.
 template <class T, int kWidth, int kThreads, bool kOperand>
 struct Steps {
     static constexpr bool kSplit = kOperand && sizeof(T) == 4;
     typedef std::conditional_t<kSplit, __bf16, T> E;  // of the tile
-    static constexpr uint32_t N = 16 / sizeof(T), kPerRow = kWidth / N, kCount = (C * kPerRow + kThreads - 1) / kThreads, kStride = kWidth + kPad<E>, kPlane = C * kStride;
-    static constexpr uint32_t kRowsEach = kThreads / kPerRow;  // rows that the lanes take together
-    static_assert(kThreads % kPerRow == 0);
+    typedef Dealt<sizeof(T), kWidth, kThreads> D;
+    static constexpr uint32_t N = D::N, kPerRow = D::kPerRow, kCount = D::kCount, kRowsEach = D::kRowsEach, kStride = kWidth + kPad<E>, kPlane = C * kStride;
     uint32_t row, col, d;
     int64_t step, offset;  // values from row to row; the lane's first vector from the chunk's first value
     u32x4 v[kCount];
 
-    __device__ __forceinline__ Steps(int64_t step, uint32_t d) : row(threadIdx.x / kPerRow), col(threadIdx.x % kPerRow * N), d(d), step(step) {
-        offset = (int64_t)row * step + (d < N ? 0u : min(col, d - N));
-    }
+    __device__ __forceinline__ Steps(int64_t step, uint32_t d) : row(D::row(threadIdx.x)), col(D::col(threadIdx.x)), d(d), step(step), offset(D::offset(row, col, d, step)) {}
     // n >= 1 rows
     __device__ __forceinline__ void ask(const T* from, uint32_t n) {
         const uint32_t d = again(this->d);
         if (d < N) return forget();
 #pragma unroll
-        for (uint32_t i = 0; i < kCount; ++i) {
-            const T* p = from + (int64_t)(i * kRowsEach) * step + offset;
-            if (n < (uint32_t)C && row + i * kRowsEach >= n) p = from + min(col, d - N);
-            __builtin_memcpy(&v[i], p, 16);
-        }
+        for (uint32_t i = 0; i < kCount; ++i) __builtin_memcpy(&v[i], D::request(from, i, n, row, col, d, step, offset), 16);
     }
     // What was asked for has been put; nothing is in flight.  (Without this the registers would be kept, and copied, from chunk to chunk.)
     __device__ __forceinline__ void forget() {
@@ -391,7 +382,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
     Steps<T, kWidthZ, kThreads, false> z_steps(s.z.step, widthB);
     uint32_t reset = 0;
     const uint32_t has_resets = cut.resets != nullptr;
-    const auto step_of = [&](uint32_t at, uint32_t n) { return again(s.reverse) ? (int64_t)(cut.n_steps - at - n) : (int64_t)at; };  // a chunk's first step in memory
+    const auto step_of = [&](uint32_t at, uint32_t n) { return first_step(again(s.reverse) != 0u, cut.n_steps, at, n); };  // a chunk's first step in memory
     const auto ask = [&](uint32_t at, uint32_t n) {
         const int64_t t = step_of(at, n);
         reset = again(has_resets) && lane < n ? resets[(t + lane) * cut.resets_step] : 0u;
@@ -816,18 +807,8 @@ void enqueue_as(const Scan* s, uint32_t roles, const Cut& cut, float* const* loc
     case A + W:                                                                                                                                   \
         hipLaunchKernelGGL((scan_kernel<T, A, W, kOut>), grid, dim3(W * 64), scan_lds(sizeof(T), A, W, kOut), st, scans, cut, roles, local[0], local[1], \
                            whole[0], whole[1]);                                                                                                   \
-        break
-    switch (cut.width + cut.waves) {
-        PXR_SCAN(32, 1);
-        PXR_SCAN(32, 2);
-        PXR_SCAN(32, 4);
-        PXR_SCAN(64, 1);
-        PXR_SCAN(64, 2);
-        PXR_SCAN(64, 4);
-        PXR_SCAN(128, 2);
-        PXR_SCAN(128, 4);
-        PXR_SCAN(256, 4);
-    }
+        break;
+    switch (cut.width + cut.waves) { PXR_SCAN_SHAPES(PXR_SCAN) }
 #undef PXR_SCAN
 }
 
