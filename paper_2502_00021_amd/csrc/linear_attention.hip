@@ -573,13 +573,17 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
 #pragma unroll
             for (int db = 0; db < A / 32; ++db) state[db] = (f32x16)0.0f;
         }
+        // In reverse, a chunk whose first step begins an episode adds nothing to the state, and its steps, all weighted with zero, are left out: there may be
+        // one among them that is no number.
+        if (!(reverse && (m & 1u))) {
 #pragma unroll
-        for (int k = 0; k < C / 16; ++k) {
-            const Parts<3> zp = split<3>(values(k ? z1 : z0) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
+            for (int k = 0; k < C / 16; ++k) {
+                const Parts<3> zp = split<3>(values(k ? z1 : z0) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
 #pragma unroll
-            for (int db = 0; db < A / 32; ++db) {
-                if (A > 64 && db == A / 32 - 1 && !last) break;
-                state[db] = mma(across_placed<kParts<T>>(ys + k * 16 * kStrideA + db * 32, kPlane, kStrideA, lane), zp, state[db]);
+                for (int db = 0; db < A / 32; ++db) {
+                    if (A > 64 && db == A / 32 - 1 && !last) break;
+                    state[db] = mma(across_placed<kParts<T>>(ys + k * 16 * kStrideA + db * 32, kPlane, kStrideA, lane), zp, state[db]);
+                }
             }
         }
         __syncthreads();

@@ -481,6 +481,39 @@ def test_attention_what_is_not_finite_reaches_only_later_steps_of_its_episode(to
     layer.close()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("B,T,at", [(2, 20, 0), (2, 20, 7), (2, 63, 32), (2, 200, 100), (2, 200, 0), (1, 1500, 640), (1, 1500, 701)])
+def test_attention_what_is_not_finite_in_a_step_that_begins_an_episode_stays_in_it(torch, pxr, B, T, at, bad, dtype):
+    """Nothing passes an episode's beginning, forward or backward, whole rollouts and such that are cut into segments: what is
+    before it is as near to the definition as it is without that value."""
+    rng = np.random.default_rng(T + at)
+    q, k, v, r, s, ld, dout, ds = inputs(torch, rng, B, T, 2, 32, 32, dtype)
+    r.zero_()
+    r[0, at] = True
+    if at:
+        r[0, at - 1] = True  # an episode of one step before it
+    layer = pxr.LinearAttention(2, 32, 32, ld)
+    args = [f64(x) for x in (dout, q, k, v)]
+    R, S, D = r.cpu().numpy(), f64(s), f64(ds)
+    ref = om.linear_attention_backward(*args, ld, layer.scale, R, S, D)
+    mag = om.linear_attention_backward(*(abs(a) for a in args), ld, abs(layer.scale), R, abs(S), abs(D))
+    bf16 = dtype == "bf16"
+    for which in range(4):
+        x = [t.clone() for t in (dout, q, k, v)]
+        x[which][0, at, 1, 5] = bad
+        got = layer.backward(*x, resets=r, state=s, dstate=ds)
+        for name, g, rf, m in zip(("dq", "dk", "dv"), got, ref, mag):
+            keep = np.ones((B, T, 2), bool)
+            # the step itself; q and dout reach no other step's dq, k and v reach those of later steps of the episode
+            keep[0, at if which < 2 or name != "dq" else slice(at, None), 1] = False
+            close(f64(g)[keep], rf[keep], m[keep], 64 + 32 + T, bf16, (which, name))
+        close(f64(got[3]), ref[3], mag[3], 64 + T, False, (which, "dstate"))
+        if at == 0:
+            assert (got[3][0] == 0).all(), which
+    layer.close()
+
+
 def test_attention_gradients_by_differences(torch, pxr):
     """The kernels' own forward pass, moved along a direction.  It is linear in each input alone, so the difference over any
     distance is the derivative; the directions are small, so that roundings are those of the results themselves."""
