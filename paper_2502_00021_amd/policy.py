@@ -5,12 +5,13 @@
 
 Acting is one step of every environment (`act`, LinearAttention.step, the state updated in place); learning takes whole
 rollouts with the episodes that begin inside them (`forward`, gradients by LinearAttention.backward and
-layer_norm_backward).  The projections are matrix products of PyTorch's.  `python -m paper_2502_00021_amd.policy` renders
-rollouts of the quadruped scene, acts on them and learns from them."""
+layer_norm_backward; a gradient of a gradient is refused).  The projections are matrix products of PyTorch's.
+`python -m paper_2502_00021_amd.policy` renders rollouts of the quadruped scene, acts on them and learns from them."""
 import math
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 from paper_2502_00021_amd import pxr
 
@@ -24,6 +25,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
         dx, dweight, dbias = pxr.layer_norm_backward(dy.contiguous(), x, mean, rstd, weight)
@@ -40,6 +42,7 @@ class _LinearAttention(torch.autograd.Function):
         return out, last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dlast):
         q, k, v, state = ctx.saved_tensors
         dout = torch.zeros_like(v, memory_format=torch.contiguous_format) if dout is None else dout.contiguous()
