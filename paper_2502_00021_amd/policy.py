@@ -36,17 +36,17 @@ class _LinearAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, layer, q, k, v, resets, state):
         out, last = layer.forward(q, k, v, resets=resets, state=state)
-        ctx.layer, ctx.resets = layer, resets
-        ctx.save_for_backward(q, k, v, state)
+        ctx.layer = layer
+        ctx.save_for_backward(q, k, v, resets, state)
         ctx.set_materialize_grads(False)
         return out, last
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout, dlast):
-        q, k, v, state = ctx.saved_tensors
+        q, k, v, resets, state = ctx.saved_tensors
         dout = torch.zeros_like(v, memory_format=torch.contiguous_format) if dout is None else dout.contiguous()
-        dq, dk, dv, dstate = ctx.layer.backward(dout, q, k, v, resets=ctx.resets, state=state,
+        dq, dk, dv, dstate = ctx.layer.backward(dout, q, k, v, resets=resets, state=state,
                                                 dstate=None if dlast is None else dlast.contiguous())
         return None, dq, dk, dv, None, dstate
 
@@ -58,7 +58,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
 
 def linear_attention(layer, q, k, v, resets=None, state=None):
     """LinearAttention.forward for torch.autograd: (out, the last state); gradients for q, k, v and the first state.  (The
-    layer's decays are constants.)"""
+    layer's decays are constants.)  A state that goes on being stepped is cloned first: the backward pass reads the one that
+    was given, and raises where it has been written since."""
     return _LinearAttention.apply(layer, q, k, v, resets, state)
 
 
@@ -96,7 +97,8 @@ class MemoryPolicy(torch.nn.Module):
         return (layer_norm(seen, self.norm_heads).flatten(-2) @ self.w_out.bfloat16()).float()
 
     def forward(self, frames, resets=None, state=None):
-        """A rollout: frames [B,T,S,H,W,3], resets [B,T], state [B,heads,d,d] or None -> actions [B,T,n], the last state."""
+        """A rollout: frames [B,T,S,H,W,3], resets [B,T], state [B,heads,d,d] or None (a clone, if `act` takes the same one before the
+        backward pass) -> actions [B,T,n], the last state."""
         B, T = frames.shape[:2]
         q, k, v = (x.unflatten(0, (B, T)) for x in self._qkv(frames.flatten(0, 1)))
         seen, last = linear_attention(self.memory, q, k, v, resets, state)

@@ -199,6 +199,12 @@ def _check(rc):
         raise PxrError(rc, lib().pxr_last_error().decode())
 
 
+def _written(torch, *tensors):
+    """Tensors of the caller's that a call has written through their pointers: autograd learns that they are other values
+    now, and refuses a backward pass that saved the ones before."""
+    torch.autograd.graph.increment_version(tensors)
+
+
 def make_scene_desc(desc):
     """Plain-dict scene description (see workloads.default_scene) -> (SceneDesc, keep-alive list)."""
     bodies = desc["bodies"]
@@ -496,6 +502,7 @@ class Conv:
         assert frames.is_cuda and frames.dtype == torch.uint8 and frames.is_contiguous()
         B = frames.shape[0]
         assert frames.shape == (B, self.S, self.H, self.W, 3), tuple(frames.shape)
+        given = out is not None
         if out is None:
             out = torch.empty((B, self.Ho, self.Wo, self.C), dtype=torch.bfloat16, device=frames.device)
         else:
@@ -503,6 +510,8 @@ class Conv:
             assert out.shape == (B, self.Ho, self.Wo, self.C)
         stream = _stream_handle(stream, frames)
         _check(_lib.pxr_conv_forward(self._h, frames.data_ptr(), B, out.data_ptr(), stream))
+        if given:
+            _written(torch, out)
         return out
 
 
@@ -549,6 +558,7 @@ class Pipeline:
         stream = _stream_handle(stream, poses)
         _check(_lib.pxr_pipeline_step(self._h, poses.data_ptr(), None if shapes is None else shapes.data_ptr(), B,
                                       int(step0), int(env0), frames.data_ptr(), features.data_ptr(), stream))
+        _written(torch, frames, features)
         return frames, features
 
 
@@ -612,6 +622,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     n, width, x_stride = _rows(x)
     dtype = x.dtype
     params = _params(torch, x, width, weight, bias)
+    given = out is not None
     if out is None:
         out, y_stride = _empty_like(torch, x, stream), width
     else:
@@ -622,6 +633,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     d = _pack_norm(_dtype_code(torch, dtype), _dtype_code(torch, params), n, width, eps, x_stride, y_stride, width)
     _check((_lib or lib()).pxr_layer_norm_forward(d, x.data_ptr(), _ptr(weight), _ptr(bias), out.data_ptr(), mean.data_ptr(),
                                                   rstd.data_ptr(), _stream_handle(stream, x)))
+    if given:
+        _written(torch, out)
     return out, mean, rstd
 
 
@@ -641,6 +654,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, params_dtype=No
         assert s.is_cuda and s.dtype == torch.float32 and s.is_contiguous() and s.numel() == n, "mean and rstd: one float32 for each row"
     params = _params(torch, x, width, weight) if weight is not None else params_dtype or torch.float32
     assert params in (torch.float32, dtype)
+    given = dx is not None
     if dx is None:
         dx, dx_stride = _empty_like(torch, x, stream), width
     else:
@@ -659,6 +673,8 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, params_dtype=No
     ws = _empty(torch, x, stream, (need,), torch.uint8) if need else None
     _check(L.pxr_layer_norm_backward(d, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dx.data_ptr(),
                                      dweight.data_ptr(), dbias.data_ptr(), _ptr(ws), need, _stream_handle(stream, x)))
+    if given:
+        _written(torch, dx)
     return dx, dweight, dbias
 
 
@@ -733,6 +749,7 @@ class LinearAttention:
         torch = _torch or _torch_module()
         assert q.dim() == 4
         r, keys, values, B, T = self._rollout(torch, q, k, v, resets, state)
+        given = [t for t in (out, state_out) if t is not None]
         out = _empty_like(torch, v, stream) if out is None else out
         if state_out is None:
             state_out = (_empty(torch, q, stream, (B, self.H, self.dk, self.dv), torch.float32) if state is None else
@@ -740,6 +757,8 @@ class LinearAttention:
         ws, need = self._workspace(torch, q, B, T, 0, stream)
         _check(_lib.pxr_linear_attention_forward(self._h, r, _pack_tokens(*self._view(out, values, q.dtype)), self._state(torch, state_out, B),
                                                  _ptr(ws), need, _stream_handle(stream, q)))
+        if given:
+            _written(torch, *given)
         return out, state_out
 
     def backward(self, dout, q, k, v, resets=None, state=None, dstate=None, stream=None):
@@ -766,9 +785,11 @@ class LinearAttention:
         torch = _torch or _torch_module()
         assert q.dim() == 3
         r, _, values, B, _ = self._rollout(torch, q, k, v, resets, None)
+        given = (state,) if out is None else (state, out)
         out = _empty_like(torch, v, stream) if out is None else out
         _check(_lib.pxr_linear_attention_step(self._h, r, self._state(torch, state, B), _pack_tokens(*self._view(out, values, q.dtype)),
                                               _stream_handle(stream, q)))
+        _written(torch, *given)
         return out
 
 

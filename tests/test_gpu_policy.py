@@ -101,3 +101,60 @@ def test_learning_lowers_the_loss(torch, policy_module):
         losses.append(float(loss.detach()))
     assert all(p.grad is not None and bool(p.grad.isfinite().all()) for p in policy.parameters())
     assert losses[-1] < 0.5 * losses[0], losses
+
+
+def test_what_is_written_in_place_between_forward_and_backward_is_noticed(torch, policy_module):
+    """A state that goes on being stepped, a buffer that is written again, resets that change: the gradients would be those of the new values."""
+    from paper_2502_00021_amd import pxr
+    layer = pxr.LinearAttention(2, 16, 16, np.float32([-0.05, -0.7]))
+
+    def start():
+        x = [torch.ones((3, 20, 2, 16), device="cuda", requires_grad=True) for _ in range(3)]
+        resets, state = torch.zeros((3, 20), dtype=torch.bool, device="cuda"), torch.ones((3, 2, 16, 16), device="cuda")
+        return x, resets, state, policy_module.linear_attention(layer, *x, resets, state)[0]
+
+    def step(x, resets, state):
+        with torch.no_grad():
+            layer.step(x[0][:, 0], x[1][:, 0], x[2][:, 0], state)
+
+    def again(x, resets, state):
+        layer.forward(x[0].detach(), x[1].detach(), x[2].detach(), state_out=state)
+
+    def outputs(x, resets, state):
+        layer.forward(*(t.detach().clone() for t in x), out=x[2].detach())
+
+    def one_output(x, resets, state):
+        layer.step(x[0].detach()[:, 0], x[1].detach()[:, 0], x[2].detach()[:, 0], state.clone(), out=x[0].detach()[:, 1])
+
+    def mark(x, resets, state):
+        resets[1, 3] = True
+    start()[3].sum().backward()
+    for write in (step, again, outputs, one_output, mark):
+        x, resets, state, out = start()
+        write(x, resets, state)
+        with pytest.raises(RuntimeError, match="inplace"):
+            out.sum().backward()
+    # layer norm: its input written by each call that takes a buffer
+    y = torch.randn((40, 64), device="cuda")
+    _, mean, rstd = pxr.layer_norm(y)
+    for write in (lambda x: pxr.layer_norm(y, out=x), lambda x: pxr.layer_norm_backward(y, y, mean, rstd, dx=x)):
+        x = torch.randn((40, 64), device="cuda", requires_grad=True)
+        out = policy_module.layer_norm(x)
+        write(x.detach())
+        with pytest.raises(RuntimeError, match="inplace"):
+            out.sum().backward()
+    layer.close()
+
+
+def test_features_written_again_before_the_backward_pass_are_noticed(torch, policy_module):
+    """The first layer's features in a buffer that the next step's take, normalised with a weight that learns."""
+    from paper_2502_00021_amd import pxr
+    conv = pxr.Conv(32, 32, 1, np.ones((3, 3, 3, 32), np.float32), np.zeros(32, np.float32))
+    frames = _frames(torch, 4, 1)[:, 0].contiguous()
+    features = conv.forward(frames)
+    weight = torch.ones(features[0].numel(), device="cuda", requires_grad=True)
+    out = policy_module.layer_norm(features.flatten(1), weight)
+    conv.forward(frames, out=features)
+    with pytest.raises(RuntimeError, match="inplace"):
+        out.float().sum().backward()
+    conv.close()

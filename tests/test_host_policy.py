@@ -62,3 +62,12 @@ def test_a_gradient_of_a_gradient_is_refused(stand_ins):
     dq, = torch.autograd.grad(out.square().sum(), q, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         (out.sum() + dq.square().sum()).backward()
+
+
+def test_resets_that_change_between_forward_and_backward_are_noticed(stand_ins):
+    q, k, v = _inputs(*[(2, 3, 1, 4)] * 3)
+    resets = torch.zeros((2, 3), dtype=torch.bool)
+    out = policy.linear_attention(stand_ins, q, k, v, resets)[0]
+    resets[0, 1] = True
+    with pytest.raises(RuntimeError, match="inplace"):
+        out.sum().backward()
