@@ -632,12 +632,14 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const NormBackward a, ui
         }
 }
 
-// The workgroups' sums in their order: 64 columns a workgroup, their sums dealt to 16 wavefronts.
+// The workgroups' sums in their order: 64 columns a workgroup, their sums dealt to 16 wavefronts.  A launch counts its threads in 32 bits, and what is
+// more is dropped without an error: rows of more than 2^27 - 32 values take several layers of kFinishAcross workgroups.
+constexpr uint32_t kFinishAcross = (1u << 22) - 1u;
 template <class P>
 __global__ __launch_bounds__(1024) void norm_finish_kernel(const float* sums, uint32_t parts, uint32_t D, P* dw, P* db) {
     __shared__ float lds[16][64];
     const uint32_t l = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const size_t i = (size_t)blockIdx.x * 64u + l;
+    const size_t i = ((size_t)blockIdx.y * kFinishAcross + blockIdx.x) * 64u + l;
     float s = 0.0f;
     if (i < 2u * (size_t)D)
 #pragma unroll 8
@@ -796,9 +798,11 @@ void backward_as(const pxr_layer_norm_desc& d, NormBackward a, float* sums, void
         }
     }
 #undef PXR_NORM
-    if ((dw || db) && !alone)
-        hipLaunchKernelGGL((norm_finish_kernel<P>), dim3((uint32_t)((2ull * d.width + 63u) / 64u)), dim3(1024), 0, st, a.sums, p.parts, d.width,
+    if ((dw || db) && !alone) {
+        const uint32_t need = (uint32_t)((2ull * d.width + 63u) / 64u), layers = (need + kFinishAcross - 1u) / kFinishAcross;
+        hipLaunchKernelGGL((norm_finish_kernel<P>), dim3(layers > 1u ? kFinishAcross : need, layers), dim3(1024), 0, st, a.sums, p.parts, d.width,
                            static_cast<P*>(dw), static_cast<P*>(db));
+    }
 }
 
 int launched(std::string& err) {

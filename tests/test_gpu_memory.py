@@ -269,6 +269,21 @@ def test_layer_norm_sums_have_one_order(torch, pxr):
             assert all(torch.equal(a, b) for a, b in zip(first, pxr.layer_norm_backward(dy, x, mean, rstd)))
 
 
+def test_layer_norm_sums_of_the_widest_rows(torch, pxr):
+    """More columns than a launch that gives 32 threads to each could count in 32 bits."""
+    D = 2 ** 27 + 1000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x, dy = (torch.randn((1, D), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    mean, rstd = torch.tensor([0.25], device="cuda"), torch.tensor([0.5], device="cuda")
+    dx, dw, db = pxr.layer_norm_backward(dy, x, mean, rstd)
+    assert torch.equal(db, dy[0].float())
+    # (one product, rounded once: a power of two scales it, and x - 0.25 has at most 16 bits where it is not rounded itself)
+    want = dy[0].double() * ((x[0].float() - 0.25) * 0.5).double()
+    assert ((dw.double() - want).abs() <= U * want.abs()).all()
+    assert dx.isfinite().all()
+
+
 # ------------------------------------------------------------------ linear attention
 
 def inputs(torch, rng, B, T, H, dk, dv, dtype, resets=0.05, state=True, layout="bthd"):
