@@ -24,6 +24,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+
 #include "pxr_internal.h"
 
 namespace pxr {
@@ -745,8 +747,22 @@ void forward_as(const pxr_layer_norm_desc& d, NormForward a, hipStream_t st) {
 #undef PXR_NORM
 }
 
+// Launches of more LDS than the 64 KB that a kernel has by default: asked for by a kernel's first such launch on a device.
+template <auto kKernel>
+hipError_t allow_lds(uint32_t bytes) {
+    static std::atomic<uint64_t> devices{0};
+    int device = 0;
+    if (bytes <= 64u * 1024u) return hipSuccess;
+    if (const hipError_t rc = hipGetDevice(&device); rc != hipSuccess) return rc;
+    const uint64_t bit = device < 64 ? 1ull << device : 0ull;
+    if (devices.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (rc == hipSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
+    return rc;
+}
+
 template <class T, class P>
-void backward_as(const pxr_layer_norm_desc& d, NormBackward a, float* sums, void* dw, void* db, hipStream_t st) {
+hipError_t backward_as(const pxr_layer_norm_desc& d, NormBackward a, float* sums, void* dw, void* db, hipStream_t st) {
     constexpr uint32_t N = Vec<T>::N;
     const Plan p = plan_of(d, kWidestBackward);
     a.lanes = p.lanes;
@@ -760,8 +776,12 @@ void backward_as(const pxr_layer_norm_desc& d, NormBackward a, float* sums, void
         return p.lanes ? sums : turns + (in_lds ? vpl * N * 1024u * 4u : 0u);
     };
     const dim3 parts(p.parts);
-#define PXR_NORM(NT, VPL, U, SUMS, GRID)                                                                                                  \
-    hipLaunchKernelGGL((norm_backward_kernel<T, P, NT, VPL, U, SUMS>), GRID, dim3(kThreadsOf(NT)), lds_of(VPL, U, SUMS && NT == 1024), st, a)
+#define PXR_NORM(NT, VPL, U, SUMS, GRID)                                                                                                      \
+    do {                                                                                                                                      \
+        const uint32_t lds = lds_of(VPL, U, SUMS && NT == 1024);                                                                              \
+        if (const hipError_t rc = allow_lds<&norm_backward_kernel<T, P, NT, VPL, U, SUMS>>(lds); rc != hipSuccess) return rc;                 \
+        hipLaunchKernelGGL((norm_backward_kernel<T, P, NT, VPL, U, SUMS>), GRID, dim3(kThreadsOf(NT)), lds, st, a);                           \
+    } while (0)
     if (p.sums_inside) {
         if (d.n_rows) {
             if (d.width < N)
@@ -803,10 +823,11 @@ void backward_as(const pxr_layer_norm_desc& d, NormBackward a, float* sums, void
         hipLaunchKernelGGL((norm_finish_kernel<P>), dim3(layers > 1u ? kFinishAcross : need, layers), dim3(1024), 0, st, a.sums, p.parts, d.width,
                            static_cast<P*>(dw), static_cast<P*>(db));
     }
+    return hipSuccess;
 }
 
-int launched(std::string& err) {
-    const hipError_t rc = hipGetLastError();
+int launched(std::string& err, hipError_t rc = hipSuccess) {
+    if (rc == hipSuccess) rc = hipGetLastError();
     if (rc == hipSuccess) return PXR_OK;
     err = std::string("kernel launch failed: ") + hipGetErrorString(rc);
     return PXR_ERR_DEVICE;
@@ -838,13 +859,9 @@ int launch_layer_norm_backward(const pxr_layer_norm_desc& d, const void* dy, con
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const NormBackward a{dy, x, mean, rstd, w, dx, nullptr, nullptr, nullptr, d.y_stride, d.x_stride, d.dx_stride, (uint32_t)d.n_rows, d.width, 0u};
     float* sums = static_cast<float*>(ws);
-    if (d.dtype == PXR_F32)
-        backward_as<float, float>(d, a, sums, dw, db, st);
-    else if (d.param_dtype == PXR_F32)
-        backward_as<__bf16, float>(d, a, sums, dw, db, st);
-    else
-        backward_as<__bf16, __bf16>(d, a, sums, dw, db, st);
-    return launched(err);
+    if (d.dtype == PXR_F32) return launched(err, backward_as<float, float>(d, a, sums, dw, db, st));
+    if (d.param_dtype == PXR_F32) return launched(err, backward_as<__bf16, float>(d, a, sums, dw, db, st));
+    return launched(err, backward_as<__bf16, __bf16>(d, a, sums, dw, db, st));
 }
 
 }  // namespace pxr
