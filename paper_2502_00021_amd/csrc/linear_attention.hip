@@ -21,10 +21,11 @@
 // operand of out^T = z^T P^T, and S the left one of S^T x^T, without a move between lanes.  z and y are also wanted with steps along the summed axis: by the
 // transposing LDS read.
 //
-// Roundings.  What is fp32 goes in as a sum of bfloat16 parts.  Of bfloat16 tensors: P and S as two (relative error 2^-17, an output has its own rounding of 2^-9
-// and no other), the weighted z as three (2^-25, the state is an fp32 result).  Of fp32 tensors: everything as three, six products of the nine, the rest is below
-// 2^-25; six instructions of 32 clocks instead of eight of 64 (128 x 256 with 8 heads of 128: 295 us with fp32 operands, 243 so; gradients 760, 593).  The
-// last parts of values under 2^-110 are below the smallest normal number and go: such values keep fewer digits.
+// Roundings.  What is fp32 (P, S, the weighted z, fp32 tensors) goes in as a sum of three bfloat16 parts.  Beside bfloat16 tensors, whose values are one part, the
+// three are 8 bits each, cut off one after the other: their sum is the value, all products are formed, and an output has fp32's rounding of sums and its own of
+// 2^-9 (P and S as two rounded parts, which leave out 2^-17, took 366 us for the gradients of 512 x 256 with 8 heads of 64, 393 so, rollouts 1 to 4 % less).  Of fp32
+// tensors: rounded parts, six products of the nine, the rest is below 2^-25; six instructions of 32 clocks instead of eight of 64 (128 x 256 with 8 heads of 128: 295 us
+// with fp32 operands, 243 so; gradients 760, 593).  The last parts of values under 2^-110 are below the smallest normal number and go: such values keep fewer digits.
 //
 // Bound by memory where heads and environments fill the device: 512 x 256 with 8 heads of 64 in bfloat16 169 us (4.0 TB/s), its gradients 400 (2.9; each step's
 // rows are read by up to three scans, from one die's L2), 4000 single steps of 8 heads 201 (5.3).  Few long rollouts are cut into segments, whose own states are
@@ -99,19 +100,25 @@ struct Parts {
     bf16x8 part[n];
 };
 
-// fp32 values to n parts: their sum, up to the rounding of the last.
-template <int n>
-__device__ __forceinline__ Parts<n> split(f32x8 rest) {
-    Parts<n> f;
+// fp32 values as three parts, for products with values of T: cut off to 8 bits each where those are one part (their sum is the value), rounded to nearest where
+// they are three themselves (the products that are left out are small).
+template <class T>
+__device__ __forceinline__ Parts<3> split(f32x8 rest) {
+    constexpr bool kCut = sizeof(T) == 2;
+    Parts<3> f;
 #pragma unroll
-    for (int k = 0; k < n; ++k) {
+    for (int k = 0; k < 3; ++k) {
         u32x4 w;  // (two values an instruction: conversions of eight at once come out one by one)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{rest[2 * i], rest[2 * i + 1]}, bf16x2));  // round to nearest even
-            if (k + 1 < n) {
-                rest[2 * i] -= __uint_as_float(w[i] << 16);
-                rest[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+            const float lo = rest[2 * i], hi = rest[2 * i + 1];
+            if (kCut)
+                w[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);  // the upper halves of both
+            else
+                w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));  // round to nearest even
+            if (k < 2) {
+                rest[2 * i] = lo - __uint_as_float(kCut ? __float_as_uint(lo) & 0xFFFF0000u : w[i] << 16);
+                rest[2 * i + 1] = hi - __uint_as_float(kCut ? __float_as_uint(hi) & 0xFFFF0000u : w[i] & 0xFFFF0000u);
             }
         }
         f.part[k] = __builtin_bit_cast(bf16x8, w);
@@ -119,7 +126,7 @@ __device__ __forceinline__ Parts<n> split(f32x8 rest) {
     return f;
 }
 
-// Products of parts whose share of the result is above the last part's rounding, the smallest first.
+// Products of parts whose share of the result is above a third part's rounding, the smallest first (all of them where one operand is one part).
 template <int n, int m>
 __device__ __forceinline__ f32x16 mma(const Parts<n>& a, const Parts<m>& b, f32x16 c) {
 #pragma unroll
@@ -183,7 +190,7 @@ __device__ __forceinline__ f32x8 values(const bf16x8& f) {
 }
 __device__ __forceinline__ f32x8 values(const f32x8& f) { return f; }
 __device__ __forceinline__ Parts<1> parts_of(const bf16x8& f) { return {{f}}; }
-__device__ __forceinline__ Parts<3> parts_of(const f32x8& f) { return split<3>(f); }
+__device__ __forceinline__ Parts<3> parts_of(const f32x8& f) { return split<float>(f); }
 // Half of a product's result in a lane, which is a run of 16 of its rows.
 __device__ __forceinline__ f32x8 half(const f32x16& c, int k) {
     return k ? __builtin_shufflevector(c, c, 8, 9, 10, 11, 12, 13, 14, 15) : __builtin_shufflevector(c, c, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -197,11 +204,9 @@ __device__ __forceinline__ f32x8 eight(const float* lo, const float* hi) {
 
 template <class T>
 constexpr uint32_t kPad = 16 / sizeof(T);
-// Parts of a value of x or y in LDS, and of the fp32 values that are multiplied again.
+// Parts of a value of x or y in LDS.
 template <class T>
 constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
-template <class T>
-constexpr int kAgain = sizeof(T) == 2 ? 2 : 3;
 
 // The largest bit patterns of the values, without their signs.
 template <class T>
@@ -493,7 +498,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
             for (int k = 0; k < A / 16; ++k) {
                 if (A > 64 && k == A / 16 - 2 && !last) break;
                 const Parts<kParts<T>> x = along<kParts<T>>(xs + col32 * kStrideA + k * 16, kPlane, h32);
-                acc = mma(split<kAgain<T>>(half(state[k / 2], k % 2)), x, acc);
+                acc = mma(split<T>(half(state[k / 2], k % 2)), x, acc);
                 p = mma(along<kParts<T>>(ys + col32 * kStrideA + k * 16, kPlane, h32), x, p);
             }
             acc *= s.out_scale * pw[reverse ? (col32 < n ? n - 1u - col32 : 0u) : col32 + 1u];
@@ -512,8 +517,8 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
 #pragma unroll
             for (int r = 0; r < 16; ++r) p[r] = lowest + ((r & 3) + 8 * (r >> 2)) < past - first ? p[r] * (kFactors ? factors[kFactors ? r : 0] : factor[f + ((r & 3) + 8 * (r >> 2))]) : 0.0f;
             // out^T += z^T P^T
-            acc = mma(parts_of(z0), split<kAgain<T>>(half(p, 0)), acc);
-            acc = mma(parts_of(z1), split<kAgain<T>>(half(p, 1)), acc);
+            acc = mma(parts_of(z0), split<T>(half(p, 0)), acc);
+            acc = mma(parts_of(z1), split<T>(half(p, 1)), acc);
             // The outputs take the place of the wavefront's own columns of z in LDS, so that they leave as 16 bytes a lane, rows of 64 or 128
             // bytes, past the caches: they are not read again (512 x 256 bfloat16 186 -> 171 us; parts of rows past the caches 345).
             T* own = zs + wave * 32u;
@@ -578,7 +583,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(wav
         if (!(reverse && (m & 1u))) {
 #pragma unroll
             for (int k = 0; k < C / 16; ++k) {
-                const Parts<3> zp = split<3>(values(k ? z1 : z0) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
+                const Parts<3> zp = split<T>(values(k ? z1 : z0) * eight(weight + k * 16 + 4 * h32, weight + k * 16 + 8 + 4 * h32));
 #pragma unroll
                 for (int db = 0; db < A / 32; ++db) {
                     if (A > 64 && db == A / 32 - 1 && !last) break;

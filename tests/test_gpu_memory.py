@@ -529,6 +529,55 @@ def test_attention_what_is_not_finite_in_a_step_that_begins_an_episode_stays_in_
     layer.close()
 
 
+@pytest.mark.parametrize("B,T,H,dk,dv", [(3, 90, 2, 32, 32), (1, 640, 1, 64, 64), (2, 33, 2, 24, 100), (2, 70, 1, 128, 96), (1, 40, 1, 100, 40)])
+@pytest.mark.parametrize("large", ["probabilities", "states"])
+def test_attention_of_whole_numbers_is_exact_up_to_the_outputs_rounding(torch, pxr, large, B, T, H, dk, dv):
+    """bfloat16 inputs that are whole numbers, no decay: every sum stays below 2^24, so that fp32 holds it, and an output is the
+    definition's, rounded once.  Probabilities and states of 17 bits and more nearly cancel in it, so that less than all of their
+    bits would not do: keys and queries of 8 bits come in pairs that differ by one, with values and gradients of opposite sign; or the
+    states are one large odd number and a few more or less, and what they are multiplied with adds up to nothing."""
+    rng = np.random.default_rng(dk + T)
+
+    def whole(*shape, most):
+        return rng.integers(-most, most + 1, shape).astype(np.float64)
+    r = np.zeros((B, T), bool)
+    r[:, 2 * rng.integers(1, T // 2, B)] = True
+    if large == "probabilities":
+        q, k, v, dout = (np.zeros((B, T, H, d)) for d in (dk, dk, dv, dv))
+        at = rng.choice(dk, 4, replace=False)
+        for x, y in ((k, v), (q, dout)):
+            x[:, ::2, :, at] = 255 - rng.integers(0, 9, x[:, ::2, :, at].shape)
+            y[:, ::2] = whole(*y[:, ::2].shape, most=1) * (rng.random(y[:, ::2].shape) < 8 / T)
+            pairs = T // 2
+            x[:, 1:2 * pairs:2], y[:, 1:2 * pairs:2] = x[:, :2 * pairs:2], -y[:, :2 * pairs:2]
+            x[:, 1:2 * pairs:2, :, at[0]] -= 1
+        s, ds = whole(B, H, dk, dv, most=3), whole(B, H, dk, dv, most=3)
+    else:
+        def paired(d):
+            x, at = np.zeros((B, T, H, d)), 2 * rng.choice(d // 2, 4, replace=False)
+            x[..., at] = whole(B, T, H, 4, most=1)
+            x[..., at + 1] = -x[..., at]
+            return x
+        q, k, v, dout = paired(dk), paired(dk), paired(dv), paired(dv)
+        big = 2 ** 20 - 2 ** 13 + 2411
+        s, ds = big + whole(B, H, dk, dv, most=9), big + whole(B, H, dk, dv, most=9)
+    ld = np.zeros(H, np.float32)
+    ref = (*om.linear_attention(q, k, v, ld, 1.0, r, s), *om.linear_attention_backward(dout, q, k, v, ld, 1.0, r, s, ds))
+    mags = [abs(x) for x in (q, k, v)]
+    most = (*om.linear_attention(*mags, ld, 1.0, r, abs(s)), *om.linear_attention_backward(abs(dout), *mags, ld, 1.0, r, abs(s), abs(ds)))
+    assert max(m.max() for m in most) < 2 ** 24
+    if large == "probabilities":
+        assert np.einsum("bihd,bjhd->bhij", q[:, :9], k[:, :9]).max() > 2 ** 17
+    else:
+        assert np.abs(s).min() > 2 ** 19
+    Q, K, V, DO = (gpu(torch, x, "bf16") for x in (q, k, v, dout))
+    layer, R = pxr.LinearAttention(H, dk, dv, ld, scale=1.0), torch.from_numpy(r).cuda()
+    got = (*layer.forward(Q, K, V, resets=R, state=gpu(torch, s)), *layer.backward(DO, Q, K, V, resets=R, state=gpu(torch, s), dstate=gpu(torch, ds)))
+    for name, g, rf in zip(("out", "state", "dq", "dk", "dv", "dstate"), got, ref):
+        assert torch.equal(g, torch.from_numpy(rf).cuda().float().to(g.dtype)), name
+    layer.close()
+
+
 def test_attention_gradients_by_differences(torch, pxr):
     """The kernels' own forward pass, moved along a direction.  It is linear in each input alone, so the difference over any
     distance is the derivative; the directions are small, so that roundings are those of the results themselves."""
