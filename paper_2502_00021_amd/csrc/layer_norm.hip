@@ -3,18 +3,21 @@
 //   mean = sum x / D,  rstd = 1 / sqrt(sum (x - mean)^2 / D + eps),  y = (x - mean) rstd w + b
 //   dx = rstd (g - sum g / D - xh sum(g xh) / D),  g = w dy,  xh = (x - mean) rstd;  dw = sum_rows dy xh,  db = sum_rows dy
 //
-// Both directions are bound by HBM: a few operations for every byte.  So a row is read once and stays in registers, as it came,
+// Both directions are bound by HBM: a few operations for every byte.  So a row of ordinary width is read once and stays in registers, as it came,
 // until it leaves: the deviations are squared after the mean is taken off (a row far from zero keeps its variance), from the
 // registers.  All sums are fp32.
 //
 // A lane holds VPL vectors of 16 bytes of a row, lanes of a row next to each other.  Who takes a row goes by the number of its
 // vectors:
 //   up to 64      a part of a wavefront, 1 to 64 lanes: eight rows of 64 bfloat16 values in a wavefront
-//   up to 256     a wavefront, two or four vectors a lane (backward: 128)
+//   up to 256     a wavefront, two or four vectors a lane (backward: up to 128, two)
 //   up to 16384   a workgroup of 256 to 1024 threads, two to sixteen vectors a lane: what a lane has in flight counts for more than lanes do
+//                 (backward: up to 32768 values, one to eight vectors)
 //                 (forward, 30000 x 7000 bfloat16: 256 threads 175 us, 512 of them 188; 9000 x 5000 fp32: 512 threads 59, 1024 of them 80; 4096 x 30752 bfloat16:
 //                 two rows at a time 85, four 98)
 //   more          a workgroup that reads the row again for each sum (from the caches, mostly): 800 x 50000 fp32 124 us, 70 from registers
+// The backward pass of rows of more than 32768 values forms the sums over rows in a kernel of its own, which reads dy and x once; the one that forms dx reads them
+// once more (bfloat16, up to 65536 values) or twice (800 x 50000 fp32 186 us, 94 at the rate of a copy).
 // What leaves is not read again by the kernel and goes past the caches that it would push x out of (524288 x 64 bfloat16 31 -> 25 us, 4096 x 30752 146 -> 110;
 // requests that go past them as well are slower where x lies in them).
 //

@@ -27,9 +27,12 @@
 // tensors: rounded parts, six products of the nine, the rest is below 2^-25; six instructions of 32 clocks instead of eight of 64 (128 x 256 with 8 heads of 128: 295 us
 // with fp32 operands, 243 so; gradients 760, 593).  The last parts of values under 2^-110 are below the smallest normal number and go: such values keep fewer digits.
 //
-// Bound by memory where heads and environments fill the device: 512 x 256 with 8 heads of 64 in bfloat16 169 us (4.0 TB/s), its gradients 400 (2.9; each step's
-// rows are read by up to three scans, from one die's L2), 4000 single steps of 8 heads 201 (5.3).  Few long rollouts are cut into segments, whose own states are
-// found first and joined: 20000 steps of 8 heads of 64 x 128 81 us, twice the reading.  A chunk alone on a compute unit takes 3 us, 5 in fp32: instructions, one after the other.
+// Bound by memory where heads and environments fill the device: 512 x 256 with 8 heads of 64 in bfloat16 179 us (3.7 TB/s), its gradients 399 (2.9; each step's
+// rows are read by up to three scans, from one die's L2, and the vector units are 78 % busy), 4000 single steps of 8 heads 199 (5.3).  Few long rollouts are cut into
+// segments, whose own states are found first and joined: 20000 steps of 8 heads of 64 x 128 75 us, twice the reading.  A chunk alone on a compute unit takes 3 us, 5 in
+// fp32: instructions, one after the other.  Heads of more than 128 do not fit the registers, and the loop over chunks keeps about 100 of a lane's values in
+// scratch: 128 x 256 with 4 heads of 256 1.01 ms in bfloat16, its gradients 2.9 (floors 0.11 and 0.17).
+// (Two figures side by side, here and below, were taken together when that choice was made; what was changed since has moved both.)
 //
 // Steps that hold an infinity or NaN (or what rounds to an infinity of bfloat16) in y or z are taken one by one: 0 times such a value would reach steps that it
 // must not.  Where it does reach, parts of an infinity are no numbers, so that a NaN may come out in its place.

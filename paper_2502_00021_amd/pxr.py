@@ -781,7 +781,7 @@ class LinearAttention:
 
     def step(self, q, k, v, state, resets=None, out=None, stream=None):
         """One step of every environment: q, k [B,H,d_key], v [B,H,d_value], resets [B] or None; state float32
-        [B,H,d_key,d_value] is updated in place.  Returns out [B,H,d_value]; enqueue only."""
+        [B,H,d_key,d_value] is updated in place (autograd is told).  Returns out [B,H,d_value]; enqueue only."""
         torch = _torch or _torch_module()
         assert q.dim() == 3
         r, _, values, B, _ = self._rollout(torch, q, k, v, resets, None)
