@@ -1,0 +1,404 @@
+"""More operators of a policy with memory and of its learner, as cases that can be timed and compared.
+
+  recurrence       pxr.gated_recurrence: a rollout at once (learning, or filling the memory from a recording)
+  recurrence_grad  pxr.gated_recurrence_backward: the gradients of inputs, gates and of the state before the rollout
+  recurrence_step  pxr.gated_recurrence_step: one time step of every environment, the state updated in place (acting)
+  heads            HeadNorm.forward: queries and keys, each head normalised and turned by its step's position
+  heads_grad       HeadNorm.backward: the gradients of queries, keys and of the two weights
+  orthogonalise    pxr.orthogonalise: a learner's update with its singular values pushed towards one
+
+The gated recurrence keeps a value per environment and channel, cut where an episode begins:
+
+  h_t = (t begins an episode ? 0 : a_t h_{t-1}) + (coupled ? 1 - a_t : 1) x_t        a_t = 1 / (1 + exp(-gate_t))
+
+A head's values x become y = x / sqrt(mean x^2 + eps) * weight, and of the first r of them the pairs (y_i, y_{i + r/2}) are turned
+by the angle position * frequency_i.  An update X [m,n], m <= n (otherwise its transpose), is divided by its Frobenius norm and
+goes through X <- a X + (b A + c A^2) X with A = X X^T.
+
+`own` picks who computes: False = the plain form below, True = the framework's kernels.
+"""
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-6
+EPS_UPDATE = 1e-7
+BASE = 10000.0
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+STEPS = 5
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+# ------------------------------------------------------------------ the cases
+
+def _recurrence(kind, envs, steps, width, dtype, resets=True, fused=True, state=True, coupled=True):
+    return dict(kind=kind, envs=envs, steps=steps, width=width, dtype=dtype, resets=resets, fused=fused, state=state, coupled=coupled)
+
+
+def _heads(kind, envs, steps, heads, key_heads, d, rotary, dtype, fused=True):
+    return dict(kind=kind, envs=envs, steps=steps, heads=heads, key_heads=key_heads, d=d, rotary=rotary, dtype=dtype, fused=fused)
+
+
+def _update(batch, rows, cols, dtype):
+    return dict(kind="orthogonalise", batch=batch, rows=rows, cols=cols, dtype=dtype)
+
+
+def listed():
+    return [
+        # The shortest rollout of a few environments while a task is being debugged: launch and latency only.
+        dict(_recurrence("recurrence", 16, 8, 64, "f32"), name="recurrence_16x8x64_f32"),
+        # A learner's ordinary rollout: 256 environments, 128 steps, 1024 channels, inputs and gates from one projection.
+        dict(_recurrence("recurrence", 256, 128, 1024, "bf16"), name="recurrence_256x128x1024_bf16"),
+        # A long recording of one environment: few rows, one long axis.
+        dict(_recurrence("recurrence", 1, 50000, 512, "bf16", resets=False, coupled=False), name="recurrence_1x50000x512_bf16"),
+        # Gradients at odd sizes, in 32 bits, inputs that are not gated.
+        dict(_recurrence("recurrence_grad", 33, 77, 201, "f32", coupled=False), name="recurrence_grad_33x77x201_f32"),
+        # The largest learning step: 512 environments, 256 steps, 1024 channels.
+        dict(_recurrence("recurrence_grad", 512, 256, 1024, "bf16"), name="recurrence_grad_512x256x1024_bf16"),
+        # 16 384 environments take one step.
+        dict(_recurrence("recurrence_step", 16384, 1, 1024, "bf16"), name="recurrence_step_16384x1024_bf16"),
+        # Sixteen environments take one step: queries and keys of 4 heads of 32.  Latency.
+        dict(_heads("heads", 16, 1, 4, 4, 32, 32, "f32"), name="heads_16_f32"),
+        # A learner's ordinary rollout: 256 environments, 128 steps, 8 heads of 64, parts of one projection's output.
+        dict(_heads("heads", 256, 128, 8, 8, 64, 64, "bf16"), name="heads_256x128_bf16"),
+        # Gradients of the largest learning step: 512 environments, 256 steps, 16 heads of 64 that share 4 heads of keys.
+        dict(_heads("heads_grad", 512, 256, 16, 4, 64, 64, "bf16"), name="heads_grad_512x256_bf16"),
+        # The three projections of a small policy's memory, side by side: 64 wide into 3 heads of 32.
+        dict(_update(3, 64, 96, "f32"), name="orthogonalise_3x64x96_f32"),
+        # The projection behind the first layer: the features of a 31 x 31 x 32 map into 256 values.
+        dict(_update(1, 30752, 256, "f32"), name="orthogonalise_30752x256_f32"),
+        # The largest update: a square matrix of a wide policy, where the products count.
+        dict(_update(1, 4096, 4096, "bf16"), name="orthogonalise_4096x4096_bf16"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+
+def draw(rng):
+    """Sizes spread over their logarithm: 1 to 16 000 environments, 1 to 50 000 steps, 1 to 4096 channels; 1 to 16 heads of 8 to
+    256 values; 1 to 8 updates of 4 to 4096 by 4 to 30 000 values."""
+    kind = rng.choice(["recurrence", "recurrence", "recurrence_grad", "recurrence_grad", "recurrence_step", "heads", "heads_grad",
+                       "orthogonalise", "orthogonalise"])
+    dtype = rng.choice(["f32", "bf16", "bf16"])
+    if kind.startswith("recurrence"):
+        width = rng.choice([64, 256, 512, 1024, _log_int(rng, 1, 4096), _log_int(rng, 1, 4096)])
+        if kind == "recurrence_step":
+            envs, steps = _log_int(rng, 1, 16000), 1
+        else:
+            steps = _log_int(rng, 1, min(50000, 60_000_000 // width))
+            envs = _log_int(rng, 1, min(16000, 60_000_000 // (width * steps)))
+        return _recurrence(kind, envs, steps, width, dtype, resets=rng.random() < 0.7, fused=rng.random() < 0.6,
+                           state=kind == "recurrence_step" or rng.random() < 0.7, coupled=rng.random() < 0.6)
+    if kind.startswith("heads"):
+        heads = rng.choice([1, 2, 3, 4, 6, 8, 12, 16])
+        key_heads = rng.choice([h for h in (1, 2, 4, heads) if heads % h == 0])
+        d = rng.choice([16, 32, 48, 64, 64, 96, 128, 256, rng.randint(8, 256)])
+        rotary = rng.choice([d // 2 * 2, d // 2 * 2, max(2, d // 4 * 2), 2 * rng.randint(1, d // 2)])
+        tokens = 100_000_000 // ((heads + key_heads) * d)
+        steps = 1 if rng.random() < 0.3 else _log_int(rng, 1, min(16000, tokens))
+        return _heads(kind, _log_int(rng, 1, min(16000, tokens // steps)), steps, heads, key_heads, d, rotary, dtype, fused=rng.random() < 0.6)
+    short = _log_int(rng, 4, 4096)
+    long = _log_int(rng, short, max(short, min(30000, 4096 ** 3 // short ** 2)))
+    batch = _log_int(rng, 1, max(1, min(8, 4096 ** 3 // (short ** 2 * long), 40_000_000 // (short * long))))
+    rows, cols = (short, long) if rng.random() < 0.5 else (long, short)
+    return _update(batch, rows, cols, dtype)
+
+
+# ------------------------------------------------------------------ inputs
+
+def _frequencies(rotary):
+    return [BASE ** (-2 * i / rotary) for i in range(rotary // 2)]
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    dtype = DTYPES[case["dtype"]]
+
+    def normal(*shape, to=dtype):
+        return torch.randn(shape, generator=g, device="cuda", dtype=torch.float32).to(to)
+
+    s = dict(case=case)
+    kind = case["kind"]
+    if kind == "orthogonalise":
+        # momentum of gradients: some directions that stand out, less and less, in noise
+        b, m, n = case["batch"], case["rows"], case["cols"]
+        r = max(1, min(m, n) // 8)
+        stand = torch.arange(1, r + 1, device="cuda", dtype=torch.float32) ** -0.5
+        x = (normal(b, m, r, to=torch.float32) * stand) @ normal(b, r, n, to=torch.float32) + 0.5 * normal(b, m, n, to=torch.float32)
+        s["x"] = (1e-3 * x).to(dtype)
+        return s
+    b, t = case["envs"], case["steps"]
+    if kind.startswith("recurrence"):
+        d = case["width"]
+        step = kind == "recurrence_step"
+        lead = (b,) if step else (b, t)
+        # channels that look back over a few steps up to some hundred
+        shift = torch.linspace(0.0, 5.0, d, device="cuda").to(dtype)
+        if case["fused"]:  # both are parts of one projection's output
+            s["x"], s["gate"] = normal(*lead, 2 * d).split([d, d], dim=-1)
+            s["gate"].add_(shift)
+        else:
+            s["x"], s["gate"] = normal(*lead, d), normal(*lead, d).add_(shift)
+        s["resets"] = torch.rand(lead, generator=g, device="cuda") < 1 / 150 if case["resets"] else None
+        s["state"] = normal(b, d, to=torch.float32) if case["state"] else None
+        if kind == "recurrence_grad":
+            s["dout"] = normal(*lead, d)
+            s["dstate"] = normal(b, d, to=torch.float32) if case["state"] else None
+        return s
+    h, hk, d = case["heads"], case["key_heads"], case["d"]
+    if case["fused"]:  # parts of one projection's output, the values behind them
+        qkv = normal(b, t, (h + 2 * hk) * d)
+        q, k, _ = qkv.split([h * d, hk * d, hk * d], dim=-1)
+        s["q"], s["k"] = q.unflatten(-1, (h, d)), k.unflatten(-1, (hk, d))
+    else:
+        s["q"], s["k"] = normal(b, t, h, d), normal(b, t, hk, d)
+    s["q_weight"], s["k_weight"] = (1 + 0.1 * normal(d, to=torch.float32) for _ in range(2))
+    # steps since the episode began; the first episode goes on, for some environments from far back
+    began = torch.where(torch.rand((b, t), generator=g, device="cuda") < 1 / 150, torch.arange(t, device="cuda"), -1)
+    far = (torch.rand((b, 1), generator=g, device="cuda") ** 8 * 1e6).long()
+    last = began.cummax(1).values
+    s["positions"] = torch.where(last >= 0, torch.arange(t, device="cuda") - last, torch.arange(t, device="cuda") + far).int()
+    if kind == "heads_grad":
+        s["dq"], s["dk"] = normal(b, t, h, d), normal(b, t, hk, d)
+    if own:
+        from paper_2502_00021_amd import pxr
+        s["layer"] = pxr.HeadNorm(d, case["rotary"], base=BASE, eps=EPS)
+    else:
+        s["frequencies"] = torch.tensor(_frequencies(case["rotary"]), dtype=torch.float64, device="cuda")
+    return s
+
+
+# ------------------------------------------------------------------ one pass
+
+def run(state):
+    kind = state["case"]["kind"]
+    if own:
+        return _run_own(kind, state)
+    return {"recurrence": _plain_recurrence, "recurrence_grad": _plain_recurrence_grad, "recurrence_step": _plain_step,
+            "heads": _plain_heads, "heads_grad": _plain_heads_grad, "orthogonalise": _plain_orthogonalise}[kind](state)
+
+
+def _run_own(kind, s):
+    from paper_2502_00021_amd import pxr
+    if kind == "orthogonalise":
+        return pxr.orthogonalise(s["x"], steps=STEPS, coefficients=COEFFICIENTS, eps=EPS_UPDATE)
+    if kind == "heads":
+        return dict(zip(("q", "k"), s["layer"].forward(s["q"], s["k"], s["q_weight"], s["k_weight"], positions=s["positions"])))
+    if kind == "heads_grad":
+        got = s["layer"].backward(s["dq"], s["dk"], s["q"], s["k"], s["q_weight"], s["k_weight"], positions=s["positions"])
+        return dict(zip(("dq", "dk", "dq_weight", "dk_weight"), got))
+    coupled = s["case"]["coupled"]
+    if kind == "recurrence":
+        return dict(zip(("out", "state"), pxr.gated_recurrence(s["x"], s["gate"], resets=s["resets"], state=s["state"], coupled=coupled)))
+    if kind == "recurrence_grad":
+        got = pxr.gated_recurrence_backward(s["dout"], s["x"], s["gate"], resets=s["resets"], state=s["state"], dstate=s["dstate"], coupled=coupled)
+        return dict(zip(("dx", "dgate", "dstate"), got))
+    return dict(out=pxr.gated_recurrence_step(s["x"], s["gate"], s["state"], resets=s["resets"], coupled=coupled), state=s["state"])
+
+
+# ------------------------------------------------------------------ plain forms, in 32 bits
+
+def _scan(a, b):
+    """h_t = a_t h_{t-1} + b_t along the steps [B,T,D], from zero: twice as many steps joined each time."""
+    reach, T = 1, a.shape[1]
+    while reach < T:
+        b = torch.cat([b[:, :reach], torch.addcmul(b[:, reach:], a[:, reach:], b[:, :-reach])], 1)
+        a = torch.cat([a[:, :reach], a[:, reach:] * a[:, :-reach]], 1)
+        reach *= 2
+    return b
+
+
+def _gates(s):
+    """What a step keeps of the state, and a and 1 - a."""
+    gate = s["gate"].float()
+    a, rest = 1 / (1 + torch.exp(-gate)), 1 / (1 + torch.exp(gate))
+    keep = a if s["resets"] is None else torch.where(s["resets"][..., None], 0.0, a)
+    return keep, a, rest
+
+
+def _hidden(s, keep, rest):
+    b = s["x"].float()
+    b = b * rest if s["case"]["coupled"] else b.clone()
+    if s["state"] is not None:
+        b[:, 0] += keep[:, 0] * s["state"]
+    return _scan(keep, b)
+
+
+def _plain_recurrence(s):
+    keep, _, rest = _gates(s)
+    h = _hidden(s, keep, rest)
+    return dict(out=h.to(s["x"].dtype), state=h[:, -1].clone())
+
+
+def _plain_recurrence_grad(s):
+    dtype, coupled, x = s["x"].dtype, s["case"]["coupled"], s["x"].float()
+    keep, a, rest = _gates(s)
+    h = _hidden(s, keep, rest)
+    first = torch.zeros_like(h[:, :1]) if s["state"] is None else s["state"][:, None]
+    before = torch.cat([first, h[:, :-1]], 1)
+    if s["resets"] is not None:
+        before = torch.where(s["resets"][..., None], 0.0, before)
+    # the gradient of h_t from all later steps: the same scan from the end
+    given = s["dout"].float()
+    if s["dstate"] is not None:
+        given[:, -1:] += s["dstate"][:, None]
+    later = torch.cat([keep[:, 1:], torch.zeros_like(keep[:, :1])], 1)
+    dh = _scan(later.flip(1), given.flip(1)).flip(1)
+    da = dh * (before - x if coupled else before)
+    return dict(dx=(dh * rest if coupled else dh).to(dtype), dgate=(da * a * rest).to(dtype),
+                dstate=None if s["state"] is None else keep[:, 0] * dh[:, 0])
+
+
+def _plain_step(s):
+    keep, _, rest = _gates(s)
+    x = s["x"].float()
+    s["state"].mul_(keep).add_(x * rest if s["case"]["coupled"] else x)
+    return dict(out=s["state"].to(s["x"].dtype), state=s["state"])
+
+
+def _turns(s):
+    """cos and sin [B,T,1,r/2] of the steps' angles, which are formed in 64 bits."""
+    angle = s["positions"].double()[:, :, None, None] * s["frequencies"]
+    return torch.cos(angle).float(), torch.sin(angle).float()
+
+
+def _turned(y, cos, sin, rotary):
+    lo, hi, rest = y.split([rotary // 2, rotary // 2, y.shape[-1] - rotary], dim=-1)
+    return torch.cat([lo * cos - hi * sin, hi * cos + lo * sin, rest], -1)
+
+
+def _plain_heads(s):
+    cos, sin = _turns(s)
+
+    def normed(x, weight):
+        f = x.float()
+        y = f * torch.rsqrt(f.square().mean(-1, keepdim=True) + EPS) * weight
+        return _turned(y, cos, sin, s["case"]["rotary"]).to(x.dtype)
+    return dict(q=normed(s["q"], s["q_weight"]), k=normed(s["k"], s["k_weight"]))
+
+
+def _plain_heads_grad(s):
+    cos, sin = _turns(s)
+
+    def grads(dy, x, weight):
+        f = x.float()
+        rstd = torch.rsqrt(f.square().mean(-1, keepdim=True) + EPS)
+        xhat = f * rstd
+        g = _turned(dy.float(), cos, -sin, s["case"]["rotary"])  # turned back
+        gw = g * weight
+        dx = rstd * (gw - xhat * (gw * xhat).mean(-1, keepdim=True))
+        return dx.to(x.dtype), (g * xhat).flatten(0, 2).sum(0)
+    dq, dq_weight = grads(s["dq"], s["q"], s["q_weight"])
+    dk, dk_weight = grads(s["dk"], s["k"], s["k_weight"])
+    return dict(dq=dq, dk=dk, dq_weight=dq_weight, dk_weight=dk_weight)
+
+
+def _plain_orthogonalise(s):
+    a, b, c = COEFFICIENTS
+    x = s["x"].float()
+    tall = x.shape[1] > x.shape[2]
+    x = x.transpose(1, 2).contiguous() if tall else x
+    x = x / (x.square().sum((1, 2), keepdim=True).sqrt() + EPS_UPDATE)
+    for _ in range(STEPS):
+        gram = x @ x.transpose(1, 2).contiguous()
+        x = a * x + (b * gram + c * (gram @ gram)) @ x
+    x = x.transpose(1, 2).contiguous() if tall else x
+    return x.to(s["x"].dtype)
+
+
+# ------------------------------------------------------------------ from the definition, in 64 bits
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "orthogonalise":
+        a, b, c = COEFFICIENTS
+        outs = []
+        for x in s["x"].double():
+            x = x / (torch.linalg.vector_norm(x) + EPS_UPDATE)
+            wide = x.shape[0] <= x.shape[1]
+            for _ in range(STEPS):  # a polynomial of the Gram matrix of the shorter side, from that side
+                xt = x.t().contiguous()
+                gram = x @ xt if wide else xt @ x
+                poly = c * gram @ gram + b * gram
+                poly.diagonal().add_(a)
+                x = poly @ x if wide else x @ poly
+            outs.append(x)
+        return torch.stack(outs)
+    if kind.startswith("heads"):
+        r, d = case["rotary"], case["d"]
+        angle = s["positions"].double()[..., None] * torch.tensor(_frequencies(r), dtype=torch.float64, device="cuda")
+        turn = torch.polar(torch.ones_like(angle), angle)[:, :, None]  # [B,T,1,r/2]
+
+        def turned(y, turn):
+            z = torch.complex(y[..., :r // 2].contiguous(), y[..., r // 2:r].contiguous()) * turn
+            return torch.cat([z.real, z.imag, y[..., r:]], -1)
+        got = {}
+        for name in "qk":
+            x, w = s[name].double(), s[name + "_weight"].double()
+            norm = (x.pow(2).sum(-1, keepdim=True) / d + EPS).sqrt()
+            if kind == "heads":
+                got[name] = turned(w * x / norm, turn)
+                continue
+            # y_i = w_i x_i / n(x), n^2 = <x, x> / d + eps: dx_i = (w g)_i / n - x_i <w g, x> / (d n^3)
+            g = turned(s["d" + name].double(), turn.conj())
+            along = (w * g * x).sum(-1, keepdim=True)
+            got["d" + name] = w * g / norm - x * along / (d * norm ** 3)
+            got["d" + name + "_weight"] = (g * x / norm).sum((0, 1, 2))
+        return got
+    x, gate = s["x"].double(), s["gate"].double()
+    if kind == "recurrence_step":
+        x, gate = x[:, None], gate[:, None]
+    coupled = case["coupled"]
+    a = torch.sigmoid(gate)
+    cut = None if s["resets"] is None else s["resets"].reshape(x.shape[0], x.shape[1], 1)
+    keep = a if cut is None else a * ~cut
+    taken = 1 - a if coupled else torch.ones_like(a)
+    h = torch.zeros_like(x[:, 0]) if s["state"] is None else s["state"].double()
+    hs = []
+    for t in range(x.shape[1]):
+        hs.append(h)
+        h = keep[:, t] * h + taken[:, t] * x[:, t]
+    if kind == "recurrence_step":
+        return dict(out=h, state=h)
+    if kind == "recurrence":
+        return dict(out=torch.stack([*hs[1:], h], 1), state=h)
+    dh = torch.zeros_like(h) if s["dstate"] is None else s["dstate"].double()
+    dx, dgate = torch.empty_like(x), torch.empty_like(x)
+    slope = a * (1 - a)
+    for t in range(x.shape[1] - 1, -1, -1):
+        dh = dh + s["dout"][:, t]
+        dx[:, t] = dh * taken[:, t]
+        seen = hs[t] if cut is None else hs[t] * ~cut[:, t]
+        dgate[:, t] = dh * slope[:, t] * (seen - x[:, t] if coupled else seen)
+        dh = dh * keep[:, t]
+    return dict(dx=dx, dgate=dgate, dstate=None if s["state"] is None else dh)
+
+
+# ------------------------------------------------------------------ what a pass cannot do without
+
+def work(case):
+    """Every input read once and every output written once; operations of the definition (a product and a sum are two; of a
+    symmetric product half)."""
+    size = 4 if case["dtype"] == "f32" else 2
+    kind = case["kind"]
+    if kind == "orthogonalise":
+        m, n = sorted((case["rows"], case["cols"]))
+        return dict(bytes=case["batch"] * 2 * m * n * size, flops=case["batch"] * (3 * m * n + STEPS * (3 * m * m * n + m * m * m)))
+    b, t = case["envs"], case["steps"]
+    if kind.startswith("heads"):
+        values, weights = b * t * (case["heads"] + case["key_heads"]) * case["d"], 2 * case["d"] * 4
+        if kind == "heads":
+            return dict(bytes=2 * values * size + weights + 4 * b * t, flops=7 * values)
+        return dict(bytes=3 * values * size + 2 * weights + 4 * b * t, flops=13 * values)
+    values, states, marks = b * t * case["width"], 4 * b * case["width"], b * t if case["resets"] else 0
+    if kind == "recurrence_step":
+        return dict(bytes=3 * values * size + 2 * states + marks, flops=7 * values)
+    if kind == "recurrence":
+        return dict(bytes=3 * values * size + (2 if case["state"] else 1) * states + marks, flops=7 * values)
+    return dict(bytes=5 * values * size + (3 if case["state"] else 0) * states + marks, flops=17 * values)
