@@ -279,7 +279,7 @@ int pxr_pipeline_set_overlap_from(pxr_pipeline* p, uint64_t bytes);
 /* Into how many chunks a step of B environments is cut (host only; no passage of the paper).  Errors: INVALID_ARG. */
 int pxr_pipeline_info(const pxr_pipeline* p, uint32_t B, uint32_t* chunks);
 
-/* ---- a policy's memory: layer norm and linear attention ----
+/* ---- a policy's memory: layer norm, linear attention, a gated recurrence ----
  * The paper's loop (section 2) ends with the first layer of a policy.  What stands behind that layer in a policy that
  * remembers: a normalisation, and a state per environment that each step reads and adds to.  Element types are fp32 and
  * bfloat16; statistics, sums and states are fp32.  All calls only enqueue: no allocation, no synchronisation. */
@@ -382,6 +382,53 @@ int pxr_linear_attention_backward(pxr_linear_attention* a, const pxr_rollout* r,
  * is updated in place (r->d_state is not read; 4-byte aligned); out must not overlap what is read.  One kernel.
  * Errors: as for the forward pass. */
 int pxr_linear_attention_step(pxr_linear_attention* a, const pxr_rollout* r, float* d_state, const pxr_tokens* out, void* hip_stream);
+
+/* A gated linear recurrence.  Every environment e and channel c has a state h:
+ *   a_t = 1 / (1 + exp(-gate_t)),   h_t = (resets[e,t] ? 0 : a_t * h_{t-1}) + (coupled ? 1 - a_t : 1) * x_t,   out_t = h_t
+ * resets as for linear attention: nothing from before a step that begins an episode reaches it, whatever the state held. */
+
+/* A view [environments, steps, width] of a device buffer: strides in elements, the values of a step adjacent.  Inputs may have any
+ * strides (0 where environments or steps share); views that are written must not overlap themselves. */
+typedef struct {
+    void* data;
+    int64_t env, step;
+} pxr_steps;
+
+typedef struct {
+    uint32_t dtype;            /* of x, gate and of everything that is [.., width]: PXR_F32 or PXR_BF16 */
+    uint32_t n_envs, n_steps, width;
+    uint32_t coupled;          /* 0 = inputs as they are, 1 = inputs times 1 - a */
+    pxr_steps x, gate;
+    const uint8_t* d_resets;   /* [n_envs,n_steps] bytes, or NULL = none */
+    int64_t resets_env, resets_step; /* its strides */
+    const float* d_state;      /* [n_envs,width] fp32 before the first step, or NULL = zeros */
+} pxr_gated_rollout;
+
+/* Bytes of workspace that the forward (backward == 0) or backward pass needs (host only; may be 0).
+ * Errors: INVALID_ARG (null, sizes that the calls refuse). */
+int pxr_gated_recurrence_workspace(uint32_t n_envs, uint32_t n_steps, uint32_t width, uint32_t backward, size_t* bytes);
+
+/* All steps of a rollout at once: out [n_envs,n_steps,width] of the rollout's type, and the state after the last step in d_state_out
+ * [n_envs,width] fp32 (NULL if not wanted; not the buffer of d_state).  n_steps == 0 passes the state on.  An infinity or NaN in a step's
+ * x or gate reaches that step and later ones of the same environment, channel and episode and nothing else (an infinity may come out as NaN).
+ * What is written must not overlap what is read.  Equal inputs give equal bits.
+ * Errors: INVALID_ARG (null, n_envs or width == 0, n_envs * ceil(width / 64) * ceil(n_steps / 128) above 2^22, n_steps above 2^31-1, a type
+ * that is none, coupled above 1, a buffer not aligned to its elements, states that overlap, workspace missing, too small or not 16-byte
+ * aligned); DEVICE. */
+int pxr_gated_recurrence_forward(const pxr_gated_rollout* r, const pxr_steps* out, float* d_state_out, void* d_workspace,
+                                 size_t workspace_bytes, void* hip_stream);
+
+/* Gradients for the outputs' gradients dout and d_dstate_out (of the state after the last step; NULL = zeros): dx, dgate
+ * [n_envs,n_steps,width] of the rollout's type and, unless NULL, d_dstate [n_envs,width] fp32, of the state before the first step.  States are
+ * computed again in fp32, nothing is kept from the forward pass.  An infinity or NaN in dout reaches that step and earlier ones of the same
+ * environment, channel and episode.  What is written must not overlap what is read.  Equal inputs give equal bits.
+ * Errors: as for the forward pass. */
+int pxr_gated_recurrence_backward(const pxr_gated_rollout* r, const pxr_steps* dout, const float* d_dstate_out, const pxr_steps* dx,
+                                  const pxr_steps* dgate, float* d_dstate, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One step of every environment: r->n_steps must be 1 (the step strides do not matter), d_state [n_envs,width] is updated in place
+ * (r->d_state is not read); out must not overlap what is read.  One kernel.  Errors: as for the forward pass. */
+int pxr_gated_recurrence_step(const pxr_gated_rollout* r, float* d_state, const pxr_steps* out, void* hip_stream);
 
 /* Scene facts for callers and tests (sizes of what pxr_create_scene built; no passage of the paper): total
  * template vertices and triangles, dynamic LDS bytes per frame workgroup, threads per workgroup.  Any out

@@ -1,5 +1,6 @@
-"""Plain float64 definitions of a policy's memory: layer norm and linear attention with a decay for each head, forward and
-backward, one step after the other.  Pinned by closed forms and by differences in tests/test_oracle_memory.py."""
+"""Plain float64 definitions of a policy's memory: layer norm, linear attention with a decay for each head and a gated recurrence,
+forward and backward, one step after the other.  Pinned by closed forms and by differences in tests/test_oracle_memory.py
+and tests/test_oracle_recurrence.py."""
 import numpy as np
 
 
@@ -60,3 +61,40 @@ def linear_attention_backward(dout, q, k, v, log_decay, scale, resets=None, stat
         if resets is not None:
             R[np.asarray(resets[:, t], bool)] = 0.0
     return dq, dk_, dv, R
+
+
+def _gates(gate):
+    """a = 1 / (1 + exp(-gate)) and 1 - a, each to its own last digits."""
+    with np.errstate(over="ignore"):
+        return 1 / (1 + np.exp(-gate)), 1 / (1 + np.exp(gate))
+
+
+def gated_recurrence(x, gate, resets=None, state=None, coupled=True):
+    """x, gate [B,T,D], resets [B,T], state [B,D] -> (out [B,T,D], the last state)."""
+    x, (a, rest) = np.asarray(x, np.float64), _gates(np.asarray(gate, np.float64))
+    h = np.zeros((x.shape[0], x.shape[2])) if state is None else np.array(state, np.float64)
+    out = np.zeros_like(x)
+    for t in range(x.shape[1]):
+        h = h * a[:, t]
+        if resets is not None:
+            h[np.asarray(resets[:, t], bool)] = 0.0
+        h = h + (rest[:, t] if coupled else 1.0) * x[:, t]
+        out[:, t] = h
+    return out, h
+
+
+def gated_recurrence_backward(dout, x, gate, resets=None, state=None, dstate=None, coupled=True):
+    """-> (dx, dgate, the gradient of the state before the first step)."""
+    dout, x, (a, rest) = np.asarray(dout, np.float64), np.asarray(x, np.float64), _gates(np.asarray(gate, np.float64))
+    out, _ = gated_recurrence(x, gate, resets, state, coupled)
+    dx, dgate = np.zeros_like(x), np.zeros_like(x)
+    r = np.zeros((x.shape[0], x.shape[2])) if dstate is None else np.array(dstate, np.float64)
+    first = np.zeros_like(r) if state is None else np.asarray(state, np.float64)
+    for t in range(x.shape[1] - 1, -1, -1):
+        cut = np.zeros(x.shape[0], bool) if resets is None else np.asarray(resets[:, t], bool)
+        before = np.where(cut[:, None], 0.0, out[:, t - 1] if t else first)
+        r = r + dout[:, t]
+        dx[:, t] = r * (rest[:, t] if coupled else 1.0)
+        dgate[:, t] = r * a[:, t] * rest[:, t] * (before - (x[:, t] if coupled else 0.0))
+        r = np.where(cut[:, None], 0.0, r * a[:, t])
+    return dx, dgate, r

@@ -1,4 +1,5 @@
-// C ABI of a policy's memory (pxr_layer_norm_*, pxr_linear_attention_* in include/pxr.h): validation, the layers' constants, launch.
+// C ABI of a policy's memory (pxr_layer_norm_*, pxr_linear_attention_*, pxr_gated_recurrence_* in include/pxr.h): validation, the
+// layers' constants, launch.
 
 #include <hip/hip_runtime.h>
 
@@ -43,6 +44,28 @@ const char* wrong_rollout(const pxr_linear_attention* a, const pxr_rollout* r, b
 bool wrong_view(const pxr_tokens* t, uint32_t dtype, uint32_t n_steps) { return !t || (n_steps && !t->data) || !aligned(t->data, element(dtype)); }
 
 bool overlap(const float* a, const float* b, size_t n) { return a && b && a < b + n && b < a + n; }
+
+// Sizes of a gated recurrence.
+const char* wrong_gated_sizes(uint32_t n_envs, uint32_t n_steps, uint32_t width) {
+    if (n_envs == 0 || width == 0) return "n_envs and width must be positive";
+    if (n_steps > 0x7FFFFFFFu) return "n_steps must be below 2^31";
+    // (a launch counts its threads in 32 bits, and the parts of a rollout are at least this large; the factors are checked one by one, none of the products wraps)
+    const uint64_t wide = (uint64_t)n_envs * ((width + 63ull) / 64ull), parts = (n_steps + 127ull) / 128ull;
+    if (wide > (1ull << 22) || wide * (parts ? parts : 1u) > (1ull << 22)) return "n_envs * ceil(width / 64) * ceil(n_steps / 128) must be at most 2^22";
+    return nullptr;
+}
+
+const char* wrong_gated(const pxr_gated_rollout* r, bool step) {
+    if (!r) return "null argument";
+    if (r->dtype > PXR_BF16) return "dtype must be fp32 or bfloat16";
+    if (r->coupled > 1u) return "coupled must be 0 or 1";
+    if (const char* why = wrong_gated_sizes(r->n_envs, r->n_steps, r->width)) return why;
+    if (step && r->n_steps != 1) return "n_steps must be 1";
+    if (!aligned(r->d_state, 4)) return "the state must be 4-byte aligned";
+    return nullptr;
+}
+
+bool wrong_view(const pxr_steps* t, uint32_t dtype, uint32_t n_steps) { return !t || (n_steps && !t->data) || !aligned(t->data, element(dtype)); }
 
 int finish(int rc, const char* call, const std::string& err) {
     return rc == PXR_OK ? PXR_OK : pxr::set_error(rc, std::string(call) + ": " + err);
@@ -188,6 +211,54 @@ int pxr_linear_attention_step(pxr_linear_attention* a, const pxr_rollout* r, flo
         return refuse(call, "a buffer is null or not aligned to its elements");
     std::string err;
     return finish(pxr::launch_linear_attention_step(a->c, *r, d_state, *out, hip_stream, err), call, err);
+}
+
+int pxr_gated_recurrence_workspace(uint32_t n_envs, uint32_t n_steps, uint32_t width, uint32_t backward, size_t* bytes) {
+    const char* call = "pxr_gated_recurrence_workspace";
+    if (const char* why = wrong_gated_sizes(n_envs, n_steps, width)) return refuse(call, why);
+    if (!bytes) return refuse(call, "null argument");
+    *bytes = pxr::gated_recurrence_workspace(n_envs, n_steps, width, backward != 0);
+    return PXR_OK;
+}
+
+int pxr_gated_recurrence_forward(const pxr_gated_rollout* r, const pxr_steps* out, float* d_state_out, void* d_workspace, size_t workspace_bytes,
+                                 void* hip_stream) {
+    const char* call = "pxr_gated_recurrence_forward";
+    if (const char* why = wrong_gated(r, false)) return refuse(call, why);
+    if (wrong_view(&r->x, r->dtype, r->n_steps) || wrong_view(&r->gate, r->dtype, r->n_steps) || wrong_view(out, r->dtype, r->n_steps) ||
+        !aligned(d_state_out, 4))
+        return refuse(call, "a buffer is null or not aligned to its elements");
+    if (overlap(r->d_state, d_state_out, (size_t)r->n_envs * r->width)) return refuse(call, "the states overlap");
+    const size_t need = pxr::gated_recurrence_workspace(r->n_envs, r->n_steps, r->width, false);
+    if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
+        return refuse(call, "the workspace is missing, too small or not 16-byte aligned");
+    std::string err;
+    return finish(pxr::launch_gated_recurrence_forward(*r, *out, d_state_out, d_workspace, hip_stream, err), call, err);
+}
+
+int pxr_gated_recurrence_backward(const pxr_gated_rollout* r, const pxr_steps* dout, const float* d_dstate_out, const pxr_steps* dx,
+                                  const pxr_steps* dgate, float* d_dstate, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    const char* call = "pxr_gated_recurrence_backward";
+    if (const char* why = wrong_gated(r, false)) return refuse(call, why);
+    for (const pxr_steps* t : {&r->x, &r->gate, dout, dx, dgate})
+        if (wrong_view(t, r->dtype, r->n_steps)) return refuse(call, "a buffer is null or not aligned to its elements");
+    if (!aligned(d_dstate_out, 4) || !aligned(d_dstate, 4)) return refuse(call, "a buffer is null or not aligned to its elements");
+    const size_t n = (size_t)r->n_envs * r->width;
+    if (overlap(r->d_state, d_dstate, n) || overlap(d_dstate_out, d_dstate, n)) return refuse(call, "the states overlap");
+    const size_t need = pxr::gated_recurrence_workspace(r->n_envs, r->n_steps, r->width, true);
+    if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
+        return refuse(call, "the workspace is missing, too small or not 16-byte aligned");
+    std::string err;
+    return finish(pxr::launch_gated_recurrence_backward(*r, *dout, d_dstate_out, *dx, *dgate, d_dstate, d_workspace, hip_stream, err), call, err);
+}
+
+int pxr_gated_recurrence_step(const pxr_gated_rollout* r, float* d_state, const pxr_steps* out, void* hip_stream) {
+    const char* call = "pxr_gated_recurrence_step";
+    if (const char* why = wrong_gated(r, true)) return refuse(call, why);
+    if (wrong_view(&r->x, r->dtype, 1) || wrong_view(&r->gate, r->dtype, 1) || wrong_view(out, r->dtype, 1) || !d_state || !aligned(d_state, 4))
+        return refuse(call, "a buffer is null or not aligned to its elements");
+    std::string err;
+    return finish(pxr::launch_gated_recurrence_step(*r, d_state, *out, hip_stream, err), call, err);
 }
 
 }  // extern "C"

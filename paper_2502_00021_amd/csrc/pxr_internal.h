@@ -254,6 +254,13 @@ int launch_linear_attention_backward(const LinearAttentionConsts& c, const pxr_r
 int launch_linear_attention_step(const LinearAttentionConsts& c, const pxr_rollout& r, float* state, const pxr_tokens& out, void* stream,
                                  std::string& err);
 
+// gated_recurrence.hip (arguments as checked by memory_api.cpp)
+size_t gated_recurrence_workspace(uint32_t n_envs, uint32_t n_steps, uint32_t width, bool backward);
+int launch_gated_recurrence_forward(const pxr_gated_rollout& r, const pxr_steps& out, float* state_out, void* ws, void* stream, std::string& err);
+int launch_gated_recurrence_backward(const pxr_gated_rollout& r, const pxr_steps& dout, const float* dstate_out, const pxr_steps& dx,
+                                     const pxr_steps& dgate, float* dstate, void* ws, void* stream, std::string& err);
+int launch_gated_recurrence_step(const pxr_gated_rollout& r, float* state, const pxr_steps& out, void* stream, std::string& err);
+
 // pipeline.cpp works through these (api.cpp / conv_api.cpp own the handles' layouts).
 constexpr uint32_t kMaxPipelineChunks = 16;
 void scene_shape(const pxr_scene* s, uint32_t* K, uint32_t* H, uint32_t* W);

@@ -3,7 +3,7 @@
 Mirrors include/pxr.h one to one: create_scene / destroy_scene /
 apply_distractor / render_batch, set_skeleton / pose_batch /
 render_batch_kinematic (+ scene_info, set_block_threads, host_tables), the policy's first layer (Conv) and its memory
-(layer_norm, layer_norm_backward, LinearAttention).  PyTorch is used only to hold device memory and name the stream.
+(layer_norm, layer_norm_backward, LinearAttention, gated_recurrence).  PyTorch is used only to hold device memory and name the stream.
 There is no fallback: a missing library or a failing call raises.
 """
 import ctypes as C
@@ -85,10 +85,22 @@ class Rollout(C.Structure):
                 ("d_resets", C.c_void_p), ("resets_env", C.c_int64), ("resets_step", C.c_int64), ("d_state", C.c_void_p)]
 
 
-# The same three as bytes: a call packs its arguments in a fraction of the time that it takes to fill the structures.
+class Steps(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("env", C.c_int64), ("step", C.c_int64)]
+
+
+class GatedRollout(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("n_envs", C.c_uint32), ("n_steps", C.c_uint32), ("width", C.c_uint32), ("coupled", C.c_uint32),
+                ("x", Steps), ("gate", Steps),
+                ("d_resets", C.c_void_p), ("resets_env", C.c_int64), ("resets_step", C.c_int64), ("d_state", C.c_void_p)]
+
+
+# Calls' structures as bytes: a call packs its arguments in a fraction of the time that it takes to fill the structures.
 _pack_norm = struct.Struct("@IIQIfqqq").pack
 _pack_tokens = struct.Struct("@Pqqq").pack
 _pack_rollout = struct.Struct("@III4xPqqqPqqqPqqqPqqP").pack
+_pack_steps = struct.Struct("@Pqq").pack
+_pack_gated = struct.Struct("@IIIII4xPqqPqqPqqP").pack
 
 
 _lib = None
@@ -162,6 +174,13 @@ def lib():
                      "linear_attention_destroy", "linear_attention_workspace", "linear_attention_forward",
                      "linear_attention_backward", "linear_attention_step"):
             getattr(L, "pxr_" + name).restype = C.c_int
+        steps = vp
+        L.pxr_gated_recurrence_workspace.argtypes = [u32, u32, u32, u32, size]
+        L.pxr_gated_recurrence_forward.argtypes = [rollout, steps, vp, vp, C.c_size_t, vp]
+        L.pxr_gated_recurrence_backward.argtypes = [rollout, steps, vp, steps, steps, vp, vp, C.c_size_t, vp]
+        L.pxr_gated_recurrence_step.argtypes = [rollout, vp, steps, vp]
+        for name in ("workspace", "forward", "backward", "step"):
+            getattr(L, "pxr_gated_recurrence_" + name).restype = C.c_int
         L.pxr_selftest_arithmetic.argtypes = [vp]
         L.pxr_selftest_arithmetic.restype = C.c_int
         L.pxr_measure_peaks.argtypes = [vp, vp, vp, vp, vp]
@@ -791,6 +810,100 @@ class LinearAttention:
                                               _stream_handle(stream, q)))
         _written(torch, *given)
         return out
+
+
+def _steps_view(x, shape, dtype):
+    """The fields of pxr_steps for a [B, T, D] or (one step) [B, D] tensor of this shape and type."""
+    assert x.is_cuda and x.dtype == dtype and x.shape == shape, (tuple(x.shape), tuple(shape), x.dtype)
+    s = x.stride()
+    assert s[-1] == 1 or shape[-1] == 1 or x.numel() == 0, "a step's values must be adjacent"
+    return (x.data_ptr(), s[0], s[1]) if len(s) == 3 else (x.data_ptr(), s[0], 0)
+
+
+def _channels(torch, state, B, D):
+    assert state.is_cuda and state.dtype == torch.float32 and state.is_contiguous() and state.shape == (B, D), tuple(state.shape)
+    return state.data_ptr()
+
+
+def _gated_rollout(torch, x, gate, resets, state, coupled):
+    """The bytes of pxr_gated_rollout; environments, steps and channels."""
+    shape, dtype = x.shape, x.dtype
+    B, T, D = shape if len(shape) == 3 else (shape[0], 1, shape[1])
+    marks = (0, 0, 0)
+    if resets is not None:
+        assert resets.is_cuda and resets.dtype in (torch.bool, torch.uint8) and resets.shape == shape[:-1], tuple(resets.shape)
+        s = resets.stride()
+        marks = (resets.data_ptr(), s[0], s[1] if len(s) == 2 else 0)
+    packed = _pack_gated(_dtype_code(torch, dtype), B, T, D, 1 if coupled else 0, *_steps_view(x, shape, dtype), *_steps_view(gate, shape, dtype),
+                         *marks, 0 if state is None else _channels(torch, state, B, D))
+    return packed, B, T, D
+
+
+_gated_asked = (None, 0)
+
+
+def _gated_workspace(torch, like, B, T, D, backward, stream):
+    global _gated_asked
+    sizes = (B, T, D, backward)
+    asked, need = _gated_asked  # (the bytes for the sizes that were asked for last are known)
+    if asked != sizes:
+        n = C.c_size_t()
+        _check((_lib or lib()).pxr_gated_recurrence_workspace(B, T, D, backward, n))
+        need = n.value
+        _gated_asked = (sizes, need)
+    return _empty(torch, like, stream, (need,), torch.uint8) if need else None, need
+
+
+def gated_recurrence(x, gate, resets=None, state=None, coupled=True, out=None, state_out=None, stream=None):
+    """h_t = (an episode begins ? 0 : a h_{t-1}) + (coupled ? 1 - a : 1) x_t with a = 1 / (1 + exp(-gate_t)), for each environment
+    and channel.  x, gate: CUDA float32 or bfloat16 [B,T,D] (any strides, a step's values adjacent); resets: bool or uint8
+    [B,T], true where a step begins an episode, or None; state: float32 [B,D] before the first step, or None = zeros.  Returns
+    (out [B,T,D], the state after the last step); enqueue only."""
+    torch = _torch or _torch_module()
+    assert x.dim() == 3
+    r, B, T, D = _gated_rollout(torch, x, gate, resets, state, coupled)
+    given = [t for t in (out, state_out) if t is not None]
+    out = _empty_like(torch, x, stream) if out is None else out
+    if state_out is None:
+        state_out = _empty(torch, x, stream, (B, D), torch.float32) if state is None else _empty_like(torch, state, stream)
+    ws, need = _gated_workspace(torch, x, B, T, D, 0, stream)
+    _check((_lib or lib()).pxr_gated_recurrence_forward(r, _pack_steps(*_steps_view(out, x.shape, x.dtype)), _channels(torch, state_out, B, D),
+                                                        _ptr(ws), need, _stream_handle(stream, x)))
+    if given:
+        _written(torch, *given)
+    return out, state_out
+
+
+def gated_recurrence_backward(dout, x, gate, resets=None, state=None, dstate=None, coupled=True, stream=None):
+    """Gradients for dout [B,T,D] and dstate [B,D] (of the state after the last step, or None = zeros) of a gated_recurrence call
+    with these inputs.  Returns (dx, dgate, the gradient of the state before the first step or, where there was none, None);
+    enqueue only."""
+    torch = _torch or _torch_module()
+    assert x.dim() == 3
+    r, B, T, D = _gated_rollout(torch, x, gate, resets, state, coupled)
+    dx = _empty_like(torch, x, stream)
+    dgate = _empty_like(torch, dx, stream)
+    dfirst = None if state is None else _empty_like(torch, state, stream)
+    ws, need = _gated_workspace(torch, x, B, T, D, 1, stream)
+    _check((_lib or lib()).pxr_gated_recurrence_backward(
+        r, _pack_steps(*_steps_view(dout, x.shape, x.dtype)), None if dstate is None else _channels(torch, dstate, B, D),
+        _pack_steps(*_steps_view(dx, x.shape, x.dtype)), _pack_steps(*_steps_view(dgate, x.shape, x.dtype)), _ptr(dfirst), _ptr(ws), need,
+        _stream_handle(stream, x)))
+    return dx, dgate, dfirst
+
+
+def gated_recurrence_step(x, gate, state, resets=None, coupled=True, out=None, stream=None):
+    """One step of every environment: x, gate [B,D], resets [B] or None; state float32 [B,D] is updated in place (autograd is
+    told).  Returns out [B,D]; enqueue only."""
+    torch = _torch or _torch_module()
+    assert x.dim() == 2
+    r, B, _, D = _gated_rollout(torch, x, gate, resets, None, coupled)
+    given = (state,) if out is None else (state, out)
+    out = _empty_like(torch, x, stream) if out is None else out
+    _check((_lib or lib()).pxr_gated_recurrence_step(r, _channels(torch, state, B, D), _pack_steps(*_steps_view(out, x.shape, x.dtype)),
+                                                     _stream_handle(stream, x)))
+    _written(torch, *given)
+    return out
 
 
 def make_skeleton_desc(skel, n_free, n_angles):

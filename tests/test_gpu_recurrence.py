@@ -1,0 +1,407 @@
+"""A policy's gated recurrence on the GPU against the float64 definition.
+
+Tolerances, from the arithmetic.  u = 2^-24 and w = 2^-8 are half a unit of fp32 and of bfloat16.  a and 1 - a come out with a relative error of
+at most c = 8 + 2 max|gate| times u (the exponential's argument is rounded once, |gate| u, the rest is a handful of operations).  A term of h_t
+passes through at most t + 20 products and sums, so with M the recurrence of the magnitudes h is off by at most c (t + 20) u M; L likewise from the
+end, dgate by both and a few operations more.  A worst case has all errors in one direction; they are independent, and memory is
+shorter than the rollout, so the root mean square is asserted as well: 2^-20 of the results'.  One rounding on the way out to
+bfloat16: w |ref|.
+"""
+import numpy as np
+import pytest
+
+from oracle import memory as om
+
+pytestmark = pytest.mark.gpu
+
+U, W = 2.0 ** -24, 2.0 ** -8
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as _torch
+    assert _torch.cuda.is_available(), "these tests need the MI355X"
+    return _torch
+
+
+@pytest.fixture(scope="module")
+def pxr():
+    from paper_2502_00021_amd import pxr as _pxr
+    _pxr.lib()
+    return _pxr
+
+
+def f64(x):
+    return x.detach().double().cpu().numpy()
+
+
+def gpu(torch, x, dtype="f32"):
+    return torch.from_numpy(np.ascontiguousarray(x, np.float32)).cuda().to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+
+
+def close(got, ref, mag, depth, bf16, what):
+    if not ref.size:
+        return
+    bound = depth * U * mag + (W * np.abs(ref) if bf16 else 0.0) + 1e-37
+    bad = ~(np.abs(got - ref) <= bound)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, first at {np.argwhere(bad)[0]}: {got[bad][0]} for {ref[bad][0]}, bound {bound[bad][0]}"
+    rms = np.sqrt((ref ** 2).mean())
+    if ref.size >= 64 and rms > 0:
+        assert np.sqrt(((got - ref) ** 2).mean()) <= (W if bf16 else 2.0 ** -20) * rms, what
+
+
+def inputs(torch, rng, B, T, D, dtype, resets=0.05, state=True, layout="btd", spread=2.0):
+    """x, gate, resets, state, dout, dstate in one of the layouts that programs have."""
+    def make(scale=1.0, shift=0.0):
+        x = rng.standard_normal((B, T, D)) * scale + shift
+        if layout == "tbd":
+            return gpu(torch, x.transpose(1, 0, 2).copy(), dtype).transpose(0, 1)
+        return gpu(torch, x, dtype)
+    shift = np.linspace(0, 4, D)
+    if layout == "fused":
+        both = gpu(torch, np.concatenate([rng.standard_normal((B, T, D)), rng.standard_normal((B, T, D)) * spread + shift], -1), dtype)
+        x, gate = both.split([D, D], -1)
+    else:
+        x, gate = make(), make(spread, shift)
+    r = torch.from_numpy(rng.random((B, T)) < resets).cuda() if resets else None
+    return x, gate, r, gpu(torch, rng.standard_normal((B, D))) if state else None, make(), gpu(torch, rng.standard_normal((B, D)))
+
+
+def check(torch, pxr, x, gate, r, s, dout, ds, coupled=True, backward=True):
+    B, T, D = x.shape
+    bf16 = x.dtype == torch.bfloat16
+    X, G = f64(x), f64(gate)
+    R, S = None if r is None else r.cpu().numpy(), None if s is None else f64(s)
+    c = 8 + 2 * min(100.0, np.abs(G).max(initial=0))
+    out, last = pxr.gated_recurrence(x, gate, resets=r, state=s, coupled=coupled)
+    assert out.dtype == x.dtype and out.shape == x.shape and last.shape == (B, D) and last.dtype == torch.float32
+    ref, rlast = om.gated_recurrence(X, G, R, S, coupled)
+    M, mlast = om.gated_recurrence(abs(X), G, R, None if S is None else abs(S), coupled)
+    close(f64(out), ref, M, c * (T + 20), bf16, "out")
+    close(f64(last), rlast, mlast, c * (T + 20), False, "state")
+    if not backward:
+        return
+    dx, dgate, dfirst = pxr.gated_recurrence_backward(dout, x, gate, resets=r, state=s, dstate=ds, coupled=coupled)
+    DO, DS = f64(dout), None if ds is None else f64(ds)
+    rx, rg, rs = om.gated_recurrence_backward(DO, X, G, R, S, DS, coupled)
+    mx, _, ms = om.gated_recurrence_backward(abs(DO), abs(X), G, R, None if S is None else abs(S), None if DS is None else abs(DS), coupled)
+    # dgate of magnitudes: |L| a (1 - a) (|h| before + |x|)
+    a, rest = om._gates(G)
+    L = om.gated_recurrence_backward(abs(DO), X, G, R, S, None if DS is None else abs(DS), False)[0]
+    first = np.zeros((B, 1, D)) if S is None else abs(S)[:, None]
+    before = np.concatenate([first, M[:, :-1]], 1) if T else M
+    if R is not None:
+        before = np.where(np.asarray(R, bool)[..., None], 0.0, before)
+    close(f64(dx), rx, mx, c * (T + 20), bf16, "dx")
+    close(f64(dgate), rg, L * a * rest * (before + (abs(X) if coupled else 0)), c * (T + 30), bf16, "dgate")
+    assert dx.dtype == dgate.dtype == x.dtype
+    if s is None:
+        assert dfirst is None
+    else:
+        close(f64(dfirst), rs, ms, c * (T + 20), False, "dstate")
+
+
+@pytest.mark.parametrize("coupled", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,D", [(1, 1, 1), (3, 5, 1), (2, 16, 2), (5, 17, 3), (4, 33, 64), (2, 128, 130), (3, 129, 65), (2, 256, 40), (2, 257, 33), (1, 1000, 7),
+                                   (17, 40, 200), (300, 9, 31), (9, 31, 300), (65, 12, 129)])
+def test_sizes(torch, pxr, B, T, D, dtype, coupled):
+    rng = np.random.default_rng(B * 1000 + T * 10 + D)
+    check(torch, pxr, *inputs(torch, rng, B, T, D, dtype), coupled=coupled)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [2, 15, 31, 32, 63, 64, 65, 127, 130, 143, 144, 255, 300, 511, 513, 700])
+def test_lengths(torch, pxr, T, dtype):
+    rng = np.random.default_rng(T)
+    check(torch, pxr, *inputs(torch, rng, 2, T, 70, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,D", [(1, 5000, 96), (2, 3333, 5), (1, 9000, 2), (3, 2049, 150), (1, 20000, 1), (400, 300, 20), (40, 700, 257)])
+def test_long_axes(torch, pxr, B, T, D, dtype):
+    """Cut into segments, or by one workgroup after the other."""
+    rng = np.random.default_rng(T)
+    check(torch, pxr, *inputs(torch, rng, B, T, D, dtype, resets=0.002))
+    check(torch, pxr, *inputs(torch, rng, B, T, D, dtype, resets=0.0), coupled=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["btd", "tbd", "fused"])
+@pytest.mark.parametrize("D", [64, 20, 9])
+def test_layouts(torch, pxr, layout, D, dtype):
+    rng = np.random.default_rng(D)
+    check(torch, pxr, *inputs(torch, rng, 3, 70, D, dtype, layout=layout))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [40, 300])
+def test_broadcast_inputs(torch, pxr, T, dtype):
+    """Strides of zero: environments or steps that share.  The gradients of what is shared are the sums over those that share it, which a
+    caller forms from the gradients of each."""
+    rng = np.random.default_rng(T)
+    x, gate, r, s, dout, ds = inputs(torch, rng, 3, T, 36, dtype)
+    check(torch, pxr, x[:1].expand(3, -1, -1), gate[:, :1].expand(-1, T, -1), r[:1].expand(3, -1), s, dout[:, :1].expand(-1, T, -1), ds)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("resets", [0.0, 0.02, 0.3, 1.0])
+@pytest.mark.parametrize("state", [True, False])
+def test_resets_and_states(torch, pxr, resets, state, dtype):
+    rng = np.random.default_rng(int(resets * 100))
+    x, gate, r, s, dout, ds = inputs(torch, rng, 4, 150, 32, dtype, resets=resets, state=state)
+    check(torch, pxr, x, gate, r, s, dout, ds if state else None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [130, 300])
+def test_resets_at_the_edges_of_chunks(torch, pxr, T, dtype):
+    rng = np.random.default_rng(1)
+    x, gate, r, s, dout, ds = inputs(torch, rng, 8, T, 40, dtype)
+    r.zero_()
+    for b, at in enumerate(([0], [1], [15, 16], [31, 32], [63, 64], [65, 128], [129], list(range(60, 70)))):
+        r[b, at] = True
+    check(torch, pxr, x, gate, r, s, dout, ds)
+    check(torch, pxr, x, gate, r.to(torch.uint8) * 255, s, dout, ds)
+    check(torch, pxr, x, gate, r.t().contiguous().t(), s, dout, ds)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gates_of_any_size(torch, pxr, dtype):
+    """Shut, wide open, and between: 1 - a keeps its digits where a is all but one."""
+    rng = np.random.default_rng(2)
+    x, gate, r, s, dout, ds = inputs(torch, rng, 2, 200, 24, dtype, resets=0.01)
+    gate.copy_(gpu(torch, np.broadcast_to(np.linspace(-40, 40, 24), (2, 200, 24)), dtype))
+    check(torch, pxr, x, gate, r, s, dout, ds)
+    check(torch, pxr, x, gate, None, s, dout, ds, coupled=False)
+    for value in (0.0, -0.0, float("inf"), float("-inf"), 1e30, -1e30, 88.0, -104.0):
+        gate.fill_(value)
+        out, last = pxr.gated_recurrence(x, gate, state=s)
+        a = 1.0 if value > 80 else 0.5 if value == 0 else 0.0
+        ref, rlast = om.gated_recurrence(f64(x), np.full(x.shape, {1.0: 800.0, 0.5: 0.0, 0.0: -800.0}[a]), None, f64(s))
+        assert np.abs(f64(last) - rlast).max() <= 2 ** -20 * np.abs(rlast).max() and np.abs(f64(out) - ref).max() <= W * np.abs(ref).max()
+        dx, dgate, dfirst = pxr.gated_recurrence_backward(dout, x, gate, state=s, dstate=ds)
+        assert dx.isfinite().all() and dgate.isfinite().all() and dfirst.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_without_steps(torch, pxr, dtype):
+    rng = np.random.default_rng(3)
+    x, gate, _, s, dout, ds = inputs(torch, rng, 3, 0, 40, dtype, resets=0)
+    out, last = pxr.gated_recurrence(x, gate, state=s)
+    assert out.shape == (3, 0, 40) and torch.equal(last, s) and (pxr.gated_recurrence(x, gate)[1] == 0).all()
+    dx, dgate, dfirst = pxr.gated_recurrence_backward(dout, x, gate, state=s, dstate=ds)
+    assert dx.shape == dgate.shape == x.shape and torch.equal(dfirst, ds)
+    assert (pxr.gated_recurrence_backward(dout, x, gate, state=s)[2] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("coupled", [True, False])
+@pytest.mark.parametrize("B,D", [(1, 1), (5, 64), (33, 201), (1000, 7), (16, 1024), (3, 4099)])
+def test_single_steps(torch, pxr, B, D, coupled, dtype):
+    """Step by step against the definition; views of one projection's output; resets that take the state away, whatever it holds."""
+    rng = np.random.default_rng(D)
+    T = 6
+    both = gpu(torch, rng.standard_normal((B, T, 2 * D)) * 2, dtype)
+    x, gate = both.split([D, D], -1)
+    r = torch.from_numpy(rng.random((B, T)) < 0.2).cuda()
+    first = gpu(torch, rng.standard_normal((B, D)))
+    state = first.clone()
+    outs = torch.stack([pxr.gated_recurrence_step(x[:, t], gate[:, t], state, resets=r[:, t], coupled=coupled) for t in range(T)], 1)
+    X, G, R, S = f64(x), f64(gate), r.cpu().numpy(), f64(first)
+    ref, rlast = om.gated_recurrence(X, G, R, S, coupled)
+    M, mlast = om.gated_recurrence(abs(X), G, R, abs(S), coupled)
+    c = 8 + 2 * np.abs(G).max()
+    close(f64(outs), ref, M, c * (T + 4), dtype == "bf16", "out")
+    close(f64(state), rlast, mlast, c * (T + 4), False, "state")
+    broken = torch.full((B, D), float("nan"), device="cuda")
+    pxr.gated_recurrence_step(x[:, 0], gate[:, 0], broken, resets=torch.ones(B, dtype=torch.uint8, device="cuda"), coupled=coupled)
+    assert broken.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("B,T,begins,at", [(2, 40, 20, 11), (2, 40, 20, 20), (2, 300, 128, 100), (2, 300, 128, 128), (1, 3000, 1000, 990), (1, 3000, 640, 640), (2, 200, 17, 15)])
+def test_what_is_not_finite_stays_in_its_episode(torch, pxr, B, T, begins, at, bad, dtype):
+    rng = np.random.default_rng(T)
+    x, gate, r, s, dout, ds = inputs(torch, rng, B, T, 33, dtype)
+    r.zero_()
+    r[0, begins] = True
+    args = dict(resets=r, state=s)
+    out, last = pxr.gated_recurrence(x, gate, **args)
+    got = pxr.gated_recurrence_backward(dout, x, gate, dstate=ds, **args)
+    mine = slice(at, begins if at < begins else None)     # what a value at step `at` may reach, forward
+    back = slice(begins if at >= begins else 0, at + 1)   # ... and backward
+
+    def same(new, old, but):
+        keep = torch.ones(new.shape, dtype=torch.bool, device="cuda")
+        for b in but:
+            keep[0, b, 5] = False
+        assert torch.equal(new[keep], old[keep])
+    for which in ("x", "gate"):
+        t = dict(x=x.clone(), gate=gate.clone())
+        t[which][0, at, 5] = bad
+        o, e = pxr.gated_recurrence(t["x"], t["gate"], **args)
+        same(o, out, [mine])
+        keep = torch.ones_like(last, dtype=torch.bool)
+        keep[0, 5] = at < begins
+        assert torch.equal(e[keep], last[keep])
+        if which == "x" or bad != bad:
+            assert not o[0, at, 5].isfinite()
+        dx, dgate, dfirst = pxr.gated_recurrence_backward(dout, t["x"], t["gate"], dstate=ds, **args)
+        same(dx, got[0], [] if which == "x" else [back])
+        same(dgate, got[1], [mine] if which == "x" else [mine, back])
+        keep[0, 5] = at >= begins
+        assert torch.equal(dfirst[keep], got[2][keep])
+    d = dout.clone()
+    d[0, at, 5] = bad
+    dx, dgate, dfirst = pxr.gated_recurrence_backward(d, x, gate, dstate=ds, **args)
+    same(dx, got[0], [back])
+    same(dgate, got[1], [back])
+    assert not dx[0, at, 5].isfinite()
+    # a state that is no number, and such a gradient of the last one
+    broken = s.clone()
+    broken[0, 5] = bad
+    o, e = pxr.gated_recurrence(x, gate, resets=r, state=broken)
+    same(o, out, [slice(0, begins)])
+    assert torch.equal(e, last) and not o[0, 0, 5].isfinite()
+    d = ds.clone()
+    d[0, 5] = bad
+    dx, dgate, dfirst = pxr.gated_recurrence_backward(dout, x, gate, dstate=d, **args)
+    same(dx, got[0], [slice(begins, None)])
+    assert torch.equal(dfirst, got[2]) and not dx[0, -1, 5].isfinite()
+
+
+def test_gradients_by_differences(torch, pxr):
+    """The kernels' own forward pass, moved along a direction."""
+    rng = np.random.default_rng(4)
+    x, gate, r, s, dout, ds = inputs(torch, rng, 3, 200, 40, "f32", spread=1.0)
+    got = pxr.gated_recurrence_backward(dout, x, gate, resets=r, state=s, dstate=ds)
+    h = 2.0 ** -6
+
+    def f(x_, gate_, s_):
+        out, last = pxr.gated_recurrence(x_, gate_, resets=r, state=s_)
+        return float((out.double() * dout.double()).sum() + (last.double() * ds.double()).sum())
+    for grad, move in zip(got, (lambda d: (x + d, gate, s), lambda d: (x, gate + d, s), lambda d: (x, gate, s + d))):
+        d = gpu(torch, rng.standard_normal(tuple(grad.shape)))
+        size = float((grad.double() * d.double()).square().sum().sqrt())
+        want = float((grad.double() * d.double()).sum())
+        # h^2 times third derivatives (order 1 a value; none for x and the state, in which f is linear), and 24000 roundings of values around 1, in the
+        # root of their number, over h
+        assert abs((f(*move(h * d)) - f(*move(-h * d))) / (2 * h) - want) < 3 * h * h * size + 16 * U * np.sqrt(24000.0) / h
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,D,pitch", [(3, 50, 33, 40), (2, 300, 64, 67), (70, 7, 5, 9), (1, 2500, 31, 34)])
+def test_writes_nothing_else_and_gives_equal_bits(torch, pxr, B, T, D, pitch, dtype):
+    rng = np.random.default_rng(D)
+    x, gate, r, s, dout, ds = inputs(torch, rng, B, T, D, dtype)
+    out, last = pxr.gated_recurrence(x, gate, resets=r, state=s)
+    wide = torch.full((B + 2, T + 3, pitch), 7.0, device="cuda", dtype=x.dtype)
+    into = wide[1:B + 1, 1:T + 1, 2:2 + D]
+    given = torch.full((B * D + 2,), 7.0, device="cuda")
+    o, e = pxr.gated_recurrence(x, gate, resets=r, state=s, out=into, state_out=given[1:-1].view(B, D))
+    assert torch.equal(o, out) and torch.equal(e, last) and given[0] == 7 and given[-1] == 7
+    into.fill_(7.0)
+    assert (wide == 7).all()
+    first = pxr.gated_recurrence_backward(dout, x, gate, resets=r, state=s, dstate=ds)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, pxr.gated_recurrence_backward(dout, x, gate, resets=r, state=s, dstate=ds)))
+    wide = torch.full((B + 2, pitch), 7.0, device="cuda", dtype=x.dtype)
+    state = torch.full((B * D + 2,), 7.0, device="cuda")
+    state[1:-1] = s.flatten()
+    pxr.gated_recurrence_step(x[:, 0], gate[:, 0], state[1:-1].view(B, D), out=wide[1:B + 1, 2:2 + D])
+    wide[1:B + 1, 2:2 + D] = 7.0
+    assert (wide == 7).all() and state[0] == 7 and state[-1] == 7
+
+
+def test_gradients_are_written_with_the_strides_that_they_are_given(torch, pxr):
+    import ctypes as C
+    rng = np.random.default_rng(5)
+    for B, T, D in ((3, 50, 33), (2, 300, 20)):
+        x, gate, r, s, dout, ds = inputs(torch, rng, B, T, D, "bf16")
+        want = pxr.gated_recurrence_backward(dout, x, gate, resets=r, state=s, dstate=ds)
+        both = torch.full((T, B, 2 * D + 1), 7.0, device="cuda", dtype=torch.bfloat16)
+        rollout = pxr.GatedRollout(1, B, T, D, 1, *(pxr.Steps(t.data_ptr(), t.stride(0), t.stride(1)) for t in (x, gate)), r.data_ptr(), T, 1, s.data_ptr())
+        need = C.c_size_t()
+        assert pxr.lib().pxr_gated_recurrence_workspace(B, T, D, 1, need) == pxr.OK
+        ws = torch.empty(max(16, need.value), device="cuda", dtype=torch.uint8)
+        at, given = both.data_ptr(), pxr.Steps(dout.data_ptr(), dout.stride(0), dout.stride(1))
+        views = [pxr.Steps(at + 2 * first, 2 * D + 1, B * (2 * D + 1)) for first in (0, D)]
+        assert pxr.lib().pxr_gated_recurrence_backward(C.byref(rollout), C.byref(given), ds.data_ptr(), *map(C.byref, views), None,
+                                                       ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == pxr.OK
+        assert torch.equal(both[..., :D].transpose(0, 1), want[0]) and torch.equal(both[..., D:2 * D].transpose(0, 1), want[1]) and (both[..., -1] == 7).all()
+
+
+def test_offsets_past_32_bits(torch, pxr):
+    """Environments that lie 2^31 values apart."""
+    D, T = 40, 20
+    rng = np.random.default_rng(6)
+    apart = 2 ** 31 + 64
+    big = torch.empty(apart + T * D + 64, device="cuda", dtype=torch.bfloat16)
+    x, gate, r, s, dout, ds = inputs(torch, rng, 2, T, D, "bf16")
+    view = big.as_strided((2, T, D), (apart, D, 1), 3)
+    view.copy_(x)
+    out, last = pxr.gated_recurrence(x, gate, resets=r, state=s)
+    o, e = pxr.gated_recurrence(view, gate, resets=r, state=s)
+    assert torch.equal(o, out) and torch.equal(e, last)
+    got = pxr.gated_recurrence_backward(dout, x, gate, resets=r, state=s, dstate=ds)
+    assert all(torch.equal(a, b) for a, b in zip(got, pxr.gated_recurrence_backward(dout, view, gate, resets=r, state=s, dstate=ds)))
+    step = pxr.gated_recurrence_step(x[:, 3], gate[:, 3], s.clone())
+    assert torch.equal(step, pxr.gated_recurrence_step(view[:, 3], gate[:, 3], s.clone()))
+    pxr.gated_recurrence(x, gate, resets=r, state=s, out=view)
+    assert torch.equal(view, out)
+
+
+def test_streams_and_graphs(torch, pxr):
+    """On a stream of the caller's, and captured and replayed with new values, with eager calls between; a segmented call's workspace lives in
+    the graph's own pool."""
+    rng = np.random.default_rng(7)
+    for B, T, D in ((4, 60, 64), (1, 3000, 96)):
+        sets = [inputs(torch, rng, B, T, D, "bf16") for _ in range(4)]
+        static = [t.clone() for t in sets[0]]
+        state = static[3].clone()
+
+        def both(x, gate, r, s, dout, ds):
+            return (*pxr.gated_recurrence(x, gate, resets=r, state=s), *pxr.gated_recurrence_backward(dout, x, gate, resets=r, state=s, dstate=ds))
+        want = [both(*t) for t in sets]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        x, gate, r, s, dout, ds = sets[1]
+        got = (*pxr.gated_recurrence(x, gate, resets=r, state=s, stream=side.cuda_stream),
+               *pxr.gated_recurrence_backward(dout, x, gate, resets=r, state=s, dstate=ds, stream=side.cuda_stream))
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip(got, want[1]))
+        graphs = []
+        for _ in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                graphs.append((g, both(*static), pxr.gated_recurrence_step(static[0][:, 0], static[1][:, 0], state)))
+        for i in (1, 2, 3, 0, 2):
+            for t, new in zip(static, sets[i]):
+                t.copy_(new)
+            state.copy_(sets[i][3])
+            for g, got, stepped in graphs:
+                g.replay()
+                eager = both(*sets[(i + 1) % 4])
+                torch.cuda.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(got, want[i])) and all(torch.equal(a, b) for a, b in zip(eager, want[(i + 1) % 4]))
+
+
+def test_refusals(torch, pxr):
+    rng = np.random.default_rng(8)
+    x, gate, r, s, dout, ds = inputs(torch, rng, 2, 10, 16, "f32")
+    for bad in (dict(x=x.half(), gate=gate.half()), dict(gate=gate.bfloat16()), dict(gate=gate[:, :9]), dict(x=x.cpu()), dict(resets=r[:, :9]), dict(resets=r.int()),
+                dict(state=s[:1]), dict(state=s.double()), dict(x=x.transpose(1, 2).contiguous().transpose(1, 2)), dict(x=x[0], gate=gate[0]),
+                dict(out=torch.empty_like(x)[:, :9]), dict(state_out=torch.empty((2, 17), device="cuda"))):
+        a = dict(dict(x=x, gate=gate, resets=r, state=s), **bad)
+        with pytest.raises(AssertionError):
+            pxr.gated_recurrence(a.pop("x"), a.pop("gate"), **a)
+    with pytest.raises(pxr.PxrError, match="overlap"):
+        pxr.gated_recurrence(x, gate, state=s, state_out=s)
+    with pytest.raises(AssertionError):
+        pxr.gated_recurrence_backward(dout[:, 1:], x, gate)
+    with pytest.raises(AssertionError):
+        pxr.gated_recurrence_step(x, gate, s)
+    with pytest.raises(pxr.PxrError, match="positive"):
+        pxr.gated_recurrence(x[:0], gate[:0])
