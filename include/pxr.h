@@ -279,7 +279,7 @@ int pxr_pipeline_set_overlap_from(pxr_pipeline* p, uint64_t bytes);
 /* Into how many chunks a step of B environments is cut (host only; no passage of the paper).  Errors: INVALID_ARG. */
 int pxr_pipeline_info(const pxr_pipeline* p, uint32_t B, uint32_t* chunks);
 
-/* ---- a policy's memory: layer norm, linear attention, a gated recurrence ----
+/* ---- a policy's memory: layer norm, linear attention, a gated recurrence, norms and rotation of heads ----
  * The paper's loop (section 2) ends with the first layer of a policy.  What stands behind that layer in a policy that
  * remembers: a normalisation, and a state per environment that each step reads and adds to.  Element types are fp32 and
  * bfloat16; statistics, sums and states are fp32.  All calls only enqueue: no allocation, no synchronisation. */
@@ -429,6 +429,53 @@ int pxr_gated_recurrence_backward(const pxr_gated_rollout* r, const pxr_steps* d
 /* One step of every environment: r->n_steps must be 1 (the step strides do not matter), d_state [n_envs,width] is updated in place
  * (r->d_state is not read); out must not overlap what is read.  One kernel.  Errors: as for the forward pass. */
 int pxr_gated_recurrence_step(const pxr_gated_rollout* r, float* d_state, const pxr_steps* out, void* hip_stream);
+
+/* Norms of queries and keys for each head, with the rotation by a step's position in the same pass: what stands before attention
+ * where queries and keys grow together or the distance between steps should count.  For a head's values x [d_head] of a step at position p:
+ *   y = x / sqrt(sum x^2 / d_head + eps) * weight
+ *   the pairs (y_i, y_{i + d_rotary/2}), i < d_rotary/2, are turned by p * frequencies[i]:  (u, v) -> (u cos - v sin, v cos + u sin)
+ * Values from d_rotary on stay as they are.  Angles keep 2^-22 of a turn up to positions of 2^31. */
+typedef struct pxr_head_norm pxr_head_norm; /* opaque, owned by the library */
+typedef struct {
+    uint32_t d_head, d_rotary;  /* d_rotary: even, at most d_head; 0 = no rotation */
+    const double* frequencies;  /* host [d_rotary/2], radians a position: finite; copied */
+    float eps;
+} pxr_head_norm_desc;
+
+/* Host only; one small allocation and upload.  Errors: INVALID_ARG (null, d_head == 0, d_rotary odd or above d_head, a frequency that
+ * is not finite or above 2^20, eps negative or not finite); UNSUPPORTED (d_head above 256); OOM; DEVICE. */
+int pxr_head_norm_create(const pxr_head_norm_desc* desc, pxr_head_norm** out);
+/* Free a layer; NULL accepted; synchronise streams still using it first. */
+int pxr_head_norm_destroy(pxr_head_norm* n);
+
+/* What the layer reads.  Single steps are n_steps == 1. */
+typedef struct {
+    uint32_t dtype, param_dtype;     /* of the heads; of the weights: PXR_F32 or dtype */
+    uint32_t n_envs, n_steps;
+    uint32_t n_heads, n_key_heads;   /* either may be 0 */
+    pxr_tokens q, k;                 /* [n_envs,n_steps,n_heads,d_head], [n_envs,n_steps,n_key_heads,d_head] */
+    const void *d_q_weight, *d_k_weight; /* [d_head] or NULL = 1 */
+    const void* d_positions;         /* [n_envs,n_steps] signed integers of position_bits bits, or NULL: step t is at first + t */
+    uint32_t position_bits;          /* 32 or 64 */
+    int64_t positions_env, positions_step; /* strides, in positions */
+    int64_t first;
+} pxr_heads;
+
+/* The normalised and turned heads to q_out and k_out (NULL where there are no such heads), views of the layout of q and k; either may be its input
+ * itself with the same strides.  Sums of squares are fp32.  A head with a NaN or an infinity comes out with NaN in it, the other heads are not touched by it.
+ * One kernel.  Errors: INVALID_ARG (null, a type that is none, position_bits that is neither, n_envs * n_steps above 2^31-1, n_heads or n_key_heads above 65535, a
+ * buffer not aligned to its elements); DEVICE. */
+int pxr_head_norm_forward(pxr_head_norm* n, const pxr_heads* r, const pxr_tokens* q_out, const pxr_tokens* k_out, void* hip_stream);
+
+/* Bytes of workspace that the backward pass needs where it forms a weight's gradient (host only).  Errors: as above (buffers are not looked at). */
+int pxr_head_norm_workspace(const pxr_head_norm* n, const pxr_heads* r, size_t* bytes);
+
+/* Gradients for those of the outputs, dq_out and dk_out: dq, dk, and the weights' d_dq_weight, d_dk_weight [d_head] of param_dtype, written (not
+ * added to), each NULL if not wanted; zeros where there are no such heads.  dq may be q or dq_out itself with the same strides, dk likewise.  Statistics and
+ * angles are computed again.  Equal inputs give equal bits.  d_workspace: 16-byte aligned, used until the call's kernels end.  Errors: as above, and INVALID_ARG
+ * (workspace missing, too small or misaligned). */
+int pxr_head_norm_backward(pxr_head_norm* n, const pxr_heads* r, const pxr_tokens* dq_out, const pxr_tokens* dk_out, const pxr_tokens* dq, const pxr_tokens* dk,
+                           void* d_dq_weight, void* d_dk_weight, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Scene facts for callers and tests (sizes of what pxr_create_scene built; no passage of the paper): total
  * template vertices and triangles, dynamic LDS bytes per frame workgroup, threads per workgroup.  Any out

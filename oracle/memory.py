@@ -1,6 +1,6 @@
 """Plain float64 definitions of a policy's memory: layer norm, linear attention with a decay for each head and a gated recurrence,
-forward and backward, one step after the other.  Pinned by closed forms and by differences in tests/test_oracle_memory.py
-and tests/test_oracle_recurrence.py."""
+norms and rotation of heads, forward and backward, one step after the other.  Pinned by closed forms and by differences in tests/test_oracle_memory.py,
+tests/test_oracle_recurrence.py and tests/test_oracle_head_norm.py."""
 import numpy as np
 
 
@@ -98,3 +98,32 @@ def gated_recurrence_backward(dout, x, gate, resets=None, state=None, dstate=Non
         dgate[:, t] = r * a[:, t] * rest[:, t] * (before - (x[:, t] if coupled else 0.0))
         r = np.where(cut[:, None], 0.0, r * a[:, t])
     return dx, dgate, r
+
+
+def _turn(y, positions, frequencies, back=False):
+    """The pairs (i, i + r/2) of y [B,T,H,d], r = 2 len(frequencies), turned by positions [B,T] times the frequencies."""
+    f = np.asarray(frequencies, np.float64)
+    n = len(f)
+    angle = (np.asarray(positions, np.float64)[:, :, None] * f)[:, :, None]
+    c, s = np.cos(angle), np.sin(-angle if back else angle)
+    out = np.array(y, np.float64)
+    out[..., :n] = y[..., :n] * c - y[..., n:2 * n] * s
+    out[..., n:2 * n] = y[..., n:2 * n] * c + y[..., :n] * s
+    return out
+
+
+def head_norm(x, weight, positions, frequencies, eps=1e-6):
+    """x [B,T,H,d], weight [d] or None, positions [B,T], frequencies [r/2] -> y."""
+    x = np.asarray(x, np.float64)
+    y = x / np.sqrt((x ** 2).mean(-1, keepdims=True) + eps) * (1.0 if weight is None else np.asarray(weight, np.float64))
+    return _turn(y, positions, frequencies)
+
+
+def head_norm_backward(dy, x, weight, positions, frequencies, eps=1e-6):
+    """-> (dx, dweight)."""
+    x = np.asarray(x, np.float64)
+    g = _turn(np.asarray(dy, np.float64), positions, frequencies, back=True)
+    rstd = 1 / np.sqrt((x ** 2).mean(-1, keepdims=True) + eps)
+    gw = g * (1.0 if weight is None else np.asarray(weight, np.float64))
+    dx = rstd * (gw - x * rstd ** 2 * (gw * x).mean(-1, keepdims=True))
+    return dx, (g * x * rstd).sum((0, 1, 2))

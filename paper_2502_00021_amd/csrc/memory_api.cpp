@@ -1,15 +1,20 @@
-// C ABI of a policy's memory (pxr_layer_norm_*, pxr_linear_attention_*, pxr_gated_recurrence_* in include/pxr.h): validation, the
-// layers' constants, launch.
+// C ABI of a policy's memory (pxr_layer_norm_*, pxr_linear_attention_*, pxr_gated_recurrence_*, pxr_head_norm_* in include/pxr.h):
+// validation, the layers' constants, launch.
 
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <initializer_list>
 #include <new>
 
 #include "pxr_internal.h"
 
 struct pxr_linear_attention {
     pxr::LinearAttentionConsts c{};
+};
+
+struct pxr_head_norm {
+    pxr::HeadNormConsts c{};
 };
 
 namespace {
@@ -66,6 +71,29 @@ const char* wrong_gated(const pxr_gated_rollout* r, bool step) {
 }
 
 bool wrong_view(const pxr_steps* t, uint32_t dtype, uint32_t n_steps) { return !t || (n_steps && !t->data) || !aligned(t->data, element(dtype)); }
+
+// Everything but the buffers.
+const char* wrong_heads(const pxr_head_norm* n, const pxr_heads* r) {
+    if (!n || !r) return "null argument";
+    if (r->dtype > PXR_BF16 || (r->param_dtype != PXR_F32 && r->param_dtype != r->dtype)) return "dtype must be fp32 or bfloat16, param_dtype fp32 or dtype";
+    if (r->position_bits != 32u && r->position_bits != 64u) return "position_bits must be 32 or 64";
+    if ((uint64_t)r->n_envs * r->n_steps > 0x7FFFFFFFull) return "n_envs * n_steps must be below 2^31";
+    if (r->n_heads > 65535u || r->n_key_heads > 65535u) return "n_heads and n_key_heads must be at most 65535";
+    return nullptr;
+}
+
+// The buffers that all passes read, and views of the queries' and of the keys' layout.
+bool wrong_head_buffers(const pxr_heads* r, std::initializer_list<const pxr_tokens*> of_q, std::initializer_list<const pxr_tokens*> of_k) {
+    const uint32_t tokens = r->n_envs && r->n_steps;
+    if (r->n_heads)
+        for (const pxr_tokens* t : of_q)
+            if (wrong_view(t, r->dtype, tokens)) return true;
+    if (r->n_key_heads)
+        for (const pxr_tokens* t : of_k)
+            if (wrong_view(t, r->dtype, tokens)) return true;
+    const size_t p = element(r->param_dtype);
+    return !aligned(r->d_q_weight, p) || !aligned(r->d_k_weight, p) || !aligned(r->d_positions, r->position_bits / 8u);
+}
 
 int finish(int rc, const char* call, const std::string& err) {
     return rc == PXR_OK ? PXR_OK : pxr::set_error(rc, std::string(call) + ": " + err);
@@ -261,6 +289,75 @@ int pxr_gated_recurrence_step(const pxr_gated_rollout* r, float* d_state, const 
     return finish(pxr::launch_gated_recurrence_step(*r, d_state, *out, hip_stream, err), call, err);
 }
 
+int pxr_head_norm_create(const pxr_head_norm_desc* d, pxr_head_norm** out) {
+    using pxr::set_error;
+    const char* call = "pxr_head_norm_create";
+    if (!d || !out || (d->d_rotary && !d->frequencies)) return refuse(call, "null argument");
+    if (d->d_head == 0 || d->d_rotary % 2u || d->d_rotary > d->d_head) return refuse(call, "d_head must be positive, d_rotary even and at most d_head");
+    if (d->d_head > 256u) return set_error(PXR_ERR_UNSUPPORTED, std::string(call) + ": d_head must be at most 256");
+    if (!(d->eps >= 0.0f) || !std::isfinite(d->eps)) return refuse(call, "eps must be finite and not negative");
+    uint64_t turns[128] = {};
+    for (uint32_t i = 0; i < d->d_rotary / 2u; ++i) {
+        if (!(std::fabs(d->frequencies[i]) <= 1048576.0)) return refuse(call, "a frequency is not finite or above 2^20");
+        turns[i] = pxr::turns_of(d->frequencies[i]);
+    }
+    pxr_head_norm* n = new (std::nothrow) pxr_head_norm();
+    if (!n) return set_error(PXR_ERR_OOM, std::string(call) + ": host allocation failed");
+    void* table = nullptr;
+    hipError_t rc = hipMalloc(&table, sizeof(turns));
+    const bool oom = rc == hipErrorOutOfMemory;
+    if (rc == hipSuccess) rc = hipMemcpy(table, turns, sizeof(turns), hipMemcpyHostToDevice);
+    if (rc != hipSuccess) {
+        (void)hipFree(table);
+        delete n;
+        return set_error(oom ? PXR_ERR_OOM : PXR_ERR_DEVICE, std::string(call) + ": " + hipGetErrorString(rc));
+    }
+    n->c.d = d->d_head;
+    n->c.r = d->d_rotary;
+    n->c.eps = d->eps;
+    n->c.turns = static_cast<const uint64_t*>(table);
+    *out = n;
+    return PXR_OK;
+}
+
+int pxr_head_norm_destroy(pxr_head_norm* n) {
+    if (!n) return PXR_OK;
+    const hipError_t rc = hipFree(const_cast<uint64_t*>(n->c.turns));
+    delete n;
+    if (rc != hipSuccess) return pxr::set_error(PXR_ERR_DEVICE, std::string("pxr_head_norm_destroy: hipFree failed: ") + hipGetErrorString(rc));
+    return PXR_OK;
+}
+
+int pxr_head_norm_forward(pxr_head_norm* n, const pxr_heads* r, const pxr_tokens* q_out, const pxr_tokens* k_out, void* hip_stream) {
+    const char* call = "pxr_head_norm_forward";
+    if (const char* why = wrong_heads(n, r)) return refuse(call, why);
+    if (wrong_head_buffers(r, {&r->q, q_out}, {&r->k, k_out})) return refuse(call, "a buffer is null or not aligned to its elements");
+    std::string err;
+    return finish(pxr::launch_head_norm_forward(n->c, *r, q_out, k_out, hip_stream, err), call, err);
+}
+
+int pxr_head_norm_workspace(const pxr_head_norm* n, const pxr_heads* r, size_t* bytes) {
+    const char* call = "pxr_head_norm_workspace";
+    if (const char* why = wrong_heads(n, r)) return refuse(call, why);
+    if (!bytes) return refuse(call, "null argument");
+    *bytes = pxr::head_norm_workspace(n->c, *r);
+    return PXR_OK;
+}
+
+int pxr_head_norm_backward(pxr_head_norm* n, const pxr_heads* r, const pxr_tokens* dq_out, const pxr_tokens* dk_out, const pxr_tokens* dq, const pxr_tokens* dk,
+                           void* d_dq_weight, void* d_dk_weight, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    const char* call = "pxr_head_norm_backward";
+    if (const char* why = wrong_heads(n, r)) return refuse(call, why);
+    const size_t p = element(r->param_dtype);
+    if (wrong_head_buffers(r, {&r->q, dq_out, dq}, {&r->k, dk_out, dk}) || !aligned(d_dq_weight, p) || !aligned(d_dk_weight, p))
+        return refuse(call, "a buffer is null or not aligned to its elements");
+    const size_t need = d_dq_weight || d_dk_weight ? pxr::head_norm_workspace(n->c, *r) : 0;
+    if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
+        return refuse(call, "the workspace is missing, too small or not 16-byte aligned");
+    std::string err;
+    return finish(pxr::launch_head_norm_backward(n->c, *r, dq_out, dk_out, dq, dk, d_dq_weight, d_dk_weight, d_workspace, hip_stream, err), call, err);
+}
+
 }  // extern "C"
 
 void pxr::fill_head(LinearAttentionHead& h, float log_decay) {
@@ -272,4 +369,12 @@ void pxr::fill_head(LinearAttentionHead& h, float log_decay) {
     split(std::exp((double)log_decay), h.decay, h.decay_rest);
     split(std::exp((double)log_decay * 32.0), h.decay_chunk, h.decay_chunk_rest);
     for (int n = 0; n <= 32; ++n) h.power[n] = (float)std::exp((double)log_decay * n);
+}
+
+// frequency / 2 pi as a fraction of 2^64, modulo whole turns.
+uint64_t pxr::turns_of(double frequency) {
+    const long double turns = (long double)frequency / 6.283185307179586476925286766559005768L;
+    const long double part = turns - std::floor(turns);  // in [0, 1]
+    const long double scaled = part * 18446744073709551616.0L;
+    return scaled >= 18446744073709551616.0L ? 0u : (uint64_t)scaled;
 }

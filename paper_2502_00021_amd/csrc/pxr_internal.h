@@ -261,6 +261,20 @@ int launch_gated_recurrence_backward(const pxr_gated_rollout& r, const pxr_steps
                                      const pxr_steps& dgate, float* dstate, void* ws, void* stream, std::string& err);
 int launch_gated_recurrence_step(const pxr_gated_rollout& r, float* state, const pxr_steps& out, void* stream, std::string& err);
 
+struct HeadNormConsts {
+    uint32_t d, r;  // values of a head, and how many of them are turned
+    float eps;
+    const uint64_t* turns;  // [r / 2] on the device: turns per position, in fractions of 2^64
+};
+
+uint64_t turns_of(double frequency);  // memory_api.cpp
+
+// head_norm.hip (arguments as checked by memory_api.cpp)
+size_t head_norm_workspace(const HeadNormConsts& c, const pxr_heads& r);
+int launch_head_norm_forward(const HeadNormConsts& c, const pxr_heads& r, const pxr_tokens* q_out, const pxr_tokens* k_out, void* stream, std::string& err);
+int launch_head_norm_backward(const HeadNormConsts& c, const pxr_heads& r, const pxr_tokens* dq_out, const pxr_tokens* dk_out, const pxr_tokens* dq,
+                              const pxr_tokens* dk, void* dq_weight, void* dk_weight, void* ws, void* stream, std::string& err);
+
 // pipeline.cpp works through these (api.cpp / conv_api.cpp own the handles' layouts).
 constexpr uint32_t kMaxPipelineChunks = 16;
 void scene_shape(const pxr_scene* s, uint32_t* K, uint32_t* H, uint32_t* W);

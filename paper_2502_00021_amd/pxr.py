@@ -3,7 +3,8 @@
 Mirrors include/pxr.h one to one: create_scene / destroy_scene /
 apply_distractor / render_batch, set_skeleton / pose_batch /
 render_batch_kinematic (+ scene_info, set_block_threads, host_tables), the policy's first layer (Conv) and its memory
-(layer_norm, layer_norm_backward, LinearAttention, gated_recurrence).  PyTorch is used only to hold device memory and name the stream.
+(layer_norm, layer_norm_backward, LinearAttention, gated_recurrence, HeadNorm).
+PyTorch is used only to hold device memory and name the stream.
 There is no fallback: a missing library or a failing call raises.
 """
 import ctypes as C
@@ -95,10 +96,22 @@ class GatedRollout(C.Structure):
                 ("d_resets", C.c_void_p), ("resets_env", C.c_int64), ("resets_step", C.c_int64), ("d_state", C.c_void_p)]
 
 
+class HeadNormDesc(C.Structure):
+    _fields_ = [("d_head", C.c_uint32), ("d_rotary", C.c_uint32), ("frequencies", C.c_void_p), ("eps", C.c_float)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("param_dtype", C.c_uint32), ("n_envs", C.c_uint32), ("n_steps", C.c_uint32),
+                ("n_heads", C.c_uint32), ("n_key_heads", C.c_uint32), ("q", Tokens), ("k", Tokens),
+                ("d_q_weight", C.c_void_p), ("d_k_weight", C.c_void_p), ("d_positions", C.c_void_p), ("position_bits", C.c_uint32),
+                ("positions_env", C.c_int64), ("positions_step", C.c_int64), ("first", C.c_int64)]
+
+
 # Calls' structures as bytes: a call packs its arguments in a fraction of the time that it takes to fill the structures.
 _pack_norm = struct.Struct("@IIQIfqqq").pack
 _pack_tokens = struct.Struct("@Pqqq").pack
 _pack_rollout = struct.Struct("@III4xPqqqPqqqPqqqPqqP").pack
+_pack_heads = struct.Struct("@IIIIIIPqqqPqqqPPPI4xqqq").pack
 _pack_steps = struct.Struct("@Pqq").pack
 _pack_gated = struct.Struct("@IIIII4xPqqPqqPqqP").pack
 
@@ -181,6 +194,14 @@ def lib():
         L.pxr_gated_recurrence_step.argtypes = [rollout, vp, steps, vp]
         for name in ("workspace", "forward", "backward", "step"):
             getattr(L, "pxr_gated_recurrence_" + name).restype = C.c_int
+        heads = vp
+        L.pxr_head_norm_create.argtypes = [C.POINTER(HeadNormDesc), C.POINTER(vp)]
+        L.pxr_head_norm_destroy.argtypes = [vp]
+        L.pxr_head_norm_forward.argtypes = [vp, heads, tokens, tokens, vp]
+        L.pxr_head_norm_workspace.argtypes = [vp, heads, size]
+        L.pxr_head_norm_backward.argtypes = [vp, heads, tokens, tokens, tokens, tokens, vp, vp, vp, C.c_size_t, vp]
+        for name in ("create", "destroy", "forward", "workspace", "backward"):
+            getattr(L, "pxr_head_norm_" + name).restype = C.c_int
         L.pxr_selftest_arithmetic.argtypes = [vp]
         L.pxr_selftest_arithmetic.restype = C.c_int
         L.pxr_measure_peaks.argtypes = [vp, vp, vp, vp, vp]
@@ -810,6 +831,114 @@ class LinearAttention:
                                               _stream_handle(stream, q)))
         _written(torch, *given)
         return out
+
+
+class HeadNorm:
+    """Owns one pxr_head_norm handle: each head of queries and keys is divided by its root mean square, multiplied by a weight, and
+    the pairs (i, i + d_rotary / 2) of its first d_rotary values are turned by position * frequencies[i]."""
+
+    def __init__(self, d_head, d_rotary=None, frequencies=None, base=10000.0, eps=1e-6):
+        """d_rotary: even, all of d_head (or all but one) unless given, 0 = no rotation; frequencies: d_rotary / 2 radians a position,
+        base ** (-2 i / d_rotary) unless given."""
+        d_head = int(d_head)
+        d_rotary = d_head // 2 * 2 if d_rotary is None else int(d_rotary)
+        if frequencies is None:
+            frequencies = [float(base) ** (-2 * i / d_rotary) for i in range(d_rotary // 2)]
+        f = np.ascontiguousarray(frequencies, dtype=np.float64)
+        assert f.shape == (d_rotary // 2,), f.shape
+        d = HeadNormDesc(d_head, d_rotary, f.ctypes.data, float(eps))
+        h = C.c_void_p()
+        _check(lib().pxr_head_norm_create(C.byref(d), C.byref(h)))
+        self._h = h
+        self._asked = (None, 0)
+        self.d, self.rotary, self.eps = d_head, d_rotary, d.eps
+
+    def close(self):
+        if getattr(self, "_h", None):
+            _check(lib().pxr_head_norm_destroy(self._h))
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _view(self, x, like):
+        """The fields of pxr_tokens for a tensor of `like`'s shape and type, [B, T, H, d] or (one step) [B, H, d]."""
+        assert x.is_cuda and x.dtype == like.dtype and x.shape == like.shape, (tuple(x.shape), tuple(like.shape), x.dtype)
+        s = x.stride()
+        assert s[-1] == 1 or x.shape[-1] == 1 or x.numel() == 0, "a head's values must be adjacent"
+        return (x.data_ptr(), s[0], s[1], s[2]) if len(s) == 4 else (x.data_ptr(), s[0], 0, s[1])
+
+    def _heads(self, torch, q, k, q_weight, k_weight, positions, first):
+        """The bytes of pxr_heads, and the weights' type."""
+        some = q if q is not None else k
+        assert some is not None and some.dim() in (3, 4) and some.shape[-1] == self.d, "queries or keys [B, T, heads, d] or [B, heads, d]"
+        lead = some.shape[:-2]
+        B, T = lead if len(lead) == 2 else (lead[0], 1)
+        counts, views = [], []
+        for x in (q, k):
+            if x is None:
+                counts.append(0)
+                views += (0, 0, 0, 0)
+                continue
+            assert x.shape[:-2] == lead and x.shape[-1] == self.d and x.dtype == some.dtype, (tuple(x.shape), tuple(some.shape))
+            counts.append(x.shape[-2])
+            views += self._view(x, x)
+        params = _params(torch, some, self.d, q_weight, k_weight)
+        bits, at = 32, (0, 0, 0)
+        if positions is not None:
+            assert positions.is_cuda and positions.dtype in (torch.int32, torch.int64) and positions.shape == lead, tuple(positions.shape)
+            assert first == 0, "positions say where every step is"
+            s = positions.stride()
+            at, bits = (positions.data_ptr(), s[0], s[1] if len(s) == 2 else 0), 64 if positions.dtype == torch.int64 else 32
+        packed = _pack_heads(_dtype_code(torch, some.dtype), _dtype_code(torch, params), B, T, *counts, *views, _ptr(q_weight) or 0, _ptr(k_weight) or 0,
+                             at[0], bits, at[1], at[2], first)
+        return packed, params
+
+    def forward(self, q, k, q_weight=None, k_weight=None, positions=None, first=0, q_out=None, k_out=None, stream=None):
+        """q, k: CUDA float32 or bfloat16 [B,T,H,d] (or, one step, [B,H,d]; any strides, a head's values adjacent; the numbers of heads may
+        differ, either may be None); weights: [d], float32 or of their type, or None; positions: int32 or int64 [B,T] (one step:
+        [B]), or None: step t is at first + t.  Returns (q, k) normalised and turned, in q_out and k_out if given (they may be
+        the inputs themselves); enqueue only."""
+        torch = _torch or _torch_module()
+        r, _ = self._heads(torch, q, k, q_weight, k_weight, positions, first)
+        given, outs = [t for t in (q_out, k_out) if t is not None], []
+        for x, out in ((q, q_out), (k, k_out)):
+            assert x is not None or out is None
+            outs.append(_empty(torch, x, stream, x.shape, x.dtype) if x is not None and out is None else out)
+        packed = [None if x is None else _pack_tokens(*self._view(o, x)) for x, o in zip((q, k), outs)]
+        _check((_lib or lib()).pxr_head_norm_forward(self._h, r, *packed, _stream_handle(stream, q if q is not None else k)))
+        if given:
+            _written(torch, *given)
+        return tuple(outs)
+
+    def backward(self, dq, dk, q, k, q_weight=None, k_weight=None, positions=None, first=0, params_dtype=None, stream=None):
+        """Gradients for dq and dk (of the outputs) of a forward call with these inputs.  Returns (of q, of k, of q_weight, of k_weight), the latter two [d] of the
+        weights' type (without weights: params_dtype, float32 unless given); None in the place of what is of no heads; enqueue only."""
+        torch = _torch or _torch_module()
+        r, params = self._heads(torch, q, k, q_weight, k_weight, positions, first)
+        some = q if q is not None else k
+        if q_weight is None and k_weight is None and params_dtype is not None:
+            assert params_dtype in (torch.float32, some.dtype)
+            params = params_dtype
+            r = r[:4] + struct.pack("@I", _dtype_code(torch, params)) + r[8:]
+        grads = [None if x is None else _empty(torch, x, stream, x.shape, x.dtype) for x in (q, k)]
+        sums = [None if x is None else _empty(torch, x, stream, (self.d,), params) for x in (q, k)]
+        given = [None if x is None else _pack_tokens(*self._view(d, x)) for x, d in zip((q, k), (dq, dk))]
+        into = [None if x is None else _pack_tokens(*self._view(g, x)) for x, g in zip((q, k), grads)]
+        L = _lib or lib()
+        sizes = r[:24]
+        asked, need = self._asked  # (the bytes for the sizes that were asked for last are known)
+        if asked != sizes:
+            n = C.c_size_t()
+            _check(L.pxr_head_norm_workspace(self._h, r, n))
+            need = n.value
+            self._asked = (sizes, need)
+        ws = _empty(torch, some, stream, (need,), torch.uint8) if need else None
+        _check(L.pxr_head_norm_backward(self._h, r, *given, *into, *(_ptr(s) for s in sums), _ptr(ws), need, _stream_handle(stream, some)))
+        return (*grads, *sums)
 
 
 def _steps_view(x, shape, dtype):
