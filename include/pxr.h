@@ -477,6 +477,33 @@ int pxr_head_norm_workspace(const pxr_head_norm* n, const pxr_heads* r, size_t* 
 int pxr_head_norm_backward(pxr_head_norm* n, const pxr_heads* r, const pxr_tokens* dq_out, const pxr_tokens* dk_out, const pxr_tokens* dq, const pxr_tokens* dk,
                            void* d_dq_weight, void* d_dk_weight, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- a learner's update with its singular values pushed towards one ----
+ * For what an optimiser is about to add to a weight matrix (a gradient, its momentum): every direction of the update counts alike.  Of a
+ * matrix x [rows,cols]; where it has more rows than columns, of its transpose:
+ *   X = x / (|x| + eps), |x| the Frobenius norm;   n_steps times  X <- a X + (b A + c A^2) X,  A = X X^T,  with (a, b, c) = coefficients of that step
+ * A singular value t goes through t <- a t + b t^3 + c t^5.  Several matrices of one size go together. */
+typedef struct {
+    uint32_t dtype;                 /* of x and of the result: PXR_F32 or PXR_BF16 */
+    uint32_t n_matrices, rows, cols;
+    int64_t x_matrix, x_row;        /* strides of x in elements; the values of a row are adjacent */
+    int64_t out_matrix, out_row;    /* of the result */
+    uint32_t n_steps;
+    const float* coefficients;      /* host [n_steps][3], read during the call */
+    float eps;
+} pxr_orthogonalise_desc;
+
+/* Bytes of workspace that pxr_orthogonalise needs for this description (host only).  Errors: as for the call (buffers are not looked at). */
+int pxr_orthogonalise_workspace(const pxr_orthogonalise_desc* d, size_t* bytes);
+
+/* The result in d_out, which may be d_x itself.  Products and sums keep 22 bits and more (fp32's, but for a few roundings of 2^-23); values below 2^-38 of the
+ * bound that the coefficients set for the singular values (1 before the first step) are zeros, so an update whose norm is far below eps comes out as zeros.  A matrix
+ * with a NaN or an infinity comes out as NaN, the others are not touched by it.  n_matrices == 0 is a call that does nothing.  Equal inputs give equal bits.
+ * d_workspace: 16-byte aligned, used until the call's kernels end.
+ * Errors: INVALID_ARG (null, rows or cols == 0, a type that is none, n_steps outside [1,64], a coefficient that is not finite, steps under which a
+ * singular value may pass 2^20 or grow by more than 10^12, eps negative or not finite, a row stride smaller than cols, matrices of the result that overlap, n_matrices above 65535, a buffer not
+ * aligned to its elements, workspace missing, too small or not 16-byte aligned); UNSUPPORTED (the smaller of rows and cols above 2^15, rows * cols above 2^32); DEVICE. */
+int pxr_orthogonalise(const pxr_orthogonalise_desc* d, const void* d_x, void* d_out, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Scene facts for callers and tests (sizes of what pxr_create_scene built; no passage of the paper): total
  * template vertices and triangles, dynamic LDS bytes per frame workgroup, threads per workgroup.  Any out
  * pointer may be NULL.  block_threads is that of launches which fill the device; smaller ones may take another.

@@ -1,0 +1,537 @@
+// A learner's update with its singular values pushed towards one (pxr_orthogonalise in include/pxr.h).  gfx950 only.
+//
+//   X_0 = x / (|x| + eps),  |x| the Frobenius norm;   X_{k+1} = a X_k + (b A + c A^2) X_k,  A = X_k X_k^T
+//
+// with X [s,l] the update or, where it has more rows than columns, its transpose: s <= l.  On a singular value t a step is the polynomial a t + b t^3 + c t^5.  Three products
+// a step, the first two symmetric (half of their tiles):
+//   A = X X^T,   B = a 1 + b A + c A A,   X <- B X
+//
+// All on the matrix cores, in fp16 operands and fp32 sums.  A value of X, A and B is held as two fp16 parts, the value rounded and what that left out, 22 bits and more
+// together, and a product is three: hi hi + hi lo + lo hi; lo lo is 2^-22 of it and left out.  fp16 has the bits that bfloat16 has not (two parts of it are 16 bits: an
+// update whose singular values lie far apart loses its small ones) and its range does not matter: a singular value of X_k, and so every value of X, A and B, has a
+// bound that follows from the coefficients alone, and each of the three is held times a power of two that puts that bound just below fp16's largest.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "pxr_internal.h"
+
+namespace pxr {
+namespace {
+
+typedef _Float16 half;
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr uint32_t kThreads = 256;
+constexpr uint32_t kPad = 128;       // rows and columns of the matrices in the workspace come in multiples of it; what is behind the matrix is zeros
+constexpr uint32_t kNormParts = 256; // of a matrix whose squares are summed, at most
+constexpr uint32_t kNormColumns = 1024;
+constexpr uint32_t kDepth = 32;      // values of the summed axis in LDS at a time
+
+__host__ __device__ constexpr uint32_t padded(uint32_t n) { return (n + kPad - 1u) / kPad * kPad; }
+
+// Two planes of fp16 parts of a batch of matrices in the workspace: [plane][matrix][rows][cols].
+struct Planes {
+    half* hi;
+    size_t plane, matrix;
+    uint32_t row;
+    __host__ __device__ half* at(uint32_t p, uint32_t m) const { return hi + p * plane + m * matrix; }
+};
+
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const __bf16* p) { return (float)*p; }
+
+struct Prepare {
+    const void* x;
+    int64_t x_matrix, x_row;
+    uint32_t rows, cols, parts;
+    double* sums;  // [matrices][parts]
+    Planes to;
+    float eps, scale;
+};
+
+// Squares in 64 bits: those of fp32 values neither overflow nor vanish.
+template <class T>
+__global__ __launch_bounds__(kThreads) void square_sums_kernel(const Prepare a) {
+    __shared__ double shared[kThreads / 64];
+    const uint32_t part = blockIdx.x, matrix = blockIdx.y;
+    const T* x = static_cast<const T*>(a.x) + (int64_t)matrix * a.x_matrix;
+    double sum = 0.0;
+    const uint32_t per_row = (a.cols + kNormColumns - 1u) / kNormColumns;
+    for (uint64_t u = part; u < (uint64_t)a.rows * per_row; u += a.parts) {
+        const uint32_t r = (uint32_t)(u / per_row), c0 = (uint32_t)(u - (uint64_t)r * per_row) * kNormColumns;
+        const T* row = x + (int64_t)r * a.x_row;
+        const uint32_t end = min(c0 + kNormColumns, a.cols);
+        for (uint32_t c = c0 + threadIdx.x; c < end; c += kThreads) {
+            const double v = (double)load1(row + c);
+            sum += v * v;
+        }
+    }
+#pragma unroll
+    for (uint32_t m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
+    if ((threadIdx.x & 63u) == 0) shared[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) a.sums[(size_t)matrix * a.parts + part] = shared[0] + shared[1] + shared[2] + shared[3];
+}
+
+__device__ __forceinline__ void split(float v, half& hi, half& lo) {
+    hi = (half)v;  // round to nearest even
+    lo = (half)(v - (float)hi);
+}
+
+// Divided by the norm and split, 64 x 64 values a workgroup, transposed where the update has more rows than columns.
+template <class T>
+__global__ __launch_bounds__(kThreads) void split_kernel(const Prepare a) {
+    __shared__ float tile[64][65];
+    __shared__ double total;
+    const uint32_t matrix = blockIdx.z;
+    double sum = 0.0;
+    if (threadIdx.x < 64u) {
+        for (uint32_t p = threadIdx.x; p < a.parts; p += 64u) sum += a.sums[(size_t)matrix * a.parts + p];
+#pragma unroll
+        for (uint32_t m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
+        if (threadIdx.x == 0) total = sum;
+    }
+    // the tile of the update: rows r0.., columns c0..
+    const bool tall = a.rows > a.cols;
+    const uint32_t r0 = (tall ? blockIdx.x : blockIdx.y) * 64u, c0 = (tall ? blockIdx.y : blockIdx.x) * 64u;
+    const T* x = static_cast<const T*>(a.x) + (int64_t)matrix * a.x_matrix;
+    for (uint32_t i = threadIdx.x; i < 64u * 64u; i += kThreads) {
+        const uint32_t r = i >> 6, c = i & 63u;
+        const float v = r0 + r < a.rows && c0 + c < a.cols ? load1(x + (int64_t)(r0 + r) * a.x_row + (c0 + c)) : 0.0f;
+        tile[tall ? c : r][tall ? r : c] = v;
+    }
+    __syncthreads();
+    const double over = (double)a.scale / (sqrt(total) + (double)a.eps);
+    half *hi = a.to.at(0, matrix), *lo = a.to.at(1, matrix);
+    for (uint32_t i = threadIdx.x; i < 64u * 8u; i += kThreads) {
+        const uint32_t r = i >> 3, c = (i & 7u) * 8u;
+        f16x8 h, l;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            half p, q;
+            split((float)((double)tile[r][c + e] * over), p, q);
+            h[e] = p;
+            l[e] = q;
+        }
+        const size_t at = (size_t)(blockIdx.y * 64u + r) * a.to.row + blockIdx.x * 64u + c;
+        *reinterpret_cast<f16x8*>(hi + at) = h;
+        *reinterpret_cast<f16x8*>(lo + at) = l;
+    }
+}
+
+// ---- products
+
+enum { kGram, kPoly, kUpdate, kLast };
+
+struct Product {
+    Planes a, b, to;     // kGram: X, X -> A;  kPoly: A, A -> B;  kUpdate: B, X -> X;  kLast: B, X -> out
+    uint32_t depth;      // the summed axis, a multiple of kDepth
+    uint32_t tiles_i, tiles_j, splits, steps_each;  // steps of kDepth that a split takes
+    float* partial;      // [matrices][splits][tiles][tile][tile], splits > 1
+    float scale;         // of the sums
+    float c0, c1;        // kPoly: on the diagonal; times A's held values
+    uint32_t s;          // rows with a diagonal
+    void* out;
+    int64_t out_matrix, out_row;
+    uint32_t rows, cols, transposed, bf16;
+};
+
+// Tiles of a symmetric product: those of its lower triangle, row by row.
+__device__ __forceinline__ void triangle(uint32_t t, uint32_t& i, uint32_t& j) {
+    i = (uint32_t)((__builtin_sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+    while (i * (i + 1u) / 2u > t) --i;
+    while ((i + 1u) * (i + 2u) / 2u <= t) ++i;
+    j = t - i * (i + 1u) / 2u;
+}
+
+// A tile's operand in LDS, one plane, kDepth values deep.  Along: rows of 64 bytes, 4 chunks of 8 values, chunk c of row r at place c ^ (r / 2 % 4): eight rows' chunks of one c lie in different banks.
+// Across (the summed axis is the rows'): rows of `kSide` values, chunk c of row k at place c ^ 2 (k % 4): four rows' pairs of chunks, as the transposing read takes them, lie in different
+// banks.  The requests that write LDS put a wavefront's lanes side by side, so it is the addresses that they ask for which are exchanged.
+template <int kSide, bool kAcross>
+struct Operand {
+    static constexpr uint32_t kChunks = kSide * kDepth / 8;  // of 16 bytes, in a plane
+    // Which value chunk number i of the plane is: row and column in the tile.
+    static __device__ __forceinline__ void place(uint32_t i, uint32_t& row, uint32_t& col) {
+        if (kAcross) {
+            row = i / (kSide / 8);
+            col = ((i % (kSide / 8)) ^ ((row & 3u) << 1)) * 8u;
+        } else {
+            row = i / 4u;
+            col = ((i % 4u) ^ (row >> 1 & 3u)) * 8u;
+        }
+    }
+    // Eight values of the summed axis, 16 k + 8 h .. + 7, of line lane % 32 from `line` on.
+    static __device__ __forceinline__ f16x8 fragment(const half* plane, uint32_t line, uint32_t k, uint32_t lane) {
+        const uint32_t h = lane >> 5;
+        if constexpr (kAcross) {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const uint32_t i = lane & 15u, row = 16u * k + 8u * h + (i >> 2), col = line + (lane & 16u) + 4u * (i & 3u);
+            const half* p = plane + row * kSide + (((col >> 3) ^ ((row & 3u) << 1)) << 3) + (col & 7u);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * kSide));
+            return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const uint32_t row = line + (lane & 31u);
+            return *reinterpret_cast<const f16x8*>(plane + row * kDepth + (((2u * k + h) ^ (row >> 1 & 3u)) << 3));
+        }
+    }
+};
+
+// Four values of a row leave: to the planes, or as the update's own (row and column of X, which has rows of the update's shorter side).
+template <bool kPolynomial>
+__device__ __forceinline__ void put_planes(const Product& p, const half* ah, const half* al, half* th, half* tl, uint32_t row, uint32_t col, f32x4 v) {
+    if constexpr (kPolynomial) {
+        const f16x4 hi = *reinterpret_cast<const f16x4*>(ah + (size_t)row * p.a.row + col), lo = *reinterpret_cast<const f16x4*>(al + (size_t)row * p.a.row + col);
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) v[e] = __builtin_fmaf((float)hi[e] + (float)lo[e], p.c1, v[e]) + (row == col + e && row < p.s ? p.c0 : 0.0f);
+    }
+    f16x4 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        half h, l;
+        split(v[e], h, l);
+        hi[e] = h;
+        lo[e] = l;
+    }
+    *reinterpret_cast<f16x4*>(th + (size_t)row * p.to.row + col) = hi;
+    *reinterpret_cast<f16x4*>(tl + (size_t)row * p.to.row + col) = lo;
+}
+
+template <class T>
+__device__ __forceinline__ void put_values(T* to, f32x4 v, uint32_t n) {
+    T w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = (T)v[e];  // round to nearest even
+    if (n >= 4u) {
+        __builtin_memcpy(to, w, sizeof(w));  // (at the address of any value)
+        return;
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 3; ++e)
+        if (e < n) to[e] = w[e];
+}
+
+// `row`, `col`: of the update itself.
+__device__ __forceinline__ void put_out(const Product& p, uint32_t matrix, uint32_t row, uint32_t col, f32x4 v) {
+    if (row >= p.rows || col >= p.cols) return;
+    const int64_t at = (int64_t)matrix * p.out_matrix + (int64_t)row * p.out_row + col;
+    if (p.bf16)
+        put_values(static_cast<__bf16*>(p.out) + at, v, p.cols - col);
+    else
+        put_values(static_cast<float*>(p.out) + at, v, p.cols - col);
+}
+
+// A tile of 64 M x 64 M values by four wavefronts, 2 x 2, each 32 M x 32 M.
+template <int kKind, int M>
+__global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
+    constexpr int kSide = 64 * M;
+    constexpr bool kSym = kKind <= kPoly;
+    typedef Operand<kSide, false> OpA;
+    typedef Operand<kSide, !kSym> OpB;
+    constexpr uint32_t kPlane = kSide * kDepth, kStage = 4 * kPlane;  // halves: A hi, A lo, B hi, B lo
+    __shared__ __align__(16) half stage[2][kStage];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.z;
+    uint32_t ti, tj;
+    const uint32_t tile = blockIdx.x, part = blockIdx.y;
+    if (kSym)
+        triangle(tile, ti, tj);
+    else {
+        ti = tile % p.tiles_i;
+        tj = tile / p.tiles_i;
+    }
+    const uint32_t i0 = ti * kSide, j0 = tj * kSide;
+    // each wavefront asks for every fourth run of 64 chunks of each plane
+    constexpr uint32_t kRuns = OpA::kChunks / 64 / 4;
+    const half *a_from[kRuns], *b_from[kRuns];
+    const uint32_t k_first = part * p.steps_each * kDepth;
+#pragma unroll
+    for (uint32_t n = 0; n < kRuns; ++n) {
+        uint32_t row, col;
+        OpA::place((n * 4u + wave) * 64u + lane, row, col);
+        a_from[n] = p.a.at(0, matrix) + (size_t)(i0 + row) * p.a.row + k_first + col;
+        OpB::place((n * 4u + wave) * 64u + lane, row, col);
+        b_from[n] = p.b.at(0, matrix) + (kSym ? (size_t)(j0 + row) * p.b.row + k_first + col : (size_t)(k_first + row) * p.b.row + j0 + col);
+    }
+    const size_t b_step = kSym ? kDepth : (size_t)kDepth * p.b.row;
+    const auto ask = [&](half* to) {
+        typedef const __attribute__((address_space(1))) void* global;
+        typedef __attribute__((address_space(3))) void* shared;
+#pragma unroll
+        for (uint32_t n = 0; n < kRuns; ++n)
+#pragma unroll
+            for (uint32_t plane = 0; plane < 2; ++plane) {
+                __builtin_amdgcn_global_load_lds((global)(a_from[n] + plane * p.a.plane), (shared)(to + plane * kPlane + (n * 4u + wave) * 512u), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((global)(b_from[n] + plane * p.b.plane), (shared)(to + (2 + plane) * kPlane + (n * 4u + wave) * 512u), 16, 0, 0);
+            }
+#pragma unroll
+        for (uint32_t n = 0; n < kRuns; ++n) {
+            a_from[n] += kDepth;
+            b_from[n] += b_step;
+        }
+    };
+    f32x16 acc[M][M];
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int j = 0; j < M; ++j) acc[i][j] = (f32x16)0.0f;
+    const uint32_t row0 = (wave >> 1) * 32 * M, col0 = (wave & 1u) * 32 * M;
+    const uint32_t steps = min(p.steps_each, p.depth / kDepth - part * p.steps_each);
+    ask(stage[0]);
+    for (uint32_t k = 0; k < steps; ++k) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (k + 1u < steps) ask(stage[(k + 1u) & 1u]);
+        const half* from = stage[k & 1u];
+#pragma unroll
+        for (uint32_t kk = 0; kk < kDepth / 16; ++kk) {
+            f16x8 a[M][2], b[M][2];
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+#pragma unroll
+                for (uint32_t plane = 0; plane < 2; ++plane) {
+                    a[i][plane] = OpA::fragment(from + plane * kPlane, row0 + 32 * i, kk, lane);
+                    b[i][plane] = OpB::fragment(from + (2 + plane) * kPlane, col0 + 32 * i, kk, lane);
+                }
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+#pragma unroll
+                for (int j = 0; j < M; ++j) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][1], b[j][0], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][1], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][0], acc[i][j], 0, 0, 0);
+                }
+        }
+    }
+    // a lane has column lane % 32 and rows 8 (r / 4) + 4 (lane / 32) + r % 4 of every 32 x 32
+    const uint32_t down = 4u * (lane >> 5), across = lane & 31u;
+    if (kSym && p.splits > 1u) {
+        const uint32_t tiles = p.tiles_i * (p.tiles_i + 1u) / 2u;
+        float* to = p.partial + (((size_t)matrix * p.splits + part) * tiles + tile) * (kSide * kSide);
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+#pragma unroll
+            for (int j = 0; j < M; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    to[(row0 + 32 * i + 8 * (r >> 2) + down + (r & 3)) * kSide + col0 + 32 * j + across] = acc[i][j][r];
+        return;
+    }
+    // Through LDS, 64 rows of the tile at a time, so that rows leave in whole lines; of a symmetric product the mirrored tile too.
+    float* const pass = reinterpret_cast<float*>(&stage[0][0]);
+    const half *ah = p.a.at(0, matrix), *al = p.a.at(1, matrix);
+    half *th = p.to.at(0, matrix), *tl = p.to.at(1, matrix);
+    const auto leave = [&](auto turned, uint32_t part64) {
+        constexpr bool kTurned = decltype(turned)::value;
+        constexpr uint32_t kRow = kTurned ? 64u + 4u : kSide + 4u, kRows = kTurned ? kSide : 64u, kQuads = (kTurned ? 64u : kSide) / 4u;
+        __syncthreads();
+        if (M == 1 || wave >> 1 == part64) {
+            const uint32_t row_in = M == 1 ? row0 : 0u;
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+#pragma unroll
+                for (int j = 0; j < M; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t row = row_in + 32 * i + 8 * q + down, col = col0 + 32 * j + across;
+                        if constexpr (kTurned) {
+                            *reinterpret_cast<f32x4*>(pass + col * kRow + row) = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) pass[(row + r) * kRow + col] = acc[i][j][4 * q + r];
+                        }
+                    }
+        }
+        __syncthreads();
+        for (uint32_t n = threadIdx.x; n < kRows * kQuads; n += kThreads) {
+            const uint32_t r = n / kQuads, c = n % kQuads * 4u;
+            const f32x4 v = *reinterpret_cast<const f32x4*>(pass + r * kRow + c) * p.scale;
+            const uint32_t row = kTurned ? j0 + r : i0 + part64 * 64u + r, col = kTurned ? i0 + part64 * 64u + c : j0 + c;
+            if constexpr (kKind == kLast)
+                put_out(p, matrix, row, col, v);
+            else
+                put_planes<kKind == kPoly>(p, ah, al, th, tl, row, col, v);
+        }
+    };
+#pragma unroll
+    for (uint32_t part64 = 0; part64 < M; ++part64) {
+        if (kKind != kLast || !p.transposed) leave(std::false_type{}, part64);
+        if (kKind == kLast ? p.transposed : kSym && ti != tj) leave(std::true_type{}, part64);
+    }
+}
+
+// A symmetric product whose summed axis was cut: the parts' sums in their order, 16 rows of a tile a workgroup.
+template <int kKind>
+__global__ __launch_bounds__(kThreads) void join_kernel(const Product p) {
+    __shared__ float turned[64][17];
+    const uint32_t tile = blockIdx.x / 4u, strip = blockIdx.x % 4u, matrix = blockIdx.z, tiles = p.tiles_i * (p.tiles_i + 1u) / 2u;
+    uint32_t ti, tj;
+    triangle(tile, ti, tj);
+    const uint32_t r = threadIdx.x >> 4, c = (threadIdx.x & 15u) * 4u;
+    const float* from = p.partial + ((size_t)matrix * p.splits * tiles + tile) * 4096u + (strip * 16u + r) * 64u + c;
+    f32x4 v = (f32x4)0.0f;
+#pragma unroll 8
+    for (uint32_t s = 0; s < p.splits; ++s) v += *reinterpret_cast<const f32x4*>(from + (size_t)s * tiles * 4096u);
+    v *= p.scale;
+    const half *ah = p.a.at(0, matrix), *al = p.a.at(1, matrix);
+    half *th = p.to.at(0, matrix), *tl = p.to.at(1, matrix);
+    const uint32_t row0 = ti * 64u + strip * 16u;
+    put_planes<kKind == kPoly>(p, ah, al, th, tl, row0 + r, tj * 64u + c, v);
+    if (ti == tj) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) turned[c + e][r] = v[e];
+    __syncthreads();
+    const uint32_t row = threadIdx.x >> 2, col = (threadIdx.x & 3u) * 4u;
+    const f32x4 w{turned[row][col], turned[row][col + 1], turned[row][col + 2], turned[row][col + 3]};
+    put_planes<kKind == kPoly>(p, ah, al, th, tl, tj * 64u + row, row0 + col, w);
+}
+
+float power_below(double v) { return (float)std::exp2(std::floor(std::log2(v))); }
+
+// Bounds of the singular values, and the powers of two by which X, A and B are held: 2 less than half of fp16's largest number, so that no rounding reaches it.
+constexpr double kMost = 30000.0, kLeast = 1e-9;
+
+struct Layout {
+    uint32_t s, l, sp, lp, parts;
+    int gram, poly, update;  // M of the products' tiles
+    uint32_t splits, steps_each;
+    size_t sums, partial, x[2], a, b, bytes;  // offsets
+};
+
+Layout layout_of(const pxr_orthogonalise_desc& d) {
+    Layout y{};
+    y.s = std::min(d.rows, d.cols);
+    y.l = std::max(d.rows, d.cols);
+    y.sp = padded(y.s);
+    y.lp = padded(y.l);
+    const uint64_t units = (uint64_t)d.rows * ((d.cols + kNormColumns - 1u) / kNormColumns);
+    y.parts = (uint32_t)std::min<uint64_t>(kNormParts, units);
+    const auto tiles = [](uint32_t n, uint32_t side) { return (uint64_t)((n + side - 1u) / side); };
+    const auto triangle_of = [&](uint32_t side) { return tiles(y.s, side) * (tiles(y.s, side) + 1u) / 2u * d.n_matrices; };
+    y.gram = y.poly = triangle_of(128u) >= 256u ? 2 : 1;
+    y.update = tiles(y.s, 128u) * tiles(y.l, 128u) * d.n_matrices >= 256u ? 2 : 1;
+    const uint32_t depth = (y.l + kDepth - 1u) / kDepth;
+    y.splits = 1u;
+    if (y.gram == 1 && triangle_of(64u) < 256u) y.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(depth / 8u, 512u / triangle_of(64u)));
+    y.steps_each = (depth + y.splits - 1u) / y.splits;
+    y.splits = (depth + y.steps_each - 1u) / y.steps_each;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t from = at;
+        at += (bytes + 255u) & ~(size_t)255u;
+        return from;
+    };
+    y.sums = take((size_t)d.n_matrices * y.parts * sizeof(double));
+    y.partial = take(y.splits > 1u ? (size_t)triangle_of(64u) * y.splits * 4096u * sizeof(float) : 0u);
+    for (size_t& x : y.x) x = take((size_t)2 * d.n_matrices * y.sp * y.lp * sizeof(half));
+    y.a = take((size_t)2 * d.n_matrices * y.sp * y.sp * sizeof(half));
+    y.b = take((size_t)2 * d.n_matrices * y.sp * y.sp * sizeof(half));
+    y.bytes = at;
+    return y;
+}
+
+template <int kKind>
+hipError_t launch_product(const Product& p, int M, uint32_t tiles, uint32_t n_matrices, hipStream_t st) {
+    const dim3 grid(tiles, p.splits, n_matrices), threads(kThreads);
+    if (M == 2)
+        hipLaunchKernelGGL((product_kernel<kKind, 2>), grid, threads, 0, st, p);
+    else
+        hipLaunchKernelGGL((product_kernel<kKind, 1>), grid, threads, 0, st, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t orthogonalise_workspace(const pxr_orthogonalise_desc& d) { return layout_of(d).bytes; }
+
+int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* out, void* ws, void* stream, std::string& err) {
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const Layout y = layout_of(d);
+    char* const base = static_cast<char*>(ws);
+    const auto planes = [&](size_t at, uint32_t cols) {
+        const size_t matrix = (size_t)y.sp * cols;
+        return Planes{reinterpret_cast<half*>(base + at), matrix * d.n_matrices, matrix, cols};
+    };
+    const Planes xs[2] = {planes(y.x[0], y.lp), planes(y.x[1], y.lp)}, as = planes(y.a, y.sp), bs = planes(y.b, y.sp);
+    double most = 1.0;  // of the singular values
+    float held = power_below(kMost / most);
+    Prepare prep{x, d.x_matrix, d.x_row, d.rows, d.cols, y.parts, reinterpret_cast<double*>(base + y.sums), xs[0], d.eps, held};
+    const dim3 threads(kThreads), sums(y.parts, d.n_matrices), tiles(y.lp / 64u, y.sp / 64u, d.n_matrices);
+    if (d.dtype == PXR_F32) {
+        hipLaunchKernelGGL((square_sums_kernel<float>), sums, threads, 0, st, prep);
+        hipLaunchKernelGGL((split_kernel<float>), tiles, threads, 0, st, prep);
+    } else {
+        hipLaunchKernelGGL((square_sums_kernel<__bf16>), sums, threads, 0, st, prep);
+        hipLaunchKernelGGL((split_kernel<__bf16>), tiles, threads, 0, st, prep);
+    }
+    hipError_t rc = hipGetLastError();
+    for (uint32_t k = 0; k < d.n_steps && rc == hipSuccess; ++k) {
+        const double a = d.coefficients[3 * k], b = d.coefficients[3 * k + 1], c = d.coefficients[3 * k + 2];
+        const OrthogonaliseBounds next = orthogonalise_bounds(a, b, c, most);
+        const float held_a = power_below(kMost / (most * most)), held_b = power_below(kMost / std::max(next.factor, kLeast));
+        const float held_x = power_below(kMost / std::max(next.most, kLeast));
+        const Planes from = xs[k & 1u], to = xs[(k + 1u) & 1u];
+        const auto triangle_of = [&](int M) { const uint32_t n = (y.s + 64u * M - 1u) / (64u * M); return n; };
+        Product p{};
+        // A
+        p.a = p.b = from;
+        p.to = as;
+        p.depth = (y.l + kDepth - 1u) / kDepth * kDepth;
+        p.tiles_i = p.tiles_j = triangle_of(y.gram);
+        p.splits = y.splits;
+        p.steps_each = y.steps_each;
+        p.partial = reinterpret_cast<float*>(base + y.partial);
+        p.scale = held_a / held / held;
+        p.s = y.s;
+        const uint32_t gram_tiles = p.tiles_i * (p.tiles_i + 1u) / 2u;
+        rc = launch_product<kGram>(p, y.gram, gram_tiles, d.n_matrices, st);
+        if (rc == hipSuccess && y.splits > 1u) {
+            hipLaunchKernelGGL((join_kernel<kGram>), dim3(gram_tiles * 4u, 1, d.n_matrices), threads, 0, st, p);
+            rc = hipGetLastError();
+        }
+        if (rc != hipSuccess) break;
+        // B
+        p.a = p.b = as;
+        p.to = bs;
+        p.depth = (y.s + kDepth - 1u) / kDepth * kDepth;
+        p.tiles_i = p.tiles_j = triangle_of(y.poly);
+        p.splits = 1u;
+        p.steps_each = p.depth / kDepth;
+        p.scale = (float)(c * held_b / held_a / held_a);
+        p.c0 = (float)(a * held_b);
+        p.c1 = (float)(b * held_b / held_a);
+        rc = launch_product<kPoly>(p, y.poly, p.tiles_i * (p.tiles_i + 1u) / 2u, d.n_matrices, st);
+        if (rc != hipSuccess) break;
+        // X
+        const bool last = k + 1u == d.n_steps;
+        p.a = bs;
+        p.b = from;
+        p.to = to;
+        p.tiles_i = triangle_of(y.update);
+        p.tiles_j = (y.l + 64u * y.update - 1u) / (64u * y.update);
+        p.scale = (last ? 1.0f : held_x) / held_b / held;
+        p.out = out;
+        p.out_matrix = d.out_matrix;
+        p.out_row = d.out_row;
+        p.rows = d.rows;
+        p.cols = d.cols;
+        p.transposed = d.rows > d.cols;
+        p.bf16 = d.dtype == PXR_BF16;
+        rc = last ? launch_product<kLast>(p, y.update, p.tiles_i * p.tiles_j, d.n_matrices, st)
+                  : launch_product<kUpdate>(p, y.update, p.tiles_i * p.tiles_j, d.n_matrices, st);
+        held = held_x;
+        most = std::max(next.most, kLeast);
+    }
+    if (rc == hipSuccess) return PXR_OK;
+    err = std::string("kernel launch failed: ") + hipGetErrorString(rc);
+    return PXR_ERR_DEVICE;
+}
+
+}  // namespace pxr

@@ -275,6 +275,16 @@ int launch_head_norm_forward(const HeadNormConsts& c, const pxr_heads& r, const 
 int launch_head_norm_backward(const HeadNormConsts& c, const pxr_heads& r, const pxr_tokens* dq_out, const pxr_tokens* dk_out, const pxr_tokens* dq,
                               const pxr_tokens* dk, void* dq_weight, void* dk_weight, void* ws, void* stream, std::string& err);
 
+// A step a t + b t^3 + c t^5 on singular values t in [0, most]: the largest |result|, and the largest |a + b t^2 + c t^4|, its factor.  learner_api.cpp
+struct OrthogonaliseBounds {
+    double most, factor;
+};
+OrthogonaliseBounds orthogonalise_bounds(double a, double b, double c, double most);
+
+// orthogonalise.hip (arguments as checked by learner_api.cpp)
+size_t orthogonalise_workspace(const pxr_orthogonalise_desc& d);
+int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* out, void* ws, void* stream, std::string& err);
+
 // pipeline.cpp works through these (api.cpp / conv_api.cpp own the handles' layouts).
 constexpr uint32_t kMaxPipelineChunks = 16;
 void scene_shape(const pxr_scene* s, uint32_t* K, uint32_t* H, uint32_t* W);

@@ -3,8 +3,8 @@
 Mirrors include/pxr.h one to one: create_scene / destroy_scene /
 apply_distractor / render_batch, set_skeleton / pose_batch /
 render_batch_kinematic (+ scene_info, set_block_threads, host_tables), the policy's first layer (Conv) and its memory
-(layer_norm, layer_norm_backward, LinearAttention, gated_recurrence, HeadNorm).
-PyTorch is used only to hold device memory and name the stream.
+(layer_norm, layer_norm_backward, LinearAttention, gated_recurrence, HeadNorm),
+a learner's update (orthogonalise).  PyTorch is used only to hold device memory and name the stream.
 There is no fallback: a missing library or a failing call raises.
 """
 import ctypes as C
@@ -107,11 +107,18 @@ class Heads(C.Structure):
                 ("positions_env", C.c_int64), ("positions_step", C.c_int64), ("first", C.c_int64)]
 
 
+class OrthogonaliseDesc(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("n_matrices", C.c_uint32), ("rows", C.c_uint32), ("cols", C.c_uint32),
+                ("x_matrix", C.c_int64), ("x_row", C.c_int64), ("out_matrix", C.c_int64), ("out_row", C.c_int64),
+                ("n_steps", C.c_uint32), ("coefficients", C.c_void_p), ("eps", C.c_float)]
+
+
 # Calls' structures as bytes: a call packs its arguments in a fraction of the time that it takes to fill the structures.
 _pack_norm = struct.Struct("@IIQIfqqq").pack
 _pack_tokens = struct.Struct("@Pqqq").pack
 _pack_rollout = struct.Struct("@III4xPqqqPqqqPqqqPqqP").pack
 _pack_heads = struct.Struct("@IIIIIIPqqqPqqqPPPI4xqqq").pack
+_pack_orthogonalise = struct.Struct("@IIIIqqqqI4xPf4x").pack
 _pack_steps = struct.Struct("@Pqq").pack
 _pack_gated = struct.Struct("@IIIII4xPqqPqqPqqP").pack
 
@@ -202,6 +209,9 @@ def lib():
         L.pxr_head_norm_backward.argtypes = [vp, heads, tokens, tokens, tokens, tokens, vp, vp, vp, C.c_size_t, vp]
         for name in ("create", "destroy", "forward", "workspace", "backward"):
             getattr(L, "pxr_head_norm_" + name).restype = C.c_int
+        L.pxr_orthogonalise_workspace.argtypes = [vp, size]
+        L.pxr_orthogonalise.argtypes = [vp, vp, vp, vp, C.c_size_t, vp]
+        L.pxr_orthogonalise_workspace.restype = L.pxr_orthogonalise.restype = C.c_int
         L.pxr_selftest_arithmetic.argtypes = [vp]
         L.pxr_selftest_arithmetic.restype = C.c_int
         L.pxr_measure_peaks.argtypes = [vp, vp, vp, vp, vp]
@@ -1032,6 +1042,64 @@ def gated_recurrence_step(x, gate, state, resets=None, coupled=True, out=None, s
     _check((_lib or lib()).pxr_gated_recurrence_step(r, _channels(torch, state, B, D), _pack_steps(*_steps_view(out, x.shape, x.dtype)),
                                                      _stream_handle(stream, x)))
     _written(torch, *given)
+    return out
+
+
+# A step that takes singular values from nearly nothing to about one within five.
+ORTHOGONALISE_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+_coefficients = (None, None, None)
+
+
+def _steps_of(coefficients, steps):
+    """float32 [n][3] for one triple, taken `steps` times (5 unless given), or for a triple for each step."""
+    global _coefficients
+    known, n, array = _coefficients  # (those of the call before, most often)
+    if known is not coefficients or n != steps or type(coefficients) is not tuple:
+        array = np.asarray(coefficients, np.float32)
+        if array.ndim == 1:
+            array = np.tile(array, (5 if steps is None else int(steps), 1))
+        assert array.ndim == 2 and array.shape[1] == 3 and (steps is None or array.shape[0] == steps), "a triple, or one for each step"
+        array = np.ascontiguousarray(array)
+        if all(type(c) is float for c in coefficients):  # (what cannot change: a tuple of numbers)
+            _coefficients = (coefficients, steps, array)
+    return array
+
+
+_orthogonalise_asked = (None, 0)
+
+
+def orthogonalise(x, steps=None, coefficients=ORTHOGONALISE_COEFFICIENTS, eps=1e-7, out=None, stream=None):
+    """A learner's update [m,n], or several [B,m,n], CUDA float32 or bfloat16 (rows at any stride, their values adjacent), with its
+    singular values pushed towards one: X = x / (|x| + eps), then for each step X <- a X + (b A + c A^2) X with A = X X^T (of the
+    transpose where m > n).  coefficients: (a, b, c), taken `steps` times (5 unless given), or a triple for each step.
+    Returns the result like x (out may be x); enqueue only."""
+    global _orthogonalise_asked
+    torch = _torch or _torch_module()
+    shape, s = x.shape, x.stride()
+    assert x.is_cuda and len(shape) in (2, 3) and shape[-2] > 0 and shape[-1] > 0, "a CUDA tensor [m,n] or [B,m,n]"
+    assert s[-1] == 1 or shape[-1] == 1, "the values of a row must be adjacent"
+    given = out is not None
+    if out is None:
+        out = _empty(torch, x, stream, shape, x.dtype)
+    else:
+        assert out.is_cuda and out.dtype == x.dtype and out.shape == shape and (out.stride(-1) == 1 or shape[-1] == 1)
+    t = out.stride()
+    c = _steps_of(coefficients, steps)
+    B = shape[0] if len(shape) == 3 else 1
+    d = _pack_orthogonalise(_dtype_code(torch, x.dtype), B, shape[-2], shape[-1], s[0] if len(s) == 3 else 0, s[-2], t[0] if len(t) == 3 else 0, t[-2],
+                            c.shape[0], c.ctypes.data, eps)
+    L = _lib or lib()
+    sizes = d[:16]
+    asked, need = _orthogonalise_asked  # (the bytes for the sizes that were asked for last are known)
+    if asked != sizes:
+        n = C.c_size_t()
+        _check(L.pxr_orthogonalise_workspace(d, n))
+        need = n.value
+        _orthogonalise_asked = (sizes, need)
+    ws = _empty(torch, x, stream, (need,), torch.uint8) if need else None
+    _check(L.pxr_orthogonalise(d, x.data_ptr(), out.data_ptr(), _ptr(ws), need, _stream_handle(stream, x)))
+    if given:
+        _written(torch, out)
     return out
 
 

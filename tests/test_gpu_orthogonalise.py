@@ -1,0 +1,212 @@
+"""A learner's update on the GPU against the float64 definition.
+
+Tolerances, from the arithmetic.  u = 2^-24, w = 2^-8 half a unit of fp32 and bfloat16.  How much an error of a step grows up to the last one goes by the matrix and the
+coefficients; what the same steps in plain fp32 are off by on the same matrix, e, measures it: fp32 rounds every value and every sum once, by u.  Here a value is held to
+2 u (two fp16 parts), a product leaves out up to 4 u (lo lo), and a sum of K products is 3 K / 16 instructions long, whose roundings add up like their root.  So the result may be off by
+(8 + sqrt(3 K / 16)) max(e, 2 u), K the longer side, relative in the Frobenius norm; and w more in bfloat16.
+"""
+import numpy as np
+import pytest
+
+from oracle import learner
+
+pytestmark = pytest.mark.gpu
+
+U, W = 2.0 ** -24, 2.0 ** -8
+QUINTIC = (3.4445, -4.7750, 2.0315)
+FIVE = [tuple(float(np.float32(c)) for c in QUINTIC)] * 5
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as _torch
+    assert _torch.cuda.is_available(), "these tests need the MI355X"
+    return _torch
+
+
+@pytest.fixture(scope="module")
+def pxr():
+    from paper_2502_00021_amd import pxr as _pxr
+    _pxr.lib()
+    return _pxr
+
+
+def plain(torch, x, coefficients, eps, dtype):
+    """The definition by PyTorch's products in `dtype`."""
+    x = x.to(dtype)
+    tall = x.shape[0] > x.shape[1]
+    x = x.t().contiguous() if tall else x
+    x = x / (x.double().square().sum().sqrt().to(dtype) + eps)
+    for a, b, c in coefficients:
+        gram = x @ x.t().contiguous()
+        x = a * x + (b * gram + c * (gram @ gram)) @ x
+    return x.t() if tall else x
+
+
+def check(torch, pxr, x, coefficients=FIVE, eps=1e-7, out=None, got=None):
+    """x [m,n] or [B,m,n] on the GPU."""
+    y = pxr.orthogonalise(x, coefficients=coefficients, eps=eps, out=out) if got is None else got
+    assert y.shape == x.shape and y.dtype == x.dtype
+    for m, g in zip(x if x.dim() == 3 else [x], y if x.dim() == 3 else [y]):
+        if m.numel() <= 1 << 16:
+            ref = torch.from_numpy(learner.orthogonalise(m.double().cpu().numpy(), coefficients, eps)).cuda()
+        else:
+            ref = plain(torch, m, coefficients, eps, torch.float64)
+        norm = float(ref.norm())
+        e = float((plain(torch, m, coefficients, eps, torch.float32).double() - ref).norm()) / norm
+        off = float((g.double() - ref).norm()) / norm
+        allowed = (8 + np.sqrt(3 * max(m.shape) / 16)) * max(e, 2 * U) + (W if x.dtype == torch.bfloat16 else 0)
+        assert off <= allowed, (tuple(x.shape), off, allowed, e)
+    return y
+
+
+def normal(torch, seed, *shape, dtype="f32", scale=1e-3):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(1, 1), (1, 7), (9, 1), (2, 2), (5, 3), (31, 33), (64, 64), (65, 63), (64, 96), (96, 64), (127, 129), (128, 128), (130, 200), (256, 64), (48, 1000), (300, 301),
+                                 (500, 257), (513, 700)])
+def test_sizes(torch, pxr, m, n, dtype):
+    check(torch, pxr, normal(torch, m * 1000 + n, m, n, dtype=dtype))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,m,n", [(3, 64, 96), (5, 17, 9), (2, 200, 1500), (9, 130, 128), (2, 5, 20000), (8, 1000, 1030), (300, 33, 20)])
+def test_batches(torch, pxr, B, m, n, dtype):
+    x = normal(torch, B, B, m, n, dtype=dtype) * torch.linspace(0.5, 100, B, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)[:, None, None]
+    y = check(torch, pxr, x[:12])
+    assert torch.equal(y[0], pxr.orthogonalise(x[:12])[0])
+    whole = pxr.orthogonalise(x)
+    check(torch, pxr, x[-3:], got=whole[-3:])
+
+
+@pytest.mark.parametrize("m,n,dtype", [(64, 30000, "f32"), (20011, 256, "f32"), (30752, 256, "bf16"), (1500, 4000, "f32"), (2050, 2100, "bf16"), (3001, 3000, "f32"), (4, 200000, "f32")])
+def test_large(torch, pxr, m, n, dtype):
+    check(torch, pxr, normal(torch, n, m, n, dtype=dtype))
+
+
+@pytest.mark.parametrize("m,n", [(60, 90), (300, 200)])
+def test_coefficients(torch, pxr, m, n):
+    """Cubic and quintic steps, few and many, of factors far from one, and another triple in every step."""
+    x = normal(torch, 1, m, n)
+    for c in ([QUINTIC], [QUINTIC] * 2, [(1.5, -0.5, 0.0)] * 12, [(15 / 8, -10 / 8, 3 / 8)] * 8, [(3.0, -3.2, 1.2), (2.5, -2.0, 0.5), (1.5, -0.5, 0.0)], [(0.5, 0.0, 0.0)], [(100.0, 0.0, 0.0)],
+              [(0.0, 1.0, 0.0)], [(-2.0, 1.0, 0.5)] * 2, [(1e-3, 0.0, 0.0), (1e3, 0.0, 0.0)]):
+        check(torch, pxr, x, [tuple(float(np.float32(v)) for v in t) for t in c])
+    assert torch.equal(pxr.orthogonalise(x), pxr.orthogonalise(x, coefficients=[QUINTIC] * 5))
+    assert torch.equal(pxr.orthogonalise(x, steps=3), pxr.orthogonalise(x, 3, list(QUINTIC)))
+    assert (pxr.orthogonalise(x, coefficients=[(0.0, 0.0, 0.0)] * 3) == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(96, 64), (140, 300)])
+def test_matrices_as_updates_have_them(torch, pxr, m, n, dtype):
+    """Singular values that lie far apart, a rank of one, rows of zeros, values far from each other, any scale."""
+    r = min(m, n)
+    u, v = torch.linalg.qr(normal(torch, 2, m, r).double())[0], torch.linalg.qr(normal(torch, 3, n, r).double())[0]
+    to = torch.bfloat16 if dtype == "bf16" else torch.float32
+    apart = (u * torch.logspace(0, -4, r, device="cuda", dtype=torch.float64)) @ v.t().contiguous()
+    check(torch, pxr, apart.to(to))
+    check(torch, pxr, (u[:, :1] @ v[:, :1].t().contiguous()).to(to))
+    check(torch, pxr, torch.eye(m, n, device="cuda").to(to))
+    x = normal(torch, 4, m, n, dtype=dtype)
+    x[::3] = 0
+    check(torch, pxr, x)
+    x = normal(torch, 4, m, n, dtype=dtype)
+    x[:, ::2] *= 2.0 ** -10
+    check(torch, pxr, x)
+    for scale in (1e-30, 1e-18, 1e18, 1e30):
+        check(torch, pxr, normal(torch, 5, m, n, dtype=dtype, scale=scale), eps=0.0)
+    assert (pxr.orthogonalise(torch.zeros((m, n), device="cuda", dtype=to)) == 0).all()
+    assert (pxr.orthogonalise(normal(torch, 5, m, n, dtype=dtype, scale=1e-30)).abs() < 1e-12).all()  # eps is what it is divided by
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,m,n,pitch", [(3, 40, 30, 33), (2, 130, 257, 300), (1, 300, 64, 65)])
+def test_strides_in_place_and_nothing_else_written(torch, pxr, B, m, n, pitch, dtype):
+    wide = normal(torch, m, B, m + 2, pitch, dtype=dtype)
+    x = wide[:, 1:-1, 2:2 + n]
+    if x.shape[-1] < n:
+        x = wide[:, 1:-1, 1:1 + n]
+    want = check(torch, pxr, x.contiguous())
+    assert torch.equal(pxr.orthogonalise(x), want)
+    into = torch.full((B + 1, m + 3, pitch + 1), 7.0, device="cuda", dtype=x.dtype)
+    view = into[:B, 2:2 + m, 1:1 + n]
+    assert torch.equal(pxr.orthogonalise(x, out=view), want)
+    view.fill_(7.0)
+    assert (into == 7).all()
+    before = wide.clone()
+    pxr.orthogonalise(x, out=x)
+    assert torch.equal(x, want)
+    x.copy_(before[:, 1:-1, x.storage_offset() % pitch:][..., :n])
+    assert torch.equal(wide, before)
+    # a batch that shares its input
+    shared = before[:1, 1:-1, :n].expand(3, -1, -1)
+    y = pxr.orthogonalise(shared)
+    assert torch.equal(y[0], y[2]) and torch.equal(y[0], pxr.orthogonalise(before[0, 1:-1, :n]))
+
+
+@pytest.mark.parametrize("m,n", [(30, 50), (200, 140), (40, 9000)])
+def test_what_is_not_finite_stays_in_its_matrix(torch, pxr, m, n):
+    x = normal(torch, m, 3, m, n)
+    want = pxr.orthogonalise(x)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        bad = x.clone()
+        bad[1, m // 2, n // 3] = value
+        y = pxr.orthogonalise(bad)
+        assert torch.equal(y[0], want[0]) and torch.equal(y[2], want[2]) and y[1].isnan().all()
+
+
+def test_offsets_past_32_bits(torch, pxr):
+    x = normal(torch, 6, 2, 70, 50, dtype="bf16")
+    want = pxr.orthogonalise(x)
+    apart, row = 2 ** 31 + 64, 2 ** 24
+    big = torch.empty(apart + 69 * row + 64, device="cuda", dtype=torch.bfloat16)
+    view = big.as_strided(x.shape, (apart, row, 1), 5)
+    view.copy_(x)
+    assert torch.equal(pxr.orthogonalise(view), want)
+    pxr.orthogonalise(x, out=view)
+    assert torch.equal(view, want)
+
+
+def test_streams_graphs_and_equal_bits(torch, pxr):
+    for shape in ((3, 64, 96), (700, 300), (40, 9000)):
+        sets = [normal(torch, i, *shape) for i in range(4)]
+        want = [pxr.orthogonalise(x) for x in sets]
+        for _ in range(3):
+            assert torch.equal(pxr.orthogonalise(sets[0]), want[0])
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        got = pxr.orthogonalise(sets[1], stream=side.cuda_stream)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, want[1])
+        static = sets[0].clone()
+        graphs = []
+        for _ in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                graphs.append((g, pxr.orthogonalise(static)))
+        for i in (1, 2, 3, 0, 2):
+            static.copy_(sets[i])
+            for g, y in graphs:
+                g.replay()
+                eager = pxr.orthogonalise(sets[(i + 1) % 4])
+                torch.cuda.synchronize()
+                assert torch.equal(y, want[i]) and torch.equal(eager, want[(i + 1) % 4])
+
+
+def test_refusals(torch, pxr):
+    x = normal(torch, 7, 20, 30)
+    for bad in (dict(x=x.half()), dict(x=x.cpu()), dict(x=x[0]), dict(x=x.t()), dict(x=x[None, None]), dict(x=x[:0]), dict(out=torch.empty_like(x)[:19]), dict(out=torch.empty_like(x).bfloat16()),
+                dict(coefficients=(1.0, 2.0)), dict(coefficients=[QUINTIC] * 3, steps=4), dict(out=torch.empty((30, 20), device="cuda").t())):
+        a = dict(dict(x=x), **bad)
+        with pytest.raises(AssertionError):
+            pxr.orthogonalise(a.pop("x"), **a)
+    for bad, why in ((dict(steps=0), "n_steps"), (dict(steps=65), "n_steps"), (dict(eps=-1.0), "eps"), (dict(coefficients=(100.0, 0.0, 0.0)), "2\\^20"), (dict(coefficients=(float("nan"), 0.0, 0.0)), "finite")):
+        with pytest.raises(pxr.PxrError, match=why):
+            pxr.orthogonalise(x, **bad)
+    with pytest.raises(pxr.PxrError, match="overlap"):
+        pxr.orthogonalise(x[None].expand(2, -1, -1), out=x[None].expand(2, -1, -1))
+    assert pxr.orthogonalise(torch.empty((0, 5, 6), device="cuda")).shape == (0, 5, 6)
