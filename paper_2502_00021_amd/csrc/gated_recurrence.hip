@@ -15,6 +15,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "pxr_internal.h"
 
@@ -42,47 +43,66 @@ struct Raw<__bf16, 1> {
     __device__ __forceinline__ float get(int) const { return __uint_as_float((uint32_t)w << 16); }
 };
 
+// Of a step that is not there: a gate that keeps everything, zeros.
 template <class T, int V>
-__device__ __forceinline__ Raw<T, V> load(const T* p) {
+__device__ __forceinline__ Raw<T, V> absent(bool gate) {
     Raw<T, V> r;
-    __builtin_memcpy(&r, p, sizeof(T) * V);  // (rows may begin at any element: the memory takes requests at any address)
+    if constexpr (sizeof(T) == 4)
+        r.w[0] = gate ? __builtin_inff() : 0.0f;
+    else
+        r.w = gate ? (V == 2 ? 0x7F807F80u : 0x7F80u) : 0u;
     return r;
 }
 
-// Values [from, V) of a vector leave (rounded to nearest even), past the caches: nothing here reads them again.
+// What follows takes a value from its register, whatever is known of it.
+__device__ __forceinline__ void as_it_is(uint32_t& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void as_it_is(float& v) { asm volatile("" : "+v"(v)); }
 template <class T, int V>
-__device__ __forceinline__ void store(T* p, const float (&f)[V], int from) {
-    T v[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = (T)f[i];
-    if (from == 0) {
-        typedef T some __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-        some s;
-        __builtin_memcpy(&s, v, sizeof(v));
-        __builtin_nontemporal_store(s, reinterpret_cast<some*>(p));
-        return;
-    }
-#pragma unroll
-    for (int i = 1; i < V; ++i)
-        if (i >= from) p[i] = v[i];
+__device__ __forceinline__ void as_it_is(Raw<T, V>& v) {
+    if constexpr (sizeof(T) == 4)
+        asm volatile("" : "+v"(v.w[0]));
+    else
+        asm volatile("" : "+v"(v.w));
 }
 
-// A gate as one number: a where it is the smaller of a and 1 - a, otherwise -(1 - a).  Each of the two is 1 less the other where that loses nothing.
+// A lane's values of a row: the row's address is the same for all lanes, and a lane's place in it a number of 32 bits, so that an address takes no vector registers.
+template <class T, int V>
+__device__ __forceinline__ Raw<T, V> load(const T* row, uint32_t place) {
+    Raw<T, V> r;
+    __builtin_memcpy(&r, reinterpret_cast<const char*>(row) + place, sizeof(T) * V);  // (rows may begin at any element: the memory takes requests at any address)
+    return r;
+}
+
+// Rounded to nearest even, past the caches: nothing here reads them again.
+template <class T, int V>
+__device__ __forceinline__ void store(T* row, uint32_t place, const float (&f)[V]) {
+    typedef T some __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    some v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (T)f[i];
+    __builtin_nontemporal_store(v, reinterpret_cast<some*>(reinterpret_cast<char*>(row) + place));
+}
+
+// What stands behind this is not begun before it: otherwise inputs of all steps are formed at once, in registers that there are not.
+__device__ __forceinline__ void in_turn() { __builtin_amdgcn_sched_barrier(0); }
+
+// A gate as one number: 1 - a where that is the smaller of a and 1 - a, otherwise -a.  Each of the two is 1 less the other where that loses nothing.
 template <class T>
 __device__ __forceinline__ float gate_of(float g) {
-    const float m = fabsf(g) > 100.0f ? 100.0f : fabsf(g);  // (a NaN stays one)
+    float m = fabsf(g);
+    if (sizeof(T) == 4 && m > 100.0f) m = 100.0f;  // (a NaN stays one)
     const float t = m * -1.44269504f;
     float e = __builtin_amdgcn_exp2f(t);  // exp(-|g|)
     // (what t has lost in 24 bits is |g| of their last one: of 32 bits' results as well)
     if (sizeof(T) == 4) e = __builtin_fmaf(e, __builtin_fmaf(m, -1.44269504f, -t) * 0.69314718f - m * 1.3346e-8f, e);
-    return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), -g);
+    return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
 }
-__device__ __forceinline__ bool mostly(float s) { return (int)__float_as_uint(s) < 0; }  // a >= 1/2
-__device__ __forceinline__ float taken(float s) { return mostly(s) ? -s : 1.0f - s; }    // 1 - a
+__device__ __forceinline__ bool mostly(float s) { return (int)__float_as_uint(s) >= 0; }  // a >= 1/2
+__device__ __forceinline__ float taken(float s) { return s + (mostly(s) ? 0.0f : 1.0f); }  // 1 - a
 // a v + b.  Where a is all but 1 it is v less a little: a itself, rounded, would be off in the same direction in every step of a gate that stays where it is (200
 // steps of gates around 10: a state off by 3e-6, 3e-7 so).
-__device__ __forceinline__ float kept(float s, float v, float b) { return __builtin_fmaf(s, v, mostly(s) ? v + b : b); }
-__device__ __forceinline__ float kept(float s, float v) { return __builtin_fmaf(s, v, mostly(s) ? v : 0.0f); }
+__device__ __forceinline__ float kept(float s, float v, float b) { return __builtin_fmaf(-s, v, (mostly(s) ? v : 0.0f) + b); }
+__device__ __forceinline__ float kept(float s, float v) { return __builtin_fmaf(-s, v, mostly(s) ? v : 0.0f); }
 
 // Products in which 0 wins, over what is not a number as well.
 __device__ __forceinline__ float times(float A, float B) { return A == 0.0f || B == 0.0f ? 0.0f : A * B; }
@@ -102,36 +122,129 @@ struct Recurrence {
 };
 
 enum { kForward, kForwardSums, kBackward, kBackwardSums };
-constexpr uint32_t kMostWaves = 8;
+constexpr int C = 16;                  // steps of a wavefront
+constexpr uint32_t kMostWaves = 16;    // of a workgroup
 
-// Where a lane's channels are.  A row that ends inside a vector has its last vector moved back to its end, lanes behind the row have that one as well: values
-// before `from` are another lane's.
-template <int V>
+// Where a lane's channels are: of environment `env`, from channel `at` on.  A row that ends inside a vector has its last vector moved back to its end: the values that
+// it shares with the vector before it are computed in both lanes, by the same operations, and written by both, the same bits.  Lanes behind the row's end, and
+// those of environments that are not there (`any` is false), take the last one's and write nothing.
+template <class T, int V>
 struct Lane {
-    uint32_t env, at;
-    int from;
+    uint32_t env0, env, at;
+    bool any;
     __device__ __forceinline__ Lane(const Recurrence& a, uint32_t rows, uint32_t strip) {
         const uint32_t lane = threadIdx.x & 63u, in_row = lane & (a.lanes - 1u);
-        const uint32_t e = rows * (64u / a.lanes) + lane / a.lanes, c = (strip * a.lanes + in_row) * V;
+        env0 = rows * (64u / a.lanes);
+        const uint32_t e = env0 + lane / a.lanes, c = (strip * a.lanes + in_row) * V;
         env = min(e, a.n_envs - 1u);
         at = min(c, a.width - V);
-        from = e < a.n_envs ? (int)min(c - at, (uint32_t)V) : V;
+        any = e < a.n_envs && c < a.width;
+    }
+    // In bytes from the first environment's row.  (The launch sees to it that these fit 32 bits.)
+    __device__ __forceinline__ uint32_t place(int64_t env_stride) const { return ((env - env0) * (uint32_t)env_stride + at) * (uint32_t)sizeof(T); }
+};
+
+// A value, or 0 where a mask says so, whatever the value is.
+__device__ __forceinline__ float masked(float v, uint32_t m) { return __uint_as_float(__float_as_uint(v) & m); }
+
+// A wavefront's steps, C of V channels a lane.  `cuts`: a bit for each step that begins an episode.  Steps that are not there keep everything and add nothing (absent()).
+template <class T, int V, int kWhat, bool kCoupled>
+struct Chunk {
+    static constexpr bool kBack = kWhat >= kBackward;
+    typedef Raw<T, V> Raws[C];
+
+    // All bits where step j goes on with what was before it.
+    static __device__ __forceinline__ uint32_t goes_on(uint32_t cuts, int j) { return (cuts >> j & 1u) - 1u; }
+    static __device__ __forceinline__ float input(float s, float x) { return kCoupled ? taken(s) * x : x; }
+
+    // By themselves: product, result from zero, and what they hand back of zero.  h, s: forward, the results and the products up to them; backward, the gates in s.
+    static __device__ __forceinline__ void alone(const Raws& xs, const Raws& gs, const Raw<T, V>* ds, uint32_t cuts, float (&A)[V], float (&H)[V], float (&R)[V], float (&h)[C][V], float (&s)[C][V]) {
+        uint32_t none = ~0u;  // that has begun an episode so far: products stay 0 after one that has, over gates that are no numbers
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const uint32_t on = goes_on(cuts, j);
+            none &= on;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float g = gate_of<T>(gs[j].get(i));
+                A[i] = masked(kept(g, A[i]), none);
+                H[i] = kept(g, masked(H[i], on), input(g, xs[j].get(i)));
+                if (kWhat == kForward) h[j][i] = H[i];
+                s[j][i] = kBack ? g : A[i];
+            }
+            in_turn();
+        }
+        if constexpr (kBack) {
+#pragma unroll
+            for (int j = C - 1; j >= 0; --j)
+#pragma unroll
+                for (int i = 0; i < V; ++i) R[i] = masked(kept(s[j][i], ds[j].get(i) + R[i]), goes_on(cuts, j));
+        }
+    }
+
+    static __device__ __forceinline__ void outputs(const float (&h)[C][V], const float (&s)[C][V], int n, uint32_t cuts, const float (&state)[V], T* out, int64_t step, uint32_t place) {
+        uint32_t none = ~0u;
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            none &= goes_on(cuts, j);
+            float y[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = __builtin_fmaf(s[j][i], masked(state[i], none), h[j][i]);
+            if (j < n) store<T, V>(out, place, y);
+            out += step;
+        }
+    }
+
+    // dx, dgate: of the last of the C steps.
+    static __device__ __forceinline__ void gradients(Raws& xs, const Raw<T, V>* ds, float (&s)[C][V], int n, uint32_t cuts, float (&state)[V], float (&later)[V], T* dx, int64_t dx_step,
+                                                     uint32_t dx_place, T* dgate, int64_t dgate_step, uint32_t dgate_place) {
+        float h[C][V];  // what a step sees of the state
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                h[j][i] = masked(state[i], goes_on(cuts, j));
+                state[i] = kept(s[j][i], h[j][i], input(s[j][i], xs[j].get(i)));
+                as_it_is(s[j][i]);  // (what it was made into, here and in front of the barrier, is made again below: there are no registers to keep it in)
+            }
+            as_it_is(xs[j]);
+            in_turn();
+        }
+#pragma unroll
+        for (int j = C - 1; j >= 0; --j) {
+            float to_x[V], to_gate[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float take = taken(s[j][i]), L = ds[j].get(i) + later[i], kept_L = kept(s[j][i], L);
+                to_x[i] = kCoupled ? take * L : L;
+                to_gate[i] = take * kept_L * (kCoupled ? h[j][i] - xs[j].get(i) : h[j][i]);
+                later[i] = masked(kept_L, goes_on(cuts, j));
+            }
+            if (j < n) {
+                store<T, V>(dx, dx_place, to_x);
+                store<T, V>(dgate, dgate_place, to_gate);
+            }
+            dx -= dx_step;
+            dgate -= dgate_step;
+            in_turn();
+        }
     }
 };
 
-// C steps of V channels a lane; kWhat: see the enum.  One workgroup: seg_steps steps (backward: at most what its wavefronts hold) of a strip of channels of
-// 64 / lanes environments.
-template <class T, int V, int C, int kWhat>
+// One workgroup: seg_steps steps (backward: at most what its wavefronts hold) of a strip of channels of 64 / lanes environments.
+template <class T, int V, int kWhat, bool kCoupled>
 __global__ __launch_bounds__(kMostWaves * 64) void recurrence_kernel(const Recurrence a) {
     constexpr bool kBack = kWhat >= kBackward, kSums = kWhat == kForwardSums || kWhat == kBackwardSums;
     constexpr int kPlanes = kBack ? 3 : 2;
+    typedef Chunk<T, V, kWhat, kCoupled> Steps;
     __shared__ float shared[kBack ? 1 : 2][kMostWaves][kPlanes][V][64];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const uint32_t strip = blockIdx.x % a.strips, rest = blockIdx.x / a.strips, seg = rest % a.segments, rows = rest / a.segments;
-    const Lane<V> at(a, rows, strip);
-    const T* x = static_cast<const T*>(a.x) + (int64_t)at.env * a.x_env + at.at;
-    const T* gate = static_cast<const T*>(a.gate) + (int64_t)at.env * a.gate_env + at.at;
-    const T* dout = kBack ? static_cast<const T*>(a.dout) + (int64_t)at.env * a.dout_env + at.at : nullptr;
+    const Lane<T, V> at(a, rows, strip);
+    const T* x = static_cast<const T*>(a.x) + (int64_t)at.env0 * a.x_env;
+    const T* gate = static_cast<const T*>(a.gate) + (int64_t)at.env0 * a.gate_env;
+    const T* dout = kBack ? static_cast<const T*>(a.dout) + (int64_t)at.env0 * a.dout_env : nullptr;
+    const uint32_t places[3] = {at.place(a.x_env), at.place(a.gate_env), at.place(a.dout_env)};
     const size_t cell = (size_t)at.env * a.width + at.at, cells = (size_t)a.n_envs * a.width;
     const uint32_t begin = seg * a.seg_steps, end = min(begin + a.seg_steps, a.n_steps);
 
@@ -145,12 +258,16 @@ __global__ __launch_bounds__(kMostWaves * 64) void recurrence_kernel(const Recur
         state[i] = a.segments > 1u ? plane[cells + cell + i] : a.state_in ? a.state_in[cell + i] : 0.0f;
         if (kBack) later[i] = a.segments > 1u ? plane[2 * cells + cell + i] : a.after ? a.after[cell + i] : 0.0f;
     }
-    float whole[V];  // the product over the segment (sums)
+    float product[V];  // over the segment (sums)
 #pragma unroll
-    for (int i = 0; i < V; ++i) whole[i] = 1.0f;
+    for (int i = 0; i < V; ++i) product[i] = 1.0f;
 
-    uint32_t turn = 0;
-    for (uint32_t block = begin; block < end; block += waves * C, turn ^= 1u) {
+    uint32_t turn = 0, block = begin;
+    do {  // (backward: once)
+        uint32_t x_place = places[0], gate_place = places[1], dout_place = places[2];
+        as_it_is(x_place);  // (otherwise an address of the whole, in vector registers, outside of the loop)
+        as_it_is(gate_place);
+        as_it_is(dout_place);
         const uint32_t first = block + wave * C;
         const int n = first < end ? (int)min(end - first, (uint32_t)C) : 0;  // this wavefront's steps
         Raw<T, V> xs[C], gs[C], ds[kBack ? C : 1];
@@ -160,50 +277,43 @@ __global__ __launch_bounds__(kMostWaves * 64) void recurrence_kernel(const Recur
             const T *g = gate + (int64_t)first * a.gate_step, *v = x + (int64_t)first * a.x_step, *d = kBack ? dout + (int64_t)first * a.dout_step : nullptr;
 #pragma unroll
             for (int j = 0; j < C; ++j) {
-                gs[j] = load<T, V>(g);
-                xs[j] = load<T, V>(v);
-                if (kBack) ds[j] = load<T, V>(d);
+                gs[j] = load<T, V>(g, gate_place);
+                xs[j] = load<T, V>(v, x_place);
+                if (kBack) ds[j] = load<T, V>(d, dout_place);
                 g += j + 1 < n ? a.gate_step : 0;
                 v += j + 1 < n ? a.x_step : 0;
                 if (kBack) d += j + 1 < n ? a.dout_step : 0;
             }
+            if (n < C)
+#pragma unroll
+                for (int j = 1; j < C; ++j)
+                    if (j >= n) {
+                        gs[j] = absent<T, V>(true);
+                        xs[j] = absent<T, V>(false);
+                        if (kBack) ds[j] = absent<T, V>(false);
+                    }
             if (a.resets) {  // the first C of an environment's lanes ask for one of its steps each
                 const uint32_t in_row = lane & (a.lanes - 1u);
                 const bool mark = in_row < (uint32_t)n && a.resets[(int64_t)at.env * a.resets_env + (int64_t)(first + in_row) * a.resets_step];
-                const uint64_t marks = __ballot(mark) >> (lane - in_row);
-                cuts = (uint32_t)marks & (C == 32 ? 0xFFFFFFFFu : (1u << (C & 31)) - 1u);
+                cuts = (uint32_t)(__ballot(mark) >> (lane - in_row)) & ((1u << C) - 1u);
             }
         }
         // each wavefront's steps by themselves
-        float A[V], H[V], R[V];
-        float h[C][V], s[C][V];  // forward: results from zero, and the products up to them; backward: the states that came in, and the gates
+        float A[V], H[V], R[V], h[C][V], s[C][V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             A[i] = 1.0f;
             H[i] = R[i] = 0.0f;
         }
-        if (n) {
+        if (n) Steps::alone(xs, gs, ds, cuts, A, H, R, h, s);
+        if (kWhat == kBackward)
 #pragma unroll
             for (int j = 0; j < C; ++j) {
-                const bool cut = cuts >> j & 1u;
+                as_it_is(xs[j]);
+                as_it_is(ds[j]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float g = gate_of<T>(gs[j].get(i)), b = a.coupled ? taken(g) * xs[j].get(i) : xs[j].get(i);
-                    if (j < n) {
-                        A[i] = cut || A[i] == 0.0f ? 0.0f : kept(g, A[i]);
-                        H[i] = cut ? b : kept(g, H[i], b);
-                    }
-                    h[j][i] = H[i];
-                    s[j][i] = kBack ? g : A[i];
-                }
+                for (int i = 0; i < V; ++i) as_it_is(s[j][i]);
             }
-            if (kBack)
-#pragma unroll
-                for (int j = C - 1; j >= 0; --j)
-#pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        if (j < n) R[i] = cuts >> j & 1u ? 0.0f : kept(s[j][i], ds[j].get(i) + R[i]);
-        }
         float(&told)[kMostWaves][kPlanes][V][64] = shared[kBack ? 0 : turn];  // (the block after the next one writes here again)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -221,7 +331,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void recurrence_kernel(const Recur
                 if (w == wave) mine[i] = state[i];
                 const float p = told[w][0][i][lane];
                 state[i] = through(p, told[w][1][i][lane], state[i]);
-                if (kSums) whole[i] = times(whole[i], p);
+                if (kSums) product[i] = times(product[i], p);
             }
             if constexpr (kBack) {
                 for (uint32_t w = waves; w-- > 0;) {
@@ -230,57 +340,27 @@ __global__ __launch_bounds__(kMostWaves * 64) void recurrence_kernel(const Recur
                 }
             }
         }
-        if (kSums || !n) continue;
+        if (kSums || !n || !at.any) continue;
         if constexpr (kWhat == kForward) {
-            T* out = static_cast<T*>(a.out) + ((int64_t)at.env * a.out_env + at.at + (int64_t)first * a.out_step);
-#pragma unroll
-            for (int j = 0; j < C; ++j) {
-                float y[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) y[i] = through(s[j][i], h[j][i], mine[i]);
-                if (j < n && at.from < V) store<T, V>(out, y, at.from);
-                out += a.out_step;
-            }
+            T* out = static_cast<T*>(a.out) + ((int64_t)at.env0 * a.out_env + (int64_t)first * a.out_step);
+            uint32_t place = at.place(a.out_env);
+            as_it_is(place);
+            Steps::outputs(h, s, n, cuts, mine, out, a.out_step, place);
         } else if constexpr (kWhat == kBackward) {
-            // the states again, now from what came in
-#pragma unroll
-            for (int j = 0; j < C; ++j)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float b = a.coupled ? taken(s[j][i]) * xs[j].get(i) : xs[j].get(i);
-                    h[j][i] = cuts >> j & 1u ? 0.0f : mine[i];
-                    mine[i] = cuts >> j & 1u ? b : kept(s[j][i], mine[i], b);
-                }
-            T* dx = static_cast<T*>(a.out) + ((int64_t)at.env * a.out_env + at.at + (int64_t)(first + n - 1) * a.out_step);
-            T* dgate = static_cast<T*>(a.dgate) + ((int64_t)at.env * a.dgate_env + at.at + (int64_t)(first + n - 1) * a.dgate_step);
-#pragma unroll
-            for (int j = C - 1; j >= 0; --j) {
-                if (j >= n) continue;
-                float to_x[V], to_gate[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float take = taken(s[j][i]), L = ds[j].get(i) + mine_later[i];
-                    to_x[i] = a.coupled ? take * L : L;
-                    const float kept_L = kept(s[j][i], L);
-                    to_gate[i] = take * kept_L * (a.coupled ? h[j][i] - xs[j].get(i) : h[j][i]);
-                    mine_later[i] = cuts >> j & 1u ? 0.0f : kept_L;
-                }
-                if (at.from < V) {
-                    store<T, V>(dx, to_x, at.from);
-                    store<T, V>(dgate, to_gate, at.from);
-                }
-                dx -= a.out_step;
-                dgate -= a.dgate_step;
-            }
+            T* dx = static_cast<T*>(a.out) + ((int64_t)at.env0 * a.out_env + (int64_t)(first + C - 1) * a.out_step);
+            T* dgate = static_cast<T*>(a.dgate) + ((int64_t)at.env0 * a.dgate_env + (int64_t)(first + C - 1) * a.dgate_step);
+            uint32_t dx_place = at.place(a.out_env), dgate_place = at.place(a.dgate_env);
+            as_it_is(dx_place);
+            as_it_is(dgate_place);
+            Steps::gradients(xs, ds, s, n, cuts, mine, mine_later, dx, a.out_step, dx_place, dgate, a.dgate_step, dgate_place);
         }
-    }
-    if (wave == 0) {
+    } while (!kBack && (turn ^= 1u, block += waves * C) < end);
+    if (wave == 0 && at.any) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (i < at.from) continue;
             if (kSums) {
                 float* plane = a.joined + (size_t)seg * kPlanes * cells + cell + i;
-                plane[0] = whole[i];
+                plane[0] = product[i];
                 plane[cells] = state[i];
                 if (kBack) plane[2 * cells] = later[i];
             } else if (kWhat == kForward) {
@@ -390,49 +470,61 @@ __global__ __launch_bounds__(256) void recurrence_pass_kernel(const float* from,
 }
 
 struct Shape {
-    uint32_t V, C, lanes, rows, strips, waves, segments, seg_steps;
+    uint32_t V, lanes, rows, strips, waves, segments, seg_steps;
 };
 
-// How a call is cut.
-Shape shape_of(uint32_t n_envs, uint32_t n_steps, uint32_t width, bool backward) {
+// How a call is cut (lanes, rows, strips: by its strides as well, in narrowed()).
+Shape shape_of(uint32_t V, uint32_t n_envs, uint32_t n_steps, uint32_t width, bool backward) {
     Shape s{};
-    s.V = width >= 2u ? 2u : 1u;
-    s.C = 16u;
-    if (backward && n_steps > kMostWaves * 16u) {
-        s.V = 1u;
-        s.C = 32u;
-    }
-    s.lanes = s.C;
+    s.V = V;
+    s.lanes = (uint32_t)C;
     while (s.lanes < 64u && s.lanes * s.V < width) s.lanes *= 2u;
     s.rows = (n_envs + 64u / s.lanes - 1u) / (64u / s.lanes);
     s.strips = (width + s.lanes * s.V - 1u) / (s.lanes * s.V);
-    const uint32_t chunks = (n_steps + s.C - 1u) / s.C, blocks = (chunks + kMostWaves - 1u) / kMostWaves;
+    const uint32_t chunks = (n_steps + C - 1u) / C, most = backward ? kMostWaves : kMostWaves / 2u, blocks = (chunks + most - 1u) / most;
     if (backward) {
-        s.segments = blocks;
         s.waves = (chunks + blocks - 1u) / blocks;
-        s.seg_steps = s.waves * s.C;
+        s.seg_steps = s.waves * C;
     } else {
-        const uint64_t groups = (uint64_t)s.rows * s.strips;
+        const uint64_t groups = (uint64_t)n_envs * ((width + 127u) / 128u);  // (by the sizes alone, like the workspace)
         const uint32_t cut = (uint32_t)std::min<uint64_t>(blocks, groups >= 1024u ? 1u : (1024u + groups - 1u) / groups);
         const uint32_t each = (blocks + cut - 1u) / cut;  // blocks of a segment
-        s.segments = (blocks + each - 1u) / each;
-        s.waves = std::min(chunks, kMostWaves);
-        s.seg_steps = each * s.waves * s.C;
+        s.waves = std::min(chunks, most);
+        s.seg_steps = each * s.waves * C;
     }
     s.segments = (n_steps + s.seg_steps - 1u) / s.seg_steps;
+    return s;
+}
+
+// Values of a lane: 4 bytes of them.
+uint32_t values_of(const pxr_gated_rollout& r) { return r.dtype == PXR_BF16 && r.width >= 2u ? 2u : 1u; }
+
+// Environments that share a wavefront are numbers of 32 bits apart, in bytes; where they lie further, or backwards, each has one to itself.
+Shape narrowed(Shape s, uint32_t n_envs, uint32_t width, std::initializer_list<int64_t> env_strides) {
+    for (const int64_t e : env_strides)
+        if (s.lanes < 64u && (e < 0 || e > (1ll << 26))) {
+            s.lanes = 64u;
+            s.rows = n_envs;
+            s.strips = (width + 64u * s.V - 1u) / (64u * s.V);
+        }
     return s;
 }
 
 template <class T, int kWhat>
 hipError_t launch_part(const Shape& s, const Recurrence& a, hipStream_t st) {
     const dim3 grid(s.rows * s.strips * s.segments), threads(s.waves * 64u);
-    constexpr bool kBack = kWhat >= kBackward;
-    if (s.V == 2u)
-        hipLaunchKernelGGL((recurrence_kernel<T, 2, 16, kWhat>), grid, threads, 0, st, a);
-    else if (s.C == 16u)
-        hipLaunchKernelGGL((recurrence_kernel<T, 1, 16, kWhat>), grid, threads, 0, st, a);
-    else if constexpr (kBack)
-        hipLaunchKernelGGL((recurrence_kernel<T, 1, 32, kWhat>), grid, threads, 0, st, a);
+    if (sizeof(T) == 2 && s.V == 2u) {
+        constexpr int V = sizeof(T) == 2 ? 2 : 1;
+        if (a.coupled)
+            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, true>), grid, threads, 0, st, a);
+        else
+            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, false>), grid, threads, 0, st, a);
+    } else {
+        if (a.coupled)
+            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, true>), grid, threads, 0, st, a);
+        else
+            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, false>), grid, threads, 0, st, a);
+    }
     return hipGetLastError();
 }
 
@@ -491,14 +583,14 @@ hipError_t pass_on(const float* from, float* to, const pxr_gated_rollout& r, hip
 
 size_t gated_recurrence_workspace(uint32_t n_envs, uint32_t n_steps, uint32_t width, bool backward) {
     if (n_steps == 0) return 0;
-    const Shape s = shape_of(n_envs, n_steps, width, backward);
+    const Shape s = shape_of(1, n_envs, n_steps, width, backward);
     return s.segments > 1u ? (size_t)s.segments * (backward ? 3 : 2) * n_envs * width * sizeof(float) : 0;
 }
 
 int launch_gated_recurrence_forward(const pxr_gated_rollout& r, const pxr_steps& out, float* state_out, void* ws, void* stream, std::string& err) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (r.n_steps == 0) return result(pass_on(r.d_state, state_out, r, st), err);
-    const Shape s = shape_of(r.n_envs, r.n_steps, r.width, false);
+    const Shape s = narrowed(shape_of(values_of(r), r.n_envs, r.n_steps, r.width, false), r.n_envs, r.width, {r.x.env, r.gate.env, out.env});
     Recurrence a = arguments(r, s, ws);
     a.out = out.data;
     a.out_env = out.env;
@@ -511,7 +603,7 @@ int launch_gated_recurrence_backward(const pxr_gated_rollout& r, const pxr_steps
                                      const pxr_steps& dgate, float* dstate, void* ws, void* stream, std::string& err) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (r.n_steps == 0) return result(pass_on(dstate_out, dstate, r, st), err);
-    const Shape s = shape_of(r.n_envs, r.n_steps, r.width, true);
+    const Shape s = narrowed(shape_of(values_of(r), r.n_envs, r.n_steps, r.width, true), r.n_envs, r.width, {r.x.env, r.gate.env, dout.env, dx.env, dgate.env});
     Recurrence a = arguments(r, s, ws);
     a.dout = dout.data;
     a.dout_env = dout.env;
