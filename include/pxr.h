@@ -492,7 +492,7 @@ typedef struct {
     float eps;
 } pxr_orthogonalise_desc;
 
-/* Bytes of workspace that pxr_orthogonalise needs for this description (host only).  Errors: as for the call (buffers are not looked at). */
+/* Bytes of workspace that pxr_orthogonalise needs for this description (host only; may be 0).  Errors: as for the call (buffers are not looked at). */
 int pxr_orthogonalise_workspace(const pxr_orthogonalise_desc* d, size_t* bytes);
 
 /* The result in d_out, which may be d_x itself.  Products and sums keep 22 bits and more (fp32's, but for a few roundings of 2^-23); values below 2^-38 of the

@@ -25,7 +25,7 @@ struct HeadsOf {
     const void *x, *dy, *weight;
     void* out;
     int64_t x_env, x_step, x_head, dy_env, dy_step, dy_head, out_env, out_step, out_head;
-    uint32_t heads, parts;  // parts of kTogether heads
+    uint32_t heads, parts;  // parts of U heads
 };
 
 struct HeadNormArgs {
@@ -40,10 +40,13 @@ struct HeadNormArgs {
 };
 
 constexpr uint32_t kThreads = 256;
-constexpr uint32_t kMostGroups = 2048;  // workgroups of a launch, which walk the tokens
+constexpr uint32_t kMostGroups = 1024;  // workgroups of a launch, which walk the tokens (gradients of 512 x 256 tokens as below: 2048 of them 219 us, 1024 214)
 
 template <class T, int N>
 __device__ __forceinline__ void load(const T* p, T (&v)[N]) { __builtin_memcpy(v, p, sizeof(v)); }  // (at the address of any value)
+
+template <class T, int N>
+__device__ __forceinline__ void store(T* p, const T (&v)[N]) { __builtin_memcpy(p, v, sizeof(v)); }
 
 // sin and cos of an angle in fractions of 2^32 of a turn: of the angle to the nearest quarter by their series (the first terms left out are below 2^-28), then
 // the quarters.
@@ -196,8 +199,8 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
                         }
                     }
                     T* to = out + (int64_t)(head0 + u) * t.out_head;
-                    if (at.any) __builtin_memcpy(to + at.lo, lo, sizeof(lo));
-                    if (at.second) __builtin_memcpy(to + at.hi, hi, sizeof(hi));
+                    if (at.any) store(to + at.lo, lo);
+                    if (at.second) store(to + at.hi, hi);
                 }
             }
         };
@@ -255,17 +258,20 @@ struct HeadNormShape {
     uint32_t V, K, lanes, split, groups;  // groups: workgroups
 };
 
-constexpr uint32_t kTogether = 4;  // heads that a group of lanes has in flight
+// Heads that a group of lanes has in flight, and the values of one of its requests: more are more registers and fewer wavefronts.  (Gradients of 512 x 256 tokens of 16 + 4 heads of 64 bfloat16: 4 heads in
+// requests of 16 bytes 358 us, 2 of them 237, 2 in requests of 8 bytes 216; forward, 256 x 128 tokens of 8 + 8 heads: 31, 32.7 and 33.)
+constexpr uint32_t together(bool backward) { return backward ? 2u : 4u; }
+constexpr uint32_t most_values(uint32_t dtype, bool backward) { return dtype == PXR_F32 || backward ? 4u : 8u; }
 
-HeadNormShape shape_of(const HeadNormConsts& c, uint32_t dtype, uint64_t tokens, uint32_t n_heads, uint32_t n_key_heads) {
+HeadNormShape shape_of(const HeadNormConsts& c, uint32_t dtype, uint64_t tokens, uint32_t n_heads, uint32_t n_key_heads, bool backward) {
     HeadNormShape s{};
     const uint32_t half = c.r / 2u, behind = c.d - c.r, slots = half + (behind + 1u) / 2u;
-    s.V = dtype == PXR_F32 ? 4u : 8u;
+    s.V = most_values(dtype, backward);
     while (s.V > 1u && (half % s.V || behind % (2u * s.V))) s.V /= 2u;
     s.lanes = 1u;
     while (s.lanes < 64u && s.lanes * s.V < slots) s.lanes *= 2u;
     s.K = s.lanes * s.V < slots ? 2u : 1u;
-    const uint32_t parts = (n_heads + kTogether - 1u) / kTogether + (n_key_heads + kTogether - 1u) / kTogether;
+    const uint32_t U = together(backward), parts = (n_heads + U - 1u) / U + (n_key_heads + U - 1u) / U;
     // a token's heads are shared out where the tokens alone are too few wavefronts
     const uint64_t waves = (tokens * s.lanes + 63u) / 64u;
     s.split = (uint32_t)std::min<uint64_t>(std::max(parts, 1u), waves ? (2048u + waves - 1u) / waves : 1u);
@@ -276,17 +282,18 @@ HeadNormShape shape_of(const HeadNormConsts& c, uint32_t dtype, uint64_t tokens,
 
 template <class T, class P, bool kBack>
 hipError_t launch(const HeadNormShape& s, const HeadNormArgs& a, hipStream_t st) {
+    constexpr int U = (int)together(kBack);
     const dim3 grid(s.groups), threads(kThreads);
     if (s.K == 2u)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 1, 2, kTogether, kBack>), grid, threads, 0, st, a);
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 1, 2, U, kBack>), grid, threads, 0, st, a);
     else if (s.V == 1u)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 1, 1, kTogether, kBack>), grid, threads, 0, st, a);
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 1, 1, U, kBack>), grid, threads, 0, st, a);
     else if (s.V == 2u)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 2, 1, kTogether, kBack>), grid, threads, 0, st, a);
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 2, 1, U, kBack>), grid, threads, 0, st, a);
     else if (s.V == 4u)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 4, 1, kTogether, kBack>), grid, threads, 0, st, a);
-    else if constexpr (sizeof(T) == 2)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 8, 1, kTogether, kBack>), grid, threads, 0, st, a);
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 4, 1, U, kBack>), grid, threads, 0, st, a);
+    else if constexpr (sizeof(T) == 2 && !kBack)
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 8, 1, U, kBack>), grid, threads, 0, st, a);
     return hipGetLastError();
 }
 
@@ -299,9 +306,10 @@ hipError_t launch_typed(const pxr_heads& r, const HeadNormShape& s, const HeadNo
 HeadNormArgs arguments(const HeadNormConsts& c, const pxr_heads& r, const HeadNormShape& s, const pxr_tokens* q_out, const pxr_tokens* k_out,
                        const pxr_tokens* dq, const pxr_tokens* dk) {
     HeadNormArgs a{};
-    const auto fill = [](HeadsOf& t, const pxr_tokens& x, const void* weight, uint32_t heads, const pxr_tokens* out, const pxr_tokens* dy) {
+    const uint32_t U = together(dq || dk);
+    const auto fill = [U](HeadsOf& t, const pxr_tokens& x, const void* weight, uint32_t heads, const pxr_tokens* out, const pxr_tokens* dy) {
         t.heads = heads;
-        t.parts = (heads + kTogether - 1u) / kTogether;
+        t.parts = (heads + U - 1u) / U;
         if (!heads) return;
         t.x = x.data;
         t.x_env = x.env;
@@ -347,11 +355,11 @@ int result(hipError_t rc, std::string& err) {
 }  // namespace
 
 size_t head_norm_workspace(const HeadNormConsts& c, const pxr_heads& r) {
-    return (size_t)shape_of(c, r.dtype, (uint64_t)r.n_envs * r.n_steps, r.n_heads, r.n_key_heads).groups * 2 * c.d * sizeof(float);
+    return (size_t)shape_of(c, r.dtype, (uint64_t)r.n_envs * r.n_steps, r.n_heads, r.n_key_heads, true).groups * 2 * c.d * sizeof(float);
 }
 
 int launch_head_norm_forward(const HeadNormConsts& c, const pxr_heads& r, const pxr_tokens* q_out, const pxr_tokens* k_out, void* stream, std::string& err) {
-    const HeadNormShape s = shape_of(c, r.dtype, (uint64_t)r.n_envs * r.n_steps, r.n_heads, r.n_key_heads);
+    const HeadNormShape s = shape_of(c, r.dtype, (uint64_t)r.n_envs * r.n_steps, r.n_heads, r.n_key_heads, false);
     if (!s.groups || r.n_heads + r.n_key_heads == 0) return PXR_OK;
     return result(launch_typed<false>(r, s, arguments(c, r, s, q_out, k_out, nullptr, nullptr), static_cast<hipStream_t>(stream)), err);
 }
@@ -359,7 +367,7 @@ int launch_head_norm_forward(const HeadNormConsts& c, const pxr_heads& r, const 
 int launch_head_norm_backward(const HeadNormConsts& c, const pxr_heads& r, const pxr_tokens* dq_out, const pxr_tokens* dk_out, const pxr_tokens* dq,
                               const pxr_tokens* dk, void* dq_weight, void* dk_weight, void* ws, void* stream, std::string& err) {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const HeadNormShape s = shape_of(c, r.dtype, (uint64_t)r.n_envs * r.n_steps, r.n_heads, r.n_key_heads);
+    const HeadNormShape s = shape_of(c, r.dtype, (uint64_t)r.n_envs * r.n_steps, r.n_heads, r.n_key_heads, true);
     HeadNormArgs a = arguments(c, r, s, dq, dk, dq_out, dk_out);
     const bool sums = dq_weight || dk_weight;
     a.sums = sums ? static_cast<float*>(ws) : nullptr;

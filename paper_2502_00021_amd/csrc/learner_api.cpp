@@ -83,7 +83,8 @@ int pxr_orthogonalise(const pxr_orthogonalise_desc* d, const void* d_x, void* d_
     if (d->n_matrices == 0) return PXR_OK;
     const size_t n = d->dtype == PXR_F32 ? 4u : 2u;
     if (!d_x || !d_out || !aligned(d_x, n) || !aligned(d_out, n)) return refuse(call, "a buffer is null or not aligned to its elements");
-    if (!d_workspace || workspace_bytes < pxr::orthogonalise_workspace(*d) || !aligned(d_workspace, 16))
+    const size_t need = pxr::orthogonalise_workspace(*d);
+    if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
         return refuse(call, "the workspace is missing, too small or not 16-byte aligned");
     std::string err;
     const int rc = pxr::launch_orthogonalise(*d, d_x, d_out, d_workspace, hip_stream, err);

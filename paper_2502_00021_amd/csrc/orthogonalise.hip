@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -393,6 +394,178 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Product p) {
     put_planes<kKind == kPoly>(p, ah, al, th, tl, tj * 64u + row, row0 + col, w);
 }
 
+// ---- small matrices: one workgroup has one from its reading to the result, X, A and then B in LDS
+
+struct Factors {
+    float gram, poly, linear, diagonal, update;  // of the three products' sums, and of A and 1 in B
+};
+
+struct Small {
+    const void* x;
+    void* out;
+    int64_t x_matrix, x_row, out_matrix, out_row;
+    uint32_t rows, cols, s, l, sp, lp, n_steps;
+    float eps, held;
+    Factors steps[64];
+};
+
+constexpr uint32_t kSmallThreads = 512, kSmallWaves = kSmallThreads / 64;
+constexpr uint32_t kLds = 160 * 1024;
+constexpr uint32_t up32(uint32_t n) { return (n + 31u) / 32u * 32u; }
+// Rows lie 16 bytes apart from a multiple of 64, so that those of eight lanes lie in different banks.
+constexpr uint32_t small_row(uint32_t n) { return n + 8u; }
+constexpr uint32_t small_lds(uint32_t sp, uint32_t lp) { return 64u + 4u * sp * (small_row(lp) + small_row(sp)); }
+bool is_small(uint32_t s, uint32_t l) {
+    const uint32_t sp = up32(s), lp = up32(l);
+    // (the tiles of the three products that a wavefront holds at once: see the kernel)
+    return sp <= 128u && lp <= 2048u && small_lds(sp, lp) <= kLds && (sp / 32u) * (lp / 32u) <= 5u * kSmallWaves;
+}
+
+__device__ __forceinline__ f16x8 along(const half* plane, uint32_t row, uint32_t stride, uint32_t k, uint32_t lane) {
+    return *reinterpret_cast<const f16x8*>(plane + (row + (lane & 31u)) * stride + k + 8u * (lane >> 5));
+}
+__device__ __forceinline__ f16x8 across(const half* plane, uint32_t k, uint32_t stride, uint32_t col, uint32_t lane) {
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const uint32_t i = lane & 15u;
+    const half* p = plane + (k + 8u * (lane >> 5) + (i >> 2)) * stride + col + (lane & 16u) + 4u * (i & 3u);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * stride));
+    return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A number that is the same in all lanes, as one that the compiler does not know.
+__device__ __forceinline__ uint32_t again(uint32_t v) {
+    v = __builtin_amdgcn_readfirstlane(v);
+    asm volatile("" : "+s"(v));
+    return v;
+}
+
+// The sum over `depth` values of a 32 x 32 tile.  Two chains of sums, so that one instruction does not wait for the last one's result.
+template <bool kAcross>
+__device__ __forceinline__ f32x16 small_product(const half* a, uint32_t a_plane, uint32_t row, uint32_t a_stride, const half* b, uint32_t b_plane, uint32_t col, uint32_t b_stride, uint32_t depth,
+                                                uint32_t lane) {
+    f32x16 main = (f32x16)0.0f, small = (f32x16)0.0f;
+#pragma nounroll
+    for (uint32_t k = 0; k < depth; k += 16u) {
+        const f16x8 ah = along(a, row, a_stride, k, lane), al = along(a + a_plane, row, a_stride, k, lane);
+        const f16x8 bh = kAcross ? across(b, k, b_stride, col, lane) : along(b, col, b_stride, k, lane);
+        const f16x8 bl = kAcross ? across(b + b_plane, k, b_stride, col, lane) : along(b + b_plane, col, b_stride, k, lane);
+        small = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, small, 0, 0, 0);
+        main = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, main, 0, 0, 0);
+        small = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, small, 0, 0, 0);
+    }
+    return main + small;
+}
+
+__device__ __forceinline__ void small_put(half* to, uint32_t plane, uint32_t row, uint32_t stride, uint32_t col, const f32x16& v, uint32_t lane) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        half hi, lo;
+        split(v[r], hi, lo);
+        half* const at = to + (row + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * stride + col + (lane & 31u);
+        at[0] = hi;
+        at[plane] = lo;
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
+    extern __shared__ __align__(16) unsigned char small_memory[];
+    double* const sums = reinterpret_cast<double*>(small_memory);
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.x;
+    uint32_t x_stride = small_row(a.lp), s_stride = small_row(a.sp);
+    const uint32_t x_plane = a.sp * x_stride, s_plane = a.sp * s_stride;
+    half* const X = reinterpret_cast<half*>(small_memory + 64);
+    half* const S = X + 2 * x_plane;
+    const bool tall = a.rows > a.cols;
+    const T* x = static_cast<const T*>(a.x) + (int64_t)matrix * a.x_matrix;
+    for (uint32_t i = threadIdx.x; i < (2 * x_plane) / 8u; i += kSmallThreads) reinterpret_cast<uint4*>(X)[i] = make_uint4(0, 0, 0, 0);
+    double sum = 0.0;
+    for (uint32_t r = wave; r < a.rows; r += kSmallWaves)
+        for (uint32_t c = lane; c < a.cols; c += 64u) {
+            const double v = (double)load1(x + (int64_t)r * a.x_row + c);
+            sum += v * v;
+        }
+#pragma unroll
+    for (uint32_t m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (uint32_t w = 0; w < kSmallWaves; ++w) sum += sums[w];
+    const double over = (double)a.held / (sqrt(sum) + (double)a.eps);
+    for (uint32_t r = wave; r < a.rows; r += kSmallWaves)
+        for (uint32_t c = lane; c < a.cols; c += 64u) {
+            half hi, lo;
+            split((float)((double)load1(x + (int64_t)r * a.x_row + c) * over), hi, lo);
+            half* const at = X + (tall ? c * x_stride + r : r * x_stride + c);
+            at[0] = hi;
+            at[x_plane] = lo;
+        }
+    const uint32_t ti = a.sp / 32u, tj = a.lp / 32u;
+    for (uint32_t step = 0; step < a.n_steps; ++step) {
+        const Factors f = a.steps[step];
+        // (the addresses of all tiles' values, formed in front of the loop over steps, would take more registers than there are)
+        x_stride = again(x_stride);
+        s_stride = again(s_stride);
+        // A, whose tiles stay with their wavefronts
+        constexpr int kSquare = 16 / kSmallWaves, kWide = 5;
+        f32x16 of_a[kSquare];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kSquare; ++n) {
+            const uint32_t t = again(wave + n * kSmallWaves), i = t / ti * 32u, j = t % ti * 32u;
+            if (t >= ti * ti) continue;
+            of_a[n] = small_product<false>(X, x_plane, i, x_stride, X, x_plane, j, x_stride, a.lp, lane) * f.gram;
+            small_put(S, s_plane, i, s_stride, j, of_a[n], lane);
+        }
+        __syncthreads();
+        // B in A's place
+        f32x16 of_b[kSquare];
+#pragma unroll
+        for (int n = 0; n < kSquare; ++n) {
+            const uint32_t t = again(wave + n * kSmallWaves), i = t / ti * 32u, j = t % ti * 32u;
+            if (t >= ti * ti) continue;
+            of_b[n] = small_product<false>(S, s_plane, i, s_stride, S, s_plane, j, s_stride, a.sp, lane);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t row = i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3), col = j + (lane & 31u);
+                of_b[n][r] = __builtin_fmaf(of_a[n][r], f.linear, of_b[n][r] * f.poly) + (row == col && row < a.s ? f.diagonal : 0.0f);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kSquare; ++n) {
+            const uint32_t t = again(wave + n * kSmallWaves);
+            if (t < ti * ti) small_put(S, s_plane, t / ti * 32u, s_stride, t % ti * 32u, of_b[n], lane);
+        }
+        __syncthreads();
+        // X in its own place
+        f32x16 of_x[kWide];
+#pragma unroll
+        for (int n = 0; n < kWide; ++n) {
+            const uint32_t t = again(wave + n * kSmallWaves);
+            if (t < ti * tj) of_x[n] = small_product<true>(S, s_plane, t / tj * 32u, s_stride, X, x_plane, t % tj * 32u, x_stride, a.sp, lane) * f.update;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kWide; ++n) {
+            const uint32_t t = again(wave + n * kSmallWaves), i = t / tj * 32u, j = t % tj * 32u;
+            if (t >= ti * tj) continue;
+            if (step + 1u < a.n_steps) {
+                small_put(X, x_plane, i, x_stride, j, of_x[n], lane);
+                continue;
+            }
+            T* out = static_cast<T*>(a.out) + (int64_t)matrix * a.out_matrix;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t row = i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3), col = j + (lane & 31u);
+                if (row < a.s && col < a.l) out[tall ? (int64_t)col * a.out_row + row : (int64_t)row * a.out_row + col] = (T)of_x[n][r];
+            }
+        }
+    }
+}
+
 float power_below(double v) { return (float)std::exp2(std::floor(std::log2(v))); }
 
 // Bounds of the singular values, and the powers of two by which X, A and B are held: 2 less than half of fp16's largest number, so that no rounding reaches it.
@@ -437,6 +610,24 @@ Layout layout_of(const pxr_orthogonalise_desc& d) {
     return y;
 }
 
+// What the steps' sums are multiplied with; the first value is what X_0 is held times.
+float factors_of(const pxr_orthogonalise_desc& d, Factors* steps) {
+    double most = 1.0;  // of the singular values
+    const float first = power_below(kMost);
+    float held = first;
+    for (uint32_t k = 0; k < d.n_steps; ++k) {
+        const double a = d.coefficients[3 * k], b = d.coefficients[3 * k + 1], c = d.coefficients[3 * k + 2];
+        const OrthogonaliseBounds next = orthogonalise_bounds(a, b, c, most);
+        most = std::max(most, kLeast);
+        const float held_a = power_below(kMost / (most * most)), held_b = power_below(kMost / std::max(next.factor, kLeast));
+        const float held_x = k + 1u < d.n_steps ? power_below(kMost / std::max(next.most, kLeast)) : 1.0f;
+        steps[k] = {held_a / held / held, (float)(c * held_b / held_a / held_a), (float)(b * held_b / held_a), (float)(a * held_b), held_x / held_b / held};
+        held = held_x;
+        most = next.most;
+    }
+    return first;
+}
+
 template <int kKind>
 hipError_t launch_product(const Product& p, int M, uint32_t tiles, uint32_t n_matrices, hipStream_t st) {
     const dim3 grid(tiles, p.splits, n_matrices), threads(kThreads);
@@ -447,12 +638,39 @@ hipError_t launch_product(const Product& p, int M, uint32_t tiles, uint32_t n_ma
     return hipGetLastError();
 }
 
+// Small kernels' LDS is more than a kernel has by default: asked for by the first launch on a device.
+template <class T>
+hipError_t launch_small(const Small& a, uint32_t n_matrices, hipStream_t st) {
+    static std::atomic<uint64_t> devices{0};
+    int device = 0;
+    if (const hipError_t rc = hipGetDevice(&device); rc != hipSuccess) return rc;
+    const uint64_t bit = device < 64 ? 1ull << device : 0ull;
+    if (!(devices.load(std::memory_order_relaxed) & bit)) {
+        if (const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(&small_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds); rc != hipSuccess) return rc;
+        devices.fetch_or(bit, std::memory_order_relaxed);
+    }
+    hipLaunchKernelGGL((small_kernel<T>), dim3(n_matrices), dim3(kSmallThreads), small_lds(a.sp, a.lp), st, a);
+    return hipGetLastError();
+}
+
+int result(hipError_t rc, std::string& err) {
+    if (rc == hipSuccess) return PXR_OK;
+    err = std::string("kernel launch failed: ") + hipGetErrorString(rc);
+    return PXR_ERR_DEVICE;
+}
+
 }  // namespace
 
-size_t orthogonalise_workspace(const pxr_orthogonalise_desc& d) { return layout_of(d).bytes; }
+size_t orthogonalise_workspace(const pxr_orthogonalise_desc& d) { return is_small(std::min(d.rows, d.cols), std::max(d.rows, d.cols)) ? 0 : layout_of(d).bytes; }
 
 int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* out, void* ws, void* stream, std::string& err) {
     hipStream_t st = static_cast<hipStream_t>(stream);
+    const uint32_t shorter = std::min(d.rows, d.cols), longer = std::max(d.rows, d.cols);
+    if (is_small(shorter, longer)) {
+        Small a{x, out, d.x_matrix, d.x_row, d.out_matrix, d.out_row, d.rows, d.cols, shorter, longer, up32(shorter), up32(longer), d.n_steps, d.eps, 0.0f, {}};
+        a.held = factors_of(d, a.steps);
+        return result(d.dtype == PXR_F32 ? launch_small<float>(a, d.n_matrices, st) : launch_small<__bf16>(a, d.n_matrices, st), err);
+    }
     const Layout y = layout_of(d);
     char* const base = static_cast<char*>(ws);
     const auto planes = [&](size_t at, uint32_t cols) {
@@ -460,8 +678,8 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         return Planes{reinterpret_cast<half*>(base + at), matrix * d.n_matrices, matrix, cols};
     };
     const Planes xs[2] = {planes(y.x[0], y.lp), planes(y.x[1], y.lp)}, as = planes(y.a, y.sp), bs = planes(y.b, y.sp);
-    double most = 1.0;  // of the singular values
-    float held = power_below(kMost / most);
+    Factors steps[64];
+    const float held = factors_of(d, steps);
     Prepare prep{x, d.x_matrix, d.x_row, d.rows, d.cols, y.parts, reinterpret_cast<double*>(base + y.sums), xs[0], d.eps, held};
     const dim3 threads(kThreads), sums(y.parts, d.n_matrices), tiles(y.lp / 64u, y.sp / 64u, d.n_matrices);
     if (d.dtype == PXR_F32) {
@@ -472,23 +690,20 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         hipLaunchKernelGGL((split_kernel<__bf16>), tiles, threads, 0, st, prep);
     }
     hipError_t rc = hipGetLastError();
+    const auto tiles_of = [](uint32_t n, int M) { return (n + 64u * M - 1u) / (64u * M); };
     for (uint32_t k = 0; k < d.n_steps && rc == hipSuccess; ++k) {
-        const double a = d.coefficients[3 * k], b = d.coefficients[3 * k + 1], c = d.coefficients[3 * k + 2];
-        const OrthogonaliseBounds next = orthogonalise_bounds(a, b, c, most);
-        const float held_a = power_below(kMost / (most * most)), held_b = power_below(kMost / std::max(next.factor, kLeast));
-        const float held_x = power_below(kMost / std::max(next.most, kLeast));
+        const Factors& f = steps[k];
         const Planes from = xs[k & 1u], to = xs[(k + 1u) & 1u];
-        const auto triangle_of = [&](int M) { const uint32_t n = (y.s + 64u * M - 1u) / (64u * M); return n; };
         Product p{};
         // A
         p.a = p.b = from;
         p.to = as;
-        p.depth = (y.l + kDepth - 1u) / kDepth * kDepth;
-        p.tiles_i = p.tiles_j = triangle_of(y.gram);
+        p.depth = up32(y.l);
+        p.tiles_i = p.tiles_j = tiles_of(y.s, y.gram);
         p.splits = y.splits;
         p.steps_each = y.steps_each;
         p.partial = reinterpret_cast<float*>(base + y.partial);
-        p.scale = held_a / held / held;
+        p.scale = f.gram;
         p.s = y.s;
         const uint32_t gram_tiles = p.tiles_i * (p.tiles_i + 1u) / 2u;
         rc = launch_product<kGram>(p, y.gram, gram_tiles, d.n_matrices, st);
@@ -500,23 +715,22 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         // B
         p.a = p.b = as;
         p.to = bs;
-        p.depth = (y.s + kDepth - 1u) / kDepth * kDepth;
-        p.tiles_i = p.tiles_j = triangle_of(y.poly);
+        p.depth = up32(y.s);
+        p.tiles_i = p.tiles_j = tiles_of(y.s, y.poly);
         p.splits = 1u;
         p.steps_each = p.depth / kDepth;
-        p.scale = (float)(c * held_b / held_a / held_a);
-        p.c0 = (float)(a * held_b);
-        p.c1 = (float)(b * held_b / held_a);
+        p.scale = f.poly;
+        p.c0 = f.diagonal;
+        p.c1 = f.linear;
         rc = launch_product<kPoly>(p, y.poly, p.tiles_i * (p.tiles_i + 1u) / 2u, d.n_matrices, st);
         if (rc != hipSuccess) break;
         // X
-        const bool last = k + 1u == d.n_steps;
         p.a = bs;
         p.b = from;
         p.to = to;
-        p.tiles_i = triangle_of(y.update);
-        p.tiles_j = (y.l + 64u * y.update - 1u) / (64u * y.update);
-        p.scale = (last ? 1.0f : held_x) / held_b / held;
+        p.tiles_i = tiles_of(y.s, y.update);
+        p.tiles_j = tiles_of(y.l, y.update);
+        p.scale = f.update;
         p.out = out;
         p.out_matrix = d.out_matrix;
         p.out_row = d.out_row;
@@ -524,14 +738,10 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         p.cols = d.cols;
         p.transposed = d.rows > d.cols;
         p.bf16 = d.dtype == PXR_BF16;
-        rc = last ? launch_product<kLast>(p, y.update, p.tiles_i * p.tiles_j, d.n_matrices, st)
-                  : launch_product<kUpdate>(p, y.update, p.tiles_i * p.tiles_j, d.n_matrices, st);
-        held = held_x;
-        most = std::max(next.most, kLeast);
+        rc = k + 1u == d.n_steps ? launch_product<kLast>(p, y.update, p.tiles_i * p.tiles_j, d.n_matrices, st)
+                                 : launch_product<kUpdate>(p, y.update, p.tiles_i * p.tiles_j, d.n_matrices, st);
     }
-    if (rc == hipSuccess) return PXR_OK;
-    err = std::string("kernel launch failed: ") + hipGetErrorString(rc);
-    return PXR_ERR_DEVICE;
+    return result(rc, err);
 }
 
 }  // namespace pxr

@@ -49,9 +49,12 @@ def test_buffers():
         for bad in (None, 66 if i < 2 else 72):
             b = [64, 64, 64]
             b[i] = bad
-            assert _call(buffers=b)[1] == pxr.ERR_INVALID_ARG, (i, bad)
-    need = _call()[2]
-    assert need > 0 and _call(workspace=need - 1)[1] == pxr.ERR_INVALID_ARG
+            if i < 2:
+                assert _call(buffers=b)[1] == pxr.ERR_INVALID_ARG, (i, bad)
+            large = dict(rows=300, cols=400, x_row=400, out_row=400)
+            assert _call(buffers=b, **large)[1] == pxr.ERR_INVALID_ARG, (i, bad)
+    need = _call(**large)[2]
+    assert need > 0 and _call(workspace=need - 1, **large)[1] == pxr.ERR_INVALID_ARG
     assert _call(n_matrices=0, buffers=(None, None, None), workspace=0) == (pxr.OK, pxr.OK, 0)  # nothing to do
 
 
