@@ -32,7 +32,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kThreads = 256;
 constexpr uint32_t kPad = 128;       // rows and columns of the matrices in the workspace come in multiples of it; what is behind the matrix is zeros
-constexpr uint32_t kNormParts = 256; // of a matrix whose squares are summed, at most
+constexpr uint32_t kNormParts = 512; // of a matrix whose squares are summed, at most
 constexpr uint32_t kNormColumns = 1024;
 constexpr uint32_t kDepth = 32;      // values of the summed axis in LDS at a time
 
@@ -69,11 +69,17 @@ __global__ __launch_bounds__(kThreads) void square_sums_kernel(const Prepare a) 
     for (uint64_t u = part; u < (uint64_t)a.rows * per_row; u += a.parts) {
         const uint32_t r = (uint32_t)(u / per_row), c0 = (uint32_t)(u - (uint64_t)r * per_row) * kNormColumns;
         const T* row = x + (int64_t)r * a.x_row;
-        const uint32_t end = min(c0 + kNormColumns, a.cols);
-        for (uint32_t c = c0 + threadIdx.x; c < end; c += kThreads) {
-            const double v = (double)load1(row + c);
-            sum += v * v;
+        constexpr uint32_t kEach = kNormColumns / kThreads;
+        const uint32_t c = c0 + threadIdx.x * kEach;
+        T v[kEach];
+        if (c + kEach <= a.cols) {
+            __builtin_memcpy(v, row + c, sizeof(v));  // (at the address of any value)
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < kEach; ++e) v[e] = c + e < a.cols ? row[c + e] : (T)0.0f;
         }
+#pragma unroll
+        for (uint32_t e = 0; e < kEach; ++e) sum += (double)load1(v + e) * (double)load1(v + e);
     }
 #pragma unroll
     for (uint32_t m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
@@ -153,20 +159,54 @@ __device__ __forceinline__ void triangle(uint32_t t, uint32_t& i, uint32_t& j) {
     j = t - i * (i + 1u) / 2u;
 }
 
-// A tile's operand in LDS, one plane, kDepth values deep.  Along: rows of 64 bytes, 4 chunks of 8 values, chunk c of row r at place c ^ (r / 2 % 4): eight rows' chunks of one c lie in different banks.
-// Across (the summed axis is the rows'): rows of `kSide` values, chunk c of row k at place c ^ 2 (k % 4): four rows' pairs of chunks, as the transposing read takes them, lie in different
-// banks.  The requests that write LDS put a wavefront's lanes side by side, so it is the addresses that they ask for which are exchanged.
+// The order in which tiles are taken: workgroups go to the eight dies in turn, so a die has a run of this order, and tiles that follow each other in it read the same
+// rows and columns: bands of kBand rows of tiles, column by column.
+constexpr uint32_t kDies = 8, kBand = 4;
+__device__ __forceinline__ uint32_t in_order(uint32_t group, uint32_t groups) { return group % kDies * (groups / kDies) + group / kDies; }
+__device__ __forceinline__ void of_band(uint32_t t, uint32_t rows, uint32_t cols, uint32_t& i, uint32_t& j) {
+    const uint32_t band = t / (kBand * cols), r = t - band * kBand * cols, high = min(kBand, rows - band * kBand);
+    j = r / high;
+    i = band * kBand + r - j * high;
+}
+// Of a symmetric product's lower triangle of tiles.  `whole` bands have 4 columns of tiles each for every band before them, and a triangle; rows behind the last whole band come one by
+// one.
+__device__ __forceinline__ void of_triangle(uint32_t t, uint32_t rows, uint32_t& i, uint32_t& j) {
+    const auto before = [](uint32_t band) { return 8u * band * band + 2u * band; };
+    const uint32_t whole = rows / kBand;
+    if (t >= before(whole)) return triangle(t - before(whole) + whole * kBand * (whole * kBand + 1u) / 2u, i, j);
+    uint32_t band = (uint32_t)__builtin_sqrtf((float)t * 0.125f);
+    while (before(band) > t) --band;
+    while (before(band + 1u) <= t) ++band;
+    const uint32_t r = t - before(band), left = band * kBand;
+    if (r < left * kBand) {
+        j = r / kBand;
+        i = left + r % kBand;
+    } else {
+        triangle(r - left * kBand, i, j);
+        i += left;
+        j += left;
+    }
+}
+
+// A tile's operand in LDS, one plane, kDepth values deep.  Along: rows of 64 bytes, 4 chunks of 8 values, chunk c of row r at place c ^ (r / 4 % 4): the 16 rows whose chunks of one c are
+// read together lie in the 64 banks once each.  Across (the summed axis is the rows'): rows of `kSide` values; the transposing read takes 32 values of four rows together, chunks of them at place
+// c ^ 4 (k % 4), or where two rows are 256 bytes c ^ 4 (k / 2 % 2).  The requests that write LDS put a wavefront's lanes side by side, so it is the addresses that they ask for which are
+// exchanged.  (Exchanged for 32 banks, half of the LDS' cycles were conflicts: 4096 x 4096 bfloat16 5250 us.)
 template <int kSide, bool kAcross>
 struct Operand {
     static constexpr uint32_t kChunks = kSide * kDepth / 8;  // of 16 bytes, in a plane
+    static __device__ __forceinline__ uint32_t turn(uint32_t row) {
+        if (!kAcross) return row >> 2 & 3u;
+        return kSide == 128 ? (row & 3u) << 2 : (row >> 1 & 1u) << 2;
+    }
     // Which value chunk number i of the plane is: row and column in the tile.
     static __device__ __forceinline__ void place(uint32_t i, uint32_t& row, uint32_t& col) {
         if (kAcross) {
             row = i / (kSide / 8);
-            col = ((i % (kSide / 8)) ^ ((row & 3u) << 1)) * 8u;
+            col = ((i % (kSide / 8)) ^ turn(row)) * 8u;
         } else {
             row = i / 4u;
-            col = ((i % 4u) ^ (row >> 1 & 3u)) * 8u;
+            col = ((i % 4u) ^ turn(row)) * 8u;
         }
     }
     // Eight values of the summed axis, 16 k + 8 h .. + 7, of line lane % 32 from `line` on.
@@ -175,13 +215,13 @@ struct Operand {
         if constexpr (kAcross) {
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
             const uint32_t i = lane & 15u, row = 16u * k + 8u * h + (i >> 2), col = line + (lane & 16u) + 4u * (i & 3u);
-            const half* p = plane + row * kSide + (((col >> 3) ^ ((row & 3u) << 1)) << 3) + (col & 7u);
+            const half* p = plane + row * kSide + (((col >> 3) ^ turn(row)) << 3) + (col & 7u);  // (four rows on: turned alike)
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * kSide));
             return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             const uint32_t row = line + (lane & 31u);
-            return *reinterpret_cast<const f16x8*>(plane + row * kDepth + (((2u * k + h) ^ (row >> 1 & 3u)) << 3));
+            return *reinterpret_cast<const f16x8*>(plane + row * kDepth + (((2u * k + h) ^ turn(row)) << 3));
         }
     }
 };
@@ -231,23 +271,26 @@ __device__ __forceinline__ void put_out(const Product& p, uint32_t matrix, uint3
 }
 
 // A tile of 64 M x 64 M values by four wavefronts, 2 x 2, each 32 M x 32 M.
+constexpr uint32_t stages(int M) { return M == 2 ? 2u : 4u; }
+
 template <int kKind, int M>
 __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
     constexpr int kSide = 64 * M;
+    constexpr uint32_t kStages = stages(M);  // of kDepth values in LDS: one that is worked on, the others on their way
     constexpr bool kSym = kKind <= kPoly;
     typedef Operand<kSide, false> OpA;
     typedef Operand<kSide, !kSym> OpB;
     constexpr uint32_t kPlane = kSide * kDepth, kStage = 4 * kPlane;  // halves: A hi, A lo, B hi, B lo
-    __shared__ __align__(16) half stage[2][kStage];
+    __shared__ __align__(16) half stage[kStages][kStage];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.z;
+    const uint32_t tiles = kSym ? p.tiles_i * (p.tiles_i + 1u) / 2u : p.tiles_i * p.tiles_j, place = in_order(blockIdx.x, gridDim.x);
+    if (place >= tiles * p.splits) return;
+    const uint32_t part = place / tiles, tile = place - part * tiles;
     uint32_t ti, tj;
-    const uint32_t tile = blockIdx.x, part = blockIdx.y;
     if (kSym)
-        triangle(tile, ti, tj);
-    else {
-        ti = tile % p.tiles_i;
-        tj = tile / p.tiles_i;
-    }
+        of_triangle(tile, p.tiles_i, ti, tj);
+    else
+        of_band(tile, p.tiles_i, p.tiles_j, ti, tj);
     const uint32_t i0 = ti * kSide, j0 = tj * kSide;
     // each wavefront asks for every fourth run of 64 chunks of each plane
     constexpr uint32_t kRuns = OpA::kChunks / 64 / 4;
@@ -285,12 +328,21 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
         for (int j = 0; j < M; ++j) acc[i][j] = (f32x16)0.0f;
     const uint32_t row0 = (wave >> 1) * 32 * M, col0 = (wave & 1u) * 32 * M;
     const uint32_t steps = min(p.steps_each, p.depth / kDepth - part * p.steps_each);
-    ask(stage[0]);
+    for (uint32_t k = 0; k + 1u < kStages && k < steps; ++k) ask(stage[k]);
+    uint32_t now = 0, next = kStages - 1u;
     for (uint32_t k = 0; k < steps; ++k) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (k + 1u < steps) ask(stage[(k + 1u) & 1u]);
-        const half* from = stage[k & 1u];
+        // the oldest stage is there (requests are answered in their order); towards the end fewer are on their way, and all are waited for
+        // (a barrier by itself: __syncthreads would wait for all of them.  The values that were read of the stage that is asked for next have been used.)
+        if (k + kStages - 1u <= steps)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2u) * kRuns * 4u) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (k + kStages - 1u < steps) ask(stage[next]);
+        const half* from = stage[now];
+        now = now + 1u == kStages ? 0u : now + 1u;
+        next = next + 1u == kStages ? 0u : next + 1u;
 #pragma unroll
         for (uint32_t kk = 0; kk < kDepth / 16; ++kk) {
             f16x8 a[M][2], b[M][2];
@@ -314,7 +366,6 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
     // a lane has column lane % 32 and rows 8 (r / 4) + 4 (lane / 32) + r % 4 of every 32 x 32
     const uint32_t down = 4u * (lane >> 5), across = lane & 31u;
     if (kSym && p.splits > 1u) {
-        const uint32_t tiles = p.tiles_i * (p.tiles_i + 1u) / 2u;
         float* to = p.partial + (((size_t)matrix * p.splits + part) * tiles + tile) * (kSide * kSide);
 #pragma unroll
         for (int i = 0; i < M; ++i)
@@ -374,7 +425,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Product p) {
     __shared__ float turned[64][17];
     const uint32_t tile = blockIdx.x / 4u, strip = blockIdx.x % 4u, matrix = blockIdx.z, tiles = p.tiles_i * (p.tiles_i + 1u) / 2u;
     uint32_t ti, tj;
-    triangle(tile, ti, tj);
+    of_triangle(tile, p.tiles_i, ti, tj);
     const uint32_t r = threadIdx.x >> 4, c = (threadIdx.x & 15u) * 4u;
     const float* from = p.partial + ((size_t)matrix * p.splits * tiles + tile) * 4096u + (strip * 16u + r) * 64u + c;
     f32x4 v = (f32x4)0.0f;
@@ -630,7 +681,7 @@ float factors_of(const pxr_orthogonalise_desc& d, Factors* steps) {
 
 template <int kKind>
 hipError_t launch_product(const Product& p, int M, uint32_t tiles, uint32_t n_matrices, hipStream_t st) {
-    const dim3 grid(tiles, p.splits, n_matrices), threads(kThreads);
+    const dim3 grid((tiles * p.splits + kDies - 1u) / kDies * kDies, 1, n_matrices), threads(kThreads);
     if (M == 2)
         hipLaunchKernelGGL((product_kernel<kKind, 2>), grid, threads, 0, st, p);
     else
