@@ -141,8 +141,9 @@ enum { kGram, kPoly, kUpdate, kLast };
 struct Product {
     Planes a, b, to;     // kGram: X, X -> A;  kPoly: A, A -> B;  kUpdate: B, X -> X;  kLast: B, X -> out
     uint32_t depth;      // the summed axis, a multiple of kDepth
-    uint32_t tiles_i, tiles_j, splits, steps_each;  // steps of kDepth that a split takes
-    float* partial;      // [matrices][splits][tiles][tile][tile], splits > 1
+    uint32_t tiles_i, tiles_j;
+    uint32_t whole, splits, steps_each;  // tiles from number `whole` on are cut along the summed axis: into `splits` parts of steps_each steps of kDepth
+    float* partial;      // [matrices][splits][tiles - whole][tile][tile]
     float scale;         // of the sums
     float c0, c1;        // kPoly: on the diagonal; times A's held values
     uint32_t s;          // rows with a diagonal
@@ -162,6 +163,7 @@ __device__ __forceinline__ void triangle(uint32_t t, uint32_t& i, uint32_t& j) {
 // The order in which tiles are taken: workgroups go to the eight dies in turn, so a die has a run of this order, and tiles that follow each other in it read the same
 // rows and columns: bands of kBand rows of tiles, column by column.
 constexpr uint32_t kDies = 8, kBand = 4;
+__host__ __device__ constexpr uint32_t on_dies(uint32_t groups) { return (groups + kDies - 1u) / kDies * kDies; }
 __device__ __forceinline__ uint32_t in_order(uint32_t group, uint32_t groups) { return group % kDies * (groups / kDies) + group / kDies; }
 __device__ __forceinline__ void of_band(uint32_t t, uint32_t rows, uint32_t cols, uint32_t& i, uint32_t& j) {
     const uint32_t band = t / (kBand * cols), r = t - band * kBand * cols, high = min(kBand, rows - band * kBand);
@@ -283,9 +285,12 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
     constexpr uint32_t kPlane = kSide * kDepth, kStage = 4 * kPlane;  // halves: A hi, A lo, B hi, B lo
     __shared__ __align__(16) half stage[kStages][kStage];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.z;
-    const uint32_t tiles = kSym ? p.tiles_i * (p.tiles_i + 1u) / 2u : p.tiles_i * p.tiles_j, place = in_order(blockIdx.x, gridDim.x);
-    if (place >= tiles * p.splits) return;
-    const uint32_t part = place / tiles, tile = place - part * tiles;
+    // (whole tiles and parts of tiles each in their own order: every die has as many of both)
+    const uint32_t tiles = kSym ? p.tiles_i * (p.tiles_i + 1u) / 2u : p.tiles_i * p.tiles_j, cut = tiles - p.whole, of_whole = on_dies(p.whole);
+    const bool partly = blockIdx.x >= of_whole;
+    const uint32_t place = partly ? in_order(blockIdx.x - of_whole, gridDim.x - of_whole) : in_order(blockIdx.x, of_whole);
+    if (place >= (partly ? cut * p.splits : p.whole)) return;
+    const uint32_t part = partly ? place / cut : 0u, tile = partly ? p.whole + place - part * cut : place;
     uint32_t ti, tj;
     if (kSym)
         of_triangle(tile, p.tiles_i, ti, tj);
@@ -327,7 +332,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
 #pragma unroll
         for (int j = 0; j < M; ++j) acc[i][j] = (f32x16)0.0f;
     const uint32_t row0 = (wave >> 1) * 32 * M, col0 = (wave & 1u) * 32 * M;
-    const uint32_t steps = min(p.steps_each, p.depth / kDepth - part * p.steps_each);
+    const uint32_t left = p.depth / kDepth - part * p.steps_each, steps = partly ? min(p.steps_each, left) : left;
     for (uint32_t k = 0; k + 1u < kStages && k < steps; ++k) ask(stage[k]);
     uint32_t now = 0, next = kStages - 1u;
     for (uint32_t k = 0; k < steps; ++k) {
@@ -365,8 +370,8 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
     }
     // a lane has column lane % 32 and rows 8 (r / 4) + 4 (lane / 32) + r % 4 of every 32 x 32
     const uint32_t down = 4u * (lane >> 5), across = lane & 31u;
-    if (kSym && p.splits > 1u) {
-        float* to = p.partial + (((size_t)matrix * p.splits + part) * tiles + tile) * (kSide * kSide);
+    if (kSym && partly) {
+        float* to = p.partial + (((size_t)matrix * p.splits + part) * cut + tile - p.whole) * (kSide * kSide);
 #pragma unroll
         for (int i = 0; i < M; ++i)
 #pragma unroll
@@ -419,30 +424,31 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
     }
 }
 
-// A symmetric product whose summed axis was cut: the parts' sums in their order, 16 rows of a tile a workgroup.
-template <int kKind>
+// The tiles of a symmetric product whose summed axis was cut: the parts' sums in their order, 16 x 64 values of a tile a workgroup.
+template <int kKind, int M>
 __global__ __launch_bounds__(kThreads) void join_kernel(const Product p) {
+    constexpr uint32_t kSide = 64 * M, kValues = kSide * kSide;
     __shared__ float turned[64][17];
-    const uint32_t tile = blockIdx.x / 4u, strip = blockIdx.x % 4u, matrix = blockIdx.z, tiles = p.tiles_i * (p.tiles_i + 1u) / 2u;
+    const uint32_t cut = p.tiles_i * (p.tiles_i + 1u) / 2u - p.whole, tile = blockIdx.x / (4u * M * M), place = blockIdx.x % (4u * M * M), matrix = blockIdx.z;
     uint32_t ti, tj;
-    of_triangle(tile, p.tiles_i, ti, tj);
-    const uint32_t r = threadIdx.x >> 4, c = (threadIdx.x & 15u) * 4u;
-    const float* from = p.partial + ((size_t)matrix * p.splits * tiles + tile) * 4096u + (strip * 16u + r) * 64u + c;
+    of_triangle(p.whole + tile, p.tiles_i, ti, tj);
+    const uint32_t row_in = place / M * 16u, col_in = place % M * 64u, r = threadIdx.x >> 4, c = (threadIdx.x & 15u) * 4u;
+    const float* from = p.partial + ((size_t)matrix * p.splits * cut + tile) * kValues + (row_in + r) * kSide + col_in + c;
     f32x4 v = (f32x4)0.0f;
 #pragma unroll 8
-    for (uint32_t s = 0; s < p.splits; ++s) v += *reinterpret_cast<const f32x4*>(from + (size_t)s * tiles * 4096u);
+    for (uint32_t s = 0; s < p.splits; ++s) v += *reinterpret_cast<const f32x4*>(from + (size_t)s * cut * kValues);
     v *= p.scale;
     const half *ah = p.a.at(0, matrix), *al = p.a.at(1, matrix);
     half *th = p.to.at(0, matrix), *tl = p.to.at(1, matrix);
-    const uint32_t row0 = ti * 64u + strip * 16u;
-    put_planes<kKind == kPoly>(p, ah, al, th, tl, row0 + r, tj * 64u + c, v);
+    const uint32_t row0 = ti * kSide + row_in, col0 = tj * kSide + col_in;
+    put_planes<kKind == kPoly>(p, ah, al, th, tl, row0 + r, col0 + c, v);
     if (ti == tj) return;
 #pragma unroll
     for (int e = 0; e < 4; ++e) turned[c + e][r] = v[e];
     __syncthreads();
     const uint32_t row = threadIdx.x >> 2, col = (threadIdx.x & 3u) * 4u;
     const f32x4 w{turned[row][col], turned[row][col + 1], turned[row][col + 2], turned[row][col + 3]};
-    put_planes<kKind == kPoly>(p, ah, al, th, tl, tj * 64u + row, row0 + col, w);
+    put_planes<kKind == kPoly>(p, ah, al, th, tl, col0 + row, row0 + col, w);
 }
 
 // ---- small matrices: one workgroup has one from its reading to the result, X, A and then B in LDS
@@ -622,12 +628,39 @@ float power_below(double v) { return (float)std::exp2(std::floor(std::log2(v)));
 // Bounds of the singular values, and the powers of two by which X, A and B are held: 2 less than half of fp16's largest number, so that no rounding reaches it.
 constexpr double kMost = 30000.0, kLeast = 1e-9;
 
+// How a symmetric product is cut.
+struct Cut {
+    int M;
+    uint32_t whole, splits, steps_each;
+};
+
 struct Layout {
     uint32_t s, l, sp, lp, parts;
-    int gram, poly, update;  // M of the products' tiles
-    uint32_t splits, steps_each;
+    Cut gram, poly;
+    int update;  // M of its tiles
     size_t sums, partial, x[2], a, b, bytes;  // offsets
 };
+
+constexpr uint64_t kLargeTiles = 136;  // tiles of 128 x 128 from which on they are taken
+constexpr uint64_t kPlaces = 512;  // workgroups that a device has room for at once, two on a compute unit
+
+uint32_t tiles_of(uint32_t n, int M) { return (n + 64u * M - 1u) / (64u * M); }
+uint32_t triangle_of(uint32_t s, int M) { return tiles_of(s, M) * (tiles_of(s, M) + 1u) / 2u; }
+
+// Tiles that do not fill the places, and those that are left when the others have filled them some times, are cut along the summed axis; no part has fewer than 8 steps.
+Cut cut_of(uint32_t s, uint32_t depth, uint32_t n_matrices) {
+    Cut c{};
+    c.M = triangle_of(s, 2) * (uint64_t)n_matrices >= kLargeTiles ? 2 : 1;
+    const uint32_t tiles = triangle_of(s, c.M), steps = (depth + kDepth - 1u) / kDepth;
+    const uint64_t all = (uint64_t)tiles * n_matrices;
+    c.whole = all < kPlaces ? 0u : n_matrices == 1u ? (uint32_t)(tiles / kPlaces * kPlaces) : tiles;
+    const uint64_t left = (uint64_t)(tiles - c.whole) * n_matrices;
+    c.splits = left ? (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(steps / 8u, kPlaces / left)) : 1u;
+    c.steps_each = (steps + c.splits - 1u) / c.splits;
+    c.splits = (steps + c.steps_each - 1u) / c.steps_each;
+    if (c.splits == 1u) c.whole = tiles;
+    return c;
+}
 
 Layout layout_of(const pxr_orthogonalise_desc& d) {
     Layout y{};
@@ -637,23 +670,18 @@ Layout layout_of(const pxr_orthogonalise_desc& d) {
     y.lp = padded(y.l);
     const uint64_t units = (uint64_t)d.rows * ((d.cols + kNormColumns - 1u) / kNormColumns);
     y.parts = (uint32_t)std::min<uint64_t>(kNormParts, units);
-    const auto tiles = [](uint32_t n, uint32_t side) { return (uint64_t)((n + side - 1u) / side); };
-    const auto triangle_of = [&](uint32_t side) { return tiles(y.s, side) * (tiles(y.s, side) + 1u) / 2u * d.n_matrices; };
-    y.gram = y.poly = triangle_of(128u) >= 256u ? 2 : 1;
-    y.update = tiles(y.s, 128u) * tiles(y.l, 128u) * d.n_matrices >= 256u ? 2 : 1;
-    const uint32_t depth = (y.l + kDepth - 1u) / kDepth;
-    y.splits = 1u;
-    if (y.gram == 1 && triangle_of(64u) < 256u) y.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(depth / 8u, 512u / triangle_of(64u)));
-    y.steps_each = (depth + y.splits - 1u) / y.splits;
-    y.splits = (depth + y.steps_each - 1u) / y.steps_each;
+    y.gram = cut_of(y.s, y.l, d.n_matrices);
+    y.poly = cut_of(y.s, y.s, d.n_matrices);
+    y.update = (uint64_t)tiles_of(y.s, 2) * tiles_of(y.l, 2) * d.n_matrices >= 256u ? 2 : 1;
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t from = at;
         at += (bytes + 255u) & ~(size_t)255u;
         return from;
     };
+    const auto partial = [&](const Cut& c) { return (size_t)(triangle_of(y.s, c.M) - c.whole) * d.n_matrices * c.splits * (4096u * c.M * c.M) * sizeof(float); };
     y.sums = take((size_t)d.n_matrices * y.parts * sizeof(double));
-    y.partial = take(y.splits > 1u ? (size_t)triangle_of(64u) * y.splits * 4096u * sizeof(float) : 0u);
+    y.partial = take(std::max(partial(y.gram), partial(y.poly)));
     for (size_t& x : y.x) x = take((size_t)2 * d.n_matrices * y.sp * y.lp * sizeof(half));
     y.a = take((size_t)2 * d.n_matrices * y.sp * y.sp * sizeof(half));
     y.b = take((size_t)2 * d.n_matrices * y.sp * y.sp * sizeof(half));
@@ -680,12 +708,21 @@ float factors_of(const pxr_orthogonalise_desc& d, Factors* steps) {
 }
 
 template <int kKind>
-hipError_t launch_product(const Product& p, int M, uint32_t tiles, uint32_t n_matrices, hipStream_t st) {
-    const dim3 grid((tiles * p.splits + kDies - 1u) / kDies * kDies, 1, n_matrices), threads(kThreads);
+hipError_t launch_product(const Product& p, int M, uint32_t n_matrices, hipStream_t st) {
+    constexpr bool kSym = kKind <= kPoly;
+    const uint32_t tiles = kSym ? p.tiles_i * (p.tiles_i + 1u) / 2u : p.tiles_i * p.tiles_j, cut = tiles - p.whole;
+    const dim3 grid(on_dies(p.whole) + on_dies(cut * p.splits), 1, n_matrices), threads(kThreads), joined(cut * 4u * M * M, 1, n_matrices);
     if (M == 2)
         hipLaunchKernelGGL((product_kernel<kKind, 2>), grid, threads, 0, st, p);
     else
         hipLaunchKernelGGL((product_kernel<kKind, 1>), grid, threads, 0, st, p);
+    if constexpr (kSym)
+        if (cut) {
+            if (M == 2)
+                hipLaunchKernelGGL((join_kernel<kKind, 2>), joined, threads, 0, st, p);
+            else
+                hipLaunchKernelGGL((join_kernel<kKind, 1>), joined, threads, 0, st, p);
+        }
     return hipGetLastError();
 }
 
@@ -741,7 +778,12 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         hipLaunchKernelGGL((split_kernel<__bf16>), tiles, threads, 0, st, prep);
     }
     hipError_t rc = hipGetLastError();
-    const auto tiles_of = [](uint32_t n, int M) { return (n + 64u * M - 1u) / (64u * M); };
+    const auto cut_as = [](Product& p, const Cut& c, uint32_t s) {
+        p.tiles_i = p.tiles_j = tiles_of(s, c.M);
+        p.whole = c.whole;
+        p.splits = c.splits;
+        p.steps_each = c.steps_each;
+    };
     for (uint32_t k = 0; k < d.n_steps && rc == hipSuccess; ++k) {
         const Factors& f = steps[k];
         const Planes from = xs[k & 1u], to = xs[(k + 1u) & 1u];
@@ -750,30 +792,21 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         p.a = p.b = from;
         p.to = as;
         p.depth = up32(y.l);
-        p.tiles_i = p.tiles_j = tiles_of(y.s, y.gram);
-        p.splits = y.splits;
-        p.steps_each = y.steps_each;
+        cut_as(p, y.gram, y.s);
         p.partial = reinterpret_cast<float*>(base + y.partial);
         p.scale = f.gram;
         p.s = y.s;
-        const uint32_t gram_tiles = p.tiles_i * (p.tiles_i + 1u) / 2u;
-        rc = launch_product<kGram>(p, y.gram, gram_tiles, d.n_matrices, st);
-        if (rc == hipSuccess && y.splits > 1u) {
-            hipLaunchKernelGGL((join_kernel<kGram>), dim3(gram_tiles * 4u, 1, d.n_matrices), threads, 0, st, p);
-            rc = hipGetLastError();
-        }
+        rc = launch_product<kGram>(p, y.gram.M, d.n_matrices, st);
         if (rc != hipSuccess) break;
         // B
         p.a = p.b = as;
         p.to = bs;
         p.depth = up32(y.s);
-        p.tiles_i = p.tiles_j = tiles_of(y.s, y.poly);
-        p.splits = 1u;
-        p.steps_each = p.depth / kDepth;
+        cut_as(p, y.poly, y.s);
         p.scale = f.poly;
         p.c0 = f.diagonal;
         p.c1 = f.linear;
-        rc = launch_product<kPoly>(p, y.poly, p.tiles_i * (p.tiles_i + 1u) / 2u, d.n_matrices, st);
+        rc = launch_product<kPoly>(p, y.poly.M, d.n_matrices, st);
         if (rc != hipSuccess) break;
         // X
         p.a = bs;
@@ -781,6 +814,8 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         p.to = to;
         p.tiles_i = tiles_of(y.s, y.update);
         p.tiles_j = tiles_of(y.l, y.update);
+        p.whole = p.tiles_i * p.tiles_j;
+        p.splits = 1u;
         p.scale = f.update;
         p.out = out;
         p.out_matrix = d.out_matrix;
@@ -789,8 +824,8 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         p.cols = d.cols;
         p.transposed = d.rows > d.cols;
         p.bf16 = d.dtype == PXR_BF16;
-        rc = k + 1u == d.n_steps ? launch_product<kLast>(p, y.update, p.tiles_i * p.tiles_j, d.n_matrices, st)
-                                 : launch_product<kUpdate>(p, y.update, p.tiles_i * p.tiles_j, d.n_matrices, st);
+        rc = k + 1u == d.n_steps ? launch_product<kLast>(p, y.update, d.n_matrices, st)
+                                 : launch_product<kUpdate>(p, y.update, d.n_matrices, st);
     }
     return result(rc, err);
 }
