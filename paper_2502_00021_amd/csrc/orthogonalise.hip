@@ -497,31 +497,49 @@ __device__ __forceinline__ uint32_t again(uint32_t v) {
     return v;
 }
 
-// The sum over `depth` values of a 32 x 32 tile.  Two chains of sums, so that one instruction does not wait for the last one's result.
+// The sum over `depth` values (a multiple of 32) of a 32 x 32 tile.  Two chains of sums, and 32 values' operands asked for together, so that one instruction does not wait for the last
+// one's result.  A lane has column lane % 32 of the tile and rows 8 (r / 4) + 4 (lane / 32) + r % 4.  kAcross: the rows are a's columns.
 template <bool kAcross>
 __device__ __forceinline__ f32x16 small_product(const half* a, uint32_t a_plane, uint32_t row, uint32_t a_stride, const half* b, uint32_t b_plane, uint32_t col, uint32_t b_stride, uint32_t depth,
                                                 uint32_t lane) {
-    f32x16 main = (f32x16)0.0f, small = (f32x16)0.0f;
+    f32x16 sum[2];
+    const auto add = [&](uint32_t k, const f32x16& from0, const f32x16& from1) {
+        f16x8 x[2][2], y[2][2];
+#pragma unroll
+        for (uint32_t n = 0; n < 2; ++n)
+#pragma unroll
+            for (uint32_t plane = 0; plane < 2; ++plane) {
+                x[n][plane] = kAcross ? across(a + plane * a_plane, k + 16u * n, a_stride, row, lane) : along(a + plane * a_plane, row, a_stride, k + 16u * n, lane);
+                y[n][plane] = along(b + plane * b_plane, col, b_stride, k + 16u * n, lane);
+            }
+        sum[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[0][0], y[0][1], from0, 0, 0, 0);
+        sum[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[0][1], y[0][0], from1, 0, 0, 0);
+        sum[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[0][0], y[0][0], sum[0], 0, 0, 0);
+        sum[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[1][1], y[1][0], sum[1], 0, 0, 0);
+        sum[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[1][0], y[1][1], sum[0], 0, 0, 0);
+        sum[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[1][0], y[1][0], sum[1], 0, 0, 0);
+    };
+    add(0, (f32x16)0.0f, (f32x16)0.0f);
 #pragma nounroll
-    for (uint32_t k = 0; k < depth; k += 16u) {
-        const f16x8 ah = along(a, row, a_stride, k, lane), al = along(a + a_plane, row, a_stride, k, lane);
-        const f16x8 bh = kAcross ? across(b, k, b_stride, col, lane) : along(b, col, b_stride, k, lane);
-        const f16x8 bl = kAcross ? across(b + b_plane, k, b_stride, col, lane) : along(b + b_plane, col, b_stride, k, lane);
-        small = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, small, 0, 0, 0);
-        main = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, main, 0, 0, 0);
-        small = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, small, 0, 0, 0);
-    }
-    return main + small;
+    for (uint32_t k = 32; k < depth; k += 32u) add(k, sum[0], sum[1]);
+    return sum[0] + sum[1];
 }
 
+// The tile's transpose, at row `col` and column `row` of a matrix in LDS: four values lie together.
 __device__ __forceinline__ void small_put(half* to, uint32_t plane, uint32_t row, uint32_t stride, uint32_t col, const f32x16& v, uint32_t lane) {
+    half* const at = to + (col + (lane & 31u)) * stride + row + 4 * (lane >> 5);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        half hi, lo;
-        split(v[r], hi, lo);
-        half* const at = to + (row + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * stride + col + (lane & 31u);
-        at[0] = hi;
-        at[plane] = lo;
+    for (int q = 0; q < 4; ++q) {
+        f16x4 hi, lo;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            half h, l;
+            split(v[4 * q + r], h, l);
+            hi[r] = h;
+            lo[r] = l;
+        }
+        *reinterpret_cast<f16x4*>(at + 8 * q) = hi;
+        *reinterpret_cast<f16x4*>(at + plane + 8 * q) = lo;
     }
 }
 
@@ -537,12 +555,37 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
     const bool tall = a.rows > a.cols;
     const T* x = static_cast<const T*>(a.x) + (int64_t)matrix * a.x_matrix;
     for (uint32_t i = threadIdx.x; i < (2 * x_plane) / 8u; i += kSmallThreads) reinterpret_cast<uint4*>(X)[i] = make_uint4(0, 0, 0, 0);
-    double sum = 0.0;
-    for (uint32_t r = wave; r < a.rows; r += kSmallWaves)
-        for (uint32_t c = lane; c < a.cols; c += 64u) {
-            const double v = (double)load1(x + (int64_t)r * a.x_row + c);
-            sum += v * v;
+    // The update is read twice (the second time from the caches), four values of a row a lane.  One compute unit's instructions are what it costs: where a value took 40 of them, 64 x 448 values
+    // took 25 us.
+    const uint32_t per_row = (a.cols + 3u) / 4u, quads = a.rows * per_row, over_row = 0xFFFFFFFFu / per_row + 1u;  // (quads * per_row < 2^32: the quotient below is exact)
+    const auto each = [&](auto&& use) {
+        constexpr uint32_t kAhead = 4;
+        for (uint32_t first = threadIdx.x; first < quads; first += kSmallThreads * kAhead) {
+            T v[kAhead][4];
+            uint32_t row[kAhead], col[kAhead];
+#pragma unroll
+            for (uint32_t n = 0; n < kAhead; ++n) {
+                const uint32_t at = min(first + n * kSmallThreads, quads - 1u);
+                row[n] = per_row == 1u ? at : __umulhi(at, over_row);
+                col[n] = (at - row[n] * per_row) * 4u;
+                const T* p = x + (int64_t)row[n] * a.x_row + col[n];
+                if (col[n] + 4u <= a.cols) {
+                    __builtin_memcpy(v[n], p, sizeof(v[n]));  // (at the address of any value)
+                } else {
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e) v[n][e] = col[n] + e < a.cols ? p[e] : (T)0.0f;
+                }
+            }
+#pragma unroll
+            for (uint32_t n = 0; n < kAhead; ++n)
+                if (first + n * kSmallThreads < quads) use(row[n], col[n], v[n]);
         }
+    };
+    double sum = 0.0;
+    each([&](uint32_t, uint32_t, const T (&v)[4]) {
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) sum = __builtin_fma((double)load1(v + e), (double)load1(v + e), sum);
+    });
 #pragma unroll
     for (uint32_t m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
     if (lane == 0) sums[wave] = sum;
@@ -550,15 +593,33 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
     sum = 0.0;
 #pragma unroll
     for (uint32_t w = 0; w < kSmallWaves; ++w) sum += sums[w];
+    // what a value is multiplied with, as a power of two and a number in [1/2, 1): the first alone may lie outside of fp32
     const double over = (double)a.held / (sqrt(sum) + (double)a.eps);
-    for (uint32_t r = wave; r < a.rows; r += kSmallWaves)
-        for (uint32_t c = lane; c < a.cols; c += 64u) {
-            half hi, lo;
-            split((float)((double)load1(x + (int64_t)r * a.x_row + c) * over), hi, lo);
-            half* const at = X + (tall ? c * x_stride + r : r * x_stride + c);
-            at[0] = hi;
-            at[x_plane] = lo;
+    const int exponent = __builtin_amdgcn_frexp_exp(over);
+    const float mantissa = (float)__builtin_amdgcn_frexp_mant(over);
+    each([&](uint32_t r, uint32_t c, const T (&v)[4]) {
+        f16x4 hi, lo;
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+            half h, l;
+            split(__builtin_amdgcn_ldexpf(load1(v + e), exponent) * mantissa, h, l);
+            hi[e] = h;
+            lo[e] = l;
         }
+        if (!tall) {  // (values behind the row's end are zeros)
+            half* const at = X + r * x_stride + c;
+            *reinterpret_cast<f16x4*>(at) = hi;
+            *reinterpret_cast<f16x4*>(at + x_plane) = lo;
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+                if (c + e < a.cols) {
+                    half* const at = X + (c + e) * x_stride + r;
+                    at[0] = hi[e];
+                    at[x_plane] = lo[e];
+                }
+        }
+    });
     const uint32_t ti = a.sp / 32u, tj = a.lp / 32u;
     for (uint32_t step = 0; step < a.n_steps; ++step) {
         const Factors f = a.steps[step];
@@ -597,12 +658,12 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
             if (t < ti * ti) small_put(S, s_plane, t / ti * 32u, s_stride, t % ti * 32u, of_b[n], lane);
         }
         __syncthreads();
-        // X in its own place
+        // X in its own place: tiles of its transpose
         f32x16 of_x[kWide];
 #pragma unroll
         for (int n = 0; n < kWide; ++n) {
             const uint32_t t = again(wave + n * kSmallWaves);
-            if (t < ti * tj) of_x[n] = small_product<true>(S, s_plane, t / tj * 32u, s_stride, X, x_plane, t % tj * 32u, x_stride, a.sp, lane) * f.update;
+            if (t < ti * tj) of_x[n] = small_product<true>(X, x_plane, t % tj * 32u, x_stride, S, s_plane, t / tj * 32u, s_stride, a.sp, lane) * f.update;
         }
         __syncthreads();
 #pragma unroll
@@ -610,16 +671,28 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
             const uint32_t t = again(wave + n * kSmallWaves), i = t / tj * 32u, j = t % tj * 32u;
             if (t >= ti * tj) continue;
             if (step + 1u < a.n_steps) {
-                small_put(X, x_plane, i, x_stride, j, of_x[n], lane);
+                small_put(X, x_plane, j, x_stride, i, of_x[n], lane);
                 continue;
             }
-            T* out = static_cast<T*>(a.out) + (int64_t)matrix * a.out_matrix;
+            // the result, as it is, in the place of both planes
+            float* const at = reinterpret_cast<float*>(X) + (i + (lane & 31u)) * x_stride + j + 4 * (lane >> 5);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t row = i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3), col = j + (lane & 31u);
-                if (row < a.s && col < a.l) out[tall ? (int64_t)col * a.out_row + row : (int64_t)row * a.out_row + col] = (T)of_x[n][r];
-            }
+            for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4*>(at + 8 * q) = f32x4{of_x[n][4 * q], of_x[n][4 * q + 1], of_x[n][4 * q + 2], of_x[n][4 * q + 3]};
         }
+    }
+    __syncthreads();
+    T* const out = static_cast<T*>(a.out) + (int64_t)matrix * a.out_matrix;
+    const float* const Y = reinterpret_cast<const float*>(X);
+    for (uint32_t at = threadIdx.x; at < quads; at += kSmallThreads) {
+        const uint32_t r = per_row == 1u ? at : __umulhi(at, over_row), c = (at - r * per_row) * 4u;
+        f32x4 v;
+        if (!tall) {
+            v = *reinterpret_cast<const f32x4*>(Y + r * x_stride + c);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) v[e] = Y[min(c + e, a.sp - 1u) * x_stride + r];
+        }
+        put_values(out + (int64_t)r * a.out_row + c, v, a.cols - c);
     }
 }
 
