@@ -874,38 +874,47 @@ class HeadNorm:
         except Exception:
             pass
 
-    def _view(self, x, like):
-        """The fields of pxr_tokens for a tensor of `like`'s shape and type, [B, T, H, d] or (one step) [B, H, d]."""
-        assert x.is_cuda and x.dtype == like.dtype and x.shape == like.shape, (tuple(x.shape), tuple(like.shape), x.dtype)
+    def _view(self, x, shape, dtype):
+        """The fields of pxr_tokens for a tensor of this shape and type, [B, T, H, d] or (one step) [B, H, d]."""
+        assert x.is_cuda and x.dtype == dtype and x.shape == shape, (tuple(x.shape), tuple(shape), x.dtype)
         s = x.stride()
-        assert s[-1] == 1 or x.shape[-1] == 1 or x.numel() == 0, "a head's values must be adjacent"
+        assert s[-1] == 1 or shape[-1] == 1 or x.numel() == 0, "a head's values must be adjacent"
         return (x.data_ptr(), s[0], s[1], s[2]) if len(s) == 4 else (x.data_ptr(), s[0], 0, s[1])
 
     def _heads(self, torch, q, k, q_weight, k_weight, positions, first):
-        """The bytes of pxr_heads, and the weights' type."""
+        """The bytes of pxr_heads; the shapes of q and of k; the heads' and the weights' type."""
         some = q if q is not None else k
-        assert some is not None and some.dim() in (3, 4) and some.shape[-1] == self.d, "queries or keys [B, T, heads, d] or [B, heads, d]"
-        lead = some.shape[:-2]
-        B, T = lead if len(lead) == 2 else (lead[0], 1)
-        counts, views = [], []
-        for x in (q, k):
-            if x is None:
-                counts.append(0)
-                views += (0, 0, 0, 0)
-                continue
-            assert x.shape[:-2] == lead and x.shape[-1] == self.d and x.dtype == some.dtype, (tuple(x.shape), tuple(some.shape))
-            counts.append(x.shape[-2])
-            views += self._view(x, x)
-        params = _params(torch, some, self.d, q_weight, k_weight)
-        bits, at = 32, (0, 0, 0)
+        assert some is not None and some.dim() in (3, 4), "queries or keys [B, T, heads, d] or [B, heads, d]"
+        dtype, shape = some.dtype, some.shape
+        lead = shape[:-2]
+        B, T = lead if len(shape) == 4 else (shape[0], 1)
+        qs = ks = None
+        qv = kv = (0, 0, 0, 0)
+        if q is not None:
+            qs = shape
+            assert qs[-1] == self.d, (tuple(qs), self.d)
+            qv = self._view(q, qs, dtype)
+        if k is not None:
+            ks = k.shape
+            assert ks[:-2] == lead and ks[-1] == self.d, (tuple(ks), tuple(shape))
+            kv = self._view(k, ks, dtype)
+        params = torch.float32 if q_weight is None and k_weight is None else _params(torch, some, self.d, q_weight, k_weight)
+        bits, at, at_env, at_step = 32, 0, 0, 0
         if positions is not None:
-            assert positions.is_cuda and positions.dtype in (torch.int32, torch.int64) and positions.shape == lead, tuple(positions.shape)
+            kind = positions.dtype
+            assert positions.is_cuda and kind in (torch.int32, torch.int64) and positions.shape == lead, tuple(positions.shape)
             assert first == 0, "positions say where every step is"
             s = positions.stride()
-            at, bits = (positions.data_ptr(), s[0], s[1] if len(s) == 2 else 0), 64 if positions.dtype == torch.int64 else 32
-        packed = _pack_heads(_dtype_code(torch, some.dtype), _dtype_code(torch, params), B, T, *counts, *views, _ptr(q_weight) or 0, _ptr(k_weight) or 0,
-                             at[0], bits, at[1], at[2], first)
-        return packed, params
+            at, at_env, at_step, bits = positions.data_ptr(), s[0], s[1] if len(s) == 2 else 0, 64 if kind == torch.int64 else 32
+        packed = _pack_heads(_dtype_code(torch, dtype), _dtype_code(torch, params), B, T, 0 if qs is None else qs[-2], 0 if ks is None else ks[-2], *qv, *kv,
+                             _ptr(q_weight) or 0, _ptr(k_weight) or 0, at, bits, at_env, at_step, first)
+        return packed, qs, ks, dtype, params
+
+    def _new(self, torch, x, shape, dtype, stream):
+        """A contiguous tensor of x's shape, and its pxr_tokens."""
+        out = _empty(torch, x, stream, shape, dtype)
+        H, d = shape[-2:]
+        return out, _pack_tokens(out.data_ptr(), (shape[1] if len(shape) == 4 else 1) * H * d, H * d, d)
 
     def forward(self, q, k, q_weight=None, k_weight=None, positions=None, first=0, q_out=None, k_out=None, stream=None):
         """q, k: CUDA float32 or bfloat16 [B,T,H,d] (or, one step, [B,H,d]; any strides, a head's values adjacent; the numbers of heads may
@@ -913,41 +922,49 @@ class HeadNorm:
         [B]), or None: step t is at first + t.  Returns (q, k) normalised and turned, in q_out and k_out if given (they may be
         the inputs themselves); enqueue only."""
         torch = _torch or _torch_module()
-        r, _ = self._heads(torch, q, k, q_weight, k_weight, positions, first)
-        given, outs = [t for t in (q_out, k_out) if t is not None], []
-        for x, out in ((q, q_out), (k, k_out)):
-            assert x is not None or out is None
-            outs.append(_empty(torch, x, stream, x.shape, x.dtype) if x is not None and out is None else out)
-        packed = [None if x is None else _pack_tokens(*self._view(o, x)) for x, o in zip((q, k), outs)]
-        _check((_lib or lib()).pxr_head_norm_forward(self._h, r, *packed, _stream_handle(stream, q if q is not None else k)))
+        r, qs, ks, dtype, _ = self._heads(torch, q, k, q_weight, k_weight, positions, first)
+        to_q = to_k = None
+        given = [t for t in (q_out, k_out) if t is not None]
+        if q_out is not None:
+            assert q is not None
+            to_q = _pack_tokens(*self._view(q_out, qs, dtype))
+        elif q is not None:
+            q_out, to_q = self._new(torch, q, qs, dtype, stream)
+        if k_out is not None:
+            assert k is not None
+            to_k = _pack_tokens(*self._view(k_out, ks, dtype))
+        elif k is not None:
+            k_out, to_k = self._new(torch, k, ks, dtype, stream)
+        _check(_lib.pxr_head_norm_forward(self._h, r, to_q, to_k, _stream_handle(stream, q if q is not None else k)))
         if given:
             _written(torch, *given)
-        return tuple(outs)
+        return q_out, k_out
 
     def backward(self, dq, dk, q, k, q_weight=None, k_weight=None, positions=None, first=0, params_dtype=None, stream=None):
         """Gradients for dq and dk (of the outputs) of a forward call with these inputs.  Returns (of q, of k, of q_weight, of k_weight), the latter two [d] of the
         weights' type (without weights: params_dtype, float32 unless given); None in the place of what is of no heads; enqueue only."""
         torch = _torch or _torch_module()
-        r, params = self._heads(torch, q, k, q_weight, k_weight, positions, first)
+        r, qs, ks, dtype, params = self._heads(torch, q, k, q_weight, k_weight, positions, first)
         some = q if q is not None else k
         if q_weight is None and k_weight is None and params_dtype is not None:
-            assert params_dtype in (torch.float32, some.dtype)
+            assert params_dtype in (torch.float32, dtype)
             params = params_dtype
             r = r[:4] + struct.pack("@I", _dtype_code(torch, params)) + r[8:]
-        grads = [None if x is None else _empty(torch, x, stream, x.shape, x.dtype) for x in (q, k)]
-        sums = [None if x is None else _empty(torch, x, stream, (self.d,), params) for x in (q, k)]
-        given = [None if x is None else _pack_tokens(*self._view(d, x)) for x, d in zip((q, k), (dq, dk))]
-        into = [None if x is None else _pack_tokens(*self._view(g, x)) for x, g in zip((q, k), grads)]
-        L = _lib or lib()
+        grads, sums, given, into = [None, None], [None, None], [None, None], [None, None]
+        for i, (x, d, shape) in enumerate(((q, dq, qs), (k, dk, ks))):
+            if x is not None:
+                given[i] = _pack_tokens(*self._view(d, shape, dtype))
+                grads[i], into[i] = self._new(torch, x, shape, dtype, stream)
+                sums[i] = _empty(torch, x, stream, (self.d,), params)
         sizes = r[:24]
         asked, need = self._asked  # (the bytes for the sizes that were asked for last are known)
         if asked != sizes:
             n = C.c_size_t()
-            _check(L.pxr_head_norm_workspace(self._h, r, n))
+            _check(_lib.pxr_head_norm_workspace(self._h, r, n))
             need = n.value
             self._asked = (sizes, need)
         ws = _empty(torch, some, stream, (need,), torch.uint8) if need else None
-        _check(L.pxr_head_norm_backward(self._h, r, *given, *into, *(_ptr(s) for s in sums), _ptr(ws), need, _stream_handle(stream, some)))
+        _check(_lib.pxr_head_norm_backward(self._h, r, *given, *into, *(_ptr(s) for s in sums), _ptr(ws), need, _stream_handle(stream, some)))
         return (*grads, *sums)
 
 
