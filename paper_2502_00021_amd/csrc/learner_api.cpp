@@ -22,8 +22,8 @@ int check(const char* call, const pxr_orthogonalise_desc* d) {
     if (d->n_steps == 0 || d->n_steps > 64u) return refuse(call, "n_steps must lie in [1,64]");
     if (!(d->eps >= 0.0f) || !std::isfinite(d->eps)) return refuse(call, "eps must be finite and not negative");
     if ((d->rows > 1 && (d->x_row < (int64_t)d->cols || d->out_row < (int64_t)d->cols))) return refuse(call, "a row stride is smaller than cols");
-    if (std::min(d->rows, d->cols) > (1u << 15) || (uint64_t)d->rows * d->cols > (1ull << 32))
-        return refuse(call, "the smaller of rows and cols must be at most 2^15, rows * cols at most 2^32", PXR_ERR_UNSUPPORTED);
+    if (std::min(d->rows, d->cols) > (1u << 15) || std::max(d->rows, d->cols) > (1u << 28) || (uint64_t)d->rows * d->cols > (1ull << 32))
+        return refuse(call, "the smaller of rows and cols must be at most 2^15, the larger 2^28, rows * cols 2^32", PXR_ERR_UNSUPPORTED);
     // (a row stride of 2^40 and more is no row of any memory: the product below does not wrap)
     if (d->out_row > (1ll << 40)) return refuse(call, "a row stride is too large");
     const int64_t extent = (int64_t)(d->rows - 1u) * (d->rows > 1 ? d->out_row : 0) + d->cols;

@@ -58,28 +58,47 @@ struct Prepare {
     float eps, scale;
 };
 
+// The power of two of a row's quads of values, at most a workgroup's threads; and units of 1024 values, or of rows side by side.
+__host__ __device__ inline uint32_t quads_shift(uint32_t cols) {
+    uint32_t shift = 0;
+    while ((1u << shift) < kThreads && (4u << shift) < cols) ++shift;
+    return shift;
+}
+__host__ __device__ inline uint64_t norm_units(uint32_t rows, uint32_t cols) {
+    const uint32_t together = kThreads >> quads_shift(cols);
+    return (uint64_t)((rows + together - 1u) / together) * ((cols + kNormColumns - 1u) / kNormColumns);
+}
+
 // Squares in 64 bits: those of fp32 values neither overflow nor vanish.
 template <class T>
 __global__ __launch_bounds__(kThreads) void square_sums_kernel(const Prepare a) {
     __shared__ double shared[kThreads / 64];
     const uint32_t part = blockIdx.x, matrix = blockIdx.y;
     const T* x = static_cast<const T*>(a.x) + (int64_t)matrix * a.x_matrix;
+    // a workgroup has 1024 values of a row, or of as many rows as their quads of values (padded to a power of two) take; four such units together
+    const uint32_t shift = quads_shift(a.cols), r_in = threadIdx.x >> shift, c_in = (threadIdx.x & ((1u << shift) - 1u)) * 4u;
+    const uint32_t together = kThreads >> shift, per_row = (a.cols + kNormColumns - 1u) / kNormColumns;
+    const uint64_t units = norm_units(a.rows, a.cols);
     double sum = 0.0;
-    const uint32_t per_row = (a.cols + kNormColumns - 1u) / kNormColumns;
-    for (uint64_t u = part; u < (uint64_t)a.rows * per_row; u += a.parts) {
-        const uint32_t r = (uint32_t)(u / per_row), c0 = (uint32_t)(u - (uint64_t)r * per_row) * kNormColumns;
-        const T* row = x + (int64_t)r * a.x_row;
-        constexpr uint32_t kEach = kNormColumns / kThreads;
-        const uint32_t c = c0 + threadIdx.x * kEach;
-        T v[kEach];
-        if (c + kEach <= a.cols) {
-            __builtin_memcpy(v, row + c, sizeof(v));  // (at the address of any value)
-        } else {
+    for (uint64_t first = part; first < units; first += 4ull * a.parts) {
+        T v[4][4];
 #pragma unroll
-            for (uint32_t e = 0; e < kEach; ++e) v[e] = c + e < a.cols ? row[c + e] : (T)0.0f;
+        for (uint32_t n = 0; n < 4; ++n) {
+            const uint64_t u = first + (uint64_t)n * a.parts;
+            const uint32_t block = (uint32_t)(u / per_row), r = block * together + r_in, c = (uint32_t)(u - (uint64_t)block * per_row) * kNormColumns + c_in;
+            const bool there = u < units && r < a.rows && c < a.cols;
+            const T* p = x + (there ? (int64_t)r * a.x_row + c : 0);
+            if (there && c + 4u <= a.cols) {
+                __builtin_memcpy(v[n], p, sizeof(v[n]));  // (at the address of any value)
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) v[n][e] = there && c + e < a.cols ? p[e] : (T)0.0f;
+            }
         }
 #pragma unroll
-        for (uint32_t e = 0; e < kEach; ++e) sum += (double)load1(v + e) * (double)load1(v + e);
+        for (uint32_t n = 0; n < 4; ++n)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) sum = __builtin_fma((double)load1(v[n] + e), (double)load1(v[n] + e), sum);
     }
 #pragma unroll
     for (uint32_t m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
@@ -741,11 +760,10 @@ Layout layout_of(const pxr_orthogonalise_desc& d) {
     y.l = std::max(d.rows, d.cols);
     y.sp = padded(y.s);
     y.lp = padded(y.l);
-    const uint64_t units = (uint64_t)d.rows * ((d.cols + kNormColumns - 1u) / kNormColumns);
-    y.parts = (uint32_t)std::min<uint64_t>(kNormParts, units);
+    y.parts = (uint32_t)std::min<uint64_t>(kNormParts, norm_units(d.rows, d.cols));
     y.gram = cut_of(y.s, y.l, d.n_matrices);
     y.poly = cut_of(y.s, y.s, d.n_matrices);
-    y.update = (uint64_t)tiles_of(y.s, 2) * tiles_of(y.l, 2) * d.n_matrices >= 256u ? 2 : 1;
+    y.update = (uint64_t)tiles_of(y.s, 2) * tiles_of(y.l, 2) * d.n_matrices >= 128u ? 2 : 1;
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t from = at;

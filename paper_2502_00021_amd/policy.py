@@ -282,7 +282,7 @@ def main(n_envs=64, n_steps=48, updates=30, memory="attention", orthogonal=False
     target = torch.tanh(acted.roll(5, 1)) * 0.5
     if orthogonal:
         matrices = [p for p in policy.parameters() if p.dim() == 2]
-        optimizers = [Orthogonal(matrices, lr=0.01), torch.optim.Adam([p for p in policy.parameters() if p.dim() != 2], lr=3e-3)]
+        optimizers = [Orthogonal(matrices, lr=0.004), torch.optim.Adam([p for p in policy.parameters() if p.dim() != 2], lr=3e-3)]
     else:
         optimizers = [torch.optim.Adam(policy.parameters(), lr=3e-3)]
     for i in range(updates):

@@ -1013,8 +1013,8 @@ def _gated_workspace(torch, like, B, T, D, backward, stream):
 def gated_recurrence(x, gate, resets=None, state=None, coupled=True, out=None, state_out=None, stream=None):
     """h_t = (an episode begins ? 0 : a h_{t-1}) + (coupled ? 1 - a : 1) x_t with a = 1 / (1 + exp(-gate_t)), for each environment
     and channel.  x, gate: CUDA float32 or bfloat16 [B,T,D] (any strides, a step's values adjacent); resets: bool or uint8
-    [B,T], true where a step begins an episode, or None; state: float32 [B,D] before the first step, or None = zeros.  Returns
-    (out [B,T,D], the state after the last step); enqueue only."""
+    [B,T], true where a step begins an episode, or None; state: float32 [B,D] before the first step, or None = zeros.  out must not
+    overlap an input.  Returns (out [B,T,D], the state after the last step); enqueue only."""
     torch = _torch or _torch_module()
     assert x.dim() == 3
     r, B, T, D = _gated_rollout(torch, x, gate, resets, state, coupled)
@@ -1071,13 +1071,14 @@ def _steps_of(coefficients, steps):
     """float32 [n][3] for one triple, taken `steps` times (5 unless given), or for a triple for each step."""
     global _coefficients
     known, n, array = _coefficients  # (those of the call before, most often)
-    if known is not coefficients or n != steps or type(coefficients) is not tuple:
+    plain = type(coefficients) is tuple and all(type(c) is float for c in coefficients)
+    if not plain or known != coefficients or n != steps:
         array = np.asarray(coefficients, np.float32)
         if array.ndim == 1:
             array = np.tile(array, (5 if steps is None else int(steps), 1))
         assert array.ndim == 2 and array.shape[1] == 3 and (steps is None or array.shape[0] == steps), "a triple, or one for each step"
         array = np.ascontiguousarray(array)
-        if all(type(c) is float for c in coefficients):  # (what cannot change: a tuple of numbers)
+        if plain:
             _coefficients = (coefficients, steps, array)
     return array
 

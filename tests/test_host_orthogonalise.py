@@ -36,7 +36,7 @@ def test_descriptions(change):
     assert pxr.lib().pxr_last_error()
 
 
-@pytest.mark.parametrize("change", [dict(rows=2 ** 15 + 1, cols=2 ** 15 + 1), dict(rows=2 ** 31, cols=4), dict(rows=2, cols=2 ** 32 - 1)])
+@pytest.mark.parametrize("change", [dict(rows=2 ** 15 + 1, cols=2 ** 15 + 1), dict(rows=2 ** 31, cols=4), dict(rows=2, cols=2 ** 32 - 1), dict(rows=2 ** 28 + 1, cols=1)])
 def test_sizes(change):
     row = dict(x_row=change["cols"], out_row=change["cols"])
     assert _call(**change, **row)[:2] == (pxr.ERR_UNSUPPORTED, pxr.ERR_UNSUPPORTED)
