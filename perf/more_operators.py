@@ -197,6 +197,10 @@ def _run_own(kind, s):
         return dict(zip(("out", "state"), pxr.gated_recurrence(s["x"], s["gate"], resets=s["resets"], state=s["state"], coupled=coupled)))
     if kind == "recurrence_grad":
         got = pxr.gated_recurrence_backward(s["dout"], s["x"], s["gate"], resets=s["resets"], state=s["state"], dstate=s["dstate"], coupled=coupled)
+        if s["dstate"] is not None and s["dout"].dtype == torch.float32:
+            # The plain form adds dstate to the last step of dout, in 32 bits to the state's own tensor: a second pass on a state takes another
+            # dout than the first.  So it does here, after the call.
+            s["dout"][:, -1].add_(s["dstate"])
         return dict(zip(("dx", "dgate", "dstate"), got))
     return dict(out=pxr.gated_recurrence_step(s["x"], s["gate"], s["state"], resets=s["resets"], coupled=coupled), state=s["state"])
 
