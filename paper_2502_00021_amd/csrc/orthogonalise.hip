@@ -34,7 +34,7 @@ constexpr uint32_t kThreads = 256;
 constexpr uint32_t kPad = 128;       // rows and columns of the matrices in the workspace come in multiples of it; what is behind the matrix is zeros
 constexpr uint32_t kNormParts = 512; // of a matrix whose squares are summed, at most
 constexpr uint32_t kNormColumns = 1024;
-constexpr uint32_t kDepth = 32;      // values of the summed axis in LDS at a time
+constexpr uint32_t depth_of(int M) { return M == 2 ? 32u : 64u; }  // values of the summed axis that a stage in LDS has
 
 __host__ __device__ constexpr uint32_t padded(uint32_t n) { return (n + kPad - 1u) / kPad * kPad; }
 
@@ -159,9 +159,9 @@ enum { kGram, kPoly, kUpdate, kLast };
 
 struct Product {
     Planes a, b, to;     // kGram: X, X -> A;  kPoly: A, A -> B;  kUpdate: B, X -> X;  kLast: B, X -> out
-    uint32_t depth;      // the summed axis, a multiple of kDepth
+    uint32_t depth;      // the summed axis, a multiple of 64
     uint32_t tiles_i, tiles_j;
-    uint32_t whole, splits, steps_each;  // tiles from number `whole` on are cut along the summed axis: into `splits` parts of steps_each steps of kDepth
+    uint32_t whole, splits, steps_each;  // tiles from number `whole` on are cut along the summed axis: into `splits` parts of steps_each steps of depth_of(M)
     float* partial;      // [matrices][splits][tiles - whole][tile][tile]
     float scale;         // of the sums
     float c0, c1;        // kPoly: on the diagonal; times A's held values
@@ -215,9 +215,9 @@ __device__ __forceinline__ void of_triangle(uint32_t t, uint32_t rows, uint32_t&
 // exchanged.  (Exchanged for 32 banks, half of the LDS' cycles were conflicts: 4096 x 4096 bfloat16 5250 us.)
 template <int kSide, bool kAcross>
 struct Operand {
-    static constexpr uint32_t kChunks = kSide * kDepth / 8;  // of 16 bytes, in a plane
+    static constexpr uint32_t kDepth = depth_of(kSide / 64), kChunks = kSide * kDepth / 8;  // of 16 bytes, in a plane
     static __device__ __forceinline__ uint32_t turn(uint32_t row) {
-        if (!kAcross) return row >> 2 & 3u;
+        if (!kAcross) return kDepth == 32u ? row >> 2 & 3u : row >> 1 & 7u;
         return kSide == 128 ? (row & 3u) << 2 : (row >> 1 & 1u) << 2;
     }
     // Which value chunk number i of the plane is: row and column in the tile.
@@ -226,8 +226,8 @@ struct Operand {
             row = i / (kSide / 8);
             col = ((i % (kSide / 8)) ^ turn(row)) * 8u;
         } else {
-            row = i / 4u;
-            col = ((i % 4u) ^ turn(row)) * 8u;
+            row = i / (kDepth / 8u);
+            col = ((i % (kDepth / 8u)) ^ turn(row)) * 8u;
         }
     }
     // Eight values of the summed axis, 16 k + 8 h .. + 7, of line lane % 32 from `line` on.
@@ -292,12 +292,12 @@ __device__ __forceinline__ void put_out(const Product& p, uint32_t matrix, uint3
 }
 
 // A tile of 64 M x 64 M values by four wavefronts, 2 x 2, each 32 M x 32 M.
-constexpr uint32_t stages(int M) { return M == 2 ? 2u : 4u; }
+constexpr uint32_t stages(int M) { return M == 2 ? 2u : 2u; }
 
 template <int kKind, int M>
 __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
     constexpr int kSide = 64 * M;
-    constexpr uint32_t kStages = stages(M);  // of kDepth values in LDS: one that is worked on, the others on their way
+    constexpr uint32_t kDepth = depth_of(M), kStages = stages(M);  // in LDS: one that is worked on, the others on their way
     constexpr bool kSym = kKind <= kPoly;
     typedef Operand<kSide, false> OpA;
     typedef Operand<kSide, !kSym> OpB;
@@ -487,6 +487,7 @@ struct Small {
 
 constexpr uint32_t kSmallThreads = 512, kSmallWaves = kSmallThreads / 64;
 constexpr uint32_t kLds = 160 * 1024;
+constexpr uint32_t up64(uint32_t n) { return (n + 63u) / 64u * 64u; }
 constexpr uint32_t up32(uint32_t n) { return (n + 31u) / 32u * 32u; }
 // Rows lie 16 bytes apart from a multiple of 64, so that those of eight lanes lie in different banks.
 constexpr uint32_t small_row(uint32_t n) { return n + 8u; }
@@ -743,11 +744,11 @@ uint32_t triangle_of(uint32_t s, int M) { return tiles_of(s, M) * (tiles_of(s, M
 Cut cut_of(uint32_t s, uint32_t depth, uint32_t n_matrices) {
     Cut c{};
     c.M = triangle_of(s, 2) * (uint64_t)n_matrices >= kLargeTiles ? 2 : 1;
-    const uint32_t tiles = triangle_of(s, c.M), steps = (depth + kDepth - 1u) / kDepth;
+    const uint32_t tiles = triangle_of(s, c.M), steps = (depth + depth_of(c.M) - 1u) / depth_of(c.M);
     const uint64_t all = (uint64_t)tiles * n_matrices;
     c.whole = all < kPlaces ? 0u : n_matrices == 1u ? (uint32_t)(tiles / kPlaces * kPlaces) : tiles;
     const uint64_t left = (uint64_t)(tiles - c.whole) * n_matrices;
-    c.splits = left ? (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(steps / 8u, kPlaces / left)) : 1u;
+    c.splits = left ? (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(steps / (256u / depth_of(c.M)), kPlaces / left)) : 1u;
     c.steps_each = (steps + c.splits - 1u) / c.splits;
     c.splits = (steps + c.steps_each - 1u) / c.steps_each;
     if (c.splits == 1u) c.whole = tiles;
@@ -882,7 +883,7 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         // A
         p.a = p.b = from;
         p.to = as;
-        p.depth = up32(y.l);
+        p.depth = up64(y.l);
         cut_as(p, y.gram, y.s);
         p.partial = reinterpret_cast<float*>(base + y.partial);
         p.scale = f.gram;
@@ -892,7 +893,7 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
         // B
         p.a = p.b = as;
         p.to = bs;
-        p.depth = up32(y.s);
+        p.depth = up64(y.s);
         cut_as(p, y.poly, y.s);
         p.scale = f.poly;
         p.c0 = f.diagonal;
