@@ -230,19 +230,32 @@ struct Operand {
             col = ((i % (kDepth / 8u)) ^ turn(row)) * 8u;
         }
     }
-    // Eight values of the summed axis, 16 k + 8 h .. + 7, of line lane % 32 from `line` on.
-    static __device__ __forceinline__ f16x8 fragment(const half* plane, uint32_t line, uint32_t k, uint32_t lane) {
+    // Eight values of the summed axis, 16 k + 8 h .. + 7, of line lane % 32 from `line` on, of both planes.
+    static __device__ __forceinline__ void fragments(const half* planes, uint32_t line, uint32_t k, uint32_t lane, f16x8 (&f)[2]) {
         const uint32_t h = lane >> 5;
         if constexpr (kAcross) {
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            // The transposing read: lane i of 16 gives the address of four columns of row i / 4 and gets four rows of column i.  Before its builtin the compiler waits for
+            // every request that writes LDS, those of the stages ahead too, so it is written out, with a wait of its own.
             const uint32_t i = lane & 15u, row = 16u * k + 8u * h + (i >> 2), col = line + (lane & 16u) + 4u * (i & 3u);
-            const half* p = plane + row * kSide + (((col >> 3) ^ turn(row)) << 3) + (col & 7u);  // (four rows on: turned alike)
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * kSide));
-            return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            const half* p = planes + row * kSide + (((col >> 3) ^ turn(row)) << 3) + (col & 7u);  // (four rows on: turned alike)
+            const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const half*)p;
+            s16x4 q[4];
+            asm volatile(
+                "ds_read_b64_tr_b16 %0, %4\n\t"
+                "ds_read_b64_tr_b16 %1, %4 offset:%5\n\t"
+                "ds_read_b64_tr_b16 %2, %4 offset:%6\n\t"
+                "ds_read_b64_tr_b16 %3, %4 offset:%7\n\t"
+                "s_waitcnt lgkmcnt(0)"
+                : "=&v"(q[0]), "=&v"(q[1]), "=&v"(q[2]), "=&v"(q[3])
+                : "v"(at), "n"(4 * kSide * 2), "n"(kSide * kDepth * 2), "n"(kSide * kDepth * 2 + 4 * kSide * 2)
+                : "memory");
+            f[0] = __builtin_bit_cast(f16x8, __builtin_shufflevector(q[0], q[1], 0, 1, 2, 3, 4, 5, 6, 7));
+            f[1] = __builtin_bit_cast(f16x8, __builtin_shufflevector(q[2], q[3], 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             const uint32_t row = line + (lane & 31u);
-            return *reinterpret_cast<const f16x8*>(plane + row * kDepth + (((2u * k + h) ^ turn(row)) << 3));
+#pragma unroll
+            for (uint32_t plane = 0; plane < 2; ++plane)
+                f[plane] = *reinterpret_cast<const f16x8*>(planes + plane * kSide * kDepth + row * kDepth + (((2u * k + h) ^ turn(row)) << 3));
         }
     }
 };
@@ -371,12 +384,10 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
         for (uint32_t kk = 0; kk < kDepth / 16; ++kk) {
             f16x8 a[M][2], b[M][2];
 #pragma unroll
-            for (int i = 0; i < M; ++i)
-#pragma unroll
-                for (uint32_t plane = 0; plane < 2; ++plane) {
-                    a[i][plane] = OpA::fragment(from + plane * kPlane, row0 + 32 * i, kk, lane);
-                    b[i][plane] = OpB::fragment(from + (2 + plane) * kPlane, col0 + 32 * i, kk, lane);
-                }
+            for (int i = 0; i < M; ++i) {
+                OpA::fragments(from, row0 + 32 * i, kk, lane, a[i]);
+                OpB::fragments(from + 2 * kPlane, col0 + 32 * i, kk, lane, b[i]);
+            }
 #pragma unroll
             for (int i = 0; i < M; ++i)
 #pragma unroll
