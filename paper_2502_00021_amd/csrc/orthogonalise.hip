@@ -745,7 +745,11 @@ struct Layout {
     size_t sums, partial, x[2], a, b, bytes;  // offsets
 };
 
-constexpr uint64_t kLargeTiles = 136;  // tiles of 128 x 128 from which on they are taken
+// Symmetric products take tiles of 128 x 128 from this many on, of one matrix or of several (whose last ones are not cut), unless a matrix has fewer than kLargeEach, whose tiles on the diagonal
+// cost more than the larger tiles save.  Calls with 64 x 64 against 128 x 128: 4096 x 4096, 528 tiles, 4630 us, 4280; 3584, 406, 3336, 3273; 3328, 351, 2744, 2759; 2048, 136, 759, 796; eight of
+// 2048, 1088, 5226, 4824; four, 544, 2527, 2635; 32 of 1024, 1152, 3143, 2999; 16, 576, 1497, 1593; 200 of 512, 10 tiles each, 3642, 3943.
+constexpr uint64_t kLargeTiles = 400, kLargeBatch = 1000;
+constexpr uint32_t kLargeEach = 32;
 constexpr uint64_t kPlaces = 512;  // workgroups that a device has room for at once, two on a compute unit
 
 uint32_t tiles_of(uint32_t n, int M) { return (n + 64u * M - 1u) / (64u * M); }
@@ -754,7 +758,7 @@ uint32_t triangle_of(uint32_t s, int M) { return tiles_of(s, M) * (tiles_of(s, M
 // Tiles that do not fill the places, and those that are left when the others have filled them some times, are cut along the summed axis; no part has fewer than 8 steps.
 Cut cut_of(uint32_t s, uint32_t depth, uint32_t n_matrices) {
     Cut c{};
-    c.M = triangle_of(s, 2) * (uint64_t)n_matrices >= kLargeTiles ? 2 : 1;
+    c.M = triangle_of(s, 2) >= kLargeEach && triangle_of(s, 2) * (uint64_t)n_matrices >= (n_matrices == 1u ? kLargeTiles : kLargeBatch) ? 2 : 1;
     const uint32_t tiles = triangle_of(s, c.M), steps = (depth + depth_of(c.M) - 1u) / depth_of(c.M);
     const uint64_t all = (uint64_t)tiles * n_matrices;
     c.whole = all < kPlaces ? 0u : n_matrices == 1u ? (uint32_t)(tiles / kPlaces * kPlaces) : tiles;

@@ -88,6 +88,15 @@ def test_large(torch, pxr, m, n, dtype):
     check(torch, pxr, normal(torch, n, m, n, dtype=dtype))
 
 
+@pytest.mark.parametrize("B,m,n,dtype", [(1, 3601, 3590, "f32"), (1, 3600, 5003, "bf16"), (28, 1020, 1030, "f32"), (4, 2050, 2060, "bf16")])
+def test_tiles_of_both_sizes(torch, pxr, B, m, n, dtype):
+    """Around the numbers of tiles from which on symmetric products take larger ones."""
+    x = normal(torch, n, B, m, n, dtype=dtype)
+    got = pxr.orthogonalise(x)
+    check(torch, pxr, x[:2], got=got[:2])
+    check(torch, pxr, x[-2:], got=got[-2:])
+
+
 @pytest.mark.parametrize("m,n", [(60, 90), (300, 200)])
 def test_coefficients(torch, pxr, m, n):
     """Cubic and quintic steps, few and many, of factors far from one, and another triple in every step."""
