@@ -8,7 +8,8 @@
 //
 // Steps in a row are one step: with A their product of k, h = A h_before + H and r = A r_after + R, H and R from zero.  A wavefront has C steps of its channels in
 // registers; the wavefronts of a workgroup have steps that follow each other and tell each other (A, H, R) through LDS, so that everything is read once.  A
-// product A of 0 passes nothing on, whatever the state holds: what is not finite stays on its side of an episode's beginning.
+// product A of +0 is that of steps among which an episode begins and passes nothing on, whatever the state holds: what is not finite stays on its side of the beginning.
+// One that is merely too small for fp32 is -0, which a state that is not finite does pass.
 //
 // Bound by HBM.
 
@@ -104,10 +105,11 @@ __device__ __forceinline__ float taken(float s) { return s + (mostly(s) ? 0.0f :
 __device__ __forceinline__ float kept(float s, float v, float b) { return __builtin_fmaf(-s, v, (mostly(s) ? v : 0.0f) + b); }
 __device__ __forceinline__ float kept(float s, float v) { return __builtin_fmaf(-s, v, mostly(s) ? v : 0.0f); }
 
-// Products in which 0 wins, over what is not a number as well.
-__device__ __forceinline__ float times(float A, float B) { return A == 0.0f || B == 0.0f ? 0.0f : A * B; }
-// What steps in a row (product A, own result H) make of a state.
-__device__ __forceinline__ float through(float A, float H, float state) { return A != 0.0f ? __builtin_fmaf(A, state, H) : H; }
+// Products of steps in a row (+0: an episode begins among them; -0: too small), and what such steps (product A, own result H) make of a state.
+__device__ __forceinline__ bool begins(float A) { return __float_as_uint(A) == 0u; }
+__device__ __forceinline__ float too_small(float A) { return A == 0.0f ? -0.0f : A; }
+__device__ __forceinline__ float times(float A, float B) { return begins(A) || begins(B) ? 0.0f : too_small(A * B); }
+__device__ __forceinline__ float through(float A, float H, float state) { return begins(A) ? H : __builtin_fmaf(A, state, H); }
 
 struct Recurrence {
     const void *x, *gate, *dout;
@@ -174,6 +176,8 @@ struct Chunk {
             }
             in_turn();
         }
+#pragma unroll
+        for (int i = 0; i < V; ++i) A[i] = masked(too_small(A[i]), none);
         if constexpr (kBack) {
 #pragma unroll
             for (int j = C - 1; j >= 0; --j)

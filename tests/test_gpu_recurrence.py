@@ -272,6 +272,31 @@ def test_what_is_not_finite_stays_in_its_episode(torch, pxr, B, T, begins, at, b
     assert torch.equal(dfirst, got[2]) and not dx[0, -1, 5].isfinite()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gate", [-3.0, -10.0, -50.0, -200.0, float("-inf")])
+@pytest.mark.parametrize("T", [40, 300, 3000, 9000])
+def test_what_is_not_finite_reaches_its_whole_episode(torch, pxr, T, gate, dtype):
+    """Through gates whose products leave fp32 as well."""
+    rng = np.random.default_rng(T)
+    x, _, r, s, dout, ds = inputs(torch, rng, 2, T, 3, dtype)
+    g = torch.full_like(x, gate)
+    r.zero_()
+    r[:, T - 5] = True
+    for bad in (float("nan"), float("inf")):
+        y = x.clone()
+        y[0, 1, 2] = bad
+        out, last = pxr.gated_recurrence(y, g, resets=r, state=s)
+        assert not out[0, 1:T - 5, 2].isfinite().any() and out[0, :, :2].isfinite().all() and out[0, T - 5:].isfinite().all() and out[1].isfinite().all() and last.isfinite().all()
+        d = dout.clone()
+        d[1, T - 6, 0] = bad
+        dx, _, dfirst = pxr.gated_recurrence_backward(d, x, g, resets=r, state=s, dstate=ds)
+        assert not dx[1, :T - 5, 0].isfinite().any() and dx[1, T - 5:].isfinite().all() and dx[0].isfinite().all() and not dfirst[1, 0].isfinite()
+        broken = s.clone()
+        broken[0, 1] = bad
+        out, last = pxr.gated_recurrence(x, g, resets=r, state=broken)
+        assert not out[0, :T - 5, 1].isfinite().any() and out[0, T - 5:].isfinite().all() and last.isfinite().all()
+
+
 def test_gradients_by_differences(torch, pxr):
     """The kernels' own forward pass, moved along a direction."""
     rng = np.random.default_rng(4)
