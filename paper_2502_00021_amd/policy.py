@@ -150,9 +150,9 @@ class Orthogonal(torch.optim.Optimizer):
                 updates = []
                 for p in params:
                     state = self.state[p]
-                    if "momentum" not in state:
-                        state["momentum"] = torch.zeros_like(p, memory_format=torch.contiguous_format)
-                    m = state["momentum"].mul_(group["momentum"]).add_(p.grad)
+                    # (in fp32, whatever the parameter's type: also after torch has loaded it as of that type)
+                    m = state["momentum"].float() if "momentum" in state else torch.zeros(p.shape, dtype=torch.float32, device=p.device)
+                    state["momentum"] = m.mul_(group["momentum"]).add_(p.grad)
                     updates.append(torch.add(p.grad, m, alpha=group["momentum"]) if group["nesterov"] else m)
                 updates = pxr.orthogonalise(torch.stack(updates), steps=group["steps"], eps=group["eps"])
                 # (a tall matrix has fewer directions than rows: the step of a row stays what it is for a square one)

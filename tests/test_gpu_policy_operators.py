@@ -186,6 +186,28 @@ def test_orthogonal_steps(torch, policy_module, nesterov):
         policy_module.Orthogonal([torch.nn.Parameter(torch.zeros(3))])
 
 
+def test_momentum_of_bfloat16_matrices_is_float32(torch, policy_module):
+    """0.95 m + g is rounded twice a step, and what is rounded fades: 2 u |m| 20 steps long."""
+    p = torch.nn.Parameter(torch.zeros(24, 40, device="cuda", dtype=torch.bfloat16))
+    rng, optimizer, want, most = np.random.default_rng(2), policy_module.Orthogonal([p], lr=0.01), 0.0, 0.0
+    for step in range(60):
+        p.grad = torch.from_numpy(rng.standard_normal(p.shape).astype(np.float32)).cuda().bfloat16()
+        want = 0.95 * want + p.grad.double().cpu().numpy()
+        most = max(most, np.abs(want).max())
+        optimizer.step()
+        if step == 30:  # a learner that goes on from its saved state; torch makes it of the parameter's type, one rounding
+            kept = optimizer.state[p]["momentum"].clone()
+            optimizer.load_state_dict(optimizer.state_dict())
+            assert (optimizer.state[p]["momentum"].float() - kept).abs().max() <= 2.0 ** -8 * most
+            optimizer.state[p]["momentum"] = kept
+    m = optimizer.state[p]["momentum"]
+    assert m.dtype == torch.float32 and np.abs(m.double().cpu().numpy() - want).max() <= 2 * 20 * 2.0 ** -24 * most
+    assert p.dtype == torch.bfloat16 and bool(p.isfinite().all()) and bool((p != 0).any())
+    optimizer.load_state_dict(optimizer.state_dict())
+    optimizer.step()
+    assert optimizer.state[p]["momentum"].dtype == torch.float32
+
+
 @pytest.mark.parametrize("memory", ["attention", "turned", "gated"])
 def test_learning_runs(torch, policy_module, memory):
     """A few updates of the whole policy by orthogonalised updates: every parameter has a finite gradient and moves."""
