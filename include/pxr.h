@@ -495,7 +495,7 @@ typedef struct {
 /* Bytes of workspace that pxr_orthogonalise needs for this description (host only; may be 0).  Errors: as for the call (buffers are not looked at). */
 int pxr_orthogonalise_workspace(const pxr_orthogonalise_desc* d, size_t* bytes);
 
-/* The result in d_out, which may be d_x itself.  Products and sums keep 22 bits and more (fp32's, but for a few roundings of 2^-23); values below 2^-38 of the
+/* The result in d_out, which may be d_x itself with the same strides.  Products and sums keep 22 bits and more (fp32's, but for a few roundings of 2^-23); values below 2^-38 of the
  * bound that the coefficients set for the singular values (1 before the first step) are zeros, so an update whose norm is far below eps comes out as zeros.  A matrix
  * with a NaN or an infinity comes out as NaN, the others are not touched by it.  n_matrices == 0 is a call that does nothing.  Equal inputs give equal bits.
  * d_workspace: 16-byte aligned, used until the call's kernels end.

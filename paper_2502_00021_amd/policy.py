@@ -68,7 +68,8 @@ class _HeadNorm(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dq, dk):
         q, k, q_weight, k_weight, positions = ctx.saved_tensors
-        dq, dk, dq_weight, dk_weight = ctx.layer.backward(dq.contiguous(), dk.contiguous(), q, k, q_weight, k_weight, positions=positions)
+        dq, dk = (None if x is None else d.contiguous() for x, d in ((q, dq), (k, dk)))
+        dq, dk, dq_weight, dk_weight = ctx.layer.backward(dq, dk, q, k, q_weight, k_weight, positions=positions)
         return None, dq, dk, None if q_weight is None else dq_weight, None if k_weight is None else dk_weight, None
 
 
@@ -103,7 +104,7 @@ def linear_attention(layer, q, k, v, resets=None, state=None):
 
 
 def head_norm(layer, q, k, q_weight=None, k_weight=None, positions=None):
-    """HeadNorm.forward for torch.autograd: (q, k) normalised and turned; gradients for q, k and the weights."""
+    """HeadNorm.forward for torch.autograd: (q, k) normalised and turned (either may be None); gradients for q, k and the weights."""
     return _HeadNorm.apply(layer, q, k, q_weight, k_weight, positions)
 
 

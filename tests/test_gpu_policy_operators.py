@@ -186,6 +186,28 @@ def test_orthogonal_steps(torch, policy_module, nesterov):
         policy_module.Orthogonal([torch.nn.Parameter(torch.zeros(3))])
 
 
+def test_heads_of_one_kind_alone(torch, policy_module):
+    """Queries without keys, and keys without queries, get the gradients that they get together; a weight's, 42 products summed in another order, within 42 u of their
+    magnitudes."""
+    from paper_2502_00021_amd import pxr
+    layer, shape = pxr.HeadNorm(32), (3, 7, 2, 32)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    make = lambda *s: torch.randn(s, generator=g, device="cuda").requires_grad_()
+    q, k, w, v, dq, dk = make(*shape), make(*shape), make(32), make(32), make(*shape), make(*shape)
+    both = policy_module.head_norm(layer, q, k, w, v)
+    want = torch.autograd.grad((both[0] * dq).sum() + (both[1] * dk).sum(), (q, k, w, v))
+    y, none = policy_module.head_norm(layer, q, None, w)
+    assert none is None and torch.equal(y, both[0])
+    got = torch.autograd.grad((y * dq).sum(), (q, w))
+    assert torch.equal(got[0], want[0]) and (got[1] - want[2]).abs().max() <= 42 * 2.0 ** -24 * want[2].abs().max().clamp(min=42.0)
+    none, y = policy_module.head_norm(layer, None, k, None, v)
+    assert none is None and torch.equal(y, both[1])
+    got = torch.autograd.grad((y * dk).sum(), (k, v))
+    assert torch.equal(got[0], want[1]) and (got[1] - want[3]).abs().max() <= 42 * 2.0 ** -24 * want[3].abs().max().clamp(min=42.0)
+    layer.close()
+
+
 def test_momentum_of_bfloat16_matrices_is_float32(torch, policy_module):
     """0.95 m + g is rounded twice a step, and what is rounded fades: 2 u |m| 20 steps long."""
     p = torch.nn.Parameter(torch.zeros(24, 40, device="cuda", dtype=torch.bfloat16))
