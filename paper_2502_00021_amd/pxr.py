@@ -664,6 +664,13 @@ def _ptr(x):
     return None if x is None else x.data_ptr()
 
 
+def _here(torch, *tensors):
+    """Tensors (and None) of the current GPU: a call's kernels go there, whatever its tensors are on."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        assert t is None or t.get_device() == device, f"a tensor of cuda:{t.get_device()}, and the current device is cuda:{device}"
+
+
 def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """x: CUDA float32 or bfloat16 [..., D] (rows a constant stride apart, their values adjacent); weight, bias: [D], float32
     or of x's type, or None.  Returns (y like x, mean, rstd: float32, x's leading shape), the latter two for
@@ -860,6 +867,7 @@ class HeadNorm:
         h = C.c_void_p()
         _check(lib().pxr_head_norm_create(C.byref(d), C.byref(h)))
         self._h = h
+        self._device = _torch_module().cuda.current_device()  # that has the frequencies
         self._asked = (None, 0)
         self.d, self.rotary, self.eps = d_head, d_rotary, d.eps
 
@@ -910,6 +918,10 @@ class HeadNorm:
                              _ptr(q_weight) or 0, _ptr(k_weight) or 0, at, bits, at_env, at_step, first)
         return packed, qs, ks, dtype, params
 
+    def _check_device(self, torch, *tensors):
+        _here(torch, *tensors)
+        assert self._device == torch._C._cuda_getDevice(), f"a layer of cuda:{self._device}"
+
     def _new(self, torch, x, shape, dtype, stream):
         """A contiguous tensor of x's shape, and its pxr_tokens."""
         out = _empty(torch, x, stream, shape, dtype)
@@ -923,6 +935,7 @@ class HeadNorm:
         the inputs themselves); enqueue only."""
         torch = _torch or _torch_module()
         r, qs, ks, dtype, _ = self._heads(torch, q, k, q_weight, k_weight, positions, first)
+        self._check_device(torch, q, k, q_weight, k_weight, positions, q_out, k_out)
         to_q = to_k = None
         given = [t for t in (q_out, k_out) if t is not None]
         if q_out is not None:
@@ -945,6 +958,7 @@ class HeadNorm:
         weights' type (without weights: params_dtype, float32 unless given); None in the place of what is of no heads; enqueue only."""
         torch = _torch or _torch_module()
         r, qs, ks, dtype, params = self._heads(torch, q, k, q_weight, k_weight, positions, first)
+        self._check_device(torch, q, k, q_weight, k_weight, positions, dq, dk)
         some = q if q is not None else k
         if q_weight is None and k_weight is None and params_dtype is not None:
             assert params_dtype in (torch.float32, dtype)
@@ -1018,6 +1032,7 @@ def gated_recurrence(x, gate, resets=None, state=None, coupled=True, out=None, s
     torch = _torch or _torch_module()
     assert x.dim() == 3
     r, B, T, D = _gated_rollout(torch, x, gate, resets, state, coupled)
+    _here(torch, x, gate, resets, state, out, state_out)
     given = [t for t in (out, state_out) if t is not None]
     out = _empty_like(torch, x, stream) if out is None else out
     if state_out is None:
@@ -1037,6 +1052,7 @@ def gated_recurrence_backward(dout, x, gate, resets=None, state=None, dstate=Non
     torch = _torch or _torch_module()
     assert x.dim() == 3
     r, B, T, D = _gated_rollout(torch, x, gate, resets, state, coupled)
+    _here(torch, dout, x, gate, resets, state, dstate)
     dx = _empty_like(torch, x, stream)
     dgate = _empty_like(torch, dx, stream)
     dfirst = None if state is None else _empty_like(torch, state, stream)
@@ -1054,6 +1070,7 @@ def gated_recurrence_step(x, gate, state, resets=None, coupled=True, out=None, s
     torch = _torch or _torch_module()
     assert x.dim() == 2
     r, B, _, D = _gated_rollout(torch, x, gate, resets, None, coupled)
+    _here(torch, x, gate, state, resets, out)
     given = (state,) if out is None else (state, out)
     out = _empty_like(torch, x, stream) if out is None else out
     _check((_lib or lib()).pxr_gated_recurrence_step(r, _channels(torch, state, B, D), _pack_steps(*_steps_view(out, x.shape, x.dtype)),
@@ -1096,6 +1113,7 @@ def orthogonalise(x, steps=None, coefficients=ORTHOGONALISE_COEFFICIENTS, eps=1e
     shape, s = x.shape, x.stride()
     assert x.is_cuda and len(shape) in (2, 3) and shape[-2] > 0 and shape[-1] > 0, "a CUDA tensor [m,n] or [B,m,n]"
     assert s[-1] == 1 or shape[-1] == 1, "the values of a row must be adjacent"
+    _here(torch, x, out)
     given = out is not None
     if out is None:
         out = _empty(torch, x, stream, shape, x.dtype)

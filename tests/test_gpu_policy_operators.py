@@ -208,6 +208,29 @@ def test_heads_of_one_kind_alone(torch, policy_module):
     layer.close()
 
 
+def test_tensors_of_another_device_are_refused(torch, monkeypatch):
+    """As where a program has made another device the current one: the kernels would go there."""
+    from paper_2502_00021_amd import pxr
+    layer = pxr.HeadNorm(8)
+    x, heads, state = torch.ones(2, 3, 8, device="cuda"), torch.ones(2, 3, 1, 8, device="cuda"), torch.zeros(2, 8, device="cuda")
+    calls = [lambda: pxr.gated_recurrence(x, x, state=state), lambda: pxr.gated_recurrence_backward(x, x, x, state=state), lambda: pxr.gated_recurrence_step(x[:, 0], x[:, 1], state),
+             lambda: layer.forward(heads, heads), lambda: layer.backward(heads, heads, heads, heads), lambda: pxr.orthogonalise(x)]
+    for call in calls:
+        call()
+    with monkeypatch.context() as m:
+        m.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+        for call in calls:
+            with pytest.raises(AssertionError, match="cuda:0, and the current device is cuda:1"):
+                call()
+    layer._device = 1
+    with pytest.raises(AssertionError, match="a layer of cuda:1"):
+        layer.forward(heads, heads)
+    layer._device = 0
+    layer.close()
+    with pytest.raises(pxr.PxrError, match="null"):
+        layer.forward(heads, heads)
+
+
 def test_momentum_of_bfloat16_matrices_is_float32(torch, policy_module):
     """0.95 m + g is rounded twice a step, and what is rounded fades: 2 u |m| 20 steps long."""
     p = torch.nn.Parameter(torch.zeros(24, 40, device="cuda", dtype=torch.bfloat16))
