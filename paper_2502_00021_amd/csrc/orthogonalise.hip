@@ -307,16 +307,18 @@ __device__ __forceinline__ void put_out(const Product& p, uint32_t matrix, uint3
 // A tile of 64 M x 64 M values by four wavefronts, 2 x 2, each 32 M x 32 M.
 constexpr uint32_t stages(int M) { return M == 2 ? 2u : 2u; }
 
-template <int kKind, int M>
-__global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
+// G groups of four wavefronts have the same tile and every Gth step of the summed axis each.
+template <int kKind, int M, int G>
+__global__ __launch_bounds__(kThreads * G) void product_kernel(const Product p) {
     constexpr int kSide = 64 * M;
     constexpr uint32_t kDepth = depth_of(M), kStages = stages(M);  // in LDS: one that is worked on, the others on their way
     constexpr bool kSym = kKind <= kPoly;
     typedef Operand<kSide, false> OpA;
     typedef Operand<kSide, !kSym> OpB;
     constexpr uint32_t kPlane = kSide * kDepth, kStage = 4 * kPlane;  // halves: A hi, A lo, B hi, B lo
-    __shared__ __align__(16) half stage[kStages][kStage];
-    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.z;
+    __shared__ __align__(16) half stages_of[G][kStages][kStage];
+    const uint32_t lane = threadIdx.x & 63u, of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = of_all & 3u, group = G == 1 ? 0u : of_all >> 2, matrix = blockIdx.z;
+    half(&stage)[kStages][kStage] = stages_of[group];
     // (whole tiles and parts of tiles each in their own order: every die has as many of both)
     const uint32_t tiles = kSym ? p.tiles_i * (p.tiles_i + 1u) / 2u : p.tiles_i * p.tiles_j, cut = tiles - p.whole, of_whole = on_dies(p.whole);
     const bool partly = blockIdx.x >= of_whole;
@@ -332,7 +334,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
     // each wavefront asks for every fourth run of 64 chunks of each plane
     constexpr uint32_t kRuns = OpA::kChunks / 64 / 4;
     const half *a_from[kRuns], *b_from[kRuns];
-    const uint32_t k_first = part * p.steps_each * kDepth;
+    const uint32_t k_first = (part * p.steps_each + group) * kDepth;
 #pragma unroll
     for (uint32_t n = 0; n < kRuns; ++n) {
         uint32_t row, col;
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
         OpB::place((n * 4u + wave) * 64u + lane, row, col);
         b_from[n] = p.b.at(0, matrix) + (kSym ? (size_t)(j0 + row) * p.b.row + k_first + col : (size_t)(k_first + row) * p.b.row + j0 + col);
     }
-    const size_t b_step = kSym ? kDepth : (size_t)kDepth * p.b.row;
+    const size_t b_step = kSym ? G * kDepth : (size_t)G * kDepth * p.b.row;
     const auto ask = [&](half* to) {
         typedef const __attribute__((address_space(1))) void* global;
         typedef __attribute__((address_space(3))) void* shared;
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
             }
 #pragma unroll
         for (uint32_t n = 0; n < kRuns; ++n) {
-            a_from[n] += kDepth;
+            a_from[n] += G * kDepth;
             b_from[n] += b_step;
         }
     };
@@ -364,10 +366,10 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
 #pragma unroll
         for (int j = 0; j < M; ++j) acc[i][j] = (f32x16)0.0f;
     const uint32_t row0 = (wave >> 1) * 32 * M, col0 = (wave & 1u) * 32 * M;
-    const uint32_t left = p.depth / kDepth - part * p.steps_each, steps = partly ? min(p.steps_each, left) : left;
+    const uint32_t left = p.depth / kDepth - part * p.steps_each, all_steps = partly ? min(p.steps_each, left) : left, steps = (all_steps + G - 1u - group) / G;
     for (uint32_t k = 0; k + 1u < kStages && k < steps; ++k) ask(stage[k]);
     uint32_t now = 0, next = kStages - 1u;
-    for (uint32_t k = 0; k < steps; ++k) {
+    for (uint32_t k = 0; k < (all_steps + G - 1u) / G; ++k) {
         // the oldest stage is there (requests are answered in their order); towards the end fewer are on their way, and all are waited for
         // (a barrier by itself: __syncthreads would wait for all of them.  The values that were read of the stage that is asked for next have been used.)
         if (k + kStages - 1u <= steps)
@@ -380,6 +382,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
         const half* from = stage[now];
         now = now + 1u == kStages ? 0u : now + 1u;
         next = next + 1u == kStages ? 0u : next + 1u;
+        if (G > 1 && k >= steps) break;  // (the last one, of a group that has one less)
 #pragma unroll
         for (uint32_t kk = 0; kk < kDepth / 16; ++kk) {
             f16x8 a[M][2], b[M][2];
@@ -398,9 +401,24 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
                 }
         }
     }
+    if constexpr (G > 1) {  // the groups' sums, in their order
+        static_assert(M == 1, "");
+        float* const sums = reinterpret_cast<float*>(&stages_of[0][0][0]);
+        __syncthreads();
+        if (group)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sums[((group - 1u) * 16u + r) * kThreads + wave * 64u + lane] = acc[0][0][r];
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+            for (uint32_t g = 0; g + 1u < G; ++g)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[0][0][r] += sums[(g * 16u + r) * kThreads + wave * 64u + lane];
+    }
     // a lane has column lane % 32 and rows 8 (r / 4) + 4 (lane / 32) + r % 4 of every 32 x 32
     const uint32_t down = 4u * (lane >> 5), across = lane & 31u;
     if (kSym && partly) {
+        if (group) return;
         float* to = p.partial + (((size_t)matrix * p.splits + part) * cut + tile - p.whole) * (kSide * kSide);
 #pragma unroll
         for (int i = 0; i < M; ++i)
@@ -412,14 +430,14 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
         return;
     }
     // Through LDS, 64 rows of the tile at a time, so that rows leave in whole lines; of a symmetric product the mirrored tile too.
-    float* const pass = reinterpret_cast<float*>(&stage[0][0]);
+    float* const pass = reinterpret_cast<float*>(&stages_of[0][0][0]);
     const half *ah = p.a.at(0, matrix), *al = p.a.at(1, matrix);
     half *th = p.to.at(0, matrix), *tl = p.to.at(1, matrix);
     const auto leave = [&](auto turned, uint32_t part64) {
         constexpr bool kTurned = decltype(turned)::value;
         constexpr uint32_t kRow = kTurned ? 64u + 4u : kSide + 4u, kRows = kTurned ? kSide : 64u, kQuads = (kTurned ? 64u : kSide) / 4u;
         __syncthreads();
-        if (M == 1 || wave >> 1 == part64) {
+        if (group == 0 && (M == 1 || wave >> 1 == part64)) {
             const uint32_t row_in = M == 1 ? row0 : 0u;
 #pragma unroll
             for (int i = 0; i < M; ++i)
@@ -437,7 +455,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Product p) {
                     }
         }
         __syncthreads();
-        for (uint32_t n = threadIdx.x; n < kRows * kQuads; n += kThreads) {
+        for (uint32_t n = threadIdx.x; n < kRows * kQuads; n += kThreads * G) {
             const uint32_t r = n / kQuads, c = n % kQuads * 4u;
             const f32x4 v = *reinterpret_cast<const f32x4*>(pass + r * kRow + c) * p.scale;
             const uint32_t row = kTurned ? j0 + r : i0 + part64 * 64u + r, col = kTurned ? i0 + part64 * 64u + c : j0 + c;
@@ -750,10 +768,17 @@ struct Layout {
 // 2048, 1088, 5226, 4824; four, 544, 2527, 2635; 32 of 1024, 1152, 3143, 2999; 16, 576, 1497, 1593; 200 of 512, 10 tiles each, 3642, 3943.
 constexpr uint64_t kLargeTiles = 400, kLargeBatch = 1000;
 constexpr uint32_t kLargeEach = 32;
+// A product of no more workgroups than compute units has two groups of wavefronts in each (at twice that many workgroups: 1300 x 1300 310 us, 290 without).
+constexpr uint64_t kFewGroups = 256;
+constexpr int kGroups = 2;
+constexpr uint32_t kJoinSteps = 6;  // that take as long as a join_kernel
 constexpr uint64_t kPlaces = 512;  // workgroups that a device has room for at once, two on a compute unit
 
 uint32_t tiles_of(uint32_t n, int M) { return (n + 64u * M - 1u) / (64u * M); }
 uint32_t triangle_of(uint32_t s, int M) { return tiles_of(s, M) * (tiles_of(s, M) + 1u) / 2u; }
+
+// The steps that a wavefront takes one after the other.
+uint32_t in_turn(uint32_t steps, uint64_t workgroups) { return workgroups <= kFewGroups ? (steps + kGroups - 1u) / kGroups : steps; }
 
 // Tiles that do not fill the places, and those that are left when the others have filled them some times, are cut along the summed axis; no part has fewer than 8 steps.
 Cut cut_of(uint32_t s, uint32_t depth, uint32_t n_matrices) {
@@ -765,6 +790,7 @@ Cut cut_of(uint32_t s, uint32_t depth, uint32_t n_matrices) {
     const uint64_t left = (uint64_t)(tiles - c.whole) * n_matrices;
     c.splits = left ? (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(steps / (256u / depth_of(c.M)), kPlaces / left)) : 1u;
     c.steps_each = (steps + c.splits - 1u) / c.splits;
+    if (c.whole == 0u && in_turn(steps, left) < in_turn(c.steps_each, left * c.splits) + kJoinSteps) c.steps_each = steps;
     c.splits = (steps + c.steps_each - 1u) / c.steps_each;
     if (c.splits == 1u) c.whole = tiles;
     return c;
@@ -820,9 +846,11 @@ hipError_t launch_product(const Product& p, int M, uint32_t n_matrices, hipStrea
     const uint32_t tiles = kSym ? p.tiles_i * (p.tiles_i + 1u) / 2u : p.tiles_i * p.tiles_j, cut = tiles - p.whole;
     const dim3 grid(on_dies(p.whole) + on_dies(cut * p.splits), 1, n_matrices), threads(kThreads), joined(cut * 4u * M * M, 1, n_matrices);
     if (M == 2)
-        hipLaunchKernelGGL((product_kernel<kKind, 2>), grid, threads, 0, st, p);
+        hipLaunchKernelGGL((product_kernel<kKind, 2, 1>), grid, threads, 0, st, p);
+    else if ((uint64_t)(p.whole + cut * p.splits) * n_matrices <= kFewGroups)
+        hipLaunchKernelGGL((product_kernel<kKind, 1, kGroups>), grid, dim3(kThreads * kGroups), 0, st, p);
     else
-        hipLaunchKernelGGL((product_kernel<kKind, 1>), grid, threads, 0, st, p);
+        hipLaunchKernelGGL((product_kernel<kKind, 1, 1>), grid, threads, 0, st, p);
     if constexpr (kSym)
         if (cut) {
             if (M == 2)
