@@ -402,18 +402,26 @@ __global__ __launch_bounds__(kThreads * G) void product_kernel(const Product p) 
         }
     }
     if constexpr (G > 1) {  // the groups' sums, in their order
-        static_assert(M == 1, "");
-        float* const sums = reinterpret_cast<float*>(&stages_of[0][0][0]);
+        constexpr uint32_t kEach = M * M * 16;
+        float* const sums = reinterpret_cast<float*>(&stages_of[0][0][0]) + wave * 64u + lane;
         __syncthreads();
         if (group)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sums[((group - 1u) * 16u + r) * kThreads + wave * 64u + lane] = acc[0][0][r];
+            for (int i = 0; i < M; ++i)
+#pragma unroll
+                for (int j = 0; j < M; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sums[((group - 1u) * kEach + (i * M + j) * 16u + r) * kThreads] = acc[i][j][r];
         __syncthreads();
         if (group == 0)
 #pragma unroll
             for (uint32_t g = 0; g + 1u < G; ++g)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[0][0][r] += sums[(g * 16u + r) * kThreads + wave * 64u + lane];
+                for (int i = 0; i < M; ++i)
+#pragma unroll
+                    for (int j = 0; j < M; ++j)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[i][j][r] += sums[(g * kEach + (i * M + j) * 16u + r) * kThreads];
     }
     // a lane has column lane % 32 and rows 8 (r / 4) + 4 (lane / 32) + r % 4 of every 32 x 32
     const uint32_t down = 4u * (lane >> 5), across = lane & 31u;
@@ -845,9 +853,13 @@ hipError_t launch_product(const Product& p, int M, uint32_t n_matrices, hipStrea
     constexpr bool kSym = kKind <= kPoly;
     const uint32_t tiles = kSym ? p.tiles_i * (p.tiles_i + 1u) / 2u : p.tiles_i * p.tiles_j, cut = tiles - p.whole;
     const dim3 grid(on_dies(p.whole) + on_dies(cut * p.splits), 1, n_matrices), threads(kThreads), joined(cut * 4u * M * M, 1, n_matrices);
-    if (M == 2)
-        hipLaunchKernelGGL((product_kernel<kKind, 2, 1>), grid, threads, 0, st, p);
-    else if ((uint64_t)(p.whole + cut * p.splits) * n_matrices <= kFewGroups)
+    const bool few = (uint64_t)(p.whole + cut * p.splits) * n_matrices <= kFewGroups;
+    if (M == 2) {  // (a symmetric product takes tiles of this size where there are many)
+        if (kSym || !few)
+            hipLaunchKernelGGL((product_kernel<kKind, 2, 1>), grid, threads, 0, st, p);
+        else if constexpr (!kSym)
+            hipLaunchKernelGGL((product_kernel<kKind, 2, kGroups>), grid, dim3(kThreads * kGroups), 0, st, p);
+    } else if (few)
         hipLaunchKernelGGL((product_kernel<kKind, 1, kGroups>), grid, dim3(kThreads * kGroups), 0, st, p);
     else
         hipLaunchKernelGGL((product_kernel<kKind, 1, 1>), grid, threads, 0, st, p);
