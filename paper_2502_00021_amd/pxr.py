@@ -633,9 +633,9 @@ def _empty(torch, like, stream, shape, dtype):
 
 
 def _empty_like(torch, like, stream):
-    """Device memory of a tensor's shape and type, contiguous (for one that is contiguous itself, at less cost)."""
-    if stream is None and like.is_contiguous():
-        return torch.empty_like(like)
+    """Device memory of a tensor's shape and type, contiguous (at less cost than _empty)."""
+    if stream is None:
+        return torch.empty_like(like) if like.is_contiguous() else torch.empty_like(like, memory_format=torch.contiguous_format)
     return _empty(torch, like, stream, like.shape, like.dtype)
 
 
@@ -922,9 +922,9 @@ class HeadNorm:
         _here(torch, *tensors)
         assert self._device == torch._C._cuda_getDevice(), f"a layer of cuda:{self._device}"
 
-    def _new(self, torch, x, shape, dtype, stream):
-        """A contiguous tensor of x's shape, and its pxr_tokens."""
-        out = _empty(torch, x, stream, shape, dtype)
+    def _new(self, torch, x, shape, stream):
+        """A contiguous tensor like x, and its pxr_tokens."""
+        out = _empty_like(torch, x, stream)
         H, d = shape[-2:]
         return out, _pack_tokens(out.data_ptr(), (shape[1] if len(shape) == 4 else 1) * H * d, H * d, d)
 
@@ -942,12 +942,12 @@ class HeadNorm:
             assert q is not None
             to_q = _pack_tokens(*self._view(q_out, qs, dtype))
         elif q is not None:
-            q_out, to_q = self._new(torch, q, qs, dtype, stream)
+            q_out, to_q = self._new(torch, q, qs, stream)
         if k_out is not None:
             assert k is not None
             to_k = _pack_tokens(*self._view(k_out, ks, dtype))
         elif k is not None:
-            k_out, to_k = self._new(torch, k, ks, dtype, stream)
+            k_out, to_k = self._new(torch, k, ks, stream)
         _check(_lib.pxr_head_norm_forward(self._h, r, to_q, to_k, _stream_handle(stream, q if q is not None else k)))
         if given:
             _written(torch, *given)
@@ -968,7 +968,7 @@ class HeadNorm:
         for i, (x, d, shape) in enumerate(((q, dq, qs), (k, dk, ks))):
             if x is not None:
                 given[i] = _pack_tokens(*self._view(d, shape, dtype))
-                grads[i], into[i] = self._new(torch, x, shape, dtype, stream)
+                grads[i], into[i] = self._new(torch, x, shape, stream)
                 sums[i] = _empty(torch, x, stream, (self.d,), params)
         sizes = r[:24]
         asked, need = self._asked  # (the bytes for the sizes that were asked for last are known)
@@ -1116,7 +1116,7 @@ def orthogonalise(x, steps=None, coefficients=ORTHOGONALISE_COEFFICIENTS, eps=1e
     _here(torch, x, out)
     given = out is not None
     if out is None:
-        out = _empty(torch, x, stream, shape, x.dtype)
+        out = _empty_like(torch, x, stream)
     else:
         assert out.is_cuda and out.dtype == x.dtype and out.shape == shape and (out.stride(-1) == 1 or shape[-1] == 1)
     t = out.stride()
