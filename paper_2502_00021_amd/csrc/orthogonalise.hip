@@ -10,6 +10,9 @@
 // together, and a product is three: hi hi + hi lo + lo hi; lo lo is 2^-22 of it and left out.  fp16 has the bits that bfloat16 has not (two parts of it are 16 bits: an
 // update whose singular values lie far apart loses its small ones) and its range does not matter: a singular value of X_k, and so every value of X, A and B, has a
 // bound that follows from the coefficients alone, and each of the three is held times a power of two that puts that bound just below fp16's largest.
+//
+// Large matrices are bound by the matrix cores, and those by the power that they may draw: 4096 x 4096 in 4.3 ms, 1.0 PFLOP/s of fp16 where a library's product of 8192 reaches 1.16 (an update's
+// product 390 us, 60 % of its clocks in matrix instructions).  Below about 1000 x 1000 it is the chain of launches, 16 to 27 of 5 to 9 us each; matrices that fit LDS have one.
 
 #include <hip/hip_runtime.h>
 
@@ -31,14 +34,14 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kThreads = 256;
-constexpr uint32_t kPad = 128;       // rows and columns of the matrices in the workspace come in multiples of it; what is behind the matrix is zeros
-constexpr uint32_t kNormParts = 512; // of a matrix whose squares are summed, at most
+constexpr uint32_t kPad = 128;       // rows and columns of the matrices in the workspace come in multiples of it, a large tile's side; what is behind the matrix is zeros
+constexpr uint32_t kNormParts = 512; // of a matrix whose squares are summed, at most (1024 and 2048: within 1 % either way)
 constexpr uint32_t kNormColumns = 1024;
 // Values of the summed axis in one chain of sums; the chains' results are added up.  (Of one chain of all, 4096 x 4096 in fp32 are off by 3.2e-6 of their norm, by 1.2e-6 of these, and in plain fp32
 // by 4.8e-6; in bfloat16 they take 4285 us instead of
 // 4235.  Chains of 256: 1.0e-6, 4319 us.)
 constexpr uint32_t kChain = 512;
-constexpr uint32_t depth_of(int M) { return M == 2 ? 32u : 64u; }  // values of the summed axis that a stage in LDS has
+constexpr uint32_t depth_of(int M) { return M == 2 ? 32u : 64u; }  // values of the summed axis that a stage in LDS has: 32 KB either way (32 of small tiles: 1024 x 1024 279 us, 64 245)
 
 __host__ __device__ constexpr uint32_t padded(uint32_t n) { return (n + kPad - 1u) / kPad * kPad; }
 
@@ -213,8 +216,8 @@ __device__ __forceinline__ void of_triangle(uint32_t t, uint32_t rows, uint32_t&
     }
 }
 
-// A tile's operand in LDS, one plane, kDepth values deep.  Along: rows of 64 bytes, 4 chunks of 8 values, chunk c of row r at place c ^ (r / 4 % 4): the 16 rows whose chunks of one c are
-// read together lie in the 64 banks once each.  Across (the summed axis is the rows'): rows of `kSide` values; the transposing read takes 32 values of four rows together, chunks of them at place
+// A tile's operand in LDS, one plane, kDepth values deep.  Along: rows of 64 or 128 bytes, chunks of 8 values, chunk c of row r at place c ^ (r / 4 % 4) or c ^ (r / 2 % 8): the 16 rows whose chunks of
+// one c are read together lie in the 64 banks once each.  Across (the summed axis is the rows'): rows of `kSide` values; the transposing read takes 32 values of four rows together, chunks of them at place
 // c ^ 4 (k % 4), or where two rows are 256 bytes c ^ 4 (k / 2 % 2).  The requests that write LDS put a wavefront's lanes side by side, so it is the addresses that they ask for which are
 // exchanged.  (Exchanged for 32 banks, half of the LDS' cycles were conflicts: 4096 x 4096 bfloat16 5250 us.)
 template <int kSide, bool kAcross>
@@ -308,21 +311,20 @@ __device__ __forceinline__ void put_out(const Product& p, uint32_t matrix, uint3
         put_values(static_cast<float*>(p.out) + at, v, p.cols - col);
 }
 
-// A tile of 64 M x 64 M values by four wavefronts, 2 x 2, each 32 M x 32 M.
-constexpr uint32_t stages(int M) { return M == 2 ? 2u : 2u; }
-
+// A tile of 64 M x 64 M values by four wavefronts, 2 x 2, each 32 M x 32 M.  Two stages in LDS, one that is worked on and one on its way, 64 KB: two workgroups a compute unit, and one's matrix
+// instructions run while the other waits.  (Three and four stages of large tiles, one workgroup: 4096 x 4096 4710 and 4740 us, with two 4260; of small ones 1000 x 4000 424 and 423, 383.)
 // G groups of four wavefronts have the same tile and every Gth step of the summed axis each.
 template <int kKind, int M, int G>
 __global__ __launch_bounds__(kThreads * G) void product_kernel(const Product p) {
     constexpr int kSide = 64 * M;
-    constexpr uint32_t kDepth = depth_of(M), kStages = stages(M);  // in LDS: one that is worked on, the others on their way
+    constexpr uint32_t kDepth = depth_of(M);
     constexpr bool kSym = kKind <= kPoly;
     typedef Operand<kSide, false> OpA;
     typedef Operand<kSide, !kSym> OpB;
     constexpr uint32_t kPlane = kSide * kDepth, kStage = 4 * kPlane;  // halves: A hi, A lo, B hi, B lo
-    __shared__ __align__(16) half stages_of[G][kStages][kStage];
+    __shared__ __align__(16) half stages_of[G][2][kStage];
     const uint32_t lane = threadIdx.x & 63u, of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = of_all & 3u, group = G == 1 ? 0u : of_all >> 2, matrix = blockIdx.z;
-    half(&stage)[kStages][kStage] = stages_of[group];
+    half(&stage)[2][kStage] = stages_of[group];
     // (whole tiles and parts of tiles each in their own order: every die has as many of both)
     const uint32_t tiles = kSym ? p.tiles_i * (p.tiles_i + 1u) / 2u : p.tiles_i * p.tiles_j, cut = tiles - p.whole, of_whole = on_dies(p.whole);
     const bool partly = blockIdx.x >= of_whole;
@@ -371,27 +373,18 @@ __global__ __launch_bounds__(kThreads * G) void product_kernel(const Product p) 
         for (int j = 0; j < M; ++j) acc[i][j] = whole[i][j] = (f32x16)0.0f;
     const uint32_t row0 = (wave >> 1) * 32 * M, col0 = (wave & 1u) * 32 * M;
     const uint32_t left = p.depth / kDepth - part * p.steps_each, all_steps = partly ? min(p.steps_each, left) : left, steps = (all_steps + G - 1u - group) / G;
-    for (uint32_t k = 0; k + 1u < kStages && k < steps; ++k) ask(stage[k]);
-    uint32_t now = 0, next = kStages - 1u;
-    const uint32_t turns = (all_steps + G - 1u) / G;
+    if (steps) ask(stage[0]);
     constexpr uint32_t kTogether = kChain / kDepth;
-    for (uint32_t first = 0; first < turns; first += kTogether) {
-        const uint32_t last = min(turns, first + kTogether);
+    for (uint32_t first = 0; first < steps; first += kTogether) {
+        const uint32_t last = min(steps, first + kTogether);
 #pragma nounroll
         for (uint32_t k = first; k < last; ++k) {
-            // the oldest stage is there (requests are answered in their order); towards the end fewer are on their way, and all are waited for
-            // (a barrier by itself: __syncthreads would wait for all of them.  The values that were read of the stage that is asked for next have been used.)
-            if (k + kStages - 1u <= steps)
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2u) * kRuns * 4u) : "memory");
-            else
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            // this stage is there, and the values that were read of the other one have been used
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (k + kStages - 1u < steps) ask(stage[next]);
-            const half* from = stage[now];
-            now = now + 1u == kStages ? 0u : now + 1u;
-            next = next + 1u == kStages ? 0u : next + 1u;
-            if (G > 1 && k >= steps) break;  // (the last one, of a group that has one less)
+            if (k + 1u < steps) ask(stage[(k + 1u) & 1u]);
+            const half* from = stage[k & 1u];
 #pragma unroll
             for (uint32_t kk = 0; kk < kDepth / 16; ++kk) {
                 f16x8 a[M][2], b[M][2];
@@ -418,6 +411,9 @@ __global__ __launch_bounds__(kThreads * G) void product_kernel(const Product p) 
                 acc[i][j] = (f32x16)0.0f;
             }
     }
+    // (A group that has a step less: the barrier of the others' last one.  Not a way out of the middle of the loop: behind such a one the compiler has left out the wait between a matrix instruction
+    // and the first use of its result.)
+    if (G > 1 && steps < (all_steps + G - 1u) / G) __builtin_amdgcn_s_barrier();
 #pragma unroll
     for (int i = 0; i < M; ++i)
 #pragma unroll
@@ -800,7 +796,7 @@ constexpr uint32_t kLargeEach = 32;
 // A product of no more workgroups than compute units has two groups of wavefronts in each (at twice that many workgroups: 1300 x 1300 310 us, 290 without).
 constexpr uint64_t kFewGroups = 256;
 constexpr int kGroups = 2;
-constexpr uint32_t kJoinSteps = 6;  // that take as long as a join_kernel
+constexpr uint32_t kJoinSteps = 6;  // that take as long as a join_kernel (4 within 2 %; 9: 200 x 1000 127 us, 114 so)
 constexpr uint64_t kPlaces = 512;  // workgroups that a device has room for at once, two on a compute unit
 
 uint32_t tiles_of(uint32_t n, int M) { return (n + 64u * M - 1u) / (64u * M); }
@@ -809,7 +805,9 @@ uint32_t triangle_of(uint32_t s, int M) { return tiles_of(s, M) * (tiles_of(s, M
 // The steps that a wavefront takes one after the other.
 uint32_t in_turn(uint32_t steps, uint64_t workgroups) { return workgroups <= kFewGroups ? (steps + kGroups - 1u) / kGroups : steps; }
 
-// Tiles that do not fill the places, and those that are left when the others have filled them some times, are cut along the summed axis; no part has fewer than 8 steps.
+// Tiles that do not fill the places, and those that are left when the others have filled them some times (4096 x 4096: 16 of 528; as whole ones 5025 us, 4560 so), are cut along the summed axis, into
+// parts of 256 values at least (of 512 or 1024: 200 x 5000 143 and 169 us, 133 so).  Tiles that fill no place twice are cut only where a part takes kJoinSteps steps less than the whole: 1024 x 1024
+// in three parts 226 us, in one 198; 700 x 2000 in one 227, in seven 200; 200 x 1500 in one 151, in five 119.
 Cut cut_of(uint32_t s, uint32_t depth, uint32_t n_matrices) {
     Cut c{};
     c.M = triangle_of(s, 2) >= kLargeEach && triangle_of(s, 2) * (uint64_t)n_matrices >= (n_matrices == 1u ? kLargeTiles : kLargeBatch) ? 2 : 1;
@@ -834,6 +832,7 @@ Layout layout_of(const pxr_orthogonalise_desc& d) {
     y.parts = (uint32_t)std::min<uint64_t>(kNormParts, norm_units(d.rows, d.cols));
     y.gram = cut_of(y.s, y.l, d.n_matrices);
     y.poly = cut_of(y.s, y.s, d.n_matrices);
+    // (1300 x 1300, 121 of them, 338 us in tiles of 128 x 128, 293 of 64 x 64; 1500 x 1500, 144, 453 and 471; 2048 x 2048, 256, 728 and 780)
     y.update = (uint64_t)tiles_of(y.s, 2) * tiles_of(y.l, 2) * d.n_matrices >= 128u ? 2 : 1;
     size_t at = 0;
     const auto take = [&](size_t bytes) {
