@@ -11,7 +11,8 @@
 // product A of +0 is that of steps among which an episode begins and passes nothing on, whatever the state holds: what is not finite stays on its side of the beginning.
 // One that is merely too small for fp32 is -0, which a state that is not finite does pass.
 //
-// Bound by HBM.
+// Bound by HBM: 256 environments of 128 steps of 1024 channels of bfloat16 take 44 us, 203 MB at 4.6 TB/s; gradients of 512 x 256 x 1024 316 us, 1.34 GB at 4.2 (79 % of the cycles issue vector
+// instructions); a step of 16384 x 1024 43 us, 235 MB at 5.5.  Few long rollouts are cut into segments: the segments' (A, H, R), what comes into each, outputs.  1 x 50000 x 512 take 26 + 7 + 27 us.
 
 #include <hip/hip_runtime.h>
 
@@ -124,7 +125,7 @@ struct Recurrence {
 };
 
 enum { kForward, kForwardSums, kBackward, kBackwardSums };
-constexpr int C = 16;                  // steps of a wavefront
+constexpr int C = 16;                  // steps of a wavefront: as many as its registers have room for (8: 256 x 128 x 1024 49 us, 46 so; gradients of 512 x 256 x 1024, then in two segments, 624, 316)
 constexpr uint32_t kMostWaves = 16;    // of a workgroup
 
 // Where a lane's channels are: of environment `env`, from channel `at` on.  A row that ends inside a vector has its last vector moved back to its end: the values that
@@ -477,6 +478,15 @@ struct Shape {
     uint32_t V, lanes, rows, strips, waves, segments, seg_steps;
 };
 
+// A workgroup takes 4.7 us for a block of its steps, one after the other, and 128 of them side by side as many bytes a second as segments do, which read everything twice: forward passes are cut into
+// segments only below that many, and from the number of blocks on that takes longer than three launches.  (100 x 600 x 1024, 800 groups: in two segments 157 us, whole 98; 24 x 1000 x 1024, 192: 57,
+// 51; 64 x 1000 x 128, 64 groups of 8 blocks: 26, 41; of 3 blocks 20, 17.)
+constexpr uint32_t kFewBlocks = 4, kFewGroups = 128;
+// Workgroups of a forward pass have half of the wavefronts that they may have, unless there is at most one for a compute unit (200 x 1000 x 128: 8 wavefronts 52 us, 16 45; 300 x 1000 x 128: 72, 82;
+// segments of 1 x 50000 x 512: 61, 78).
+constexpr uint32_t kHalfWaves = kMostWaves / 2, kUnits = 256;
+constexpr uint32_t kManyGroups = 2048;  // that segments make (1 x 50000 x 512: 1024 of them 67 us, 2048 62)
+
 // How a call is cut (lanes, rows, strips: by its strides as well, in narrowed()).
 Shape shape_of(uint32_t V, uint32_t n_envs, uint32_t n_steps, uint32_t width, bool backward) {
     Shape s{};
@@ -485,22 +495,23 @@ Shape shape_of(uint32_t V, uint32_t n_envs, uint32_t n_steps, uint32_t width, bo
     while (s.lanes < 64u && s.lanes * s.V < width) s.lanes *= 2u;
     s.rows = (n_envs + 64u / s.lanes - 1u) / (64u / s.lanes);
     s.strips = (width + s.lanes * s.V - 1u) / (s.lanes * s.V);
-    const uint32_t chunks = (n_steps + C - 1u) / C, most = backward ? kMostWaves : kMostWaves / 2u, blocks = (chunks + most - 1u) / most;
-    if (backward) {
+    const uint32_t chunks = (n_steps + C - 1u) / C;
+    const auto blocks_of = [&](uint32_t waves) { return (chunks + waves - 1u) / waves; };
+    const uint64_t groups = (uint64_t)n_envs * ((width + 127u) / 128u);  // (by the sizes alone, like the workspace)
+    if (backward || blocks_of(kHalfWaves) <= kFewBlocks || groups >= kFewGroups) {
+        const uint32_t blocks = blocks_of(backward || (uint64_t)s.rows * s.strips <= kUnits ? kMostWaves : kHalfWaves);
         s.waves = (chunks + blocks - 1u) / blocks;
-        s.seg_steps = s.waves * C;
+        s.seg_steps = (backward ? 1u : blocks) * s.waves * C;
     } else {
-        const uint64_t groups = (uint64_t)n_envs * ((width + 127u) / 128u);  // (by the sizes alone, like the workspace)
-        const uint32_t cut = (uint32_t)std::min<uint64_t>(blocks, groups >= 1024u ? 1u : (1024u + groups - 1u) / groups);
-        const uint32_t each = (blocks + cut - 1u) / cut;  // blocks of a segment
-        s.waves = std::min(chunks, most);
-        s.seg_steps = each * s.waves * C;
+        const uint32_t blocks = blocks_of(kHalfWaves), cut = (uint32_t)std::min<uint64_t>(blocks, (kManyGroups + groups - 1u) / groups);
+        s.waves = kHalfWaves;
+        s.seg_steps = (blocks + cut - 1u) / cut * s.waves * C;
     }
     s.segments = (n_steps + s.seg_steps - 1u) / s.seg_steps;
     return s;
 }
 
-// Values of a lane: 4 bytes of them.
+// Values of a lane: 4 bytes of them.  (Of bfloat16 one: 256 x 128 x 1024 55 us, 46 so; gradients of 512 x 256 x 1024 348, 316.)
 uint32_t values_of(const pxr_gated_rollout& r) { return r.dtype == PXR_BF16 && r.width >= 2u ? 2u : 1u; }
 
 // Environments that share a wavefront are numbers of 32 bits apart, in bytes; where they lie further, or backwards, each has one to itself.

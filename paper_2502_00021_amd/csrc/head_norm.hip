@@ -9,7 +9,8 @@
 // The angle is formed in whole numbers: f / 2 pi as a fraction of 2^64, times the position, modulo 2^64 is the angle in turns modulo one, exact but for the fraction's
 // own rounding: positions of 2^31 are off by 2^-22 turns, where a product in fp32 has lost them all.
 //
-// Bound by HBM.
+// Bound by HBM: 256 x 128 steps of 8 + 8 heads of 64 bfloat16 29 us, 134 MB at 4.6 TB/s; gradients of 512 x 256 of 16 + 4 heads 206 us, 1.01 GB at 4.9.  (Stores past the caches: no faster, since what
+// follows finds the heads there.)
 
 #include <hip/hip_runtime.h>
 
@@ -272,7 +273,7 @@ HeadNormShape shape_of(const HeadNormConsts& c, uint32_t dtype, uint64_t tokens,
     while (s.lanes < 64u && s.lanes * s.V < slots) s.lanes *= 2u;
     s.K = s.lanes * s.V < slots ? 2u : 1u;
     const uint32_t U = together(backward), parts = (n_heads + U - 1u) / U + (n_key_heads + U - 1u) / U;
-    // a token's heads are shared out where the tokens alone are too few wavefronts
+    // a token's heads are shared out where the tokens alone are too few wavefronts (512 and 4096 of them: 16 x 100 steps of 8 + 2 heads 14.1 and 14.4 us, 13.4 so)
     const uint64_t waves = (tokens * s.lanes + 63u) / 64u;
     s.split = (uint32_t)std::min<uint64_t>(std::max(parts, 1u), waves ? (2048u + waves - 1u) / waves : 1u);
     const uint32_t per_group = kThreads / s.lanes;
