@@ -11,8 +11,8 @@
 // update whose singular values lie far apart loses its small ones) and its range does not matter: a singular value of X_k, and so every value of X, A and B, has a
 // bound that follows from the coefficients alone, and each of the three is held times a power of two that puts that bound just below fp16's largest.
 //
-// Large matrices are bound by the matrix cores, and those by the power that they may draw: 4096 x 4096 in 4.3 ms, 1.0 PFLOP/s of fp16 where a library's product of 8192 reaches 1.16 (an update's
-// product 390 us, 60 % of its clocks in matrix instructions).  Below about 1000 x 1000 it is the chain of launches, 16 to 27 of 5 to 9 us each; matrices that fit LDS have one.
+// Large matrices are bound by the matrix cores, and those by the power that they may draw: 4096 x 4096 in 4.3 ms, 0.95 PFLOP/s of fp16 where a library's product of 8192 reaches 1.16 (an
+// update's product 395 us, 60 % of its clocks in matrix instructions).  Below about 1000 x 1000 it is the chain of launches, 17 to 27 of 5 to 9 us each; matrices that fit LDS have one.
 
 #include <hip/hip_runtime.h>
 
