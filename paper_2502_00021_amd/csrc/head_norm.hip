@@ -69,20 +69,50 @@ __device__ __forceinline__ void sine(uint32_t turn, float& s, float& c) {
     c = (quarter + 1u) & 2u ? -b : b;
 }
 
-// Where V slots from `slot` on lie in a head, and how many of their second values there are (kOne: of a head of any size; otherwise
-// vectors are whole).
-template <int V>
+// Where the slots of vector number `vector` lie in a head, V of them next to each other, and which of their second values there are.
+// kMoved: vectors end where the turned values, or those behind them, do: the last ones are moved back, over values that the vectors before them have too (both write the same bits; in sums they
+// are the latter's, own_lo and own_hi say from which value on they are this one's).  Fewer than 2 V values behind the turned ones have no second half, and where their vector reaches into those it writes only what is its own.
+template <int V, bool kMoved>
 struct Slots {
-    uint32_t lo, hi;
-    bool any, second;
-    __device__ __forceinline__ Slots(const HeadNormArgs& a, uint32_t slot) {
-        const bool turned = slot < a.half;
-        any = slot < a.half + a.rest;
-        lo = any ? (turned ? slot : a.half + slot) : 0u;
-        hi = turned ? slot + a.half : a.half + a.rest + slot;
-        second = any && hi + V <= a.d;
-        if (!second) hi = lo;
+    uint32_t lo, hi, slot, own_lo, own_hi;
+    bool any, second, whole;
+    __device__ __forceinline__ Slots(const HeadNormArgs& a, uint32_t vector) {
+        slot = vector * V;
+        own_lo = own_hi = 0;
+        whole = true;
+        if constexpr (kMoved) {
+            const uint32_t turned = (a.half + V - 1u) / V, behind = a.d - 2u * a.half;
+            if (vector < turned) {
+                lo = min(slot, a.half - V);
+                own_lo = own_hi = slot - lo;
+                slot = lo;
+                hi = lo + a.half;
+                any = second = true;
+            } else {
+                const uint32_t s = slot - turned * V, seconds = behind >= 2u * V ? behind / 2u : 0u, firsts = behind - seconds;
+                any = s < firsts;
+                second = s < seconds;
+                const int at = min((int)s, (int)firsts - V);
+                lo = any ? (uint32_t)((int)(2u * a.half) + at) : 0u;
+                own_lo = s - (uint32_t)at;
+                whole = at >= 0;
+                const uint32_t at_hi = second ? min(s, seconds - V) : 0u;
+                hi = second ? 2u * a.half + firsts + at_hi : lo;
+                own_hi = s - at_hi;
+                slot = a.half;
+            }
+        } else {
+            const bool turned = slot < a.half;
+            any = slot < a.half + a.rest;
+            lo = any ? (turned ? slot : a.half + slot) : 0u;
+            hi = turned ? slot + a.half : a.half + a.rest + slot;
+            second = any && hi + V <= a.d;
+            if (!second) hi = lo;
+        }
     }
+    // Whether value v of the first ones, or of the second ones, is there and is this vector's.
+    __device__ __forceinline__ bool has_lo(int v) const { return any && (!kMoved || (uint32_t)v >= own_lo); }
+    __device__ __forceinline__ bool has_hi(int v) const { return second && (!kMoved || (uint32_t)v >= own_hi); }
 };
 
 // Sums over the lanes of a head, the same bits in each of them.
@@ -94,7 +124,7 @@ __device__ __forceinline__ void head_sums(float (&v)[U], uint32_t lanes) {
 }
 
 // K vectors of V slots a lane, U heads at a time.
-template <class T, class P, int V, int K, int U, bool kBack>
+template <class T, class P, int V, int K, int U, bool kMoved, bool kBack>
 __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs a) {
     __shared__ float shared[kBack ? kThreads / 64 * 2 * 256 : 1];
     const uint32_t lanes = a.lanes, l = threadIdx.x & (lanes - 1u), group = threadIdx.x / lanes, groups = kThreads / lanes;
@@ -102,11 +132,10 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
     uint64_t turns[K][V];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const Slots<V> at(a, (l + k * lanes) * V);
+        const Slots<V, kMoved> at(a, l + k * lanes);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t slot = (l + k * lanes) * V + v;
-            turns[k][v] = slot < a.half ? a.turns[slot] : 0u;
+            turns[k][v] = at.slot + v < a.half ? a.turns[at.slot + v] : 0u;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const P* p = static_cast<const P*>(w ? a.k.weight : a.q.weight);
@@ -140,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
                 const int64_t head = min(head0 + u, t.heads - 1u);  // (past the last one: the last one again)
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    const Slots<V> at(a, (l + k * lanes) * V);
+                    const Slots<V, kMoved> at(a, l + k * lanes);
                     load(x + head * t.x_head + at.lo, xs[u][k][0]);
                     load(x + head * t.x_head + at.hi, xs[u][k][1]);
                     if constexpr (kBack) {
@@ -155,10 +184,10 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
                 float s = 0.0f, along = 0.0f;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    const Slots<V> at(a, (l + k * lanes) * V);
+                    const Slots<V, kMoved> at(a, l + k * lanes);
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        const float lo = at.any ? (float)xs[u][k][0][v] : 0.0f, hi = at.second ? (float)xs[u][k][1][v] : 0.0f;
+                        const float lo = at.has_lo(v) ? (float)xs[u][k][0][v] : 0.0f, hi = at.has_hi(v) ? (float)xs[u][k][1][v] : 0.0f;
                         s = __builtin_fmaf(lo, lo, s);
                         s = __builtin_fmaf(hi, hi, s);
                         if constexpr (kBack) {
@@ -181,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
                 if constexpr (kBack) back = both[U + u] * rstd / a.width * rstd;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    const Slots<V> at(a, (l + k * lanes) * V);
+                    const Slots<V, kMoved> at(a, l + k * lanes);
                     T lo[V], hi[V];
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
@@ -200,8 +229,13 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
                         }
                     }
                     T* to = out + (int64_t)(head0 + u) * t.out_head;
-                    if (at.any) store(to + at.lo, lo);
+                    if (at.any && at.whole) store(to + at.lo, lo);
                     if (at.second) store(to + at.hi, hi);
+                    if constexpr (kMoved)
+                        if (at.any && !at.whole)
+#pragma unroll
+                            for (int v = 0; v < V; ++v)
+                                if (at.has_lo(v)) to[at.lo + v] = lo[v];
                 }
             }
         };
@@ -218,14 +252,14 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const Slots<V> at(a, (l + k * lanes) * V);
+                const Slots<V, kMoved> at(a, l + k * lanes);
 #pragma unroll
                 for (int side = 0; side < 2; ++side)
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
                         float s = dw[t][k][side][v];
                         for (uint32_t m = lanes; m < 64u; m <<= 1) s += __shfl_xor(s, m);
-                        if (lane < lanes && (side ? at.second : at.any)) shared[(wave * 2 + t) * 256 + (side ? at.hi : at.lo) + v] = s;
+                        if (lane < lanes && (side ? at.has_hi(v) : at.has_lo(v))) shared[(wave * 2 + t) * 256 + (side ? at.hi : at.lo) + v] = s;
                     }
             }
         __syncthreads();
@@ -257,10 +291,12 @@ __global__ __launch_bounds__(256) void head_norm_sums_kernel(const float* sums, 
 
 struct HeadNormShape {
     uint32_t V, K, lanes, split, groups;  // groups: workgroups
+    bool moved;
 };
 
 // Heads that a group of lanes has in flight, and the values of one of its requests: more are more registers and fewer wavefronts.  (Gradients of 512 x 256 tokens of 16 + 4 heads of 64 bfloat16: 4 heads in
 // requests of 16 bytes 358 us, 2 of them 237, 2 in requests of 8 bytes 216; forward, 256 x 128 tokens of 8 + 8 heads: 31, 32.7 and 33.)
+constexpr uint32_t kMovedValues = 4;  // of a vector that is moved back
 constexpr uint32_t together(bool backward) { return backward ? 2u : 4u; }
 constexpr uint32_t most_values(uint32_t dtype, bool backward) { return dtype == PXR_F32 || backward ? 4u : 8u; }
 
@@ -269,9 +305,17 @@ HeadNormShape shape_of(const HeadNormConsts& c, uint32_t dtype, uint64_t tokens,
     const uint32_t half = c.r / 2u, behind = c.d - c.r, slots = half + (behind + 1u) / 2u;
     s.V = most_values(dtype, backward);
     while (s.V > 1u && (half % s.V || behind % (2u * s.V))) s.V /= 2u;
+    uint32_t vectors = slots / s.V;
+    // Where whole vectors are short, they are of kMovedValues and the last ones moved back.  (256 x 128 steps of 8 + 8 heads of bfloat16, 100 values, 50 of them turned: one by one 100 us, so 59, gradients 154
+    // and 107; 20 of 100 turned: by twos 62, so 54, but gradients 100 and 102 and, in fp32, 36 of 64 turned 51 and 53.)
+    if ((s.V == 1u || (s.V == 2u && 2u * kMovedValues == most_values(dtype, backward))) && (half == 0u || half >= kMovedValues) && c.d >= kMovedValues) {
+        s.V = kMovedValues;
+        s.moved = true;
+        vectors = (half + s.V - 1u) / s.V + ((behind >= 2u * s.V ? (behind + 1u) / 2u : behind) + s.V - 1u) / s.V;
+    }
     s.lanes = 1u;
-    while (s.lanes < 64u && s.lanes * s.V < slots) s.lanes *= 2u;
-    s.K = s.lanes * s.V < slots ? 2u : 1u;
+    while (s.lanes < 64u && s.lanes < vectors) s.lanes *= 2u;
+    s.K = s.lanes < vectors ? 2u : 1u;
     const uint32_t U = together(backward), parts = (n_heads + U - 1u) / U + (n_key_heads + U - 1u) / U;
     // a token's heads are shared out where the tokens alone are too few wavefronts (512 and 4096 of them: 16 x 100 steps of 8 + 2 heads 14.1 and 14.4 us, 13.4 so)
     const uint64_t waves = (tokens * s.lanes + 63u) / 64u;
@@ -285,16 +329,18 @@ template <class T, class P, bool kBack>
 hipError_t launch(const HeadNormShape& s, const HeadNormArgs& a, hipStream_t st) {
     constexpr int U = (int)together(kBack);
     const dim3 grid(s.groups), threads(kThreads);
-    if (s.K == 2u)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 1, 2, U, kBack>), grid, threads, 0, st, a);
+    if (s.moved)
+        hipLaunchKernelGGL((head_norm_kernel<T, P, kMovedValues, 1, U, true, kBack>), grid, threads, 0, st, a);
+    else if (s.K == 2u)
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 1, 2, U, false, kBack>), grid, threads, 0, st, a);
     else if (s.V == 1u)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 1, 1, U, kBack>), grid, threads, 0, st, a);
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 1, 1, U, false, kBack>), grid, threads, 0, st, a);
     else if (s.V == 2u)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 2, 1, U, kBack>), grid, threads, 0, st, a);
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 2, 1, U, false, kBack>), grid, threads, 0, st, a);
     else if (s.V == 4u)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 4, 1, U, kBack>), grid, threads, 0, st, a);
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 4, 1, U, false, kBack>), grid, threads, 0, st, a);
     else if constexpr (sizeof(T) == 2 && !kBack)
-        hipLaunchKernelGGL((head_norm_kernel<T, P, 8, 1, U, kBack>), grid, threads, 0, st, a);
+        hipLaunchKernelGGL((head_norm_kernel<T, P, 8, 1, U, false, kBack>), grid, threads, 0, st, a);
     return hipGetLastError();
 }
 

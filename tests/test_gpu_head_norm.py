@@ -131,6 +131,21 @@ def test_sizes_of_heads(torch, pxr, d, r, dtype, params):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,r", [(4, 0), (5, 0), (6, 0), (7, 0), (9, 0), (17, 0), (9, 8), (10, 10), (11, 10), (13, 8), (15, 8), (16, 10), (17, 8), (18, 10), (23, 10), (37, 20), (50, 26), (64, 30), (70, 70),
+                                 (83, 40), (100, 50), (101, 58), (157, 156), (160, 154), (199, 90), (253, 250), (255, 8), (256, 246)])
+def test_heads_that_are_no_whole_vectors(torch, pxr, d, r, dtype):
+    rng = np.random.default_rng(d * 300 + r)
+    layer = pxr.HeadNorm(d, r, frequencies(r))
+    q, k, qw, kw, at, dq, dk = inputs(torch, rng, 3, 11, 3, 2, d, dtype)
+    check(torch, pxr, layer, q, k, qw, kw, at, dq, dk, frequencies(r))
+    # in place: the vectors share values
+    want = layer.forward(q, k, qw, kw, positions=at)
+    a, b = q.clone(), k.clone()
+    layer.forward(a, b, qw, kw, positions=at, q_out=a, k_out=b)
+    assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("B,T,H,Hk", [(1, 1, 1, 1), (1, 1, 16, 4), (16, 1, 4, 4), (5, 3, 7, 7), (2, 50, 9, 3), (300, 7, 4, 1), (1, 4000, 2, 1), (64, 128, 8, 8), (1, 1, 100, 33)])
 def test_numbers_of_tokens_and_heads(torch, pxr, B, T, H, Hk, dtype):
     rng = np.random.default_rng(B + T)
