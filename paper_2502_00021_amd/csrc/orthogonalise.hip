@@ -770,6 +770,173 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
     }
 }
 
+// ---- long matrices of at most 32 rows (or columns): X is read twice.  Every X_k is a product P_k X_0 with P_0 = 1, P_{k+1} = B_k P_k, and A_{k+1} = B_k A_k B_k: a sum over the long axis, steps on matrices
+// of 32 x 32, and a product.  All in fp64, on its matrix cores: in fp32 this way loses the small singular values, whose squares A has from the beginning on.  |x|^2 is A's trace.  10 x 28196 in fp32: sums
+// 6 us, steps 15, product 5; what is left is three launches and the chain of the steps.
+
+constexpr uint32_t kNarrow = 32, kNarrowRow = kNarrow + 1;
+constexpr uint32_t kNarrowParts = 256, kNarrowGroups = 2048;  // of a matrix, at most (32 x 200000: 64 of them 163 us, so 100), and of all
+constexpr uint32_t kNarrowAhead = 2;                          // requests of a wavefront, 16 values of the long axis each
+
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+struct Narrow {
+    const void* x;
+    void* out;
+    int64_t x_matrix, x_row, out_matrix, out_row;
+    uint32_t rows, cols, s, l, parts, each, n_steps;  // each: values of the long axis of a part, a multiple of 64
+    double *sums, *products;  // [matrices][parts][32][32]; [matrices][32][32], of X as it is
+    float eps;
+    float coefficients[64][3];
+};
+
+// A lane has row lane % 16 of a's 16 and column lane % 16 of b's, value lane / 16 of the summed axis' four; of the result column lane % 16 and rows 4 r + lane / 16.
+__device__ __forceinline__ f64x4 product64(double a, double b, f64x4 sum) { return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, sum, 0, 0, 0); }
+
+// A part's share of A = X X^T.  A wavefront takes 16 values of the long axis at a time, four of each row a lane.
+template <class T>
+__global__ __launch_bounds__(256) void narrow_sums_kernel(const Narrow a) {
+    __shared__ double total[3][256][4];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.y, row = lane & 15u;
+    const bool tall = a.rows > a.cols;
+    const T* x = static_cast<const T*>(a.x) + (int64_t)matrix * a.x_matrix;
+    const int64_t along = tall ? a.x_row : 1, down = tall ? 1 : a.x_row;
+    const uint32_t begin = blockIdx.x * a.each, end = min(begin + a.each, a.l);
+    f64x4 sum[3] = {(f64x4)0.0, (f64x4)0.0, (f64x4)0.0};
+    for (uint32_t first = begin + 16u * wave; first < end; first += 64u * kNarrowAhead) {
+        T v[kNarrowAhead][2][4];
+#pragma unroll
+        for (uint32_t n = 0; n < kNarrowAhead; ++n)
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half) {
+                const uint32_t r = row + 16u * half, p = first + 64u * n + 4u * (lane >> 4);
+                const T* at = x + ((int64_t)r * down + (int64_t)p * along);
+                if (r < a.s && !tall && p + 4u <= end) {
+                    __builtin_memcpy(v[n][half], at, sizeof(v[n][half]));  // (at the address of any value)
+                } else {
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e) v[n][half][e] = r < a.s && p + e < end ? at[(int64_t)e * along] : (T)0.0f;
+                }
+            }
+#pragma unroll
+        for (uint32_t n = 0; n < kNarrowAhead; ++n)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                const double lo = (double)load1(&v[n][0][e]), hi = (double)load1(&v[n][1][e]);
+                sum[0] = product64(lo, lo, sum[0]);
+                if (a.s > 16u) {
+                    sum[1] = product64(hi, lo, sum[1]);
+                    sum[2] = product64(hi, hi, sum[2]);
+                }
+            }
+    }
+    // the wavefronts' sums, in their order
+    double* const to = a.sums + ((size_t)matrix * a.parts + blockIdx.x) * (kNarrow * kNarrow);
+#pragma unroll
+    for (uint32_t t = 0; t < 3; ++t)
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) total[t][threadIdx.x][r] = sum[t][r];
+    __syncthreads();
+    for (uint32_t n = threadIdx.x; n < 3u * 256u; n += 256u) {
+        const uint32_t t = n >> 8, r = n >> 6 & 3u, from = n & 63u;
+        const double v = total[t][from][r] + total[t][from + 64u][r] + total[t][from + 128u][r] + total[t][from + 192u][r];
+        const uint32_t i = 4u * r + (from >> 4) + (t ? 16u : 0u), j = (from & 15u) + (t == 2u ? 16u : 0u);
+        to[i * kNarrow + j] = v;
+        if (t == 1u) to[j * kNarrow + i] = v;
+    }
+}
+
+// The steps: a workgroup has a matrix' A, B and P in LDS.  All of its wavefronts add up the parts' sums, four of them have a tile of 16 x 16 each then.
+__global__ __launch_bounds__(kNarrow * kNarrow) void narrow_steps_kernel(const Narrow a) {
+    __shared__ double A[kNarrow][kNarrowRow], B[kNarrow][kNarrowRow], P[kNarrow][kNarrowRow], T[kNarrow][kNarrowRow];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.x, row0 = wave / 2u * 16u, col0 = wave % 2u * 16u;
+    const uint32_t row = threadIdx.x / kNarrow, col = threadIdx.x % kNarrow;
+    const double* from = a.sums + (size_t)matrix * a.parts * (kNarrow * kNarrow) + threadIdx.x;
+    double v = 0.0;
+    for (uint32_t first = 0; first < a.parts; first += 16u) {
+        double some[16];
+#pragma unroll
+        for (uint32_t n = 0; n < 16; ++n) some[n] = first + n < a.parts ? from[(size_t)(first + n) * (kNarrow * kNarrow)] : 0.0;
+#pragma unroll
+        for (uint32_t n = 0; n < 16; ++n) v += some[n];
+    }
+    A[row][col] = v;
+    __syncthreads();
+    double trace = 0.0;
+#pragma unroll
+    for (uint32_t i = 0; i < kNarrow; ++i) trace += A[i][i];  // (zeros behind the last row)
+    const double over = 1.0 / (sqrt(trace) + (double)a.eps);
+    __syncthreads();
+    A[row][col] = v * over * over;
+    __syncthreads();
+    const auto multiplied = [&](const double (&p)[kNarrow][kNarrowRow], const double (&q)[kNarrow][kNarrowRow]) {
+        f64x4 sum[2] = {(f64x4)0.0, (f64x4)0.0};
+#pragma unroll
+        for (uint32_t k = 0; k < kNarrow; k += 4u) sum[k >> 2 & 1u] = product64(p[row0 + (lane & 15u)][k + (lane >> 4)], q[k + (lane >> 4)][col0 + (lane & 15u)], sum[k >> 2 & 1u]);
+        return sum[0] + sum[1];
+    };
+    const auto put = [&](double (&to)[kNarrow][kNarrowRow], f64x4 tile) {
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) to[row0 + 4u * r + (lane >> 4)][col0 + (lane & 15u)] = tile[r];
+    };
+    const bool works = wave < 4u;
+    for (uint32_t step = 0; step < a.n_steps; ++step) {
+        const double c0 = a.coefficients[step][0], c1 = a.coefficients[step][1], c2 = a.coefficients[step][2];
+        f64x4 b = (f64x4)0.0, p = b, t = b;
+        if (works) {
+            b = multiplied(A, A);
+#pragma unroll
+            for (uint32_t r = 0; r < 4; ++r) {
+                const uint32_t i = row0 + 4u * r + (lane >> 4), j = col0 + (lane & 15u);
+                b[r] = c2 * b[r] + c1 * A[i][j] + (i == j ? c0 : 0.0);
+            }
+            put(B, b);
+        }
+        __syncthreads();
+        if (works) {
+            p = step ? multiplied(B, P) : b;
+            t = multiplied(A, B);
+            put(T, t);
+        }
+        __syncthreads();
+        if (works) {
+            put(P, p);
+            put(A, multiplied(T, B));
+        }
+        __syncthreads();
+    }
+    a.products[(size_t)matrix * (kNarrow * kNarrow) + threadIdx.x] = P[row][col] * over;
+}
+
+// P X: a workgroup has 64 places on the long axis, whose values each of its wavefronts reads before any of them writes its share of the rows.
+template <class T>
+__global__ __launch_bounds__(256) void narrow_product_kernel(const Narrow a) {
+    typedef const __attribute__((address_space(4))) double* Constant;  // (P's values are all lanes': scalar registers)
+    const uint32_t matrix = blockIdx.y;
+    const Constant P = (Constant)(a.products + (size_t)matrix * (kNarrow * kNarrow));
+    const uint32_t at = blockIdx.x * 64u + (threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), each = (a.s + 3u) / 4u;
+    const bool tall = a.rows > a.cols, there = at < a.l;
+    const T* x = static_cast<const T*>(a.x) + ((int64_t)matrix * a.x_matrix + (there ? (int64_t)at * (tall ? a.x_row : 1) : 0));
+    T* out = static_cast<T*>(a.out) + ((int64_t)matrix * a.out_matrix + (int64_t)at * (tall ? a.out_row : 1));
+    const int64_t down = tall ? 1 : a.x_row, out_down = tall ? 1 : a.out_row;
+    T raw[kNarrow];
+#pragma unroll
+    for (uint32_t k = 0; k < kNarrow; ++k) raw[k] = k < a.s ? x[(int64_t)k * down] : (T)0.0f;
+    __syncthreads();
+    if (!there) return;
+#pragma unroll 2
+    for (uint32_t i = wave * each; i < min(a.s, (wave + 1u) * each); ++i) {
+        double sum[4] = {};
+#pragma unroll
+        for (uint32_t k = 0; k < kNarrow; ++k) sum[k & 3u] = __builtin_fma(P[i * kNarrow + k], (double)load1(&raw[k]), sum[k & 3u]);
+        out[(int64_t)i * out_down] = (T)(float)(sum[0] + sum[1] + (sum[2] + sum[3]));  // (to bfloat16 by way of fp32: 2^-24 more)
+    }
+}
+
+// (32 x 1200 by one workgroup in LDS 64 us, so 28; 32 x 300 26 and 27; 8 x 400 27 and 22.  10 x 28196 by the products of large matrices 139 us, so 35.)
+bool is_narrow(uint32_t s, uint32_t l) { return s <= kNarrow && l > 320u; }
+uint32_t narrow_parts(uint32_t l, uint32_t n_matrices) { return std::min({kNarrowParts, std::max(1u, kNarrowGroups / n_matrices), (l + 255u) / 256u}); }
+
 float power_below(double v) { return (float)std::exp2(std::floor(std::log2(v))); }
 
 // Bounds of the singular values, and the powers of two by which X, A and B are held: 2 less than half of fp16's largest number, so that no rounding reaches it.
@@ -908,6 +1075,15 @@ hipError_t launch_small(const Small& a, uint32_t n_matrices, hipStream_t st) {
     return hipGetLastError();
 }
 
+template <class T>
+hipError_t launch_narrow(const Narrow& a, uint32_t n_matrices, hipStream_t st) {
+    const dim3 threads(256);
+    hipLaunchKernelGGL((narrow_sums_kernel<T>), dim3(a.parts, n_matrices), threads, 0, st, a);
+    hipLaunchKernelGGL(narrow_steps_kernel, dim3(n_matrices), dim3(kNarrow * kNarrow), 0, st, a);
+    hipLaunchKernelGGL((narrow_product_kernel<T>), dim3((a.l + 63u) / 64u, n_matrices), threads, 0, st, a);
+    return hipGetLastError();
+}
+
 int result(hipError_t rc, std::string& err) {
     if (rc == hipSuccess) return PXR_OK;
     err = std::string("kernel launch failed: ") + hipGetErrorString(rc);
@@ -916,11 +1092,23 @@ int result(hipError_t rc, std::string& err) {
 
 }  // namespace
 
-size_t orthogonalise_workspace(const pxr_orthogonalise_desc& d) { return is_small(std::min(d.rows, d.cols), std::max(d.rows, d.cols)) ? 0 : layout_of(d).bytes; }
+size_t orthogonalise_workspace(const pxr_orthogonalise_desc& d) {
+    const uint32_t shorter = std::min(d.rows, d.cols), longer = std::max(d.rows, d.cols);
+    if (is_narrow(shorter, longer)) return (size_t)d.n_matrices * (narrow_parts(longer, d.n_matrices) + 1u) * (kNarrow * kNarrow) * sizeof(double);
+    return is_small(shorter, longer) ? 0 : layout_of(d).bytes;
+}
 
 int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* out, void* ws, void* stream, std::string& err) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     const uint32_t shorter = std::min(d.rows, d.cols), longer = std::max(d.rows, d.cols);
+    if (is_narrow(shorter, longer)) {
+        Narrow a{x, out, d.x_matrix, d.x_row, d.out_matrix, d.out_row, d.rows, d.cols, shorter, longer, narrow_parts(longer, d.n_matrices), 0, d.n_steps, static_cast<double*>(ws), nullptr, d.eps, {}};
+        a.products = a.sums + (size_t)d.n_matrices * a.parts * (kNarrow * kNarrow);
+        a.each = ((longer + a.parts - 1u) / a.parts + 63u) / 64u * 64u;
+        a.parts = (longer + a.each - 1u) / a.each;
+        std::copy_n(d.coefficients, 3 * d.n_steps, &a.coefficients[0][0]);
+        return result(d.dtype == PXR_F32 ? launch_narrow<float>(a, d.n_matrices, st) : launch_narrow<__bf16>(a, d.n_matrices, st), err);
+    }
     if (is_small(shorter, longer)) {
         Small a{x, out, d.x_matrix, d.x_row, d.out_matrix, d.out_row, d.rows, d.cols, shorter, longer, up32(shorter), up32(longer), d.n_steps, d.eps, 0.0f, {}};
         a.held = factors_of(d, a.steps);

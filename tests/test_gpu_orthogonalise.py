@@ -97,6 +97,45 @@ def test_tiles_of_both_sizes(torch, pxr, B, m, n, dtype):
     check(torch, pxr, x[-2:], got=got[-2:])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,m,n", [(1, 1, 3000), (2, 2001, 1), (1, 5, 30000), (4, 14982, 5), (1, 16, 2500), (3, 17, 4097), (1, 28196, 31), (1, 32, 1300), (2, 1301, 32), (1, 32, 100000), (70, 20, 1500), (1, 33, 2000), (2, 20, 320), (2, 321, 20),
+                                   (3000, 3, 1300)])
+def test_long_matrices_of_few_rows(torch, pxr, B, m, n, dtype):
+    x = normal(torch, m + n, B, m, n, dtype=dtype)
+    got = pxr.orthogonalise(x)
+    check(torch, pxr, x[:3], got=got[:3])
+    check(torch, pxr, x[-1], got=got[-1])
+    again = x.clone()
+    pxr.orthogonalise(again, out=again)
+    assert torch.equal(again, got)
+    assert (pxr.orthogonalise(torch.zeros_like(x[:2])) == 0).all()
+
+
+def test_long_matrices_as_updates_have_them(torch, pxr):
+    """Singular values that lie far apart, a rank of one, rows of zeros, any scale, other steps, and what is not finite."""
+    m, n = 24, 5000
+    u, v = torch.linalg.qr(normal(torch, 2, m, m).double())[0], torch.linalg.qr(normal(torch, 3, n, m).double())[0]
+    apart = ((u * torch.logspace(0, -4, m, device="cuda", dtype=torch.float64)) @ v.t().contiguous()).float()
+    one = (u[:, :1] @ v[:, :1].t().contiguous()).float()
+    rows = normal(torch, 4, m, n)
+    rows[::3] = 0
+    for x in (apart, one, rows, apart * 1e-30, apart * 1e30, rows * 1e-20):
+        check(torch, pxr, x, eps=0.0)
+        check(torch, pxr, x.t().contiguous(), eps=0.0)
+        for c in ([QUINTIC], [(1.5, -0.5, 0.0)] * 12, [(3.0, -3.2, 1.2), (2.5, -2.0, 0.5), (1.5, -0.5, 0.0)], [(0.5, 0.0, 0.0)]):
+            check(torch, pxr, x, [tuple(float(np.float32(v)) for v in t) for t in c], eps=0.0)
+    x = torch.stack([rows, apart, one])
+    want = pxr.orthogonalise(x)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        bad = x.clone()
+        bad[1, m // 2, n // 3] = value
+        for c in ([QUINTIC] * 2, [(1.5, -0.5, 0.0)], [(0.5, 0.0, 0.0)]):
+            got = pxr.orthogonalise(bad, coefficients=c)
+            assert got[1].isnan().all() and got[0].isfinite().all() and got[2].isfinite().all()
+        got = pxr.orthogonalise(bad)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+
+
 @pytest.mark.parametrize("m,n", [(60, 90), (300, 200)])
 def test_coefficients(torch, pxr, m, n):
     """Cubic and quintic steps, few and many, of factors far from one, and another triple in every step."""
