@@ -242,7 +242,9 @@ __global__ __launch_bounds__(kMostWaves * 64) void recurrence_kernel(const Recur
     constexpr bool kBack = kWhat >= kBackward, kSums = kWhat == kForwardSums || kWhat == kBackwardSums;
     constexpr int kPlanes = kBack ? 3 : 2;
     typedef Chunk<T, V, kWhat, kCoupled> Steps;
-    __shared__ float shared[kBack ? 1 : 2][kMostWaves][kPlanes][V][64];
+    typedef float Told[kPlanes][V][64];
+    extern __shared__ float recurrence_memory[];  // of as many wavefronts as there are, twice where there are several blocks
+    Told* const shared = reinterpret_cast<Told*>(recurrence_memory);
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const uint32_t strip = blockIdx.x % a.strips, rest = blockIdx.x / a.strips, seg = rest % a.segments, rows = rest / a.segments;
     const Lane<T, V> at(a, rows, strip);
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void recurrence_kernel(const Recur
 #pragma unroll
                 for (int i = 0; i < V; ++i) as_it_is(s[j][i]);
             }
-        float(&told)[kMostWaves][kPlanes][V][64] = shared[kBack ? 0 : turn];  // (the block after the next one writes here again)
+        Told* const told = shared + (kBack ? 0u : turn * waves);  // (the block after the next one writes here again)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             told[wave][0][i][lane] = A[i];
@@ -528,17 +530,19 @@ Shape narrowed(Shape s, uint32_t n_envs, uint32_t width, std::initializer_list<i
 template <class T, int kWhat>
 hipError_t launch_part(const Shape& s, const Recurrence& a, hipStream_t st) {
     const dim3 grid(s.rows * s.strips * s.segments), threads(s.waves * 64u);
+    constexpr bool kBack = kWhat >= kBackward;
+    const uint32_t lds = (!kBack && s.seg_steps > s.waves * C ? 2u : 1u) * s.waves * (kBack ? 3u : 2u) * s.V * 64u * (uint32_t)sizeof(float);
     if (sizeof(T) == 2 && s.V == 2u) {
         constexpr int V = sizeof(T) == 2 ? 2 : 1;
         if (a.coupled)
-            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, true>), grid, threads, 0, st, a);
+            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, true>), grid, threads, lds, st, a);
         else
-            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, false>), grid, threads, 0, st, a);
+            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, false>), grid, threads, lds, st, a);
     } else {
         if (a.coupled)
-            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, true>), grid, threads, 0, st, a);
+            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, true>), grid, threads, lds, st, a);
         else
-            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, false>), grid, threads, 0, st, a);
+            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, false>), grid, threads, lds, st, a);
     }
     return hipGetLastError();
 }
