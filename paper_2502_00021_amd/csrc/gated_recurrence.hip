@@ -125,7 +125,10 @@ struct Recurrence {
 };
 
 enum { kForward, kForwardSums, kBackward, kBackwardSums };
-constexpr int C = 16;                  // steps of a wavefront: as many as its registers have room for (8: 256 x 128 x 1024 49 us, 46 so; gradients of 512 x 256 x 1024, then in two segments, 624, 316)
+// Steps of a wavefront: as many as its registers have room for (8: 256 x 128 x 1024 50 us, 46 so; gradients of 512 x 256 x 1024, then in two segments, 625, 313), and few for rollouts that are shorter
+// than kFewSteps (16000 x 4 x 256: 16 of them 52 us, 4 of them 24; 16000 x 8 x 256 62 and 44, gradients 87 and 69; of 16 steps 75 and 87).
+constexpr int kSteps = 16, kStepsOfFew = 4;
+constexpr uint32_t kFewSteps = 8;
 constexpr uint32_t kMostWaves = 16;    // of a workgroup
 
 // Where a lane's channels are: of environment `env`, from channel `at` on.  A row that ends inside a vector has its last vector moved back to its end: the values that
@@ -151,7 +154,7 @@ struct Lane {
 __device__ __forceinline__ float masked(float v, uint32_t m) { return __uint_as_float(__float_as_uint(v) & m); }
 
 // A wavefront's steps, C of V channels a lane.  `cuts`: a bit for each step that begins an episode.  Steps that are not there keep everything and add nothing (absent()).
-template <class T, int V, int kWhat, bool kCoupled>
+template <class T, int V, int kWhat, bool kCoupled, int C>
 struct Chunk {
     static constexpr bool kBack = kWhat >= kBackward;
     typedef Raw<T, V> Raws[C];
@@ -237,11 +240,11 @@ struct Chunk {
 };
 
 // One workgroup: seg_steps steps (backward: at most what its wavefronts hold) of a strip of channels of 64 / lanes environments.
-template <class T, int V, int kWhat, bool kCoupled>
+template <class T, int V, int kWhat, bool kCoupled, int C>
 __global__ __launch_bounds__(kMostWaves * 64) void recurrence_kernel(const Recurrence a) {
     constexpr bool kBack = kWhat >= kBackward, kSums = kWhat == kForwardSums || kWhat == kBackwardSums;
     constexpr int kPlanes = kBack ? 3 : 2;
-    typedef Chunk<T, V, kWhat, kCoupled> Steps;
+    typedef Chunk<T, V, kWhat, kCoupled, C> Steps;
     typedef float Told[kPlanes][V][64];
     extern __shared__ float recurrence_memory[];  // of as many wavefronts as there are, twice where there are several blocks
     Told* const shared = reinterpret_cast<Told*>(recurrence_memory);
@@ -477,7 +480,7 @@ __global__ __launch_bounds__(256) void recurrence_pass_kernel(const float* from,
 }
 
 struct Shape {
-    uint32_t V, lanes, rows, strips, waves, segments, seg_steps;
+    uint32_t V, C, lanes, rows, strips, waves, segments, seg_steps;
 };
 
 // A workgroup takes 4.7 us for a block of its steps, one after the other, and 128 of them side by side as many bytes a second as segments do, which read everything twice: forward passes are cut into
@@ -493,21 +496,22 @@ constexpr uint32_t kManyGroups = 2048;  // that segments make (1 x 50000 x 512: 
 Shape shape_of(uint32_t V, uint32_t n_envs, uint32_t n_steps, uint32_t width, bool backward) {
     Shape s{};
     s.V = V;
-    s.lanes = (uint32_t)C;
+    s.C = n_steps <= kFewSteps ? kStepsOfFew : kSteps;
+    s.lanes = s.C;
     while (s.lanes < 64u && s.lanes * s.V < width) s.lanes *= 2u;
     s.rows = (n_envs + 64u / s.lanes - 1u) / (64u / s.lanes);
     s.strips = (width + s.lanes * s.V - 1u) / (s.lanes * s.V);
-    const uint32_t chunks = (n_steps + C - 1u) / C;
+    const uint32_t chunks = (n_steps + s.C - 1u) / s.C;
     const auto blocks_of = [&](uint32_t waves) { return (chunks + waves - 1u) / waves; };
     const uint64_t groups = (uint64_t)n_envs * ((width + 127u) / 128u);  // (by the sizes alone, like the workspace)
     if (backward || blocks_of(kHalfWaves) <= kFewBlocks || groups >= kFewGroups) {
         const uint32_t blocks = blocks_of(backward || (uint64_t)s.rows * s.strips <= kUnits ? kMostWaves : kHalfWaves);
         s.waves = (chunks + blocks - 1u) / blocks;
-        s.seg_steps = (backward ? 1u : blocks) * s.waves * C;
+        s.seg_steps = (backward ? 1u : blocks) * s.waves * s.C;
     } else {
         const uint32_t blocks = blocks_of(kHalfWaves), cut = (uint32_t)std::min<uint64_t>(blocks, (kManyGroups + groups - 1u) / groups);
         s.waves = kHalfWaves;
-        s.seg_steps = (blocks + cut - 1u) / cut * s.waves * C;
+        s.seg_steps = (blocks + cut - 1u) / cut * s.waves * s.C;
     }
     s.segments = (n_steps + s.seg_steps - 1u) / s.seg_steps;
     return s;
@@ -527,7 +531,7 @@ Shape narrowed(Shape s, uint32_t n_envs, uint32_t width, std::initializer_list<i
     return s;
 }
 
-template <class T, int kWhat>
+template <class T, int kWhat, int C>
 hipError_t launch_part(const Shape& s, const Recurrence& a, hipStream_t st) {
     const dim3 grid(s.rows * s.strips * s.segments), threads(s.waves * 64u);
     constexpr bool kBack = kWhat >= kBackward;
@@ -535,30 +539,31 @@ hipError_t launch_part(const Shape& s, const Recurrence& a, hipStream_t st) {
     if (sizeof(T) == 2 && s.V == 2u) {
         constexpr int V = sizeof(T) == 2 ? 2 : 1;
         if (a.coupled)
-            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, true>), grid, threads, lds, st, a);
+            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, true, C>), grid, threads, lds, st, a);
         else
-            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, false>), grid, threads, lds, st, a);
+            hipLaunchKernelGGL((recurrence_kernel<T, V, kWhat, false, C>), grid, threads, lds, st, a);
     } else {
         if (a.coupled)
-            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, true>), grid, threads, lds, st, a);
+            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, true, C>), grid, threads, lds, st, a);
         else
-            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, false>), grid, threads, lds, st, a);
+            hipLaunchKernelGGL((recurrence_kernel<T, 1, kWhat, false, C>), grid, threads, lds, st, a);
     }
     return hipGetLastError();
 }
 
 template <class T, bool kBack>
 hipError_t launch_all(const Shape& s, const Recurrence& a, hipStream_t st) {
+    if (s.C == kStepsOfFew) return launch_part<T, kBack ? kBackward : kForward, kStepsOfFew>(s, a, st);  // (one segment)
     hipError_t rc = hipSuccess;
     if (s.segments > 1u) {
-        rc = launch_part<T, kBack ? kBackwardSums : kForwardSums>(s, a, st);
+        rc = launch_part<T, kBack ? kBackwardSums : kForwardSums, kSteps>(s, a, st);
         if (rc == hipSuccess) {
             const uint64_t cells = (uint64_t)a.n_envs * a.width;
             hipLaunchKernelGGL((recurrence_join_kernel<kBack>), dim3((uint32_t)((cells + 63u) / 64u)), dim3(kJoinWaves * 64u), 0, st, a);
             rc = hipGetLastError();
         }
     }
-    return rc == hipSuccess ? launch_part<T, kBack ? kBackward : kForward>(s, a, st) : rc;
+    return rc == hipSuccess ? launch_part<T, kBack ? kBackward : kForward, kSteps>(s, a, st) : rc;
 }
 
 Recurrence arguments(const pxr_gated_rollout& r, const Shape& s, void* ws) {

@@ -118,6 +118,14 @@ def test_lengths(torch, pxr, T, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 7, 8, 9])
+@pytest.mark.parametrize("B,D", [(37, 1), (50, 3), (19, 9), (700, 20), (3, 130), (65, 257)])
+def test_short_rollouts(torch, pxr, B, T, D, dtype):
+    rng = np.random.default_rng(T * 100 + D)
+    check(torch, pxr, *inputs(torch, rng, B, T, D, dtype, resets=0.2, layout="tbd" if T % 2 else "btd"), coupled=bool(T % 3))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("B,T,D", [(1, 5000, 96), (2, 3333, 5), (1, 9000, 2), (3, 2049, 150), (1, 20000, 1), (400, 300, 20), (40, 700, 257)])
 def test_long_axes(torch, pxr, B, T, D, dtype):
     """Cut into segments, or by one workgroup after the other."""
