@@ -1,7 +1,7 @@
 """The compiled kernels wait long enough between a matrix instruction and the first use of its result.
 
-A 32 x 32 x 16 product of fp16 takes 8 passes, and what reads or overwrites its result without being a matrix instruction may be issued 11 states behind it at the earliest: the hardware does
-not wait by itself, the compiler puts instructions or s_nop between.  It has left them out behind a loop with a way out of its middle, and what was read then was an older value."""
+A 32 x 32 x 16 product of fp16 takes 8 passes, one of 16 x 16 x 4 in fp64 16, and what reads or overwrites its result without being a matrix instruction may be issued 3 states behind those at the
+earliest: the hardware does not wait by itself, the compiler puts instructions or s_nop between.  It has left them out behind a loop with a way out of its middle, and what was read then was an older value."""
 import os
 import re
 import subprocess
@@ -10,7 +10,9 @@ import pytest
 
 from paper_2502_00021_amd import build
 
-PASSES, STATES = 8, 11
+
+def passes(name):
+    return 16 if "f64" in name else 8
 
 
 def registers(text):
@@ -38,16 +40,16 @@ def too_soon(assembly):
         if not name.startswith("v_mfma"):
             continue
         products += 1
-        result, paths, seen = registers(operands[0]), [(i + 1, 0)], {}
+        result, paths, seen, enough = registers(operands[0]), [(i + 1, 0)], {}, passes(name) + 3
         while paths:
             at, states = paths.pop()
-            while states < STATES and at < len(code) and seen.get(at, STATES) > states:
+            while states < enough and at < len(code) and seen.get(at, enough) > states:
                 seen[at] = states
                 name, operands = code[at]
                 if name == "s_endpgm":
                     break
                 if name.startswith("v_mfma"):
-                    states += PASSES
+                    states += passes(name)
                 elif name == "s_nop":
                     states += int(operands[0], 0) + 1
                 else:
@@ -68,6 +70,8 @@ def test_the_search_itself():
     straight = "\tv_mfma_f32_32x32x16_f16 v[0:15], v[20:23], v[24:27], v[0:15]\n"
     assert too_soon(straight + "\ts_nop 10\n\tv_add_f32_e32 v30, v3, v30\n\ts_endpgm\n") == (1, [])
     assert len(too_soon(straight + "\ts_nop 9\n\tv_add_f32_e32 v30, v3, v30\n\ts_endpgm\n")[1]) == 1
+    twice = "\tv_mfma_f64_16x16x4_f64 v[0:7], v[20:21], v[24:25], v[0:7]\n\ts_nop 15\n\ts_nop {}\n\tv_add_f64 v[30:31], v[6:7], v[30:31]\n\ts_endpgm\n"
+    assert too_soon(twice.format(2)) == (1, []) and len(too_soon(twice.format(1))[1]) == 1
     assert len(too_soon(straight + "\ts_nop 9\n\tv_add_f32_e32 v30, v16, v30\n\ts_endpgm\n")[1]) == 0
     loop = ("\ts_branch .L2\n.L1:\n" + straight + "\ts_cbranch_scc1 .L1\n\ts_cbranch_vccz .L3\n.L2:\n\ts_nop 15\n\ts_branch .L1\n.L3:\n{}\tglobal_store_dwordx4 v[40:41], v[4:7], off\n\ts_endpgm\n")
     assert len(too_soon(loop.format(""))[1]) == 1 and too_soon(loop.format("\ts_nop 8\n"))[1] == []
