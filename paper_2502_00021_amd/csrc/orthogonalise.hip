@@ -805,24 +805,27 @@ __global__ __launch_bounds__(256) void narrow_sums_kernel(const Narrow a) {
     f64x4 sum[3] = {(f64x4)0.0, (f64x4)0.0, (f64x4)0.0};
     for (uint32_t first = begin + 16u * wave; first < end; first += 64u * kNarrowAhead) {
         T v[kNarrowAhead][2][4];
+        const bool whole = !tall && first + 64u * kNarrowAhead - 48u <= end;
 #pragma unroll
         for (uint32_t n = 0; n < kNarrowAhead; ++n)
 #pragma unroll
             for (uint32_t half = 0; half < 2; ++half) {
-                const uint32_t r = row + 16u * half, p = first + 64u * n + 4u * (lane >> 4);
-                const T* at = x + ((int64_t)r * down + (int64_t)p * along);
-                if (r < a.s && !tall && p + 4u <= end) {
-                    __builtin_memcpy(v[n][half], at, sizeof(v[n][half]));  // (at the address of any value)
+                // (of rows and places that are not there the last one's: requests without conditions do not wait for each other)
+                const uint32_t r = min(row + 16u * half, a.s - 1u), p = first + 64u * n + 4u * (lane >> 4);
+                const T* at = x + (int64_t)r * down;
+                if (whole) {
+                    __builtin_memcpy(v[n][half], at + p, sizeof(v[n][half]));  // (at the address of any value)
                 } else {
 #pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e) v[n][half][e] = r < a.s && p + e < end ? at[(int64_t)e * along] : (T)0.0f;
+                    for (uint32_t e = 0; e < 4; ++e) v[n][half][e] = at[(int64_t)min(p + e, end - 1u) * along];
                 }
             }
 #pragma unroll
         for (uint32_t n = 0; n < kNarrowAhead; ++n)
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e) {
-                const double lo = (double)load1(&v[n][0][e]), hi = (double)load1(&v[n][1][e]);
+                const bool there = first + 64u * n + 4u * (lane >> 4) + e < end;
+                const double lo = there && row < a.s ? (double)load1(&v[n][0][e]) : 0.0, hi = there && row + 16u < a.s ? (double)load1(&v[n][1][e]) : 0.0;
                 sum[0] = product64(lo, lo, sum[0]);
                 if (a.s > 16u) {
                     sum[1] = product64(hi, lo, sum[1]);
@@ -921,9 +924,12 @@ __global__ __launch_bounds__(256) void narrow_product_kernel(const Narrow a) {
     const int64_t down = tall ? 1 : a.x_row, out_down = tall ? 1 : a.out_row;
     T raw[kNarrow];
 #pragma unroll
-    for (uint32_t k = 0; k < kNarrow; ++k) raw[k] = k < a.s ? x[(int64_t)k * down] : (T)0.0f;
+    for (uint32_t k = 0; k < kNarrow; ++k) raw[k] = x[(int64_t)min(k, a.s - 1u) * down];
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (they have come, not only been asked for: out may be x)
     __syncthreads();
     if (!there) return;
+#pragma unroll
+    for (uint32_t k = 0; k < kNarrow; ++k) raw[k] = k < a.s ? raw[k] : (T)0.0f;
 #pragma unroll 2
     for (uint32_t i = wave * each; i < min(a.s, (wave + 1u) * each); ++i) {
         double sum[4] = {};
