@@ -772,10 +772,10 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
 
 // ---- long matrices of at most 32 rows (or columns): X is read twice.  Every X_k is a product P_k X_0 with P_0 = 1, P_{k+1} = B_k P_k, and A_{k+1} = B_k A_k B_k: a sum over the long axis, steps on matrices
 // of 32 x 32, and a product.  All in fp64, on its matrix cores: in fp32 this way loses the small singular values, whose squares A has from the beginning on.  |x|^2 is A's trace.  10 x 28196 in fp32: sums
-// 6 us, steps 15, product 5; what is left is three launches and the chain of the steps.
+// 8 us, steps 12, product 4; what is left is three launches and the chain of the steps.
 
 constexpr uint32_t kNarrow = 32, kNarrowRow = kNarrow + 1;
-constexpr uint32_t kNarrowParts = 256, kNarrowGroups = 2048;  // of a matrix, at most (32 x 200000: 64 of them 163 us, so 100), and of all
+constexpr uint32_t kNarrowParts = 128, kNarrowGroups = 2048;  // of a matrix, at most (32 x 200000: 256 of them 78 us, 128 76), and of all
 constexpr uint32_t kNarrowAhead = 2;                          // requests of a wavefront, 16 values of the long axis each
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
@@ -939,9 +939,12 @@ __global__ __launch_bounds__(256) void narrow_product_kernel(const Narrow a) {
     }
 }
 
-// (32 x 1200 by one workgroup in LDS 64 us, so 28; 32 x 300 26 and 27; 8 x 400 27 and 22.  10 x 28196 by the products of large matrices 139 us, so 35.)
+// (32 x 1200 by one workgroup in LDS 64 us, so 28; 32 x 300 26 and 27; 8 x 400 27 and 22.  10 x 28196 by the products of large matrices 139 us, so 30.)
 bool is_narrow(uint32_t s, uint32_t l) { return s <= kNarrow && l > 320u; }
-uint32_t narrow_parts(uint32_t l, uint32_t n_matrices) { return std::min({kNarrowParts, std::max(1u, kNarrowGroups / n_matrices), (l + 255u) / 256u}); }
+// Parts of 256 values, of 512 where those are more than 32: the steps' workgroup reads all of their sums.  (10 x 28196: of 256 35 us, of 512 30; 31 x 4000: 27 and 31.)
+uint32_t narrow_parts(uint32_t l, uint32_t n_matrices) {
+    return std::min({kNarrowParts, std::max(1u, kNarrowGroups / n_matrices), std::max(std::min((l + 255u) / 256u, 32u), (l + 511u) / 512u)});
+}
 
 float power_below(double v) { return (float)std::exp2(std::floor(std::log2(v))); }
 
