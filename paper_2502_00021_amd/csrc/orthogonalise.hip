@@ -772,7 +772,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
 
 // ---- long matrices of at most 32 rows (or columns): X is read twice.  Every X_k is a product P_k X_0 with P_0 = 1, P_{k+1} = B_k P_k, and A_{k+1} = B_k A_k B_k: a sum over the long axis, steps on matrices
 // of 32 x 32, and a product.  All in fp64, on its matrix cores: in fp32 this way loses the small singular values, whose squares A has from the beginning on.  |x|^2 is A's trace.  10 x 28196 in fp32: sums
-// 8 us, steps 12, product 4; what is left is three launches and the chain of the steps.
+// 7 us, steps 17, product 4; what is left is three launches and the chain of the steps.
 
 constexpr uint32_t kNarrow = 32, kNarrowRow = kNarrow + 1;
 constexpr uint32_t kNarrowParts = 128, kNarrowGroups = 2048;  // of a matrix, at most (32 x 200000: 256 of them 78 us, 128 76), and of all
