@@ -773,22 +773,36 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
 // ---- long matrices of at most 32 rows (or columns): X is read twice.  Every X_k is a product P_k X_0 with P_0 = 1, P_{k+1} = B_k P_k, and A_{k+1} = B_k A_k B_k: a sum over the long axis, steps on matrices
 // of 32 x 32, and a product.  All in fp64, on its matrix cores: in fp32 this way loses the small singular values, whose squares A has from the beginning on.  |x|^2 is A's trace.  10 x 28196 in fp32: sums
 // 7 us, steps 17, product 4; what is left is three launches and the chain of the steps.
+//
+// A that is carried along is off by its first roundings, 2^-53, times the square of what the steps multiply a small singular value with.  Where X has no such direction those roundings are all that A has of it; they
+// may be negative, and then the steps' terms add up instead of cancelling (32 x 400 of rank 5 in fp32: off by 2e-3 after 14 steps, NaN after 20).  So the steps come in rounds, each of which forms A from X
+// again: X = P X in fp64 in the workspace.  A round ends before the step in front of which its steps have multiplied by kNarrowGrowth: A is off by 2^-33 then.
 
 constexpr uint32_t kNarrow = 32, kNarrowRow = kNarrow + 1;
 constexpr uint32_t kNarrowParts = 128, kNarrowGroups = 2048;  // of a matrix, at most (32 x 200000: 256 of them 78 us, 128 76), and of all
 constexpr uint32_t kNarrowAhead = 2;                          // requests of a wavefront, 16 values of the long axis each
+constexpr double kNarrowGrowth = 1024.0;
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
 struct Narrow {
     const void* x;
     void* out;
-    int64_t x_matrix, x_row, out_matrix, out_row;
-    uint32_t rows, cols, s, l, parts, each, n_steps;  // each: values of the long axis of a part, a multiple of 64
+    int64_t x_matrix, x_down, x_along, out_matrix, out_down, out_along;  // from one of the at most 32 rows to the next, and along them
+    uint32_t s, l, parts, each, begin, end;  // each: values of the long axis of a part, a multiple of 64; begin, end: the round's steps
     double *sums, *products;  // [matrices][parts][32][32]; [matrices][32][32], of X as it is
     float eps;
     float coefficients[64][3];
 };
+
+__device__ __forceinline__ double load1(const double* p) { return *p; }
+template <class O>
+__device__ __forceinline__ O rounded(double v) {
+    if constexpr (sizeof(O) == 8)
+        return v;
+    else
+        return (O)(float)v;  // (to bfloat16 by way of fp32: 2^-24 more)
+}
 
 // A lane has row lane % 16 of a's 16 and column lane % 16 of b's, value lane / 16 of the summed axis' four; of the result column lane % 16 and rows 4 r + lane / 16.
 __device__ __forceinline__ f64x4 product64(double a, double b, f64x4 sum) { return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, sum, 0, 0, 0); }
@@ -798,26 +812,24 @@ template <class T>
 __global__ __launch_bounds__(256) void narrow_sums_kernel(const Narrow a) {
     __shared__ double total[3][256][4];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), matrix = blockIdx.y, row = lane & 15u;
-    const bool tall = a.rows > a.cols;
     const T* x = static_cast<const T*>(a.x) + (int64_t)matrix * a.x_matrix;
-    const int64_t along = tall ? a.x_row : 1, down = tall ? 1 : a.x_row;
     const uint32_t begin = blockIdx.x * a.each, end = min(begin + a.each, a.l);
     f64x4 sum[3] = {(f64x4)0.0, (f64x4)0.0, (f64x4)0.0};
     for (uint32_t first = begin + 16u * wave; first < end; first += 64u * kNarrowAhead) {
         T v[kNarrowAhead][2][4];
-        const bool whole = !tall && first + 64u * kNarrowAhead - 48u <= end;
+        const bool whole = a.x_along == 1 && first + 64u * kNarrowAhead - 48u <= end;
 #pragma unroll
         for (uint32_t n = 0; n < kNarrowAhead; ++n)
 #pragma unroll
             for (uint32_t half = 0; half < 2; ++half) {
                 // (of rows and places that are not there the last one's: requests without conditions do not wait for each other)
                 const uint32_t r = min(row + 16u * half, a.s - 1u), p = first + 64u * n + 4u * (lane >> 4);
-                const T* at = x + (int64_t)r * down;
+                const T* at = x + (int64_t)r * a.x_down;
                 if (whole) {
                     __builtin_memcpy(v[n][half], at + p, sizeof(v[n][half]));  // (at the address of any value)
                 } else {
 #pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e) v[n][half][e] = at[(int64_t)min(p + e, end - 1u) * along];
+                    for (uint32_t e = 0; e < 4; ++e) v[n][half][e] = at[(int64_t)min(p + e, end - 1u) * a.x_along];
                 }
             }
 #pragma unroll
@@ -868,7 +880,7 @@ __global__ __launch_bounds__(kNarrow * kNarrow) void narrow_steps_kernel(const N
     double trace = 0.0;
 #pragma unroll
     for (uint32_t i = 0; i < kNarrow; ++i) trace += A[i][i];  // (zeros behind the last row)
-    const double over = 1.0 / (sqrt(trace) + (double)a.eps);
+    const double over = a.begin ? 1.0 : 1.0 / (sqrt(trace) + (double)a.eps);
     __syncthreads();
     A[row][col] = v * over * over;
     __syncthreads();
@@ -883,7 +895,7 @@ __global__ __launch_bounds__(kNarrow * kNarrow) void narrow_steps_kernel(const N
         for (uint32_t r = 0; r < 4; ++r) to[row0 + 4u * r + (lane >> 4)][col0 + (lane & 15u)] = tile[r];
     };
     const bool works = wave < 4u;
-    for (uint32_t step = 0; step < a.n_steps; ++step) {
+    for (uint32_t step = a.begin; step < a.end; ++step) {
         const double c0 = a.coefficients[step][0], c1 = a.coefficients[step][1], c2 = a.coefficients[step][2];
         f64x4 b = (f64x4)0.0, p = b, t = b;
         if (works) {
@@ -897,7 +909,7 @@ __global__ __launch_bounds__(kNarrow * kNarrow) void narrow_steps_kernel(const N
         }
         __syncthreads();
         if (works) {
-            p = step ? multiplied(B, P) : b;
+            p = step > a.begin ? multiplied(B, P) : b;
             t = multiplied(A, B);
             put(T, t);
         }
@@ -912,19 +924,18 @@ __global__ __launch_bounds__(kNarrow * kNarrow) void narrow_steps_kernel(const N
 }
 
 // P X: a workgroup has 64 places on the long axis, whose values each of its wavefronts reads before any of them writes its share of the rows.
-template <class T>
+template <class T, class O>
 __global__ __launch_bounds__(256) void narrow_product_kernel(const Narrow a) {
     typedef const __attribute__((address_space(4))) double* Constant;  // (P's values are all lanes': scalar registers)
     const uint32_t matrix = blockIdx.y;
     const Constant P = (Constant)(a.products + (size_t)matrix * (kNarrow * kNarrow));
     const uint32_t at = blockIdx.x * 64u + (threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), each = (a.s + 3u) / 4u;
-    const bool tall = a.rows > a.cols, there = at < a.l;
-    const T* x = static_cast<const T*>(a.x) + ((int64_t)matrix * a.x_matrix + (there ? (int64_t)at * (tall ? a.x_row : 1) : 0));
-    T* out = static_cast<T*>(a.out) + ((int64_t)matrix * a.out_matrix + (int64_t)at * (tall ? a.out_row : 1));
-    const int64_t down = tall ? 1 : a.x_row, out_down = tall ? 1 : a.out_row;
+    const bool there = at < a.l;
+    const T* x = static_cast<const T*>(a.x) + ((int64_t)matrix * a.x_matrix + (there ? (int64_t)at * a.x_along : 0));
+    O* out = static_cast<O*>(a.out) + ((int64_t)matrix * a.out_matrix + (int64_t)at * a.out_along);
     T raw[kNarrow];
 #pragma unroll
-    for (uint32_t k = 0; k < kNarrow; ++k) raw[k] = x[(int64_t)min(k, a.s - 1u) * down];
+    for (uint32_t k = 0; k < kNarrow; ++k) raw[k] = x[(int64_t)min(k, a.s - 1u) * a.x_down];
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (they have come, not only been asked for: out may be x)
     __syncthreads();
     if (!there) return;
@@ -935,7 +946,7 @@ __global__ __launch_bounds__(256) void narrow_product_kernel(const Narrow a) {
         double sum[4] = {};
 #pragma unroll
         for (uint32_t k = 0; k < kNarrow; ++k) sum[k & 3u] = __builtin_fma(P[i * kNarrow + k], (double)load1(&raw[k]), sum[k & 3u]);
-        out[(int64_t)i * out_down] = (T)(float)(sum[0] + sum[1] + (sum[2] + sum[3]));  // (to bfloat16 by way of fp32: 2^-24 more)
+        out[(int64_t)i * a.out_down] = rounded<O>(sum[0] + sum[1] + (sum[2] + sum[3]));
     }
 }
 
@@ -944,6 +955,24 @@ bool is_narrow(uint32_t s, uint32_t l) { return s <= kNarrow && l > 320u; }
 // Parts of 256 values, of 512 where those are more than 32: the steps' workgroup reads all of their sums.  (10 x 28196: of 256 35 us, of 512 30; 31 x 4000: 27 and 31.)
 uint32_t narrow_parts(uint32_t l, uint32_t n_matrices) {
     return std::min({kNarrowParts, std::max(1u, kNarrowGroups / n_matrices), std::max(std::min((l + 255u) / 256u, 32u), (l + 511u) / 512u)});
+}
+
+// Where the rounds of steps end, and how many there are.
+uint32_t narrow_rounds(const pxr_orthogonalise_desc& d, uint32_t (&ends)[64]) {
+    uint32_t rounds = 0;
+    double most = 1.0, grown = 1.0;
+    for (uint32_t k = 0; k < d.n_steps; ++k) {
+        if (grown > kNarrowGrowth) {
+            ends[rounds++] = k;
+            grown = 1.0;
+        }
+        const float* c = d.coefficients + 3 * k;
+        const OrthogonaliseBounds next = orthogonalise_bounds(c[0], c[1], c[2], most);
+        grown = std::max(grown, 1.0) * next.factor;  // (steps that make everything smaller make room for no more roundings)
+        most = next.most;
+    }
+    ends[rounds++] = d.n_steps;
+    return rounds;
 }
 
 float power_below(double v) { return (float)std::exp2(std::floor(std::log2(v))); }
@@ -1084,13 +1113,41 @@ hipError_t launch_small(const Small& a, uint32_t n_matrices, hipStream_t st) {
     return hipGetLastError();
 }
 
+// `a`: of all rounds at once, from the update to the result; `held`: X between rounds, [matrices][s][l].
 template <class T>
-hipError_t launch_narrow(const Narrow& a, uint32_t n_matrices, hipStream_t st) {
-    const dim3 threads(256);
-    hipLaunchKernelGGL((narrow_sums_kernel<T>), dim3(a.parts, n_matrices), threads, 0, st, a);
-    hipLaunchKernelGGL(narrow_steps_kernel, dim3(n_matrices), dim3(kNarrow * kNarrow), 0, st, a);
-    hipLaunchKernelGGL((narrow_product_kernel<T>), dim3((a.l + 63u) / 64u, n_matrices), threads, 0, st, a);
-    return hipGetLastError();
+hipError_t launch_narrow(const Narrow& a, const uint32_t* ends, uint32_t rounds, double* held, uint32_t n_matrices, hipStream_t st) {
+    const dim3 threads(256), parts(a.parts, n_matrices), places((a.l + 63u) / 64u, n_matrices);
+    Narrow n = a;
+    for (uint32_t round = 0; round < rounds; ++round) {
+        const bool first = round == 0u, last = round + 1u == rounds;
+        n.begin = first ? 0u : ends[round - 1u];
+        n.end = ends[round];
+        if (!first) {
+            n.x = held;
+            n.x_matrix = (int64_t)a.s * a.l;
+            n.x_down = a.l;
+            n.x_along = 1;
+        }
+        n.out = last ? a.out : held;
+        n.out_matrix = last ? a.out_matrix : (int64_t)a.s * a.l;
+        n.out_down = last ? a.out_down : a.l;
+        n.out_along = last ? a.out_along : 1;
+        if (first)
+            hipLaunchKernelGGL((narrow_sums_kernel<T>), parts, threads, 0, st, n);
+        else
+            hipLaunchKernelGGL((narrow_sums_kernel<double>), parts, threads, 0, st, n);
+        hipLaunchKernelGGL(narrow_steps_kernel, dim3(n_matrices), dim3(kNarrow * kNarrow), 0, st, n);
+        if (first && last)
+            hipLaunchKernelGGL((narrow_product_kernel<T, T>), places, threads, 0, st, n);
+        else if (first)
+            hipLaunchKernelGGL((narrow_product_kernel<T, double>), places, threads, 0, st, n);
+        else if (last)
+            hipLaunchKernelGGL((narrow_product_kernel<double, T>), places, threads, 0, st, n);
+        else
+            hipLaunchKernelGGL((narrow_product_kernel<double, double>), places, threads, 0, st, n);
+        if (const hipError_t rc = hipGetLastError(); rc != hipSuccess) return rc;
+    }
+    return hipSuccess;
 }
 
 int result(hipError_t rc, std::string& err) {
@@ -1103,7 +1160,11 @@ int result(hipError_t rc, std::string& err) {
 
 size_t orthogonalise_workspace(const pxr_orthogonalise_desc& d) {
     const uint32_t shorter = std::min(d.rows, d.cols), longer = std::max(d.rows, d.cols);
-    if (is_narrow(shorter, longer)) return (size_t)d.n_matrices * (narrow_parts(longer, d.n_matrices) + 1u) * (kNarrow * kNarrow) * sizeof(double);
+    if (is_narrow(shorter, longer)) {
+        uint32_t ends[64];
+        const size_t held = narrow_rounds(d, ends) > 1u ? (size_t)shorter * longer : 0u;
+        return (size_t)d.n_matrices * ((narrow_parts(longer, d.n_matrices) + 1u) * (kNarrow * kNarrow) + held) * sizeof(double);
+    }
     return is_small(shorter, longer) ? 0 : layout_of(d).bytes;
 }
 
@@ -1111,12 +1172,17 @@ int launch_orthogonalise(const pxr_orthogonalise_desc& d, const void* x, void* o
     hipStream_t st = static_cast<hipStream_t>(stream);
     const uint32_t shorter = std::min(d.rows, d.cols), longer = std::max(d.rows, d.cols);
     if (is_narrow(shorter, longer)) {
-        Narrow a{x, out, d.x_matrix, d.x_row, d.out_matrix, d.out_row, d.rows, d.cols, shorter, longer, narrow_parts(longer, d.n_matrices), 0, d.n_steps, static_cast<double*>(ws), nullptr, d.eps, {}};
+        const bool tall = d.rows > d.cols;
+        Narrow a{x, out, d.x_matrix, tall ? 1 : d.x_row, tall ? d.x_row : 1, d.out_matrix, tall ? 1 : d.out_row, tall ? d.out_row : 1, shorter, longer, narrow_parts(longer, d.n_matrices), 0, 0, 0,
+                 static_cast<double*>(ws), nullptr, d.eps, {}};
         a.products = a.sums + (size_t)d.n_matrices * a.parts * (kNarrow * kNarrow);
+        double* const held = a.products + (size_t)d.n_matrices * (kNarrow * kNarrow);
         a.each = ((longer + a.parts - 1u) / a.parts + 63u) / 64u * 64u;
         a.parts = (longer + a.each - 1u) / a.each;
         std::copy_n(d.coefficients, 3 * d.n_steps, &a.coefficients[0][0]);
-        return result(d.dtype == PXR_F32 ? launch_narrow<float>(a, d.n_matrices, st) : launch_narrow<__bf16>(a, d.n_matrices, st), err);
+        uint32_t ends[64];
+        const uint32_t rounds = narrow_rounds(d, ends);
+        return result(d.dtype == PXR_F32 ? launch_narrow<float>(a, ends, rounds, held, d.n_matrices, st) : launch_narrow<__bf16>(a, ends, rounds, held, d.n_matrices, st), err);
     }
     if (is_small(shorter, longer)) {
         Small a{x, out, d.x_matrix, d.x_row, d.out_matrix, d.out_row, d.rows, d.cols, shorter, longer, up32(shorter), up32(longer), d.n_steps, d.eps, 0.0f, {}};

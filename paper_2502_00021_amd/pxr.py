@@ -1125,8 +1125,8 @@ def orthogonalise(x, steps=None, coefficients=ORTHOGONALISE_COEFFICIENTS, eps=1e
     d = _pack_orthogonalise(_dtype_code(torch, x.dtype), B, shape[-2], shape[-1], s[0] if len(s) == 3 else 0, s[-2], t[0] if len(t) == 3 else 0, t[-2],
                             c.shape[0], c.ctypes.data, eps)
     L = _lib or lib()
-    sizes = d[:16]
-    asked, need = _orthogonalise_asked  # (the bytes for the sizes that were asked for last are known)
+    sizes = d[:16] + c.tobytes()
+    asked, need = _orthogonalise_asked  # (the bytes for the sizes and steps that were asked for last are known)
     if asked != sizes:
         n = C.c_size_t()
         _check(L.pxr_orthogonalise_workspace(d, n))

@@ -258,3 +258,90 @@ def test_refusals(torch, pxr):
     with pytest.raises(pxr.PxrError, match="overlap"):
         pxr.orthogonalise(x[None].expand(2, -1, -1), out=x[None].expand(2, -1, -1))
     assert pxr.orthogonalise(torch.empty((0, 5, 6), device="cuda")).shape == (0, 5, 6)
+
+
+def _of_rank(rng, m, n, rank, whole):
+    """[m,n] of this rank but for fp32's rounding, or of whole numbers small enough for bfloat16, and of this rank exactly."""
+    if whole:
+        return (rng.integers(-1, 2, (m, rank)) @ rng.integers(-4, 5, (rank, n))).astype(np.float32)
+    return (rng.standard_normal((m, rank)) @ rng.standard_normal((rank, n))).astype(np.float32)
+
+
+def _in_80_bits(x, coefficients):
+    x = x.astype(np.longdouble)
+    x = x / np.sqrt((x ** 2).sum())
+    for a, b, c in coefficients:
+        gram = x @ x.T
+        x = a * x + (b * gram + c * (gram @ gram)) @ x
+    return x.astype(np.float64)
+
+
+@pytest.mark.parametrize("tall", [False, True])
+@pytest.mark.parametrize("step,n_steps", [(QUINTIC, 6), (QUINTIC, 7), (QUINTIC, 14), (QUINTIC, 16), (QUINTIC, 24), (QUINTIC, 64), ((1.5, -0.5, 0.0), 24), ((1.5, -0.5, 0.0), 40), ((1.5, -0.5, 0.0), 64)])
+def test_long_matrices_of_lower_rank_take_many_steps(torch, pxr, step, n_steps, tall):
+    """As where a batch had fewer examples than the matrix has rows.  In every step that a singular value is far below one it is multiplied by 3.4 (1.5), and the definition's own roundings in 64 bits with
+    it: e, what those steps in fp64 are off by from the same ones in 80 bits.  Here A is formed from X again before the steps have multiplied it by 1024 and the next step's factor, and is off by that, squared, of the roundings of its sums, s of
+    2^-53; the result by 8 e for other orders, that, and its own rounding.  Where e leaves nothing to compare with, singular values have the bound that the steps have: the quintic's is 1.2025, the cubic's 1, from their
+    values at most 1, and a chain of roundings beside it."""
+    rng = np.random.default_rng(n_steps)
+    five = tuple(float(np.float32(c)) for c in step)
+    sets = [(_of_rank(rng, 32, 400, 5, False), "f32"), (_of_rank(rng, 32, 400, 5, True), "f32"), (_of_rank(rng, 7, 3000, 3, True), "bf16"), (_of_rank(rng, 20, 1000, 1, False), "f32")]
+    for x, dtype in sets:
+        t = torch.from_numpy(x.T.copy() if tall else x).cuda().to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+        got = pxr.orthogonalise(t, coefficients=[five] * n_steps, eps=0.0)
+        assert got.dtype == t.dtype and bool(got.isfinite().all())
+        out = got.double().cpu().numpy()
+        out = out.T if tall else out
+        assert np.linalg.norm(out, 2) <= (1.2025 if step == QUINTIC else 1.0) * (1 + 2.0 ** -10) + (W if dtype == "bf16" else 0) * np.linalg.norm(out)
+        ref = _in_80_bits(x, [five] * n_steps)
+        e = np.linalg.norm(learner.orthogonalise(x, [five] * n_steps, 0.0) - ref) / np.linalg.norm(ref)
+        allowed = U + len(x) * 2.0 ** -53 * (1024 * step[0]) ** 2 + 8 * e + (W if dtype == "bf16" else 0)
+        if e <= 0.01:
+            assert np.linalg.norm(out - ref) <= allowed * np.linalg.norm(ref), (x.shape, dtype, e)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rounds_of_steps_of_several_long_matrices(torch, pxr, dtype):
+    """Each matrix by itself, in place, with rows apart, beside one that is not finite, in a graph; nothing else is written."""
+    many = dict(steps=20)
+    for B, m, n in ((3, 9, 2000), (2, 1500, 30)):
+        x = normal(torch, n, B, m, n, dtype=dtype)
+        want = pxr.orthogonalise(x, **many)
+        for i in range(B):
+            assert torch.equal(pxr.orthogonalise(x[i], **many), want[i])
+        wide = torch.full((B + 1, m + 2, n + 5), 7.0, device="cuda", dtype=x.dtype)
+        view = wide[:B, 1:-1, 3:3 + n]
+        view.copy_(x)
+        pxr.orthogonalise(view, out=view, **many)
+        assert torch.equal(view, want)
+        view.fill_(7.0)
+        assert (wide == 7).all()
+        bad = x.clone()
+        bad[0, m // 2, n // 3] = float("inf")
+        got = pxr.orthogonalise(bad, **many)
+        assert got[0].isnan().all() and torch.equal(got[1:], want[1:])
+        assert (pxr.orthogonalise(torch.zeros_like(x), **many) == 0).all()
+        # the workspace goes by the steps as well: fewer and more of them in turn
+        for steps in (5, 20, 6, 7):
+            assert bool(pxr.orthogonalise(x, steps=steps).isfinite().all())
+        static, g = x.clone(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            y = pxr.orthogonalise(static, **many)
+        for i in (1, 2, 1):
+            static.copy_(x * i)
+            g.replay()
+            eager = pxr.orthogonalise(x * i, **many)
+            torch.cuda.synchronize()
+            assert torch.equal(y, eager)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(32, 300), (100, 90), (40, 3000), (300, 200)])
+def test_other_matrices_of_lower_rank_take_many_steps(torch, pxr, m, n, dtype):
+    """Directions that a matrix does not have are made of the parts' roundings, 2^-23, after some 13 steps, as they are of fp32's: they stay below the bound of the singular values that it has."""
+    x = torch.from_numpy(_of_rank(np.random.default_rng(m), m, n, 5, True)).cuda().to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    for step, most in ((QUINTIC, 1.2025), ((1.5, -0.5, 0.0), 1.0)):
+        for n_steps in (16, 24, 64):
+            got = pxr.orthogonalise(x, n_steps, step, eps=0.0)
+            assert bool(got.isfinite().all())
+            assert float(torch.linalg.matrix_norm(got.double().cpu(), 2)) <= most * 1.01 + (W if dtype == "bf16" else 0) * float(got.double().norm())

@@ -72,3 +72,16 @@ def test_bounds_of_singular_values():
             got = fn(a, b, c, most)
             value, factor = np.abs(a * t + b * t ** 3 + c * t ** 5).max(), np.abs(a + b * t ** 2 + c * t ** 4).max()
             assert value <= got.most <= value * 1.002 + 1e-6 and factor <= got.factor * (1 + 1e-12) <= factor * 1.001 + 1e-6, (a, b, c, most)
+
+
+@pytest.mark.parametrize("steps", [(QUINTIC,) * 7, ((1.5, -0.5, 0.0),) * 19, ((1100.0, 0.0, 0.0), (0.001, 0.0, 0.0))])
+def test_long_matrices_of_few_rows_take_many_steps_in_rounds(steps):
+    """A has to be formed from X again before the steps have multiplied its roundings by their factors' squares, 1024^2 and more: X is held between two rounds, [rows,cols] in fp64."""
+    one, two = (_call(rows=8, cols=5000, x_row=5000, out_row=5000, coefficients=c)[2] for c in (steps[:-1], steps))
+    assert two == one + 8 * 8 * 5000
+    assert _call(rows=5000, cols=8, x_row=8, out_row=8, n_matrices=3, out_matrix=40000, coefficients=steps)[2] == 3 * two
+    assert _call(rows=5000, cols=8, x_row=8, out_row=8, coefficients=steps, workspace=two - 1)[1] == pxr.ERR_INVALID_ARG
+    # smaller ones, and those of more rows, form it in every step
+    for m, n in ((8, 300), (40, 5000)):
+        need = [_call(rows=m, cols=n, x_row=n, out_row=n, coefficients=c) for c in (steps[:1], steps)]
+        assert need[0][0] == pxr.OK and need[0][2] == need[1][2]
