@@ -53,7 +53,12 @@ __device__ __forceinline__ void store(T* p, const T (&v)[N]) { __builtin_memcpy(
 // the quarters.
 __device__ __forceinline__ void sine(uint32_t turn, float& s, float& c) {
     const uint32_t quarter = (turn + 0x20000000u) >> 30;
-    const float x = (float)(int)(turn - (quarter << 30)) * 1.46291807926715968e-9f;  // 2 pi / 2^32
+    // 2 pi / 2^32 times 30 bits, both in two parts: rounded once (a sixth of the root mean square of the sines' errors)
+    constexpr double kTurn = 1.46291807926715968e-9;
+    constexpr float kFirst = (float)kTurn, kRest = (float)(kTurn - (double)kFirst);
+    const int whole = (int)(turn - (quarter << 30));
+    const float first = (float)whole, rest = (float)(whole - (int)first);
+    const float x = __builtin_fmaf(first, kFirst, __builtin_fmaf(first, kRest, rest * kFirst));
     const float z = x * x;
     float p = __builtin_fmaf(z, 2.75573192e-6f, -1.98412698e-4f);
     p = __builtin_fmaf(z, p, 8.33333333e-3f);
@@ -67,6 +72,13 @@ __device__ __forceinline__ void sine(uint32_t turn, float& s, float& c) {
     const float a = quarter & 1u ? far : near, b = quarter & 1u ? near : far;
     s = quarter & 2u ? -a : a;
     c = (quarter + 1u) & 2u ? -b : b;
+}
+
+// 1 / sqrt(v), the last digit of the two roundings given back (a tenth of the root mean square of all errors of a turned value).
+__device__ __forceinline__ float reciprocal_root(float v) {
+    const float r = 1.0f / sqrtf(v), h = v * r;
+    const float off = __builtin_fmaf(-h, r, 1.0f) - __builtin_fmaf(v, r, -h) * r;  // 1 - v r^2
+    return v > 0.0f && v < __builtin_inff() ? __builtin_fmaf(0.5f * r, off, r) : r;
 }
 
 // Where the slots of vector number `vector` lie in a head, V of them next to each other, and which of their second values there are.
@@ -192,7 +204,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
                         s = __builtin_fmaf(hi, hi, s);
                         if constexpr (kBack) {
                             const float dlo = at.any ? (float)ds[u][k][0][v] : 0.0f, dhi = at.second ? (float)ds[u][k][1][v] : 0.0f;
-                            const float glo = dlo * cos[k][v] + dhi * sin[k][v], ghi = dhi * cos[k][v] - dlo * sin[k][v];
+                            const float glo = __builtin_fmaf(dlo, cos[k][v], dhi * sin[k][v]), ghi = __builtin_fmaf(dhi, cos[k][v], -(dlo * sin[k][v]));
                             along = __builtin_fmaf(w[k][0][v] * glo, lo, along);
                             along = __builtin_fmaf(w[k][1][v] * ghi, hi, along);
                         }
@@ -205,7 +217,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (head0 + u >= t.heads) continue;
-                const float rstd = 1.0f / sqrtf(both[u] / a.width + a.eps);
+                const float rstd = reciprocal_root(both[u] / a.width + a.eps);
                 float back = 0.0f;
                 if constexpr (kBack) back = both[U + u] * rstd / a.width * rstd;
 #pragma unroll
@@ -217,15 +229,15 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(const HeadNormArgs 
                         const float xlo = (float)xs[u][k][0][v] , xhi = (float)xs[u][k][1][v];
                         if constexpr (kBack) {
                             const float dlo = (float)ds[u][k][0][v], dhi = at.second ? (float)ds[u][k][1][v] : 0.0f;
-                            const float glo = dlo * cos[k][v] + dhi * sin[k][v], ghi = dhi * cos[k][v] - dlo * sin[k][v];
-                            lo[v] = (T)(rstd * (w[k][0][v] * glo - xlo * back));
-                            hi[v] = (T)(rstd * (w[k][1][v] * ghi - xhi * back));
+                            const float glo = __builtin_fmaf(dlo, cos[k][v], dhi * sin[k][v]), ghi = __builtin_fmaf(dhi, cos[k][v], -(dlo * sin[k][v]));
+                            lo[v] = (T)(rstd * __builtin_fmaf(w[k][0][v], glo, -(xlo * back)));
+                            hi[v] = (T)(rstd * __builtin_fmaf(w[k][1][v], ghi, -(xhi * back)));
                             sum[k][0][v] = __builtin_fmaf(glo, xlo * rstd, sum[k][0][v]);
                             sum[k][1][v] = __builtin_fmaf(ghi, xhi * rstd, sum[k][1][v]);
                         } else {
                             const float ylo = xlo * rstd * w[k][0][v], yhi = xhi * rstd * w[k][1][v];
-                            lo[v] = (T)(ylo * cos[k][v] - yhi * sin[k][v]);
-                            hi[v] = (T)(yhi * cos[k][v] + ylo * sin[k][v]);
+                            lo[v] = (T)__builtin_fmaf(ylo, cos[k][v], -(yhi * sin[k][v]));
+                            hi[v] = (T)__builtin_fmaf(yhi, cos[k][v], ylo * sin[k][v]);
                         }
                     }
                     T* to = out + (int64_t)(head0 + u) * t.out_head;
