@@ -371,10 +371,15 @@ void pxr::fill_head(LinearAttentionHead& h, float log_decay) {
     for (int n = 0; n <= 32; ++n) h.power[n] = (float)std::exp((double)log_decay * n);
 }
 
-// frequency / 2 pi as a fraction of 2^64, modulo whole turns.
+// frequency / 2 pi as a fraction of 2^64, modulo whole turns, rounded once: the frequency's 53 bits times 128 bits of 1 / 2 pi in whole numbers (frequencies are below 2^21, so of the bits in front of the point
+// at most 18 go, and what is cut off before the rounding is below 2^-31 of a unit).
 uint64_t pxr::turns_of(double frequency) {
-    const long double turns = (long double)frequency / 6.283185307179586476925286766559005768L;
-    const long double part = turns - std::floor(turns);  // in [0, 1]
-    const long double scaled = part * 18446744073709551616.0L;
-    return scaled >= 18446744073709551616.0L ? 0u : (uint64_t)scaled;
+    typedef unsigned __int128 wide;
+    constexpr uint64_t kHigh = 0x28BE60DB9391054Aull, kLow = 0x7F09D5F47D4D3770ull;  // 1 / 2 pi in fractions of 2^128
+    int exponent;
+    const uint64_t bits = (uint64_t)std::ldexp(std::frexp(std::fabs(frequency), &exponent), 53);  // times 2^(exponent - 53)
+    const wide high = (wide)bits * kHigh + (((wide)bits * kLow) >> 64);  // in fractions of 2^64, times 2^(exponent - 53)
+    const int down = 53 - exponent;  // at least 32
+    const uint64_t turns = down > 127 ? 0u : (uint64_t)(((high >> (down - 1)) + 1u) >> 1);
+    return frequency < 0.0 ? 0u - turns : turns;
 }

@@ -54,3 +54,16 @@ def test_angles_of_far_positions():
             off = min(off, 2 ** 200 - off) / 2 ** 200
             # f in turns has a rounding of 2^-64 of its size (long double) or of one turn, whichever is more
             assert off <= abs(position) * 2.0 ** -63 * max(1.0, abs(f)), (f, position)
+
+
+def test_turns_are_rounded_once():
+    """Of any frequency that a layer takes, and whatever its size: frequency / 2 pi as the nearest fraction of 2^64 (or, where two are within 2^-31 of as near, either), so that an angle keeps 2^-22 turns up to positions of 2^31
+    (2^-34 of its fraction, 2^-32 of the fraction's upper half, the rest of fp32)."""
+    two_pi = 6283185307179586476925286766559005768394338798750211641949889184615632812572417997256069650684234135964296173026564613294187689219101164463450718816256962
+    digits = 10 ** (len(str(two_pi)) - 1)
+    rng = np.random.default_rng(1)
+    some = [1000003.7, 2.0 ** 20, 1e6, 16384.0, 2 * math.pi, 40 * math.pi, 1.0, 1e-9, 1e-30, 5e-324, 0.0, -0.0, *(2.0 ** rng.uniform(-70, 20, 200)), *(rng.integers(1, 2 ** 20, 50) + 0.0)]
+    for f in [s * float(x) for x in some for s in (1, -1)]:
+        num, den = f.as_integer_ratio()
+        off = (_turns(f) * 2 ** 136 - num * 2 ** 200 * digits // (den * two_pi)) % 2 ** 200
+        assert min(off, 2 ** 200 - off) <= 2 ** 135 * (1 + 2.0 ** -30), f
