@@ -410,7 +410,8 @@ int pxr_gated_recurrence_workspace(uint32_t n_envs, uint32_t n_steps, uint32_t w
 
 /* All steps of a rollout at once: out [n_envs,n_steps,width] of the rollout's type, and the state after the last step in d_state_out
  * [n_envs,width] fp32 (NULL if not wanted; not the buffer of d_state).  n_steps == 0 passes the state on.  An infinity or NaN in a step's
- * x or gate reaches that step and later ones of the same environment, channel and episode and nothing else (an infinity may come out as NaN).
+ * x or gate reaches that step and later ones of the same environment, channel and episode and nothing else (an infinity may come out as NaN); where coupled is 0, the gate
+ * of a step that begins an episode is not looked at, and its gradient is 0 (where those of the outputs are finite).
  * What is written must not overlap what is read.  Equal inputs give equal bits.
  * Errors: INVALID_ARG (null, n_envs or width == 0, n_envs * ceil(width / 64) * ceil(n_steps / 128) above 2^22, n_steps above 2^31-1, a type
  * that is none, coupled above 1, a buffer not aligned to its elements, states that overlap, workspace missing, too small or not 16-byte

@@ -171,7 +171,8 @@ struct Chunk {
             none &= on;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float g = gate_of<T>(gs[j].get(i));
+                // (where inputs are taken as they are, a step that begins an episode has no use for its gate, whatever that is)
+                const float gate = gate_of<T>(gs[j].get(i)), g = kCoupled ? gate : masked(gate, on);
                 A[i] = masked(kept(g, A[i]), none);
                 H[i] = kept(g, masked(H[i], on), input(g, xs[j].get(i)));
                 if (kWhat == kForward) h[j][i] = H[i];

@@ -438,3 +438,30 @@ def test_refusals(torch, pxr):
         pxr.gated_recurrence_step(x, gate, s)
     with pytest.raises(pxr.PxrError, match="positive"):
         pxr.gated_recurrence(x[:0], gate[:0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,D", [(3, 6, 5), (2, 40, 33), (1, 2500, 3), (4, 300, 20)])
+def test_gates_that_are_not_looked_at(torch, pxr, B, T, D, dtype):
+    """Where inputs are taken as they are, the gate of a step that begins an episode multiplies nothing: whatever it is, a rollout, its gradients and the same steps one by one are those of another gate there, and its gradient is 0."""
+    rng = np.random.default_rng(T)
+    x, gate, r, s, dout, ds = inputs(torch, rng, B, T, D, dtype, resets=0.1)
+    r[0, T // 2] = r[0, 0] = r[-1, T - 1] = True
+    plain = torch.where(r[..., None], 0.0, gate)
+    want = pxr.gated_recurrence(x, plain, resets=r, state=s, coupled=False)
+    grads = pxr.gated_recurrence_backward(dout, x, plain, resets=r, state=s, dstate=ds, coupled=False)
+    check(torch, pxr, x, plain, r, s, dout, ds, coupled=False)
+    for value in (float("nan"), float("inf"), -float("inf"), 3.0):
+        bad = torch.where(r[..., None], value, gate)
+        got = pxr.gated_recurrence(x, bad, resets=r, state=s, coupled=False)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        got = pxr.gated_recurrence_backward(dout, x, bad, resets=r, state=s, dstate=ds, coupled=False)
+        assert all(torch.equal(a, b) for a, b in zip(got, grads)) and (got[1][r] == 0).all()
+        # a step's own way of writing the same sum: as many roundings, of the recurrence of the magnitudes
+        state, stepped = s.clone(), []
+        for t in range(min(T, 60)):
+            stepped.append(pxr.gated_recurrence_step(x[:, t], bad[:, t], state, resets=r[:, t], coupled=False))
+        ref, _ = om.gated_recurrence(f64(x), f64(plain), r.cpu().numpy(), f64(s), False)
+        M, _ = om.gated_recurrence(abs(f64(x)), f64(plain), r.cpu().numpy(), abs(f64(s)), False)
+        n = len(stepped)
+        close(f64(torch.stack(stepped, 1)), ref[:, :n], M[:, :n], (8 + 2 * np.abs(f64(plain)).max()) * (n + 4), dtype == "bf16", "steps")
