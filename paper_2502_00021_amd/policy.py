@@ -127,7 +127,8 @@ def episode_positions(n_envs, n_steps, resets=None, first=None):
 
 class Orthogonal(torch.optim.Optimizer):
     """Steps weight matrices by their momentum with its singular values pushed towards one (pxr.orthogonalise), so that every direction
-    of an update counts alike.  Matrices of one size and type go together.  Only matrices: vectors have no such update."""
+    of an update counts alike.  Matrices of one size and type go together.  Only matrices: vectors have no such update.  A matrix [m,n] with
+    m > n takes lr * sqrt(m / n) of its update, the others lr of theirs.  Parameters are of the current device; a step that is refused has written nothing."""
 
     def __init__(self, params, lr=0.02, momentum=0.95, nesterov=True, steps=5, eps=1e-7):
         super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, steps=steps, eps=eps))
@@ -142,24 +143,34 @@ class Orthogonal(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        together = []
         for group in self.param_groups:
             same = {}
             for p in group["params"]:
                 if p.grad is not None:
                     same.setdefault((p.shape, p.dtype, p.device), []).append(p)
-            for (shape, _, _), params in same.items():
-                updates = []
-                for p in params:
-                    state = self.state[p]
-                    # (in fp32, whatever the parameter's type: also after torch has loaded it as of that type)
-                    m = state["momentum"].float() if "momentum" in state else torch.zeros(p.shape, dtype=torch.float32, device=p.device)
-                    state["momentum"] = m.mul_(group["momentum"]).add_(p.grad)
-                    updates.append(torch.add(p.grad, m, alpha=group["momentum"]) if group["nesterov"] else m)
-                updates = pxr.orthogonalise(torch.stack(updates), steps=group["steps"], eps=group["eps"])
-                # (a tall matrix has fewer directions than rows: the step of a row stays what it is for a square one)
-                size = group["lr"] * max(1.0, shape[0] / shape[1]) ** 0.5
-                for p, update in zip(params, updates):
-                    p.sub_(update, alpha=size)
+            together += [(group, params) for params in same.values()]
+        # (what a call refuses is refused here, before any momentum or parameter is another one)
+        for group, params in together:
+            pxr.orthogonalise_workspace(len(params), *params[0].shape, steps=group["steps"], eps=group["eps"])
+            for p in params:
+                if not (p.is_cuda and p.is_floating_point() and p.grad.layout == torch.strided):
+                    raise ValueError(f"only dense gradients of real matrices on the GPU, not {p.dtype} {p.grad.layout} on {p.device}")
+                pxr._here(torch, p)
+        for group, params in together:
+            updates = []
+            for p in params:
+                state = self.state[p]
+                # (in fp32, whatever the parameter's type: also after torch has loaded it as of that type)
+                m = state["momentum"].float() if "momentum" in state else torch.zeros(p.shape, dtype=torch.float32, device=p.device)
+                state["momentum"] = m.mul_(group["momentum"]).add_(p.grad)
+                updates.append(torch.add(p.grad, m, alpha=group["momentum"]).float() if group["nesterov"] else m)
+            updates = pxr.orthogonalise(torch.stack(updates), steps=group["steps"], eps=group["eps"])
+            # (a tall matrix has fewer directions than rows: the step of a row stays what it is for a square one)
+            m, n = params[0].shape
+            size = group["lr"] * max(1.0, m / n) ** 0.5
+            for p, update in zip(params, updates):
+                p.sub_(update, alpha=size)
         return loss
 
 

@@ -1103,6 +1103,17 @@ def _steps_of(coefficients, steps):
 _orthogonalise_asked = (None, 0)
 
 
+def orthogonalise_workspace(n_matrices, rows, cols, dtype=None, steps=None, coefficients=ORTHOGONALISE_COEFFICIENTS, eps=1e-7):
+    """Bytes of workspace of an orthogonalise call on n_matrices [rows, cols] (float32 unless dtype says otherwise); raises what that call would refuse of its sizes
+    and steps.  Host only."""
+    torch = _torch or _torch_module()
+    c = _steps_of(coefficients, steps)
+    n = C.c_size_t()
+    _check(lib().pxr_orthogonalise_workspace(_pack_orthogonalise(0 if dtype is None else _dtype_code(torch, dtype), n_matrices, rows, cols, rows * cols, cols, rows * cols, cols,
+                                                                 c.shape[0], c.ctypes.data, eps), n))
+    return n.value
+
+
 def orthogonalise(x, steps=None, coefficients=ORTHOGONALISE_COEFFICIENTS, eps=1e-7, out=None, stream=None):
     """A learner's update [m,n], or several [B,m,n], CUDA float32 or bfloat16 (rows at any stride, their values adjacent), with its
     singular values pushed towards one: X = x / (|x| + eps), then for each step X <- a X + (b A + c A^2) X with A = X X^T (of the

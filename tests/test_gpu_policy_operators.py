@@ -281,3 +281,55 @@ def test_learning_runs(torch, policy_module, memory):
 def test_the_command_runs(torch, policy_module, memory, capsys):
     policy_module.main(n_envs=8, n_steps=12, updates=2, memory=memory, orthogonal=True)
     assert "update 1" in capsys.readouterr().out
+
+
+def test_a_step_that_is_refused_leaves_everything_as_it_was(torch, policy_module, monkeypatch):
+    """Whatever stands behind it in another group, or in the same one: no momentum, no parameter is another one; and the next step is as if nothing had been."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    make = lambda *s: torch.nn.Parameter(torch.randn(s, generator=g, device="cuda"))
+    good, bad = [make(24, 40), make(24, 40), make(300, 20)], make(8, 6)
+    for p in [*good, bad]:
+        p.grad = torch.randn(p.shape, generator=g, device="cuda")
+    optimizer = policy_module.Orthogonal([dict(params=good), dict(params=[bad])])
+    optimizer.step()
+    empty, host, whole = torch.nn.Parameter(torch.zeros(0, 5, device="cuda")), torch.nn.Parameter(torch.zeros(3, 4)), bad.grad
+    empty.grad, host.grad = torch.zeros_like(empty), torch.zeros_like(host)
+    state = lambda: [t.clone() for p in [*good, bad] for t in (p.detach(), optimizer.state[p]["momentum"])]
+    before = state()
+
+    def refused(error, match):
+        with pytest.raises(error, match=match):
+            optimizer.step()
+        assert all(torch.equal(a, b) for a, b in zip(state(), before))
+    for other, match in ((empty, "positive"), (host, "GPU")):
+        optimizer.param_groups[1]["params"] = [bad, other]
+        refused((ValueError, policy_module.pxr.PxrError), match)
+    optimizer.param_groups[1]["params"] = [bad]
+    bad.grad = whole.to_sparse()
+    refused(ValueError, "dense")
+    bad.grad = whole
+    for name, value, match in (("steps", 0, "n_steps"), ("eps", -1.0, "eps")):
+        kept = optimizer.param_groups[1][name]
+        optimizer.param_groups[1][name] = value
+        refused(policy_module.pxr.PxrError, match)
+        optimizer.param_groups[1][name] = kept
+    with monkeypatch.context() as m:
+        m.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+        refused(AssertionError, "current device is cuda:1")
+    optimizer.step()
+    assert all(not torch.equal(a, b) for a, b in zip(state(), before))
+
+
+def test_orthogonal_steps_of_float64_matrices(torch, policy_module):
+    """Their momentum and update are of 32 bits."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    start, grad = (torch.randn((20, 30), generator=g, device="cuda") for _ in range(2))
+    for nesterov in (True, False):
+        one, two = (torch.nn.Parameter(start.to(to)) for to in (torch.float32, torch.float64))
+        one.grad, two.grad = grad.clone(), grad.double()
+        for p in (one, two):
+            policy_module.Orthogonal([p], nesterov=nesterov).step()
+        # the same update but for the rounding of a gradient's sum with its momentum, and of the parameter's
+        assert two.dtype == torch.float64 and (one.detach().double() - two.detach()).abs().max() <= 2.0 ** -22 * start.abs().max()

@@ -71,3 +71,14 @@ def test_resets_that_change_between_forward_and_backward_are_noticed(stand_ins):
     resets[0, 1] = True
     with pytest.raises(RuntimeError, match="inplace"):
         out.sum().backward()
+
+
+def test_a_step_that_is_refused_has_written_nothing():
+    """Matrices that are not on a GPU, the last of them; sizes and steps that the library refuses."""
+    for shape, change in (((3, 4), {}), ((3, 4), dict(steps=65)), ((3, 4), dict(eps=-1.0)), ((0, 4), {}), ((2 ** 16, 2 ** 16), {})):
+        p = torch.nn.Parameter(torch.zeros(1, 1).expand(shape))
+        p.grad = torch.zeros(1, 1).expand(shape)
+        optimizer = policy.Orthogonal([p], **change)
+        with pytest.raises((ValueError, policy.pxr.PxrError)):
+            optimizer.step()
+        assert "momentum" not in optimizer.state[p]
