@@ -414,21 +414,21 @@ int pxr_gated_recurrence_workspace(uint32_t n_envs, uint32_t n_steps, uint32_t w
  * of a step that begins an episode is not looked at, and its gradient is 0 (where those of the outputs are finite).
  * What is written must not overlap what is read.  Equal inputs give equal bits.
  * Errors: INVALID_ARG (null, n_envs or width == 0, n_envs * ceil(width / 64) * ceil(n_steps / 128) above 2^22, n_steps above 2^31-1, a type
- * that is none, coupled above 1, a buffer not aligned to its elements, states that overlap, workspace missing, too small or not 16-byte
- * aligned); DEVICE. */
+ * that is none, coupled above 1, a buffer not aligned to its elements, states that overlap, a view that is written and has values in common with another of
+ * the same strides, workspace missing, too small or not 16-byte aligned); DEVICE. */
 int pxr_gated_recurrence_forward(const pxr_gated_rollout* r, const pxr_steps* out, float* d_state_out, void* d_workspace,
                                  size_t workspace_bytes, void* hip_stream);
 
 /* Gradients for the outputs' gradients dout and d_dstate_out (of the state after the last step; NULL = zeros): dx, dgate
  * [n_envs,n_steps,width] of the rollout's type and, unless NULL, d_dstate [n_envs,width] fp32, of the state before the first step.  States are
  * computed again in fp32, nothing is kept from the forward pass.  An infinity or NaN in dout reaches that step and earlier ones of the same
- * environment, channel and episode.  What is written must not overlap what is read.  Equal inputs give equal bits.
+ * environment, channel and episode.  What is written must not overlap what is read, or itself.  Equal inputs give equal bits.
  * Errors: as for the forward pass. */
 int pxr_gated_recurrence_backward(const pxr_gated_rollout* r, const pxr_steps* dout, const float* d_dstate_out, const pxr_steps* dx,
                                   const pxr_steps* dgate, float* d_dstate, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 /* One step of every environment: r->n_steps must be 1 (the step strides do not matter), d_state [n_envs,width] is updated in place
- * (r->d_state is not read); out must not overlap what is read.  One kernel.  Errors: as for the forward pass. */
+ * (r->d_state is not read); out must not overlap what is read, but may be x or gate itself.  One kernel.  Errors: as for the forward pass. */
 int pxr_gated_recurrence_step(const pxr_gated_rollout* r, float* d_state, const pxr_steps* out, void* hip_stream);
 
 /* Norms of queries and keys for each head, with the rotation by a step's position in the same pass: what stands before attention

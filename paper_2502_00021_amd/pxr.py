@@ -1066,7 +1066,7 @@ def gated_recurrence_backward(dout, x, gate, resets=None, state=None, dstate=Non
 
 def gated_recurrence_step(x, gate, state, resets=None, coupled=True, out=None, stream=None):
     """One step of every environment: x, gate [B,D], resets [B] or None; state float32 [B,D] is updated in place (autograd is
-    told).  Returns out [B,D]; enqueue only."""
+    told); out may be x or gate itself.  Returns out [B,D]; enqueue only."""
     torch = _torch or _torch_module()
     assert x.dim() == 2
     r, B, _, D = _gated_rollout(torch, x, gate, resets, None, coupled)

@@ -465,3 +465,28 @@ def test_gates_that_are_not_looked_at(torch, pxr, B, T, D, dtype):
         M, _ = om.gated_recurrence(abs(f64(x)), f64(plain), r.cpu().numpy(), abs(f64(s)), False)
         n = len(stepped)
         close(f64(torch.stack(stepped, 1)), ref[:, :n], M[:, :n], (8 + 2 * np.abs(f64(plain)).max()) * (n + 4), dtype == "bf16", "steps")
+
+
+def test_outputs_in_the_place_of_inputs(torch, pxr):
+    """Of a rollout refused, whole or a step on; parts of one buffer side by side are none; a single step's output may be its input."""
+    rng = np.random.default_rng(9)
+    for dtype, B, T, D in (("f32", 3, 40, 33), ("bf16", 2, 300, 129)):
+        x, gate, r, s, dout, ds = inputs(torch, rng, B, T, D, dtype)
+        want, last = pxr.gated_recurrence(x, gate, resets=r, state=s)
+        for out in (x, gate):
+            with pytest.raises(pxr.PxrError, match="overlaps"):
+                pxr.gated_recurrence(x, gate, resets=r, state=s, out=out)
+        wide = torch.zeros((B, T + 1, D), device="cuda", dtype=x.dtype)
+        with pytest.raises(pxr.PxrError, match="overlaps"):
+            pxr.gated_recurrence(wide[:, :-1], gate, out=wide[:, 1:])
+        three = torch.cat([x, gate, torch.zeros_like(x)], -1)
+        a, b, c = three.split([D] * 3, -1)
+        assert torch.equal(pxr.gated_recurrence(a, b, resets=r, state=s, out=c)[0], want) and torch.equal(a, x) and torch.equal(b, gate)
+        step = lambda out: pxr.gated_recurrence_step(a[:, 3], b[:, 3], s.clone(), resets=r[:, 3], out=out)
+        stepped = step(None)
+        kept = three.clone()
+        for out in (a[:, 3], b[:, 3]):
+            assert torch.equal(step(out), stepped)
+            three.copy_(kept)
+        with pytest.raises(pxr.PxrError, match="overlaps"):
+            pxr.gated_recurrence_step(a[:, 3], b[:, 3], s.clone(), out=three[:, 3, 1:1 + D])
