@@ -465,7 +465,7 @@ typedef struct {
 /* The normalised and turned heads to q_out and k_out (NULL where there are no such heads), views of the layout of q and k; either may be its input
  * itself with the same strides.  Sums of squares are fp32.  A head with a NaN or an infinity comes out with NaN in it, the other heads are not touched by it.
  * One kernel.  Errors: INVALID_ARG (null, a type that is none, position_bits that is neither, n_envs * n_steps above 2^31-1, n_heads or n_key_heads above 65535, a
- * buffer not aligned to its elements); DEVICE. */
+ * buffer not aligned to its elements, heads that are written and have values in common with others of the same strides than their own inputs); DEVICE. */
 int pxr_head_norm_forward(pxr_head_norm* n, const pxr_heads* r, const pxr_tokens* q_out, const pxr_tokens* k_out, void* hip_stream);
 
 /* Bytes of workspace that the backward pass needs where it forms a weight's gradient (host only).  Errors: as above (buffers are not looked at). */

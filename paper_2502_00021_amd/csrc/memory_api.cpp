@@ -3,12 +3,12 @@
 
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 #include <new>
 
 #include "pxr_internal.h"
+#include "views.h"
 
 struct pxr_linear_attention {
     pxr::LinearAttentionConsts c{};
@@ -73,40 +73,8 @@ const char* wrong_gated(const pxr_gated_rollout* r, bool step) {
 
 bool wrong_view(const pxr_steps* t, uint32_t dtype, uint32_t n_steps) { return !t || (n_steps && !t->data) || !aligned(t->data, element(dtype)); }
 
-// Whether two views [n_envs,n_steps,width] of one type have a value in common.  Exact where their strides are the same and one of them is as large as all that the other reaches over, as it is in views that do not
-// overlap themselves; of others only the first steps are compared.
-bool share(const pxr_steps& a, const pxr_steps& b, const pxr_gated_rollout& r) {
-    typedef __int128 wide;  // (strides are any numbers)
-    if (r.n_steps == 0) return false;
-    const wide n = element(r.dtype), values = n * r.width, envs = r.n_envs, steps = r.n_steps;
-    const auto stride = [n](wide count, int64_t of) { return count > 1 ? n * of : (wide)0; };
-    const wide a_env = stride(envs, a.env), a_step = stride(steps, a.step), b_env = stride(envs, b.env), b_step = stride(steps, b.step);
-    const wide apart = (wide)reinterpret_cast<uintptr_t>(b.data) - (wide)reinterpret_cast<uintptr_t>(a.data);
-    const auto size = [](wide v) { return v < 0 ? -v : v; };
-    // where each begins and ends, from a's first value on
-    const auto low = [&](wide e, wide s) { return (e < 0 ? e * (envs - 1) : 0) + (s < 0 ? s * (steps - 1) : 0); };
-    const auto high = [&](wide e, wide s) { return (e > 0 ? e * (envs - 1) : 0) + (s > 0 ? s * (steps - 1) : 0) + values; };
-    if (apart + low(b_env, b_step) >= high(a_env, a_step) || low(a_env, a_step) >= apart + high(b_env, b_step)) return false;
-    if (a_env != b_env || a_step != b_step) return size(apart) < values;
-    // i environments and j steps of one from the other: |apart + i large + j small| < values
-    const bool by_env = size(a_env) >= size(a_step);
-    const wide large = by_env ? a_env : a_step, small = by_env ? a_step : a_env, larges = by_env ? envs : steps, smalls = by_env ? steps : envs;
-    const auto near = [&](wide rest, wide of, wide count, wide step) {  // the multiple of `of` number `step` behind the one that leaves the least of `rest`, among the views' own
-        const wide at = of ? -rest / of + step : 0;
-        return std::max(1 - count, std::min(count - 1, at));
-    };
-    for (int i = -2; i <= 2; ++i)
-        for (int j = -1; j <= 1; ++j) {
-            const wide rest = apart + near(apart, large, larges, i) * large;
-            if (size(rest + near(rest, small, smalls, j) * small) < values) return true;
-        }
-    return false;
-}
-
-bool share_any(const pxr_steps& written, std::initializer_list<const pxr_steps*> read, const pxr_gated_rollout& r) {
-    for (const pxr_steps* t : read)
-        if (share(written, *t, r)) return true;
-    return false;
+pxr::View view(const pxr_steps& t, const pxr_gated_rollout& r) {
+    return {t.data, element(r.dtype), r.width, {{r.n_envs, t.env}, {r.n_steps, t.step}, {1, 0}}};
 }
 
 // Everything but the buffers.
@@ -130,6 +98,23 @@ bool wrong_head_buffers(const pxr_heads* r, std::initializer_list<const pxr_toke
             if (wrong_view(t, r->dtype, tokens)) return true;
     const size_t p = element(r->param_dtype);
     return !aligned(r->d_q_weight, p) || !aligned(r->d_k_weight, p) || !aligned(r->d_positions, r->position_bits / 8u);
+}
+
+// Whether heads that are written, of queries and of keys, lie where others are read or written: each may be in the place of what the same heads are read from (`own`), itself.
+bool heads_overlap(const pxr_heads* r, uint32_t d, const pxr_tokens* q_to, const pxr_tokens* k_to, std::initializer_list<const pxr_tokens*> of_q, std::initializer_list<const pxr_tokens*> of_k) {
+    const auto view = [&](const pxr_tokens* t, uint32_t heads) { return pxr::View{t->data, element(r->dtype), d, {{r->n_envs, t->env}, {r->n_steps, t->step}, {heads, t->head}}}; };
+    const auto overlaps = [&](const pxr_tokens* to, uint32_t heads, std::initializer_list<const pxr_tokens*> own, uint32_t others, std::initializer_list<const pxr_tokens*> other) {
+        if (!heads) return false;
+        const pxr::View v = view(to, heads);
+        for (const pxr_tokens* t : own)
+            if (!pxr::itself(v, view(t, heads)) && pxr::share(v, view(t, heads))) return true;
+        if (others)
+            for (const pxr_tokens* t : other)
+                if (pxr::share(v, view(t, others))) return true;
+        return false;
+    };
+    return overlaps(q_to, r->n_heads, of_q, r->n_key_heads, of_k) || overlaps(k_to, r->n_key_heads, of_k, r->n_heads, of_q) ||
+           (r->n_heads && r->n_key_heads && pxr::share(view(q_to, r->n_heads), view(k_to, r->n_key_heads)));
 }
 
 int finish(int rc, const char* call, const std::string& err) {
@@ -294,7 +279,7 @@ int pxr_gated_recurrence_forward(const pxr_gated_rollout* r, const pxr_steps* ou
         !aligned(d_state_out, 4))
         return refuse(call, "a buffer is null or not aligned to its elements");
     if (overlap(r->d_state, d_state_out, (size_t)r->n_envs * r->width)) return refuse(call, "the states overlap");
-    if (share_any(*out, {&r->x, &r->gate}, *r)) return refuse(call, "out overlaps what is read");
+    if (pxr::share(view(*out, *r), {view(r->x, *r), view(r->gate, *r)})) return refuse(call, "out overlaps what is read");
     const size_t need = pxr::gated_recurrence_workspace(r->n_envs, r->n_steps, r->width, false);
     if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
         return refuse(call, "the workspace is missing, too small or not 16-byte aligned");
@@ -311,7 +296,8 @@ int pxr_gated_recurrence_backward(const pxr_gated_rollout* r, const pxr_steps* d
     if (!aligned(d_dstate_out, 4) || !aligned(d_dstate, 4)) return refuse(call, "a buffer is null or not aligned to its elements");
     const size_t n = (size_t)r->n_envs * r->width;
     if (overlap(r->d_state, d_dstate, n) || overlap(d_dstate_out, d_dstate, n)) return refuse(call, "the states overlap");
-    if (share_any(*dx, {&r->x, &r->gate, dout, dgate}, *r) || share_any(*dgate, {&r->x, &r->gate, dout}, *r)) return refuse(call, "dx or dgate overlaps what is read, or each other");
+    const pxr::View x = view(r->x, *r), gate = view(r->gate, *r), given = view(*dout, *r), to_gate = view(*dgate, *r);
+    if (pxr::share(view(*dx, *r), {x, gate, given, to_gate}) || pxr::share(to_gate, {x, gate, given})) return refuse(call, "dx or dgate overlaps what is read, or each other");
     const size_t need = pxr::gated_recurrence_workspace(r->n_envs, r->n_steps, r->width, true);
     if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
         return refuse(call, "the workspace is missing, too small or not 16-byte aligned");
@@ -324,10 +310,8 @@ int pxr_gated_recurrence_step(const pxr_gated_rollout* r, float* d_state, const 
     if (const char* why = wrong_gated(r, true)) return refuse(call, why);
     if (wrong_view(&r->x, r->dtype, 1) || wrong_view(&r->gate, r->dtype, 1) || wrong_view(out, r->dtype, 1) || !d_state || !aligned(d_state, 4))
         return refuse(call, "a buffer is null or not aligned to its elements");
-    for (const pxr_steps* t : {&r->x, &r->gate}) {
-        const bool itself = out->data == t->data && (r->n_envs == 1 || out->env == t->env);  // (read before it is written, by the same lane)
-        if (!itself && share(*out, *t, *r)) return refuse(call, "out overlaps what is read");
-    }
+    for (const pxr_steps* t : {&r->x, &r->gate})  // (a lane has read its values before it writes them)
+        if (!pxr::itself(view(*out, *r), view(*t, *r)) && pxr::share(view(*out, *r), view(*t, *r))) return refuse(call, "out overlaps what is read");
     std::string err;
     return finish(pxr::launch_gated_recurrence_step(*r, d_state, *out, hip_stream, err), call, err);
 }
@@ -375,6 +359,7 @@ int pxr_head_norm_forward(pxr_head_norm* n, const pxr_heads* r, const pxr_tokens
     const char* call = "pxr_head_norm_forward";
     if (const char* why = wrong_heads(n, r)) return refuse(call, why);
     if (wrong_head_buffers(r, {&r->q, q_out}, {&r->k, k_out})) return refuse(call, "a buffer is null or not aligned to its elements");
+    if (heads_overlap(r, n->c.d, q_out, k_out, {&r->q}, {&r->k})) return refuse(call, "q_out or k_out overlaps heads that it is not itself");
     std::string err;
     return finish(pxr::launch_head_norm_forward(n->c, *r, q_out, k_out, hip_stream, err), call, err);
 }
@@ -394,6 +379,7 @@ int pxr_head_norm_backward(pxr_head_norm* n, const pxr_heads* r, const pxr_token
     const size_t p = element(r->param_dtype);
     if (wrong_head_buffers(r, {&r->q, dq_out, dq}, {&r->k, dk_out, dk}) || !aligned(d_dq_weight, p) || !aligned(d_dk_weight, p))
         return refuse(call, "a buffer is null or not aligned to its elements");
+    if (heads_overlap(r, n->c.d, dq, dk, {&r->q, dq_out}, {&r->k, dk_out})) return refuse(call, "dq or dk overlaps heads that it is not itself");
     const size_t need = d_dq_weight || d_dk_weight ? pxr::head_norm_workspace(n->c, *r) : 0;
     if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
         return refuse(call, "the workspace is missing, too small or not 16-byte aligned");

@@ -440,3 +440,37 @@ def test_is_as_exact_as_elementary_operations(torch, pxr, d, r):
             ours, plain = ((t.double() - ref).square().mean().sqrt() for t in (ours, plain))
             assert float(ours) <= 1.02 * float(plain)
     layer.close()
+
+
+def test_outputs_in_the_place_of_other_heads(torch, pxr):
+    """Of the other kind, of the other output, a step or a head on: refused.  Parts of one buffer side by side are none of these."""
+    rng = np.random.default_rng(10)
+    B, T, d = 3, 20, 16
+    layer = pxr.HeadNorm(d)
+    q, k, qw, kw, at, dq, dk = inputs(torch, rng, B, T, 4, 2, d, "f32")
+    args = dict(positions=at)
+    want = layer.forward(q, k, qw, kw, **args)
+    wide = torch.cat([q, k, torch.zeros_like(q), torch.zeros_like(k)], 2)
+    a, b, c, e = wide.split([4, 2, 4, 2], 2)
+    got = layer.forward(a, b, qw, kw, **args, q_out=c, k_out=e)
+    assert torch.equal(c, want[0]) and torch.equal(e, want[1]) and torch.equal(a, q) and torch.equal(b, k)
+    for outs in (dict(q_out=wide[:, :, 1:5]), dict(q_out=wide[:, :, 5:9]), dict(k_out=wide[:, :, 3:5]), dict(k_out=wide[:, :, 5:7]), dict(q_out=c, k_out=wide[:, :, 9:11]), dict(q_out=wide[:, :, 2:6], k_out=b)):
+        with pytest.raises(pxr.PxrError, match="overlaps"):
+            layer.forward(a, b, qw, kw, **args, **outs)
+    one = k.clone()
+    for outs in (dict(q_out=one), dict(k_out=one)):  # queries that are the keys: neither can take their place
+        with pytest.raises(pxr.PxrError, match="overlaps"):
+            layer.forward(one, one, qw, kw, **args, **outs)
+    longer = torch.zeros((B, T + 1, 4, d), device="cuda")
+    with pytest.raises(pxr.PxrError, match="overlaps"):
+        layer.forward(longer[:, 1:], k, qw, kw, **args, q_out=longer[:, :-1])
+    # gradients, by the C call
+    L, at32 = pxr.lib(), at.int()
+    t = dict(q=q.clone(), k=k.clone(), dq=dq.clone(), dk=dk.clone())
+    v = {name: pxr.Tokens(x.data_ptr(), *x.stride()[:3]) for name, x in t.items()}
+    r = pxr.Heads(0, 0, B, T, 4, 2, v["q"], v["k"], qw.data_ptr(), kw.data_ptr(), at32.data_ptr(), 32, T, 1, 0)
+    moved = lambda name, by: pxr.Tokens(v[name].data + 4 * by, v[name].env, v[name].step, v[name].head)
+    for to_q, to_k in ((v["k"], v["dk"]), (v["dk"], v["k"]), (v["q"], v["q"]), (v["dq"], v["dq"]), (v["q"], v["dq"]), (moved("q", d), v["k"]), (v["q"], moved("dk", 1))):
+        assert L.pxr_head_norm_backward(layer._h, C.byref(r), C.byref(v["dq"]), C.byref(v["dk"]), C.byref(to_q), C.byref(to_k), None, None, None, 0, None) == pxr.ERR_INVALID_ARG
+        assert "overlaps" in L.pxr_last_error().decode()
+    layer.close()
