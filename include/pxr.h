@@ -501,8 +501,8 @@ int pxr_orthogonalise_workspace(const pxr_orthogonalise_desc* d, size_t* bytes);
  * with a NaN or an infinity comes out as NaN, the others are not touched by it.  n_matrices == 0 is a call that does nothing.  Equal inputs give equal bits.
  * d_workspace: 16-byte aligned, used until the call's kernels end.
  * Errors: INVALID_ARG (null, rows or cols == 0, a type that is none, n_steps outside [1,64], a coefficient that is not finite, steps under which a
- * singular value may pass 2^20 or grow by more than 10^12, eps negative or not finite, a row stride smaller than cols, matrices of the result that overlap, n_matrices above 65535, a buffer not
- * aligned to its elements, workspace missing, too small or not 16-byte aligned); UNSUPPORTED (the smaller of rows and cols above 2^15, the larger above 2^28, rows * cols above 2^32);
+ * singular value may pass 2^20 or grow by more than 10^12, eps negative or not finite, a row stride smaller than cols, matrices of the result that overlap, a result that has values
+ * in common with x of the same strides and is not x itself, n_matrices above 65535, a buffer not aligned to its elements, workspace missing, too small or not 16-byte aligned); UNSUPPORTED (the smaller of rows and cols above 2^15, the larger above 2^28, rows * cols above 2^32);
  * DEVICE. */
 int pxr_orthogonalise(const pxr_orthogonalise_desc* d, const void* d_x, void* d_out, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 

@@ -6,6 +6,7 @@
 #include <cmath>
 
 #include "pxr_internal.h"
+#include "views.h"
 
 namespace {
 
@@ -83,6 +84,9 @@ int pxr_orthogonalise(const pxr_orthogonalise_desc* d, const void* d_x, void* d_
     if (d->n_matrices == 0) return PXR_OK;
     const size_t n = d->dtype == PXR_F32 ? 4u : 2u;
     if (!d_x || !d_out || !aligned(d_x, n) || !aligned(d_out, n)) return refuse(call, "a buffer is null or not aligned to its elements");
+    const auto view = [&](const void* data, int64_t matrix, int64_t row) { return pxr::View{data, n, d->cols, {{d->n_matrices, matrix}, {d->rows, row}, {1, 0}}}; };
+    const pxr::View x = view(d_x, d->x_matrix, d->x_row), out = view(d_out, d->out_matrix, d->out_row);
+    if (!pxr::itself(out, x) && pxr::share(out, x)) return refuse(call, "the result overlaps x, and is not x itself");
     const size_t need = pxr::orthogonalise_workspace(*d);
     if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)))
         return refuse(call, "the workspace is missing, too small or not 16-byte aligned");

@@ -85,3 +85,20 @@ def test_long_matrices_of_few_rows_take_many_steps_in_rounds(steps):
     for m, n in ((8, 300), (40, 5000)):
         need = [_call(rows=m, cols=n, x_row=n, out_row=n, coefficients=c) for c in (steps[:1], steps)]
         assert need[0][0] == pxr.OK and need[0][2] == need[1][2]
+
+
+def test_results_that_share_values_with_the_update():
+    """Refused before the workspace is looked at: a row, a value or a matrix on; parts of one buffer side by side, and x itself, are not."""
+    base = 1 << 24
+    for m, n, B, pitch in ((40, 5000, 1, 5000), (600, 64, 3, 200), (5000, 7, 2, 21)):
+        d = dict(rows=m, cols=n, n_matrices=B, x_row=pitch, out_row=pitch, x_matrix=m * pitch, out_matrix=m * pitch)
+        assert _call(**d)[2] > 0
+        why = lambda x, out: (_call(buffers=(4 * x, 4 * out, None), **d)[1], pxr.lib().pxr_last_error().decode())
+        for by in (1, -1, pitch, 1 - n, (m - 1) * pitch, B * m * pitch - 1 if B > 1 else pitch, -pitch + 1):
+            shared = any(abs(by + i * m * pitch + j * pitch) < n for i in range(1 - B, B) for j in range(1 - m, m))
+            code, message = why(base, base + by)
+            assert code == pxr.ERR_INVALID_ARG and ("overlaps x" if shared else "workspace") in message, (m, n, by)
+        for x, out in ((base, base), (base, base + B * m * pitch), (base, base - B * m * pitch), *(((base, base + n), (base + 2 * n, base)) if pitch >= 3 * n else ())):
+            assert "workspace" in why(x, out)[1]
+        d["out_row"], d["out_matrix"] = pitch + 1, m * (pitch + 1)
+        assert "overlaps x" in why(base, base)[1]
