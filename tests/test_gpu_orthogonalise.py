@@ -345,3 +345,27 @@ def test_other_matrices_of_lower_rank_take_many_steps(torch, pxr, m, n, dtype):
             got = pxr.orthogonalise(x, n_steps, step, eps=0.0)
             assert bool(got.isfinite().all())
             assert float(torch.linalg.matrix_norm(got.double().cpu(), 2)) <= most * 1.01 + (W if dtype == "bf16" else 0) * float(got.double().norm())
+
+
+@pytest.mark.parametrize("m,n", [(64, 30000), (20011, 256), (513, 700), (700, 9000), (1500, 4000), (3001, 3000)])
+def test_errors_do_not_grow_with_the_long_side(torch, pxr, m, n):
+    """Sums go in chains of 512 values, 96 matrix instructions of three products, and the chains' results, K / 512 of them, are added up, K the longer side: (8 + sqrt(96) + sqrt(K / 512)) max(e, 2 u), where one chain of everything
+    would have sqrt(3 K / 16).  Without the low parts in the first product 20011 x 256 would be off by 8.5e-5, and 4.5e-5 are allowed; 513 x 700 by 5e-4, of 3.6e-5."""
+    x = normal(torch, n, m, n)
+    ref = plain(torch, x, FIVE, 1e-7, torch.float64)
+    e = float((plain(torch, x, FIVE, 1e-7, torch.float32).double() - ref).norm() / ref.norm())
+    assert float((pxr.orthogonalise(x).double() - ref).norm() / ref.norm()) <= (8 + np.sqrt(96) + np.sqrt(max(m, n) / 512)) * max(e, 2 * U)
+
+
+@pytest.mark.parametrize("m,n", [(90, 100), (64, 30000), (20011, 256), (700, 900), (1500, 2000), (30011, 40)])
+def test_a_step_of_one_direction_keeps_all_bits(torch, pxr, m, n):
+    """Signs, of rank one: every value is the same but for its sign, and what its second part leaves out has one direction too.  One step makes a + b + c of each.  What it is off by, relative: A 16 u (two values of 2 u, 4 u of
+    products left out, as much again for its own two parts and the squares') and its sums' roundings, sqrt(96) + sqrt(K / 512) u; of that |a| + |b| + 2 |c| times, over |a + b + c| = 0.70.  The low parts left out of one
+    product are 2^-12 of each value, over the same: 8e-5 to 2e-3 for most of these sizes in each of the three products, where 2.7e-5 to 3.5e-5 are allowed."""
+    rng = np.random.default_rng(m)
+    signs = np.outer(rng.choice([-1.0, 1.0], m), rng.choice([-1.0, 1.0], n))
+    a, b, c = (float(np.float32(v)) for v in QUINTIC)
+    got = pxr.orthogonalise(torch.from_numpy(signs.astype(np.float32)).cuda(), steps=1, eps=0.0).double().cpu().numpy()
+    want = (a + b + c) / np.sqrt(m * n)
+    off = np.linalg.norm(got * signs - want) / np.sqrt(m * n) / abs(want)
+    assert off <= (abs(a) + abs(b) + 2 * abs(c)) / abs(a + b + c) * (16 + np.sqrt(96) + np.sqrt(max(m, n) / 512)) * U, off
