@@ -497,7 +497,9 @@ typedef struct {
 int pxr_orthogonalise_workspace(const pxr_orthogonalise_desc* d, size_t* bytes);
 
 /* The result in d_out, which may be d_x itself with the same strides.  Products and sums keep 22 bits and more (fp32's, but for a few roundings of 2^-23); values below 2^-38 of the
- * bound that the coefficients set for the singular values (1 before the first step) are zeros, so an update whose norm is far below eps comes out as zeros.  A matrix
+ * bound that the coefficients set for the singular values (1 before the first step) are zeros, so an update whose norm is far below eps comes out as zeros.  Where the smaller of rows and cols is at
+ * most 32 and the larger above 320, products, sums and values between the steps are fp64: no value is lost so, and such an update comes out small.  Directions that a matrix does not have are made of those roundings, 2^-23 or 2^-53, which
+ * grow with its small singular values: after some 13 steps of 3.4, or 30, they are as large as the others.  A matrix
  * with a NaN or an infinity comes out as NaN, the others are not touched by it.  n_matrices == 0 is a call that does nothing.  Equal inputs give equal bits.
  * d_workspace: 16-byte aligned, used until the call's kernels end.
  * Errors: INVALID_ARG (null, rows or cols == 0, a type that is none, n_steps outside [1,64], a coefficient that is not finite, steps under which a

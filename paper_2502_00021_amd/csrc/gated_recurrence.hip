@@ -11,9 +11,10 @@
 // product A of +0 is that of steps among which an episode begins and passes nothing on, whatever the state holds: what is not finite stays on its side of the beginning.
 // One that is merely too small for fp32 is -0, which a state that is not finite does pass.
 //
-// Bound by HBM: 256 environments of 128 steps of 1024 channels of bfloat16 take 44 us, 203 MB at 4.6 TB/s; gradients of 512 x 256 x 1024 316 us, 1.34 GB at 4.2 (79 % of the cycles issue vector
-// instructions); a step of 16384 x 1024 43 us, 235 MB at 5.5.  Few long rollouts are cut into segments: the segments' (A, H, R), what comes into each, outputs.  1 x 50000 x 512 take 57 us, of which
-// the sums are 23, the join 9.
+// Bound by HBM: 256 environments of 128 steps of 1024 channels of bfloat16 take 44 us, 203 MB at 4.6 TB/s; gradients of 512 x 256 x 1024 314 us, 1.34 GB at 4.3 (79 % of the cycles issue vector
+// instructions); a step of 16384 x 1024 43 us, 235 MB at 5.5.  Few long rollouts are cut into segments: the segments' (A, H, R), what comes into each, outputs.  1 x 50000 x 512 take 58 us, of which
+// the sums are 23, the join 9.  Gradients of more than 256 steps are cut so whatever their number, and read everything twice: 256 x 512 x 1024 523 us, 512 x 1024 x 256 503, for 267.
+// (Two figures beside a rule below compare its two sides at the time when it was made; what a call takes now stands here.)
 
 #include <hip/hip_runtime.h>
 

@@ -772,7 +772,8 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Small a) {
 
 // ---- long matrices of at most 32 rows (or columns): X is read twice.  Every X_k is a product P_k X_0 with P_0 = 1, P_{k+1} = B_k P_k, and A_{k+1} = B_k A_k B_k: a sum over the long axis, steps on matrices
 // of 32 x 32, and a product.  All in fp64, on its matrix cores: in fp32 this way loses the small singular values, whose squares A has from the beginning on.  |x|^2 is A's trace.  10 x 28196 in fp32: sums
-// 7 us, steps 17, product 4; what is left is three launches and the chain of the steps.
+// 7 us, steps 17, product 4; what is left is three launches and the chain of the steps.  32 x 200000: 32, 26 and 20, where 26 and 51 MB would take 5 and 10: the sums have a compute unit for each of 128 parts, half of
+// them, because the steps' workgroup reads all of the parts' sums, 17 us of its 26 (five steps are 9).
 //
 // A that is carried along is off by its first roundings, 2^-53, times the square of what the steps multiply a small singular value with.  Where X has no such direction those roundings are all that A has of it; they
 // may be negative, and then the steps' terms add up instead of cancelling (32 x 400 of rank 5 in fp32: off by 2e-3 after 14 steps, NaN after 20).  So the steps come in rounds, each of which forms A from X
